@@ -377,6 +377,145 @@ emb_status emb_workspace_status(const void* ws, size_t ws_bytes, int32_t* status
  * that call's. */
 size_t emb_workspace_error_offset(void);
 
+/* ------------------------------------------------------------------------
+ * Sequences of tokens: the operators a language or behaviour model needs
+ * beside the tables.  A batch's bags are then sequences, in order: every
+ * token is looked up for itself (no pooling), a gated linear recurrence mixes
+ * the rows of a sequence, and what the backward pass needs of the
+ * activations can be kept in 8 bits.
+ *
+ * Matrices of activations are row-major with any row stride: */
+
+typedef enum { EMB_SAVED8 = 2 } emb_saved; /* emb_mat.dtype of a checkpoint in 8 bits */
+
+typedef struct {
+  void* data;    /* device; row r, column c is element r * ld + c */
+  int64_t ld;    /* elements from one row to the next, >= the columns used */
+  int32_t dtype; /* EMB_FP32, EMB_BF16 or EMB_SAVED8 (data: the int8 codes) */
+  const uint8_t* exps; /* EMB_SAVED8: device, the exponents of row r's groups from r * ld_exps */
+  int64_t ld_exps;
+} emb_mat;
+
+/* Lookup of single tokens: out[j][d] = scale * W[key(j)][d] for every position
+ * j of the batch, computed in fp32 and rounded once to out's type (fp32 or
+ * bf16).  Tokens whose key is pad_row (a global row; negative: none) give
+ * zeros, as do ids outside their table.  out: N rows of dim columns, aligned
+ * to its element type. */
+typedef struct {
+  float scale;
+  int64_t pad_row;
+} emb_token;
+
+emb_status emb_token_fwd(const emb_tables* tables, const emb_batch* batch, const emb_token* token,
+                         const emb_mat* out, void* stream);
+
+/* Where emb_token_grad leaves gradient rows:
+ *   EMB_ROWS       grad[u] = g_u for u < U (as emb_grad_reduce)
+ *   EMB_TABLE      grad[r] for every row r of the stacked tables: g_u at
+ *                  r = unique_keys[u], zeros elsewhere
+ *   EMB_TABLE_ADD  grad[unique_keys[u]] += g_u, other rows untouched */
+typedef enum { EMB_ROWS = 0, EMB_TABLE = 1, EMB_TABLE_ADD = 2 } emb_grad_layout;
+
+/* Gradient of emb_token_fwd by sorted tokens:
+ *   g_u[d] = scale * sum over sorted positions k in segment u of grad_out[sort_perm[k]][d]
+ * summed in fp32 in a fixed order (segments of more than 64 tokens in pieces
+ * of 64, the pieces in double); the padding row's is zero.  grad_out: N rows
+ * of dim columns, fp32 or bf16.  grad: device fp32, laid out as `layout`
+ * says, or NULL with fuse.  fuse: NULL, or the optimizer step applied to the
+ * looked-up rows but the padding row, as in emb_grad_reduce (grad must then
+ * be NULL).  The dedup's outputs and ws are those emb_unique_ids left for this
+ * batch, unmodified.  EMB_EUNSUPPORTED for rows of more than 8192 values.
+ * After a dedup that failed on the device no table row is written, and
+ * gradient rows are written as zeros (EMB_ROWS, EMB_TABLE) or left. */
+emb_status emb_token_grad(const emb_tables* tables, const emb_batch* batch, const emb_token* token,
+                          const emb_mat* grad_out, const int32_t* sort_perm, const int32_t* seg_offsets,
+                          const uint32_t* unique_keys, const int32_t* num_unique, float* grad, int32_t layout,
+                          const emb_update* fuse, void* ws, size_t ws_bytes, void* stream);
+
+/* Gated linear recurrence over ragged sequences, one state per column:
+ *   a_t = sigmoid(f_t + bias)                      (forget gate)
+ *   h_t = a_t * h_{t-1} + (1 - a_t) * x_t          (1 - a_t = sigmoid(-(f_t + bias)))
+ *   y_t = sigmoid(o_t) * h_t                       (output gate; y_t = h_t without one)
+ * Sequence m holds positions offsets[m] .. offsets[m+1]-1 (device int32
+ * [num_seqs + 1], offsets[0] = 0, nondecreasing, offsets[num_seqs] =
+ * num_tokens; empty sequences are allowed) and starts from h0[m], or zero.
+ * x, f, o: num_tokens rows of dim columns of one type (fp32 or bf16; in the
+ * backward EMB_SAVED8 too); o.data NULL: no output gate.  Arithmetic and
+ * states are fp32. */
+typedef struct {
+  int64_t num_tokens; /* N, host, 0 <= N < 2^31 - 64 */
+  int32_t num_seqs;   /* M >= 0 */
+  int32_t dim;        /* D >= 1 */
+  const int32_t* offsets;
+  emb_mat x, f, o;
+  const float* bias;  /* device [D] or NULL */
+  const float* h0;    /* device [M][D] or NULL */
+} emb_scan;
+
+/* Positions between kept states: states[c] is h before position c * 64. */
+#define EMB_SCAN_SPAN 64
+
+/* Bytes of workspace of emb_scan_fwd and emb_scan_bwd for up to num_tokens
+ * tokens of dim columns (0 for invalid sizes); it needs no initialisation and
+ * carries nothing between calls. */
+size_t emb_scan_workspace_size(int64_t num_tokens, int32_t dim);
+
+/* y: N rows of dim columns, of x's type.  h_last: device fp32 [M][D], the
+ * state after each sequence (h0 or zero for an empty one), or NULL.  states:
+ * device fp32 [ceil(N / 64)][D] for emb_scan_bwd, or NULL. */
+emb_status emb_scan_fwd(const emb_scan* scan, const emb_mat* y, float* h_last, float* states, void* ws,
+                        size_t ws_bytes, void* stream);
+
+/* Backward of emb_scan_fwd from its states (h is recomputed from states[c] at
+ * every 64th position, so with x, f, o restored from checkpoints it stays
+ * within 64 steps of the forward's):
+ *   dh_t = sigmoid(o_t) * dy_t + a_{t+1} * dh_{t+1}   (+ dh_last[m] at the end)
+ *   dx_t = (1 - a_t) * dh_t
+ *   df_t = dh_t * (h_{t-1} - x_t) * a_t * (1 - a_t)
+ *   do_t = dy_t * h_t * sigmoid(o_t) * (1 - sigmoid(o_t))
+ *   dbias = sum over all positions of df_t (before it is rounded)
+ *   dh0[m] = a * dh at the sequence's first position (dh_last[m] if empty)
+ * dy, dx, df, dO: N rows of dim columns, all of one type: x's, or fp32 or
+ * bf16 where x is EMB_SAVED8.  dO.data is ignored without an output gate.
+ * dh_last (fp32 [M][D]), dbias (fp32 [D]), dh0 (fp32 [M][D]): each may be
+ * NULL.  Outputs may not overlap inputs. */
+emb_status emb_scan_bwd(const emb_scan* scan, const float* states, const emb_mat* dy, const float* dh_last,
+                        const emb_mat* dx, const emb_mat* df, const emb_mat* dO, float* dbias, float* dh0,
+                        void* ws, size_t ws_bytes, void* stream);
+
+/* One token of each of num_tokens running sequences (serving): row i of x, f,
+ * o and y is the next token of the sequence whose state is state[slots[i]]
+ * (device fp32, rows of dim columns, updated in place; slots: device int32, or
+ * NULL for slot i).  A token whose slot lies outside 0..num_slots-1 gets a y of
+ * zeros and touches no state.  Slots must be distinct. */
+emb_status emb_scan_step(int64_t num_tokens, int32_t dim, const emb_mat* x, const emb_mat* f, const emb_mat* o,
+                         const float* bias, float* state, int64_t num_slots, const int32_t* slots, const emb_mat* y,
+                         void* stream);
+
+/* Activations kept in 8 bits.  A row's columns in groups of 32 share an
+ * exponent: e is the smallest with max |v| <= 127 * 2^e, within -120 .. 121
+ * (so magnitudes past 127 * 2^121 saturate); code = v * 2^-e rounded to the
+ * nearest integer (ties to even) within -127 .. 127, and exps holds e + 127.
+ * A group with an infinity or NaN gets 255 and is restored as NaN.  A restored
+ * value code * 2^e has 7 significant bits, so bf16 holds it exactly.
+ * dst / src (EMB_SAVED8): ld >= dim rounded up to 32, a multiple of 32, data
+ * 32-byte aligned; the codes of the last group's unused columns are written as
+ * zeros.  The other matrix: fp32 or bf16. */
+#define EMB_SAVED_GROUP 32
+emb_status emb_save(int64_t rows, int32_t dim, const emb_mat* src, const emb_mat* dst, void* stream);
+emb_status emb_restore(int64_t rows, int32_t dim, const emb_mat* src, const emb_mat* dst, void* stream);
+
+/* Gradient of a projection's weights from its input's checkpoint:
+ *   dw[k][c] = sum over rows r of restored x[r][k] * dy[r][c]  (+ dw[k][c] with add)
+ * x: EMB_SAVED8, `rows` rows of dim columns; dy: fp32 or bf16, cols columns;
+ * dw: device fp32 [dim][cols].  Products of bf16 values (an fp32 dy is split
+ * into three that hold all of it) are summed in fp32, pieces of the rows apart
+ * where there are few tiles of dw; ws: device, 256-byte aligned, ws_bytes >=
+ * emb_weight_grad_workspace_size (which may be 0). */
+size_t emb_weight_grad_workspace_size(int64_t rows, int32_t dim, int32_t cols);
+emb_status emb_weight_grad(int64_t rows, int32_t dim, int32_t cols, const emb_mat* x, const emb_mat* dy, float* dw,
+                           int32_t add, void* ws, size_t ws_bytes, void* stream);
+
 const char* emb_status_string(int32_t status);
 
 #ifdef __cplusplus

@@ -30,7 +30,9 @@ EXPORTED = ("emb_pool_fwd", "emb_workspace_size", "emb_workspace_init", "emb_uni
             "emb_grad_reduce",
             "emb_sparse_update", "emb_validate_batch", "emb_workspace_error_offset", "emb_workspace_status",
             "emb_status_string", "emb_route_workspace_size", "emb_route_ids", "emb_route_ids_noalloc",
-            "emb_pipeline_steps", "emb_unique_ids_batched")
+            "emb_pipeline_steps", "emb_unique_ids_batched",
+            "emb_token_fwd", "emb_token_grad", "emb_scan_workspace_size", "emb_scan_fwd", "emb_scan_bwd",
+            "emb_scan_step", "emb_save", "emb_restore", "emb_weight_grad_workspace_size", "emb_weight_grad")
 
 
 class EmbError(RuntimeError):
@@ -138,6 +140,8 @@ def lib():
         L.emb_workspace_status.argtypes = [vp, sz, vp, vp]
         L.emb_status_string.restype = ctypes.c_char_p
         L.emb_status_string.argtypes = [i32]
+        from .sequence import _declare
+        _declare(L)
         _lib = L
     return _lib
 
@@ -731,3 +735,7 @@ class Pipeline:
         for st in self.status(stream):
             if st[0]:
                 raise StepFailed(*st)
+
+
+from .sequence import (Checkpoint, Mat, Recurrence, Scan, TokenLayer, scan_step, scan_workspace_size,  # noqa: E402
+                       token_fwd, token_grad)

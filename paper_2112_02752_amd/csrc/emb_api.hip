@@ -4,6 +4,7 @@
 
 #include "emb_common.h"
 #include "kernels.h"
+#include "seq_common.h"
 
 using namespace emb;
 
@@ -131,6 +132,72 @@ emb_status route_prepare(const emb_tables* tables, const emb_batch* batch, int32
   return EMB_OK;
 }
 
+// ---- sequences of tokens
+
+constexpr int64_t kMaxTokens = ((int64_t)1 << 31) - 64 - 1;
+
+emb_status check_token(const emb_token* t, int64_t R) {
+  return t == nullptr || t->pad_row >= R ? EMB_EINVAL : EMB_OK;
+}
+
+// a matrix with `cols` columns in use; saved: an 8-bit checkpoint, else fp32 or bf16
+emb_status check_mat(const emb_mat* m, int32_t cols, bool saved) {
+  if (m == nullptr || m->data == nullptr) return EMB_EINVAL;
+  if (saved) {
+    if (m->dtype != EMB_SAVED8 || m->exps == nullptr) return EMB_EINVAL;
+    const int64_t groups = (cols + (int64_t)EMB_SAVED_GROUP - 1) / EMB_SAVED_GROUP;
+    if (m->ld < groups * EMB_SAVED_GROUP || m->ld_exps < groups) return EMB_EINVAL;
+    if (m->ld % EMB_SAVED_GROUP != 0 || ((uintptr_t)m->data & 31u) != 0) return EMB_EINVAL;
+    return EMB_OK;
+  }
+  const int size = dtype_bytes(m->dtype);
+  if (size == 0 || m->ld < cols) return EMB_EINVAL;
+  return ((uintptr_t)m->data & (uintptr_t)(size - 1)) != 0 ? EMB_EINVAL : EMB_OK;
+}
+
+Rows rows_of(const emb_mat& m) {
+  return Rows{static_cast<char*>(m.data), m.ld * (m.dtype == EMB_SAVED8 ? 1 : dtype_bytes(m.dtype)), m.exps, m.ld_exps};
+}
+
+// whether a lane may take two 16-bit columns of a row (or two codes) as one word
+bool pairs(const emb_mat& m) {
+  return m.dtype == EMB_SAVED8 || (m.dtype == EMB_BF16 && m.ld % 2 == 0 && ((uintptr_t)m.data & 3u) == 0);
+}
+
+emb_status check_scan(const emb_scan* s, const void* ws, size_t ws_bytes, ScanLaunch* p) {
+  if (s == nullptr || s->num_tokens < 0 || s->num_seqs < 0 || s->dim < 1) return EMB_EINVAL;
+  if (s->num_tokens > kMaxTokens) return EMB_EUNSUPPORTED;
+  const int64_t spans = (s->num_tokens + kSpan - 1) / kSpan, slices = ((int64_t)s->dim + 63) / 64;
+  // (block numbers are 32 bits)
+  if (spans * slices + (s->num_seqs + 63) / 64 >= (int64_t)1 << 31) return EMB_EUNSUPPORTED;
+  if (s->num_tokens > 0 && s->num_seqs == 0) return EMB_EINVAL;
+  if (s->offsets == nullptr) return EMB_EINVAL;
+  p->N = s->num_tokens;
+  p->M = s->num_seqs;
+  p->D = s->dim;
+  p->offsets = s->offsets;
+  p->bias = s->bias;
+  p->h0 = s->h0;
+  if (s->num_tokens == 0) return EMB_OK;
+  const bool saved = s->x.dtype == EMB_SAVED8;
+  p->dtype = s->x.dtype;
+  p->gated = s->o.data != nullptr;
+  p->vector = s->dim % 2 == 0 ? 2 : 1;
+  const emb_mat* all[3] = {&s->x, &s->f, &s->o};
+  for (int i = 0; i < (p->gated ? 3 : 2); ++i) {
+    const emb_status st = check_mat(all[i], s->dim, saved);
+    if (st != EMB_OK) return st;
+    if (all[i]->dtype != s->x.dtype) return EMB_EINVAL;
+    if (!pairs(*all[i])) p->vector = 1;
+  }
+  p->x = rows_of(s->x);
+  p->f = rows_of(s->f);
+  if (p->gated) p->o = rows_of(s->o);
+  if (ws == nullptr) return EMB_EINVAL;
+  if (((uintptr_t)ws & 255u) != 0 || ws_bytes < scan_ws_bytes(s->num_tokens, s->dim)) return EMB_EWORKSPACE;
+  p->ws = static_cast<char*>(const_cast<void*>(ws));
+  return EMB_OK;
+}
 
 }  // namespace
 
@@ -498,6 +565,235 @@ emb_status emb_validate_batch(const emb_tables* tables, const emb_batch* batch, 
   p.N = batch->num_indices;
   p.flag = flag;
   return hip_status(launch_validate(p, (hipStream_t)stream));
+}
+
+emb_status emb_token_fwd(const emb_tables* tables, const emb_batch* batch, const emb_token* token,
+                         const emb_mat* out, void* stream) {
+  TokenFwdLaunch p{};
+  int64_t R = 0;
+  emb_status st = check_tables(tables, &p.ro, &R);
+  if (st != EMB_OK) return st;
+  int32_t M = 0;
+  if ((st = check_batch(batch, tables->num_tables, &M)) != EMB_OK) return st;
+  if ((st = check_token(token, R)) != EMB_OK) return st;
+  if (batch->num_indices == 0) return EMB_OK;
+  if ((st = check_mat(out, tables->dim, false)) != EMB_OK) return st;
+  p.W = tables->weights;
+  p.idx = batch->indices;
+  p.idx64 = batch->index_bytes == 8;
+  p.offsets = batch->offsets;
+  p.T = tables->num_tables;
+  p.B = batch->bags_per_table;
+  p.D = tables->dim;
+  p.dtype = tables->dtype;
+  p.out_dtype = out->dtype;
+  p.rows = (uint32_t)R;
+  p.N = batch->num_indices;
+  p.ld = out->ld;
+  p.pad = token->pad_row < 0 ? kNoRow : (uint32_t)token->pad_row;
+  p.scale = token->scale;
+  p.out = out->data;
+  return hip_status(launch_token_fwd(p, (hipStream_t)stream));
+}
+
+emb_status emb_token_grad(const emb_tables* tables, const emb_batch* batch, const emb_token* token,
+                          const emb_mat* grad_out, const int32_t* sort_perm, const int32_t* seg_offsets,
+                          const uint32_t* unique_keys, const int32_t* num_unique, float* grad, int32_t layout,
+                          const emb_update* fuse, void* ws, size_t ws_bytes, void* stream) {
+  TableOffsets ro;
+  int64_t R = 0;
+  emb_status st = check_tables(tables, &ro, &R);
+  if (st != EMB_OK) return st;
+  int32_t M = 0;
+  if ((st = check_batch(batch, tables->num_tables, &M)) != EMB_OK) return st;
+  if ((st = check_token(token, R)) != EMB_OK) return st;
+  if ((fuse == nullptr) == (grad == nullptr)) return EMB_EINVAL;
+  if (fuse != nullptr && (st = check_update(fuse)) != EMB_OK) return st;
+  if (layout != EMB_ROWS && layout != EMB_TABLE && layout != EMB_TABLE_ADD) return EMB_EINVAL;
+  if (((uintptr_t)grad & 15u) != 0) return EMB_EINVAL;
+  // (rows of more than 4096 values are read eight columns a lane)
+  if (tables->dim > kTokenMaxDim || (tables->dim > kTokenMaxDim / 2 && tables->dim % 8 != 0)) return EMB_EUNSUPPORTED;
+  TokenGradLaunch p{};
+  if ((st = check_ws(ws, ws_bytes, batch->num_indices, M, tables->dim, &p.lay)) != EMB_OK) return st;
+  if (batch->num_indices > 0) {
+    if ((st = check_mat(grad_out, tables->dim, false)) != EMB_OK) return st;
+    if (sort_perm == nullptr || seg_offsets == nullptr || unique_keys == nullptr || num_unique == nullptr)
+      return EMB_EINVAL;
+    p.dy = grad_out->data;
+    p.dy_dtype = grad_out->dtype;
+    p.ld = grad_out->ld;
+  } else if (layout == EMB_TABLE && grad != nullptr && num_unique == nullptr) {
+    return EMB_EINVAL;
+  }
+  p.perm = sort_perm;
+  p.seg = seg_offsets;
+  p.ukeys = unique_keys;
+  p.num_unique = num_unique;
+  p.N = (int32_t)batch->num_indices;
+  p.D = tables->dim;
+  p.rows = (uint32_t)R;
+  p.pad = token->pad_row < 0 ? kNoRow : (uint32_t)token->pad_row;
+  p.scale = token->scale;
+  p.grad = grad;
+  p.layout = layout;
+  p.ws = ws;
+  p.fuse = fuse != nullptr;
+  p.dtype = tables->dtype;
+  p.W = tables->weights;
+  if (fuse != nullptr) {
+    p.opt = fuse->opt;
+    p.lr = fuse->lr;
+    p.eps = fuse->eps;
+    p.rounding = fuse->rounding;
+    p.seed = fuse->seed;
+    p.state = fuse->state;
+    if (fuse->opt == EMB_OPT_ADAGRAD_ELEMENTWISE && ((uintptr_t)fuse->state & 15u) != 0) return EMB_EINVAL;
+  }
+  return hip_status(launch_token_grad(p, (hipStream_t)stream));
+}
+
+size_t emb_scan_workspace_size(int64_t num_tokens, int32_t dim) {
+  if (num_tokens < 0 || num_tokens > kMaxTokens || dim < 1) return 0;
+  return scan_ws_bytes(num_tokens, dim);
+}
+
+emb_status emb_scan_fwd(const emb_scan* scan, const emb_mat* y, float* h_last, float* states, void* ws,
+                        size_t ws_bytes, void* stream) {
+  ScanLaunch p{};
+  emb_status st = check_scan(scan, ws, ws_bytes, &p);
+  if (st != EMB_OK) return st;
+  if (scan->num_tokens > 0) {
+    if (p.dtype == EMB_SAVED8) return EMB_EUNSUPPORTED;
+    if ((st = check_mat(y, scan->dim, false)) != EMB_OK) return st;
+    if (y->dtype != p.dtype) return EMB_EINVAL;
+    p.y = rows_of(*y);
+    p.vector = p.vector == 2 && pairs(*y) ? 2 : 1;
+  }
+  p.h_last = h_last;
+  p.states = states;
+  return hip_status(launch_scan_fwd(p, (hipStream_t)stream));
+}
+
+emb_status emb_scan_bwd(const emb_scan* scan, const float* states, const emb_mat* dy, const float* dh_last,
+                        const emb_mat* dx, const emb_mat* df, const emb_mat* dO, float* dbias, float* dh0,
+                        void* ws, size_t ws_bytes, void* stream) {
+  ScanLaunch p{};
+  emb_status st = check_scan(scan, ws, ws_bytes, &p);
+  if (st != EMB_OK) return st;
+  if (scan->num_tokens > 0) {
+    if (states == nullptr) return EMB_EINVAL;
+    const emb_mat* all[4] = {dy, dx, df, dO};
+    for (int i = 0; i < (p.gated ? 4 : 3); ++i) {
+      if ((st = check_mat(all[i], scan->dim, false)) != EMB_OK) return st;
+      if (all[i]->dtype != dy->dtype) return EMB_EINVAL;
+      if (!pairs(*all[i])) p.vector = 1;
+    }
+    if (p.dtype != EMB_SAVED8 && dy->dtype != p.dtype) return EMB_EINVAL;
+    p.grad_dtype = dy->dtype;
+    p.dy = rows_of(*dy);
+    p.dx = rows_of(*dx);
+    p.df = rows_of(*df);
+    if (p.gated) p.dO = rows_of(*dO);
+  }
+  p.states = const_cast<float*>(states);
+  p.dh_last = dh_last;
+  p.dbias = dbias;
+  p.dh0 = dh0;
+  return hip_status(launch_scan_bwd(p, (hipStream_t)stream));
+}
+
+emb_status emb_scan_step(int64_t num_tokens, int32_t dim, const emb_mat* x, const emb_mat* f, const emb_mat* o,
+                         const float* bias, float* state, int64_t num_slots, const int32_t* slots, const emb_mat* y,
+                         void* stream) {
+  if (num_tokens < 0 || dim < 1 || num_slots < 0) return EMB_EINVAL;
+  if (num_tokens > kMaxTokens || num_tokens * (int64_t)dim >= (int64_t)1 << 38) return EMB_EUNSUPPORTED;
+  if (num_tokens == 0) return EMB_OK;
+  if (num_slots > 0 && state == nullptr) return EMB_EINVAL;
+  StepLaunch p{};
+  p.gated = o != nullptr && o->data != nullptr;
+  const emb_mat* all[4] = {y, x, f, o};
+  p.vector = 2;
+  for (int i = 0; i < (p.gated ? 4 : 3); ++i) {
+    const emb_status st = check_mat(all[i], dim, false);
+    if (st != EMB_OK) return st;
+    if (all[i]->dtype != y->dtype) return EMB_EINVAL;
+    if (!pairs(*all[i])) p.vector = 1;
+  }
+  if (dim % 2 != 0) p.vector = 1;
+  p.N = num_tokens;
+  p.D = dim;
+  p.dtype = y->dtype;
+  p.x = rows_of(*x);
+  p.f = rows_of(*f);
+  if (p.gated) p.o = rows_of(*o);
+  p.y = rows_of(*y);
+  p.bias = bias;
+  p.state = state;
+  p.num_slots = num_slots;
+  p.slots = slots;
+  return hip_status(launch_scan_step(p, (hipStream_t)stream));
+}
+
+static emb_status save_prepare(int64_t rows, int32_t dim, const emb_mat* full, const emb_mat* saved, SaveLaunch* p) {
+  if (rows < 0 || dim < 1) return EMB_EINVAL;
+  if (rows > kMaxTokens || rows * (int64_t)dim >= (int64_t)1 << 40) return EMB_EUNSUPPORTED;
+  p->N = rows;
+  p->D = dim;
+  if (rows == 0) return EMB_OK;
+  emb_status st = check_mat(full, dim, false);
+  if (st != EMB_OK) return st;
+  if ((st = check_mat(saved, dim, true)) != EMB_OK) return st;
+  p->dtype = full->dtype;
+  p->full = rows_of(*full);
+  p->saved = rows_of(*saved);
+  p->aligned = (((uintptr_t)p->full.p | (uintptr_t)p->full.ld) & 15u) == 0;
+  return EMB_OK;
+}
+
+emb_status emb_save(int64_t rows, int32_t dim, const emb_mat* src, const emb_mat* dst, void* stream) {
+  SaveLaunch p{};
+  const emb_status st = save_prepare(rows, dim, src, dst, &p);
+  if (st != EMB_OK || rows == 0) return st;
+  return hip_status(launch_save(p, (hipStream_t)stream));
+}
+
+emb_status emb_restore(int64_t rows, int32_t dim, const emb_mat* src, const emb_mat* dst, void* stream) {
+  SaveLaunch p{};
+  const emb_status st = save_prepare(rows, dim, dst, src, &p);
+  if (st != EMB_OK || rows == 0) return st;
+  return hip_status(launch_restore(p, (hipStream_t)stream));
+}
+
+size_t emb_weight_grad_workspace_size(int64_t rows, int32_t dim, int32_t cols) {
+  if (rows < 0 || rows > kMaxTokens || dim < 1 || cols < 1) return 0;
+  return weight_grad_ws_bytes(rows, dim, cols);
+}
+
+emb_status emb_weight_grad(int64_t rows, int32_t dim, int32_t cols, const emb_mat* x, const emb_mat* dy, float* dw,
+                           int32_t add, void* ws, size_t ws_bytes, void* stream) {
+  if (rows < 0 || dim < 1 || cols < 1 || dw == nullptr) return EMB_EINVAL;
+  // (block numbers of the tiles and parts are 32 bits)
+  if (rows > kMaxTokens || (int64_t)dim * cols >= (int64_t)1 << 40) return EMB_EUNSUPPORTED;
+  WeightGradLaunch p{};
+  if (rows > 0) {
+    emb_status st = check_mat(x, dim, true);
+    if (st != EMB_OK) return st;
+    if ((st = check_mat(dy, cols, false)) != EMB_OK) return st;
+    p.dtype = dy->dtype;
+    p.x = rows_of(*x);
+    p.dy = rows_of(*dy);
+    p.aligned = (((uintptr_t)p.dy.p | (uintptr_t)p.dy.ld) & (dy->dtype == EMB_BF16 ? 7u : 15u)) == 0;
+  }
+  const size_t need = weight_grad_ws_bytes(rows, dim, cols);
+  if (need > 0 && ws == nullptr) return EMB_EINVAL;
+  if (ws_bytes < need || ((uintptr_t)ws & 255u) != 0) return EMB_EWORKSPACE;
+  p.N = rows;
+  p.K = dim;
+  p.F = cols;
+  p.add = add != 0;
+  p.dw = dw;
+  p.ws = static_cast<float*>(ws);
+  return hip_status(launch_weight_grad(p, (hipStream_t)stream));
 }
 
 }  // extern "C"

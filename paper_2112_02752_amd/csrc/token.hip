@@ -1,0 +1,559 @@
+// Lookup of single tokens and its gradient by sorted tokens (gfx950).
+//
+//   out[j] = scale * W[key(j)]                       (padding tokens: zeros)
+//   g_u    = scale * sum over sorted positions k of segment u of dy[perm[k]]
+//
+// Forward: a row is read by G lanes (a power of two, at most a block) as
+// vectors of V values; a lane has kAhead rows in flight.
+//
+// Gradient: a wavefront walks the 64 sorted positions of one chunk for 64 * EL
+// columns, in batches whose rows (and the table rows of the segments that end
+// in the batch) are in flight together.  What is walked is the same for the
+// whole wavefront, so rows and segment ends live in scalar registers.  A
+// segment of at most 64 positions belongs to the chunk it starts in; a longer
+// one leaves a partial row per chunk, which k_token_combine adds up.  Every
+// sum runs in a fixed order: results are the same from run to run.
+#include "reduce_common.h"
+#include "seq_common.h"
+
+namespace emb {
+
+namespace {
+
+// ---------------------------------------------------------------- forward
+
+constexpr int kFwdThreads = 256;
+
+struct TokFwd {
+  const char* W;
+  const void* idx;
+  const int32_t* offsets;
+  char* out;
+  int64_t N, row_bytes, out_bytes;  // bytes from one row to the next
+  int32_t idx64, T, B, vectors, log_g, aligned;
+  uint32_t rows, pad;
+  float scale;
+};
+// (a kernel of one table does not get the table offsets)
+template <bool MANY>
+struct Stacked {};
+template <>
+struct Stacked<true> {
+  TableOffsets ro;
+};
+
+template <typename TW, typename TO, int V, int AHEAD, bool MANY>
+__global__ __launch_bounds__(kFwdThreads) void k_token_fwd(TokFwd a, Stacked<MANY> st) {
+  const int lanes = 1 << a.log_g, per = kFwdThreads >> a.log_g;
+  const int c = (int)blockIdx.y * lanes + (int)(threadIdx.x & (lanes - 1));
+  const int64_t j0 = (int64_t)blockIdx.x * (per * AHEAD) + (threadIdx.x >> a.log_g);
+  if (c >= a.vectors) return;
+  uint32_t key[AHEAD];
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u) {
+    const int64_t j = j0 + (int64_t)u * per;
+    key[u] = kNoRow;
+    if (j < a.N) {
+      const int32_t id = load_id(a.idx, a.idx64, j);
+      if constexpr (MANY) {
+        // the table whose sequences hold position j: the last with a first position at or before it
+        int t = 0, n = a.T;
+        while (n > 1) {
+          const int half = n / 2;
+          if ((int64_t)a.offsets[(int64_t)(t + half) * a.B] <= j) t += half, n -= half;
+          else n = half;
+        }
+        const uint32_t r0 = st.ro.off[t];
+        key[u] = (uint32_t)id < st.ro.off[t + 1] - r0 ? r0 + (uint32_t)id : kNoRow;
+      } else {
+        key[u] = (uint32_t)id;
+      }
+      if (key[u] == a.pad) key[u] = kNoRow;
+    }
+  }
+  Vec<TW, V> v[AHEAD];
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u) {
+    if (key[u] < a.rows) v[u].load(a.W + (int64_t)key[u] * a.row_bytes + (int64_t)c * Vec<TW, V>::kBytes);
+    else v[u].zero();
+  }
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u) {
+    const int64_t j = j0 + (int64_t)u * per;
+    if (j >= a.N) break;
+    float x[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = key[u] < a.rows ? a.scale * v[u].get(i) : 0.f;
+    char* q = a.out + j * a.out_bytes + (int64_t)c * Vec<TO, V>::kBytes;
+    if (a.aligned) Vec<TO, V>::store(q, x);
+    else Vec<TO, V>::store_each(q, x);
+  }
+}
+
+// ---------------------------------------------------------------- gradient
+
+enum Kind { kStore = 0, kSgd = 1, kAdaRow = 2, kAdaElem = 3 };
+constexpr int kMostParts = 16;  // wavefronts of a block that share a chunk's columns (row-wise Adagrad)
+
+struct TokGrad {
+  const char* dy;
+  int64_t ld;  // bytes from one row to the next
+  const int32_t* perm;
+  const int32_t* seg;
+  const uint32_t* ukeys;
+  const int32_t* num_unique;
+  const int32_t* chunk_seg;
+  const void* hdr;
+  float* partials;  // [nchunks][2][D]: rows of long segments, of the one that holds a chunk's first position, of another
+  float* grad;
+  int32_t N, D, nchunks, parts, layout, aligned;
+  uint32_t rows, pad;
+  float scale;
+  Upd up;
+};
+
+__device__ __forceinline__ bool failed(const TokGrad& a) {
+  const WsHeader* h = static_cast<const WsHeader*>(a.hdr);
+  return (call_errors(h, h->gen) & kDedupErrors) != 0u;
+}
+
+// a table row's columns c .. c + EL - 1
+template <typename TW, int EL>
+__device__ __forceinline__ void store_row(const Upd& up, uint32_t key, int c, const float (&o)[EL]) {
+  char* q = static_cast<char*>(up.W) + ((int64_t)key * up.D + c) * (int64_t)sizeof(TW);
+  if constexpr (sizeof(TW) == 2) {
+    if (up.rounding) {
+      uint32_t b[EL];
+#pragma unroll
+      for (int e = 0; e < EL; ++e)
+        b[e] = bf16_stochastic(o[e], up.seed, (uint64_t)key * (uint64_t)up.D + (uint64_t)(c + e));
+      if constexpr (EL == 1) {
+        *reinterpret_cast<uint16_t*>(q) = (uint16_t)b[0];
+      } else {
+#pragma unroll
+        for (int e = 0; e < EL / 2; ++e) reinterpret_cast<uint32_t*>(q)[e] = b[2 * e] | (b[2 * e + 1] << 16);
+      }
+      return;
+    }
+  }
+  Vec<TW, EL>::store(q, o);
+}
+
+// Optimizer on columns c .. of row `key` with gradient g; w, h: the table row's
+// columns and, element-wise Adagrad, its accumulators; step: lr, or row-wise
+// Adagrad's lr / (sqrt(h) + eps).
+template <typename TW, int EL, int KIND>
+__device__ __forceinline__ void apply(const Upd& up, uint32_t key, int c, const float (&g)[EL], const Vec<TW, EL>& w,
+                                      const Vec<float, EL>& h, float step) {
+#pragma clang fp contract(off)
+  float o[EL];
+  if constexpr (KIND == kAdaElem) {
+    float hn[EL];
+#pragma unroll
+    for (int e = 0; e < EL; ++e) {
+      hn[e] = __builtin_fmaf(g[e], g[e], h.get(e));
+      o[e] = w.get(e) - up.lr * g[e] / (sqrtf(hn[e]) + up.eps);
+    }
+    Vec<float, EL>::store(up.state + (int64_t)key * up.D + c, hn);
+  } else {
+#pragma unroll
+    for (int e = 0; e < EL; ++e) o[e] = __builtin_fmaf(-step, g[e], w.get(e));
+  }
+  store_row<TW, EL>(up, key, c, o);
+}
+
+__device__ __forceinline__ float wave_total(float x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, kWave);
+  return x;
+}
+
+// EL columns a lane, B positions a batch.  ROWWISE blocks are the `parts`
+// wavefronts of one chunk; others four wavefronts of any.
+template <typename TG, typename TW, int EL, int B, int KIND>
+__global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) void k_token_reduce(TokGrad a) {
+  const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
+  int c, part;
+  if constexpr (KIND == kAdaRow) {
+    c = blockIdx.x, part = wave;
+  } else {
+    const int at = blockIdx.x * 4 + wave;
+    c = at / a.parts, part = at % a.parts;
+  }
+  __shared__ float s_sq[2][kMostParts][B];
+  if (c >= a.nchunks) return;
+  const int col = (part * kWave + lane) * EL;
+  const bool in = col < a.D;
+  const int cs = in ? col : 0;
+  const int p0 = c * kChunk, p1 = min(a.N, p0 + kChunk);
+  if (failed(a)) {
+    if (KIND == kStore && a.layout == EMB_ROWS && in) {
+      float z[EL] = {};
+      for (int p = p0; p < p1; ++p) Vec<float, EL>::store(a.grad + (int64_t)p * a.D + col, z);
+    }
+    return;
+  }
+  const int U = a.num_unique[0];
+  const int u0 = uniform(a.chunk_seg[c]);
+  const int s0 = uniform(a.seg[u0]);
+  // lane l: the end of segment u0 + l, its key; positions' rows (a segment that starts here ends before p1 + 64)
+  const int ends = a.seg[min(u0 + 1 + lane, U)];
+  const uint32_t keys = a.ukeys[min(u0 + lane, U - 1)];
+  const int row_a = a.perm[min(p0 + lane, a.N - 1)], row_b = a.perm[min(p0 + kChunk + lane, a.N - 1)];
+  const int before = __shfl_up(ends, 1, kWave);
+  const int len = ends - (lane == 0 ? s0 : before);
+  const uint64_t heavy = __ballot(len > kChunk);
+  // the segment that holds the chunk's last position
+  const int n_ended = __popcll(__ballot(u0 + lane < U && ends <= p1 - 1));
+  const int last = min(n_ended, kWave - 1);
+  const bool old_light = s0 < p0 && !(heavy & 1u);  // the previous chunk's wavefront has its positions
+  const int fin = (heavy >> last) & 1u ? p1 : lane_at(ends, last);
+  int i = 0, q = p0;
+  if (old_light) {
+    q = lane_at(ends, 0);
+    i = 1;
+    if (q >= p1) return;
+  }
+  float acc[EL] = {};
+  int parity = 0;
+  while (q < fin) {
+    // a padding segment has no gradient: its positions are not read
+    if (lane_at(keys, i) == a.pad) {
+      if constexpr (KIND == kStore) {
+        if (!((heavy >> i) & 1u) && in && a.layout != EMB_TABLE_ADD) {
+          float z[EL] = {};
+          Vec<float, EL>::store(a.grad + (int64_t)(a.layout == EMB_ROWS ? (uint32_t)(u0 + i) : a.pad) * a.D + col, z);
+        }
+      }
+      // (a batch may have ended inside it)
+#pragma unroll
+      for (int e = 0; e < EL; ++e) acc[e] = 0.f;
+      q = min(lane_at(ends, i), fin);
+      ++i;
+      continue;
+    }
+    Vec<TG, EL> g[B];
+    Vec<TW, EL> w[B];
+    Vec<float, EL> h[B];
+    float done[B][EL];
+    int seg_of[B];  // the segment that ends at the batch's position, or -1
+    const int n = min(B, fin - q);
+    int j = i;
+#pragma unroll
+    for (int k = 0; k < B; ++k) {
+      const int pos = min(q + k, fin - 1) - p0;
+      const int row = pos < kWave ? lane_at(row_a, pos) : lane_at(row_b, pos - kWave);
+      const char* src = a.dy + (int64_t)row * a.ld + (int64_t)cs * (Vec<TG, EL>::kBytes / EL);
+      if (a.aligned) g[k].load(src);
+      else g[k].load_each(src);
+    }
+#pragma unroll
+    for (int k = 0; k < B; ++k) {
+      seg_of[k] = -1;
+      if (k < n && q + k + 1 == min(lane_at(ends, j), fin)) {
+        seg_of[k] = j;
+        if constexpr (KIND != kStore) {
+          const uint32_t key = lane_at(keys, j);
+          if (!((heavy >> j) & 1u) && key < a.rows && key != a.pad) {
+            w[k].load(static_cast<const char*>(a.up.W) + ((int64_t)key * a.D + cs) * (int64_t)sizeof(TW));
+            if constexpr (KIND == kAdaElem) h[k].load(a.up.state + (int64_t)key * a.D + cs);
+          }
+        }
+        j = min(j + 1, kWave - 1);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < B; ++k) {
+#pragma unroll
+      for (int e = 0; e < EL; ++e) {
+        acc[e] += k < n ? g[k].get(e) : 0.f;
+        done[k][e] = acc[e] * a.scale;
+      }
+      if (seg_of[k] >= 0) {
+#pragma unroll
+        for (int e = 0; e < EL; ++e) acc[e] = 0.f;
+        if ((heavy >> seg_of[k]) & 1u) {
+          if (in)
+            Vec<float, EL>::store(a.partials + ((int64_t)c * 2 + (seg_of[k] == 0 ? 0 : 1)) * a.D + col, done[k]);
+          seg_of[k] = -1;
+        }
+      }
+    }
+    if constexpr (KIND == kStore) {
+#pragma unroll
+      for (int k = 0; k < B; ++k) {
+        if (seg_of[k] < 0) continue;
+        const uint32_t key = lane_at(keys, seg_of[k]);
+        if (a.layout != EMB_ROWS && key >= a.rows) continue;
+        if (!in) continue;
+        float* dst = a.grad + (int64_t)(a.layout == EMB_ROWS ? (uint32_t)(u0 + seg_of[k]) : key) * a.D + col;
+        if (key == a.pad) {
+          if (a.layout == EMB_TABLE_ADD) continue;
+#pragma unroll
+          for (int e = 0; e < EL; ++e) done[k][e] = 0.f;
+        }
+        if (a.layout == EMB_TABLE_ADD) {
+          Vec<float, EL> old;
+          old.load(dst);
+#pragma unroll
+          for (int e = 0; e < EL; ++e) done[k][e] += old.get(e);
+        }
+        Vec<float, EL>::store(dst, done[k]);
+      }
+    } else {
+      float total[B];
+      if constexpr (KIND == kAdaRow) {
+#pragma unroll
+        for (int k = 0; k < B; ++k) {
+          float sq = 0.f;
+#pragma unroll
+          for (int e = 0; e < EL; ++e) sq = __builtin_fmaf(done[k][e], done[k][e], sq);
+          total[k] = seg_of[k] >= 0 ? wave_total(in ? sq : 0.f) : 0.f;
+        }
+        if (a.parts > 1) {
+          // (a batch's sums are read before the batch after next is summed, a barrier later)
+          if (lane == 0) {
+#pragma unroll
+            for (int k = 0; k < B; ++k) s_sq[parity][wave][k] = total[k];
+          }
+          __syncthreads();
+#pragma unroll
+          for (int k = 0; k < B; ++k) {
+            total[k] = 0.f;
+            for (int p = 0; p < a.parts; ++p) total[k] += s_sq[parity][p][k];
+          }
+          parity ^= 1;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < B; ++k) {
+        if (seg_of[k] < 0) continue;
+        const uint32_t key = lane_at(keys, seg_of[k]);
+        if (key >= a.rows || key == a.pad) continue;
+        float step = a.up.lr;
+        if constexpr (KIND == kAdaRow) {
+          const float hn = a.up.state[key] + total[k] / (float)a.D;
+          step = a.up.lr / (sqrtf(hn) + a.up.eps);
+          if (a.parts > 1) __syncthreads();  // every wavefront has read the accumulator
+          if (wave == 0 && lane == 0) a.up.state[key] = hn;
+        }
+        if (in) apply<TW, EL, KIND>(a.up, key, col, done[k], w[k], h[k], step);
+      }
+    }
+    i = j;
+    q += n;
+  }
+}
+
+// Rows of the table that no token named: zeros.  One wavefront per 64 rows.
+__global__ __launch_bounds__(256) void k_token_zero(TokGrad a) {
+  const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
+  const int64_t r0 = ((int64_t)blockIdx.x * 4 + wave) * kWave;
+  if (r0 >= (int64_t)a.rows) return;
+  const int U = failed(a) ? 0 : a.num_unique[0];
+  uint64_t named = 0;
+  if (U > 0) {
+    const int u = r0 == 0 ? 0 : wave_upper_bound<uint32_t>(a.ukeys, U, (uint32_t)r0 - 1u, lane);
+    const uint32_t key = u + lane < U ? a.ukeys[u + lane] : kNoRow;
+    uint64_t bit = (uint64_t)key < (uint64_t)r0 + kWave ? 1ull << (key - (uint32_t)r0) : 0ull;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1)
+      bit |= ((uint64_t)(uint32_t)__shfl_xor((int)(bit >> 32), o, kWave) << 32) |
+             (uint32_t)__shfl_xor((int)(uint32_t)bit, o, kWave);
+    named = bit;
+  }
+  const int n = (int)min((int64_t)kWave, (int64_t)a.rows - r0);
+  for (int r = 0; r < n; ++r) {
+    if ((named >> r) & 1ull) continue;
+    float* dst = a.grad + (r0 + r) * (int64_t)a.D;
+    for (int c = lane * 4; c < a.D; c += kWave * 4) *reinterpret_cast<f32x4*>(dst + c) = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+}
+
+// A segment of more than 64 positions: the partial rows of its chunks added in
+// double, in chunk order, by the block of the chunk it starts in.
+template <typename TW, int KIND>
+__global__ __launch_bounds__(256) void k_token_combine(TokGrad a) {
+  const int c = blockIdx.x, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  const int p0 = c * kChunk, p1 = min(a.N, p0 + kChunk);
+  if (failed(a)) return;
+  const int U = a.num_unique[0];
+  // the segment that holds the chunk's last position, if it is long and starts here
+  const int next = a.chunk_seg[c + 1];  // (U after the last chunk)
+  const int u = next == U || a.seg[next] >= p1 ? next - 1 : next;
+  const int s = a.seg[u], e = a.seg[u + 1];
+  if (s < p0 || e - s <= kChunk) return;
+  const uint32_t key = a.ukeys[u];
+  const bool pad = key == a.pad;
+  if (pad && KIND != kStore) return;
+  if (key >= a.rows && !(KIND == kStore && a.layout == EMB_ROWS)) return;
+  const int last = (e - 1) / kChunk;
+  const float* first = a.partials + ((int64_t)c * 2 + (s == p0 ? 0 : 1)) * a.D;
+  auto sum = [&](int col) {
+    double t = first[col];
+    int k = c + 1;
+    for (; k + 8 <= last + 1; k += 8) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = a.partials[(int64_t)(k + i) * 2 * a.D + col];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t += (double)x[i];
+    }
+    for (; k <= last; ++k) t += (double)a.partials[(int64_t)k * 2 * a.D + col];
+    return (float)t;
+  };
+  if constexpr (KIND == kStore) {
+    if (pad && a.layout == EMB_TABLE_ADD) return;
+    float* dst = a.grad + (int64_t)(a.layout == EMB_ROWS ? (uint32_t)u : key) * a.D;
+    for (int col = threadIdx.x; col < a.D; col += 256) {
+      const float g = pad ? 0.f : sum(col);
+      dst[col] = a.layout == EMB_TABLE_ADD ? dst[col] + g : g;
+    }
+  } else {
+    __shared__ float s_sq[4];
+    float step = a.up.lr;
+    float* row = const_cast<float*>(first);  // (the sums, where the squares are needed first)
+    if constexpr (KIND == kAdaRow) {
+      float sq = 0.f;
+      for (int col = threadIdx.x; col < a.D; col += 256) {
+        const float g = sum(col);
+        row[col] = g;
+        sq = __builtin_fmaf(g, g, sq);
+      }
+      sq = wave_total(sq);
+      if (lane == 0) s_sq[wave] = sq;
+      const float old = a.up.state[key];
+      __syncthreads();
+      const float hn = old + (s_sq[0] + s_sq[1] + s_sq[2] + s_sq[3]) / (float)a.D;
+      step = a.up.lr / (sqrtf(hn) + a.up.eps);
+      if (threadIdx.x == 0) a.up.state[key] = hn;
+    }
+    for (int col = threadIdx.x; col < a.D; col += 256) {
+      float g[1] = {KIND == kAdaRow ? row[col] : sum(col)};
+      Vec<TW, 1> w;
+      Vec<float, 1> h;
+      w.load(static_cast<const char*>(a.up.W) + ((int64_t)key * a.D + col) * (int64_t)sizeof(TW));
+      if constexpr (KIND == kAdaElem) h.load(a.up.state + (int64_t)key * a.D + col);
+      apply<TW, 1, KIND>(a.up, key, col, g, w, h, step);
+    }
+  }
+}
+
+template <typename TG, typename TW, int KIND>
+hipError_t grad_kernels(TokGrad a, hipStream_t s) {
+  // columns a lane: 1 for rows of up to 64 values, 4, or 8 above 4096
+  const int el = a.D <= kWave ? 1 : (a.D <= kMostParts * kWave * 4 ? 4 : 8);
+  a.parts = (a.D + kWave * el - 1) / (kWave * el);
+  constexpr bool kRow = KIND == kAdaRow;
+  const dim3 block(kRow ? a.parts * kWave : 4 * kWave);
+  const dim3 grid(kRow ? a.nchunks : (a.nchunks * a.parts + 3) / 4);
+  const uintptr_t at = reinterpret_cast<uintptr_t>(a.dy) | (uintptr_t)a.ld;
+  const int vec = el * (int)(sizeof(TG));
+  a.aligned = at % (uintptr_t)(vec < 16 ? vec : 16) == 0;
+  if (el == 1) k_token_reduce<TG, TW, 1, 8, KIND><<<grid, block, 0, s>>>(a);
+  else if (el == 4) k_token_reduce<TG, TW, 4, 8, KIND><<<grid, block, 0, s>>>(a);
+  else k_token_reduce<TG, TW, 8, 4, KIND><<<grid, block, 0, s>>>(a);
+  k_token_combine<TW, KIND><<<a.nchunks, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <typename TG, typename TW>
+hipError_t update_kernels(const TokGrad& a, int opt, hipStream_t s) {
+  if (opt == EMB_OPT_SGD) return grad_kernels<TG, TW, kSgd>(a, s);
+  if (opt == EMB_OPT_ADAGRAD_ROWWISE) return grad_kernels<TG, TW, kAdaRow>(a, s);
+  return grad_kernels<TG, TW, kAdaElem>(a, s);
+}
+
+template <typename TW, typename TO, int V, bool MANY>
+void fwd_kernel(TokFwd a, const Stacked<MANY>& st, hipStream_t s) {
+  a.aligned = (reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)a.out_bytes) % (Vec<TO, V>::kBytes < 16 ? Vec<TO, V>::kBytes : 16) == 0;
+  int lg = 0;
+  while (lg < 8 && (1 << lg) < a.vectors) ++lg;
+  a.log_g = lg;
+  const int per = kFwdThreads >> lg;
+  const unsigned parts = (unsigned)((a.vectors + (1 << lg) - 1) >> lg);
+  // four rows a lane in flight once one row a lane would fill the device
+  if (a.N * parts / per >= 2048) {
+    const dim3 grid((unsigned)((a.N + per * 4 - 1) / (per * 4)), parts);
+    k_token_fwd<TW, TO, V, 4, MANY><<<grid, kFwdThreads, 0, s>>>(a, st);
+  } else {
+    const dim3 grid((unsigned)((a.N + per - 1) / per), parts);
+    k_token_fwd<TW, TO, V, 1, MANY><<<grid, kFwdThreads, 0, s>>>(a, st);
+  }
+}
+
+template <bool MANY>
+hipError_t fwd_types(TokFwd a, const Stacked<MANY>& st, int dtype, int out, int D, hipStream_t s) {
+  // 16 bytes of the table's row a lane
+  a.vectors = D / (dtype == EMB_BF16 ? 8 : 4);
+  if (dtype == EMB_BF16) {
+    if (out == EMB_BF16) fwd_kernel<bf16, bf16, 8, MANY>(a, st, s);
+    else fwd_kernel<bf16, float, 8, MANY>(a, st, s);
+  } else {
+    if (out == EMB_BF16) fwd_kernel<float, bf16, 4, MANY>(a, st, s);
+    else fwd_kernel<float, float, 4, MANY>(a, st, s);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_token_fwd(const TokenFwdLaunch& p, hipStream_t s) {
+  TokFwd a{};
+  a.W = static_cast<const char*>(p.W);
+  a.idx = p.idx;
+  a.idx64 = p.idx64;
+  a.offsets = p.offsets;
+  a.out = static_cast<char*>(p.out);
+  a.N = p.N;
+  a.row_bytes = (int64_t)p.D * (p.dtype == EMB_BF16 ? 2 : 4);
+  a.out_bytes = p.ld * (p.out_dtype == EMB_BF16 ? 2 : 4);
+  a.T = p.T;
+  a.B = p.B;
+  a.rows = p.rows;
+  a.pad = p.pad;
+  a.scale = p.scale;
+  if (p.T == 1) return fwd_types<false>(a, Stacked<false>{}, p.dtype, p.out_dtype, p.D, s);
+  return fwd_types<true>(a, Stacked<true>{p.ro}, p.dtype, p.out_dtype, p.D, s);
+}
+
+hipError_t launch_token_grad(const TokenGradLaunch& p, hipStream_t s) {
+  char* ws = static_cast<char*>(p.ws);
+  TokGrad a{};
+  a.dy = static_cast<const char*>(p.dy);
+  a.ld = p.ld * (p.dy_dtype == EMB_BF16 ? 2 : 4);
+  a.perm = p.perm;
+  a.seg = p.seg;
+  a.ukeys = p.ukeys;
+  a.num_unique = p.num_unique;
+  a.chunk_seg = reinterpret_cast<const int32_t*>(ws + p.lay.chunk_seg);
+  a.hdr = ws + p.lay.hdr;
+  a.partials = reinterpret_cast<float*>(ws + p.lay.partials);
+  a.grad = p.grad;
+  a.N = p.N;
+  a.D = p.D;
+  a.nchunks = (p.N + kChunk - 1) / kChunk;
+  a.layout = p.layout;
+  a.rows = p.rows;
+  a.pad = p.pad;
+  a.scale = p.scale;
+  a.up.W = p.W;
+  a.up.state = p.state;
+  a.up.D = p.D;
+  a.up.opt = p.opt;
+  a.up.lr = p.lr;
+  a.up.eps = p.eps;
+  a.up.rounding = p.rounding;
+  a.up.seed = p.seed;
+  if (!p.fuse) {
+    if (p.layout == EMB_TABLE && p.rows > 0) k_token_zero<<<(unsigned)(((int64_t)p.rows + 255) / 256), 256, 0, s>>>(a);
+    if (p.N == 0) return hipGetLastError();
+    return p.dy_dtype == EMB_BF16 ? grad_kernels<bf16, float, kStore>(a, s) : grad_kernels<float, float, kStore>(a, s);
+  }
+  if (p.N == 0) return hipSuccess;
+  if (p.dtype == EMB_BF16)
+    return p.dy_dtype == EMB_BF16 ? update_kernels<bf16, bf16>(a, p.opt, s) : update_kernels<float, bf16>(a, p.opt, s);
+  return p.dy_dtype == EMB_BF16 ? update_kernels<bf16, float>(a, p.opt, s) : update_kernels<float, float>(a, p.opt, s);
+}
+
+}  // namespace emb

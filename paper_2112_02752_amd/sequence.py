@@ -1,0 +1,408 @@
+"""Sequences of tokens over the layer's tables: lookup of single tokens with
+the gradient by sorted tokens, a gated linear recurrence, activations kept in
+8 bits, and the layer that runs them together.
+
+As the rest of the binding this only marshals arguments (and checks the
+shapes, which the C ABI cannot see); every step runs in the library's kernels.
+The projections of ``SequenceLayer`` are plain matrix products of PyTorch's.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional
+
+from . import (BF16, FP32, Batch, CUpdate, DedupBuffers, StepFailed, Tables, _check, _ptr, _stream, _update, lib,
+               workspace_status)
+
+SAVED8 = 2
+SPAN = 64           # EMB_SCAN_SPAN: positions between kept states
+GROUP = 32          # EMB_SAVED_GROUP: columns that share an exponent
+LAYOUT = {"rows": 0, "table": 1, "table_add": 2}
+
+
+class CMat(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("ld", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("exps", ctypes.c_void_p), ("ld_exps", ctypes.c_int64)]
+
+
+class CToken(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("pad_row", ctypes.c_int64)]
+
+
+class CScan(ctypes.Structure):
+    _fields_ = [("num_tokens", ctypes.c_int64), ("num_seqs", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("offsets", ctypes.c_void_p), ("x", CMat), ("f", CMat), ("o", CMat), ("bias", ctypes.c_void_p),
+                ("h0", ctypes.c_void_p)]
+
+
+def _declare(L) -> None:
+    vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+    from . import CBatch, CTables
+    T, B, Up = ctypes.POINTER(CTables), ctypes.POINTER(CBatch), ctypes.POINTER(CUpdate)
+    M, Tok, S = ctypes.POINTER(CMat), ctypes.POINTER(CToken), ctypes.POINTER(CScan)
+    for name, res, args in (
+            ("emb_token_fwd", i32, [T, B, Tok, M, vp]),
+            ("emb_token_grad", i32, [T, B, Tok, M, vp, vp, vp, vp, vp, i32, Up, vp, sz, vp]),
+            ("emb_scan_workspace_size", sz, [i64, i32]),
+            ("emb_scan_fwd", i32, [S, M, vp, vp, vp, sz, vp]),
+            ("emb_scan_bwd", i32, [S, vp, M, vp, M, M, M, vp, vp, vp, sz, vp]),
+            ("emb_scan_step", i32, [i64, i32, M, M, M, vp, vp, i64, vp, M, vp]),
+            ("emb_save", i32, [i64, i32, M, M, vp]),
+            ("emb_restore", i32, [i64, i32, M, M, vp]),
+            ("emb_weight_grad_workspace_size", sz, [i64, i32, i32]),
+            ("emb_weight_grad", i32, [i64, i32, i32, M, M, vp, i32, vp, sz, vp])):
+        fn = getattr(L, name)
+        fn.restype, fn.argtypes = res, args
+
+
+def _device(t, what: str):
+    if not t.is_cuda:
+        raise ValueError(f"{what} must lie on the GPU")
+    return t
+
+
+class Mat:
+    """A matrix of activations as the C ABI takes it: a 2-d fp32 or bf16
+    tensor whose columns are contiguous, rows at any stride (a slice of a wider
+    tensor's columns); an 8-bit one comes from ``Checkpoint.columns``.  Kept by
+    a program between calls, it costs a call one address check."""
+
+    __slots__ = ("tensor", "exps", "rows", "cols", "_c", "_at", "ref", "_first")
+
+    def __init__(self, tensor, exps=None, first: int = 0, cols: Optional[int] = None):
+        import torch
+        if tensor.dim() != 2 or (tensor.shape[1] > 1 and tensor.stride(1) != 1):
+            raise ValueError("a matrix has two dimensions and contiguous columns")
+        _device(tensor, "a matrix")
+        self.tensor, self.exps, self._first = tensor, exps, first
+        self.rows = int(tensor.shape[0])
+        self.cols = int(tensor.shape[1]) if cols is None else cols
+        ld = int(tensor.stride(0)) if self.rows > 1 else max(int(tensor.stride(0)), int(tensor.shape[1]))
+        if exps is not None:
+            if tensor.dtype != torch.int8 or exps.dtype != torch.uint8:
+                raise ValueError("a checkpoint holds int8 codes and uint8 exponents")
+            le = int(exps.stride(0)) if self.rows > 1 else int(exps.shape[1])
+            self._c = CMat(0, ld, SAVED8, 0, le)
+        else:
+            if tensor.dtype not in (torch.float32, torch.bfloat16):
+                raise ValueError("a matrix is fp32 or bf16")
+            self._c = CMat(0, ld, BF16 if tensor.dtype == torch.bfloat16 else FP32, None, 0)
+        if ld < int(tensor.shape[1]):
+            raise ValueError("rows overlap")
+        self._at = None
+        self.ref = ctypes.byref(self._c)
+        self.c()
+
+    @property
+    def dtype(self) -> int:
+        return self._c.dtype
+
+    def c(self) -> CMat:
+        at = self.tensor.data_ptr()
+        if at != self._at:
+            self._at = at
+            self._c.data = at + self._first if at else None
+            if self.exps is not None:
+                self._c.exps = self.exps.data_ptr() + self._first // GROUP
+        return self._c
+
+
+def _mat(m) -> Mat:
+    if not isinstance(m, Mat):
+        return Mat(m)
+    m.c()
+    return m
+
+
+def _want(m: Mat, rows: int, cols: int, what: str) -> None:
+    if m.rows != rows or m.cols != cols:
+        raise ValueError(f"{what} has {m.rows} x {m.cols} values, {rows} x {cols} are wanted")
+
+
+def _floats(t, shape, what: str) -> Optional[int]:
+    """Address of a contiguous fp32 tensor of this shape, or None."""
+    if t is None:
+        return None
+    import torch
+    if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{what} is a contiguous fp32 tensor of shape {shape}")
+    return _device(t, what).data_ptr()
+
+
+# ---------------------------------------------------------------- tokens
+
+def token_fwd(tables: Tables, batch: Batch, out, scale: float = 1.0, pad_row: int = -1, stream=None) -> None:
+    """out[j] = scale * W[key(j)] for every token of the batch's sequences
+    (emb_token_fwd); zeros for tokens of the global row ``pad_row``."""
+    out = _mat(out)
+    _want(out, int(batch.indices.numel()), int(tables.weights.shape[1]), "out")
+    tok = CToken(scale, pad_row)
+    _check("emb_token_fwd", lib().emb_token_fwd(ctypes.byref(tables.c()), ctypes.byref(batch.c()), ctypes.byref(tok),
+                                                out.ref, _stream(stream)))
+
+
+def token_grad(tables: Tables, batch: Batch, grad_out, dedup: DedupBuffers, grad=None, layout: str = "rows",
+               scale: float = 1.0, pad_row: int = -1, opt: Optional[str] = None, lr: float = 0.0, eps: float = 0.0,
+               state=None, rounding: str = "nearest", seed: int = 0, stream=None) -> None:
+    """Gradient of ``token_fwd`` by sorted tokens (emb_token_grad), after
+    ``unique_ids`` of the same batch into ``dedup``: gradient rows in ``grad``
+    as ``layout`` says, or with ``opt`` the optimizer step."""
+    grad_out = _mat(grad_out)
+    n, D = int(batch.indices.numel()), int(tables.weights.shape[1])
+    _want(grad_out, n, D, "grad_out")
+    if grad is not None:
+        rows = n if layout == "rows" else int(tables.row_offset[-1])
+        if int(grad.shape[0]) < rows:
+            raise ValueError("grad has too few rows")
+        _floats(grad, (int(grad.shape[0]), D), "grad")
+    tok = CToken(scale, pad_row)
+    upd = ctypes.byref(_update(opt, lr, eps, state, rounding, seed)) if opt is not None else None
+    d = dedup
+    _check("emb_token_grad", lib().emb_token_grad(
+        ctypes.byref(tables.c()), ctypes.byref(batch.c()), ctypes.byref(tok), grad_out.ref, _ptr(d.sort_perm),
+        _ptr(d.seg_offsets), _ptr(d.unique_keys), _ptr(d.num_unique), _ptr(grad), LAYOUT[layout], upd, _ptr(d.ws),
+        d.ws.numel(), _stream(stream)))
+
+
+class TokenLayer:
+    """Lookup of single tokens from the tables, scaled, with its backward:
+    the table's gradient or the optimizer step on the rows that were looked up.
+    ``pad_row`` (a global row, or -1) stands for padding: it gives zeros and is
+    never trained.  ``max_tokens`` sizes the dedup of the backward (0: a layer
+    that only looks up).  Calls on one layer must be ordered."""
+
+    def __init__(self, tables: Tables, scale: float = 1.0, pad_row: int = -1, opt: Optional[str] = None,
+                 lr: float = 0.0, eps: float = 1e-8, state=None, max_tokens: int = 0, max_seqs: int = 0,
+                 rounding: str = "nearest", seed: int = 0):
+        self.tables, self.opt = tables, opt
+        self.dim = int(tables.weights.shape[1])
+        self._rows = int(tables.row_offset[-1])
+        self._tok = CToken(scale, pad_row)
+        self._tokp = ctypes.byref(self._tok)
+        self.max_tokens = max_tokens
+        self.seed, self.steps_done = seed, 0
+        self.dedup = None
+        if max_tokens > 0:
+            d = self.dedup = DedupBuffers(tables.weights.device, max_tokens, max_seqs, self.dim)
+            self._dd = tuple(_ptr(t) for t in (d.unique_keys, d.counts, d.seg_offsets, d.sort_perm, d.num_unique,
+                                               d.ws)) + (d.ws.numel(),)
+        self._upd = None
+        if opt is not None:
+            self._updc = _update(opt, lr, eps, state, rounding, seed)
+            self._upd = ctypes.byref(self._updc)
+            self._state = state
+
+    def forward(self, batch: Batch, out, stream=None) -> None:
+        out = _mat(out)
+        _want(out, batch.indices.numel(), self.dim, "out")
+        _check("emb_token_fwd", lib().emb_token_fwd(ctypes.byref(self.tables.c()), ctypes.byref(batch.c()),
+                                                    self._tokp, out.ref, _stream(stream)))
+
+    def _backward(self, batch: Batch, grad_out, grad, layout: int, upd, stream) -> None:
+        n = batch.indices.numel()
+        if n > self.max_tokens:
+            raise ValueError("batch larger than the layer's buffers")
+        if self.dedup is None:
+            raise ValueError("a layer without max_tokens only looks up")
+        g = _mat(grad_out)
+        _want(g, n, self.dim, "grad_out")
+        L, s = lib(), _stream(stream)
+        uk, cnt, seg, perm, nu, ws, wsb = self._dd
+        ct, cb = ctypes.byref(self.tables.c()), ctypes.byref(batch.c())
+        _check("emb_unique_ids", L.emb_unique_ids(ct, cb, uk, cnt, seg, perm, nu, ws, wsb, s))
+        _check("emb_token_grad", L.emb_token_grad(ct, cb, self._tokp, g.ref, perm, seg, uk, nu, grad, layout, upd, ws,
+                                                  wsb, s))
+
+    def table_grad(self, batch: Batch, grad_out, grad, add: bool = False, stream=None) -> None:
+        """The gradient of every row of the tables into ``grad`` (fp32, rows x
+        dim): written, or with ``add`` added to what is there."""
+        self._backward(batch, grad_out, _floats(grad, (self._rows, self.dim), "grad"),
+                       LAYOUT["table_add" if add else "table"], None, stream)
+
+    def row_grads(self, batch: Batch, grad_out, grad_rows, stream=None) -> None:
+        """Gradient rows of the batch's distinct tokens (``dedup.unique_keys``,
+        ``dedup.num_unique``) into ``grad_rows`` (fp32, at least a row a token)."""
+        if int(grad_rows.shape[0]) < batch.indices.numel():
+            raise ValueError("grad_rows has too few rows")
+        self._backward(batch, grad_out, _floats(grad_rows, (int(grad_rows.shape[0]), self.dim), "grad_rows"),
+                       LAYOUT["rows"], None, stream)
+
+    def update(self, batch: Batch, grad_out, stream=None) -> None:
+        """The optimizer step on the rows that were looked up."""
+        if self._upd is None:
+            raise ValueError("a layer without an optimizer cannot update")
+        self._updc.seed = self.seed + self.steps_done
+        self._backward(batch, grad_out, None, LAYOUT["rows"], self._upd, stream)
+        self.steps_done += 1
+
+    def check(self, stream=None) -> None:
+        """Raise StepFailed if the last backward failed on the device (it then
+        wrote no table row)."""
+        import torch
+        st = torch.zeros(4, dtype=torch.int32, device=self.dedup.ws.device)
+        workspace_status(self.dedup.ws, st, stream)
+        st = tuple(int(x) for x in st.cpu())
+        if st[0]:
+            raise StepFailed(*st)
+
+
+# ---------------------------------------------------------------- recurrence
+
+class Scan:
+    """The inputs of a gated linear recurrence over ragged sequences (see
+    emb_scan): int32 offsets [M + 1] on the GPU, values, forget gates and output
+    gates (None: no output gate) as N x D matrices of one type, fp32 bias [D]
+    and first states [M][D] or None."""
+
+    def __init__(self, offsets, x, f, o=None, bias=None, h0=None):
+        import torch
+        if offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.numel() < 1 or not offsets.is_contiguous():
+            raise ValueError("offsets are a contiguous int32 vector")
+        _device(offsets, "offsets")
+        self.x, self.f, self.o = _mat(x), _mat(f), _mat(o) if o is not None else None
+        self.tokens, self.dim = self.x.rows, self.x.cols
+        self.seqs = int(offsets.numel()) - 1
+        _want(self.f, self.tokens, self.dim, "f")
+        if self.o is not None:
+            _want(self.o, self.tokens, self.dim, "o")
+        self.offsets, self.bias, self.h0 = offsets, bias, h0
+        self._c = CScan(self.tokens, self.seqs, self.dim, offsets.data_ptr(), self.x.c(), self.f.c(),
+                        self.o.c() if self.o is not None else CMat(), _floats(bias, (self.dim,), "bias"),
+                        _floats(h0, (self.seqs, self.dim), "h0"))
+        self.ref = ctypes.byref(self._c)
+
+
+def scan_workspace_size(num_tokens: int, dim: int) -> int:
+    return int(lib().emb_scan_workspace_size(num_tokens, dim))
+
+
+class Recurrence:
+    """The gated linear recurrence with its workspace, for batches of up to
+    ``max_tokens`` tokens; with ``train`` the forward keeps a state every 64
+    positions for the backward of the same batch.  Calls on one object must be
+    ordered."""
+
+    def __init__(self, max_tokens: int, max_seqs: int, dim: int, device="cuda", train: bool = True):
+        import torch
+        n = max(1, max_tokens)
+        size = scan_workspace_size(n, dim)
+        if size == 0:
+            raise ValueError("batch too large for one call")
+        self.max_tokens, self.max_seqs, self.dim = n, max_seqs, dim
+        self.ws = torch.empty(size, dtype=torch.uint8, device=device)
+        self._ws, self._wsb = self.ws.data_ptr(), size
+        self.states = torch.empty(((n + SPAN - 1) // SPAN, dim), device=device) if train else None
+        self._states = _ptr(self.states)
+        self._tokens = None
+
+    def _scan(self, scan: Scan):
+        if scan.tokens > self.max_tokens or scan.dim != self.dim:
+            raise ValueError("batch larger than the recurrence's buffers, or of another width")
+        return scan.ref
+
+    def forward(self, scan: Scan, y, h_last=None, stream=None) -> None:
+        """y (and the state after each sequence into ``h_last``, fp32 [M][D])."""
+        y = _mat(y)
+        _want(y, scan.tokens, self.dim, "y")
+        _check("emb_scan_fwd", lib().emb_scan_fwd(self._scan(scan), y.ref,
+                                                  _floats(h_last, (scan.seqs, self.dim), "h_last"), self._states,
+                                                  self._ws, self._wsb, _stream(stream)))
+        self._tokens = scan.tokens
+
+    def backward(self, scan: Scan, dy, dx, df, do=None, dbias=None, dh_last=None, dh0=None, stream=None) -> None:
+        """Gradients of the last forward: of the inputs, the bias and the first
+        states, from those of y and of the last states.  ``scan`` is the
+        forward's, or one whose matrices are restored from its checkpoints."""
+        if self.states is None or self._tokens != scan.tokens:
+            raise ValueError("backward follows the forward of the same batch on a recurrence made with train")
+        mats = [_mat(m) for m in (dy, dx, df)] + ([_mat(do)] if scan.o is not None else [])
+        for m, name in zip(mats, ("dy", "dx", "df", "do")):
+            _want(m, scan.tokens, self.dim, name)
+        each = (scan.seqs, self.dim)
+        _check("emb_scan_bwd", lib().emb_scan_bwd(
+            self._scan(scan), self._states, mats[0].ref, _floats(dh_last, each, "dh_last"), mats[1].ref, mats[2].ref,
+            mats[3].ref if scan.o is not None else None, _floats(dbias, (self.dim,), "dbias"),
+            _floats(dh0, each, "dh0"), self._ws, self._wsb, _stream(stream)))
+
+
+def scan_step(x, f, o, state, y, bias=None, slots=None, stream=None) -> None:
+    """One token of each running sequence (emb_scan_step): row i of x, f, o (or
+    None) and y belongs to state row ``slots[i]`` (int32; None: row i), which is
+    updated in place; tokens whose slot is no row of ``state`` get zeros."""
+    x, f, y = _mat(x), _mat(f), _mat(y)
+    n, D = x.rows, x.cols
+    _want(f, n, D, "f")
+    _want(y, n, D, "y")
+    if o is not None:
+        o = _mat(o)
+        _want(o, n, D, "o")
+    rows = state.shape[0]
+    sp = None
+    if slots is not None:
+        if slots.numel() != n or slots.element_size() != 4 or slots.is_floating_point() or not slots.is_contiguous():
+            raise ValueError("slots are a contiguous int32 vector, one a token")
+        sp = _device(slots, "slots").data_ptr()
+    _check("emb_scan_step", lib().emb_scan_step(n, D, x.ref, f.ref, o.ref if o is not None else None,
+                                                _floats(bias, (D,), "bias"), _floats(state, (rows, D), "state"), rows,
+                                                sp, y.ref, _stream(stream)))
+
+
+# ---------------------------------------------------------------- checkpoints
+
+class Checkpoint:
+    """Activations kept in 8 bits: codes (int8) and an exponent a group of 32
+    columns, for up to ``rows`` rows of ``dim`` columns."""
+
+    def __init__(self, rows: int, dim: int, device="cuda"):
+        import torch
+        groups = (dim + GROUP - 1) // GROUP
+        self._take(torch.empty((rows, groups * GROUP), dtype=torch.int8, device=device),
+                   torch.empty((rows, groups), dtype=torch.uint8, device=device), dim)
+
+    @classmethod
+    def of(cls, codes, exps, dim: int) -> "Checkpoint":
+        """A checkpoint that exists already: codes [rows][dim rounded up to
+        32] and exponents [rows][groups]."""
+        groups = (dim + GROUP - 1) // GROUP
+        if tuple(codes.shape) != (codes.shape[0], groups * GROUP) or tuple(exps.shape) != (codes.shape[0], groups):
+            raise ValueError("codes and exponents of whole groups are wanted")
+        if not (codes.is_contiguous() and exps.is_contiguous()):
+            raise ValueError("codes and exponents are contiguous")
+        self = cls.__new__(cls)
+        self._take(codes, exps, dim)
+        return self
+
+    def _take(self, codes, exps, dim: int) -> None:
+        self.codes, self.exps, self.dim, self.rows = codes, exps, dim, int(codes.shape[0])
+        self.mat = Mat(codes, exps, 0, dim)
+        self._ws = None
+
+    def columns(self, first: int, count: int) -> Mat:
+        """Columns first .. first + count - 1 as a matrix (for ``Scan``)."""
+        if first % GROUP != 0 or first < 0 or count < 1 or first + count > self.dim:
+            raise ValueError("columns of a checkpoint start at a group's first")
+        return Mat(self.codes[:, first:], self.exps[:, first // GROUP:], 0, count)
+
+    def pack(self, src, stream=None) -> None:
+        src = _mat(src)
+        _want(src, self.rows, self.dim, "src")
+        _check("emb_save", lib().emb_save(self.rows, self.dim, src.ref, self.mat.ref, _stream(stream)))
+
+    def unpack(self, dst, stream=None) -> None:
+        dst = _mat(dst)
+        _want(dst, self.rows, self.dim, "dst")
+        _check("emb_restore", lib().emb_restore(self.rows, self.dim, self.mat.ref, dst.ref, _stream(stream)))
+
+    def weight_grad(self, dy, dw, add: bool = False, stream=None) -> None:
+        """dw[k][c] = sum over rows of the restored value times dy[row][c]: the
+        gradient of the weights [dim][cols] (fp32) of a projection of what was
+        packed (emb_weight_grad)."""
+        dy = _mat(dy)
+        _want(dy, self.rows, dy.cols, "dy")
+        size = lib().emb_weight_grad_workspace_size(self.rows, self.dim, dy.cols)
+        if size and (self._ws is None or self._ws.numel() < size):
+            import torch
+            self._ws = torch.empty(size, dtype=torch.uint8, device=self.codes.device)
+        _check("emb_weight_grad", lib().emb_weight_grad(
+            self.rows, self.dim, dy.cols, self.mat.ref, dy.ref, _floats(dw, (self.dim, dy.cols), "dw"), int(add),
+            _ptr(self._ws) if size else None, size, _stream(stream)))
