@@ -136,6 +136,8 @@ emb_status route_prepare(const emb_tables* tables, const emb_batch* batch, int32
 
 constexpr int64_t kMaxTokens = ((int64_t)1 << 31) - 64 - 1;
 
+constexpr int64_t kMaxRowBytes = (int64_t)1 << 24;
+
 emb_status check_token(const emb_token* t, int64_t R) {
   return t == nullptr || t->pad_row >= R ? EMB_EINVAL : EMB_OK;
 }
@@ -782,7 +784,9 @@ emb_status emb_weight_grad(int64_t rows, int32_t dim, int32_t cols, const emb_ma
     p.dtype = dy->dtype;
     p.x = rows_of(*x);
     p.dy = rows_of(*dy);
-    p.aligned = (((uintptr_t)p.dy.p | (uintptr_t)p.dy.ld) & (dy->dtype == EMB_BF16 ? 7u : 15u)) == 0;
+    p.aligned = (((uintptr_t)p.dy.p | (uintptr_t)p.dy.ld) & 3u) == 0;
+    // (offsets within a step's rows are 32 bits)
+    if (p.x.ld > kMaxRowBytes || p.dy.ld > kMaxRowBytes || p.x.ld_exps > kMaxRowBytes) return EMB_EUNSUPPORTED;
   }
   const size_t need = weight_grad_ws_bytes(rows, dim, cols);
   if (need > 0 && ws == nullptr) return EMB_EINVAL;

@@ -4,11 +4,18 @@
 //
 // on the matrix units, in bf16: a restored x has 7 significant bits and is exact
 // in bf16; an fp32 dy is split into three bf16 parts that hold all of its 24
-// bits.  Sums are fp32.  Both operands lie with the summed index (the rows)
-// slowest, while a matrix instruction wants eight consecutive rows of a column
-// in a lane, so a lane loads four columns of eight rows and turns them in
-// registers on their way to LDS, where a column's eight rows are 16 bytes.  Few
-// tiles of dw: the rows are cut into parts whose sums are added in order.
+// bits.  Sums are fp32.
+//
+// Both operands lie with the summed index (the rows) slowest, while a matrix
+// instruction wants eight consecutive rows of a column in a lane.  So a lane
+// loads four columns of eight rows and turns them in registers (two permutes
+// for two columns of two rows; codes become bf16 on the way) into LDS, where a
+// column's eight rows are 16 bytes.  Columns 4 q + j of a group of 128 lie by j,
+// then q: lanes write and read consecutive 16 bytes, and the instruction of
+// slice j gives a lane column 4 q + j, so the four slices of a lane are four
+// consecutive columns of dw.
+//
+// Few tiles of dw: the rows are cut into parts whose sums are added in order.
 #include "seq_common.h"
 
 namespace emb {
@@ -18,9 +25,9 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kTile = 128;  // columns of x, and of dy, a block's tile has
 constexpr int kStep = 64;   // rows a step takes
 constexpr int kOct = kStep / 8;
+constexpr int kGroup = 128;  // columns of an LDS group
 constexpr int kThreads = 256;
 
 struct WArgs {
@@ -29,83 +36,97 @@ struct WArgs {
   const char* dy;
   float* out;        // dw, or [parts][K][F]
   int64_t ld_x, ld_e, ld_dy;  // bytes
-  int32_t N, K, F, steps_per_part, parts, tiles_k, tiles_f, add, aligned;
+  int32_t N, K, F, steps_per_part, parts, tiles_k, tiles_f, add;
 };
 
 // unsigned halves of two words: lo | hi << 16
 __device__ __forceinline__ uint32_t halves_lo(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ uint32_t halves_hi(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
-template <int SPLIT>  // 1: dy is bf16; 3: fp32 in three parts
-__global__ __launch_bounds__(kThreads) void k_weight_grad(WArgs a) {
-  __shared__ u32x4 s_x[kOct][kTile], s_y[SPLIT][kOct][kTile];
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  const int tile = blockIdx.x % (a.tiles_k * a.tiles_f), part = blockIdx.x / (a.tiles_k * a.tiles_f);
-  const int k0 = tile % a.tiles_k * kTile, c0 = tile / a.tiles_k * kTile;
-  // this thread loads columns 4 * (t % 32) .. of rows 8 * (t / 32) .. of a step
-  const int quad = threadIdx.x % 32, oct = threadIdx.x / 32;
-  const int kx = k0 + 4 * quad, cy = c0 + 4 * quad;
-  const bool k_in = kx < a.K;  // (a row of codes is padded to whole groups)
-  const int64_t r_begin = (int64_t)part * a.steps_per_part * kStep;
-  const int64_t r_end = min((int64_t)a.N, r_begin + (int64_t)a.steps_per_part * kStep);
-  f32x16 acc[2][2] = {};
-  const int wk = (wave & 1) * 64, wc = (wave >> 1) * 64;
-  uint32_t xr[8], er[8], yr[8][SPLIT == 1 ? 2 : 4];
-  auto load = [&](int64_t r0) {
+// The rows of a step from p on, `left` of them in the matrix, ld bytes apart,
+// `row` bytes of a row readable: what lies beyond reads as zero, so neither the
+// last rows nor the last tile's columns need a branch (columns beyond the
+// matrix only reach sums that are not stored).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const char* p, int left, int ld, int row) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, left > 0 ? (left - 1) * ld + max(row, 0) : 0,
+                                           0x00020000);
+}
+__device__ __forceinline__ int rows_left(const WArgs& a, int64_t r0) {
+  return (int)min((int64_t)kStep, (int64_t)a.N - r0);
+}
+
+// One group of 128 columns of x: four columns of eight rows a lane.
+struct XLoad {
+  uint32_t w[8], e[8];
+  __device__ __forceinline__ void load(const WArgs& a, int64_t r0, int k0, int quad, int oct) {
+    // (a row of codes is whole groups)
+    const int left = rows_left(a, r0), groups = (a.K - k0 + EMB_SAVED_GROUP - 1) / EMB_SAVED_GROUP;
+    const auto rx = rows_at(a.x + r0 * a.ld_x + k0, left, (int)a.ld_x, groups * EMB_SAVED_GROUP);
+    const auto re = rows_at(reinterpret_cast<const char*>(a.exps) + r0 * a.ld_e + k0 / EMB_SAVED_GROUP, left, (int)a.ld_e,
+                            groups);
+    const int at = 8 * oct * (int)a.ld_x + 4 * quad, ae = 8 * oct * (int)a.ld_e + 4 * quad / EMB_SAVED_GROUP;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int64_t r = r0 + 8 * oct + i;
-      const bool ok = r < r_end;
-      xr[i] = ok && k_in ? *reinterpret_cast<const uint32_t*>(a.x + r * a.ld_x + kx) : 0u;
-      er[i] = ok && k_in ? a.exps[r * a.ld_e + kx / EMB_SAVED_GROUP] : 0u;
-      const char* q = a.dy + r * a.ld_dy + (int64_t)cy * (SPLIT == 1 ? 2 : 4);
-      if constexpr (SPLIT == 1) {
-        yr[i][0] = yr[i][1] = 0u;
-        if (ok && a.aligned && cy + 4 <= a.F) {
-          const u32x2 t = *reinterpret_cast<const u32x2*>(q);
-          yr[i][0] = t.x, yr[i][1] = t.y;
-        } else if (ok) {
-          const uint16_t* h = reinterpret_cast<const uint16_t*>(q);
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (cy + j < a.F) yr[i][j / 2] |= (uint32_t)h[j] << (16 * (j % 2));
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) yr[i][j] = 0u;
-        if (ok && a.aligned && cy + 4 <= a.F) {
-          const u32x4 t = *reinterpret_cast<const u32x4*>(q);
-          yr[i][0] = t.x, yr[i][1] = t.y, yr[i][2] = t.z, yr[i][3] = t.w;
-        } else if (ok) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (cy + j < a.F) yr[i][j] = reinterpret_cast<const uint32_t*>(q)[j];
-        }
-      }
+      w[i] = __builtin_amdgcn_raw_buffer_load_b32(rx, at + i * (int)a.ld_x, 0, 0);
+      e[i] = __builtin_amdgcn_raw_buffer_load_b8(re, ae + i * (int)a.ld_e, 0, 0);
     }
-  };
-  auto put = [&]() {
-    // x: columns j of rows 2i and 2i + 1 to one word each
+  }
+  __device__ __forceinline__ void put(u32x4* lds, int quad) const {
     uint32_t o[4][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float u0 = __uint_as_float(er[2 * i] << 23), u1 = __uint_as_float(er[2 * i + 1] << 23);
+      // (exponent 255: the codes are zeros, and zero times infinity is NaN)
+      const float u0 = __uint_as_float((e[2 * i] & 0xffu) << 23), u1 = __uint_as_float((e[2 * i + 1] & 0xffu) << 23);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float v0 = (float)(int8_t)(xr[2 * i] >> (8 * j)) * u0, v1 = (float)(int8_t)(xr[2 * i + 1] >> (8 * j)) * u1;
+        const float v0 = (float)(int8_t)(w[2 * i] >> (8 * j)) * u0, v1 = (float)(int8_t)(w[2 * i + 1] >> (8 * j)) * u1;
         o[j][i] = halves_hi(__float_as_uint(v0), __float_as_uint(v1));
       }
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) s_x[oct][4 * quad + j] = u32x4{o[j][0], o[j][1], o[j][2], o[j][3]};
+    for (int j = 0; j < 4; ++j) lds[32 * j + quad] = u32x4{o[j][0], o[j][1], o[j][2], o[j][3]};
+  }
+};
+
+// One group of 128 columns of dy.  SPLIT 1: bf16; 3: fp32 in three parts, whose
+// groups lie `apart` 16-byte words from one another.
+template <int SPLIT, bool PAIRS>
+struct YLoad {
+  static constexpr int kWords = SPLIT == 1 ? 2 : 4;
+  uint32_t w[8][kWords];
+  __device__ __forceinline__ void load(const WArgs& a, int64_t r0, int c0, int quad, int oct) {
+    constexpr int kSize = SPLIT == 1 ? 2 : 4;
+    // (an odd last column's word is read whole)
+    const auto ry = rows_at(a.dy + r0 * a.ld_dy + (int64_t)c0 * kSize, rows_left(a, r0), (int)a.ld_dy,
+                            PAIRS ? ((a.F - c0) * kSize + 3) & ~3 : (a.F - c0) * kSize);
+    const int at = 8 * oct * (int)a.ld_dy + 4 * kSize * quad;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int row = at + i * (int)a.ld_dy;
+      if constexpr (SPLIT == 3) {
+        const u32x4 t = __builtin_amdgcn_raw_buffer_load_b128(ry, row, 0, 0);
+        w[i][0] = t.x, w[i][1] = t.y, w[i][2] = t.z, w[i][3] = t.w;
+      } else if constexpr (PAIRS) {
+        const u32x2 t = __builtin_amdgcn_raw_buffer_load_b64(ry, row, 0, 0);
+        w[i][0] = t.x, w[i][1] = t.y;
+      } else {
+        // rows or values that are not aligned to words
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          w[i][j] = (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(ry, row + 4 * j, 0, 0) |
+                    (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(ry, row + 4 * j + 2, 0, 0) << 16;
+      }
+    }
+  }
+  __device__ __forceinline__ void put(u32x4* lds, int apart, int quad) const {
     if constexpr (SPLIT == 1) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        uint32_t w[4];
+        uint32_t o[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          w[i] = j % 2 ? halves_hi(yr[2 * i][j / 2], yr[2 * i + 1][j / 2]) : halves_lo(yr[2 * i][j / 2], yr[2 * i + 1][j / 2]);
-        s_y[0][oct][4 * quad + j] = u32x4{w[0], w[1], w[2], w[3]};
+          o[i] = j % 2 ? halves_hi(w[2 * i][j / 2], w[2 * i + 1][j / 2]) : halves_lo(w[2 * i][j / 2], w[2 * i + 1][j / 2]);
+        lds[32 * j + quad] = u32x4{o[0], o[1], o[2], o[3]};
       }
     } else {
       // v = p0 + p1 + p2: each part the leading 8 bits of what the parts before it leave (cut off, so every
@@ -114,13 +135,13 @@ __global__ __launch_bounds__(kThreads) void k_weight_grad(WArgs a) {
       for (int j = 0; j < 4; ++j) {
         float v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(yr[i][j]);
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i][j]);
 #pragma unroll
         for (int p = 0; p < SPLIT; ++p) {
-          uint32_t w[4];
+          uint32_t o[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = halves_hi(__float_as_uint(v[2 * i]), __float_as_uint(v[2 * i + 1]));
-          s_y[p][oct][4 * quad + j] = u32x4{w[0], w[1], w[2], w[3]};
+          for (int i = 0; i < 4; ++i) o[i] = halves_hi(__float_as_uint(v[2 * i]), __float_as_uint(v[2 * i + 1]));
+          lds[p * apart + 32 * j + quad] = u32x4{o[0], o[1], o[2], o[3]};
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const uint32_t u = __float_as_uint(v[i]);
@@ -129,44 +150,141 @@ __global__ __launch_bounds__(kThreads) void k_weight_grad(WArgs a) {
         }
       }
     }
+  }
+};
+
+// G groups of 128 columns each way a block, four wavefronts as 2 x 2; S slices
+// of a group each way a wavefront (G 2: a group, S 4; G 1: half of one, S 2).
+template <int G, int SPLIT, bool PAIRS>
+__global__ __launch_bounds__(kThreads, G == 2 ? 1 : 2) void k_weight_grad(WArgs a) {
+  constexpr int S = 2 * G, kTile = kGroup * G, kBufs = SPLIT == 1 ? 2 : 1;
+  constexpr int kApart = kOct * G * kGroup;
+  __shared__ u32x4 s_x[kBufs][kOct][G * kGroup], s_y[kBufs][SPLIT][kOct][G * kGroup];
+  const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
+  const int tiles = a.tiles_k * a.tiles_f;
+  const int tile = blockIdx.x % tiles, part = blockIdx.x / tiles;
+  const int k0 = tile % a.tiles_k * kTile, c0 = tile / a.tiles_k * kTile;
+  const int quad = threadIdx.x % 32, oct = threadIdx.x / 32;
+  const int64_t r_begin = (int64_t)part * a.steps_per_part * kStep;
+  const int64_t r_end = min((int64_t)a.N, r_begin + (int64_t)a.steps_per_part * kStep);
+  f32x16 acc[S][S] = {};
+  const int wk = (wave & 1) * 32 * S, wc = (wave >> 1) * 32 * S;
+  XLoad x[G];
+  YLoad<SPLIT, PAIRS> y[G];
+  auto load = [&](int64_t r0) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      x[g].load(a, r0, k0 + g * kGroup, quad, oct);
+      y[g].load(a, r0, c0 + g * kGroup, quad, oct);
+    }
   };
-  if (r_begin < r_end) load(r_begin);
-  for (int64_t r0 = r_begin; r0 < r_end; r0 += kStep) {
-    __syncthreads();
-    put();
-    __syncthreads();
-    if (r0 + kStep < r_end) load(r0 + kStep);
-    // 16 rows an instruction: lane l holds column l % 32, rows 8 * (l / 32) .. of the 16
+  // a quarter of a step: 16 rows, of which lane l holds 8 * (l / 32) ..
+  bf16x8 fx[2][S], fy[2][S];
+  auto fetch = [&](int buf, int n, int p, int to) {
+    const int o = 2 * n + lane / 32, c = lane % 32;
+    if (p == 0) {
 #pragma unroll
-    for (int g = 0; g < kOct / 2; ++g) {
-      const int o = 2 * g + lane / 32, c = lane % 32;
-      bf16x8 fx[2], fy[2];
+      for (int i = 0; i < S; ++i) fx[to][i] = __builtin_bit_cast(bf16x8, s_x[buf][o][wk + 32 * i + c]);
+    }
 #pragma unroll
-      for (int i = 0; i < 2; ++i) fx[i] = __builtin_bit_cast(bf16x8, s_x[o][wk + 32 * i + c]);
+    for (int i = 0; i < S; ++i) fy[to][i] = __builtin_bit_cast(bf16x8, s_y[buf][p][o][wc + 32 * i + c]);
+  };
+  auto sum = [&](int xs, int ys) {
 #pragma unroll
-      for (int p = 0; p < SPLIT; ++p) {
+    for (int i = 0; i < S; ++i)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) fy[i] = __builtin_bit_cast(bf16x8, s_y[p][o][wc + 32 * i + c]);
+      for (int j = 0; j < S; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[xs][i], fy[ys][j], acc[i][j], 0, 0, 0);
+  };
+  if (r_begin < r_end) {
+    load(r_begin);
+    if constexpr (kBufs == 1) {
+      for (int64_t r0 = r_begin; r0 < r_end; r0 += kStep) {
+        __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int g = 0; g < G; ++g) {
+          x[g].put(&s_x[0][oct][g * kGroup], quad);
+          y[g].put(&s_y[0][0][oct][g * kGroup], kApart, quad);
+        }
+        __syncthreads();
+        if (r0 + kStep < r_end) load(r0 + kStep);
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[i], fy[j], acc[i][j], 0, 0, 0);
+        for (int n = 0; n < 4; ++n) {
+#pragma unroll
+          for (int p = 0; p < SPLIT; ++p) {
+            fetch(0, n, p, 0);
+            sum(0, 0);
+          }
+        }
+      }
+    } else {
+      // two buffers: a step's values go to LDS while the step before them is summed, and are loaded a step earlier
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        x[g].put(&s_x[0][oct][g * kGroup], quad);
+        y[g].put(&s_y[0][0][oct][g * kGroup], kApart, quad);
+      }
+      load(r_begin + kStep);  // (rows past the end read as zeros)
+      __syncthreads();
+      int buf = 0;
+      for (int64_t r0 = r_begin; r0 < r_end; r0 += kStep) {
+        fetch(buf, 0, 0, 0);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          if (n < 3) fetch(buf, n + 1, 0, (n + 1) & 1);
+          sum(n & 1, n & 1);
+          const int g = n / 2;
+          if (g < G) {
+            if (n % 2 == 0) {
+              x[g].put(&s_x[buf ^ 1][oct][g * kGroup], quad);
+              x[g].load(a, r0 + 2 * kStep, k0 + g * kGroup, quad, oct);
+            } else {
+              y[g].put(&s_y[buf ^ 1][0][oct][g * kGroup], kApart, quad);
+              y[g].load(a, r0 + 2 * kStep, c0 + g * kGroup, quad, oct);
+            }
+          }
+          // the matrix unit takes 32 cycles an instruction: what else there is to do goes between
+          if constexpr (G == 2) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);  // LDS reads
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // one product
+              __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);  // vector instructions
+              if (i % 3 == 2) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);  // an LDS write
+              __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);  // a load
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+        __syncthreads();
+        buf ^= 1;
       }
     }
   }
+  // slice i of a group holds columns 4 q + i: a wavefront's slices begin at slice (wk / 32) % 4 of group wk / 128
   float* out = a.out + (a.parts > 1 ? (int64_t)part * a.K * a.F : 0);
+  const int kb = k0 + wk / kGroup * kGroup + wk / 32 % 4, cb = c0 + wc / kGroup * kGroup + wc / 32 % 4 + 4 * (lane % 32);
+  const bool add = a.parts == 1 && a.add;
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int v = 0; v < 16; ++v) {
+    const int q = 8 * (v / 4) + 4 * (lane / 32) + v % 4;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int i = 0; i < S; ++i) {
+      const int k = kb + 4 * q + i;
+      if (k >= a.K) continue;
+      float* d = out + (int64_t)k * a.F + cb;
+      float t[S];
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int k = k0 + wk + 32 * i + 8 * (v / 4) + 4 * (lane / 32) + v % 4, c = c0 + wc + 32 * j + lane % 32;
-        if (k >= a.K || c >= a.F) continue;
-        float* d = out + (int64_t)k * a.F + c;
-        *d = a.parts == 1 && a.add ? *d + acc[i][j][v] : acc[i][j][v];
+      for (int j = 0; j < S; ++j) t[j] = acc[i][j][v];
+      if (!add && cb + S <= a.F && a.F % S == 0) {
+        Vec<float, S>::store(d, t);
+      } else {
+#pragma unroll
+        for (int j = 0; j < S; ++j)
+          if (cb + j < a.F) d[j] = add ? d[j] + t[j] : t[j];
       }
+    }
+  }
 }
 
 __global__ __launch_bounds__(256) void k_weight_parts(const float* parts, float* dw, int64_t n, int count, int add) {
@@ -177,20 +295,31 @@ __global__ __launch_bounds__(256) void k_weight_parts(const float* parts, float*
   }
 }
 
-// Parts the rows are cut into: as many as give each compute unit a block or
-// two, of at least four steps each.
-int part_count(int64_t N, int32_t K, int32_t F) {
-  const int64_t tiles = (int64_t)((K + kTile - 1) / kTile) * ((F + kTile - 1) / kTile);
+struct Plan {
+  int groups, parts, steps;  // groups of 128 columns a tile has each way; parts of so many steps
+};
+Plan plan_for(int64_t N, int32_t K, int32_t F, bool small) {
   const int64_t steps = (N + kStep - 1) / kStep;
-  int64_t p = 512 / tiles;
-  if (p > steps / 4) p = steps / 4;
-  return (int)(p < 1 ? 1 : p);
+  auto cut = [&](int64_t tile, int64_t blocks, int64_t least) {
+    const int64_t tiles = ((K + tile - 1) / tile) * ((F + tile - 1) / tile);
+    int64_t p = blocks / tiles;
+    if (p > steps / least) p = steps / least;
+    if (p < 1) p = 1;
+    const int64_t per = (steps + p - 1) / p;
+    return Plan{(int)(tile / kGroup), (int)(per > 0 ? (steps + per - 1) / per : 1), (int)per};
+  };
+  const Plan big = cut(2 * kGroup, 256, 16);
+  const int64_t tiles = (int64_t)((K + 255) / 256) * ((F + 255) / 256);
+  if (!small && big.parts * tiles >= 128) return big;
+  Plan s = cut(kGroup, 512, 4);
+  if (s.parts < 1) s.parts = 1;
+  return s;
 }
 
 }  // namespace
 
 size_t weight_grad_ws_bytes(int64_t N, int32_t K, int32_t F) {
-  const int p = part_count(N, K, F);
+  const int a = plan_for(N, K, F, false).parts, b = plan_for(N, K, F, true).parts, p = a > b ? a : b;
   return p > 1 ? align256(sizeof(float) * (size_t)p * (size_t)K * (size_t)F) : 0;
 }
 
@@ -206,16 +335,18 @@ hipError_t launch_weight_grad(const WeightGradLaunch& p, hipStream_t s) {
   a.K = p.K;
   a.F = p.F;
   a.add = p.add;
-  a.aligned = p.aligned;
-  a.parts = part_count(p.N, p.K, p.F);
-  const int64_t steps = (p.N + kStep - 1) / kStep;
-  a.steps_per_part = (int32_t)((steps + a.parts - 1) / a.parts);
-  a.tiles_k = (p.K + kTile - 1) / kTile;
-  a.tiles_f = (p.F + kTile - 1) / kTile;
+  const Plan pl = plan_for(p.N, p.K, p.F, p.dtype == EMB_FP32 || !p.aligned);
+  const int tile = pl.groups * kGroup;
+  a.parts = pl.parts < 1 ? 1 : pl.parts;
+  a.steps_per_part = pl.steps;
+  a.tiles_k = (p.K + tile - 1) / tile;
+  a.tiles_f = (p.F + tile - 1) / tile;
   a.out = a.parts > 1 ? p.ws : p.dw;
   const unsigned blocks = (unsigned)(a.tiles_k * a.tiles_f * a.parts);
-  if (p.dtype == EMB_BF16) k_weight_grad<1><<<blocks, kThreads, 0, s>>>(a);
-  else k_weight_grad<3><<<blocks, kThreads, 0, s>>>(a);
+  if (p.dtype == EMB_FP32) k_weight_grad<1, 3, true><<<blocks, kThreads, 0, s>>>(a);
+  else if (!p.aligned) k_weight_grad<1, 1, false><<<blocks, kThreads, 0, s>>>(a);
+  else if (pl.groups == 2) k_weight_grad<2, 1, true><<<blocks, kThreads, 0, s>>>(a);
+  else k_weight_grad<1, 1, true><<<blocks, kThreads, 0, s>>>(a);
   if (a.parts > 1) {
     const int64_t n = (int64_t)p.K * p.F;
     k_weight_parts<<<(unsigned)((n + 255) / 256 < 4096 ? (n + 255) / 256 : 4096), 256, 0, s>>>(p.ws, p.dw, n, a.parts,
