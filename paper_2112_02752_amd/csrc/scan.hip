@@ -3,18 +3,24 @@
 //   a_t = sigmoid(f_t + bias),  h_t = a_t h_{t-1} + (1 - a_t) x_t,  y_t = sigmoid(o_t) h_t
 //
 // Steps h -> a h + b compose: (A1, B1) then (A2, B2) is (A1 A2, A2 B1 + B2), so
-// the positions are cut into spans of 64, whatever sequences they belong to (a
+// the positions are cut into spans, whatever sequences they belong to (a
 // sequence's first position discards what came before it).  A block takes one
-// span of 64 or 128 columns: each wavefront holds a part of the span's
-// positions in registers, a lane one or two columns, and the parts are joined
-// through LDS.  With more than one span:
-//   k_scan_sums   each span's (A, B) from zero
-//   k_scan_carry  the state before each span (16 wavefronts share the spans of
-//                 64 columns)
-//   k_scan_fwd    the span again, from its state
-// The backward is the same scan from the last position to the first on
+// span of 64 or 128 columns (a slice): each wavefront holds its part of the
+// span's positions in registers, a lane one or two columns, and the parts are
+// joined through LDS.  Every value is read and written once: a block publishes
+// its span's (A, B), then takes what enters the span from the spans before it,
+// and publishes what leaves it:
+//  - blocks take their span's number from a counter of the slice, so a span's
+//    block waits for blocks that have started before it, and every wait ends;
+//  - it looks at the 32 spans before it at once, and starts from the nearest
+//    whose outgoing state is known, through the (A, B) of those after that one:
+//    the same steps in the same order wherever it starts, so results do not
+//    depend on timing;
+//  - published words are stored and read at device scope, a flag after the
+//    words it announces; flags and counters are cleared by a kernel before.
+// The backward is the same from the last position to the first on
 // dh_t = sigmoid(o_t) dy_t + a_{t+1} dh_{t+1}, with h recomputed inside each
-// span from the state the forward kept.
+// span of 64 from the state the forward kept.
 //
 // A span that holds a first position passes nothing on of what it receives:
 // its A is kResets, not a product with zero, which would carry an infinity or
@@ -26,9 +32,12 @@ namespace emb {
 namespace {
 
 constexpr float kResets = -1.0f;  // (products of a's are never negative)
-constexpr int kP = 16;            // positions a wavefront holds
-constexpr int kW = kSpan / kP;    // wavefronts of a block
+constexpr int kW = 8;             // wavefronts of a block
 constexpr int kThreads = kW * kWave;
+constexpr int kFwdP = 16;         // positions a wavefront holds: spans of 128 forward,
+constexpr int kBackP = kSpan / kW;  // of 64 (the kept states') backward
+constexpr int kFwdSpan = kFwdP * kW;
+constexpr int kLook = 32;         // spans a block looks back at
 
 struct Saved8 {};
 
@@ -37,7 +46,8 @@ template <typename T, int V>
 struct In {
   Vec<T, V> v;
   __device__ __forceinline__ void load(const Rows& m, int64_t row, int col) {
-    v.load(m.p + row * m.ld + (int64_t)col * (Vec<T, V>::kBytes / V));
+    // (the row is the wavefront's, the column a lane's 32-bit offset)
+    v.load(m.p + row * m.ld + (uint32_t)col * (uint32_t)(Vec<T, V>::kBytes / V));
   }
   __device__ __forceinline__ float get(int i) const { return v.get(i); }
 };
@@ -45,10 +55,10 @@ template <int V>
 struct In<Saved8, V> {
   uint32_t codes, e;
   __device__ __forceinline__ void load(const Rows& m, int64_t row, int col) {
-    const char* p = m.p + row * m.ld + col;
+    const char* p = m.p + row * m.ld + (uint32_t)col;
     if constexpr (V == 1) codes = *reinterpret_cast<const uint8_t*>(p);
     else codes = *reinterpret_cast<const uint16_t*>(p);
-    e = m.exps[row * m.ld_exps + col / EMB_SAVED_GROUP];
+    e = (m.exps + row * m.ld_exps)[(uint32_t)col / EMB_SAVED_GROUP];
   }
   // (exponent 255: the codes are zeros, and zero times infinity is NaN)
   __device__ __forceinline__ float get(int i) const {
@@ -59,7 +69,7 @@ struct In<Saved8, V> {
 // sigmoid(z) and sigmoid(-z), the latter without cancellation; NaN stays NaN
 __device__ __forceinline__ void forget(float z, float& a, float& q) {
   float t = -1.44269504f * z;
-  t = t > 126.f ? 126.f : t;
+  t = __builtin_elementwise_minimum(t, 126.f);
   const float e = __builtin_amdgcn_exp2f(t);
   a = __builtin_amdgcn_rcpf(1.f + e);
   q = e * a;
@@ -76,44 +86,175 @@ __device__ __forceinline__ float through(float A, float B, float h) {
 struct Scan {
   const int32_t* offsets;
   Rows x, f, o, y, dy, dx, df, dO;
-  const float *bias, *h0, *states, *dh_last;
-  float *h_last, *dh0, *dbias;  // dbias: [spans][D], one row a span
-  float *A, *B;                 // [spans][D]
-  float* carry;                 // [spans][D]: what enters each span
+  const float *bias, *h0, *dh_last;
+  float *states, *h_last, *dh0, *dbias;  // dbias: [spans][D], one row a span
   int32_t N, M, D, spans, slices;
+  // what spans publish, by (span in the order they are taken, slice)
+  uint32_t* taken;  // [slices]
+  uint32_t* flags;  // [slices][spans]
+  uint64_t* steps;  // [spans][slices][V * 64]: A and B
+  uint32_t* out;    // [spans][slices][V * 64]: the state that leaves the span
 };
+enum Flag : uint32_t { kNothing = 0, kSteps = 1, kOut = 2 };
 
-// First and last positions of sequences among a wavefront's kP positions from
-// q0 on, and the sequence of each.
+// First and last positions of sequences among a wavefront's P positions from
+// q0 on, and the sequence of each.  Offsets are read by scalar loads, which do
+// not wait behind the vector loads of the positions' values.
+template <int P>
 struct Marks {
   uint32_t starts;  // bit t: position q0 + t is its sequence's first
   uint32_t ends;    // bit t: position q0 + t is its sequence's last
   int seq;          // lane t: the sequence of position q0 + t
   __device__ __forceinline__ Marks(const Scan& a, int q0, int lane) {
-    const int m = min(max(wave_upper_bound<int32_t>(a.offsets, a.M + 1, q0, lane) - 1, 0), a.M - 1);
-    // the next 64 offsets, one a lane; more only where sequences of no positions fill them
-    int v = a.offsets[min(m + 1 + lane, a.M)], at = m + 1;
-    uint32_t s = uniform(a.offsets[m]) == q0 ? 1u : 0u;
-    seq = m;
-    for (;;) {
-#pragma unroll
-      for (int t = 0; t <= kP; ++t) {
-        const uint64_t upto = __ballot(v <= q0 + t && at + lane < a.M);
-        seq += lane == t ? __popcll(upto) : 0;
-        if (t > 0) s |= __ballot(v == q0 + t) ? 1u << t : 0u;
-      }
-      if (at + kWave > a.M || lane_at(v, kWave - 1) > q0 + kP) break;
-      at += kWave;
-      v = a.offsets[min(at + lane, a.M)];
+    const auto* off = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)a.offsets;
+    // the last sequence that begins at or before q0
+    int m = 0, n = a.M;
+    while (n > 1) {
+      const int half = n / 2;
+      const bool up = off[m + half] <= q0;
+      m = up ? m + half : m;
+      n = up ? n - half : half;
     }
-    starts = s & ((1u << kP) - 1u);
+    seq = m;
+    uint32_t s = off[m] == q0 ? 1u : 0u;
+    for (int k = m + 1; k <= a.M; ++k) {
+      const int t = off[k] - q0;
+      if (t > P) break;
+      s |= 1u << t;
+      if (k < a.M && lane >= t) seq = k;
+    }
+    starts = s & ((1u << P) - 1u);
     ends = s >> 1;
-    if (a.N - q0 <= kP) ends |= 1u << (a.N - q0 - 1);
+    if (a.N - q0 <= P) ends |= 1u << (a.N - q0 - 1);
   }
   __device__ __forceinline__ bool start(int t) const { return (starts >> t) & 1u; }
   __device__ __forceinline__ bool end(int t) const { return (ends >> t) & 1u; }
+  // whether a sequence begins at or before t, or ends at or after it, within the wavefront's positions
+  __device__ __forceinline__ bool begun(int t) const { return (starts & ((2u << t) - 1u)) != 0u; }
+  __device__ __forceinline__ bool closed(int t) const { return (ends >> t) != 0u; }
   __device__ __forceinline__ int of(int t) const { return lane_at(seq, t); }
 };
+
+// V values of a row of the sequences' states
+template <int V>
+__device__ __forceinline__ void store_f32(float* p, bool in, const float (&v)[V]) {
+  if (in) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) p[i] = v[i];
+  }
+}
+
+// ---------------------------------------------------------------- the spans' chain
+
+__device__ __forceinline__ void publish_flag(uint32_t* flag, Flag value, int lane) {
+  // the words before it have reached the device's memory
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  if (lane == 0) __hip_atomic_store(flag, (uint32_t)value, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint32_t ld_u32(const uint32_t* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+template <int V>
+struct Chain {
+  static constexpr int kCols = V * kWave;
+  uint32_t* flags;  // of the slice
+  uint64_t* steps;
+  uint32_t* out;
+  int64_t apart;    // words from one span's to the next's
+  int idx;          // this block's place among the slice's spans
+  __device__ __forceinline__ Chain(const Scan& a, int slice, int span) {
+    flags = a.flags + (int64_t)slice * a.spans;
+    apart = (int64_t)a.slices * kCols;
+    steps = a.steps + (int64_t)slice * kCols;
+    out = a.out + (int64_t)slice * kCols;
+    idx = span;
+  }
+  __device__ __forceinline__ void publish_steps(const float (&A)[V], const float (&B)[V], int lane) const {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      st_u64(steps + idx * apart + i * kWave + lane, ((uint64_t)__float_as_uint(A[i]) << 32) | __float_as_uint(B[i]));
+    publish_flag(flags + idx, kSteps, lane);
+  }
+  __device__ __forceinline__ void publish_out(const float (&h)[V], int lane) const {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      __hip_atomic_store(out + idx * apart + i * kWave + lane, __float_as_uint(h[i]), __ATOMIC_RELAXED,
+                         __HIP_MEMORY_SCOPE_AGENT);
+    publish_flag(flags + idx, kOut, lane);
+  }
+};
+
+// What a block gathers of the spans before its own.
+template <int V>
+struct Look {
+  uint64_t steps[kLook][V * kWave];
+  float out[V * kWave];
+  int from;  // the span whose outgoing state is known, counted back
+};
+
+// The state that enters span idx.  One wavefront waits until the outgoing state
+// of one of the 32 spans before it and the steps of those after that one are
+// published (a span before the first counts as one whose state is zero); then
+// all fetch a share of the steps, and apply them in order.
+template <int V>
+__device__ __forceinline__ void look_back(const Chain<V>& ch, Look<V>& lk, float (&h)[V], int wave, int lane) {
+  if (wave == kW - 1) {
+    const uint64_t t0 = wait_clock();
+    int j;
+    for (;;) {
+      const int at = ch.idx - 1 - lane;
+      const uint32_t flag = lane >= kLook ? (uint32_t)kNothing : (at >= 0 ? ld_u32(ch.flags + at) : (uint32_t)kOut);
+      const uint32_t known = (uint32_t)__ballot(flag == kOut), some = (uint32_t)__ballot(flag != kNothing);
+      j = known ? __builtin_ctz(known) : kLook;
+      if (known && (~some & ((1u << j) - 1u)) == 0u) break;
+      // (not reached: the blocks waited for are running; two seconds are no healthy wait)
+      if (wait_clock() - t0 > 200000000ull) {
+        j = -1;
+        break;
+      }
+      __builtin_amdgcn_s_sleep(1);
+    }
+    if (lane == 0) lk.from = j;
+  }
+  __syncthreads();
+  const int j = uniform(lk.from);
+#pragma unroll
+  for (int r = 0; r < kLook / kW; ++r) {
+    const int k = wave + r * kW;
+    if (k < j) {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        lk.steps[k][i * kWave + lane] = ld_relaxed_u64(ch.steps + (ch.idx - 1 - k) * ch.apart + i * kWave + lane);
+    }
+  }
+  if (wave == kW - 1) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      uint32_t w = j < 0 ? 0x7fc00000u : 0u;
+      if (j >= 0 && ch.idx - 1 - j >= 0) w = ld_u32(ch.out + (ch.idx - 1 - j) * ch.apart + i * kWave + lane);
+      lk.out[i * kWave + lane] = __uint_as_float(w);
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < V; ++i) h[i] = lk.out[i * kWave + lane];
+#pragma unroll 4
+  for (int k = j - 1; k >= 0; --k) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const uint64_t w = lk.steps[k][i * kWave + lane];
+      h[i] = through(__uint_as_float((uint32_t)(w >> 32)), __uint_as_float((uint32_t)w), h[i]);
+    }
+  }
+}
+
+// this block's span among its slice's, in the order the blocks start
+__device__ __forceinline__ int take(uint32_t* counter, int* s) {
+  if (threadIdx.x == 0) *s = (int)atomic_add_u32(counter, 1u);
+  __syncthreads();
+  return uniform(*s);
+}
 
 template <int V>
 __device__ __forceinline__ void load_f32(const float* p, int col, float (&v)[V]) {
@@ -123,12 +264,12 @@ __device__ __forceinline__ void load_f32(const float* p, int col, float (&v)[V])
 
 // ---------------------------------------------------------------- forward
 
-// FULL: from the span's state, with outputs; else the span's sums alone
-template <typename T, int V, bool GATED, bool FULL>
-__global__ __launch_bounds__(kThreads) void k_scan_fwd(Scan a) {
+template <typename T, int V, bool GATED>
+__global__ __launch_bounds__(kThreads, 4) void k_scan_fwd(Scan a) {
+  constexpr int P = kFwdP;
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
   const int main_blocks = a.spans * a.slices;
-  if (FULL && (int)blockIdx.x >= main_blocks) {
+  if ((int)blockIdx.x >= main_blocks) {
     // sequences of no positions keep their first state
     const int m0 = ((int)blockIdx.x - main_blocks) * kWave;
     for (int m = m0 + wave; m < min(a.M, m0 + kWave); m += kW) {
@@ -138,41 +279,34 @@ __global__ __launch_bounds__(kThreads) void k_scan_fwd(Scan a) {
     }
     return;
   }
-  const int c = blockIdx.x / a.slices, col0 = ((int)blockIdx.x % a.slices * kWave + lane) * V;
+  __shared__ float s_A[kW][V * kWave], s_B[kW][V * kWave];
+  __shared__ Look<V> s_look;
+  __shared__ int s_take, s_first;
+  const int slice = (int)blockIdx.x % a.slices;
+  const int c = a.spans > 1 ? take(a.taken + slice, &s_take) : 0;
+  const int col0 = (slice * kWave + lane) * V;
   const bool in = col0 < a.D;
   const int col = in ? col0 : 0;
-  const int q0 = c * kSpan + wave * kP;
-  const int n = min(kP, a.N - q0);  // (0 or less: this wavefront has no positions)
-  __shared__ float s_A[kW][V * kWave], s_B[kW][V * kWave];
-  float A[V], B[V], fa[kP][V], fb[kP][V];
-  In<T, V> go[GATED ? kP : 1];
+  const int q0 = c * kFwdSpan + wave * P;
+  const int n = min(P, a.N - q0);  // (0 or less: this wavefront has no positions)
+  // the state after position t is At[t] times the one that enters the wavefront's positions plus Bt[t]
+  float A[V], B[V], At[P][V], Bt[P][V], Ae[V], Be[V], bias[V];
+  In<T, V> gx[P], gf[P], go[GATED ? P : 1];
 #pragma unroll
-  for (int i = 0; i < V; ++i) A[i] = 1.f, B[i] = 0.f;
-  Marks mk(a, min(q0, a.N - 1), lane);
+  for (int i = 0; i < V; ++i) A[i] = 1.f, B[i] = Ae[i] = Be[i] = 0.f;
+#pragma unroll
+  for (int t = 0; t < P; ++t) {
+    const int64_t row = min(q0 + t, a.N - 1);
+    gx[t].load(a.x, row, col);
+    gf[t].load(a.f, row, col);
+    if constexpr (GATED) go[t].load(a.o, row, col);
+  }
+  const Marks<P> mk(a, min(q0, a.N - 1), lane);
+  load_f32<V>(a.bias, col, bias);
   if (n > 0) {
-    In<T, V> gx[kP], gf[kP];
 #pragma unroll
-    for (int t = 0; t < kP; ++t) {
-      const int64_t row = min(q0 + t, a.N - 1);
-      gx[t].load(a.x, row, col);
-      gf[t].load(a.f, row, col);
-      if constexpr (FULL && GATED) go[t].load(a.o, row, col);
-    }
-    float bias[V];
-    load_f32<V>(a.bias, col, bias);
-#pragma unroll
-    for (int t = 0; t < kP; ++t) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        float q;
-        forget(gf[t].get(i) + bias[i], fa[t][i], q);
-        fb[t][i] = q * gx[t].get(i);
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < kP; ++t) {
-      if (t >= n) continue;
-      if (mk.start(t)) {
+    for (int t = 0; t < P; ++t) {
+      if (t < n && mk.start(t)) {
         float h0[V] = {};
         if (a.h0) load_f32<V>(a.h0 + (int64_t)mk.of(t) * a.D, col, h0);
 #pragma unroll
@@ -180,8 +314,21 @@ __global__ __launch_bounds__(kThreads) void k_scan_fwd(Scan a) {
       }
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        A[i] *= fa[t][i];
-        B[i] = __builtin_fmaf(fa[t][i], B[i], fb[t][i]);
+        float fa, fq;
+        forget(gf[t].get(i) + bias[i], fa, fq);
+        A[i] *= fa;
+        B[i] = __builtin_fmaf(fa, B[i], fq * gx[t].get(i));
+        At[t][i] = A[i];
+        Bt[t][i] = B[i];
+      }
+      if (a.h_last && t < n && mk.end(t)) {
+        if (mk.begun(t)) {
+          store_f32<V>(a.h_last + (int64_t)mk.of(t) * a.D + col, in, B);
+        } else {
+          // (the one sequence that came in: its state is not known yet)
+#pragma unroll
+          for (int i = 0; i < V; ++i) Ae[i] = A[i], Be[i] = B[i];
+        }
       }
     }
     if (mk.starts) {
@@ -194,186 +341,74 @@ __global__ __launch_bounds__(kThreads) void k_scan_fwd(Scan a) {
     s_A[wave][i * kWave + lane] = A[i];
     s_B[wave][i * kWave + lane] = B[i];
   }
+  if (threadIdx.x == 0) s_first = mk.start(0);
   __syncthreads();
-  if constexpr (!FULL) {
-    if (wave != 0) return;
+  const Chain<V> ch(a, slice, c);
+  const bool leads = a.spans > 1 && wave == 0 && c + 1 < a.spans;  // what leaves the span is to be published
+  bool resets = false;
+  if (leads) {
+    // the span's steps; past a first position they are its outgoing state
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
+    for (int w = 1; w < kW; ++w) {
 #pragma unroll
-      for (int w = 1; w < kW; ++w) {
+      for (int i = 0; i < V; ++i) {
         const float A2 = s_A[w][i * kWave + lane], B2 = s_B[w][i * kWave + lane];
         B[i] = through(A2, B2, B[i]);
         A[i] = A2 < 0.f || A[i] < 0.f ? kResets : A[i] * A2;
       }
-      if (in) {
-        a.A[(int64_t)c * a.D + col + i] = A[i];
-        a.B[(int64_t)c * a.D + col + i] = B[i];
-      }
     }
-  } else {
-    if (n <= 0) return;
-    float h[V];
-    load_f32<V>(c > 0 ? a.carry + (int64_t)c * a.D : nullptr, col, h);
-    for (int w = 0; w < wave; ++w) {
+    resets = uniform(A[0] < 0.f);
+    if (resets) ch.publish_out(B, lane);
+    else ch.publish_steps(A, B, lane);
+  }
+  // the output gates, while the spans before this one publish
+  if constexpr (GATED) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) h[i] = through(s_A[w][i * kWave + lane], s_B[w][i * kWave + lane], h[i]);
-    }
-#pragma unroll
-    for (int t = 0; t < kP; ++t) {
-      if (t >= n) continue;
-      if (mk.start(t)) {
-        float h0[V] = {};
-        if (a.h0) load_f32<V>(a.h0 + (int64_t)mk.of(t) * a.D, col, h0);
-#pragma unroll
-        for (int i = 0; i < V; ++i) h[i] = h0[i];
-      }
-      float y[V];
+    for (int t = 0; t < P; ++t) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        h[i] = __builtin_fmaf(fa[t][i], h[i], fb[t][i]);
-        y[i] = GATED ? gate(go[t].get(i)) * h[i] : h[i];
-      }
-      if (in) Vec<T, V>::store(a.y.p + (int64_t)(q0 + t) * a.y.ld + (int64_t)col * (Vec<T, V>::kBytes / V), y);
-      if (a.h_last && mk.end(t)) {
-        float* dst = a.h_last + (int64_t)mk.of(t) * a.D + col;
-        if (in) {
-#pragma unroll
-          for (int i = 0; i < V; ++i) dst[i] = h[i];
-        }
+        const float g = gate(go[t].get(i));
+        At[t][i] *= g;
+        Bt[t][i] *= g;
       }
     }
   }
-}
-
-// What enters each span, from the spans' sums: carry[c] = through(A, B of c - 1,
-// carry[c - 1]), or from the last span to the first.  A lane has one column;
-// 16 wavefronts share the spans: each joins its part, the parts are joined
-// through LDS, each goes over its part again.
-constexpr int kCarryWaves = 16;
-template <bool BACK>
-__global__ __launch_bounds__(kCarryWaves * kWave) void k_scan_carry(const float* A, const float* B, float* carry,
-                                                                    int spans, int D) {
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  const int col0 = blockIdx.x * kWave + lane;
-  const bool in = col0 < D;
-  const int64_t col = in ? col0 : 0;
-  __shared__ float s_A[kCarryWaves][kWave], s_B[kCarryWaves][kWave];
-  const int per = (spans + kCarryWaves - 1) / kCarryWaves;
-  const int first = wave * per, last = min(spans, first + per);
-  constexpr int kAhead = 8;
-  auto place = [&](int k) { return (int64_t)(BACK ? spans - 1 - k : k) * D + col; };
-  float a1 = 1.f, b1 = 0.f;
-  for (int k = first; k < last; k += kAhead) {
-    float x[kAhead], y[kAhead];
+  float h[V] = {};
+  if (a.spans > 1 && !s_first) {
+    look_back<V>(ch, s_look, h, wave, lane);
+    if (leads && !resets) {
+      float leaves[V];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int64_t at = place(min(k + i, last - 1));
-      x[i] = A[at], y[i] = B[at];
-    }
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      if (k + i >= last) break;
-      b1 = through(x[i], y[i], b1);
-      a1 = x[i] < 0.f || a1 < 0.f ? kResets : a1 * x[i];
+      for (int i = 0; i < V; ++i) leaves[i] = through(A[i], B[i], h[i]);
+      ch.publish_out(leaves, lane);
     }
   }
-  s_A[wave][lane] = a1;
-  s_B[wave][lane] = b1;
-  __syncthreads();
-  float h = 0.f;
-  for (int w = 0; w < wave; ++w) h = through(s_A[w][lane], s_B[w][lane], h);
-  for (int k = first; k < last; k += kAhead) {
-    float x[kAhead], y[kAhead];
+  if (n <= 0) return;
+  for (int w = 0; w < wave; ++w) {
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int64_t at = place(min(k + i, last - 1));
-      x[i] = A[at], y[i] = B[at];
-    }
+    for (int i = 0; i < V; ++i) h[i] = through(s_A[w][i * kWave + lane], s_B[w][i * kWave + lane], h[i]);
+  }
+  if (a.states && q0 % kSpan == 0) store_f32<V>(a.states + (int64_t)(q0 / kSpan) * a.D + col, in, h);
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      if (k + i >= last) break;
-      if (in) carry[place(k + i)] = h;
-      h = through(x[i], y[i], h);
+  for (int t = 0; t < P; ++t) {
+    if (t >= n) continue;
+    float y[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) y[i] = mk.begun(t) ? Bt[t][i] : __builtin_fmaf(At[t][i], h[i], Bt[t][i]);
+    if (in) Vec<T, V>::store(a.y.p + (int64_t)(q0 + t) * a.y.ld + (uint32_t)col * (uint32_t)(Vec<T, V>::kBytes / V), y);
+    if (a.h_last && mk.end(t) && !mk.begun(t)) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) y[i] = __builtin_fmaf(Ae[i], h[i], Be[i]);
+      store_f32<V>(a.h_last + (int64_t)mk.of(t) * a.D + col, in, y);
     }
   }
 }
 
 // ---------------------------------------------------------------- backward
 
-// The span's sums from its last position to its first: what position p0 - 1
-// receives, a_p0 dh_p0, as (A, B) of what position p1 - 1 receives.
 template <typename T, typename TG, int V, bool GATED>
-__global__ __launch_bounds__(kThreads) void k_scan_back_sums(Scan a) {
-  const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
-  const int c = blockIdx.x / a.slices, col0 = ((int)blockIdx.x % a.slices * kWave + lane) * V;
-  const bool in = col0 < a.D;
-  const int col = in ? col0 : 0;
-  const int q0 = c * kSpan + wave * kP;
-  const int n = min(kP, a.N - q0);
-  __shared__ float s_A[kW][V * kWave], s_B[kW][V * kWave];
-  float A[V], B[V];
-#pragma unroll
-  for (int i = 0; i < V; ++i) A[i] = 1.f, B[i] = 0.f;
-  Marks mk(a, min(q0, a.N - 1), lane);
-  if (n > 0) {
-    In<T, V> gf[kP], go[GATED ? kP : 1];
-    In<TG, V> gy[kP];
-#pragma unroll
-    for (int t = 0; t < kP; ++t) {
-      const int64_t row = min(q0 + t, a.N - 1);
-      gf[t].load(a.f, row, col);
-      gy[t].load(a.dy, row, col);
-      if constexpr (GATED) go[t].load(a.o, row, col);
-    }
-    float bias[V];
-    load_f32<V>(a.bias, col, bias);
-#pragma unroll
-    for (int t = kP - 1; t >= 0; --t) {
-      if (t >= n) continue;
-      if (mk.end(t)) {
-        float g[V] = {};
-        if (a.dh_last) load_f32<V>(a.dh_last + (int64_t)mk.of(t) * a.D, col, g);
-#pragma unroll
-        for (int i = 0; i < V; ++i) B[i] = g[i];
-      }
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        float fa, fq;
-        forget(gf[t].get(i) + bias[i], fa, fq);
-        const float u = GATED ? gate(go[t].get(i)) * gy[t].get(i) : gy[t].get(i);
-        A[i] *= fa;
-        B[i] = fa * (u + B[i]);
-      }
-    }
-    if (mk.ends) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) A[i] = kResets;
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    s_A[wave][i * kWave + lane] = A[i];
-    s_B[wave][i * kWave + lane] = B[i];
-  }
-  __syncthreads();
-  if (wave != kW - 1) return;
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-#pragma unroll
-    for (int w = kW - 2; w >= 0; --w) {
-      const float A2 = s_A[w][i * kWave + lane], B2 = s_B[w][i * kWave + lane];
-      B[i] = through(A2, B2, B[i]);
-      A[i] = A2 < 0.f || A[i] < 0.f ? kResets : A[i] * A2;
-    }
-    if (in) {
-      a.A[(int64_t)c * a.D + col + i] = A[i];
-      a.B[(int64_t)c * a.D + col + i] = B[i];
-    }
-  }
-}
-
-template <typename T, typename TG, int V, bool GATED>
-__global__ __launch_bounds__(kThreads) void k_scan_bwd(Scan a) {
+__global__ __launch_bounds__(kThreads, 4) void k_scan_bwd(Scan a) {
+  constexpr int P = kBackP;
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
   const int main_blocks = a.spans * a.slices;
   if ((int)blockIdx.x >= main_blocks) {
@@ -386,34 +421,56 @@ __global__ __launch_bounds__(kThreads) void k_scan_bwd(Scan a) {
     }
     return;
   }
-  const int c = blockIdx.x / a.slices, col0 = ((int)blockIdx.x % a.slices * kWave + lane) * V;
+  __shared__ float s_A[2][kW][V * kWave], s_B[2][kW][V * kWave];
+  __shared__ Look<V> s_look;
+  __shared__ int s_take, s_last;
+  const int slice = (int)blockIdx.x % a.slices;
+  const int taken = a.spans > 1 ? take(a.taken + slice, &s_take) : 0;
+  const int c = a.spans - 1 - taken;
+  const int col0 = (slice * kWave + lane) * V;
   const bool in = col0 < a.D;
   const int col = in ? col0 : 0;
-  const int q0 = c * kSpan + wave * kP;
-  const int n = min(kP, a.N - q0);
-  __shared__ float s_A[2][kW][V * kWave], s_B[2][kW][V * kWave];
-  float A[V], B[V], A2[V], B2[V], fa[kP][V], fq[kP][V];
-  In<T, V> gx[kP], go[GATED ? kP : 1];
-  In<TG, V> gy[kP];
+  const int q0 = c * kSpan + wave * P;
+  const int n = min(P, a.N - q0);
+  // fa, fq: a and 1 - a; u: the gradient that reaches the state through y; v: that of the output gate by the state.
+  // Then dh at position t is W times the gradient that enters the wavefront's positions plus U; fq and u become
+  // (1 - a) W and (1 - a) U, and r = (h before - x) a.
+  float A[V], B[V], A2[V], B2[V], state[V], bias[V], W0[V], U0[V];
+  float fa[P][V], fq[P][V], u[P][V], v[GATED ? P : 1][V], r[P][V];
+  In<T, V> gx[P];
 #pragma unroll
-  for (int i = 0; i < V; ++i) A[i] = A2[i] = 1.f, B[i] = B2[i] = 0.f;
-  Marks mk(a, min(q0, a.N - 1), lane);
-  if (n > 0) {
-    In<T, V> gf[kP];
+  for (int i = 0; i < V; ++i) A[i] = A2[i] = 1.f, B[i] = B2[i] = W0[i] = U0[i] = 0.f;
+  {
+    In<T, V> gf[P], go[GATED ? P : 1];
+    In<TG, V> gy[P];
 #pragma unroll
-    for (int t = 0; t < kP; ++t) {
+    for (int t = 0; t < P; ++t) {
       const int64_t row = min(q0 + t, a.N - 1);
-      gx[t].load(a.x, row, col);
       gf[t].load(a.f, row, col);
+      gx[t].load(a.x, row, col);
       gy[t].load(a.dy, row, col);
       if constexpr (GATED) go[t].load(a.o, row, col);
     }
-    float bias[V];
     load_f32<V>(a.bias, col, bias);
+    load_f32<V>(c > 0 ? a.states + (int64_t)c * a.D : nullptr, col, state);
 #pragma unroll
-    for (int t = 0; t < kP; ++t) {
+    for (int t = 0; t < P; ++t) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) forget(gf[t].get(i) + bias[i], fa[t][i], fq[t][i]);
+      for (int i = 0; i < V; ++i) {
+        forget(gf[t].get(i) + bias[i], fa[t][i], fq[t][i]);
+        u[t][i] = gy[t].get(i);
+        if constexpr (GATED) {
+          const float s = gate(go[t].get(i));
+          u[t][i] *= s;
+          v[t][i] = u[t][i] * (1.f - s);
+        }
+      }
+    }
+  }
+  const Marks<P> mk(a, min(q0, a.N - 1), lane);
+  if (n > 0) {
+#pragma unroll
+    for (int t = 0; t < P; ++t) {
       if (t >= n) continue;
       if (mk.start(t)) {
         float h0[V] = {};
@@ -428,7 +485,7 @@ __global__ __launch_bounds__(kThreads) void k_scan_bwd(Scan a) {
       }
     }
 #pragma unroll
-    for (int t = kP - 1; t >= 0; --t) {
+    for (int t = P - 1; t >= 0; --t) {
       if (t >= n) continue;
       if (mk.end(t)) {
         float g[V] = {};
@@ -438,9 +495,8 @@ __global__ __launch_bounds__(kThreads) void k_scan_bwd(Scan a) {
       }
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float u = GATED ? gate(go[t].get(i)) * gy[t].get(i) : gy[t].get(i);
         A2[i] *= fa[t][i];
-        B2[i] = fa[t][i] * (u + B2[i]);
+        B2[i] = fa[t][i] * (u[t][i] + B2[i]);
       }
     }
 #pragma unroll
@@ -456,74 +512,125 @@ __global__ __launch_bounds__(kThreads) void k_scan_bwd(Scan a) {
     s_A[1][wave][i * kWave + lane] = A2[i];
     s_B[1][wave][i * kWave + lane] = B2[i];
   }
+  // whether the span's last position is its sequence's last
+  if (wave == kW - 1 && lane == 0) s_last = n <= 0 || mk.end(P - 1);
   __syncthreads();
-  float sum[V] = {};
+  const Chain<V> ch(a, slice, taken);
+  const bool leads = a.spans > 1 && wave == 0 && c > 0;
+  bool resets = false;
+  if (leads) {
+    // from the span's last wavefront to its first
+#pragma unroll
+    for (int i = 0; i < V; ++i) A2[i] = s_A[1][kW - 1][i * kWave + lane], B2[i] = s_B[1][kW - 1][i * kWave + lane];
+#pragma unroll
+    for (int w = kW - 2; w >= 0; --w) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float An = s_A[1][w][i * kWave + lane], Bn = s_B[1][w][i * kWave + lane];
+        B2[i] = through(An, Bn, B2[i]);
+        A2[i] = An < 0.f || A2[i] < 0.f ? kResets : A2[i] * An;
+      }
+    }
+    resets = uniform(A2[0] < 0.f);
+    if (resets) ch.publish_out(B2, lane);
+    else ch.publish_steps(A2, B2, lane);
+  }
+  const uint32_t at = (uint32_t)col * (uint32_t)(Vec<TG, V>::kBytes / V);
   if (n > 0) {
-    float h[V], g[V], hs[kP][V];
-    load_f32<V>(c > 0 ? a.states + (int64_t)c * a.D : nullptr, col, h);
+    // the states, and what does not need the gradients of later spans, while those publish
+    float h[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) h[i] = state[i];
     for (int w = 0; w < wave; ++w) {
 #pragma unroll
       for (int i = 0; i < V; ++i) h[i] = through(s_A[0][w][i * kWave + lane], s_B[0][w][i * kWave + lane], h[i]);
     }
-    load_f32<V>(c + 1 < a.spans ? a.carry + (int64_t)c * a.D : nullptr, col, g);
-    for (int w = kW - 1; w > wave; --w) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) g[i] = through(s_A[1][w][i * kWave + lane], s_B[1][w][i * kWave + lane], g[i]);
-    }
-    // hs[t]: the state before position t
-#pragma unroll
-    for (int t = 0; t < kP; ++t) {
+    for (int t = 0; t < P; ++t) {
       if (t < n && mk.start(t)) {
         float h0[V] = {};
         if (a.h0) load_f32<V>(a.h0 + (int64_t)mk.of(t) * a.D, col, h0);
 #pragma unroll
         for (int i = 0; i < V; ++i) h[i] = h0[i];
       }
+      float dO[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        hs[t][i] = h[i];
-        h[i] = __builtin_fmaf(fa[t][i], h[i], fq[t][i] * gx[t].get(i));
+        const float x = gx[t].get(i);
+        r[t][i] = (h[i] - x) * fa[t][i];
+        h[i] = __builtin_fmaf(fa[t][i], h[i], fq[t][i] * x);
+        if constexpr (GATED) dO[i] = v[t][i] * h[i];
+      }
+      if constexpr (GATED) {
+        if (in && t < n) Vec<TG, V>::store(a.dO.p + (int64_t)(q0 + t) * a.dO.ld + at, dO);
       }
     }
+    float W[V], U[V];
 #pragma unroll
-    for (int t = kP - 1; t >= 0; --t) {
+    for (int i = 0; i < V; ++i) W[i] = 1.f, U[i] = 0.f;
+#pragma unroll
+    for (int t = P - 1; t >= 0; --t) {
       if (t >= n) continue;
       if (mk.end(t)) {
-        float last[V] = {};
-        if (a.dh_last) load_f32<V>(a.dh_last + (int64_t)mk.of(t) * a.D, col, last);
+        float g[V] = {};
+        if (a.dh_last) load_f32<V>(a.dh_last + (int64_t)mk.of(t) * a.D, col, g);
 #pragma unroll
-        for (int i = 0; i < V; ++i) g[i] = last[i];
+        for (int i = 0; i < V; ++i) U[i] = g[i];
       }
-      float dx[V], df[V], dO[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float dy = gy[t].get(i), x = gx[t].get(i);
-        float u = dy;
-        if constexpr (GATED) {
-          const float s = gate(go[t].get(i));
-          const float ht = __builtin_fmaf(fa[t][i], hs[t][i], fq[t][i] * x);
-          u = s * dy;
-          dO[i] = u * ht * (1.f - s);
-        }
-        const float dh = u + g[i];
-        dx[i] = fq[t][i] * dh;
-        df[i] = dx[i] * (hs[t][i] - x) * fa[t][i];
-        sum[i] += df[i];
-        g[i] = fa[t][i] * dh;
-      }
-      if (in) {
-        constexpr int kB = Vec<TG, V>::kBytes / V;
-        const int64_t row = q0 + t;
-        Vec<TG, V>::store(a.dx.p + row * a.dx.ld + (int64_t)col * kB, dx);
-        Vec<TG, V>::store(a.df.p + row * a.df.ld + (int64_t)col * kB, df);
-        if constexpr (GATED) Vec<TG, V>::store(a.dO.p + row * a.dO.ld + (int64_t)col * kB, dO);
+        U[i] += u[t][i];
+        u[t][i] = fq[t][i] * U[i];
+        fq[t][i] *= W[i];
+        U[i] *= fa[t][i];
+        W[i] *= fa[t][i];
       }
       if (a.dh0 && mk.start(t)) {
-        float* dst = a.dh0 + (int64_t)mk.of(t) * a.D + col;
-        if (in) {
+        if (mk.closed(t)) {
+          store_f32<V>(a.dh0 + (int64_t)mk.of(t) * a.D + col, in, U);
+        } else {
+          // (the one sequence that goes on: its gradient is not known yet)
 #pragma unroll
-          for (int i = 0; i < V; ++i) dst[i] = g[i];
+          for (int i = 0; i < V; ++i) W0[i] = W[i], U0[i] = U[i];
         }
+      }
+    }
+  }
+  float g[V] = {};
+  if (a.spans > 1 && !s_last) {
+    look_back<V>(ch, s_look, g, wave, lane);
+    if (leads && !resets) {
+      float leaves[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) leaves[i] = through(A2[i], B2[i], g[i]);
+      ch.publish_out(leaves, lane);
+    }
+  }
+  float sum[V] = {};
+  if (n > 0) {
+    for (int w = kW - 1; w > wave; --w) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) g[i] = through(s_A[1][w][i * kWave + lane], s_B[1][w][i * kWave + lane], g[i]);
+    }
+#pragma unroll
+    for (int t = P - 1; t >= 0; --t) {
+      if (t >= n) continue;
+      float dx[V], df[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        dx[i] = mk.closed(t) ? u[t][i] : __builtin_fmaf(fq[t][i], g[i], u[t][i]);
+        df[i] = dx[i] * r[t][i];
+        sum[i] += df[i];
+      }
+      if (in) {
+        const int64_t row = q0 + t;
+        Vec<TG, V>::store(a.dx.p + row * a.dx.ld + at, dx);
+        Vec<TG, V>::store(a.df.p + row * a.df.ld + at, df);
+      }
+      if (a.dh0 && mk.start(t) && !mk.closed(t)) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) dx[i] = __builtin_fmaf(W0[i], g[i], U0[i]);
+        store_f32<V>(a.dh0 + (int64_t)mk.of(t) * a.D + col, in, dx);
       }
     }
   }
@@ -532,44 +639,49 @@ __global__ __launch_bounds__(kThreads) void k_scan_bwd(Scan a) {
 #pragma unroll
     for (int i = 0; i < V; ++i) s_A[0][wave][i * kWave + lane] = sum[i];
     __syncthreads();
-    if (wave == 0 && in) {
+    if (wave == 0) {
+      float t[V] = {};
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        float t = 0.f;
+      for (int w = 0; w < kW; ++w) {
 #pragma unroll
-        for (int w = 0; w < kW; ++w) t += s_A[0][w][i * kWave + lane];
-        a.dbias[(int64_t)c * a.D + col + i] = t;
+        for (int i = 0; i < V; ++i) t[i] += s_A[0][w][i * kWave + lane];
       }
+      store_f32<V>(a.dbias + (int64_t)c * a.D + col, in, t);
     }
   }
 }
 
-// The spans' rows of the bias gradient, added in double: 16 wavefronts share
-// the spans of 64 columns.
-__global__ __launch_bounds__(kCarryWaves * kWave) void k_scan_dbias(const float* rows, float* dbias, int spans, int D) {
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  const int col = blockIdx.x * kWave + lane;
-  __shared__ double s_sum[kCarryWaves][kWave];
+// The spans' rows of the bias gradient, added in double: a block takes 16
+// columns, 64 rows at a time.
+constexpr int kBiasCols = 16, kBiasRows = 64;
+__global__ __launch_bounds__(kBiasCols * kBiasRows) void k_scan_dbias(const float* rows, float* dbias, int spans, int D) {
+  const int c = threadIdx.x % kBiasCols, r = threadIdx.x / kBiasCols;
+  const int col = blockIdx.x * kBiasCols + c;
+  __shared__ double s_sum[kBiasRows][kBiasCols];
   double t = 0.;
   if (col < D) {
     constexpr int kAhead = 8;
-    for (int k = wave; k < spans; k += kCarryWaves * kAhead) {
+    for (int k = r; k < spans; k += kBiasRows * kAhead) {
       float x[kAhead];
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
-        const int at = k + i * kCarryWaves;
+        const int at = k + i * kBiasRows;
         x[i] = at < spans ? rows[(int64_t)at * D + col] : 0.f;
       }
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) t += (double)x[i];
     }
   }
-  s_sum[wave][lane] = t;
-  __syncthreads();
-  if (wave == 0 && col < D) {
-    for (int w = 1; w < kCarryWaves; ++w) t += s_sum[w][lane];
-    dbias[col] = (float)t;
+  s_sum[r][c] = t;
+  for (int half = kBiasRows / 2; half > 0; half /= 2) {
+    __syncthreads();
+    if (r < half) s_sum[r][c] += s_sum[r + half][c];
   }
+  if (r == 0 && col < D) dbias[col] = (float)s_sum[0][c];
+}
+
+__global__ __launch_bounds__(256) void k_scan_clear(uint32_t* words, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) words[i] = 0u;
 }
 
 // no positions at all: empty sequences' states and gradients, a zero dbias
@@ -614,11 +726,30 @@ __global__ __launch_bounds__(256) void k_scan_step(StepLaunch a) {
 
 // ---------------------------------------------------------------- launches
 
-size_t span_rows(int64_t N, int32_t D) {
-  return align256(sizeof(float) * (size_t)((N + kSpan - 1) / kSpan) * (size_t)D);
+// The workspace: counters and flags, steps, outgoing states, rows of the bias
+// gradient; for spans of 64 (the backward's; the forward's are fewer).
+struct Room {
+  int64_t spans, slices, cols;
+  size_t flags, steps, out, dbias, total;
+};
+Room room(int64_t N, int32_t D) {
+  Room r{};
+  r.spans = (N + kSpan - 1) / kSpan;
+  r.slices = ((int64_t)D + kWave - 1) / kWave;
+  r.cols = ((int64_t)D + 2 * kWave - 1) / (2 * kWave) * (2 * kWave);
+  size_t at = 0;
+  r.flags = at;
+  at = align256(at + sizeof(uint32_t) * (size_t)(r.slices * (r.spans + 1)));
+  r.steps = at;
+  at = align256(at + sizeof(uint64_t) * (size_t)(r.spans * r.cols));
+  r.out = at;
+  at = align256(at + sizeof(uint32_t) * (size_t)(r.spans * r.cols));
+  r.dbias = at;
+  r.total = align256(at + sizeof(float) * (size_t)r.spans * (size_t)D);
+  return r;
 }
 
-Scan arguments(const ScanLaunch& p) {
+Scan arguments(const ScanLaunch& p, int V, int span) {
   Scan a{};
   a.offsets = p.offsets;
   a.x = p.x, a.f = p.f, a.o = p.o, a.y = p.y;
@@ -626,51 +757,43 @@ Scan arguments(const ScanLaunch& p) {
   a.bias = p.bias, a.h0 = p.h0, a.h_last = p.h_last;
   a.states = p.states, a.dh_last = p.dh_last, a.dh0 = p.dh0;
   a.N = (int32_t)p.N, a.M = p.M, a.D = p.D;
-  a.spans = (int32_t)((p.N + kSpan - 1) / kSpan);
-  const size_t rows = span_rows(p.N, p.D);
-  a.A = reinterpret_cast<float*>(p.ws);
-  a.B = reinterpret_cast<float*>(p.ws + rows);
-  a.carry = reinterpret_cast<float*>(p.ws + 2 * rows);
-  a.dbias = p.dbias ? reinterpret_cast<float*>(p.ws + 3 * rows) : nullptr;
+  a.spans = (int32_t)((p.N + span - 1) / span);
+  a.slices = (p.D + kWave * V - 1) / (kWave * V);
+  const Room r = room(p.N, p.D);
+  a.taken = reinterpret_cast<uint32_t*>(p.ws + r.flags);
+  a.flags = a.taken + a.slices;
+  a.steps = reinterpret_cast<uint64_t*>(p.ws + r.steps);
+  a.out = reinterpret_cast<uint32_t*>(p.ws + r.out);
+  a.dbias = p.dbias ? reinterpret_cast<float*>(p.ws + r.dbias) : nullptr;
   return a;
 }
-int empties(const Scan& a, const float* out) { return out ? (a.M + kWave - 1) / kWave : 0; }
-
-template <typename T, int V, bool GATED>
-hipError_t fwd(Scan a, float* states, hipStream_t s) {
-  a.slices = (a.D + kWave * V - 1) / (kWave * V);
-  const unsigned main = (unsigned)(a.spans * a.slices);
-  if (states) a.carry = states;
-  if (a.spans > 1) {
-    k_scan_fwd<T, V, GATED, false><<<main, kThreads, 0, s>>>(a);
-  }
-  if (a.spans == 1) nothing(nullptr, states, a.D, s);
-  else
-    k_scan_carry<false><<<(a.D + kWave - 1) / kWave, kCarryWaves * kWave, 0, s>>>(a.A, a.B, a.carry, a.spans, a.D);
-  k_scan_fwd<T, V, GATED, true><<<main + empties(a, a.h_last), kThreads, 0, s>>>(a);
-  return hipGetLastError();
+unsigned empties(const Scan& a, const float* out) { return out ? (unsigned)(a.M + kWave - 1) / kWave : 0u; }
+void clear(const Scan& a, hipStream_t s) {
+  const int64_t n = (int64_t)a.slices * (a.spans + 1), blocks = (n + 255) / 256;
+  if (a.spans > 1) k_scan_clear<<<(unsigned)(blocks < 256 ? blocks : 256), 256, 0, s>>>(a.taken, n);
 }
+
 template <typename T, int V>
-hipError_t fwd_gated(const ScanLaunch& p, hipStream_t s) {
-  return p.gated ? fwd<T, V, true>(arguments(p), p.states, s) : fwd<T, V, false>(arguments(p), p.states, s);
-}
-
-template <typename T, typename TG, int V, bool GATED>
-hipError_t bwd(Scan a, float* dbias, hipStream_t s) {
-  a.slices = (a.D + kWave * V - 1) / (kWave * V);
-  const unsigned main = (unsigned)(a.spans * a.slices);
-  const unsigned cols = (unsigned)(a.D + kWave - 1) / kWave;
-  if (a.spans > 1) {
-    k_scan_back_sums<T, TG, V, GATED><<<main, kThreads, 0, s>>>(a);
-    k_scan_carry<true><<<cols, kCarryWaves * kWave, 0, s>>>(a.A, a.B, a.carry, a.spans, a.D);
-  }
-  k_scan_bwd<T, TG, V, GATED><<<main + empties(a, a.dh0), kThreads, 0, s>>>(a);
-  if (dbias) k_scan_dbias<<<cols, kCarryWaves * kWave, 0, s>>>(a.dbias, dbias, a.spans, a.D);
+hipError_t fwd(const ScanLaunch& p, hipStream_t s) {
+  const Scan a = arguments(p, V, kFwdSpan);
+  const unsigned blocks = (unsigned)(a.spans * a.slices) + empties(a, a.h_last);
+  clear(a, s);
+  if (p.gated) k_scan_fwd<T, V, true><<<blocks, kThreads, 0, s>>>(a);
+  else k_scan_fwd<T, V, false><<<blocks, kThreads, 0, s>>>(a);
   return hipGetLastError();
 }
+
 template <typename T, typename TG, int V>
-hipError_t bwd_gated(const ScanLaunch& p, hipStream_t s) {
-  return p.gated ? bwd<T, TG, V, true>(arguments(p), p.dbias, s) : bwd<T, TG, V, false>(arguments(p), p.dbias, s);
+hipError_t bwd(const ScanLaunch& p, hipStream_t s) {
+  const Scan a = arguments(p, V, kSpan);
+  const unsigned blocks = (unsigned)(a.spans * a.slices) + empties(a, a.dh0);
+  clear(a, s);
+  if (p.gated) k_scan_bwd<T, TG, V, true><<<blocks, kThreads, 0, s>>>(a);
+  else k_scan_bwd<T, TG, V, false><<<blocks, kThreads, 0, s>>>(a);
+  if (p.dbias)
+    k_scan_dbias<<<(unsigned)((a.D + kBiasCols - 1) / kBiasCols), kBiasCols * kBiasRows, 0, s>>>(a.dbias, p.dbias, a.spans,
+                                                                                             a.D);
+  return hipGetLastError();
 }
 
 template <typename T, int V>
@@ -683,15 +806,15 @@ hipError_t step(const StepLaunch& p, hipStream_t s) {
 
 }  // namespace
 
-size_t scan_ws_bytes(int64_t N, int32_t D) { return 4 * span_rows(N > 0 ? N : 1, D); }
+size_t scan_ws_bytes(int64_t N, int32_t D) { return room(N > 0 ? N : 1, D).total; }
 
 hipError_t launch_scan_fwd(const ScanLaunch& p, hipStream_t s) {
   if (p.N == 0) {
     nothing(p.h0, p.h_last, (int64_t)p.M * p.D, s);
     return hipGetLastError();
   }
-  if (p.dtype == EMB_FP32) return fwd_gated<float, 1>(p, s);
-  return p.vector == 2 ? fwd_gated<bf16, 2>(p, s) : fwd_gated<bf16, 1>(p, s);
+  if (p.dtype == EMB_FP32) return fwd<float, 1>(p, s);
+  return p.vector == 2 ? fwd<bf16, 2>(p, s) : fwd<bf16, 1>(p, s);
 }
 
 hipError_t launch_scan_bwd(const ScanLaunch& p, hipStream_t s) {
@@ -700,10 +823,10 @@ hipError_t launch_scan_bwd(const ScanLaunch& p, hipStream_t s) {
     nothing(nullptr, p.dbias, p.D, s);
     return hipGetLastError();
   }
-  if (p.dtype == EMB_FP32) return bwd_gated<float, float, 1>(p, s);
-  if (p.dtype == EMB_BF16) return p.vector == 2 ? bwd_gated<bf16, bf16, 2>(p, s) : bwd_gated<bf16, bf16, 1>(p, s);
-  if (p.grad_dtype == EMB_FP32) return bwd_gated<Saved8, float, 1>(p, s);
-  return p.vector == 2 ? bwd_gated<Saved8, bf16, 2>(p, s) : bwd_gated<Saved8, bf16, 1>(p, s);
+  if (p.dtype == EMB_FP32) return bwd<float, float, 1>(p, s);
+  if (p.dtype == EMB_BF16) return p.vector == 2 ? bwd<bf16, bf16, 2>(p, s) : bwd<bf16, bf16, 1>(p, s);
+  if (p.grad_dtype == EMB_FP32) return bwd<Saved8, float, 1>(p, s);
+  return p.vector == 2 ? bwd<Saved8, bf16, 2>(p, s) : bwd<Saved8, bf16, 1>(p, s);
 }
 
 hipError_t launch_scan_step(const StepLaunch& p, hipStream_t s) {
