@@ -164,10 +164,27 @@ def _ptr(t) -> Optional[int]:
     return int(t.data_ptr())
 
 
+_current = None
+
+
+def _current_stream() -> int:
+    """The current stream of the current device: PyTorch's raw handle where it
+    offers one (0.2 us a call; building its Stream object takes 3 us)."""
+    global _current
+    if _current is None:
+        import torch
+        raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+        if raw is not None and device is not None:
+            torch.cuda.init()
+            _current = lambda: raw(device())  # noqa: E731
+        else:
+            _current = lambda: int(torch.cuda.current_stream().cuda_stream)  # noqa: E731
+    return _current()
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        import torch
-        return int(torch.cuda.current_stream().cuda_stream)
+        return _current_stream()
     if isinstance(stream, int):
         return stream
     return int(stream.cuda_stream)

@@ -93,6 +93,7 @@ __global__ __launch_bounds__(kFwdThreads) void k_token_fwd(TokFwd a, Stacked<MAN
 // ---------------------------------------------------------------- gradient
 
 enum Kind { kStore = 0, kSgd = 1, kAdaRow = 2, kAdaElem = 3 };
+constexpr int kMostSplit = 4, kSplitWaves = 8192;
 constexpr int kMostParts = 16;  // wavefronts of a block that share a chunk's columns (row-wise Adagrad)
 
 struct TokGrad {
@@ -106,7 +107,7 @@ struct TokGrad {
   const void* hdr;
   float* partials;  // [nchunks][2][D]: rows of long segments, of the one that holds a chunk's first position, of another
   float* grad;
-  int32_t N, D, nchunks, parts, layout, aligned;
+  int32_t N, D, nchunks, parts, split, blocks, zero_blocks, layout, aligned;  // split: 2^split wavefronts share a chunk's columns
   uint32_t rows, pad;
   float scale;
   Upd up;
@@ -162,34 +163,98 @@ __device__ __forceinline__ void apply(const Upd& up, uint32_t key, int c, const 
   store_row<TW, EL>(up, key, c, o);
 }
 
+// x summed over the wavefront, in every lane
+template <int CTRL>
+__device__ __forceinline__ float add_lane(float x) {
+  return x + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xf, 0xf, true));
+}
 __device__ __forceinline__ float wave_total(float x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, kWave);
-  return x;
+  // lanes 1 and 2 apart, then the mirrors of half rows and rows (whose lanes hold equal sums), then rows and halves
+  return add_across<32>(add_across<16>(add_lane<0x140>(add_lane<0x141>(add_lane<0x4e>(add_lane<0xb1>(x))))));
 }
 
-// EL columns a lane, B positions a batch.  ROWWISE blocks are the `parts`
-// wavefronts of one chunk; others four wavefronts of any.
+// Rows of the table that no token named: zeros.  One wavefront per kZeroRows
+// rows.
+constexpr int kZeroRows = 16;
+__device__ __forceinline__ void zero_rows(const TokGrad& a, int64_t r0, int lane) {
+  if (r0 >= (int64_t)a.rows) return;
+  const int U = failed(a) ? 0 : a.num_unique[0];
+  uint32_t named = 0;
+  if (U > 0) {
+    const int u = r0 == 0 ? 0 : wave_upper_bound<uint32_t>(a.ukeys, U, (uint32_t)r0 - 1u, lane);
+    const uint32_t key = u + lane < U ? a.ukeys[u + lane] : kNoRow;
+#pragma unroll
+    for (int r = 0; r < kZeroRows; ++r) named |= __ballot(key == (uint32_t)r0 + r) ? 1u << r : 0u;
+  }
+  const int n = (int)min((int64_t)kZeroRows, (int64_t)a.rows - r0);
+  for (int r = 0; r < n; ++r) {
+    if ((named >> r) & 1u) continue;
+    float* dst = a.grad + (r0 + r) * (int64_t)a.D;
+    for (int c = lane * 4; c < a.D; c += kWave * 4) *reinterpret_cast<f32x4*>(dst + c) = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+}
+
+// of the a.blocks + a.zero_blocks blocks, those of zeros among the first b
+__device__ __forceinline__ int zero_blocks_before(const TokGrad& a, int b) {
+  return (int)((uint64_t)(uint32_t)b * (uint32_t)a.zero_blocks / (uint32_t)(a.blocks + a.zero_blocks));
+}
+
+// a finished gradient row's columns, where `layout` wants them
+template <int EL>
+__device__ __forceinline__ void store_grad(const TokGrad& a, int u, uint32_t key, int col, bool in, float (&g)[EL]) {
+  if (!in || (a.layout != EMB_ROWS && key >= a.rows)) return;
+  float* dst = a.grad + (int64_t)(a.layout == EMB_ROWS ? (uint32_t)u : key) * a.D + col;
+  if (key == a.pad) {
+    if (a.layout == EMB_TABLE_ADD) return;
+#pragma unroll
+    for (int e = 0; e < EL; ++e) g[e] = 0.f;
+  }
+  if (a.layout == EMB_TABLE_ADD) {
+    Vec<float, EL> old;
+    old.load(dst);
+#pragma unroll
+    for (int e = 0; e < EL; ++e) g[e] += old.get(e);
+  }
+  Vec<float, EL>::store(dst, g);
+}
+
+// EL columns a lane, B positions a batch.  Row-wise Adagrad's blocks are the
+// `parts` wavefronts of one chunk, which add up their rows' squares through
+// LDS; others are four wavefronts of any.  EMB_TABLE's zeros are written by
+// blocks of their own.
 template <typename TG, typename TW, int EL, int B, int KIND>
 __global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) void k_token_reduce(TokGrad a) {
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
-  int c, part;
-  if constexpr (KIND == kAdaRow) {
-    c = blockIdx.x, part = wave;
-  } else {
-    const int at = blockIdx.x * 4 + wave;
-    c = at / a.parts, part = at % a.parts;
+  int block = blockIdx.x;
+  if constexpr (KIND == kStore) {
+    // blocks of zeros come among the others evenly: these write while those wait for rows
+    const int z = zero_blocks_before(a, block), more = zero_blocks_before(a, block + 1);
+    if (more > z) {
+      zero_rows(a, ((int64_t)z * 4 + wave) * kZeroRows, lane);
+      return;
+    }
+    block -= z;
   }
+  // the chunk, the share of it whose segments start here, the columns
+  int at, part;
+  if constexpr (KIND == kAdaRow) {
+    at = block, part = wave;
+  } else {
+    at = block * 4 + wave;
+    part = at % a.parts, at /= a.parts;
+  }
+  const int c = at >> a.split, sub = at & ((1 << a.split) - 1);
   __shared__ float s_sq[2][kMostParts][B];
   if (c >= a.nchunks) return;
   const int col = (part * kWave + lane) * EL;
   const bool in = col < a.D;
   const int cs = in ? col : 0;
   const int p0 = c * kChunk, p1 = min(a.N, p0 + kChunk);
+  const int b0 = p0 + sub * (kChunk >> a.split), b1 = min(p1, b0 + (kChunk >> a.split));
   if (failed(a)) {
     if (KIND == kStore && a.layout == EMB_ROWS && in) {
       float z[EL] = {};
-      for (int p = p0; p < p1; ++p) Vec<float, EL>::store(a.grad + (int64_t)p * a.D + col, z);
+      for (int p = b0; p < b1; ++p) Vec<float, EL>::store(a.grad + (int64_t)p * a.D + col, z);
     }
     return;
   }
@@ -203,16 +268,19 @@ __global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) v
   const int before = __shfl_up(ends, 1, kWave);
   const int len = ends - (lane == 0 ? s0 : before);
   const uint64_t heavy = __ballot(len > kChunk);
-  // the segment that holds the chunk's last position
-  const int n_ended = __popcll(__ballot(u0 + lane < U && ends <= p1 - 1));
-  const int last = min(n_ended, kWave - 1);
-  const bool old_light = s0 < p0 && !(heavy & 1u);  // the previous chunk's wavefront has its positions
-  const int fin = (heavy >> last) & 1u ? p1 : lane_at(ends, last);
-  int i = 0, q = p0;
-  if (old_light) {
-    q = lane_at(ends, 0);
-    i = 1;
-    if (q >= p1) return;
+  // the segments that start in b0 .. b1 - 1, and with them a long one's piece that came in with the chunk; a light
+  // segment that came in belongs to another wavefront
+  const bool came_in = s0 < p0 && sub == 0 && (heavy & 1u);
+  int i = s0 >= b0 || came_in ? 0 : 1 + (int)__popcll(__ballot(ends < b0));
+  const int last = (int)__popcll(__ballot(ends < b1));
+  if (i > last) return;
+  const int fin = (heavy >> last) & 1u ? min(p1, lane_at(ends, last)) : lane_at(ends, last);
+  int q = i == 0 ? p0 : lane_at(ends, i - 1);
+  // the row-wise accumulators of the segments, a lane each, read before any wavefront of the block writes one
+  float accum = 0.f;
+  if constexpr (KIND == kAdaRow) {
+    if (keys < a.rows) accum = a.up.state[keys];
+    asm volatile("" : "+v"(accum)::"memory");
   }
   float acc[EL] = {};
   int parity = 0;
@@ -220,9 +288,9 @@ __global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) v
     // a padding segment has no gradient: its positions are not read
     if (lane_at(keys, i) == a.pad) {
       if constexpr (KIND == kStore) {
-        if (!((heavy >> i) & 1u) && in && a.layout != EMB_TABLE_ADD) {
+        if (!((heavy >> i) & 1u)) {
           float z[EL] = {};
-          Vec<float, EL>::store(a.grad + (int64_t)(a.layout == EMB_ROWS ? (uint32_t)(u0 + i) : a.pad) * a.D + col, z);
+          store_grad<EL>(a, u0 + i, a.pad, col, in, z);
         }
       }
       // (a batch may have ended inside it)
@@ -233,82 +301,77 @@ __global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) v
       continue;
     }
     Vec<TG, EL> g[B];
-    Vec<TW, EL> w[B];
-    Vec<float, EL> h[B];
-    float done[B][EL];
-    int seg_of[B];  // the segment that ends at the batch's position, or -1
     const int n = min(B, fin - q);
-    int j = i;
 #pragma unroll
     for (int k = 0; k < B; ++k) {
       const int pos = min(q + k, fin - 1) - p0;
       const int row = pos < kWave ? lane_at(row_a, pos) : lane_at(row_b, pos - kWave);
-      const char* src = a.dy + (int64_t)row * a.ld + (int64_t)cs * (Vec<TG, EL>::kBytes / EL);
+      const char* src = a.dy + (int64_t)row * a.ld + (uint32_t)cs * (uint32_t)(Vec<TG, EL>::kBytes / EL);
       if (a.aligned) g[k].load(src);
       else g[k].load_each(src);
-    }
-#pragma unroll
-    for (int k = 0; k < B; ++k) {
-      seg_of[k] = -1;
-      if (k < n && q + k + 1 == min(lane_at(ends, j), fin)) {
-        seg_of[k] = j;
-        if constexpr (KIND != kStore) {
-          const uint32_t key = lane_at(keys, j);
-          if (!((heavy >> j) & 1u) && key < a.rows && key != a.pad) {
-            w[k].load(static_cast<const char*>(a.up.W) + ((int64_t)key * a.D + cs) * (int64_t)sizeof(TW));
-            if constexpr (KIND == kAdaElem) h[k].load(a.up.state + (int64_t)key * a.D + cs);
-          }
-        }
-        j = min(j + 1, kWave - 1);
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < B; ++k) {
-#pragma unroll
-      for (int e = 0; e < EL; ++e) {
-        acc[e] += k < n ? g[k].get(e) : 0.f;
-        done[k][e] = acc[e] * a.scale;
-      }
-      if (seg_of[k] >= 0) {
-#pragma unroll
-        for (int e = 0; e < EL; ++e) acc[e] = 0.f;
-        if ((heavy >> seg_of[k]) & 1u) {
-          if (in)
-            Vec<float, EL>::store(a.partials + ((int64_t)c * 2 + (seg_of[k] == 0 ? 0 : 1)) * a.D + col, done[k]);
-          seg_of[k] = -1;
-        }
-      }
     }
     if constexpr (KIND == kStore) {
 #pragma unroll
       for (int k = 0; k < B; ++k) {
-        if (seg_of[k] < 0) continue;
-        const uint32_t key = lane_at(keys, seg_of[k]);
-        if (a.layout != EMB_ROWS && key >= a.rows) continue;
-        if (!in) continue;
-        float* dst = a.grad + (int64_t)(a.layout == EMB_ROWS ? (uint32_t)(u0 + seg_of[k]) : key) * a.D + col;
-        if (key == a.pad) {
-          if (a.layout == EMB_TABLE_ADD) continue;
+        if (k >= n) continue;
 #pragma unroll
-          for (int e = 0; e < EL; ++e) done[k][e] = 0.f;
-        }
-        if (a.layout == EMB_TABLE_ADD) {
-          Vec<float, EL> old;
-          old.load(dst);
+        for (int e = 0; e < EL; ++e) acc[e] += g[k].get(e);
+        if (q + k + 1 != min(lane_at(ends, i), fin)) continue;
+        float done[EL];
 #pragma unroll
-          for (int e = 0; e < EL; ++e) done[k][e] += old.get(e);
+        for (int e = 0; e < EL; ++e) done[e] = acc[e] * a.scale, acc[e] = 0.f;
+        if ((heavy >> i) & 1u) {
+          if (in) Vec<float, EL>::store(a.partials + ((int64_t)c * 2 + (i == 0 ? 0 : 1)) * a.D + col, done);
+        } else {
+          store_grad<EL>(a, u0 + i, lane_at(keys, i), col, in, done);
         }
-        Vec<float, EL>::store(dst, done[k]);
+        i = min(i + 1, kWave - 1);
       }
     } else {
+      Vec<TW, EL> w[B];
+      Vec<float, EL> h[KIND == kAdaElem ? B : 1];
+      float done[B][EL];
+      int seg_of[B];  // the segment that ends at the batch's position, or -1
+#pragma unroll
+      for (int k = 0; k < B; ++k) {
+        seg_of[k] = -1;
+        if (k < n && q + k + 1 == min(lane_at(ends, i), fin)) {
+          seg_of[k] = i;
+          const uint32_t key = lane_at(keys, i);
+          if (!((heavy >> i) & 1u) && key < a.rows && key != a.pad) {
+            w[k].load(static_cast<const char*>(a.up.W) + ((int64_t)key * a.D + cs) * (int64_t)sizeof(TW));
+            if constexpr (KIND == kAdaElem) h[k].load(a.up.state + (int64_t)key * a.D + cs);
+          }
+          i = min(i + 1, kWave - 1);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < B; ++k) {
+#pragma unroll
+        for (int e = 0; e < EL; ++e) {
+          acc[e] += k < n ? g[k].get(e) : 0.f;
+          done[k][e] = acc[e] * a.scale;
+        }
+        if (seg_of[k] >= 0) {
+#pragma unroll
+          for (int e = 0; e < EL; ++e) acc[e] = 0.f;
+          if ((heavy >> seg_of[k]) & 1u) {
+            if (in)
+              Vec<float, EL>::store(a.partials + ((int64_t)c * 2 + (seg_of[k] == 0 ? 0 : 1)) * a.D + col, done[k]);
+            seg_of[k] = -1;
+          }
+        }
+      }
       float total[B];
       if constexpr (KIND == kAdaRow) {
 #pragma unroll
         for (int k = 0; k < B; ++k) {
+          total[k] = 0.f;
+          if (seg_of[k] < 0) continue;
           float sq = 0.f;
 #pragma unroll
           for (int e = 0; e < EL; ++e) sq = __builtin_fmaf(done[k][e], done[k][e], sq);
-          total[k] = seg_of[k] >= 0 ? wave_total(in ? sq : 0.f) : 0.f;
+          total[k] = wave_total(in ? sq : 0.f);
         }
         if (a.parts > 1) {
           // (a batch's sums are read before the batch after next is summed, a barrier later)
@@ -332,112 +395,134 @@ __global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) v
         if (key >= a.rows || key == a.pad) continue;
         float step = a.up.lr;
         if constexpr (KIND == kAdaRow) {
-          const float hn = a.up.state[key] + total[k] / (float)a.D;
+          const float hn = __int_as_float(lane_at(__float_as_int(accum), seg_of[k])) + total[k] / (float)a.D;
           step = a.up.lr / (sqrtf(hn) + a.up.eps);
-          if (a.parts > 1) __syncthreads();  // every wavefront has read the accumulator
-          if (wave == 0 && lane == 0) a.up.state[key] = hn;
+          if (wave == (a.parts > 1 ? 0 : wave) && lane == 0) a.up.state[key] = hn;
         }
-        if (in) apply<TW, EL, KIND>(a.up, key, col, done[k], w[k], h[k], step);
+        if (in) apply<TW, EL, KIND>(a.up, key, col, done[k], w[k], h[KIND == kAdaElem ? k : 0], step);
       }
     }
-    i = j;
     q += n;
   }
 }
 
-// Rows of the table that no token named: zeros.  One wavefront per 64 rows.
 __global__ __launch_bounds__(256) void k_token_zero(TokGrad a) {
-  const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
-  const int64_t r0 = ((int64_t)blockIdx.x * 4 + wave) * kWave;
-  if (r0 >= (int64_t)a.rows) return;
-  const int U = failed(a) ? 0 : a.num_unique[0];
-  uint64_t named = 0;
-  if (U > 0) {
-    const int u = r0 == 0 ? 0 : wave_upper_bound<uint32_t>(a.ukeys, U, (uint32_t)r0 - 1u, lane);
-    const uint32_t key = u + lane < U ? a.ukeys[u + lane] : kNoRow;
-    uint64_t bit = (uint64_t)key < (uint64_t)r0 + kWave ? 1ull << (key - (uint32_t)r0) : 0ull;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1)
-      bit |= ((uint64_t)(uint32_t)__shfl_xor((int)(bit >> 32), o, kWave) << 32) |
-             (uint32_t)__shfl_xor((int)(uint32_t)bit, o, kWave);
-    named = bit;
-  }
-  const int n = (int)min((int64_t)kWave, (int64_t)a.rows - r0);
-  for (int r = 0; r < n; ++r) {
-    if ((named >> r) & 1ull) continue;
-    float* dst = a.grad + (r0 + r) * (int64_t)a.D;
-    for (int c = lane * 4; c < a.D; c += kWave * 4) *reinterpret_cast<f32x4*>(dst + c) = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  zero_rows(a, ((int64_t)blockIdx.x * 4 + threadIdx.x / kWave) * kZeroRows, threadIdx.x & (kWave - 1));
 }
 
 // A segment of more than 64 positions: the partial rows of its chunks added in
-// double, in chunk order, by the block of the chunk it starts in.
+// double by the block of the chunk it starts in.  A lane takes four columns; a
+// row leaves room for blockDim / (D / 4) groups of lanes (16 for rows of 64 values,
+// 4 for 1024),
+// which take every so many-th chunk and are added up through LDS in order.  Bound
+// by latency: what tells the segment is read in two rounds, eight chunks' rows a
+// lane in one.
+constexpr int kCombineCols = 4, kCombineLanes = 1024;
 template <typename TW, int KIND>
-__global__ __launch_bounds__(256) void k_token_combine(TokGrad a) {
+__global__ __launch_bounds__(kCombineLanes) void k_token_combine(TokGrad a) {
   const int c = blockIdx.x, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   const int p0 = c * kChunk, p1 = min(a.N, p0 + kChunk);
   if (failed(a)) return;
   const int U = a.num_unique[0];
   // the segment that holds the chunk's last position, if it is long and starts here
   const int next = a.chunk_seg[c + 1];  // (U after the last chunk)
-  const int u = next == U || a.seg[next] >= p1 ? next - 1 : next;
-  const int s = a.seg[u], e = a.seg[u + 1];
+  const int here = min(next, U - 1), prior = max(next - 1, 0);
+  const int s_prior = a.seg[prior], s_here = a.seg[here], e_here = a.seg[here + 1];
+  const uint32_t k_prior = a.ukeys[prior], k_here = a.ukeys[here];
+  const bool back = next == U || s_here >= p1;
+  const int u = back ? prior : here, s = back ? s_prior : s_here;
+  const int e = back && next != U ? s_here : e_here;
   if (s < p0 || e - s <= kChunk) return;
-  const uint32_t key = a.ukeys[u];
+  const uint32_t key = back ? k_prior : k_here;
   const bool pad = key == a.pad;
   if (pad && KIND != kStore) return;
   if (key >= a.rows && !(KIND == kStore && a.layout == EMB_ROWS)) return;
   const int last = (e - 1) / kChunk;
+  const int vectors = a.D / kCombineCols;
+  const int lanes = blockDim.x, groups = vectors >= lanes ? 1 : lanes / vectors;
+  const int group = groups == 1 ? 0 : (int)threadIdx.x / vectors, v0 = groups == 1 ? (int)threadIdx.x : (int)threadIdx.x % vectors;
+  const int stride = groups == 1 ? lanes : vectors;  // (a row of 4096 values or more is gone over in turns)
+  __shared__ double s_part[kCombineLanes][kCombineCols];
+  __shared__ float s_sq[kCombineLanes / kWave];
   const float* first = a.partials + ((int64_t)c * 2 + (s == p0 ? 0 : 1)) * a.D;
-  auto sum = [&](int col) {
-    double t = first[col];
-    int k = c + 1;
-    for (; k + 8 <= last + 1; k += 8) {
-      float x[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = a.partials[(int64_t)(k + i) * 2 * a.D + col];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) t += (double)x[i];
-    }
-    for (; k <= last; ++k) t += (double)a.partials[(int64_t)k * 2 * a.D + col];
-    return (float)t;
-  };
-  if constexpr (KIND == kStore) {
-    if (pad && a.layout == EMB_TABLE_ADD) return;
-    float* dst = a.grad + (int64_t)(a.layout == EMB_ROWS ? (uint32_t)u : key) * a.D;
-    for (int col = threadIdx.x; col < a.D; col += 256) {
-      const float g = pad ? 0.f : sum(col);
-      dst[col] = a.layout == EMB_TABLE_ADD ? dst[col] + g : g;
-    }
-  } else {
-    __shared__ float s_sq[4];
-    float step = a.up.lr;
-    float* row = const_cast<float*>(first);  // (the sums, where the squares are needed first)
-    if constexpr (KIND == kAdaRow) {
-      float sq = 0.f;
-      for (int col = threadIdx.x; col < a.D; col += 256) {
-        const float g = sum(col);
-        row[col] = g;
-        sq = __builtin_fmaf(g, g, sq);
-      }
-      sq = wave_total(sq);
-      if (lane == 0) s_sq[wave] = sq;
-      const float old = a.up.state[key];
-      __syncthreads();
-      const float hn = old + (s_sq[0] + s_sq[1] + s_sq[2] + s_sq[3]) / (float)a.D;
-      step = a.up.lr / (sqrtf(hn) + a.up.eps);
-      if (threadIdx.x == 0) a.up.state[key] = hn;
-    }
-    for (int col = threadIdx.x; col < a.D; col += 256) {
-      float g[1] = {KIND == kAdaRow ? row[col] : sum(col)};
-      Vec<TW, 1> w;
-      Vec<float, 1> h;
+  float sq = 0.f;
+  const float old = KIND == kAdaRow ? a.up.state[key] : 0.f;
+  auto finish = [&](int col, float (&g)[kCombineCols], float step) {
+    if constexpr (KIND == kStore) {
+      store_grad<kCombineCols>(a, u, key, col, true, g);
+    } else {
+      Vec<TW, kCombineCols> w;
+      Vec<float, kCombineCols> h;
       w.load(static_cast<const char*>(a.up.W) + ((int64_t)key * a.D + col) * (int64_t)sizeof(TW));
       if constexpr (KIND == kAdaElem) h.load(a.up.state + (int64_t)key * a.D + col);
-      apply<TW, 1, KIND>(a.up, key, col, g, w, h, step);
+      apply<TW, kCombineCols, KIND>(a.up, key, col, g, w, h, step);
+    }
+  };
+  for (int v = v0; v - v0 < vectors; v += stride) {
+    const bool in = v < vectors && group < groups;
+    const int col = in ? v * kCombineCols : 0;
+    double t[kCombineCols] = {};
+    if (in && !pad) {
+      // chunk c itself counts as the first of the list
+      constexpr int kAhead = 8;
+      for (int k = c + group; k <= last; k += groups * kAhead) {
+        Vec<float, kCombineCols> x[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          const int at = k + i * groups;
+          if (at > last) x[i].zero();
+          else x[i].load((at == c ? first : a.partials + (int64_t)at * 2 * a.D) + col);
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+          for (int j = 0; j < kCombineCols; ++j) t[j] += (double)x[i].get(j);
+      }
+    }
+    if (groups > 1) {
+#pragma unroll
+      for (int j = 0; j < kCombineCols; ++j) s_part[threadIdx.x][j] = t[j];
+      __syncthreads();
+      if (group == 0) {
+        for (int k = 1; k < groups; ++k)
+#pragma unroll
+          for (int j = 0; j < kCombineCols; ++j) t[j] += s_part[k * vectors + v0][j];
+      }
+    }
+    if (!in || group != 0) continue;
+    float g[kCombineCols];
+#pragma unroll
+    for (int j = 0; j < kCombineCols; ++j) g[j] = (float)t[j];
+    if constexpr (KIND == kAdaRow) {
+      // (the sums wait in the first partial row until the squares of all columns are known)
+      Vec<float, kCombineCols>::store(const_cast<float*>(first) + col, g);
+#pragma unroll
+      for (int j = 0; j < kCombineCols; ++j) sq = __builtin_fmaf(g[j], g[j], sq);
+    } else {
+      finish(col, g, a.up.lr);
+    }
+  }
+  if constexpr (KIND == kAdaRow) {
+    sq = wave_total(sq);
+    if (lane == 0) s_sq[wave] = sq;
+    __syncthreads();
+    float total = 0.f;
+    for (int w = 0; w < lanes / kWave; ++w) total += s_sq[w];
+    const float hn = old + total / (float)a.D;
+    const float step = a.up.lr / (sqrtf(hn) + a.up.eps);
+    if (threadIdx.x == 0) a.up.state[key] = hn;
+    for (int v = threadIdx.x; v < vectors; v += lanes) {
+      Vec<float, kCombineCols> x;
+      x.load(first + v * kCombineCols);
+      float g[kCombineCols];
+#pragma unroll
+      for (int j = 0; j < kCombineCols; ++j) g[j] = x.get(j);
+      finish(v * kCombineCols, g, step);
     }
   }
 }
+
+int zero_blocks(uint32_t rows) { return (int)(((int64_t)rows + 4 * kZeroRows - 1) / (4 * kZeroRows)); }
 
 template <typename TG, typename TW, int KIND>
 hipError_t grad_kernels(TokGrad a, hipStream_t s) {
@@ -446,14 +531,22 @@ hipError_t grad_kernels(TokGrad a, hipStream_t s) {
   a.parts = (a.D + kWave * el - 1) / (kWave * el);
   constexpr bool kRow = KIND == kAdaRow;
   const dim3 block(kRow ? a.parts * kWave : 4 * kWave);
-  const dim3 grid(kRow ? a.nchunks : (a.nchunks * a.parts + 3) / 4);
+  a.split = 0;
+  while (a.split < kMostSplit && ((int64_t)a.nchunks * a.parts << a.split) < kSplitWaves) ++a.split;
+  a.blocks = kRow ? a.nchunks << a.split : ((a.nchunks * a.parts << a.split) + 3) / 4;
+  a.zero_blocks = KIND == kStore && a.layout == EMB_TABLE ? zero_blocks(a.rows) : 0;
+  const unsigned grid = (unsigned)(a.blocks + a.zero_blocks);
   const uintptr_t at = reinterpret_cast<uintptr_t>(a.dy) | (uintptr_t)a.ld;
   const int vec = el * (int)(sizeof(TG));
   a.aligned = at % (uintptr_t)(vec < 16 ? vec : 16) == 0;
-  if (el == 1) k_token_reduce<TG, TW, 1, 8, KIND><<<grid, block, 0, s>>>(a);
-  else if (el == 4) k_token_reduce<TG, TW, 4, 8, KIND><<<grid, block, 0, s>>>(a);
-  else k_token_reduce<TG, TW, 8, 4, KIND><<<grid, block, 0, s>>>(a);
-  k_token_combine<TW, KIND><<<a.nchunks, 256, 0, s>>>(a);
+  // positions a batch: as many loads in flight as registers allow at four wavefronts a SIMD
+  constexpr int kB1 = 8, kB4 = KIND == kStore ? 16 : (KIND == kAdaElem ? 4 : 8), kB8 = KIND == kStore ? 8 : (KIND == kSgd ? 4 : 2);
+  if (el == 1) k_token_reduce<TG, TW, 1, kB1, KIND><<<grid, block, 0, s>>>(a);
+  else if (el == 4) k_token_reduce<TG, TW, 4, kB4, KIND><<<grid, block, 0, s>>>(a);
+  else k_token_reduce<TG, TW, 8, kB8, KIND><<<grid, block, 0, s>>>(a);
+  // (a long segment has more than one chunk)
+  if (a.nchunks > 1)
+    k_token_combine<TW, KIND><<<a.nchunks, a.D <= 256 ? kCombineLanes / 4 : kCombineLanes, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -546,8 +639,11 @@ hipError_t launch_token_grad(const TokenGradLaunch& p, hipStream_t s) {
   a.up.rounding = p.rounding;
   a.up.seed = p.seed;
   if (!p.fuse) {
-    if (p.layout == EMB_TABLE && p.rows > 0) k_token_zero<<<(unsigned)(((int64_t)p.rows + 255) / 256), 256, 0, s>>>(a);
-    if (p.N == 0) return hipGetLastError();
+    if (p.N == 0) {
+      if (p.layout == EMB_TABLE && p.rows > 0)
+        k_token_zero<<<(unsigned)zero_blocks(p.rows), 256, 0, s>>>(a);
+      return hipGetLastError();
+    }
     return p.dy_dtype == EMB_BF16 ? grad_kernels<bf16, float, kStore>(a, s) : grad_kernels<float, float, kStore>(a, s);
   }
   if (p.N == 0) return hipSuccess;

@@ -123,10 +123,11 @@ def _floats(t, shape, what: str) -> Optional[int]:
     """Address of a contiguous fp32 tensor of this shape, or None."""
     if t is None:
         return None
-    import torch
-    if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
+    if t.shape != shape or t.element_size() != 4 or not t.is_floating_point() or not t.is_contiguous():
         raise ValueError(f"{what} is a contiguous fp32 tensor of shape {shape}")
-    return _device(t, what).data_ptr()
+    if not t.is_cuda:
+        _device(t, what)
+    return t.data_ptr()
 
 
 # ---------------------------------------------------------------- tokens
