@@ -261,6 +261,18 @@ __device__ __forceinline__ void load_f32(const float* p, int col, float (&v)[V])
 #pragma unroll
   for (int i = 0; i < V; ++i) v[i] = p ? p[col + i] : 0.f;
 }
+// The same where few positions need it: the values are waited for here, in the
+// branch that needs them, not by all that comes after it (whose wait would be
+// for every load in flight).
+template <int V>
+__device__ __forceinline__ void load_rare(const float* p, int col, float (&v)[V]) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) v[i] = p ? p[col + i] : 0.f;
+  if (p) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) asm volatile("" : "+v"(v[i]));
+  }
+}
 
 // ---------------------------------------------------------------- forward
 
@@ -299,7 +311,10 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_fwd(Scan a) {
     const int64_t row = min(q0 + t, a.N - 1);
     gx[t].load(a.x, row, col);
     gf[t].load(a.f, row, col);
-    if constexpr (GATED) go[t].load(a.o, row, col);
+  }
+  if constexpr (GATED) {
+#pragma unroll
+    for (int t = 0; t < P; ++t) go[t].load(a.o, min(q0 + t, a.N - 1), col);
   }
   const Marks<P> mk(a, min(q0, a.N - 1), lane);
   load_f32<V>(a.bias, col, bias);
@@ -307,8 +322,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_fwd(Scan a) {
 #pragma unroll
     for (int t = 0; t < P; ++t) {
       if (t < n && mk.start(t)) {
-        float h0[V] = {};
-        if (a.h0) load_f32<V>(a.h0 + (int64_t)mk.of(t) * a.D, col, h0);
+        float h0[V];
+        load_rare<V>(a.h0 ? a.h0 + (int64_t)mk.of(t) * a.D : nullptr, col, h0);
 #pragma unroll
         for (int i = 0; i < V; ++i) B[i] = h0[i];
       }
@@ -473,8 +488,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_bwd(Scan a) {
     for (int t = 0; t < P; ++t) {
       if (t >= n) continue;
       if (mk.start(t)) {
-        float h0[V] = {};
-        if (a.h0) load_f32<V>(a.h0 + (int64_t)mk.of(t) * a.D, col, h0);
+        float h0[V];
+        load_rare<V>(a.h0 ? a.h0 + (int64_t)mk.of(t) * a.D : nullptr, col, h0);
 #pragma unroll
         for (int i = 0; i < V; ++i) B[i] = h0[i];
       }
@@ -488,8 +503,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_bwd(Scan a) {
     for (int t = P - 1; t >= 0; --t) {
       if (t >= n) continue;
       if (mk.end(t)) {
-        float g[V] = {};
-        if (a.dh_last) load_f32<V>(a.dh_last + (int64_t)mk.of(t) * a.D, col, g);
+        float g[V];
+        load_rare<V>(a.dh_last ? a.dh_last + (int64_t)mk.of(t) * a.D : nullptr, col, g);
 #pragma unroll
         for (int i = 0; i < V; ++i) B2[i] = g[i];
       }
@@ -548,8 +563,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_bwd(Scan a) {
 #pragma unroll
     for (int t = 0; t < P; ++t) {
       if (t < n && mk.start(t)) {
-        float h0[V] = {};
-        if (a.h0) load_f32<V>(a.h0 + (int64_t)mk.of(t) * a.D, col, h0);
+        float h0[V];
+        load_rare<V>(a.h0 ? a.h0 + (int64_t)mk.of(t) * a.D : nullptr, col, h0);
 #pragma unroll
         for (int i = 0; i < V; ++i) h[i] = h0[i];
       }
@@ -572,8 +587,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_bwd(Scan a) {
     for (int t = P - 1; t >= 0; --t) {
       if (t >= n) continue;
       if (mk.end(t)) {
-        float g[V] = {};
-        if (a.dh_last) load_f32<V>(a.dh_last + (int64_t)mk.of(t) * a.D, col, g);
+        float g[V];
+        load_rare<V>(a.dh_last ? a.dh_last + (int64_t)mk.of(t) * a.D : nullptr, col, g);
 #pragma unroll
         for (int i = 0; i < V; ++i) U[i] = g[i];
       }
