@@ -78,6 +78,13 @@ __device__ __forceinline__ float gate(float z) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * z));
 }
 
+// (kernels of their own for the two kinds of stores: behind a branch they become one)
+template <typename T, int V, bool STREAM>
+__device__ __forceinline__ void put(void* p, const float (&v)[V]) {
+  if constexpr (STREAM) Vec<T, V>::stream(p, v);
+  else Vec<T, V>::store(p, v);
+}
+
 // (A, B) applied to a state
 __device__ __forceinline__ float through(float A, float B, float h) {
   return A < 0.f ? B : __builtin_fmaf(A, h, B);
@@ -276,7 +283,7 @@ __device__ __forceinline__ void load_rare(const float* p, int col, float (&v)[V]
 
 // ---------------------------------------------------------------- forward
 
-template <typename T, int V, bool GATED>
+template <typename T, int V, bool GATED, bool STREAM>
 __global__ __launch_bounds__(kThreads, 4) void k_scan_fwd(Scan a) {
   constexpr int P = kFwdP;
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
@@ -410,7 +417,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_fwd(Scan a) {
     float y[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) y[i] = mk.begun(t) ? Bt[t][i] : __builtin_fmaf(At[t][i], h[i], Bt[t][i]);
-    if (in) Vec<T, V>::store(a.y.p + (int64_t)(q0 + t) * a.y.ld + (uint32_t)col * (uint32_t)(Vec<T, V>::kBytes / V), y);
+    if (in)
+      put<T, V, STREAM>(a.y.p + (int64_t)(q0 + t) * a.y.ld + (uint32_t)col * (uint32_t)(Vec<T, V>::kBytes / V), y);
     if (a.h_last && mk.end(t) && !mk.begun(t)) {
 #pragma unroll
       for (int i = 0; i < V; ++i) y[i] = __builtin_fmaf(Ae[i], h[i], Be[i]);
@@ -421,7 +429,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_fwd(Scan a) {
 
 // ---------------------------------------------------------------- backward
 
-template <typename T, typename TG, int V, bool GATED>
+template <typename T, typename TG, int V, bool GATED, bool STREAM>
 __global__ __launch_bounds__(kThreads, 4) void k_scan_bwd(Scan a) {
   constexpr int P = kBackP;
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
@@ -577,7 +585,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_bwd(Scan a) {
         if constexpr (GATED) dO[i] = v[t][i] * h[i];
       }
       if constexpr (GATED) {
-        if (in && t < n) Vec<TG, V>::store(a.dO.p + (int64_t)(q0 + t) * a.dO.ld + at, dO);
+        if (in && t < n) put<TG, V, STREAM>(a.dO.p + (int64_t)(q0 + t) * a.dO.ld + at, dO);
       }
     }
     float W[V], U[V];
@@ -639,8 +647,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_bwd(Scan a) {
       }
       if (in) {
         const int64_t row = q0 + t;
-        Vec<TG, V>::store(a.dx.p + row * a.dx.ld + at, dx);
-        Vec<TG, V>::store(a.df.p + row * a.df.ld + at, df);
+        put<TG, V, STREAM>(a.dx.p + row * a.dx.ld + at, dx);
+        put<TG, V, STREAM>(a.df.p + row * a.df.ld + at, df);
       }
       if (a.dh0 && mk.start(t) && !mk.closed(t)) {
 #pragma unroll
@@ -788,27 +796,37 @@ void clear(const Scan& a, hipStream_t s) {
   if (a.spans > 1) k_scan_clear<<<(unsigned)(blocks < 256 ? blocks : 256), 256, 0, s>>>(a.taken, n);
 }
 
-template <typename T, int V>
+template <typename T, int V, bool STREAM>
 hipError_t fwd(const ScanLaunch& p, hipStream_t s) {
   const Scan a = arguments(p, V, kFwdSpan);
   const unsigned blocks = (unsigned)(a.spans * a.slices) + empties(a, a.h_last);
   clear(a, s);
-  if (p.gated) k_scan_fwd<T, V, true><<<blocks, kThreads, 0, s>>>(a);
-  else k_scan_fwd<T, V, false><<<blocks, kThreads, 0, s>>>(a);
+  if (p.gated) k_scan_fwd<T, V, true, STREAM><<<blocks, kThreads, 0, s>>>(a);
+  else k_scan_fwd<T, V, false, STREAM><<<blocks, kThreads, 0, s>>>(a);
   return hipGetLastError();
 }
+template <typename T, int V>
+hipError_t fwd(const ScanLaunch& p, hipStream_t s) {
+  const bool big = p.N * p.D * (int64_t)(Vec<T, V>::kBytes / V) > kStreamBytes;
+  return big ? fwd<T, V, true>(p, s) : fwd<T, V, false>(p, s);
+}
 
-template <typename T, typename TG, int V>
+template <typename T, typename TG, int V, bool STREAM>
 hipError_t bwd(const ScanLaunch& p, hipStream_t s) {
   const Scan a = arguments(p, V, kSpan);
   const unsigned blocks = (unsigned)(a.spans * a.slices) + empties(a, a.dh0);
   clear(a, s);
-  if (p.gated) k_scan_bwd<T, TG, V, true><<<blocks, kThreads, 0, s>>>(a);
-  else k_scan_bwd<T, TG, V, false><<<blocks, kThreads, 0, s>>>(a);
+  if (p.gated) k_scan_bwd<T, TG, V, true, STREAM><<<blocks, kThreads, 0, s>>>(a);
+  else k_scan_bwd<T, TG, V, false, STREAM><<<blocks, kThreads, 0, s>>>(a);
   if (p.dbias)
     k_scan_dbias<<<(unsigned)((a.D + kBiasCols - 1) / kBiasCols), kBiasCols * kBiasRows, 0, s>>>(a.dbias, p.dbias, a.spans,
                                                                                              a.D);
   return hipGetLastError();
+}
+template <typename T, typename TG, int V>
+hipError_t bwd(const ScanLaunch& p, hipStream_t s) {
+  const bool big = p.N * p.D * (int64_t)(Vec<TG, V>::kBytes / V) > kStreamBytes;
+  return big ? bwd<T, TG, V, true>(p, s) : bwd<T, TG, V, false>(p, s);
 }
 
 template <typename T, int V>

@@ -4,7 +4,7 @@
 //   g_u    = scale * sum over sorted positions k of segment u of dy[perm[k]]
 //
 // Forward: a row is read by G lanes (a power of two, at most a block) as
-// vectors of V values; a lane has kAhead rows in flight.
+// vectors of V values; a lane has one or two rows in flight.
 //
 // Gradient: a wavefront walks the 64 sorted positions of one chunk for 64 * EL
 // columns, in batches whose rows (and the table rows of the segments that end
@@ -42,7 +42,7 @@ struct Stacked<true> {
   TableOffsets ro;
 };
 
-template <typename TW, typename TO, int V, int AHEAD, bool MANY>
+template <typename TW, typename TO, int V, int AHEAD, bool STREAM, bool MANY>
 __global__ __launch_bounds__(kFwdThreads) void k_token_fwd(TokFwd a, Stacked<MANY> st) {
   const int lanes = 1 << a.log_g, per = kFwdThreads >> a.log_g;
   const int c = (int)blockIdx.y * lanes + (int)(threadIdx.x & (lanes - 1));
@@ -85,14 +85,17 @@ __global__ __launch_bounds__(kFwdThreads) void k_token_fwd(TokFwd a, Stacked<MAN
 #pragma unroll
     for (int i = 0; i < V; ++i) x[i] = key[u] < a.rows ? a.scale * v[u].get(i) : 0.f;
     char* q = a.out + j * a.out_bytes + (int64_t)c * Vec<TO, V>::kBytes;
-    if (a.aligned) Vec<TO, V>::store(q, x);
-    else Vec<TO, V>::store_each(q, x);
+    if (!a.aligned) Vec<TO, V>::store_each(q, x);
+    else if constexpr (STREAM) Vec<TO, V>::stream(q, x);
+    else Vec<TO, V>::store(q, x);
   }
 }
 
 // ---------------------------------------------------------------- gradient
 
-enum Kind { kStore = 0, kSgd = 1, kAdaRow = 2, kAdaElem = 3 };
+// what becomes of a gradient row: stored (past the caches: kStream), or applied
+enum Kind { kStore, kStream, kSgd, kAdaRow, kAdaElem };
+constexpr bool stores(int kind) { return kind == kStore || kind == kStream; }
 constexpr int kMostSplit = 4, kSplitWaves = 8192;
 constexpr int kMostParts = 16;  // wavefronts of a block that share a chunk's columns (row-wise Adagrad)
 
@@ -176,6 +179,7 @@ __device__ __forceinline__ float wave_total(float x) {
 // Rows of the table that no token named: zeros.  One wavefront per kZeroRows
 // rows.
 constexpr int kZeroRows = 16;
+template <bool STREAM>
 __device__ __forceinline__ void zero_rows(const TokGrad& a, int64_t r0, int lane) {
   if (r0 >= (int64_t)a.rows) return;
   const int U = failed(a) ? 0 : a.num_unique[0];
@@ -190,7 +194,11 @@ __device__ __forceinline__ void zero_rows(const TokGrad& a, int64_t r0, int lane
   for (int r = 0; r < n; ++r) {
     if ((named >> r) & 1u) continue;
     float* dst = a.grad + (r0 + r) * (int64_t)a.D;
-    for (int c = lane * 4; c < a.D; c += kWave * 4) *reinterpret_cast<f32x4*>(dst + c) = f32x4{0.f, 0.f, 0.f, 0.f};
+    const float z[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int c = lane * 4; c < a.D; c += kWave * 4) {
+      if constexpr (STREAM) Vec<float, 4>::stream(dst + c, z);
+      else Vec<float, 4>::store(dst + c, z);
+    }
   }
 }
 
@@ -200,7 +208,7 @@ __device__ __forceinline__ int zero_blocks_before(const TokGrad& a, int b) {
 }
 
 // a finished gradient row's columns, where `layout` wants them
-template <int EL>
+template <int EL, bool STREAM>
 __device__ __forceinline__ void store_grad(const TokGrad& a, int u, uint32_t key, int col, bool in, float (&g)[EL]) {
   if (!in || (a.layout != EMB_ROWS && key >= a.rows)) return;
   float* dst = a.grad + (int64_t)(a.layout == EMB_ROWS ? (uint32_t)u : key) * a.D + col;
@@ -215,7 +223,8 @@ __device__ __forceinline__ void store_grad(const TokGrad& a, int u, uint32_t key
 #pragma unroll
     for (int e = 0; e < EL; ++e) g[e] += old.get(e);
   }
-  Vec<float, EL>::store(dst, g);
+  if constexpr (STREAM) Vec<float, EL>::stream(dst, g);
+  else Vec<float, EL>::store(dst, g);
 }
 
 // EL columns a lane, B positions a batch.  Row-wise Adagrad's blocks are the
@@ -226,11 +235,11 @@ template <typename TG, typename TW, int EL, int B, int KIND>
 __global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) void k_token_reduce(TokGrad a) {
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
   int block = blockIdx.x;
-  if constexpr (KIND == kStore) {
+  if constexpr (stores(KIND)) {
     // blocks of zeros come among the others evenly: these write while those wait for rows
     const int z = zero_blocks_before(a, block), more = zero_blocks_before(a, block + 1);
     if (more > z) {
-      zero_rows(a, ((int64_t)z * 4 + wave) * kZeroRows, lane);
+      zero_rows<KIND == kStream>(a, ((int64_t)z * 4 + wave) * kZeroRows, lane);
       return;
     }
     block -= z;
@@ -252,7 +261,7 @@ __global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) v
   const int p0 = c * kChunk, p1 = min(a.N, p0 + kChunk);
   const int b0 = p0 + sub * (kChunk >> a.split), b1 = min(p1, b0 + (kChunk >> a.split));
   if (failed(a)) {
-    if (KIND == kStore && a.layout == EMB_ROWS && in) {
+    if (stores(KIND) && a.layout == EMB_ROWS && in) {
       float z[EL] = {};
       for (int p = b0; p < b1; ++p) Vec<float, EL>::store(a.grad + (int64_t)p * a.D + col, z);
     }
@@ -287,10 +296,10 @@ __global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) v
   while (q < fin) {
     // a padding segment has no gradient: its positions are not read
     if (lane_at(keys, i) == a.pad) {
-      if constexpr (KIND == kStore) {
+      if constexpr (stores(KIND)) {
         if (!((heavy >> i) & 1u)) {
           float z[EL] = {};
-          store_grad<EL>(a, u0 + i, a.pad, col, in, z);
+          store_grad<EL, KIND == kStream>(a, u0 + i, a.pad, col, in, z);
         }
       }
       // (a batch may have ended inside it)
@@ -310,7 +319,7 @@ __global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) v
       if (a.aligned) g[k].load(src);
       else g[k].load_each(src);
     }
-    if constexpr (KIND == kStore) {
+    if constexpr (stores(KIND)) {
 #pragma unroll
       for (int k = 0; k < B; ++k) {
         if (k >= n) continue;
@@ -323,7 +332,7 @@ __global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) v
         if ((heavy >> i) & 1u) {
           if (in) Vec<float, EL>::store(a.partials + ((int64_t)c * 2 + (i == 0 ? 0 : 1)) * a.D + col, done);
         } else {
-          store_grad<EL>(a, u0 + i, lane_at(keys, i), col, in, done);
+          store_grad<EL, KIND == kStream>(a, u0 + i, lane_at(keys, i), col, in, done);
         }
         i = min(i + 1, kWave - 1);
       }
@@ -407,7 +416,7 @@ __global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) v
 }
 
 __global__ __launch_bounds__(256) void k_token_zero(TokGrad a) {
-  zero_rows(a, ((int64_t)blockIdx.x * 4 + threadIdx.x / kWave) * kZeroRows, threadIdx.x & (kWave - 1));
+  zero_rows<false>(a, ((int64_t)blockIdx.x * 4 + threadIdx.x / kWave) * kZeroRows, threadIdx.x & (kWave - 1));
 }
 
 // A segment of more than 64 positions: the partial rows of its chunks added in
@@ -435,8 +444,8 @@ __global__ __launch_bounds__(kCombineLanes) void k_token_combine(TokGrad a) {
   if (s < p0 || e - s <= kChunk) return;
   const uint32_t key = back ? k_prior : k_here;
   const bool pad = key == a.pad;
-  if (pad && KIND != kStore) return;
-  if (key >= a.rows && !(KIND == kStore && a.layout == EMB_ROWS)) return;
+  if (pad && !stores(KIND)) return;
+  if (key >= a.rows && !(stores(KIND) && a.layout == EMB_ROWS)) return;
   const int last = (e - 1) / kChunk;
   const int vectors = a.D / kCombineCols;
   const int lanes = blockDim.x, groups = vectors >= lanes ? 1 : lanes / vectors;
@@ -448,8 +457,8 @@ __global__ __launch_bounds__(kCombineLanes) void k_token_combine(TokGrad a) {
   float sq = 0.f;
   const float old = KIND == kAdaRow ? a.up.state[key] : 0.f;
   auto finish = [&](int col, float (&g)[kCombineCols], float step) {
-    if constexpr (KIND == kStore) {
-      store_grad<kCombineCols>(a, u, key, col, true, g);
+    if constexpr (stores(KIND)) {
+      store_grad<kCombineCols, false>(a, u, key, col, true, g);
     } else {
       Vec<TW, kCombineCols> w;
       Vec<float, kCombineCols> h;
@@ -534,19 +543,19 @@ hipError_t grad_kernels(TokGrad a, hipStream_t s) {
   a.split = 0;
   while (a.split < kMostSplit && ((int64_t)a.nchunks * a.parts << a.split) < kSplitWaves) ++a.split;
   a.blocks = kRow ? a.nchunks << a.split : ((a.nchunks * a.parts << a.split) + 3) / 4;
-  a.zero_blocks = KIND == kStore && a.layout == EMB_TABLE ? zero_blocks(a.rows) : 0;
+  a.zero_blocks = stores(KIND) && a.layout == EMB_TABLE ? zero_blocks(a.rows) : 0;
   const unsigned grid = (unsigned)(a.blocks + a.zero_blocks);
   const uintptr_t at = reinterpret_cast<uintptr_t>(a.dy) | (uintptr_t)a.ld;
   const int vec = el * (int)(sizeof(TG));
   a.aligned = at % (uintptr_t)(vec < 16 ? vec : 16) == 0;
   // positions a batch: as many loads in flight as registers allow at four wavefronts a SIMD
-  constexpr int kB1 = 8, kB4 = KIND == kStore ? 16 : (KIND == kAdaElem ? 4 : 8), kB8 = KIND == kStore ? 8 : (KIND == kSgd ? 4 : 2);
+  constexpr int kB1 = 8, kB4 = stores(KIND) ? 16 : (KIND == kAdaElem ? 4 : 8), kB8 = stores(KIND) ? 8 : (KIND == kSgd ? 4 : 2);
   if (el == 1) k_token_reduce<TG, TW, 1, kB1, KIND><<<grid, block, 0, s>>>(a);
   else if (el == 4) k_token_reduce<TG, TW, 4, kB4, KIND><<<grid, block, 0, s>>>(a);
   else k_token_reduce<TG, TW, 8, kB8, KIND><<<grid, block, 0, s>>>(a);
   // (a long segment has more than one chunk)
   if (a.nchunks > 1)
-    k_token_combine<TW, KIND><<<a.nchunks, a.D <= 256 ? kCombineLanes / 4 : kCombineLanes, 0, s>>>(a);
+    k_token_combine<TW, KIND == kStream ? kStore : KIND><<<a.nchunks, a.D <= 256 ? kCombineLanes / 4 : kCombineLanes, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -565,13 +574,14 @@ void fwd_kernel(TokFwd a, const Stacked<MANY>& st, hipStream_t s) {
   a.log_g = lg;
   const int per = kFwdThreads >> lg;
   const unsigned parts = (unsigned)((a.vectors + (1 << lg) - 1) >> lg);
-  // four rows a lane in flight once one row a lane would fill the device
-  if (a.N * parts / per >= 2048) {
-    const dim3 grid((unsigned)((a.N + per * 4 - 1) / (per * 4)), parts);
-    k_token_fwd<TW, TO, V, 4, MANY><<<grid, kFwdThreads, 0, s>>>(a, st);
+  // outputs that are streamed fill the device with two rows a lane in flight (as fast as one or four there, eight are
+  // 7% slower); smaller ones spread over as many lanes as they can
+  if (a.N * a.vectors * Vec<TO, V>::kBytes > kStreamBytes) {
+    const dim3 grid((unsigned)((a.N + per * 2 - 1) / (per * 2)), parts);
+    k_token_fwd<TW, TO, V, 2, true, MANY><<<grid, kFwdThreads, 0, s>>>(a, st);
   } else {
     const dim3 grid((unsigned)((a.N + per - 1) / per), parts);
-    k_token_fwd<TW, TO, V, 1, MANY><<<grid, kFwdThreads, 0, s>>>(a, st);
+    k_token_fwd<TW, TO, V, 1, false, MANY><<<grid, kFwdThreads, 0, s>>>(a, st);
   }
 }
 
@@ -644,6 +654,8 @@ hipError_t launch_token_grad(const TokenGradLaunch& p, hipStream_t s) {
         k_token_zero<<<(unsigned)zero_blocks(p.rows), 256, 0, s>>>(a);
       return hipGetLastError();
     }
+    if ((p.layout == EMB_TABLE ? (int64_t)p.rows : (int64_t)p.N) * p.D * 4 > kStreamBytes)
+      return p.dy_dtype == EMB_BF16 ? grad_kernels<bf16, float, kStream>(a, s) : grad_kernels<float, float, kStream>(a, s);
     return p.dy_dtype == EMB_BF16 ? grad_kernels<bf16, float, kStore>(a, s) : grad_kernels<float, float, kStore>(a, s);
   }
   if (p.N == 0) return hipSuccess;
