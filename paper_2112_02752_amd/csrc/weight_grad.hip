@@ -287,14 +287,46 @@ __global__ __launch_bounds__(kThreads, G == 2 ? 1 : 2) void k_weight_grad(WArgs 
   }
 }
 
+// The parts' sums, in order; four values a lane where the rows of dw allow it.
+// Bound by latency: eight parts' values are in flight together.
+template <int V>
 __global__ __launch_bounds__(256) void k_weight_parts(const float* parts, float* dw, int64_t n, int count, int add) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    float t = 0.f;
-    for (int p = 0; p < count; ++p) t += parts[(int64_t)p * n + i];
-    dw[i] = add ? dw[i] + t : t;
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V; i < n; i += (int64_t)gridDim.x * 256 * V) {
+    float t[V] = {};
+    constexpr int kAhead = 8;
+    for (int p = 0; p < count; p += kAhead) {
+      Vec<float, V> x[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        if (p + k < count) x[k].load(parts + (int64_t)(p + k) * n + i);
+        else x[k].zero();
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+        for (int v = 0; v < V; ++v) t[v] += x[k].get(v);
+    }
+    if (add) {
+      Vec<float, V> old;
+      old.load(dw + i);
+#pragma unroll
+      for (int v = 0; v < V; ++v) t[v] += old.get(v);
+    }
+    Vec<float, V>::store(dw + i, t);
   }
 }
 
+// Tiles of 128 x 128 with the rows cut into as many parts as give each compute
+// unit a block, of at least six steps.  2048 x 512 x 1536: 19.1 us (20.9 with
+// twice the blocks and four steps), 512 x 2048 x 2048: 16.0 (26.8), 8192 x 512 x
+// 1536: 36.2 (32.5), 2048 x 256 x 256: 14.1 (12.3).
+constexpr int kSmallBlocks = 256, kSmallSteps = 6;
+// Tiles of 256 x 256 where parts of at least 16 steps make more than 128 blocks
+// (us, these tiles against the small ones): 32768 x 2048 x 6144 855 (1102),
+// 32768 x 1024 x 1024 92 (128), 8192 x 2048 x 2048 92 (123), 2048 x 2048 x 6144
+// 71 (84); with 128 blocks or fewer 2048 x 2048 x 2048 49 (38), 8192 x 1024 x 1024
+// 47 (45), 8192 x 512 x 512 40 (21).
+constexpr int kBigBlocks = 256, kBigSteps = 16, kBigLeast = 129;
 struct Plan {
   int groups, parts, steps;  // groups of 128 columns a tile has each way; parts of so many steps
 };
@@ -308,10 +340,10 @@ Plan plan_for(int64_t N, int32_t K, int32_t F, bool small) {
     const int64_t per = (steps + p - 1) / p;
     return Plan{(int)(tile / kGroup), (int)(per > 0 ? (steps + per - 1) / per : 1), (int)per};
   };
-  const Plan big = cut(2 * kGroup, 256, 16);
+  const Plan big = cut(2 * kGroup, kBigBlocks, kBigSteps);
   const int64_t tiles = (int64_t)((K + 255) / 256) * ((F + 255) / 256);
-  if (!small && big.parts * tiles >= 128) return big;
-  Plan s = cut(kGroup, 512, 4);
+  if (!small && big.parts * tiles >= kBigLeast) return big;
+  Plan s = cut(kGroup, kSmallBlocks, kSmallSteps);
   if (s.parts < 1) s.parts = 1;
   return s;
 }
@@ -349,8 +381,11 @@ hipError_t launch_weight_grad(const WeightGradLaunch& p, hipStream_t s) {
   else k_weight_grad<1, 1, true><<<blocks, kThreads, 0, s>>>(a);
   if (a.parts > 1) {
     const int64_t n = (int64_t)p.K * p.F;
-    k_weight_parts<<<(unsigned)((n + 255) / 256 < 4096 ? (n + 255) / 256 : 4096), 256, 0, s>>>(p.ws, p.dw, n, a.parts,
-                                                                                               p.add);
+    const bool four = n % 4 == 0 && (reinterpret_cast<uintptr_t>(p.dw) & 15u) == 0;
+    const int64_t want = (four ? n / 4 + 255 : n + 255) / 256;
+    const unsigned grid = (unsigned)(want < 8192 ? want : 8192);
+    if (four) k_weight_parts<4><<<grid, 256, 0, s>>>(p.ws, p.dw, n, a.parts, p.add);
+    else k_weight_parts<1><<<grid, 256, 0, s>>>(p.ws, p.dw, n, a.parts, p.add);
   }
   return hipGetLastError();
 }
