@@ -754,5 +754,5 @@ class Pipeline:
                 raise StepFailed(*st)
 
 
-from .sequence import (Checkpoint, Mat, Recurrence, Scan, TokenLayer, scan_step, scan_workspace_size,  # noqa: E402
-                       token_fwd, token_grad)
+from .sequence import (Checkpoint, Mat, Recurrence, Scan, SequenceLayer, TokenLayer, scan_step,  # noqa: E402
+                       scan_workspace_size, token_fwd, token_grad)

@@ -67,14 +67,14 @@ class Mat:
     tensor's columns); an 8-bit one comes from ``Checkpoint.columns``.  Kept by
     a program between calls, it costs a call one address check."""
 
-    __slots__ = ("tensor", "exps", "rows", "cols", "_c", "_at", "ref", "_first")
+    __slots__ = ("tensor", "exps", "rows", "cols", "_c", "_at", "ref")
 
-    def __init__(self, tensor, exps=None, first: int = 0, cols: Optional[int] = None):
+    def __init__(self, tensor, exps=None, cols: Optional[int] = None):
         import torch
         if tensor.dim() != 2 or (tensor.shape[1] > 1 and tensor.stride(1) != 1):
             raise ValueError("a matrix has two dimensions and contiguous columns")
         _device(tensor, "a matrix")
-        self.tensor, self.exps, self._first = tensor, exps, first
+        self.tensor, self.exps = tensor, exps
         self.rows = int(tensor.shape[0])
         self.cols = int(tensor.shape[1]) if cols is None else cols
         ld = int(tensor.stride(0)) if self.rows > 1 else max(int(tensor.stride(0)), int(tensor.shape[1]))
@@ -101,9 +101,9 @@ class Mat:
         at = self.tensor.data_ptr()
         if at != self._at:
             self._at = at
-            self._c.data = at + self._first if at else None
+            self._c.data = at or None
             if self.exps is not None:
-                self._c.exps = self.exps.data_ptr() + self._first // GROUP
+                self._c.exps = self.exps.data_ptr()
         return self._c
 
 
@@ -375,14 +375,14 @@ class Checkpoint:
 
     def _take(self, codes, exps, dim: int) -> None:
         self.codes, self.exps, self.dim, self.rows = codes, exps, dim, int(codes.shape[0])
-        self.mat = Mat(codes, exps, 0, dim)
+        self.mat = Mat(codes, exps, dim)
         self._ws = None
 
     def columns(self, first: int, count: int) -> Mat:
         """Columns first .. first + count - 1 as a matrix (for ``Scan``)."""
         if first % GROUP != 0 or first < 0 or count < 1 or first + count > self.dim:
             raise ValueError("columns of a checkpoint start at a group's first")
-        return Mat(self.codes[:, first:], self.exps[:, first // GROUP:], 0, count)
+        return Mat(self.codes[:, first:], self.exps[:, first // GROUP:], count)
 
     def pack(self, src, stream=None) -> None:
         src = _mat(src)
@@ -407,3 +407,95 @@ class Checkpoint:
         _check("emb_weight_grad", lib().emb_weight_grad(
             self.rows, self.dim, dy.cols, self.mat.ref, dy.ref, _floats(dw, (self.dim, dy.cols), "dw"), int(add),
             _ptr(self._ws) if size else None, size, _stream(stream)))
+
+
+# ---------------------------------------------------------------- together
+
+class SequenceLayer:
+    """A sequence layer over the tables: token rows, a projection to values,
+    forget gates and output gates, the gated recurrence.
+
+        rows = scale * W[token]                    (N x D, bf16)
+        x | f | o = rows @ weight                  (N x 3H, bf16)
+        y = sigmoid(o) * scan(x, f + bias)         (N x H, bf16)
+
+    A training step is ``forward``, the caller's loss, ``backward``.  Between
+    the two only checkpoints are kept, in 8 bits: of the rows (for the
+    projection's weight gradient) and of the projection (for the recurrence's
+    backward), 1.03 bytes a value instead of 2; the full-width buffers serve
+    every call.  ``step`` is one token of each running sequence (serving), with
+    states in a pool of slots.
+
+    ``weight`` is a bf16 D x 3H tensor and ``bias`` an fp32 one of H values, both
+    the caller's: ``backward`` leaves their gradients in fp32 and trains the
+    tables' rows itself (TokenLayer.update).  H is a multiple of 32."""
+
+    def __init__(self, tables: Tables, weight, bias, max_tokens: int, max_seqs: int, scale: float = 1.0,
+                 pad_row: int = -1, opt: str = "adagrad", lr: float = 0.01, eps: float = 1e-8, state=None,
+                 rounding: str = "nearest", seed: int = 0):
+        import torch
+        dim, cols = (int(x) for x in weight.shape)
+        if weight.dtype != torch.bfloat16 or cols % (3 * GROUP) != 0 or dim != int(tables.weights.shape[1]):
+            raise ValueError("weight is a bf16 D x 3H tensor, H a multiple of 32")
+        self.dim, self.hidden = dim, cols // 3
+        self.weight, self.bias = weight, bias
+        dev = tables.weights.device
+        self.tokens = TokenLayer(tables, scale=scale, pad_row=pad_row, opt=opt, lr=lr, eps=eps, state=state,
+                                 max_tokens=max_tokens, max_seqs=max_seqs, rounding=rounding, seed=seed)
+        self.recurrence = Recurrence(max_tokens, max_seqs, self.hidden, dev)
+        b16 = dict(dtype=torch.bfloat16, device=dev)
+        self._rows = torch.empty((max_tokens, dim), **b16)
+        self._proj = torch.empty((max_tokens, cols), **b16)
+        self._saved = None
+        self._n = -1
+
+    def _project(self, batch: Batch, n: int):
+        import torch
+        rows, proj = self._rows[:n], self._proj[:n]
+        self.tokens.forward(batch, rows)
+        torch.mm(rows, self.weight, out=proj)
+        return rows, proj, [Mat(proj[:, i * self.hidden:(i + 1) * self.hidden]) for i in range(3)]
+
+    def forward(self, batch: Batch, y, h_last=None, h0=None, train: bool = True) -> None:
+        """y (N x H, bf16) and the state after each sequence (fp32 M x H) of
+        the batch's sequences, from first states ``h0`` or zero; with ``train``
+        what the backward needs is kept.  Runs on the current stream."""
+        n = int(batch.indices.numel())
+        if n > self.recurrence.max_tokens:
+            raise ValueError("batch larger than the layer's buffers")
+        rows, proj, parts = self._project(batch, n)
+        self.recurrence.forward(Scan(batch.offsets, *parts, bias=self.bias, h0=h0), y, h_last)
+        self._n = -1
+        if train:
+            if self._saved is None or self._saved[0].rows != n:
+                self._saved = (Checkpoint(n, self.dim, rows.device), Checkpoint(n, 3 * self.hidden, rows.device))
+            self._saved[0].pack(rows)
+            self._saved[1].pack(proj)
+            self._n, self._h0 = n, h0
+
+    def backward(self, batch: Batch, dy, dweight, dbias, dh_last=None, dh0=None, add: bool = False) -> None:
+        """Backward of the last ``forward``, whose batch this is: the gradients of
+        the weights (fp32 D x 3H, with ``add`` added to what is there) and the
+        bias (fp32), and the optimizer's step on the table rows."""
+        import torch
+        n, H = int(batch.indices.numel()), self.hidden
+        if n != self._n:
+            raise ValueError("backward follows a training forward of the same batch")
+        self._n = -1
+        saved_rows, saved_proj = self._saved
+        scan = Scan(batch.offsets, *(saved_proj.columns(i * H, H) for i in range(3)), bias=self.bias, h0=self._h0)
+        dproj, drows = self._proj[:n], self._rows[:n]
+        self.recurrence.backward(scan, dy, *(Mat(dproj[:, i * H:(i + 1) * H]) for i in range(3)), dbias=dbias,
+                                 dh_last=dh_last, dh0=dh0)
+        saved_rows.weight_grad(dproj, dweight, add=add)
+        torch.mm(dproj, self.weight.t(), out=drows)
+        self.tokens.update(batch, drows)
+
+    def step(self, batch: Batch, state, y, slots=None) -> None:
+        """The next token of each running sequence (one a sequence in
+        ``batch``): y (N x H, bf16), the states updated in their slots."""
+        n = int(batch.indices.numel())
+        if n > self.recurrence.max_tokens:
+            raise ValueError("batch larger than the layer's buffers")
+        _, _, (x, f, o) = self._project(batch, n)
+        scan_step(x, f, o, state, y, bias=self.bias, slots=slots)
