@@ -16,6 +16,11 @@
 // consecutive columns of dw.
 //
 // Few tiles of dw: the rows are cut into parts whose sums are added in order.
+//
+// Bound: 2 N K F operations on the matrix units.  32768 x 2048 x 6144 (bf16 dy):
+// 785 us, 1050 TFLOP/s, of 1216 that a library product of 8192^3 reaches; the four
+// parts' sums are 75 us of it.  2048 x 512 x 1536: 19 us, of which the products
+// take 15 (six steps a block, each a wait for memory) and the parts' sums 4.
 #include "seq_common.h"
 
 namespace emb {
@@ -29,6 +34,7 @@ constexpr int kStep = 64;   // rows a step takes
 constexpr int kOct = kStep / 8;
 constexpr int kGroup = 128;  // columns of an LDS group
 constexpr int kThreads = 256;
+constexpr int kBand = 8;     // tiles
 
 struct WArgs {
   const char* x;
@@ -162,8 +168,18 @@ __global__ __launch_bounds__(kThreads, G == 2 ? 1 : 2) void k_weight_grad(WArgs 
   __shared__ u32x4 s_x[kBufs][kOct][G * kGroup], s_y[kBufs][SPLIT][kOct][G * kGroup];
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
   const int tiles = a.tiles_k * a.tiles_f;
-  const int tile = blockIdx.x % tiles, part = blockIdx.x / tiles;
-  const int k0 = tile % a.tiles_k * kTile, c0 = tile / a.tiles_k * kTile;
+  int at = (int)blockIdx.x;
+  if constexpr (G == 2) {
+    // Blocks go to the eight XCDs in turn: an XCD takes neighbouring tiles, which read the same columns
+    // (32768 x 2048 x 6144 811 us, 846 with every XCD reading all of dy; small tiles wait for memory and gain nothing)
+    const int each = (int)gridDim.x / 8;
+    if (at < 8 * each) at = at % 8 * each + at / 8;
+  }
+  const int tile = at % tiles, part = at / tiles;
+  // (tiles in bands of eight down the columns of x: 32 neighbours read some eight column groups of x and four of dy)
+  const int band = tile / (kBand * a.tiles_f), in_band = tile - band * kBand * a.tiles_f;
+  const int high = min(kBand, a.tiles_k - band * kBand);
+  const int k0 = (band * kBand + in_band % high) * kTile, c0 = in_band / high * kTile;
   const int quad = threadIdx.x % 32, oct = threadIdx.x / 32;
   const int64_t r_begin = (int64_t)part * a.steps_per_part * kStep;
   const int64_t r_end = min((int64_t)a.N, r_begin + (int64_t)a.steps_per_part * kStep);
@@ -321,12 +337,20 @@ __global__ __launch_bounds__(256) void k_weight_parts(const float* parts, float*
 // twice the blocks and four steps), 512 x 2048 x 2048: 16.0 (26.8), 8192 x 512 x
 // 1536: 36.2 (32.5), 2048 x 256 x 256: 14.1 (12.3).
 constexpr int kSmallBlocks = 256, kSmallSteps = 6;
-// Tiles of 256 x 256 where parts of at least 16 steps make more than 128 blocks
-// (us, these tiles against the small ones): 32768 x 2048 x 6144 855 (1102),
-// 32768 x 1024 x 1024 92 (128), 8192 x 2048 x 2048 92 (123), 2048 x 2048 x 6144
-// 71 (84); with 128 blocks or fewer 2048 x 2048 x 2048 49 (38), 8192 x 1024 x 1024
-// 47 (45), 8192 x 512 x 512 40 (21).
+// Tiles of 256 x 256 (one block a compute unit: 256 sums a lane, 128 KB of LDS)
+// where parts of at least 16 steps make more than 128 blocks (us, these tiles
+// against the small ones): 32768 x 2048 x 6144 855 (1102), 32768 x 1024 x 1024 92
+// (128), 8192 x 2048 x 2048 92 (123), 2048 x 2048 x 6144 71 (84); with 128 blocks
+// or fewer 2048 x 2048 x 2048 49 (38), 8192 x 1024 x 1024 47 (45), 8192 x 512 x 512
+// 40 (21).
 constexpr int kBigBlocks = 256, kBigSteps = 16, kBigLeast = 129;
+// As many parts as fill one to four rounds of blocks, whichever is estimated to
+// take least: a step costs 0.85 us, and 1 us more the more compute units are busy
+// (the clock falls), a part's sums 1.8 us a million.  192 tiles of 512 steps: four
+// parts in three full rounds 785 us, one part 811; 96 tiles of 512 steps 416 (434);
+// 96 tiles of 256 steps stay at two parts, 231 (251 with five).
+constexpr int kMostRounds = 4;
+constexpr double kStepUs = 0.85, kBusyUs = 1.0, kPartUs = 1.8e-6;
 struct Plan {
   int groups, parts, steps;  // groups of 128 columns a tile has each way; parts of so many steps
 };
@@ -342,7 +366,19 @@ Plan plan_for(int64_t N, int32_t K, int32_t F, bool small) {
   };
   const Plan big = cut(2 * kGroup, kBigBlocks, kBigSteps);
   const int64_t tiles = (int64_t)((K + 255) / 256) * ((F + 255) / 256);
-  if (!small && big.parts * tiles >= kBigLeast) return big;
+  if (!small && big.parts * tiles >= kBigLeast) {
+    Plan best{};
+    double least = 0.;
+    for (int r = 1; r <= kMostRounds; ++r) {
+      const Plan q = cut(2 * kGroup, r * kBigBlocks, kBigSteps);
+      const int64_t blocks = q.parts * tiles, rounds = (blocks + kBigBlocks - 1) / kBigBlocks;
+      const double busy = (double)blocks / (double)(rounds * kBigBlocks);
+      const double us = (double)(rounds * q.steps) * (kStepUs + kBusyUs * busy) +
+                        (q.parts > 1 ? (double)q.parts * K * F * kPartUs : 0.);
+      if (r == 1 || us < least) best = q, least = us;
+    }
+    return best;
+  }
   Plan s = cut(kGroup, kSmallBlocks, kSmallSteps);
   if (s.parts < 1) s.parts = 1;
   return s;
