@@ -260,20 +260,28 @@ __global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) v
   const int cs = in ? col : 0;
   const int p0 = c * kChunk, p1 = min(a.N, p0 + kChunk);
   const int b0 = p0 + sub * (kChunk >> a.split), b1 = min(p1, b0 + (kChunk >> a.split));
-  if (failed(a)) {
+  // What a chunk needs comes in as few dependent loads as there can be: the
+  // dedup's state, its counts and the positions' rows; then the segments.  Until
+  // the state is known to be sound the counts only index after being clamped.
+  const WsHeader* h = static_cast<const WsHeader*>(a.hdr);
+  const uint32_t gen = h->gen;
+  const uint64_t err = __hip_atomic_load(&h->err, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  int U = a.num_unique[0], u0 = a.chunk_seg[c];
+  const int row_a = a.perm[min(p0 + lane, a.N - 1)], row_b = a.perm[min(p0 + kChunk + lane, a.N - 1)];
+  asm volatile("" : "+v"(U), "+v"(u0) : "v"(row_a), "v"(row_b));
+  U = uniform(min(max(U, 1), a.N));
+  u0 = uniform(min(max(u0, 0), U - 1));
+  // lane l: the end of segment u0 + l, its key; positions' rows (a segment that starts here ends before p1 + 64)
+  const int s0 = uniform(a.seg[u0]);
+  const int ends = a.seg[min(u0 + 1 + lane, U)];
+  const uint32_t keys = a.ukeys[min(u0 + lane, U - 1)];
+  if ((err_bits_of(err, gen) & kDedupErrors) != 0u) {
     if (stores(KIND) && a.layout == EMB_ROWS && in) {
       float z[EL] = {};
       for (int p = b0; p < b1; ++p) Vec<float, EL>::store(a.grad + (int64_t)p * a.D + col, z);
     }
     return;
   }
-  const int U = a.num_unique[0];
-  const int u0 = uniform(a.chunk_seg[c]);
-  const int s0 = uniform(a.seg[u0]);
-  // lane l: the end of segment u0 + l, its key; positions' rows (a segment that starts here ends before p1 + 64)
-  const int ends = a.seg[min(u0 + 1 + lane, U)];
-  const uint32_t keys = a.ukeys[min(u0 + lane, U - 1)];
-  const int row_a = a.perm[min(p0 + lane, a.N - 1)], row_b = a.perm[min(p0 + kChunk + lane, a.N - 1)];
   const int before = __shfl_up(ends, 1, kWave);
   const int len = ends - (lane == 0 ? s0 : before);
   const uint64_t heavy = __ballot(len > kChunk);
@@ -285,11 +293,10 @@ __global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) v
   if (i > last) return;
   const int fin = (heavy >> last) & 1u ? min(p1, lane_at(ends, last)) : lane_at(ends, last);
   int q = i == 0 ? p0 : lane_at(ends, i - 1);
-  // the row-wise accumulators of the segments, a lane each, read before any wavefront of the block writes one
+  // the row-wise accumulators of the segments, a lane each
   float accum = 0.f;
   if constexpr (KIND == kAdaRow) {
     if (keys < a.rows) accum = a.up.state[keys];
-    asm volatile("" : "+v"(accum)::"memory");
   }
   float acc[EL] = {};
   int parity = 0;
@@ -383,7 +390,9 @@ __global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) v
           total[k] = wave_total(in ? sq : 0.f);
         }
         if (a.parts > 1) {
-          // (a batch's sums are read before the batch after next is summed, a barrier later)
+          // (the accumulators are here before any wavefront of the block writes one; a batch's sums are read before the
+          // batch after next is summed, a barrier later)
+          asm volatile("" : "+v"(accum)::"memory");
           if (lane == 0) {
 #pragma unroll
             for (int k = 0; k < B; ++k) s_sq[parity][wave][k] = total[k];
