@@ -227,6 +227,40 @@ __device__ __forceinline__ void store_grad(const TokGrad& a, int u, uint32_t key
   else Vec<float, EL>::store(dst, g);
 }
 
+// Chunk c's positions and segments.  They come in as few dependent loads as
+// there can be: the dedup's state, its counts and the positions' rows; then the
+// segments.  Until the state is known to be sound the counts only index after
+// being clamped.
+struct Chunk {
+  bool failed;
+  int u0, s0;          // the segment that holds the chunk's first position, its beginning
+  int ends;            // lane l: the end of segment u0 + l
+  uint32_t keys;       // its key
+  int row_a, row_b;    // rows of the chunk's positions and the next one's (a segment that starts here ends before those end)
+  uint64_t heavy;      // segments of more than a chunk's positions
+  __device__ __forceinline__ Chunk(const TokGrad& a, int c, int lane) {
+    const int p0 = c * kChunk;
+    const WsHeader* h = static_cast<const WsHeader*>(a.hdr);
+    const uint32_t gen = h->gen;
+    const uint64_t err = __hip_atomic_load(&h->err, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    int U = a.num_unique[0];
+    u0 = a.chunk_seg[c];
+    row_a = a.perm[min(p0 + lane, a.N - 1)], row_b = a.perm[min(p0 + kChunk + lane, a.N - 1)];
+    asm volatile("" : "+v"(U), "+v"(u0) : "v"(row_a), "v"(row_b));
+    U = uniform(min(max(U, 1), a.N));
+    u0 = uniform(min(max(u0, 0), U - 1));
+    s0 = uniform(a.seg[u0]);
+    ends = a.seg[min(u0 + 1 + lane, U)];
+    keys = a.ukeys[min(u0 + lane, U - 1)];
+    failed = (err_bits_of(err, gen) & kDedupErrors) != 0u;
+    const int before = __shfl_up(ends, 1, kWave);
+    heavy = __ballot(ends - (lane == 0 ? s0 : before) > kChunk);
+  }
+  __device__ __forceinline__ int row(int pos) const {
+    return pos < kWave ? lane_at(row_a, pos) : lane_at(row_b, pos - kWave);
+  }
+};
+
 // EL columns a lane, B positions a batch.  Row-wise Adagrad's blocks are the
 // `parts` wavefronts of one chunk, which add up their rows' squares through
 // LDS; others are four wavefronts of any.  EMB_TABLE's zeros are written by
@@ -260,31 +294,17 @@ __global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) v
   const int cs = in ? col : 0;
   const int p0 = c * kChunk, p1 = min(a.N, p0 + kChunk);
   const int b0 = p0 + sub * (kChunk >> a.split), b1 = min(p1, b0 + (kChunk >> a.split));
-  // What a chunk needs comes in as few dependent loads as there can be: the
-  // dedup's state, its counts and the positions' rows; then the segments.  Until
-  // the state is known to be sound the counts only index after being clamped.
-  const WsHeader* h = static_cast<const WsHeader*>(a.hdr);
-  const uint32_t gen = h->gen;
-  const uint64_t err = __hip_atomic_load(&h->err, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  int U = a.num_unique[0], u0 = a.chunk_seg[c];
-  const int row_a = a.perm[min(p0 + lane, a.N - 1)], row_b = a.perm[min(p0 + kChunk + lane, a.N - 1)];
-  asm volatile("" : "+v"(U), "+v"(u0) : "v"(row_a), "v"(row_b));
-  U = uniform(min(max(U, 1), a.N));
-  u0 = uniform(min(max(u0, 0), U - 1));
-  // lane l: the end of segment u0 + l, its key; positions' rows (a segment that starts here ends before p1 + 64)
-  const int s0 = uniform(a.seg[u0]);
-  const int ends = a.seg[min(u0 + 1 + lane, U)];
-  const uint32_t keys = a.ukeys[min(u0 + lane, U - 1)];
-  if ((err_bits_of(err, gen) & kDedupErrors) != 0u) {
+  const Chunk ch(a, c, lane);
+  if (ch.failed) {
     if (stores(KIND) && a.layout == EMB_ROWS && in) {
       float z[EL] = {};
       for (int p = b0; p < b1; ++p) Vec<float, EL>::store(a.grad + (int64_t)p * a.D + col, z);
     }
     return;
   }
-  const int before = __shfl_up(ends, 1, kWave);
-  const int len = ends - (lane == 0 ? s0 : before);
-  const uint64_t heavy = __ballot(len > kChunk);
+  const int u0 = ch.u0, s0 = ch.s0, ends = ch.ends;
+  const uint32_t keys = ch.keys;
+  const uint64_t heavy = ch.heavy;
   // the segments that start in b0 .. b1 - 1, and with them a long one's piece that came in with the chunk; a light
   // segment that came in belongs to another wavefront
   const bool came_in = s0 < p0 && sub == 0 && (heavy & 1u);
@@ -321,7 +341,7 @@ __global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) v
 #pragma unroll
     for (int k = 0; k < B; ++k) {
       const int pos = min(q + k, fin - 1) - p0;
-      const int row = pos < kWave ? lane_at(row_a, pos) : lane_at(row_b, pos - kWave);
+      const int row = ch.row(pos);
       const char* src = a.dy + (int64_t)row * a.ld + (uint32_t)cs * (uint32_t)(Vec<TG, EL>::kBytes / EL);
       if (a.aligned) g[k].load(src);
       else g[k].load_each(src);
@@ -421,6 +441,115 @@ __global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) v
       }
     }
     q += n;
+  }
+}
+
+// The same for few positions, whose time is that of dependent loads and of
+// fetching the code: a wavefront to each position and part of the columns, for
+// the segment that starts there or the long one's piece that came in with the
+// chunk, all of whose loads but those of later batches are in flight together.
+template <typename TG, typename TW, int EL, int B, int KIND>
+__global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) void k_token_reduce_each(TokGrad a) {
+  const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
+  int block = blockIdx.x;
+  if constexpr (stores(KIND)) {
+    const int z = zero_blocks_before(a, block), more = zero_blocks_before(a, block + 1);
+    if (more > z) {
+      zero_rows<KIND == kStream>(a, ((int64_t)z * 4 + wave) * kZeroRows, lane);
+      return;
+    }
+    block -= z;
+  }
+  int p, part;
+  if constexpr (KIND == kAdaRow) {
+    p = block, part = wave;
+  } else {
+    p = block * 4 + wave;
+    part = p % a.parts, p /= a.parts;
+  }
+  __shared__ float s_sq[kMostParts];
+  if (p >= a.N) return;
+  const int col = (part * kWave + lane) * EL;
+  const bool in = col < a.D;
+  const int cs = in ? col : 0;
+  const int c = p / kChunk, p0 = c * kChunk;
+  const Chunk ch(a, c, lane);
+  if (ch.failed) {
+    if (stores(KIND) && a.layout == EMB_ROWS && in) {
+      float z[EL] = {};
+      Vec<float, EL>::store(a.grad + (int64_t)p * a.D + col, z);
+    }
+    return;
+  }
+  int i = 0;
+  if (p != p0 || (ch.s0 < p0 && !(ch.heavy & 1u))) {
+    const uint64_t starts = __ballot(ch.ends == p);
+    if (starts == 0u) return;
+    i = (int)__builtin_ctzll(starts) + 1;
+  }
+  const bool longs = (ch.heavy >> i) & 1u;
+  const int fin = longs ? min(min(a.N, p0 + kChunk), lane_at(ch.ends, i)) : lane_at(ch.ends, i);
+  const uint32_t key = lane_at(ch.keys, i);
+  float acc[EL] = {};
+  if (key == a.pad) {
+    if constexpr (stores(KIND)) {
+      if (!longs) store_grad<EL, KIND == kStream>(a, ch.u0 + i, key, col, in, acc);
+    }
+    return;
+  }
+  const bool applies = !stores(KIND) && !longs && key < a.rows;
+  Vec<TW, EL> w;
+  Vec<float, EL> h;
+  float accum = 0.f;
+  if constexpr (!stores(KIND)) {
+    if (applies) {
+      w.load(static_cast<const char*>(a.up.W) + ((int64_t)key * a.D + cs) * (int64_t)sizeof(TW));
+      if constexpr (KIND == kAdaElem) h.load(a.up.state + (int64_t)key * a.D + cs);
+      if constexpr (KIND == kAdaRow) accum = a.up.state[key];
+    }
+  }
+  for (int q = p; q < fin; q += B) {
+    Vec<TG, EL> g[B];
+#pragma unroll
+    for (int k = 0; k < B; ++k) {
+      const char* src = a.dy + (int64_t)ch.row(min(q + k, fin - 1) - p0) * a.ld +
+                        (uint32_t)cs * (uint32_t)(Vec<TG, EL>::kBytes / EL);
+      if (a.aligned) g[k].load(src);
+      else g[k].load_each(src);
+    }
+#pragma unroll
+    for (int k = 0; k < B; ++k)
+#pragma unroll
+      for (int e = 0; e < EL; ++e) acc[e] += q + k < fin ? g[k].get(e) : 0.f;
+  }
+#pragma unroll
+  for (int e = 0; e < EL; ++e) acc[e] *= a.scale;
+  if (longs) {
+    if (in) Vec<float, EL>::store(a.partials + ((int64_t)c * 2 + (i == 0 ? 0 : 1)) * a.D + col, acc);
+    return;
+  }
+  if constexpr (stores(KIND)) {
+    store_grad<EL, KIND == kStream>(a, ch.u0 + i, key, col, in, acc);
+  } else {
+    float step = a.up.lr;
+    if constexpr (KIND == kAdaRow) {
+      float sq = 0.f;
+#pragma unroll
+      for (int e = 0; e < EL; ++e) sq = __builtin_fmaf(acc[e], acc[e], sq);
+      float total = wave_total(in ? sq : 0.f);
+      if (a.parts > 1) {
+        if (lane == 0) s_sq[wave] = total;
+        // (the accumulator is here before a wavefront of the block writes it)
+        asm volatile("" : "+v"(accum)::"memory");
+        __syncthreads();
+        total = 0.f;
+        for (int k = 0; k < a.parts; ++k) total += s_sq[k];
+      }
+      const float hn = accum + total / (float)a.D;
+      step = a.up.lr / (sqrtf(hn) + a.up.eps);
+      if (applies && part == 0 && lane == 0) a.up.state[key] = hn;
+    }
+    if (in && applies) apply<TW, EL, KIND>(a.up, key, col, acc, w, h, step);
   }
 }
 
@@ -542,6 +671,14 @@ __global__ __launch_bounds__(kCombineLanes) void k_token_combine(TokGrad a) {
 
 int zero_blocks(uint32_t rows) { return (int)(((int64_t)rows + 4 * kZeroRows - 1) / (4 * kZeroRows)); }
 
+// Up to so many wavefronts, one to a position and its columns' parts; above, a
+// wavefront walks a chunk's (us with the dedup, the former against the latter).
+// Row-wise Adagrad, whose chunk costs a barrier a batch: 2000 x 64 18.0 (24.6),
+// 500 x 1024 20.1 (38.3), 8000 x 1024 45.4 (54.4), 30000 x 256 56.3 (54.5).  SGD:
+// 500 x 64 16.5 (20.9), 8000 x 256 31.8 (36.7), 8000 x 1024 44.6 (39.3).  Stored:
+// 2000 x 64 18.6 (20.6), 2000 x 256 22.9 (23.9), 2000 x 1024 31.8 (29.8).
+constexpr int64_t each_waves(int kind) { return kind == kAdaRow ? 32768 : stores(kind) ? 4096 : 8192; }
+
 template <typename TG, typename TW, int KIND>
 hipError_t grad_kernels(TokGrad a, hipStream_t s) {
   // columns a lane: 1 for rows of up to 64 values, 4, or 8 above 4096
@@ -549,9 +686,11 @@ hipError_t grad_kernels(TokGrad a, hipStream_t s) {
   a.parts = (a.D + kWave * el - 1) / (kWave * el);
   constexpr bool kRow = KIND == kAdaRow;
   const dim3 block(kRow ? a.parts * kWave : 4 * kWave);
+  const bool each = (int64_t)a.N * a.parts <= each_waves(KIND);
   a.split = 0;
   while (a.split < kMostSplit && ((int64_t)a.nchunks * a.parts << a.split) < kSplitWaves) ++a.split;
-  a.blocks = kRow ? a.nchunks << a.split : ((a.nchunks * a.parts << a.split) + 3) / 4;
+  a.blocks = each ? (kRow ? a.N : (a.N * a.parts + 3) / 4)
+                  : (kRow ? a.nchunks << a.split : ((a.nchunks * a.parts << a.split) + 3) / 4);
   a.zero_blocks = stores(KIND) && a.layout == EMB_TABLE ? zero_blocks(a.rows) : 0;
   const unsigned grid = (unsigned)(a.blocks + a.zero_blocks);
   const uintptr_t at = reinterpret_cast<uintptr_t>(a.dy) | (uintptr_t)a.ld;
@@ -559,7 +698,11 @@ hipError_t grad_kernels(TokGrad a, hipStream_t s) {
   a.aligned = at % (uintptr_t)(vec < 16 ? vec : 16) == 0;
   // positions a batch: as many loads in flight as registers allow at four wavefronts a SIMD
   constexpr int kB1 = 8, kB4 = stores(KIND) ? 16 : (KIND == kAdaElem ? 4 : 8), kB8 = stores(KIND) ? 8 : (KIND == kSgd ? 4 : 2);
-  if (el == 1) k_token_reduce<TG, TW, 1, kB1, KIND><<<grid, block, 0, s>>>(a);
+  if (each) {
+    if (el == 1) k_token_reduce_each<TG, TW, 1, 16, KIND><<<grid, block, 0, s>>>(a);
+    else if (el == 4) k_token_reduce_each<TG, TW, 4, 8, KIND><<<grid, block, 0, s>>>(a);
+    else k_token_reduce_each<TG, TW, 8, 8, KIND><<<grid, block, 0, s>>>(a);
+  } else if (el == 1) k_token_reduce<TG, TW, 1, kB1, KIND><<<grid, block, 0, s>>>(a);
   else if (el == 4) k_token_reduce<TG, TW, 4, kB4, KIND><<<grid, block, 0, s>>>(a);
   else k_token_reduce<TG, TW, 8, kB8, KIND><<<grid, block, 0, s>>>(a);
   // (a long segment has more than one chunk)

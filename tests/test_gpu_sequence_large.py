@@ -4,6 +4,7 @@ large tiles of a weight gradient; with tolerances as in test_gpu_sequence."""
 import numpy as np
 import pytest
 
+from tests import test_gpu_sequence as small
 from tests.test_gpu_sequence import U, _dt, _np, _plain_backward, _plain_forward, _saved_plain, _steps
 
 pytestmark = pytest.mark.gpu
@@ -62,6 +63,23 @@ def test_table_gradient_past_the_caches(dy_type):
     np.add.at(mag, key[keep], np.abs(rows))
     assert (np.abs(_np(grad) - want) <= 67 * U * mag).all()
     assert (_np(grad)[mag.sum(1) == 0] == 0).all()
+
+
+# so many positions and columns that a wavefront takes a chunk's positions (n, D, rows, gap, shift, hottest's share, sequences)
+MANY = [(33001, 48, [300, 2000], 3, 0, 0.2, 11), (9001, 1028, [4000], 0, 1, 0.1, 9), (3701, 4104, [50, 900], 8, 0, 0.3, 2)]
+
+
+@pytest.mark.parametrize("dy_type", ["fp32", "bf16"])
+@pytest.mark.parametrize("case", MANY)
+def test_token_gradient_of_many(case, dy_type):
+    small.test_token_gradient_layouts(case, dy_type)
+
+
+@pytest.mark.parametrize("opt", ["sgd", "adagrad", "adagrad_ew"])
+@pytest.mark.parametrize("table,dy_type", [("fp32", "fp32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("case", MANY)
+def test_token_update_of_many(case, table, dy_type, opt):
+    small.test_token_update(case, table, dy_type, opt)
 
 
 def _check_scan(rng, offs, D, dtype):
