@@ -34,9 +34,10 @@ namespace {
 constexpr float kResets = -1.0f;  // (products of a's are never negative)
 constexpr int kW = 8;             // wavefronts of a block
 constexpr int kThreads = kW * kWave;
-constexpr int kFwdP = 16;         // positions a wavefront holds: spans of 128 forward,
-constexpr int kBackP = kSpan / kW;  // of 64 (the kept states') backward
-constexpr int kFwdSpan = kFwdP * kW;
+// Positions a wavefront holds: spans of 128 forward (of 64 where those would be
+// at most 96 blocks), of 64 (the kept states') backward.
+constexpr int kFwdP = 16, kFwdFewP = 8, kFwdFewBlocks = 96;
+constexpr int kBackP = kSpan / kW;
 constexpr int kLook = 32;         // spans a block looks back at
 
 struct Saved8 {};
@@ -283,9 +284,8 @@ __device__ __forceinline__ void load_rare(const float* p, int col, float (&v)[V]
 
 // ---------------------------------------------------------------- forward
 
-template <typename T, int V, bool GATED, bool STREAM>
+template <typename T, int V, int P, bool GATED, bool STREAM>
 __global__ __launch_bounds__(kThreads, 4) void k_scan_fwd(Scan a) {
-  constexpr int P = kFwdP;
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
   const int main_blocks = a.spans * a.slices;
   if ((int)blockIdx.x >= main_blocks) {
@@ -306,7 +306,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_fwd(Scan a) {
   const int col0 = (slice * kWave + lane) * V;
   const bool in = col0 < a.D;
   const int col = in ? col0 : 0;
-  const int q0 = c * kFwdSpan + wave * P;
+  const int q0 = (c * kW + wave) * P;
   const int n = min(P, a.N - q0);  // (0 or less: this wavefront has no positions)
   // the state after position t is At[t] times the one that enters the wavefront's positions plus Bt[t]
   float A[V], B[V], At[P][V], Bt[P][V], Ae[V], Be[V], bias[V];
@@ -796,29 +796,34 @@ void clear(const Scan& a, hipStream_t s) {
   if (a.spans > 1) k_scan_clear<<<(unsigned)(blocks < 256 ? blocks : 256), 256, 0, s>>>(a.taken, n);
 }
 
-template <typename T, int V, bool STREAM>
-hipError_t fwd(const ScanLaunch& p, hipStream_t s) {
-  const Scan a = arguments(p, V, kFwdSpan);
+template <typename T, int V, int P, bool STREAM>
+hipError_t fwd(const ScanLaunch& p, const Scan& a, hipStream_t s) {
   const unsigned blocks = (unsigned)(a.spans * a.slices) + empties(a, a.h_last);
   clear(a, s);
-  if (p.gated) k_scan_fwd<T, V, true, STREAM><<<blocks, kThreads, 0, s>>>(a);
-  else k_scan_fwd<T, V, false, STREAM><<<blocks, kThreads, 0, s>>>(a);
+  if (p.gated) k_scan_fwd<T, V, P, true, STREAM><<<blocks, kThreads, 0, s>>>(a);
+  else k_scan_fwd<T, V, P, false, STREAM><<<blocks, kThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 template <typename T, int V>
 hipError_t fwd(const ScanLaunch& p, hipStream_t s) {
-  const bool big = p.N * p.D * (int64_t)(Vec<T, V>::kBytes / V) > kStreamBytes;
-  return big ? fwd<T, V, true>(p, s) : fwd<T, V, false>(p, s);
+  const Scan a = arguments(p, V, kFwdP * kW);
+  if (p.N * p.D * (int64_t)(Vec<T, V>::kBytes / V) > kStreamBytes) return fwd<T, V, kFwdP, true>(p, a, s);
+  // (us, the shorter spans against the longer ones: 500 x 2000 11.5 and 13.1, 1500 x 512 11.9 and 13.1, 8000 x 100 12.8
+  // and 13.9; 128 blocks of the longer ones as fast; 192, 1500 x 2000, 18.2 and 16.0; one span 7.1 and 6.4)
+  if (a.spans > 1 && a.spans * a.slices <= kFwdFewBlocks)
+    return fwd<T, V, kFwdFewP, false>(p, arguments(p, V, kFwdFewP * kW), s);
+  return fwd<T, V, kFwdP, false>(p, a, s);
 }
 
 template <typename T, typename TG, int V, bool STREAM>
 hipError_t bwd(const ScanLaunch& p, hipStream_t s) {
-  const Scan a = arguments(p, V, kSpan);
+  Scan a = arguments(p, V, kSpan);
+  if (a.spans == 1) a.dbias = p.dbias;  // (its one row is the sum)
   const unsigned blocks = (unsigned)(a.spans * a.slices) + empties(a, a.dh0);
   clear(a, s);
   if (p.gated) k_scan_bwd<T, TG, V, true, STREAM><<<blocks, kThreads, 0, s>>>(a);
   else k_scan_bwd<T, TG, V, false, STREAM><<<blocks, kThreads, 0, s>>>(a);
-  if (p.dbias)
+  if (p.dbias && a.spans > 1)
     k_scan_dbias<<<(unsigned)((a.D + kBiasCols - 1) / kBiasCols), kBiasCols * kBiasRows, 0, s>>>(a.dbias, p.dbias, a.spans,
                                                                                              a.D);
   return hipGetLastError();

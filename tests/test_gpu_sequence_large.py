@@ -151,3 +151,13 @@ def test_weight_gradient_large_tiles():
     first = dw.clone()
     ck.weight_grad(dy.to(DEV), dw)
     assert torch.equal(dw, first)
+
+
+@pytest.mark.parametrize("dtype,n,D", [("bf16", 2100, 1602), ("bf16", 1900, 803), ("fp32", 1900, 801)])
+def test_scan_of_many_blocks(dtype, n, D):
+    """Above 96 blocks of long spans, below 32 MB."""
+    rng = np.random.default_rng(D)
+    lens = [1, 0, n - 800, 127, 129, 543]
+    offs = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    assert offs[-1] == n
+    _check_scan(rng, offs, D, dtype)
