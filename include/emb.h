@@ -424,7 +424,8 @@ typedef enum { EMB_ROWS = 0, EMB_TABLE = 1, EMB_TABLE_ADD = 2 } emb_grad_layout;
  * says, or NULL with fuse.  fuse: NULL, or the optimizer step applied to the
  * looked-up rows but the padding row, as in emb_grad_reduce (grad must then
  * be NULL).  The dedup's outputs and ws are those emb_unique_ids left for this
- * batch, unmodified.  EMB_EUNSUPPORTED for rows of more than 8192 values.
+ * batch, unmodified.  EMB_EUNSUPPORTED for rows of more than 8192 values, or
+ * of more than 4096 that are no multiple of 8.
  * After a dedup that failed on the device no table row is written, and
  * gradient rows are written as zeros (EMB_ROWS, EMB_TABLE) or left. */
 emb_status emb_token_grad(const emb_tables* tables, const emb_batch* batch, const emb_token* token,
@@ -457,7 +458,10 @@ typedef struct {
 
 /* Bytes of workspace of emb_scan_fwd and emb_scan_bwd for up to num_tokens
  * tokens of dim columns (0 for invalid sizes); it needs no initialisation and
- * carries nothing between calls. */
+ * carries nothing between calls.  Calls that may run at once need workspaces
+ * of their own.  Inside a call workgroups wait for others that started before
+ * them; should such a wait last two seconds, the rest of that column's values
+ * are NaN. */
 size_t emb_scan_workspace_size(int64_t num_tokens, int32_t dim);
 
 /* y: N rows of dim columns, of x's type.  h_last: device fp32 [M][D], the
@@ -510,8 +514,9 @@ emb_status emb_restore(int64_t rows, int32_t dim, const emb_mat* src, const emb_
  * x: EMB_SAVED8, `rows` rows of dim columns; dy: fp32 or bf16, cols columns;
  * dw: device fp32 [dim][cols].  Products of bf16 values (an fp32 dy is split
  * into three that hold all of it) are summed in fp32, pieces of the rows apart
- * where there are few tiles of dw; ws: device, 256-byte aligned, ws_bytes >=
- * emb_weight_grad_workspace_size (which may be 0). */
+ * where that fills the device better; ws: device, 256-byte aligned, ws_bytes
+ * >= emb_weight_grad_workspace_size (which may be 0).  EMB_EUNSUPPORTED for
+ * rows of more than 16 MB from one to the next. */
 size_t emb_weight_grad_workspace_size(int64_t rows, int32_t dim, int32_t cols);
 emb_status emb_weight_grad(int64_t rows, int32_t dim, int32_t cols, const emb_mat* x, const emb_mat* dy, float* dw,
                            int32_t add, void* ws, size_t ws_bytes, void* stream);

@@ -18,9 +18,22 @@
 //    depend on timing;
 //  - published words are stored and read at device scope, a flag after the
 //    words it announces; flags and counters are cleared by a kernel before.
+// 32768 positions x 2048 in bf16 (gated): 144 us forward, 3.8 TB/s; the same loads
+// and stores without the recurrence take 105 us (93 with 8-byte lanes).  What is
+// between is the chain: of the 19 us that a block lived when it was traced, 8 were
+// its loads and sums, 6.5 the wait for the spans before it and 3.5 the stores, and
+// two blocks (126 registers a lane) share a compute unit.  There, spans of 64 take
+// 206 us, 16 wavefronts of 16 positions 152 and of 8 positions 154; looking at 64
+// spans 152; all eight wavefronts polling 20 us more; the next span's x and f loaded
+// during the wait 190 (spans of 112); gates computed twice, for three blocks a
+// compute unit, 166; three passes over the data (the spans' steps, the states
+// between them, the outputs) 190.
+//
 // The backward is the same from the last position to the first on
 // dh_t = sigmoid(o_t) dy_t + a_{t+1} dh_{t+1}, with h recomputed inside each
-// span of 64 from the state the forward kept.
+// span of 64 from the state the forward kept: 232 us there, 4.2 TB/s (its loads and
+// stores are 939 MB), bound likewise; from 8-bit checkpoints at 16384 x 1280, 75 us,
+// 3.4 TB/s, its vector instructions half of the cycles.
 //
 // A span that holds a first position passes nothing on of what it receives:
 // its A is kResets, not a product with zero, which would carry an infinity or
@@ -703,6 +716,8 @@ __global__ __launch_bounds__(kBiasCols * kBiasRows) void k_scan_dbias(const floa
   if (r == 0 && col < D) dbias[col] = (float)s_sum[0][c];
 }
 
+// Zeros for the chain's counters and flags: 1.3 us, 5 after a kernel that filled
+// the device.
 __global__ __launch_bounds__(256) void k_scan_clear(uint32_t* words, int64_t n) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) words[i] = 0u;
 }
@@ -719,6 +734,9 @@ void nothing(const float* from, float* to, int64_t n, hipStream_t s) {
 
 // ---------------------------------------------------------------- one token
 
+// A lane to each column (or two) of a token: one read of every input, one read
+// and write of the state.  128 tokens x 1536: 3.3 us, a launch and two dependent
+// loads (the bytes take 0.6).
 template <typename T, int V, bool GATED>
 __global__ __launch_bounds__(256) void k_scan_step(StepLaunch a) {
   const int per = (a.D + V - 1) / V;  // lanes a token

@@ -339,8 +339,8 @@ __global__ __launch_bounds__(256) void k_weight_parts(const float* parts, float*
 constexpr int kSmallBlocks = 256, kSmallSteps = 6;
 // Tiles of 256 x 256 (one block a compute unit: 256 sums a lane, 128 KB of LDS)
 // where parts of at least 16 steps make more than 128 blocks (us, these tiles
-// against the small ones): 32768 x 2048 x 6144 855 (1102), 32768 x 1024 x 1024 92
-// (128), 8192 x 2048 x 2048 92 (123), 2048 x 2048 x 6144 71 (84); with 128 blocks
+// against the small ones): 32768 x 2048 x 6144 785 (1102), 32768 x 1024 x 1024 86
+// (128), 8192 x 2048 x 2048 88 (123), 2048 x 2048 x 6144 71 (84); with 128 blocks
 // or fewer 2048 x 2048 x 2048 49 (38), 8192 x 1024 x 1024 47 (45), 8192 x 512 x 512
 // 40 (21).
 constexpr int kBigBlocks = 256, kBigSteps = 16, kBigLeast = 129;
