@@ -345,8 +345,8 @@ constexpr int kSmallBlocks = 256, kSmallSteps = 6;
 // 40 (21).
 constexpr int kBigBlocks = 256, kBigSteps = 16, kBigLeast = 129;
 // As many parts as fill one to four rounds of blocks, whichever is estimated to
-// take least: a step costs 0.85 us, and 1 us more the more compute units are busy
-// (the clock falls), a part's sums 1.8 us a million.  192 tiles of 512 steps: four
+// take least: a step costs 0.85 us, and up to 1 us more the more compute units are
+// busy (as measured), a part's sums 1.8 us a million.  192 tiles of 512 steps: four
 // parts in three full rounds 785 us, one part 811; 96 tiles of 512 steps 416 (434);
 // 96 tiles of 256 steps stay at two parts, 231 (251 with five).
 constexpr int kMostRounds = 4;
