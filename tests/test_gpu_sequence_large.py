@@ -161,3 +161,71 @@ def test_scan_of_many_blocks(dtype, n, D):
     offs = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
     assert offs[-1] == n
     _check_scan(rng, offs, D, dtype)
+
+
+def test_matrices_of_more_than_four_gigabytes():
+    """Rows 8 MB apart: the last ones lie beyond 2^32 bytes (and 2^32 / 2 elements)."""
+    import torch
+    import paper_2112_02752_amd as emb
+    rng = np.random.default_rng(4)
+    n, D, F = 700, 96, 200
+    base = torch.empty((n, 1 << 22), dtype=torch.bfloat16, device=DEV)
+    view = [base[:, 1000 * i: 1000 * i + D] for i in range(9)]
+    near = [torch.empty((n, D), dtype=torch.bfloat16, device=DEV) for _ in range(9)]
+    for k in range(4):
+        near[k].copy_(torch.from_numpy(rng.standard_normal((n, D)).astype(np.float32)))
+        view[k].copy_(near[k])
+    offs = torch.tensor([0, 3, 3, 650, n], dtype=torch.int32, device=DEV)
+    bias = torch.linspace(-1, 3, D, device=DEV)
+    sums = []
+    for v in (near, view):
+        rec, db = emb.Recurrence(n, 4, D), torch.empty(D, device=DEV)
+        scan = emb.Scan(offs, v[0], v[1], v[2], bias=bias)
+        rec.forward(scan, v[4])
+        rec.backward(scan, v[3], v[5], v[6], v[7], dbias=db)
+        sums.append(db)
+    assert torch.equal(*sums)
+    for k in (4, 5, 6, 7):
+        assert torch.equal(view[k], near[k])
+    state = [torch.ones((n, D), device=DEV) for _ in range(2)]
+    for v, st in zip((near, view), state):
+        emb.scan_step(v[0], v[1], v[2], st, v[8], bias=bias)
+    assert torch.equal(view[8], near[8]) and torch.equal(*state)
+    ck = [emb.Checkpoint(n, D) for _ in range(2)]
+    back = [near[8], view[8]]
+    for c, v, b in zip(ck, (near, view), back):
+        c.pack(v[0])
+        c.unpack(b)
+    assert torch.equal(*back)
+    wide = torch.from_numpy(rng.standard_normal((n, F)).astype(np.float32)).bfloat16().to(DEV)
+    base[:, 20000:20000 + F] = wide
+    dw = [torch.empty((D, F), device=DEV) for _ in range(2)]
+    ck[0].weight_grad(wide, dw[0])
+    ck[0].weight_grad(base[:, 20000:20000 + F], dw[1])
+    assert torch.equal(*dw)
+
+
+def test_tables_of_more_than_four_gigabytes():
+    import torch
+    import paper_2112_02752_amd as emb
+    R, D, n = 600_001, 2048, 301
+    rng = np.random.default_rng(6)
+    key = np.concatenate([rng.integers(R - 2000, R, n - 3), [0, R - 1, R - 1]])
+    ids = torch.from_numpy(key).to(DEV)
+    W = torch.zeros((R, D), device=DEV)
+    W[ids] = torch.arange(n, device=DEV, dtype=torch.float32)[:, None] + 1
+    W[R - 1] = 77
+    batch = emb.Batch(torch.tensor([0, n], dtype=torch.int32, device=DEV), ids, 1)
+    tables = emb.Tables(W, [0, R])
+    y = torch.empty((n, D), device=DEV)
+    layer = emb.TokenLayer(tables, opt="sgd", lr=0.5, max_tokens=n, max_seqs=1)
+    layer.forward(batch, y)
+    assert torch.equal(y, W[ids])
+    dy = torch.full((n, D), 0.25, device=DEV)
+    grad = torch.full((R, D), 3.0, device=DEV)
+    layer.table_grad(batch, dy, grad)
+    count = torch.zeros(R, device=DEV).index_add_(0, ids, torch.full((n,), 0.25, device=DEV))
+    assert bool((grad == count[:, None]).all())
+    want = W[ids] - 0.5 * count[ids][:, None]
+    layer.update(batch, dy)
+    assert torch.equal(W[ids], want)
