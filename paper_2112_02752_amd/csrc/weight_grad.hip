@@ -19,8 +19,9 @@
 //
 // Bound: 2 N K F operations on the matrix units.  32768 x 2048 x 6144 (bf16 dy):
 // 785 us, 1050 TFLOP/s, of 1216 that a library product of 8192^3 reaches; the four
-// parts' sums are 75 us of it.  2048 x 512 x 1536: 19 us, of which the products
-// take 15 (six steps a block, each a wait for memory) and the parts' sums 4.
+// parts' sums are 75 us of it.  2048 x 512 x 1536: 18.6 us, of which the products
+// take 14 (what is read and the parts are 44 MB; small tiles with four wavefronts a
+// block 15.5) and the parts' sums 4.
 #include "seq_common.h"
 
 namespace emb {
@@ -33,7 +34,6 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr int kStep = 64;   // rows a step takes
 constexpr int kOct = kStep / 8;
 constexpr int kGroup = 128;  // columns of an LDS group
-constexpr int kThreads = 256;
 constexpr int kBand = 8;     // tiles
 
 struct WArgs {
@@ -159,11 +159,24 @@ struct YLoad {
   }
 };
 
-// G groups of 128 columns each way a block, four wavefronts as 2 x 2; S slices
-// of a group each way a wavefront (G 2: a group, S 4; G 1: half of one, S 2).
+// G groups of 128 columns each way a block.  G 2: four wavefronts as 2 x 2, each
+// a group by a group (4 x 4 slices), every thread bringing in x and dy.  G 1: eight
+// as 4 x 2, each 1 x 2 slices, four bringing in x and four dy (few steps a block:
+// two wavefronts a SIMD, of which one converts while the other multiplies).
+template <int G>
+struct Shape;
+template <>
+struct Shape<2> {
+  static constexpr int kThreads = 256, kSx = 4, kSy = 4, kWavesK = 2;
+};
+template <>
+struct Shape<1> {
+  static constexpr int kThreads = 512, kSx = 1, kSy = 2, kWavesK = 4;
+};
+
 template <int G, int SPLIT, bool PAIRS>
-__global__ __launch_bounds__(kThreads, G == 2 ? 1 : 2) void k_weight_grad(WArgs a) {
-  constexpr int S = 2 * G, kTile = kGroup * G, kBufs = SPLIT == 1 ? 2 : 1;
+__global__ __launch_bounds__(Shape<G>::kThreads, G == 2 ? 1 : PAIRS ? 4 : 2) void k_weight_grad(WArgs a) {
+  constexpr int SX = Shape<G>::kSx, SY = Shape<G>::kSy, kTile = kGroup * G, kBufs = SPLIT == 1 ? 2 : 1;
   constexpr int kApart = kOct * G * kGroup;
   __shared__ u32x4 s_x[kBufs][kOct][G * kGroup], s_y[kBufs][SPLIT][kOct][G * kGroup];
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
@@ -171,7 +184,8 @@ __global__ __launch_bounds__(kThreads, G == 2 ? 1 : 2) void k_weight_grad(WArgs 
   int at = (int)blockIdx.x;
   if constexpr (G == 2) {
     // Blocks go to the eight XCDs in turn: an XCD takes neighbouring tiles, which read the same columns
-    // (32768 x 2048 x 6144 811 us, 846 with every XCD reading all of dy; small tiles wait for memory and gain nothing)
+    // (32768 x 2048 x 6144 811 us, 846 with every XCD reading all of dy;
+    // small tiles gain nothing, and 2048 x 512 x 1536 takes 21.4 us instead of 18.6)
     const int each = (int)gridDim.x / 8;
     if (at < 8 * each) at = at % 8 * each + at / 8;
   }
@@ -180,36 +194,44 @@ __global__ __launch_bounds__(kThreads, G == 2 ? 1 : 2) void k_weight_grad(WArgs 
   const int band = tile / (kBand * a.tiles_f), in_band = tile - band * kBand * a.tiles_f;
   const int high = min(kBand, a.tiles_k - band * kBand);
   const int k0 = (band * kBand + in_band % high) * kTile, c0 = in_band / high * kTile;
-  const int quad = threadIdx.x % 32, oct = threadIdx.x / 32;
+  const int quad = threadIdx.x % 32, oct = threadIdx.x / 32 % kOct;
+  const bool takes_x = G == 2 || wave < 4, takes_y = G == 2 || wave >= 4;
   const int64_t r_begin = (int64_t)part * a.steps_per_part * kStep;
   const int64_t r_end = min((int64_t)a.N, r_begin + (int64_t)a.steps_per_part * kStep);
-  f32x16 acc[S][S] = {};
-  const int wk = (wave & 1) * 32 * S, wc = (wave >> 1) * 32 * S;
+  f32x16 acc[SX][SY] = {};
+  const int wk = wave % Shape<G>::kWavesK * 32 * SX, wc = wave / Shape<G>::kWavesK * 32 * SY;
   XLoad x[G];
   YLoad<SPLIT, PAIRS> y[G];
   auto load = [&](int64_t r0) {
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      x[g].load(a, r0, k0 + g * kGroup, quad, oct);
-      y[g].load(a, r0, c0 + g * kGroup, quad, oct);
+      if (takes_x) x[g].load(a, r0, k0 + g * kGroup, quad, oct);
+      if (takes_y) y[g].load(a, r0, c0 + g * kGroup, quad, oct);
+    }
+  };
+  auto put = [&](int buf) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      if (takes_x) x[g].put(&s_x[buf][oct][g * kGroup], quad);
+      if (takes_y) y[g].put(&s_y[buf][0][oct][g * kGroup], kApart, quad);
     }
   };
   // a quarter of a step: 16 rows, of which lane l holds 8 * (l / 32) ..
-  bf16x8 fx[2][S], fy[2][S];
+  bf16x8 fx[2][SX], fy[2][SY];
   auto fetch = [&](int buf, int n, int p, int to) {
     const int o = 2 * n + lane / 32, c = lane % 32;
     if (p == 0) {
 #pragma unroll
-      for (int i = 0; i < S; ++i) fx[to][i] = __builtin_bit_cast(bf16x8, s_x[buf][o][wk + 32 * i + c]);
+      for (int i = 0; i < SX; ++i) fx[to][i] = __builtin_bit_cast(bf16x8, s_x[buf][o][wk + 32 * i + c]);
     }
 #pragma unroll
-    for (int i = 0; i < S; ++i) fy[to][i] = __builtin_bit_cast(bf16x8, s_y[buf][p][o][wc + 32 * i + c]);
+    for (int i = 0; i < SY; ++i) fy[to][i] = __builtin_bit_cast(bf16x8, s_y[buf][p][o][wc + 32 * i + c]);
   };
   auto sum = [&](int xs, int ys) {
 #pragma unroll
-    for (int i = 0; i < S; ++i)
+    for (int i = 0; i < SX; ++i)
 #pragma unroll
-      for (int j = 0; j < S; ++j)
+      for (int j = 0; j < SY; ++j)
         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[xs][i], fy[ys][j], acc[i][j], 0, 0, 0);
   };
   if (r_begin < r_end) {
@@ -217,11 +239,7 @@ __global__ __launch_bounds__(kThreads, G == 2 ? 1 : 2) void k_weight_grad(WArgs 
     if constexpr (kBufs == 1) {
       for (int64_t r0 = r_begin; r0 < r_end; r0 += kStep) {
         __syncthreads();
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-          x[g].put(&s_x[0][oct][g * kGroup], quad);
-          y[g].put(&s_y[0][0][oct][g * kGroup], kApart, quad);
-        }
+        put(0);
         __syncthreads();
         if (r0 + kStep < r_end) load(r0 + kStep);
 #pragma unroll
@@ -235,22 +253,28 @@ __global__ __launch_bounds__(kThreads, G == 2 ? 1 : 2) void k_weight_grad(WArgs 
       }
     } else {
       // two buffers: a step's values go to LDS while the step before them is summed, and are loaded a step earlier
-#pragma unroll
-      for (int g = 0; g < G; ++g) {
-        x[g].put(&s_x[0][oct][g * kGroup], quad);
-        y[g].put(&s_y[0][0][oct][g * kGroup], kApart, quad);
-      }
+      put(0);
       load(r_begin + kStep);  // (rows past the end read as zeros)
       __syncthreads();
       int buf = 0;
       for (int64_t r0 = r_begin; r0 < r_end; r0 += kStep) {
         fetch(buf, 0, 0, 0);
+        if constexpr (G == 1) {
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-          if (n < 3) fetch(buf, n + 1, 0, (n + 1) & 1);
-          sum(n & 1, n & 1);
-          const int g = n / 2;
-          if (g < G) {
+          for (int n = 0; n < 4; ++n) {
+            if (n < 3) fetch(buf, n + 1, 0, (n + 1) & 1);
+            sum(n & 1, n & 1);
+            if (n == 1) {
+              put(buf ^ 1);
+              load(r0 + 2 * kStep);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            if (n < 3) fetch(buf, n + 1, 0, (n + 1) & 1);
+            sum(n & 1, n & 1);
+            const int g = n / 2;
             if (n % 2 == 0) {
               x[g].put(&s_x[buf ^ 1][oct][g * kGroup], quad);
               x[g].load(a, r0 + 2 * kStep, k0 + g * kGroup, quad, oct);
@@ -258,9 +282,7 @@ __global__ __launch_bounds__(kThreads, G == 2 ? 1 : 2) void k_weight_grad(WArgs 
               y[g].put(&s_y[buf ^ 1][0][oct][g * kGroup], kApart, quad);
               y[g].load(a, r0 + 2 * kStep, c0 + g * kGroup, quad, oct);
             }
-          }
-          // the matrix unit takes 32 cycles an instruction: what else there is to do goes between
-          if constexpr (G == 2) {
+            // the matrix unit takes 32 cycles an instruction: what else there is to do goes between
             __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);  // LDS reads
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -285,18 +307,18 @@ __global__ __launch_bounds__(kThreads, G == 2 ? 1 : 2) void k_weight_grad(WArgs 
   for (int v = 0; v < 16; ++v) {
     const int q = 8 * (v / 4) + 4 * (lane / 32) + v % 4;
 #pragma unroll
-    for (int i = 0; i < S; ++i) {
+    for (int i = 0; i < SX; ++i) {
       const int k = kb + 4 * q + i;
       if (k >= a.K) continue;
       float* d = out + (int64_t)k * a.F + cb;
-      float t[S];
+      float t[SY];
 #pragma unroll
-      for (int j = 0; j < S; ++j) t[j] = acc[i][j][v];
-      if (!add && cb + S <= a.F && a.F % S == 0) {
-        Vec<float, S>::store(d, t);
+      for (int j = 0; j < SY; ++j) t[j] = acc[i][j][v];
+      if (!add && cb + SY <= a.F && a.F % SY == 0) {
+        Vec<float, SY>::store(d, t);
       } else {
 #pragma unroll
-        for (int j = 0; j < S; ++j)
+        for (int j = 0; j < SY; ++j)
           if (cb + j < a.F) d[j] = add ? d[j] + t[j] : t[j];
       }
     }
@@ -333,55 +355,45 @@ __global__ __launch_bounds__(256) void k_weight_parts(const float* parts, float*
 }
 
 // Tiles of 128 x 128 with the rows cut into as many parts as give each compute
-// unit a block, of at least six steps.  2048 x 512 x 1536: 19.1 us (20.9 with
-// twice the blocks and four steps), 512 x 2048 x 2048: 16.0 (26.8), 8192 x 512 x
-// 1536: 36.2 (32.5), 2048 x 256 x 256: 14.1 (12.3).
-constexpr int kSmallBlocks = 256, kSmallSteps = 6;
+// unit a block, of at least four steps: 2048 x 256 x 256 11.7 us (13.9 with eight),
+// 2048 x 512 x 1536 18.6 and 18.6.
 // Tiles of 256 x 256 (one block a compute unit: 256 sums a lane, 128 KB of LDS)
-// where parts of at least 16 steps make more than 128 blocks (us, these tiles
-// against the small ones): 32768 x 2048 x 6144 785 (1102), 32768 x 1024 x 1024 86
-// (128), 8192 x 2048 x 2048 88 (123), 2048 x 2048 x 6144 71 (84); with 128 blocks
-// or fewer 2048 x 2048 x 2048 49 (38), 8192 x 1024 x 1024 47 (45), 8192 x 512 x 512
-// 40 (21).
-constexpr int kBigBlocks = 256, kBigSteps = 16, kBigLeast = 129;
-// As many parts as fill one to four rounds of blocks, whichever is estimated to
-// take least: a step costs 0.85 us, and up to 1 us more the more compute units are
-// busy (as measured), a part's sums 1.8 us a million.  192 tiles of 512 steps: four
-// parts in three full rounds 785 us, one part 811; 96 tiles of 512 steps 416 (434);
-// 96 tiles of 256 steps stay at two parts, 231 (251 with five).
-constexpr int kMostRounds = 4;
-constexpr double kStepUs = 0.85, kBusyUs = 1.0, kPartUs = 1.8e-6;
+// with as many parts of at least 16 steps as fill one to four rounds of blocks.
+// The way that is estimated to take least is taken; the figures (us) are fitted to
+// some forty measurements: a block's beginning and end; a step of a small tile with one block a
+// compute unit; a step of a large one, more the more compute units are busy; the
+// writing and adding of a million parts' sums.  Measured, large against small tiles:
+// 32768 x 1024 x 1024 87 (126), 1024 x 2048 x 6144 42 (55), 4096 x 1500 x 2500 60 (65),
+// 8192 x 500 x 2500 53 (51), 2048 x 2048 x 2048 48 (38), 20000 x 300 x 800 50 (36); four
+// parts of 192 large tiles in three full rounds against one part 785 (811), of 96
+// tiles 416 (434).
+constexpr int kBlocks = 256, kSmallSteps = 4, kBigSteps = 16, kMostRounds = 4;
+constexpr double kSmallUs = 6., kSmallStepUs = 0.9, kBigUs = 11., kBigStepUs = 0.85, kBusyUs = 1., kPartUs = 1.5e-6;
 struct Plan {
   int groups, parts, steps;  // groups of 128 columns a tile has each way; parts of so many steps
+  double us;
 };
 Plan plan_for(int64_t N, int32_t K, int32_t F, bool small) {
   const int64_t steps = (N + kStep - 1) / kStep;
-  auto cut = [&](int64_t tile, int64_t blocks, int64_t least) {
-    const int64_t tiles = ((K + tile - 1) / tile) * ((F + tile - 1) / tile);
-    int64_t p = blocks / tiles;
+  auto cut = [&](int groups, int rounds, int64_t least) {
+    const int64_t tile = groups * kGroup, tiles = ((K + tile - 1) / tile) * ((F + tile - 1) / tile);
+    int64_t p = rounds * kBlocks / tiles;
     if (p > steps / least) p = steps / least;
     if (p < 1) p = 1;
-    const int64_t per = (steps + p - 1) / p;
-    return Plan{(int)(tile / kGroup), (int)(per > 0 ? (steps + per - 1) / per : 1), (int)per};
+    Plan q{groups, 1, (int)((steps + p - 1) / p), 0.};
+    if (q.steps > 0) q.parts = (int)((steps + q.steps - 1) / q.steps);
+    const double blocks = (double)q.parts * (double)tiles / kBlocks, full = (double)(int64_t)(blocks + 1. - 0.5 / kBlocks);
+    q.us = groups == 1 ? kSmallUs + q.steps * kSmallStepUs * (blocks > 1. ? blocks : 1.)
+                       : kBigUs + q.steps * (kBigStepUs + kBusyUs * blocks / full) * full;
+    if (q.parts > 1) q.us += (double)q.parts * K * F * kPartUs;
+    return q;
   };
-  const Plan big = cut(2 * kGroup, kBigBlocks, kBigSteps);
-  const int64_t tiles = (int64_t)((K + 255) / 256) * ((F + 255) / 256);
-  if (!small && big.parts * tiles >= kBigLeast) {
-    Plan best{};
-    double least = 0.;
-    for (int r = 1; r <= kMostRounds; ++r) {
-      const Plan q = cut(2 * kGroup, r * kBigBlocks, kBigSteps);
-      const int64_t blocks = q.parts * tiles, rounds = (blocks + kBigBlocks - 1) / kBigBlocks;
-      const double busy = (double)blocks / (double)(rounds * kBigBlocks);
-      const double us = (double)(rounds * q.steps) * (kStepUs + kBusyUs * busy) +
-                        (q.parts > 1 ? (double)q.parts * K * F * kPartUs : 0.);
-      if (r == 1 || us < least) best = q, least = us;
-    }
-    return best;
+  Plan best = cut(1, 1, kSmallSteps);
+  for (int r = 1; !small && r <= kMostRounds; ++r) {
+    const Plan q = cut(2, r, kBigSteps);
+    if (q.us < best.us) best = q;
   }
-  Plan s = cut(kGroup, kSmallBlocks, kSmallSteps);
-  if (s.parts < 1) s.parts = 1;
-  return s;
+  return best;
 }
 
 }  // namespace
@@ -405,16 +417,16 @@ hipError_t launch_weight_grad(const WeightGradLaunch& p, hipStream_t s) {
   a.add = p.add;
   const Plan pl = plan_for(p.N, p.K, p.F, p.dtype == EMB_FP32 || !p.aligned);
   const int tile = pl.groups * kGroup;
-  a.parts = pl.parts < 1 ? 1 : pl.parts;
+  a.parts = pl.parts;
   a.steps_per_part = pl.steps;
   a.tiles_k = (p.K + tile - 1) / tile;
   a.tiles_f = (p.F + tile - 1) / tile;
   a.out = a.parts > 1 ? p.ws : p.dw;
   const unsigned blocks = (unsigned)(a.tiles_k * a.tiles_f * a.parts);
-  if (p.dtype == EMB_FP32) k_weight_grad<1, 3, true><<<blocks, kThreads, 0, s>>>(a);
-  else if (!p.aligned) k_weight_grad<1, 1, false><<<blocks, kThreads, 0, s>>>(a);
-  else if (pl.groups == 2) k_weight_grad<2, 1, true><<<blocks, kThreads, 0, s>>>(a);
-  else k_weight_grad<1, 1, true><<<blocks, kThreads, 0, s>>>(a);
+  if (p.dtype == EMB_FP32) k_weight_grad<1, 3, true><<<blocks, Shape<1>::kThreads, 0, s>>>(a);
+  else if (!p.aligned) k_weight_grad<1, 1, false><<<blocks, Shape<1>::kThreads, 0, s>>>(a);
+  else if (pl.groups == 2) k_weight_grad<2, 1, true><<<blocks, Shape<2>::kThreads, 0, s>>>(a);
+  else k_weight_grad<1, 1, true><<<blocks, Shape<1>::kThreads, 0, s>>>(a);
   if (a.parts > 1) {
     const int64_t n = (int64_t)p.K * p.F;
     const bool four = n % 4 == 0 && (reinterpret_cast<uintptr_t>(p.dw) & 15u) == 0;

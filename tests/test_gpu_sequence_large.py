@@ -229,3 +229,25 @@ def test_tables_of_more_than_four_gigabytes():
     want = W[ids] - 0.5 * count[ids][:, None]
     layer.update(batch, dy)
     assert torch.equal(W[ids], want)
+
+
+@pytest.mark.parametrize("n,K,F", [(2100, 2048, 6146), (8200, 1024, 2050)])
+def test_weight_gradient_large_tiles_whole_and_in_parts(n, K, F):
+    import torch
+    import paper_2112_02752_amd as emb
+    rng = np.random.default_rng(n)
+    x = torch.from_numpy(rng.standard_normal((n, K)).astype(np.float32)).to(DEV)
+    ck = emb.Checkpoint(n, K)
+    ck.pack(x)
+    back = _saved_plain(x.double().cpu().numpy())[2]
+    dy = torch.from_numpy(rng.standard_normal((n, F)).astype(np.float32)).bfloat16()
+    y = dy.double().numpy()
+    want, mag = back.T @ y, np.abs(back).T @ np.abs(y)
+    dw = torch.full((K, F), 5.0, device=DEV)
+    ck.weight_grad(dy.to(DEV), dw)
+    assert (np.abs(_np(dw) - want) <= (n + 8) * 2 * U * mag).all()
+    first = dw.clone()
+    ck.weight_grad(dy.to(DEV), dw, add=True)
+    assert (np.abs(_np(dw) - 2 * want) <= (2 * n + 20) * 2 * U * mag + 4 * U * np.abs(want)).all()
+    ck.weight_grad(dy.to(DEV), dw)
+    assert torch.equal(dw, first)
