@@ -102,7 +102,7 @@ __global__ __launch_bounds__(kFwdThreads) void k_token_fwd(TokFwd a, Stacked<MAN
 // what becomes of a gradient row: stored (past the caches: kStream), or applied
 enum Kind { kStore, kStream, kSgd, kAdaRow, kAdaElem };
 constexpr bool stores(int kind) { return kind == kStore || kind == kStream; }
-constexpr int kMostSplit = 4, kSplitWaves = 8192;
+constexpr int kMostSplit = 4, kSplitWaves = 8192, kZeroWaves = 1024;
 constexpr int kMostParts = 16;  // wavefronts of a block that share a chunk's columns (row-wise Adagrad)
 
 struct TokGrad {
@@ -116,7 +116,7 @@ struct TokGrad {
   const void* hdr;
   float* partials;  // [nchunks][2][D]: rows of long segments, of the one that holds a chunk's first position, of another
   float* grad;
-  int32_t N, D, nchunks, parts, split, blocks, zero_blocks, layout, aligned;  // split: 2^split wavefronts share a chunk's columns
+  int32_t N, D, nchunks, parts, split, blocks, zero_blocks, zero_rows, layout, aligned;  // split: 2^split wavefronts share a chunk's columns
   uint32_t rows, pad;
   float scale;
   Upd up;
@@ -182,29 +182,30 @@ __device__ __forceinline__ float wave_total(float x) {
   return add_across<32>(add_across<16>(add_lane<0x140>(add_lane<0x141>(add_lane<0x4e>(add_lane<0xb1>(x))))));
 }
 
-// Rows of the table that no token named: zeros.  One wavefront per kZeroRows
-// rows.
+// Rows of the table that no token named: zeros.  A wavefront takes zero_rows (up
+// to kZeroRows) of them as one run of values; row = value / D by a multiplication
+// (exact below 2^17 values for rows of up to 2^13).
 constexpr int kZeroRows = 16;
+static_assert(kZeroRows * kTokenMaxDim <= 1 << 17 && kTokenMaxDim <= 1 << 13, "the quotients are exact");
 template <bool STREAM>
-__device__ __forceinline__ void zero_rows(const TokGrad& a, int64_t r0, int lane) {
+__device__ __forceinline__ void zero_rows(const TokGrad& a, int64_t share, int lane) {
+  const int64_t r0 = share * a.zero_rows;
   if (r0 >= (int64_t)a.rows) return;
+  const int n = (int)min((int64_t)a.zero_rows, (int64_t)a.rows - r0);
   const int U = failed(a) ? 0 : a.num_unique[0];
   uint32_t named = 0;
   if (U > 0) {
     const int u = r0 == 0 ? 0 : wave_upper_bound<uint32_t>(a.ukeys, U, (uint32_t)r0 - 1u, lane);
     const uint32_t key = u + lane < U ? a.ukeys[u + lane] : kNoRow;
-#pragma unroll
-    for (int r = 0; r < kZeroRows; ++r) named |= __ballot(key == (uint32_t)r0 + r) ? 1u << r : 0u;
+    for (int r = 0; r < n; ++r) named |= __ballot(key == (uint32_t)r0 + r) ? 1u << r : 0u;
   }
-  const int n = (int)min((int64_t)kZeroRows, (int64_t)a.rows - r0);
-  for (int r = 0; r < n; ++r) {
-    if ((named >> r) & 1u) continue;
-    float* dst = a.grad + (r0 + r) * (int64_t)a.D;
-    const float z[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int c = lane * 4; c < a.D; c += kWave * 4) {
-      if constexpr (STREAM) Vec<float, 4>::stream(dst + c, z);
-      else Vec<float, 4>::store(dst + c, z);
-    }
+  const uint32_t by = 0xffffffffu / (uint32_t)a.D + 1u;
+  const float z[4] = {0.f, 0.f, 0.f, 0.f};
+  float* dst = a.grad + r0 * (int64_t)a.D;
+  for (int i = lane * 4; i < n * a.D; i += kWave * 4) {
+    if ((named >> __umulhi((uint32_t)i, by)) & 1u) continue;
+    if constexpr (STREAM) Vec<float, 4>::stream(dst + i, z);
+    else Vec<float, 4>::store(dst + i, z);
   }
 }
 
@@ -280,7 +281,7 @@ __global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) v
     // blocks of zeros come among the others evenly: these write while those wait for rows
     const int z = zero_blocks_before(a, block), more = zero_blocks_before(a, block + 1);
     if (more > z) {
-      zero_rows<KIND == kStream>(a, ((int64_t)z * 4 + wave) * kZeroRows, lane);
+      zero_rows<KIND == kStream>(a, (int64_t)z * 4 + wave, lane);
       return;
     }
     block -= z;
@@ -462,7 +463,7 @@ __global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) v
   if constexpr (stores(KIND)) {
     const int z = zero_blocks_before(a, block), more = zero_blocks_before(a, block + 1);
     if (more > z) {
-      zero_rows<KIND == kStream>(a, ((int64_t)z * 4 + wave) * kZeroRows, lane);
+      zero_rows<KIND == kStream>(a, (int64_t)z * 4 + wave, lane);
       return;
     }
     block -= z;
@@ -561,7 +562,7 @@ __global__ __launch_bounds__(KIND == kAdaRow ? kMostParts * kWave : 4 * kWave) v
 }
 
 __global__ __launch_bounds__(256) void k_token_zero(TokGrad a) {
-  zero_rows<false>(a, ((int64_t)blockIdx.x * 4 + threadIdx.x / kWave) * kZeroRows, threadIdx.x & (kWave - 1));
+  zero_rows<false>(a, (int64_t)blockIdx.x * 4 + threadIdx.x / kWave, threadIdx.x & (kWave - 1));
 }
 
 // A segment of more than 64 positions: the partial rows of its chunks added in
@@ -675,7 +676,14 @@ __global__ __launch_bounds__(kCombineLanes) void k_token_combine(TokGrad a) {
   }
 }
 
-int zero_blocks(uint32_t rows) { return (int)(((int64_t)rows + 4 * kZeroRows - 1) / (4 * kZeroRows)); }
+// blocks of zeros, of four wavefronts: as many rows to one (a power of two) as leave 1024 wavefronts (9 tokens of
+// 2401 rows x 1352 11.7 us, 14.2 with 16 rows always; 4096 wavefronts 49.8 us where these take 46.5, 9000 tokens of 3000
+// rows x 2000)
+int zero_blocks(TokGrad& a) {
+  a.zero_rows = kZeroRows;
+  while (a.zero_rows > 1 && (int64_t)a.rows < (int64_t)a.zero_rows * kZeroWaves) a.zero_rows /= 2;
+  return (int)(((int64_t)a.rows + 4 * a.zero_rows - 1) / (4 * a.zero_rows));
+}
 
 // Up to so many wavefronts, one to a position and its columns' parts; above, a
 // wavefront walks a chunk's (us with the dedup, the former against the latter).
@@ -697,7 +705,7 @@ hipError_t grad_kernels(TokGrad a, hipStream_t s) {
   while (a.split < kMostSplit && ((int64_t)a.nchunks * a.parts << a.split) < kSplitWaves) ++a.split;
   a.blocks = each ? (kRow ? a.N : (a.N * a.parts + 3) / 4)
                   : (kRow ? a.nchunks << a.split : ((a.nchunks * a.parts << a.split) + 3) / 4);
-  a.zero_blocks = stores(KIND) && a.layout == EMB_TABLE ? zero_blocks(a.rows) : 0;
+  a.zero_blocks = stores(KIND) && a.layout == EMB_TABLE ? zero_blocks(a) : 0;
   const unsigned grid = (unsigned)(a.blocks + a.zero_blocks);
   const uintptr_t at = reinterpret_cast<uintptr_t>(a.dy) | (uintptr_t)a.ld;
   const int vec = el * (int)(sizeof(TG));
@@ -809,7 +817,10 @@ hipError_t launch_token_grad(const TokenGradLaunch& p, hipStream_t s) {
   if (!p.fuse) {
     if (p.N == 0) {
       if (p.layout == EMB_TABLE && p.rows > 0)
-        k_token_zero<<<(unsigned)zero_blocks(p.rows), 256, 0, s>>>(a);
+        {
+        const unsigned blocks = (unsigned)zero_blocks(a);
+        k_token_zero<<<blocks, 256, 0, s>>>(a);
+      }
       return hipGetLastError();
     }
     if ((p.layout == EMB_TABLE ? (int64_t)p.rows : (int64_t)p.N) * p.D * 4 > kStreamBytes)
