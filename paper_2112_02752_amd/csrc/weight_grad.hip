@@ -23,6 +23,7 @@
 // take 14 (what is read and the parts are 44 MB; small tiles with four wavefronts a
 // block 15.5) and the parts' sums 4.
 #include "seq_common.h"
+#include "weight_plan.h"
 
 namespace emb {
 
@@ -31,10 +32,8 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kStep = 64;   // rows a step takes
 constexpr int kOct = kStep / 8;
-constexpr int kGroup = 128;  // columns of an LDS group
-constexpr int kBand = 8;     // tiles
+constexpr int kBand = 8;  // tiles
 
 struct WArgs {
   const char* x;
@@ -54,11 +53,10 @@ __device__ __forceinline__ uint32_t halves_hi(uint32_t a, uint32_t b) { return _
 // last rows nor the last tile's columns need a branch (columns beyond the
 // matrix only reach sums that are not stored).
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const char* p, int left, int ld, int row) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, left > 0 ? (left - 1) * ld + max(row, 0) : 0,
-                                           0x00020000);
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, rows_bytes(left, ld, row), 0x00020000);
 }
 __device__ __forceinline__ int rows_left(const WArgs& a, int64_t r0) {
-  return (int)min((int64_t)kStep, (int64_t)a.N - r0);
+  return step_rows(a.N, r0);
 }
 
 // One group of 128 columns of x: four columns of eight rows a lane.
@@ -66,7 +64,7 @@ struct XLoad {
   uint32_t w[8], e[8];
   __device__ __forceinline__ void load(const WArgs& a, int64_t r0, int k0, int quad, int oct) {
     // (a row of codes is whole groups)
-    const int left = rows_left(a, r0), groups = (a.K - k0 + EMB_SAVED_GROUP - 1) / EMB_SAVED_GROUP;
+    const int left = rows_left(a, r0), groups = groups_left(a.K, k0);
     const auto rx = rows_at(a.x + r0 * a.ld_x + k0, left, (int)a.ld_x, groups * EMB_SAVED_GROUP);
     const auto re = rows_at(reinterpret_cast<const char*>(a.exps) + r0 * a.ld_e + k0 / EMB_SAVED_GROUP, left, (int)a.ld_e,
                             groups);
@@ -102,9 +100,8 @@ struct YLoad {
   uint32_t w[8][kWords];
   __device__ __forceinline__ void load(const WArgs& a, int64_t r0, int c0, int quad, int oct) {
     constexpr int kSize = SPLIT == 1 ? 2 : 4;
-    // (an odd last column's word is read whole)
     const auto ry = rows_at(a.dy + r0 * a.ld_dy + (int64_t)c0 * kSize, rows_left(a, r0), (int)a.ld_dy,
-                            PAIRS ? ((a.F - c0) * kSize + 3) & ~3 : (a.F - c0) * kSize);
+                            dy_row_bytes(a.F, c0, kSize, PAIRS));
     const int at = 8 * oct * (int)a.ld_dy + 4 * kSize * quad;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -352,48 +349,6 @@ __global__ __launch_bounds__(256) void k_weight_parts(const float* parts, float*
     }
     Vec<float, V>::store(dw + i, t);
   }
-}
-
-// Tiles of 128 x 128 with the rows cut into as many parts as give each compute
-// unit a block, of at least four steps: 2048 x 256 x 256 11.7 us (13.9 with eight),
-// 2048 x 512 x 1536 18.6 and 18.6.
-// Tiles of 256 x 256 (one block a compute unit: 256 sums a lane, 128 KB of LDS)
-// with as many parts of at least 16 steps as fill one to four rounds of blocks.
-// The way that is estimated to take least is taken; the figures (us) are fitted to
-// some forty measurements: a block's beginning and end; a step of a small tile with one block a
-// compute unit; a step of a large one, more the more compute units are busy; the
-// writing and adding of a million parts' sums.  Measured, large against small tiles:
-// 32768 x 1024 x 1024 87 (126), 1024 x 2048 x 6144 42 (55), 4096 x 1500 x 2500 60 (65),
-// 8192 x 500 x 2500 53 (51), 2048 x 2048 x 2048 48 (38), 20000 x 300 x 800 50 (36); four
-// parts of 192 large tiles in three full rounds against one part 785 (811), of 96
-// tiles 416 (434).
-constexpr int kBlocks = 256, kSmallSteps = 4, kBigSteps = 16, kMostRounds = 4;
-constexpr double kSmallUs = 6., kSmallStepUs = 0.9, kBigUs = 11., kBigStepUs = 0.85, kBusyUs = 1., kPartUs = 1.5e-6;
-struct Plan {
-  int groups, parts, steps;  // groups of 128 columns a tile has each way; parts of so many steps
-  double us;
-};
-Plan plan_for(int64_t N, int32_t K, int32_t F, bool small) {
-  const int64_t steps = (N + kStep - 1) / kStep;
-  auto cut = [&](int groups, int rounds, int64_t least) {
-    const int64_t tile = groups * kGroup, tiles = ((K + tile - 1) / tile) * ((F + tile - 1) / tile);
-    int64_t p = rounds * kBlocks / tiles;
-    if (p > steps / least) p = steps / least;
-    if (p < 1) p = 1;
-    Plan q{groups, 1, (int)((steps + p - 1) / p), 0.};
-    if (q.steps > 0) q.parts = (int)((steps + q.steps - 1) / q.steps);
-    const double blocks = (double)q.parts * (double)tiles / kBlocks, full = (double)(int64_t)(blocks + 1. - 0.5 / kBlocks);
-    q.us = groups == 1 ? kSmallUs + q.steps * kSmallStepUs * (blocks > 1. ? blocks : 1.)
-                       : kBigUs + q.steps * (kBigStepUs + kBusyUs * blocks / full) * full;
-    if (q.parts > 1) q.us += (double)q.parts * K * F * kPartUs;
-    return q;
-  };
-  Plan best = cut(1, 1, kSmallSteps);
-  for (int r = 1; !small && r <= kMostRounds; ++r) {
-    const Plan q = cut(2, r, kBigSteps);
-    if (q.us < best.us) best = q;
-  }
-  return best;
 }
 
 }  // namespace
