@@ -350,9 +350,22 @@ def scan_step(x, f, o, state, y, bias=None, slots=None, stream=None) -> None:
 
 # ---------------------------------------------------------------- checkpoints
 
+def _scratch(size: int, device, stream):
+    """Workspace of one call on ``stream``, taken from the caching allocator in
+    that stream's order and given back in it: neither a call on another stream
+    nor what is allocated after this call gets it while the call may run."""
+    import torch
+    if stream is None:
+        return torch.empty(size, dtype=torch.uint8, device=device)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
+        return torch.empty(size, dtype=torch.uint8, device=device)
+
+
 class Checkpoint:
     """Activations kept in 8 bits: codes (int8) and an exponent a group of 32
-    columns, for up to ``rows`` rows of ``dim`` columns."""
+    columns, for ``rows`` rows of ``dim`` columns."""
 
     def __init__(self, rows: int, dim: int, device="cuda"):
         import torch
@@ -376,7 +389,6 @@ class Checkpoint:
     def _take(self, codes, exps, dim: int) -> None:
         self.codes, self.exps, self.dim, self.rows = codes, exps, dim, int(codes.shape[0])
         self.mat = Mat(codes, exps, dim)
-        self._ws = None
 
     def columns(self, first: int, count: int) -> Mat:
         """Columns first .. first + count - 1 as a matrix (for ``Scan``)."""
@@ -401,12 +413,10 @@ class Checkpoint:
         dy = _mat(dy)
         _want(dy, self.rows, dy.cols, "dy")
         size = lib().emb_weight_grad_workspace_size(self.rows, self.dim, dy.cols)
-        if size and (self._ws is None or self._ws.numel() < size):
-            import torch
-            self._ws = torch.empty(size, dtype=torch.uint8, device=self.codes.device)
+        ws = _scratch(size, self.codes.device, stream) if size else None
         _check("emb_weight_grad", lib().emb_weight_grad(
             self.rows, self.dim, dy.cols, self.mat.ref, dy.ref, _floats(dw, (self.dim, dy.cols), "dw"), int(add),
-            _ptr(self._ws) if size else None, size, _stream(stream)))
+            _ptr(ws), size, _stream(stream)))
 
 
 # ---------------------------------------------------------------- together

@@ -41,3 +41,38 @@ def test_weight_gradient_of_large_tiles_that_the_matrix_ends_in(n, K, F):
     want, mag = b.t().contiguous() @ y, b.abs().t().contiguous() @ y.abs()
     assert bool(((dw.double() - want).abs() <= (n + 8) * 2 * U * mag).all())
     assert float((dw.double() - want).norm()) <= 8 * 2 * U * float(mag.norm())
+
+
+def test_weight_gradients_on_another_stream_keep_to_their_own_workspace():
+    """Calls that cut the rows into parts, queued behind other work on a side
+    stream, of few columns first and then of more: what the current stream
+    allocates and fills meanwhile keeps its values, and the results are the
+    current stream's."""
+    import torch
+    import paper_2112_02752_amd as emb
+    n, K, widths = 4096, 256, (256, 640, 256)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    ck = emb.Checkpoint(n, K)
+    ck.pack(torch.randn((n, K), generator=g, device=DEV).bfloat16())
+    dys = [torch.randn((n, w), generator=g, device=DEV).bfloat16() for w in widths]
+    sizes = [emb.lib().emb_weight_grad_workspace_size(n, K, w) for w in widths]
+    assert all(sizes) and sizes[1] > sizes[0]
+    busy = torch.randn((8192, 8192), generator=g, device=DEV).bfloat16()
+    for as_int in (False, True):
+        outs = [torch.zeros((K, w), device=DEV) for w in widths]
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for _ in range(10):
+                busy @ busy
+        filled = []
+        for dy, dw, size in zip(dys, outs, sizes):
+            ck.weight_grad(dy, dw, stream=side.cuda_stream if as_int else side)
+            filled += [torch.full((size,), 7, dtype=torch.uint8, device=DEV) for _ in range(2)]
+        torch.cuda.synchronize()
+        assert all(bool((f == 7).all()) for f in filled)
+        for dy, dw in zip(dys, outs):
+            want = torch.empty_like(dw)
+            ck.weight_grad(dy, want)
+            assert torch.equal(dw, want)
