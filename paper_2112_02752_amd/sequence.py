@@ -132,6 +132,19 @@ def _floats(t, shape, what: str) -> Optional[int]:
 
 # ---------------------------------------------------------------- tokens
 
+def _check_state(opt: Optional[str], state, rows: int, dim: int) -> None:
+    """Refuse accumulators that the kernels would read or write past, or whose
+    values are no fp32: one a row ("adagrad") or one a value ("adagrad_ew")."""
+    if state is None or opt not in ("adagrad", "adagrad_ew"):
+        return
+    per = dim if opt == "adagrad_ew" else 1
+    flat = state.dim() == 1 or (state.dim() > 1 and state.numel() == state.shape[0] * per)
+    if not flat or state.numel() < rows * per or state.element_size() != 4 or not state.is_floating_point() \
+            or not state.is_contiguous() or (per == 1 and state.numel() != state.shape[0]):
+        raise ValueError(f"state is a contiguous fp32 tensor of {rows}{f' x {dim}' if per > 1 else ''} accumulators")
+    _device(state, "state")
+
+
 def token_fwd(tables: Tables, batch: Batch, out, scale: float = 1.0, pad_row: int = -1, stream=None) -> None:
     """out[j] = scale * W[key(j)] for every token of the batch's sequences
     (emb_token_fwd); zeros for tokens of the global row ``pad_row``."""
@@ -156,6 +169,7 @@ def token_grad(tables: Tables, batch: Batch, grad_out, dedup: DedupBuffers, grad
         if int(grad.shape[0]) < rows:
             raise ValueError("grad has too few rows")
         _floats(grad, (int(grad.shape[0]), D), "grad")
+    _check_state(opt, state, int(tables.row_offset[-1]), D)
     tok = CToken(scale, pad_row)
     upd = ctypes.byref(_update(opt, lr, eps, state, rounding, seed)) if opt is not None else None
     d = dedup
@@ -189,6 +203,7 @@ class TokenLayer:
                                                d.ws)) + (d.ws.numel(),)
         self._upd = None
         if opt is not None:
+            _check_state(opt, state, self._rows, self.dim)
             self._updc = _update(opt, lr, eps, state, rounding, seed)
             self._upd = ctypes.byref(self._updc)
             self._state = state
