@@ -243,10 +243,15 @@ class TokenLayer:
         self._backward(batch, grad_out, _floats(grad_rows, (int(grad_rows.shape[0]), self.dim), "grad_rows"),
                        LAYOUT["rows"], None, stream)
 
-    def update(self, batch: Batch, grad_out, stream=None) -> None:
-        """The optimizer step on the rows that were looked up."""
+    def _can_update(self) -> None:
         if self._upd is None:
             raise ValueError("a layer without an optimizer cannot update")
+        if self.opt != "sgd" and self._state is None:
+            raise ValueError(f"{self.opt} needs its accumulators as state")
+
+    def update(self, batch: Batch, grad_out, stream=None) -> None:
+        """The optimizer step on the rows that were looked up."""
+        self._can_update()
         self._updc.seed = self.seed + self.steps_done
         self._backward(batch, grad_out, None, LAYOUT["rows"], self._upd, stream)
         self.steps_done += 1
@@ -472,7 +477,7 @@ class SequenceLayer:
         self._rows = torch.empty((max_tokens, dim), **b16)
         self._proj = torch.empty((max_tokens, cols), **b16)
         self._saved = None
-        self._n = -1
+        self._n, self._offsets = -1, 0
 
     def _project(self, batch: Batch, n: int):
         import torch
@@ -496,7 +501,7 @@ class SequenceLayer:
                 self._saved = (Checkpoint(n, self.dim, rows.device), Checkpoint(n, 3 * self.hidden, rows.device))
             self._saved[0].pack(rows)
             self._saved[1].pack(proj)
-            self._n, self._h0 = n, h0
+            self._n, self._offsets, self._h0 = n, int(batch.offsets.numel()), h0
 
     def backward(self, batch: Batch, dy, dweight, dbias, dh_last=None, dh0=None, add: bool = False) -> None:
         """Backward of the last ``forward``, whose batch this is: the gradients of
@@ -504,8 +509,19 @@ class SequenceLayer:
         bias (fp32), and the optimizer's step on the table rows."""
         import torch
         n, H = int(batch.indices.numel()), self.hidden
-        if n != self._n:
+        if n != self._n or int(batch.offsets.numel()) != self._offsets:
             raise ValueError("backward follows a training forward of the same batch")
+        # (all that can be refused is, before the first kernel: the step can then be repeated)
+        self.tokens._can_update()
+        dy = _mat(dy)
+        _want(dy, n, H, "dy")
+        if dy.dtype != BF16:
+            raise ValueError("dy is bf16")
+        if _floats(dweight, (self.dim, 3 * H), "dweight") is None:
+            raise ValueError("dweight is wanted")
+        _floats(dbias, (H,), "dbias")
+        for t, name in ((dh_last, "dh_last"), (dh0, "dh0")):
+            _floats(t, (self._offsets - 1, H), name)
         self._n = -1
         saved_rows, saved_proj = self._saved
         scan = Scan(batch.offsets, *(saved_proj.columns(i * H, H) for i in range(3)), bias=self.bias, h0=self._h0)

@@ -76,3 +76,55 @@ def test_weight_gradients_on_another_stream_keep_to_their_own_workspace():
             want = torch.empty_like(dw)
             ck.weight_grad(dy, want)
             assert torch.equal(dw, want)
+
+
+# ---------------------------------------------------------------- the sequence layer
+
+def _layer(opt, state, lens=(7, 0, 30, 1, 66), R=50, D=40, H=32, seed=4, **kw):
+    import torch
+    import paper_2112_02752_amd as emb
+    g = torch.Generator().manual_seed(seed)
+    offs = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    n, M = int(offs[-1]), len(lens)
+    tables = emb.Tables(torch.randn((R, D), generator=g).to(DEV), [0, R])
+    weight = (torch.randn((D, 3 * H), generator=g) * D ** -0.5).bfloat16().to(DEV)
+    bias = torch.linspace(-1, 3, H, device=DEV)
+    layer = emb.SequenceLayer(tables, weight, bias, n, M, opt=opt, lr=0.1, state=state, **kw)
+    batch = emb.Batch(torch.from_numpy(offs).to(DEV), torch.randint(0, R, (n,), generator=g).to(DEV), M)
+    dy = torch.randn((n, H), generator=g).bfloat16().to(DEV)
+    y = torch.empty((n, H), dtype=torch.bfloat16, device=DEV)
+    return layer, batch, y, dy
+
+
+def test_a_refused_backward_runs_nothing_and_can_be_repeated():
+    import torch
+    import paper_2112_02752_amd as emb
+    for opt in (None, "adagrad"):
+        layer, batch, y, dy = _layer(opt, None)
+        layer.forward(batch, y)
+        dw, db = torch.full((40, 96), 5.0, device=DEV), torch.full((32,), 5.0, device=DEV)
+        with pytest.raises(ValueError, match="optimizer|accumulators"):
+            layer.backward(batch, dy, dw, db)
+        torch.cuda.synchronize()
+        assert bool((dw == 5).all()) and bool((db == 5).all())
+        with pytest.raises(ValueError, match="optimizer|accumulators"):
+            layer.tokens.update(batch, torch.zeros((dy.shape[0], 40), dtype=torch.bfloat16, device=DEV))
+    layer, batch, y, dy = _layer("sgd", None)
+    plain, batch2, y2, dy2 = _layer("sgd", None)
+    layer.forward(batch, y)
+    plain.forward(batch2, y2)
+    fewer = emb.Batch(batch.offsets[:-1].contiguous(), batch.indices, 4)
+    bad = [dict(dy=dy.float()), dict(dy=dy[:-1]), dict(dweight=dw[:-1]), dict(dbias=db[:-1]), dict(dweight=None),
+           dict(dh_last=torch.zeros(4, 32, device=DEV)), dict(dh0=torch.zeros(5, 31, device=DEV)), dict(batch=fewer)]
+    before = layer.tokens.tables.weights.clone()
+    for kw in bad:
+        args = dict(dict(batch=batch, dy=dy, dweight=dw, dbias=db), **kw)
+        with pytest.raises(ValueError):
+            layer.backward(**args)
+    torch.cuda.synchronize()
+    assert bool((dw == 5).all()) and bool((db == 5).all()) and torch.equal(before, layer.tokens.tables.weights)
+    dw2, db2 = torch.empty_like(dw), torch.empty_like(db)
+    layer.backward(batch, dy, dw, db)
+    plain.backward(batch2, dy2, dw2, db2)
+    assert torch.equal(dw, dw2) and torch.equal(db, db2)
+    assert torch.equal(layer.tokens.tables.weights, plain.tokens.tables.weights)
