@@ -399,8 +399,9 @@ typedef struct {
 /* Lookup of single tokens: out[j][d] = scale * W[key(j)][d] for every position
  * j of the batch, computed in fp32 and rounded once to out's type (fp32 or
  * bf16).  Tokens whose key is pad_row (a global row; negative: none) give
- * zeros, as do ids outside their table.  out: N rows of dim columns, aligned
- * to its element type. */
+ * zeros, as do ids outside their table, of 32 or 64 bits (the gradient wants
+ * ids within their tables).  out: N rows of dim columns, aligned to its
+ * element type. */
 typedef struct {
   float scale;
   int64_t pad_row;
@@ -424,7 +425,8 @@ typedef enum { EMB_ROWS = 0, EMB_TABLE = 1, EMB_TABLE_ADD = 2 } emb_grad_layout;
  * says, or NULL with fuse.  fuse: NULL, or the optimizer step applied to the
  * looked-up rows but the padding row, as in emb_grad_reduce (grad must then
  * be NULL).  The dedup's outputs and ws are those emb_unique_ids left for this
- * batch, unmodified.  EMB_EUNSUPPORTED for rows of more than 8192 values, or
+ * batch, unmodified; its ids lie within their tables, as that call wants them
+ * (emb_validate_batch tells).  EMB_EUNSUPPORTED for rows of more than 8192 values, or
  * of more than 4096 that are no multiple of 8.
  * After a dedup that failed on the device no table row is written, and
  * gradient rows are written as zeros (EMB_ROWS, EMB_TABLE) or left. */

@@ -48,6 +48,16 @@ struct Stacked<true> {
   TableOffsets ro;
 };
 
+// id j, or kNoRow for one that is negative or has more than 32 bits (no table has that many rows, nor row kNoRow)
+__device__ __forceinline__ uint32_t load_row(const void* idx, int32_t idx64, int64_t j) {
+  if (idx64) {
+    const u32x2 id = static_cast<const u32x2*>(idx)[j];
+    return id.y == 0u ? id.x : kNoRow;
+  }
+  const int32_t id = static_cast<const int32_t*>(idx)[j];
+  return id >= 0 ? (uint32_t)id : kNoRow;
+}
+
 template <typename TW, typename TO, int V, int AHEAD, bool STREAM, bool MANY>
 __global__ __launch_bounds__(kFwdThreads) void k_token_fwd(TokFwd a, Stacked<MANY> st) {
   const int lanes = 1 << a.log_g, per = kFwdThreads >> a.log_g;
@@ -60,7 +70,7 @@ __global__ __launch_bounds__(kFwdThreads) void k_token_fwd(TokFwd a, Stacked<MAN
     const int64_t j = j0 + (int64_t)u * per;
     key[u] = kNoRow;
     if (j < a.N) {
-      const int32_t id = load_id(a.idx, a.idx64, j);
+      const uint32_t id = load_row(a.idx, a.idx64, j);
       if constexpr (MANY) {
         // the table whose sequences hold position j: the last with a first position at or before it
         int t = 0, n = a.T;
@@ -70,9 +80,9 @@ __global__ __launch_bounds__(kFwdThreads) void k_token_fwd(TokFwd a, Stacked<MAN
           else n = half;
         }
         const uint32_t r0 = st.ro.off[t];
-        key[u] = (uint32_t)id < st.ro.off[t + 1] - r0 ? r0 + (uint32_t)id : kNoRow;
+        key[u] = id < st.ro.off[t + 1] - r0 ? r0 + id : kNoRow;
       } else {
-        key[u] = (uint32_t)id;
+        key[u] = id;
       }
       if (key[u] == a.pad) key[u] = kNoRow;
     }

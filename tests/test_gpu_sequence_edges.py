@@ -128,3 +128,30 @@ def test_a_refused_backward_runs_nothing_and_can_be_repeated():
     plain.backward(batch2, dy2, dw2, db2)
     assert torch.equal(dw, dw2) and torch.equal(db, db2)
     assert torch.equal(layer.tokens.tables.weights, plain.tokens.tables.weights)
+
+
+# ---------------------------------------------------------------- tokens
+
+@pytest.mark.parametrize("bits", [32, 64])
+@pytest.mark.parametrize("rows", [[10], [10, 5]])
+def test_lookup_of_ids_outside_the_table(rows, bits):
+    """Zeros for them, whatever their low 32 bits are; so too where those are
+    the padding row's."""
+    import torch
+    import paper_2112_02752_amd as emb
+    W = torch.arange(1, 1 + sum(rows) * 8, dtype=torch.float32, device=DEV).view(-1, 8)
+    big = [2 ** 32 + 3, -2 ** 32 + 3, 2 ** 63 - 1, -2 ** 63, 2 ** 31, 2 ** 40] if bits == 64 else [2 ** 31 - 1, -2 ** 31]
+    one = [3, 0, 10, -1] + big
+    ids = one + ([4, 5, -1, 0] + big if len(rows) > 1 else [])
+    offs = [0, len(one)] + ([len(ids)] if len(rows) > 1 else [])
+    batch = emb.Batch(torch.tensor(offs, dtype=torch.int32, device=DEV),
+                      torch.tensor(ids, dtype=torch.int64 if bits == 64 else torch.int32, device=DEV), 1)
+    start = [0] + list(np.cumsum(rows))
+    for pad in (-1, 3):
+        out = torch.full((len(ids), 8), 7.0, device=DEV)
+        emb.token_fwd(emb.Tables(W, start), batch, out, pad_row=pad)
+        for j, i in enumerate(ids):
+            t = 0 if j < len(one) else 1
+            key = start[t] + i if 0 <= i < rows[t] else -1
+            want = W[key] if key >= 0 and key != pad else torch.zeros(8, device=DEV)
+            assert torch.equal(out[j], want), (j, i)
