@@ -133,12 +133,13 @@ struct YLoad {
       }
     } else {
       // v = p0 + p1 + p2: each part the leading 8 bits of what the parts before it leave (cut off, so every
-      // difference is exact); an infinity or NaN is all in p0
+      // difference is exact); an infinity or NaN is all in p0 (a signalling NaN, whose bits may all be among those cut
+      // off, as the quiet one)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         float v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i][j]);
+        for (int i = 0; i < 8; ++i) v[i] = __builtin_canonicalizef(__uint_as_float(w[i][j]));
 #pragma unroll
         for (int p = 0; p < SPLIT; ++p) {
           uint32_t o[4];

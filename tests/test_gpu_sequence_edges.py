@@ -78,6 +78,24 @@ def test_weight_gradients_on_another_stream_keep_to_their_own_workspace():
             assert torch.equal(dw, want)
 
 
+def test_weight_gradient_of_any_nan():
+    """A column of dy with a NaN of any bits gives NaN, the others sums of ones."""
+    import torch
+    import paper_2112_02752_amd as emb
+    bits = [0x7f800001, 0x7f80ffff, 0xff800001 - 2 ** 32, 0x7fc00000, 0x7fbfffff, 0xffffffff - 2 ** 32]
+    dy = torch.ones(70, 24, device=DEV)
+    for i, b in enumerate(bits):
+        dy.view(torch.int32)[11 * i, 2 * i] = b
+    assert dy.isnan().sum() == len(bits)
+    ck = emb.Checkpoint(70, 64)
+    ck.pack(torch.ones(70, 64, device=DEV))
+    dw = torch.zeros(64, 24, device=DEV)
+    ck.weight_grad(dy, dw)
+    dirty = torch.zeros(24, dtype=torch.bool, device=DEV)
+    dirty[0:2 * len(bits):2] = True
+    assert bool(dw[:, dirty].isnan().all()) and bool((dw[:, ~dirty] == 70).all())
+
+
 # ---------------------------------------------------------------- the sequence layer
 
 def _layer(opt, state, lens=(7, 0, 30, 1, 66), R=50, D=40, H=32, seed=4, **kw):
