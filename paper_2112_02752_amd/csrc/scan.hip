@@ -138,11 +138,24 @@ struct Marks {
     }
     seq = m;
     uint32_t s = off[m] == q0 ? 1u : 0u;
-    for (int k = m + 1; k <= a.M; ++k) {
-      const int t = off[k] - q0;
-      if (t > P) break;
+    int k = m + 1, at = k <= a.M ? off[k] : INT32_MAX;
+    while (at - q0 <= P) {
+      int next = k < a.M ? off[k + 1] : INT32_MAX;
+      if (next == at) {
+        // Of the sequences that begin there the last is the one with positions, and there may be millions: from k on
+        // by doubling steps, then by halving ones (80 ns each one by one: 10000 of them took a call from 20 us to 820)
+        int d = 1;
+        for (; d <= a.M - k && off[k + d] == at; d *= 2) k += d;
+        for (d /= 2; d > 0; d /= 2) {
+          if (d <= a.M - k && off[k + d] == at) k += d;
+        }
+        next = k < a.M ? off[k + 1] : INT32_MAX;
+      }
+      const int t = at - q0;
       s |= 1u << t;
       if (k < a.M && lane >= t) seq = k;
+      ++k;
+      at = next;
     }
     starts = s & ((1u << P) - 1u);
     ends = s >> 1;

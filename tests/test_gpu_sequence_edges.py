@@ -173,3 +173,65 @@ def test_lookup_of_ids_outside_the_table(rows, bits):
             key = start[t] + i if 0 <= i < rows[t] else -1
             want = W[key] if key >= 0 and key != pad else torch.zeros(8, device=DEV)
             assert torch.equal(out[j], want), (j, i)
+
+
+# ---------------------------------------------------------------- recurrence
+
+def _run_scan(offs, x, f, o, dy, bias=None, h0=None, dhl=None, per_seq=True):
+    """y, last states, dx, df, do, dbias, dh0 of one forward and backward (numpy)."""
+    import torch
+    import paper_2112_02752_amd as emb
+    dev = lambda v: torch.from_numpy(np.ascontiguousarray(v)).to(DEV) if v is not None else None  # noqa: E731
+    n, D = x.shape
+    M = len(offs) - 1
+    rec = emb.Recurrence(n, M, D)
+    scan = emb.Scan(dev(offs), dev(x), dev(f), dev(o), bias=dev(bias), h0=dev(h0))
+    y, g = torch.empty(n, D, device=DEV), [torch.empty(n, D, device=DEV) for _ in range(3)]
+    db = torch.empty(D, device=DEV)
+    last, dh0 = (torch.empty(M, D, device=DEV) if per_seq else None for _ in range(2))
+    rec.forward(scan, y, last)
+    rec.backward(scan, dev(dy), *g, dbias=db, dh_last=dev(dhl), dh0=dh0)
+    return [v.cpu().numpy() if v is not None else None for v in (y, last, *g, db, dh0)]
+
+
+@pytest.mark.parametrize("run", [1, 2, 3, 4, 5, 6, 7, 8, 15, 16, 17, 1000])
+def test_scan_past_runs_of_empty_sequences(run):
+    """The same values as without the empty sequences, bit for bit, and theirs
+    handed through."""
+    D = 5
+    rng = np.random.default_rng(run)
+    lens = [1, 3, 12, 16, 1, 128, 64, 2, 300, 1]
+    offs = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    n, M = int(offs[-1]), len(lens)
+    x, f, o, dy = rng.standard_normal((4, n, D)).astype(np.float32)
+    h0, dhl = rng.standard_normal((2, M, D)).astype(np.float32)
+    want = _run_scan(offs, x, f, o, dy, None, h0, dhl)
+    # runs of `run` and run // 2 empty sequences before, between and after them
+    more, real = [], []
+    for m in range(M):
+        more += [0] * (run if m % 2 == 0 else run // 2)
+        real.append(len(more))
+        more.append(lens[m])
+    more += [0] * run
+    h0m, dhlm = rng.standard_normal((2, len(more), D)).astype(np.float32)
+    h0m[real], dhlm[real] = h0, dhl
+    got = _run_scan(np.concatenate([[0], np.cumsum(more)]).astype(np.int32), x, f, o, dy, None, h0m, dhlm)
+    empty = np.setdiff1d(np.arange(len(more)), real)
+    for i in (0, 2, 3, 4, 5):
+        assert np.array_equal(got[i], want[i]), i
+    assert np.array_equal(got[1][real], want[1]) and np.array_equal(got[6][real], want[6])
+    assert np.array_equal(got[1][empty], h0m[empty]) and np.array_equal(got[6][empty], dhlm[empty])
+
+
+def test_scan_past_millions_of_empty_sequences():
+    """Thirty million of them where the span begins, ends and in the middle: the
+    spans after them wait for no walk along them."""
+    n, D = 500, 3
+    rng = np.random.default_rng(2)
+    x, f, o, dy = rng.standard_normal((4, n, D)).astype(np.float32)
+    places = [0, 128, 130, 300, n]
+    want = _run_scan(np.array(places, dtype=np.int32), x, f, o, dy, per_seq=False)
+    offs = np.repeat(np.array(places, dtype=np.int32), [6_000_001, 6_000_000, 6_000_003, 6_000_000, 6_000_000])
+    got = _run_scan(offs, x, f, o, dy, per_seq=False)
+    for i in (0, 2, 3, 4, 5):
+        assert np.array_equal(got[i], want[i]), i
