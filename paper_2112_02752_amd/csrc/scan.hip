@@ -92,6 +92,13 @@ __device__ __forceinline__ float gate(float z) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * z));
 }
 
+// with 1 - sigmoid(z), without cancellation; times sigmoid(z), as here, it may be anything finite where that is zero
+__device__ __forceinline__ float gate(float z, float& rest) {
+  const float e = __builtin_amdgcn_exp2f(-1.44269504f * z), s = __builtin_amdgcn_rcpf(1.f + e);
+  rest = __builtin_elementwise_minimum(e, 0x1p126f) * s;
+  return s;
+}
+
 // (kernels of their own for the two kinds of stores: behind a branch they become one)
 template <typename T, int V, bool STREAM>
 __device__ __forceinline__ void put(void* p, const float (&v)[V]) {
@@ -509,9 +516,9 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_bwd(Scan a) {
         forget(gf[t].get(i) + bias[i], fa[t][i], fq[t][i]);
         u[t][i] = gy[t].get(i);
         if constexpr (GATED) {
-          const float s = gate(go[t].get(i));
-          u[t][i] *= s;
-          v[t][i] = u[t][i] * (1.f - s);
+          float rest;
+          u[t][i] *= gate(go[t].get(i), rest);
+          v[t][i] = u[t][i] * rest;
         }
       }
     }

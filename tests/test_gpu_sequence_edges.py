@@ -235,3 +235,22 @@ def test_scan_past_millions_of_empty_sequences():
     got = _run_scan(offs, x, f, o, dy, per_seq=False)
     for i in (0, 2, 3, 4, 5):
         assert np.array_equal(got[i], want[i]), i
+
+
+def test_gradient_of_an_output_gate_that_is_nearly_open_or_shut():
+    """do = dy h s (1 - s) to fp32's precision of each factor: for a gate of |z|
+    the exponent's rounding gives (|z| + 8) u of either factor's smaller one, the
+    state and the products 8 u; sequences of one position, where h = x / 2."""
+    z = np.array([-80, -60, -30, -16, -8, -2, -1e-3, 0, 1e-3, 2, 8, 12, 16, 20, 30, 60, 80], dtype=np.float32)
+    n, D = 70, len(z)
+    rng = np.random.default_rng(9)
+    x, dy = rng.standard_normal((2, n, D)).astype(np.float32)
+    o = np.tile(z, (n, 1))
+    got = _run_scan(np.arange(n + 1, dtype=np.int32), x, np.zeros_like(x), o, dy)
+    zd = o.astype(np.float64)
+    want = dy.astype(np.float64) * x / 2 / ((1 + np.exp(-zd)) * (1 + np.exp(zd)))
+    assert (np.abs(got[4] - want) <= (np.abs(zd) + 24) * U * np.abs(want)).all()
+    # ends of the type: no gradient, no NaN
+    o[:, 0], o[:, 1], o[:, 2], o[:, 3] = np.inf, -np.inf, 3e38, -3e38
+    got = _run_scan(np.arange(n + 1, dtype=np.int32), x, np.zeros_like(x), o, dy)
+    assert (got[4][:, :4] == 0).all() and np.isfinite(got[4]).all()
