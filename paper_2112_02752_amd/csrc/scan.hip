@@ -110,6 +110,24 @@ __device__ __forceinline__ void put(void* p, const float (&v)[V]) {
 __device__ __forceinline__ float through(float A, float B, float h) {
   return A < 0.f ? B : __builtin_fmaf(A, h, B);
 }
+// A product of gates is above zero, however many: where it has underflowed, the least number stands for it, so that
+// an infinite state stays one.  (NaN stays NaN.)
+__device__ __forceinline__ float above_zero(float A) { return __builtin_elementwise_maximum(A, 0x1p-149f); }
+// the product of two that may be kResets
+__device__ __forceinline__ float join(float A, float A2) { return A2 < 0.f || A < 0.f ? kResets : above_zero(A * A2); }
+// whether a state of the wavefront is infinite: rare, and only then the products for single positions matter so
+template <int V>
+__device__ __forceinline__ bool any_infinite(const float (&h)[V]) {
+  bool some = false;
+#pragma unroll
+  for (int i = 0; i < V; ++i) some |= __builtin_isinf(h[i]);
+  return __ballot(some) != 0u;
+}
+template <int V>
+__device__ __forceinline__ void above_zero(float (&A)[V], const float (&h)[V]) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) A[i] = __builtin_isinf(h[i]) ? above_zero(A[i]) : A[i];
+}
 
 struct Scan {
   const int32_t* offsets;
@@ -386,10 +404,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_fwd(Scan a) {
         }
       }
     }
-    if (mk.starts) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) A[i] = kResets;
-    }
+    for (int i = 0; i < V; ++i) A[i] = mk.starts ? kResets : above_zero(A[i]);
   }
 #pragma unroll
   for (int i = 0; i < V; ++i) {
@@ -409,7 +425,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_fwd(Scan a) {
       for (int i = 0; i < V; ++i) {
         const float A2 = s_A[w][i * kWave + lane], B2 = s_B[w][i * kWave + lane];
         B[i] = through(A2, B2, B[i]);
-        A[i] = A2 < 0.f || A[i] < 0.f ? kResets : A[i] * A2;
+        A[i] = join(A[i], A2);
       }
     }
     resets = uniform(A[0] < 0.f);
@@ -456,6 +472,24 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_fwd(Scan a) {
 #pragma unroll
       for (int i = 0; i < V; ++i) y[i] = __builtin_fmaf(Ae[i], h[i], Be[i]);
       store_f32<V>(a.h_last + (int64_t)mk.of(t) * a.D + col, in, y);
+    }
+  }
+  // (after the others, whose stores then do not wait for the question)
+  if (any_infinite<V>(h)) {
+#pragma unroll
+    for (int t = 0; t < P; ++t) {
+      if (t >= n || mk.begun(t)) continue;
+      float y[V];
+      above_zero<V>(At[t], h);
+#pragma unroll
+      for (int i = 0; i < V; ++i) y[i] = __builtin_fmaf(At[t][i], h[i], Bt[t][i]);
+      if (in) Vec<T, V>::store(a.y.p + (int64_t)(q0 + t) * a.y.ld + (uint32_t)col * (uint32_t)(Vec<T, V>::kBytes / V), y);
+      if (a.h_last && mk.end(t)) {
+        above_zero<V>(Ae, h);
+#pragma unroll
+        for (int i = 0; i < V; ++i) y[i] = __builtin_fmaf(Ae[i], h[i], Be[i]);
+        store_f32<V>(a.h_last + (int64_t)mk.of(t) * a.D + col, in, y);
+      }
     }
   }
 }
@@ -557,8 +591,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_bwd(Scan a) {
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      if (mk.starts) A[i] = kResets;
-      if (mk.ends) A2[i] = kResets;
+      A[i] = mk.starts ? kResets : above_zero(A[i]);
+      A2[i] = mk.ends ? kResets : above_zero(A2[i]);
     }
   }
 #pragma unroll
@@ -584,7 +618,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_bwd(Scan a) {
       for (int i = 0; i < V; ++i) {
         const float An = s_A[1][w][i * kWave + lane], Bn = s_B[1][w][i * kWave + lane];
         B2[i] = through(An, Bn, B2[i]);
-        A2[i] = An < 0.f || A2[i] < 0.f ? kResets : A2[i] * An;
+        A2[i] = join(A2[i], An);
       }
     }
     resets = uniform(A2[0] < 0.f);
@@ -667,6 +701,11 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan_bwd(Scan a) {
     for (int w = kW - 1; w > wave; --w) {
 #pragma unroll
       for (int i = 0; i < V; ++i) g[i] = through(s_A[1][w][i * kWave + lane], s_B[1][w][i * kWave + lane], g[i]);
+    }
+    if (any_infinite<V>(g)) {
+      above_zero<V>(W0, g);
+#pragma unroll
+      for (int t = 0; t < P; ++t) above_zero<V>(fq[t], g);
     }
 #pragma unroll
     for (int t = P - 1; t >= 0; --t) {

@@ -254,3 +254,28 @@ def test_gradient_of_an_output_gate_that_is_nearly_open_or_shut():
     o[:, 0], o[:, 1], o[:, 2], o[:, 3] = np.inf, -np.inf, 3e38, -3e38
     got = _run_scan(np.arange(n + 1, dtype=np.int32), x, np.zeros_like(x), o, dy)
     assert (got[4][:, :4] == 0).all() and np.isfinite(got[4]).all()
+
+
+@pytest.mark.parametrize("n", [100, 300, 3000])
+def test_scan_keeps_an_infinite_state_past_products_that_underflow(n):
+    """An infinity in a sequence stays one to its end (gates of a half: their
+    products underflow after 150 positions), and so does one in the gradient to
+    its beginning; the other columns are finite."""
+    from tests.test_gpu_sequence import _plain_backward, _plain_forward
+    D = 6
+    rng = np.random.default_rng(n)
+    x, f, o, dy = rng.standard_normal((4, n, D)).astype(np.float32)
+    f[:, 2:4] -= 4
+    x[20, 0], x[20, 2], dy[n - 10, 1], dy[n - 10, 3] = np.inf, -np.inf, np.inf, -np.inf
+    offs = np.array([0, 5, n], dtype=np.int32)
+    h0 = rng.standard_normal((2, D)).astype(np.float32)
+    got = _run_scan(offs, x, f, o, dy, None, h0, None)
+    xd, fd, od, dyd = (v.astype(np.float64) for v in (x, f, o, dy))
+    with np.errstate(invalid="ignore"):
+        a, q, before, h, y, last = _plain_forward(offs, xd, fd, od, None, h0.astype(np.float64))
+        dh, dx, df, do, db, dh0 = _plain_backward(offs, xd, a, q, before, h, od, dyd, None)
+    assert np.isinf(y[20:, 0]).all() and np.isinf(dx[5:n - 9, 1]).all()
+    for v, w in zip(got, (y, last, dx, df, do, None, dh0)):
+        if w is not None:
+            assert np.array_equal(np.isnan(v), np.isnan(w)) and np.array_equal(np.isinf(v), np.isinf(w))
+            assert np.array_equal(np.sign(v[np.isinf(w)]), np.sign(w[np.isinf(w)]))
