@@ -67,43 +67,47 @@ class Mat:
     tensor's columns); an 8-bit one comes from ``Checkpoint.columns``.  Kept by
     a program between calls, it costs a call one address check."""
 
-    __slots__ = ("tensor", "exps", "rows", "cols", "_c", "_at", "ref")
+    __slots__ = ("tensor", "exps", "rows", "cols", "_c", "_at", "_at_exps", "_fixed", "_taken", "ref")
 
     def __init__(self, tensor, exps=None, cols: Optional[int] = None):
+        self.tensor, self.exps, self._fixed = tensor, exps, cols
+        self._c = CMat()
+        self.ref = ctypes.byref(self._c)
+        self._taken = 0     # how often the descriptor was made
+        self._take()
+
+    def _take(self) -> None:
         import torch
+        tensor, exps = self.tensor, self.exps
         if tensor.dim() != 2 or (tensor.shape[1] > 1 and tensor.stride(1) != 1):
             raise ValueError("a matrix has two dimensions and contiguous columns")
         _device(tensor, "a matrix")
-        self.tensor, self.exps = tensor, exps
-        self.rows = int(tensor.shape[0])
-        self.cols = int(tensor.shape[1]) if cols is None else cols
-        ld = int(tensor.stride(0)) if self.rows > 1 else max(int(tensor.stride(0)), int(tensor.shape[1]))
+        rows, wide = int(tensor.shape[0]), int(tensor.shape[1])
+        ld = int(tensor.stride(0)) if rows > 1 else max(int(tensor.stride(0)), wide)
         if exps is not None:
             if tensor.dtype != torch.int8 or exps.dtype != torch.uint8:
                 raise ValueError("a checkpoint holds int8 codes and uint8 exponents")
-            le = int(exps.stride(0)) if self.rows > 1 else int(exps.shape[1])
-            self._c = CMat(0, ld, SAVED8, 0, le)
+            dtype, le = SAVED8, int(exps.stride(0)) if rows > 1 else int(exps.shape[1])
         else:
             if tensor.dtype not in (torch.float32, torch.bfloat16):
                 raise ValueError("a matrix is fp32 or bf16")
-            self._c = CMat(0, ld, BF16 if tensor.dtype == torch.bfloat16 else FP32, None, 0)
-        if ld < int(tensor.shape[1]):
+            dtype, le = BF16 if tensor.dtype == torch.bfloat16 else FP32, 0
+        if ld < wide:
             raise ValueError("rows overlap")
-        self._at = None
-        self.ref = ctypes.byref(self._c)
-        self.c()
+        self.rows, self.cols = rows, wide if self._fixed is None else self._fixed
+        self._at, self._at_exps = tensor.data_ptr(), exps.data_ptr() if exps is not None else None
+        c = self._c
+        c.data, c.ld, c.dtype, c.exps, c.ld_exps = self._at or None, ld, dtype, self._at_exps or None, le
+        self._taken += 1
 
     @property
     def dtype(self) -> int:
         return self._c.dtype
 
     def c(self) -> CMat:
-        at = self.tensor.data_ptr()
-        if at != self._at:
-            self._at = at
-            self._c.data = at or None
-            if self.exps is not None:
-                self._c.exps = self.exps.data_ptr()
+        """The C descriptor; made again if a tensor has got other memory."""
+        if self.tensor.data_ptr() != self._at or (self.exps is not None and self.exps.data_ptr() != self._at_exps):
+            self._take()
         return self._c
 
 
@@ -206,7 +210,7 @@ class TokenLayer:
             _check_state(opt, state, self._rows, self.dim)
             self._updc = _update(opt, lr, eps, state, rounding, seed)
             self._upd = ctypes.byref(self._updc)
-            self._state = state
+            self._state, self._state_at = state, _ptr(state)
 
     def forward(self, batch: Batch, out, stream=None) -> None:
         out = _mat(out)
@@ -248,6 +252,9 @@ class TokenLayer:
             raise ValueError("a layer without an optimizer cannot update")
         if self.opt != "sgd" and self._state is None:
             raise ValueError(f"{self.opt} needs its accumulators as state")
+        if _ptr(self._state) != self._state_at:     # the tensor has got other memory
+            _check_state(self.opt, self._state, self._rows, self.dim)
+            self._updc.state = self._state_at = _ptr(self._state)
 
     def update(self, batch: Batch, grad_out, stream=None) -> None:
         """The optimizer step on the rows that were looked up."""
@@ -281,16 +288,34 @@ class Scan:
             raise ValueError("offsets are a contiguous int32 vector")
         _device(offsets, "offsets")
         self.x, self.f, self.o = _mat(x), _mat(f), _mat(o) if o is not None else None
-        self.tokens, self.dim = self.x.rows, self.x.cols
-        self.seqs = int(offsets.numel()) - 1
-        _want(self.f, self.tokens, self.dim, "f")
-        if self.o is not None:
-            _want(self.o, self.tokens, self.dim, "o")
         self.offsets, self.bias, self.h0 = offsets, bias, h0
-        self._c = CScan(self.tokens, self.seqs, self.dim, offsets.data_ptr(), self.x.c(), self.f.c(),
-                        self.o.c() if self.o is not None else CMat(), _floats(bias, (self.dim,), "bias"),
-                        _floats(h0, (self.seqs, self.dim), "h0"))
+        self._c = CScan()
         self.ref = ctypes.byref(self._c)
+        self._key = None
+        self.c()
+
+    def c(self) -> CScan:
+        """The C descriptor; made again if a tensor has got other memory."""
+        x, f, o, bias, h0 = self.x, self.f, self.o, self.bias, self.h0
+        x.c()
+        f.c()
+        if o is not None:
+            o.c()
+        key = (self.offsets.data_ptr(), self.offsets.numel(), x, x._taken, f, f._taken, o,
+               o._taken if o is not None else 0, bias.data_ptr() if bias is not None else 0,
+               h0.data_ptr() if h0 is not None else 0)
+        if key != self._key:
+            self.tokens, self.dim, self.seqs = x.rows, x.cols, key[1] - 1
+            _want(f, self.tokens, self.dim, "f")
+            if o is not None:
+                _want(o, self.tokens, self.dim, "o")
+            c = self._c
+            c.num_tokens, c.num_seqs, c.dim, c.offsets = self.tokens, self.seqs, self.dim, key[0]
+            c.x, c.f, c.o = x._c, f._c, o._c if o is not None else CMat()
+            c.bias = _floats(bias, (self.dim,), "bias")
+            c.h0 = _floats(h0, (self.seqs, self.dim), "h0")
+            self._key = key
+        return self._c
 
 
 def scan_workspace_size(num_tokens: int, dim: int) -> int:
@@ -317,15 +342,17 @@ class Recurrence:
         self._tokens = None
 
     def _scan(self, scan: Scan):
+        scan.c()
         if scan.tokens > self.max_tokens or scan.dim != self.dim:
             raise ValueError("batch larger than the recurrence's buffers, or of another width")
         return scan.ref
 
     def forward(self, scan: Scan, y, h_last=None, stream=None) -> None:
         """y (and the state after each sequence into ``h_last``, fp32 [M][D])."""
+        ref = self._scan(scan)
         y = _mat(y)
         _want(y, scan.tokens, self.dim, "y")
-        _check("emb_scan_fwd", lib().emb_scan_fwd(self._scan(scan), y.ref,
+        _check("emb_scan_fwd", lib().emb_scan_fwd(ref, y.ref,
                                                   _floats(h_last, (scan.seqs, self.dim), "h_last"), self._states,
                                                   self._ws, self._wsb, _stream(stream)))
         self._tokens = scan.tokens
@@ -334,6 +361,7 @@ class Recurrence:
         """Gradients of the last forward: of the inputs, the bias and the first
         states, from those of y and of the last states.  ``scan`` is the
         forward's, or one whose matrices are restored from its checkpoints."""
+        ref = self._scan(scan)
         if self.states is None or self._tokens != scan.tokens:
             raise ValueError("backward follows the forward of the same batch on a recurrence made with train")
         mats = [_mat(m) for m in (dy, dx, df)] + ([_mat(do)] if scan.o is not None else [])
@@ -341,7 +369,7 @@ class Recurrence:
             _want(m, scan.tokens, self.dim, name)
         each = (scan.seqs, self.dim)
         _check("emb_scan_bwd", lib().emb_scan_bwd(
-            self._scan(scan), self._states, mats[0].ref, _floats(dh_last, each, "dh_last"), mats[1].ref, mats[2].ref,
+            ref, self._states, mats[0].ref, _floats(dh_last, each, "dh_last"), mats[1].ref, mats[2].ref,
             mats[3].ref if scan.o is not None else None, _floats(dbias, (self.dim,), "dbias"),
             _floats(dh0, each, "dh0"), self._ws, self._wsb, _stream(stream)))
 

@@ -279,3 +279,73 @@ def test_scan_keeps_an_infinite_state_past_products_that_underflow(n):
         if w is not None:
             assert np.array_equal(np.isnan(v), np.isnan(w)) and np.array_equal(np.isinf(v), np.isinf(w))
             assert np.array_equal(np.sign(v[np.isinf(w)]), np.sign(w[np.isinf(w)]))
+
+
+# ---------------------------------------------------------------- the caller's objects
+
+def test_descriptors_follow_their_tensors():
+    """Tensors that get other memory (as an optimizer or a checkpoint's loading
+    gives a parameter) are read and written there; what they had stays alive
+    beside them and keeps its values."""
+    import torch
+    import paper_2112_02752_amd as emb
+    g = torch.Generator(device=DEV).manual_seed(6)
+    n, M, D = 90, 3, 64
+    rnd = lambda *s: torch.randn(*s, generator=g, device=DEV)  # noqa: E731
+    offs = torch.tensor([0, 40, 50, n], dtype=torch.int32, device=DEV)
+    t = dict(x=rnd(n, D), f=rnd(n, D), o=rnd(n, D), bias=rnd(D), h0=rnd(M, D), offsets=offs)
+    y, last = torch.empty(n, D, device=DEV), torch.empty(M, D, device=DEV)
+    scan = emb.Scan(t["offsets"], t["x"], t["f"], t["o"], bias=t["bias"], h0=t["h0"])
+    y_mat, rec = emb.Mat(y), emb.Recurrence(200, 5, D)
+    rec.forward(scan, y_mat, last)
+
+    def follows():
+        rec.forward(scan, y_mat, last)
+        want, want_last = torch.empty_like(y), torch.empty_like(last)
+        rec.forward(emb.Scan(*(t[k].clone() for k in ("offsets", "x", "f", "o")), bias=t["bias"].clone(),
+                             h0=t["h0"].clone()), want, want_last)
+        assert torch.equal(y, want) and torch.equal(last, want_last)
+
+    kept = []
+    for name, new in (("x", rnd(n, D)), ("f", rnd(n, D)), ("o", rnd(n, D)), ("bias", rnd(D)), ("h0", rnd(M, D)),
+                      ("offsets", torch.tensor([0, 7, 7, n], dtype=torch.int32, device=DEV))):
+        kept.append(t[name].detach().clone()), kept.append(t[name].detach())
+        t[name].data = new
+        follows()
+    kept.append(y.detach()), kept.append(y.clone())
+    y.data = torch.empty(n, D, device=DEV)
+    t["x"].data = rnd(n, D)
+    follows()
+    for a, b in zip(kept[::2], kept[1::2]):
+        assert torch.equal(a, b)
+    # a wider or longer one by its own rows
+    for name in ("x", "f", "o"):
+        t[name].data = rnd(n + 5, 2 * D)[:, :D]
+    t["offsets"].data = torch.tensor([0, 40, 50, n + 5], dtype=torch.int32, device=DEV)
+    y.data = torch.empty(n + 5, D, device=DEV)
+    follows()
+    t["bias"].data = rnd(D - 1)
+    with pytest.raises(ValueError, match="bias"):
+        rec.forward(scan, y_mat, last)
+    t["bias"].data = rnd(D)
+    t["f"].data = rnd(n, D)
+    with pytest.raises(ValueError, match="f has"):
+        rec.forward(scan, y_mat, last)
+
+
+def test_accumulators_that_move_are_followed():
+    import torch
+    import paper_2112_02752_amd as emb
+    W = torch.ones(10, 16, device=DEV)
+    state = torch.zeros(10, device=DEV)
+    layer = emb.TokenLayer(emb.Tables(W, [0, 10]), opt="adagrad", lr=0.1, state=state, max_tokens=4, max_seqs=1)
+    batch = emb.Batch(torch.tensor([0, 2], dtype=torch.int32, device=DEV), torch.tensor([3, 5], device=DEV), 1)
+    dy = torch.ones(2, 16, device=DEV)
+    layer.update(batch, dy)
+    old = state.detach()
+    state.data = torch.full((10,), 2.0, device=DEV)
+    layer.update(batch, dy)
+    assert old.tolist() == [0, 0, 0, 1, 0, 1, 0, 0, 0, 0] and state.tolist() == [2, 2, 2, 3, 2, 3, 2, 2, 2, 2]
+    state.data = torch.zeros(9, device=DEV)
+    with pytest.raises(ValueError, match="accumulators"):
+        layer.update(batch, dy)
