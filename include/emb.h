@@ -384,6 +384,12 @@ size_t emb_workspace_error_offset(void);
  * the rows of a sequence, and what the backward pass needs of the
  * activations can be kept in 8 bits.
  *
+ * A call whose kernel would have 2^32 work-items or more is refused with
+ * EMB_EUNSUPPORTED before anything is enqueued (the smallest such: 2^32 values
+ * of fp32 by single tokens, 2^35 saved or restored, outputs of 32 GB or more of
+ * a lookup, recurrences of 2^23 spans of 64 positions in slices of 64 columns,
+ * 2^29 sequences, the gradient of a whole table of 2^30 rows).
+ *
  * Matrices of activations are row-major with any row stride: */
 
 typedef enum { EMB_SAVED8 = 2 } emb_saved; /* emb_mat.dtype of a checkpoint in 8 bits */

@@ -92,7 +92,9 @@ emb_status check_update(const emb_update* u) {
   return EMB_OK;
 }
 
-emb_status hip_status(hipError_t e) { return e == hipSuccess ? EMB_OK : EMB_EHIP; }
+emb_status hip_status(hipError_t e) {
+  return e == hipSuccess ? EMB_OK : (e == hipErrorNotSupported ? EMB_EUNSUPPORTED : EMB_EHIP);
+}
 
 // host checks of a routing call; fills the launch descriptor (ws left null)
 emb_status route_prepare(const emb_tables* tables, const emb_batch* batch, int32_t world_size,
@@ -774,7 +776,6 @@ size_t emb_weight_grad_workspace_size(int64_t rows, int32_t dim, int32_t cols) {
 emb_status emb_weight_grad(int64_t rows, int32_t dim, int32_t cols, const emb_mat* x, const emb_mat* dy, float* dw,
                            int32_t add, void* ws, size_t ws_bytes, void* stream) {
   if (rows < 0 || dim < 1 || cols < 1 || dw == nullptr) return EMB_EINVAL;
-  // (block numbers of the tiles and parts are 32 bits)
   if (rows > kMaxTokens || (int64_t)dim * cols >= (int64_t)1 << 40) return EMB_EUNSUPPORTED;
   WeightGradLaunch p{};
   if (rows > 0) {

@@ -95,6 +95,7 @@ __global__ __launch_bounds__(256) void k_restore(SaveLaunch a) {
 
 hipError_t launch_save(const SaveLaunch& p, hipStream_t s) {
   const int64_t lanes = (int64_t)((p.D + EMB_SAVED_GROUP - 1) / EMB_SAVED_GROUP) * kLanes * p.N;
+  if (!launchable((lanes + 255) / 256, 256)) return hipErrorNotSupported;
   const unsigned blocks = (unsigned)((lanes + 255) / 256);
   if (p.dtype == EMB_BF16) k_save<bf16><<<blocks, 256, 0, s>>>(p);
   else k_save<float><<<blocks, 256, 0, s>>>(p);
@@ -103,6 +104,7 @@ hipError_t launch_save(const SaveLaunch& p, hipStream_t s) {
 
 hipError_t launch_restore(const SaveLaunch& p, hipStream_t s) {
   const int64_t lanes = (int64_t)((p.D + kCols - 1) / kCols) * p.N;
+  if (!launchable((lanes + 255) / 256, 256)) return hipErrorNotSupported;
   const unsigned blocks = (unsigned)((lanes + 255) / 256);
   if (p.dtype == EMB_BF16) k_restore<bf16><<<blocks, 256, 0, s>>>(p);
   else k_restore<float><<<blocks, 256, 0, s>>>(p);

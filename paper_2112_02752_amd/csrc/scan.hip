@@ -876,6 +876,7 @@ void clear(const Scan& a, hipStream_t s) {
 template <typename T, int V, int P, bool STREAM>
 hipError_t fwd(const ScanLaunch& p, const Scan& a, hipStream_t s) {
   const unsigned blocks = (unsigned)(a.spans * a.slices) + empties(a, a.h_last);
+  if (!launchable(blocks, kThreads)) return hipErrorNotSupported;
   clear(a, s);
   if (p.gated) k_scan_fwd<T, V, P, true, STREAM><<<blocks, kThreads, 0, s>>>(a);
   else k_scan_fwd<T, V, P, false, STREAM><<<blocks, kThreads, 0, s>>>(a);
@@ -897,6 +898,7 @@ hipError_t bwd(const ScanLaunch& p, hipStream_t s) {
   Scan a = arguments(p, V, kSpan);
   if (a.spans == 1) a.dbias = p.dbias;  // (its one row is the sum)
   const unsigned blocks = (unsigned)(a.spans * a.slices) + empties(a, a.dh0);
+  if (!launchable(blocks, kThreads)) return hipErrorNotSupported;
   clear(a, s);
   if (p.gated) k_scan_bwd<T, TG, V, true, STREAM><<<blocks, kThreads, 0, s>>>(a);
   else k_scan_bwd<T, TG, V, false, STREAM><<<blocks, kThreads, 0, s>>>(a);
@@ -914,6 +916,7 @@ hipError_t bwd(const ScanLaunch& p, hipStream_t s) {
 template <typename T, int V>
 hipError_t step(const StepLaunch& p, hipStream_t s) {
   const int64_t per = (p.D + V - 1) / V, blocks = (p.N * per + 255) / 256;
+  if (!launchable(blocks, 256)) return hipErrorNotSupported;
   if (p.gated) k_scan_step<T, V, true><<<(unsigned)blocks, 256, 0, s>>>(p);
   else k_scan_step<T, V, false><<<(unsigned)blocks, 256, 0, s>>>(p);
   return hipGetLastError();

@@ -8,6 +8,11 @@
 namespace emb {
 
 // ------------------------------------------------------------ launches
+// (each enqueues nothing and returns hipErrorNotSupported where a kernel's grid
+// would be too large)
+
+// HIP takes fewer than 2^32 work-items in a dimension of a grid
+inline bool launchable(int64_t blocks, int threads) { return blocks < ((int64_t)1 << 32) / threads; }
 
 struct TokenFwdLaunch {
   const void* W;

@@ -716,7 +716,9 @@ hipError_t grad_kernels(TokGrad a, hipStream_t s) {
   a.blocks = each ? (kRow ? a.N : (a.N * a.parts + 3) / 4)
                   : (kRow ? a.nchunks << a.split : ((a.nchunks * a.parts << a.split) + 3) / 4);
   a.zero_blocks = stores(KIND) && a.layout == EMB_TABLE ? zero_blocks(a) : 0;
-  const unsigned grid = (unsigned)(a.blocks + a.zero_blocks);
+  const unsigned grid = (unsigned)a.blocks + (unsigned)a.zero_blocks;
+  const int combine = a.D <= 256 ? kCombineLanes / 4 : kCombineLanes;
+  if (!launchable(grid, (int)block.x) || !launchable(a.nchunks, combine)) return hipErrorNotSupported;
   const uintptr_t at = reinterpret_cast<uintptr_t>(a.dy) | (uintptr_t)a.ld;
   const int vec = el * (int)(sizeof(TG));
   a.aligned = at % (uintptr_t)(vec < 16 ? vec : 16) == 0;
@@ -731,7 +733,7 @@ hipError_t grad_kernels(TokGrad a, hipStream_t s) {
   else k_token_reduce<TG, TW, 8, kB8, KIND><<<grid, block, 0, s>>>(a);
   // (a long segment has more than one chunk)
   if (a.nchunks > 1)
-    k_token_combine<TW, KIND == kStream ? kStore : KIND><<<a.nchunks, a.D <= 256 ? kCombineLanes / 4 : kCombineLanes, 0, s>>>(a);
+    k_token_combine<TW, KIND == kStream ? kStore : KIND><<<a.nchunks, combine, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -743,7 +745,7 @@ hipError_t update_kernels(const TokGrad& a, int opt, hipStream_t s) {
 }
 
 template <typename TW, typename TO, int V, bool MANY>
-void fwd_kernel(TokFwd a, const Stacked<MANY>& st, hipStream_t s) {
+hipError_t fwd_kernel(TokFwd a, const Stacked<MANY>& st, hipStream_t s) {
   a.aligned = (reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)a.out_bytes) % (Vec<TO, V>::kBytes < 16 ? Vec<TO, V>::kBytes : 16) == 0;
   int lg = 0;
   while (lg < 8 && (1 << lg) < a.vectors) ++lg;
@@ -753,12 +755,15 @@ void fwd_kernel(TokFwd a, const Stacked<MANY>& st, hipStream_t s) {
   // outputs that are streamed fill the device with two rows a lane in flight (as fast as one or four there, eight are
   // 7% slower); smaller ones spread over as many lanes as they can
   if (a.N * a.vectors * Vec<TO, V>::kBytes > kStreamBytes) {
-    const dim3 grid((unsigned)((a.N + per * 2 - 1) / (per * 2)), parts);
+    const int64_t blocks = (a.N + per * 2 - 1) / (per * 2);
+    if (!launchable(blocks, kFwdThreads)) return hipErrorNotSupported;
+    const dim3 grid((unsigned)blocks, parts);
     k_token_fwd<TW, TO, V, 2, true, MANY><<<grid, kFwdThreads, 0, s>>>(a, st);
   } else {
     const dim3 grid((unsigned)((a.N + per - 1) / per), parts);
     k_token_fwd<TW, TO, V, 1, false, MANY><<<grid, kFwdThreads, 0, s>>>(a, st);
   }
+  return hipGetLastError();
 }
 
 template <bool MANY>
@@ -766,13 +771,11 @@ hipError_t fwd_types(TokFwd a, const Stacked<MANY>& st, int dtype, int out, int 
   // 16 bytes of the table's row a lane
   a.vectors = D / (dtype == EMB_BF16 ? 8 : 4);
   if (dtype == EMB_BF16) {
-    if (out == EMB_BF16) fwd_kernel<bf16, bf16, 8, MANY>(a, st, s);
-    else fwd_kernel<bf16, float, 8, MANY>(a, st, s);
-  } else {
-    if (out == EMB_BF16) fwd_kernel<float, bf16, 4, MANY>(a, st, s);
-    else fwd_kernel<float, float, 4, MANY>(a, st, s);
+    if (out == EMB_BF16) return fwd_kernel<bf16, bf16, 8, MANY>(a, st, s);
+    return fwd_kernel<bf16, float, 8, MANY>(a, st, s);
   }
-  return hipGetLastError();
+  if (out == EMB_BF16) return fwd_kernel<float, bf16, 4, MANY>(a, st, s);
+  return fwd_kernel<float, float, 4, MANY>(a, st, s);
 }
 
 }  // namespace
@@ -826,9 +829,9 @@ hipError_t launch_token_grad(const TokenGradLaunch& p, hipStream_t s) {
   a.up.seed = p.seed;
   if (!p.fuse) {
     if (p.N == 0) {
-      if (p.layout == EMB_TABLE && p.rows > 0)
-        {
+      if (p.layout == EMB_TABLE && p.rows > 0) {
         const unsigned blocks = (unsigned)zero_blocks(a);
+        if (!launchable(blocks, 256)) return hipErrorNotSupported;
         k_token_zero<<<blocks, 256, 0, s>>>(a);
       }
       return hipGetLastError();

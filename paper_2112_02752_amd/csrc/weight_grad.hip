@@ -375,10 +375,13 @@ hipError_t launch_weight_grad(const WeightGradLaunch& p, hipStream_t s) {
   const int tile = pl.groups * kGroup;
   a.parts = pl.parts;
   a.steps_per_part = pl.steps;
-  a.tiles_k = (p.K + tile - 1) / tile;
-  a.tiles_f = (p.F + tile - 1) / tile;
+  const int64_t tiles_k = ((int64_t)p.K + tile - 1) / tile, tiles_f = ((int64_t)p.F + tile - 1) / tile;
+  const int64_t all = tiles_k * tiles_f * pl.parts;
+  if (!launchable(all, Shape<1>::kThreads)) return hipErrorNotSupported;
+  a.tiles_k = (int32_t)tiles_k;
+  a.tiles_f = (int32_t)tiles_f;
   a.out = a.parts > 1 ? p.ws : p.dw;
-  const unsigned blocks = (unsigned)(a.tiles_k * a.tiles_f * a.parts);
+  const unsigned blocks = (unsigned)all;
   if (p.dtype == EMB_FP32) k_weight_grad<1, 3, true><<<blocks, Shape<1>::kThreads, 0, s>>>(a);
   else if (!p.aligned) k_weight_grad<1, 1, false><<<blocks, Shape<1>::kThreads, 0, s>>>(a);
   else if (pl.groups == 2) k_weight_grad<2, 1, true><<<blocks, Shape<2>::kThreads, 0, s>>>(a);
