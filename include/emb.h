@@ -468,8 +468,10 @@ typedef struct {
  * tokens of dim columns (0 for invalid sizes); it needs no initialisation and
  * carries nothing between calls.  Calls that may run at once need workspaces
  * of their own.  Inside a call workgroups wait for others that started before
- * them; should such a wait last two seconds, the rest of that column's values
- * are NaN. */
+ * them; should such a wait last two seconds, the rest of those columns' values
+ * are NaN, and the workspace's first 256 bytes record it: zeroed once
+ * beforehand (emb_workspace_init), emb_workspace_status reads them as
+ * status[0] 8, status[1] 0x400, status[2] and [3] as above, of all calls since. */
 size_t emb_scan_workspace_size(int64_t num_tokens, int32_t dim);
 
 /* y: N rows of dim columns, of x's type.  h_last: device fp32 [M][D], the

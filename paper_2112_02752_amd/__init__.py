@@ -45,14 +45,16 @@ class StepFailed(RuntimeError):
     """A dedup (and the reduce after it) failed on the device: one of its
     bounded waits for a word another workgroup publishes ran out, or a sort
     pass found inconsistent digit totals.  No table or state row was written
-    by that step."""
+    by that step.  Or a wait of a recurrence ran out: its values are NaN from
+    there on."""
 
     SITES = {0x100: "sort pass {p}: tile waiting for its digit offsets",
              0x102: "sort pass {p}: prefix block waiting for its group's counts",
              0x103: "sort pass {p}: prefix block waiting for the group sums",
              0x104: "sort pass {p}: prefix block waiting for the later passes' counts",
              0x105: "sort pass {p}: range block waiting for its tiles' counts",
-             0x200: "unique scan look-back", 0x300: "gradient combine"}
+             0x200: "unique scan look-back", 0x300: "gradient combine",
+             0x400: "recurrence: span waiting for those before it"}
 
     def __init__(self, bits: int, site: int, block: int, timeouts: int):
         self.bits, self.site, self.block, self.timeouts = bits, site, block, timeouts
@@ -63,6 +65,8 @@ class StepFailed(RuntimeError):
             what.append("a sort pass found digit totals inconsistent with its keys (workspace not initialised?)")
         if bits & 4:
             what.append("a gradient-combine wait ran out")
+        if bits & 8:
+            what.append("a recurrence wait ran out (NaN from there on)")
         desc = self.SITES.get(site & ~0xf0, "none").format(p=(site >> 4) & 0xf) if site else "none"
         super().__init__(f"embedding step failed on the device: {'; '.join(what)} (error bits {bits}); first wait "
                          f"that ran out since the workspace was initialised: {desc}, workgroup {block}; "

@@ -135,6 +135,7 @@ struct Scan {
   const float *bias, *h0, *dh_last;
   float *states, *h_last, *dh0, *dbias;  // dbias: [spans][D], one row a span
   int32_t N, M, D, spans, slices;
+  WsHeader* hdr;  // of the workspace: the record of waits that ran out
   // what spans publish, by (span in the order they are taken, slice)
   uint32_t* taken;  // [slices]
   uint32_t* flags;  // [slices][spans]
@@ -217,12 +218,14 @@ __device__ __forceinline__ uint32_t ld_u32(const uint32_t* p) {
 template <int V>
 struct Chain {
   static constexpr int kCols = V * kWave;
+  WsHeader* hdr;
   uint32_t* flags;  // of the slice
   uint64_t* steps;
   uint32_t* out;
   int64_t apart;    // words from one span's to the next's
   int idx;          // this block's place among the slice's spans
   __device__ __forceinline__ Chain(const Scan& a, int slice, int span) {
+    hdr = a.hdr;
     flags = a.flags + (int64_t)slice * a.spans;
     apart = (int64_t)a.slices * kCols;
     steps = a.steps + (int64_t)slice * kCols;
@@ -267,8 +270,16 @@ __device__ __forceinline__ void look_back(const Chain<V>& ch, Look<V>& lk, float
       const uint32_t known = (uint32_t)__ballot(flag == kOut), some = (uint32_t)__ballot(flag != kNothing);
       j = known ? __builtin_ctz(known) : kLook;
       if (known && (~some & ((1u << j) - 1u)) == 0u) break;
-      // (not reached: the blocks waited for are running; two seconds are no healthy wait)
+      // (not reached: the blocks waited for are running.  Two seconds, not the dedup's 20 ms: what a block would go on
+      // with is wrong values, not a call that it can still undo, and a device shared with others may stop it for longer)
       if (wait_clock() - t0 > 200000000ull) {
+        if (lane == 0) {
+          // (the header's generation is 0: no dedup has used it)
+          __hip_atomic_fetch_or(&ch.hdr->err, (uint64_t)kScanError, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          atomic_add_u32(&ch.hdr->timeouts, 1u);
+          ch.hdr->timeout_site = kSiteScan;
+          ch.hdr->timeout_block = blockIdx.x;
+        }
         j = -1;
         break;
       }
@@ -826,7 +837,7 @@ __global__ __launch_bounds__(256) void k_scan_step(StepLaunch a) {
 
 // ---------------------------------------------------------------- launches
 
-// The workspace: counters and flags, steps, outgoing states, rows of the bias
+// The workspace: header, counters and flags, steps, outgoing states, rows of the bias
 // gradient; for spans of 64 (the backward's; the forward's are fewer).
 struct Room {
   int64_t spans, slices, cols;
@@ -837,7 +848,7 @@ Room room(int64_t N, int32_t D) {
   r.spans = (N + kSpan - 1) / kSpan;
   r.slices = ((int64_t)D + kWave - 1) / kWave;
   r.cols = ((int64_t)D + 2 * kWave - 1) / (2 * kWave) * (2 * kWave);
-  size_t at = 0;
+  size_t at = sizeof(WsHeader);
   r.flags = at;
   at = align256(at + sizeof(uint32_t) * (size_t)(r.slices * (r.spans + 1)));
   r.steps = at;
@@ -860,6 +871,7 @@ Scan arguments(const ScanLaunch& p, int V, int span) {
   a.spans = (int32_t)((p.N + span - 1) / span);
   a.slices = (p.D + kWave * V - 1) / (kWave * V);
   const Room r = room(p.N, p.D);
+  a.hdr = reinterpret_cast<WsHeader*>(p.ws);
   a.taken = reinterpret_cast<uint32_t*>(p.ws + r.flags);
   a.flags = a.taken + a.slices;
   a.steps = reinterpret_cast<uint64_t*>(p.ws + r.steps);

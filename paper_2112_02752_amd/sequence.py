@@ -12,7 +12,7 @@ import ctypes
 from typing import Optional
 
 from . import (BF16, FP32, Batch, CUpdate, DedupBuffers, StepFailed, Tables, _check, _ptr, _stream, _update, lib,
-               workspace_status)
+               read_status, workspace_init)
 
 SAVED8 = 2
 SPAN = 64           # EMB_SCAN_SPAN: positions between kept states
@@ -183,6 +183,12 @@ def token_grad(tables: Tables, batch: Batch, grad_out, dedup: DedupBuffers, grad
         d.ws.numel(), _stream(stream)))
 
 
+def _check_status(ws, stream) -> None:
+    st = read_status(ws, stream)
+    if st[0]:
+        raise StepFailed(*st)
+
+
 class TokenLayer:
     """Lookup of single tokens from the tables, scaled, with its backward:
     the table's gradient or the optimizer step on the rows that were looked up.
@@ -266,12 +272,7 @@ class TokenLayer:
     def check(self, stream=None) -> None:
         """Raise StepFailed if the last backward failed on the device (it then
         wrote no table row)."""
-        import torch
-        st = torch.zeros(4, dtype=torch.int32, device=self.dedup.ws.device)
-        workspace_status(self.dedup.ws, st, stream)
-        st = tuple(int(x) for x in st.cpu())
-        if st[0]:
-            raise StepFailed(*st)
+        _check_status(self.dedup.ws, stream)
 
 
 # ---------------------------------------------------------------- recurrence
@@ -337,6 +338,7 @@ class Recurrence:
         self.max_tokens, self.max_seqs, self.dim = n, max_seqs, dim
         self.ws = torch.empty(size, dtype=torch.uint8, device=device)
         self._ws, self._wsb = self.ws.data_ptr(), size
+        workspace_init(self.ws[:256])
         self.states = torch.empty(((n + SPAN - 1) // SPAN, dim), device=device) if train else None
         self._states = _ptr(self.states)
         self._tokens = None
@@ -372,6 +374,12 @@ class Recurrence:
             ref, self._states, mats[0].ref, _floats(dh_last, each, "dh_last"), mats[1].ref, mats[2].ref,
             mats[3].ref if scan.o is not None else None, _floats(dbias, (self.dim,), "dbias"),
             _floats(dh0, each, "dh0"), self._ws, self._wsb, _stream(stream)))
+
+
+    def check(self, stream=None) -> None:
+        """Raise StepFailed if a wait inside a call since this object was made
+        ran out (values are NaN from there on)."""
+        _check_status(self.ws, stream)
 
 
 def scan_step(x, f, o, state, y, bias=None, slots=None, stream=None) -> None:
@@ -559,6 +567,13 @@ class SequenceLayer:
         saved_rows.weight_grad(dproj, dweight, add=add)
         torch.mm(dproj, self.weight.t(), out=drows)
         self.tokens.update(batch, drows)
+
+    def check(self) -> None:
+        """Raise StepFailed if the last backward's dedup or a recurrence failed on
+        the device."""
+        if self.tokens.dedup is not None:
+            self.tokens.check()
+        self.recurrence.check()
 
     def step(self, batch: Batch, state, y, slots=None) -> None:
         """The next token of each running sequence (one a sequence in

@@ -349,3 +349,50 @@ def test_accumulators_that_move_are_followed():
     state.data = torch.zeros(9, device=DEV)
     with pytest.raises(ValueError, match="accumulators"):
         layer.update(batch, dy)
+
+
+# ---------------------------------------------------------------- failures
+
+def test_a_recurrences_record_of_waits():
+    """Sound calls leave no record, whatever the workspace held; one that is there
+    (put there from the host) is reported until the workspace is initialised."""
+    import torch
+    import paper_2112_02752_amd as emb
+    n, D = 700, 70
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x, f, o, dy = (torch.randn((n, D), generator=g, device=DEV) for _ in range(4))
+    scan = emb.Scan(torch.tensor([0, n], dtype=torch.int32, device=DEV), x, f, o)
+    rec = emb.Recurrence(n, 1, D)
+    outs = [torch.empty_like(x) for _ in range(4)]
+
+    def both():
+        rec.forward(scan, outs[0])
+        rec.backward(scan, dy, *outs[1:])
+        return [v.clone() for v in outs]
+
+    want = both()
+    rec.check()
+    at = emb.workspace_error_offset()
+    words = rec.ws[:256].view(torch.int32)
+    words[at // 4] = 8
+    with pytest.raises(emb.StepFailed, match="recurrence"):
+        rec.check()
+    assert all(torch.equal(a, b) for a, b in zip(both(), want))
+    with pytest.raises(emb.StepFailed, match="recurrence"):
+        rec.check()
+    emb.workspace_init(rec.ws)
+    rec.check()
+    rec.ws.fill_(255)      # no call needs it initialised
+    assert all(torch.equal(a, b) for a, b in zip(both(), want))
+
+
+def test_the_sequence_layers_check():
+    import torch
+    import paper_2112_02752_amd as emb
+    layer, batch, y, dy = _layer("sgd", None)
+    layer.forward(batch, y)
+    layer.backward(batch, dy, torch.empty((40, 96), device=DEV), torch.empty(32, device=DEV))
+    layer.check()
+    layer.recurrence.ws[:256].view(torch.int32)[emb.workspace_error_offset() // 4] = 8
+    with pytest.raises(emb.StepFailed):
+        layer.check()
