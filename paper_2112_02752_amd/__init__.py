@@ -367,7 +367,11 @@ def read_status(ws, stream=None):
     """The workspace's last-call status as host ints (synchronises)."""
     import torch
     st = torch.zeros(4, dtype=torch.int32, device=ws.device)
+    if stream is not None:
+        torch.cuda.synchronize(ws.device)   # (the zeros are the current stream's)
     workspace_status(ws, st, stream)
+    if stream is not None:
+        torch.cuda.synchronize(ws.device)   # (and the copy below waits for the current stream alone)
     return tuple(int(x) for x in st.cpu())
 
 
@@ -447,7 +451,10 @@ class Layer:
         """Status of the last step (emb_workspace_status): (error bits,
         first timed-out wait's site, its workgroup, waits that ran out since
         the workspace was initialised); synchronises."""
+        import torch
         workspace_status(self.ws, self._status, stream)
+        if stream is not None:
+            torch.cuda.synchronize(self.ws.device)   # (the copy waits for the current stream alone)
         return tuple(int(x) for x in self._status.cpu())
 
     def check(self, stream=None) -> None:

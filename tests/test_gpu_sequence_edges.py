@@ -396,3 +396,25 @@ def test_the_sequence_layers_check():
     layer.recurrence.ws[:256].view(torch.int32)[emb.workspace_error_offset() // 4] = 8
     with pytest.raises(emb.StepFailed):
         layer.check()
+
+
+def test_a_record_is_read_behind_another_streams_work():
+    """The status asked for on a busy side stream is that stream's, not what the
+    current stream finds meanwhile."""
+    import torch
+    import paper_2112_02752_amd as emb
+    tables = emb.Tables(torch.ones(10, 16, device=DEV), [0, 10])
+    tokens = emb.TokenLayer(tables, opt="sgd", lr=0.1, max_tokens=4, max_seqs=1)
+    pooled = emb.Layer(tables, "sum", "sgd", 0.1, max_indices=4, max_bags=1)
+    rec = emb.Recurrence(10, 1, 16)
+    busy = torch.randn((8192, 8192), device=DEV).bfloat16()
+    for obj, ws in ((tokens, tokens.dedup.ws), (pooled, pooled.ws), (rec, rec.ws)):
+        obj.check()
+        ws[:256].view(torch.int32)[emb.workspace_error_offset() // 4] = 8
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for _ in range(10):
+                busy @ busy
+        with pytest.raises(emb.StepFailed):
+            obj.check(stream=side)
