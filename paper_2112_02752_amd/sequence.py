@@ -488,9 +488,11 @@ class SequenceLayer:
     A training step is ``forward``, the caller's loss, ``backward``.  Between
     the two only checkpoints are kept, in 8 bits: of the rows (for the
     projection's weight gradient) and of the projection (for the recurrence's
-    backward), 1.03 bytes a value instead of 2; the full-width buffers serve
-    every call.  ``step`` is one token of each running sequence (serving), with
-    states in a pool of slots.
+    backward), 1.03 bytes a value instead of 2.  The layer holds room for those
+    of ``max_tokens`` tokens from its first training forward on; rows and
+    projection in full width are the caching allocator's for the length of a
+    call, so a model's layers share them.  ``step`` is one token of each running
+    sequence (serving), with states in a pool of slots.
 
     ``weight`` is a bf16 D x 3H tensor and ``bias`` an fp32 one of H values, both
     the caller's: ``backward`` leaves their gradients in fp32 and trains the
@@ -509,15 +511,19 @@ class SequenceLayer:
         self.tokens = TokenLayer(tables, scale=scale, pad_row=pad_row, opt=opt, lr=lr, eps=eps, state=state,
                                  max_tokens=max_tokens, max_seqs=max_seqs, rounding=rounding, seed=seed)
         self.recurrence = Recurrence(max_tokens, max_seqs, self.hidden, dev)
-        b16 = dict(dtype=torch.bfloat16, device=dev)
-        self._rows = torch.empty((max_tokens, dim), **b16)
-        self._proj = torch.empty((max_tokens, cols), **b16)
-        self._saved = None
+        self._max, self._dev = max_tokens, dev
+        self._room = self._saved = None
         self._n, self._offsets = -1, 0
+
+    def _full(self, n: int):
+        """Rows and projection of n tokens in full width, for one call."""
+        import torch
+        b16 = dict(dtype=torch.bfloat16, device=self._dev)
+        return torch.empty((n, self.dim), **b16), torch.empty((n, 3 * self.hidden), **b16)
 
     def _project(self, batch: Batch, n: int):
         import torch
-        rows, proj = self._rows[:n], self._proj[:n]
+        rows, proj = self._full(n)
         self.tokens.forward(batch, rows)
         torch.mm(rows, self.weight, out=proj)
         return rows, proj, [Mat(proj[:, i * self.hidden:(i + 1) * self.hidden]) for i in range(3)]
@@ -533,8 +539,10 @@ class SequenceLayer:
         self.recurrence.forward(Scan(batch.offsets, *parts, bias=self.bias, h0=h0), y, h_last)
         self._n = -1
         if train:
+            if self._room is None:
+                self._room = tuple(Checkpoint(self._max, d, self._dev) for d in (self.dim, 3 * self.hidden))
             if self._saved is None or self._saved[0].rows != n:
-                self._saved = (Checkpoint(n, self.dim, rows.device), Checkpoint(n, 3 * self.hidden, rows.device))
+                self._saved = tuple(Checkpoint.of(c.codes[:n], c.exps[:n], c.dim) for c in self._room)
             self._saved[0].pack(rows)
             self._saved[1].pack(proj)
             self._n, self._offsets, self._h0 = n, int(batch.offsets.numel()), h0
@@ -561,7 +569,7 @@ class SequenceLayer:
         self._n = -1
         saved_rows, saved_proj = self._saved
         scan = Scan(batch.offsets, *(saved_proj.columns(i * H, H) for i in range(3)), bias=self.bias, h0=self._h0)
-        dproj, drows = self._proj[:n], self._rows[:n]
+        drows, dproj = self._full(n)
         self.recurrence.backward(scan, dy, *(Mat(dproj[:, i * H:(i + 1) * H]) for i in range(3)), dbias=dbias,
                                  dh_last=dh_last, dh0=dh0)
         saved_rows.weight_grad(dproj, dweight, add=add)

@@ -148,6 +148,52 @@ def test_a_refused_backward_runs_nothing_and_can_be_repeated():
     assert torch.equal(layer.tokens.tables.weights, plain.tokens.tables.weights)
 
 
+def test_a_layer_keeps_checkpoints_alone():
+    """What a layer holds, beside its workspaces, before a training forward
+    (nothing) and until its backward (codes and exponents of most tokens)."""
+    import torch
+    import paper_2112_02752_amd as emb
+    n, D, H = 4096, 64, 64
+    kw = dict(R=50, D=D, H=H)
+    warm = _layer("sgd", None, lens=(n,), **kw)
+    warm[0].forward(warm[1], warm[2])
+
+    def held(layer):
+        parts = [layer.recurrence.ws, layer.recurrence.states, layer.tokens.dedup.ws]
+        parts += [v for v in vars(layer.tokens.dedup).values() if v is not layer.tokens.dedup.ws]
+        parts += [layer.tokens.tables.weights, layer.weight, layer.bias]
+        return sum(-(-v.numel() * v.element_size() // 512) * 512 for v in parts)
+
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    layer, batch, y, dy = _layer("sgd", None, lens=(n,), **kw)
+    mine = sum(-(-v.numel() * v.element_size() // 512) * 512 for v in (batch.offsets, batch.indices, y, dy))
+    full = 2 * n * (D + 3 * H)
+    assert torch.cuda.memory_allocated() - before - mine - held(layer) < full // 16
+    layer.forward(batch, y, train=False)
+    assert torch.cuda.memory_allocated() - before - mine - held(layer) < full // 16
+    layer.forward(batch, y)
+    kept = n * (D + 3 * H) * 33 // 32
+    assert kept <= torch.cuda.memory_allocated() - before - mine - held(layer) < kept + full // 16
+
+
+def test_steps_of_changing_lengths_are_those_of_a_fresh_layer():
+    import torch
+    lens = [(60, 3), (5,), (40, 0, 1), (90,), (1,)]
+    long = _layer("sgd", None, lens=(120,))[0]
+    for some in lens:
+        fresh, batch, y, dy = _layer("sgd", None, lens=some)
+        long.tokens.tables.weights.copy_(fresh.tokens.tables.weights)
+        long.weight.copy_(fresh.weight)
+        out = []
+        for layer in (fresh, long):
+            dw, db = torch.empty((40, 96), device=DEV), torch.empty(32, device=DEV)
+            layer.forward(batch, y)
+            layer.backward(batch, dy, dw, db)
+            out.append((y.clone(), dw, db, layer.tokens.tables.weights.clone()))
+        assert all(torch.equal(a, b) for a, b in zip(*out)), some
+
+
 # ---------------------------------------------------------------- tokens
 
 @pytest.mark.parametrize("bits", [32, 64])
