@@ -64,13 +64,14 @@ def _device(t, what: str):
 class Mat:
     """A matrix of activations as the C ABI takes it: a 2-d fp32 or bf16
     tensor whose columns are contiguous, rows at any stride (a slice of a wider
-    tensor's columns); an 8-bit one comes from ``Checkpoint.columns``.  Kept by
-    a program between calls, it costs a call one address check."""
+    tensor's columns, or ``cols`` of them from column ``first`` on); an 8-bit one
+    comes from ``Checkpoint.columns``.  Kept by a program between calls, it
+    costs a call one address check."""
 
-    __slots__ = ("tensor", "exps", "rows", "cols", "_c", "_at", "_at_exps", "_fixed", "_taken", "ref")
+    __slots__ = ("tensor", "exps", "rows", "cols", "_c", "_at", "_at_exps", "_fixed", "_first", "_taken", "ref")
 
-    def __init__(self, tensor, exps=None, cols: Optional[int] = None):
-        self.tensor, self.exps, self._fixed = tensor, exps, cols
+    def __init__(self, tensor, exps=None, cols: Optional[int] = None, first: int = 0):
+        self.tensor, self.exps, self._fixed, self._first = tensor, exps, cols, first
         self._c = CMat()
         self.ref = ctypes.byref(self._c)
         self._taken = 0     # how often the descriptor was made
@@ -94,10 +95,16 @@ class Mat:
             dtype, le = BF16 if tensor.dtype == torch.bfloat16 else FP32, 0
         if ld < wide:
             raise ValueError("rows overlap")
-        self.rows, self.cols = rows, wide if self._fixed is None else self._fixed
-        self._at, self._at_exps = tensor.data_ptr(), exps.data_ptr() if exps is not None else None
+        first, cols = self._first, self._fixed
+        if first < 0 or (cols is not None and (cols < 0 or first + cols > wide)) or first > wide:
+            raise ValueError(f"columns {first} on of {wide}")
+        self.rows, self.cols = rows, wide - first if cols is None else cols
+        at = self._at = tensor.data_ptr()
+        self._at_exps = exps.data_ptr() if exps is not None else None
         c = self._c
-        c.data, c.ld, c.dtype, c.exps, c.ld_exps = self._at or None, ld, dtype, self._at_exps or None, le
+        c.ld, c.dtype, c.ld_exps = ld, dtype, le
+        c.data = at + first * (1 if exps is not None else 4 if dtype == FP32 else 2) if at else None
+        c.exps = self._at_exps + first // GROUP if self._at_exps else None
         self._taken += 1
 
     @property
@@ -450,7 +457,7 @@ class Checkpoint:
         """Columns first .. first + count - 1 as a matrix (for ``Scan``)."""
         if first % GROUP != 0 or first < 0 or count < 1 or first + count > self.dim:
             raise ValueError("columns of a checkpoint start at a group's first")
-        return Mat(self.codes[:, first:], self.exps[:, first // GROUP:], count)
+        return Mat(self.codes, self.exps, count, first)
 
     def pack(self, src, stream=None) -> None:
         src = _mat(src)
@@ -526,7 +533,7 @@ class SequenceLayer:
         rows, proj = self._full(n)
         self.tokens.forward(batch, rows)
         torch.mm(rows, self.weight, out=proj)
-        return rows, proj, [Mat(proj[:, i * self.hidden:(i + 1) * self.hidden]) for i in range(3)]
+        return rows, proj, [Mat(proj, cols=self.hidden, first=i * self.hidden) for i in range(3)]
 
     def forward(self, batch: Batch, y, h_last=None, h0=None, train: bool = True) -> None:
         """y (N x H, bf16) and the state after each sequence (fp32 M x H) of
@@ -570,7 +577,7 @@ class SequenceLayer:
         saved_rows, saved_proj = self._saved
         scan = Scan(batch.offsets, *(saved_proj.columns(i * H, H) for i in range(3)), bias=self.bias, h0=self._h0)
         drows, dproj = self._full(n)
-        self.recurrence.backward(scan, dy, *(Mat(dproj[:, i * H:(i + 1) * H]) for i in range(3)), dbias=dbias,
+        self.recurrence.backward(scan, dy, *(Mat(dproj, cols=H, first=i * H) for i in range(3)), dbias=dbias,
                                  dh_last=dh_last, dh0=dh0)
         saved_rows.weight_grad(dproj, dweight, add=add)
         torch.mm(dproj, self.weight.t(), out=drows)

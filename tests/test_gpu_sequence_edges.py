@@ -464,3 +464,28 @@ def test_a_record_is_read_behind_another_streams_work():
                 busy @ busy
         with pytest.raises(emb.StepFailed):
             obj.check(stream=side)
+
+
+def test_columns_of_a_matrix():
+    """Columns named by their first and number are those of a slice."""
+    import torch
+    import paper_2112_02752_amd as emb
+    wide = torch.randn(40, 200, device=DEV).bfloat16()
+    for t in (wide, wide.float(), wide[:1], wide[:0]):
+        for first, cols in ((0, 200), (32, 64), (64, 1), (199, 1), (200, 0)):
+            a, b = emb.Mat(t, cols=cols, first=first), emb.Mat(t[:, first:first + cols]) if cols else None
+            if b is not None and t.shape[0]:
+                assert (a.rows, a.cols, a.c().data, a.c().dtype) == (b.rows, b.cols, b.c().data, b.c().dtype)
+                assert t.shape[0] == 1 or a.c().ld == b.c().ld
+        for first, cols in ((-1, 3), (0, 201), (190, 11), (201, None)):
+            with pytest.raises(ValueError, match="columns"):
+                emb.Mat(t, cols=cols, first=first)
+    ck = emb.Checkpoint(40, 200)
+    ck.pack(wide)
+    back = torch.empty(40, 200, device=DEV)
+    ck.unpack(back)
+    for first, cols in ((0, 200), (32, 64), (160, 40), (192, 8)):
+        part, m = torch.empty(40, cols, device=DEV), ck.columns(first, cols)
+        assert emb.lib().emb_restore(40, cols, m.ref, emb.Mat(part).ref, None) == 0
+        torch.cuda.synchronize()
+        assert torch.equal(part, back[:, first:first + cols])
