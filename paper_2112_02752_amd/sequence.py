@@ -556,8 +556,8 @@ class SequenceLayer:
 
     def backward(self, batch: Batch, dy, dweight, dbias, dh_last=None, dh0=None, add: bool = False) -> None:
         """Backward of the last ``forward``, whose batch this is: the gradients of
-        the weights (fp32 D x 3H, with ``add`` added to what is there) and the
-        bias (fp32), and the optimizer's step on the table rows."""
+        the weights (fp32 D x 3H) and the bias (fp32 H, or None), with ``add``
+        added to what is there, and the optimizer's step on the table rows."""
         import torch
         n, H = int(batch.indices.numel()), self.hidden
         if n != self._n or int(batch.offsets.numel()) != self._offsets:
@@ -577,8 +577,11 @@ class SequenceLayer:
         saved_rows, saved_proj = self._saved
         scan = Scan(batch.offsets, *(saved_proj.columns(i * H, H) for i in range(3)), bias=self.bias, h0=self._h0)
         drows, dproj = self._full(n)
-        self.recurrence.backward(scan, dy, *(Mat(dproj, cols=H, first=i * H) for i in range(3)), dbias=dbias,
+        db = torch.empty_like(dbias) if add and dbias is not None else dbias
+        self.recurrence.backward(scan, dy, *(Mat(dproj, cols=H, first=i * H) for i in range(3)), dbias=db,
                                  dh_last=dh_last, dh0=dh0)
+        if db is not dbias:
+            dbias += db
         saved_rows.weight_grad(dproj, dweight, add=add)
         torch.mm(dproj, self.weight.t(), out=drows)
         self.tokens.update(batch, drows)

@@ -148,6 +148,30 @@ def test_a_refused_backward_runs_nothing_and_can_be_repeated():
     assert torch.equal(layer.tokens.tables.weights, plain.tokens.tables.weights)
 
 
+def test_gradients_of_two_batches_added():
+    """With ``add`` the weights' and the bias's gradients both hold the sums (one
+    more rounding of each: 2^-24, and the weights' sums meet what is there)."""
+    import torch
+    got = []
+    for add in (False, True):
+        sums = []
+        layer, batch, y, dy = _layer("sgd", None)
+        layer.tokens._updc.lr = 0.0
+        dw, db = torch.zeros((40, 96), device=DEV), torch.zeros(32, device=DEV)
+        for k in range(2):
+            layer.forward(batch, y)
+            layer.backward(batch, dy * (k + 1), dw, db, add=add)
+            sums.append((dw.double().cpu(), db.double().cpu()))
+        got.append(sums)
+    for i in range(2):
+        parts = [s[i] for s in got[0]]
+        want = parts[0] + parts[1]
+        mag = parts[0].abs() + parts[1].abs()
+        assert bool(((got[1][1][i] - want).abs() <= 4 * U * mag).all())
+    layer.forward(batch, y)
+    layer.backward(batch, dy, dw, None, add=True)
+
+
 def test_a_layer_keeps_checkpoints_alone():
     """What a layer holds, beside its workspaces, before a training forward
     (nothing) and until its backward (codes and exponents of most tokens)."""
