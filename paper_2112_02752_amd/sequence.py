@@ -279,6 +279,8 @@ class TokenLayer:
     def check(self, stream=None) -> None:
         """Raise StepFailed if the last backward failed on the device (it then
         wrote no table row)."""
+        if self.dedup is None:
+            raise ValueError("a layer without max_tokens only looks up")
         _check_status(self.dedup.ws, stream)
 
 

@@ -56,3 +56,8 @@ def test_no_accumulators_are_needed_without_adagrad():
     emb.TokenLayer(_tables(), opt="sgd")
     emb.TokenLayer(_tables())
     emb.TokenLayer(_tables(), opt="adagrad")      # looks up; an update asks for them
+
+
+def test_a_layer_that_only_looks_up_has_no_backward_to_check():
+    with pytest.raises(ValueError, match="only looks up"):
+        emb.TokenLayer(_tables()).check()
