@@ -540,11 +540,14 @@ class SequenceLayer:
     def forward(self, batch: Batch, y, h_last=None, h0=None, train: bool = True) -> None:
         """y (N x H, bf16) and the state after each sequence (fp32 M x H) of
         the batch's sequences, from first states ``h0`` or zero; with ``train``
-        what the backward needs is kept.  Runs on the current stream."""
+        what the backward needs is kept (``h0`` too: the caller may write to it
+        before the backward, or give it as ``h_last``).  Runs on the current
+        stream."""
         n = int(batch.indices.numel())
         if n > self.recurrence.max_tokens:
             raise ValueError("batch larger than the layer's buffers")
         rows, proj, parts = self._project(batch, n)
+        first = h0.clone() if train and h0 is not None else None
         self.recurrence.forward(Scan(batch.offsets, *parts, bias=self.bias, h0=h0), y, h_last)
         self._n = -1
         if train:
@@ -554,7 +557,7 @@ class SequenceLayer:
                 self._saved = tuple(Checkpoint.of(c.codes[:n], c.exps[:n], c.dim) for c in self._room)
             self._saved[0].pack(rows)
             self._saved[1].pack(proj)
-            self._n, self._offsets, self._h0 = n, int(batch.offsets.numel()), h0
+            self._n, self._offsets, self._h0 = n, int(batch.offsets.numel()), first
 
     def backward(self, batch: Batch, dy, dweight, dbias, dh_last=None, dh0=None, add: bool = False) -> None:
         """Backward of the last ``forward``, whose batch this is: the gradients of

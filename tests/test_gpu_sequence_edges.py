@@ -172,6 +172,25 @@ def test_gradients_of_two_batches_added():
     layer.backward(batch, dy, dw, None, add=True)
 
 
+def test_first_states_may_be_written_to_before_the_backward():
+    """States carried from batch to batch in one buffer: the last states written
+    over the first ones, or another batch's put there, change no gradient."""
+    import torch
+    got = []
+    for kind in ("apart", "same", "later"):
+        layer, batch, y, dy = _layer("sgd", None)
+        state = torch.randn((5, 32), generator=torch.Generator().manual_seed(3)).to(DEV)
+        last = state if kind == "same" else torch.empty_like(state)
+        layer.forward(batch, y, last, h0=state)
+        if kind == "later":
+            state.copy_(last)
+        dw, db, dh0 = (torch.empty(s, device=DEV) for s in ((40, 96), (32,), (5, 32)))
+        layer.backward(batch, dy, dw, db, dh0=dh0)
+        got.append((y, last, dw, db, dh0, layer.tokens.tables.weights))
+    for other in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], other))
+
+
 def test_a_layer_keeps_checkpoints_alone():
     """What a layer holds, beside its workspaces, before a training forward
     (nothing) and until its backward (codes and exponents of most tokens)."""
