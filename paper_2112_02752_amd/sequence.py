@@ -345,7 +345,7 @@ class Recurrence:
         if size == 0:
             raise ValueError("batch too large for one call")
         self.max_tokens, self.max_seqs, self.dim = n, max_seqs, dim
-        self.ws = torch.empty(size, dtype=torch.uint8, device=device)
+        self.ws = _device(torch.empty(size, dtype=torch.uint8, device=device), "a recurrence's workspace")
         self._ws, self._wsb = self.ws.data_ptr(), size
         workspace_init(self.ws[:256])
         self.states = torch.empty(((n + SPAN - 1) // SPAN, dim), device=device) if train else None

@@ -61,3 +61,8 @@ def test_no_accumulators_are_needed_without_adagrad():
 def test_a_layer_that_only_looks_up_has_no_backward_to_check():
     with pytest.raises(ValueError, match="only looks up"):
         emb.TokenLayer(_tables()).check()
+
+
+def test_a_recurrence_off_the_gpu():
+    with pytest.raises(ValueError, match="GPU"):
+        emb.Recurrence(100, 1, 16, device="cpu")
