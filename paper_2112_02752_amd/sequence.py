@@ -68,13 +68,12 @@ class Mat:
     comes from ``Checkpoint.columns``.  Kept by a program between calls, it
     costs a call one address check."""
 
-    __slots__ = ("tensor", "exps", "rows", "cols", "_c", "_at", "_at_exps", "_fixed", "_first", "_taken", "ref")
+    __slots__ = ("tensor", "exps", "rows", "cols", "_c", "_at", "_at_exps", "_fixed", "_first", "ref")
 
     def __init__(self, tensor, exps=None, cols: Optional[int] = None, first: int = 0):
         self.tensor, self.exps, self._fixed, self._first = tensor, exps, cols, first
         self._c = CMat()
         self.ref = ctypes.byref(self._c)
-        self._taken = 0     # how often the descriptor was made
         self._take()
 
     def _take(self) -> None:
@@ -105,7 +104,6 @@ class Mat:
         c.ld, c.dtype, c.ld_exps = ld, dtype, le
         c.data = at + first * (1 if exps is not None else 4 if dtype == FP32 else 2) if at else None
         c.exps = self._at_exps + first // GROUP if self._at_exps else None
-        self._taken += 1
 
     @property
     def dtype(self) -> int:
@@ -307,14 +305,16 @@ class Scan:
     def c(self) -> CScan:
         """The C descriptor; made again if a tensor has got other memory."""
         x, f, o, bias, h0 = self.x, self.f, self.o, self.bias, self.h0
-        x.c()
-        f.c()
-        if o is not None:
-            o.c()
-        key = (self.offsets.data_ptr(), self.offsets.numel(), x, x._taken, f, f._taken, o,
-               o._taken if o is not None else 0, bias.data_ptr() if bias is not None else 0,
+        key = (self.offsets.data_ptr(), self.offsets.numel(), x.tensor.data_ptr(), f.tensor.data_ptr(),
+               o.tensor.data_ptr() if o is not None else 0, bias.data_ptr() if bias is not None else 0,
                h0.data_ptr() if h0 is not None else 0)
+        if x.exps is not None:
+            key += tuple(m.exps.data_ptr() for m in (x, f, o) if m is not None and m.exps is not None)
         if key != self._key:
+            x.c()
+            f.c()
+            if o is not None:
+                o.c()
             self.tokens, self.dim, self.seqs = x.rows, x.cols, key[1] - 1
             _want(f, self.tokens, self.dim, "f")
             if o is not None:
