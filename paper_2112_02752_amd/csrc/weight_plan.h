@@ -25,7 +25,11 @@ EMB_HD inline int dy_row_bytes(int32_t F, int c0, int size, bool words) {
 // Bytes readable from a step's first row on, at one column, where `left` rows lie ld bytes apart and `row` bytes of
 // the last one follow the column: none where the column is past the matrix (row 0 or less).  A tile's second group of
 // columns may be.
-EMB_HD inline int rows_bytes(int left, int ld, int row) { return left > 0 && row > 0 ? (left - 1) * ld + row : 0; }
+EMB_HD inline int rows_bytes(int left, int ld, int row) {
+  // (in this form 32768 x 2048 x 6144 takes 803 us, with one condition of both 809)
+  const int rows = row > 0 ? left : 0;
+  return rows > 0 ? (rows - 1) * ld + row : 0;
+}
 
 // Tiles of 128 x 128 with the rows cut into as many parts as give each compute
 // unit a block, of at least four steps: 2048 x 256 x 256 11.7 us (13.9 with eight),
