@@ -427,8 +427,8 @@ typedef enum { EMB_ROWS = 0, EMB_TABLE = 1, EMB_TABLE_ADD = 2 } emb_grad_layout;
  *   g_u[d] = scale * sum over sorted positions k in segment u of grad_out[sort_perm[k]][d]
  * summed in fp32 in a fixed order (segments of more than 64 tokens in pieces
  * of 64, the pieces in double); the padding row's is zero.  grad_out: N rows
- * of dim columns, fp32 or bf16.  grad: device fp32, laid out as `layout`
- * says, or NULL with fuse.  fuse: NULL, or the optimizer step applied to the
+ * of dim columns, fp32 or bf16.  grad: device fp32, 16-byte aligned, laid out
+ * as `layout` says, or NULL with fuse.  fuse: NULL, or the optimizer step applied to the
  * looked-up rows but the padding row, as in emb_grad_reduce (grad must then
  * be NULL).  The dedup's outputs and ws are those emb_unique_ids left for this
  * batch, unmodified; its ids lie within their tables, as that call wants them
@@ -476,7 +476,8 @@ size_t emb_scan_workspace_size(int64_t num_tokens, int32_t dim);
 
 /* y: N rows of dim columns, of x's type.  h_last: device fp32 [M][D], the
  * state after each sequence (h0 or zero for an empty one), or NULL.  states:
- * device fp32 [ceil(N / 64)][D] for emb_scan_bwd, or NULL. */
+ * device fp32 [ceil(N / 64)][D] for emb_scan_bwd, or NULL.  Outputs may not
+ * overlap inputs, but h_last may be h0 itself. */
 emb_status emb_scan_fwd(const emb_scan* scan, const emb_mat* y, float* h_last, float* states, void* ws,
                         size_t ws_bytes, void* stream);
 

@@ -18,7 +18,7 @@
 //    depend on timing;
 //  - published words are stored and read at device scope, a flag after the
 //    words it announces; flags and counters are cleared by a kernel before.
-// 32768 positions x 2048 in bf16 (gated): 144 us forward, 3.8 TB/s; the same loads
+// 32768 positions x 2048 in bf16 (gated): 145 us forward, 3.8 TB/s; the same loads
 // and stores without the recurrence take 105 us (93 with 8-byte lanes).  What is
 // between is the chain: of the 19 us that a block lived when it was traced, 8 were
 // its loads and sums, 6.5 the wait for the spans before it and 3.5 the stores, and
@@ -31,9 +31,13 @@
 //
 // The backward is the same from the last position to the first on
 // dh_t = sigmoid(o_t) dy_t + a_{t+1} dh_{t+1}, with h recomputed inside each
-// span of 64 from the state the forward kept: 232 us there, 4.2 TB/s (its loads and
+// span of 64 from the state the forward kept: 238 us there, 4.1 TB/s (its loads and
 // stores are 939 MB), bound likewise; from 8-bit checkpoints at 16384 x 1280, 75 us,
 // 3.4 TB/s, its vector instructions half of the cycles.
+//
+// Gates are the hardware's exponential and reciprocal on fp32's product of z and
+// log2(e), whose rounding moves the smaller of a gate and its rest by about |z| 2^-24
+// of its size, twice what the rounding of z itself does; the others add a few units.
 //
 // A span that holds a first position passes nothing on of what it receives:
 // its A is kResets, not a product with zero, which would carry an infinity or

@@ -17,7 +17,7 @@
 // one leaves a partial row per chunk, which k_token_combine adds up.  Every
 // sum runs in a fixed order: results are the same from run to run.  Few
 // positions get a wavefront each.  32768 tokens x 1024 (bf16 in, every row of a
-// table of 50000 out): 47 us, 5.8 TB/s, most of it the table's 205 MB; the combine
+// table of 50000 out): 48 us, 5.7 TB/s, most of it the table's 205 MB; the combine
 // 6 us.  2000 tokens x 64 by row-wise Adagrad: 7 + 4 us, chains of dependent loads.
 #include "reduce_common.h"
 #include "seq_common.h"

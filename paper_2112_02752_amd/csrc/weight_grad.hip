@@ -18,10 +18,12 @@
 // Few tiles of dw: the rows are cut into parts whose sums are added in order.
 //
 // Bound: 2 N K F operations on the matrix units.  32768 x 2048 x 6144 (bf16 dy):
-// 785 us, 1050 TFLOP/s, of 1216 that a library product of 8192^3 reaches; adding
-// its four parts is 39 us of it.  2048 x 512 x 1536: 18.6 us, of which the products
+// 808 us, 1020 TFLOP/s, of 1216 that a library product of 8192^3 reaches; adding
+// its four parts is 39 us of it.  2048 x 512 x 1536: 17.7 us, of which the products
 // take 14 (what is read and the parts are 44 MB; small tiles with four wavefronts a
-// block 15.5) and the parts' sums 4.
+// block 15.5) and the parts' sums 4.  An fp32 dy makes three products of one and has
+// one LDS buffer: 3160 us there, of 2035 at the library's rate.  Times that compare
+// two ways below are of repeated calls on one set of inputs.
 #include "seq_common.h"
 #include "weight_plan.h"
 

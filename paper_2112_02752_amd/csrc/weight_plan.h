@@ -43,7 +43,7 @@ EMB_HD inline int rows_bytes(int left, int ld, int row) {
 // 32768 x 1024 x 1024 87 (126), 1024 x 2048 x 6144 42 (55), 4096 x 1500 x 2500 60 (65),
 // 8192 x 500 x 2500 53 (51), 2048 x 2048 x 2048 48 (38), 20000 x 300 x 800 50 (36); four
 // parts of 192 large tiles in three full rounds against one part 785 (811), of 96
-// tiles 416 (434).
+// tiles 416 (434).  (Repeated calls on one set of inputs.)
 constexpr int kBlocks = 256, kSmallSteps = 4, kBigSteps = 16, kMostRounds = 4;
 constexpr double kSmallUs = 6., kSmallStepUs = 0.9, kBigUs = 11., kBigStepUs = 0.85, kBusyUs = 1., kPartUs = 1.5e-6;
 struct Plan {

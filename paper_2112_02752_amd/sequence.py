@@ -334,9 +334,10 @@ def scan_workspace_size(num_tokens: int, dim: int) -> int:
 
 class Recurrence:
     """The gated linear recurrence with its workspace, for batches of up to
-    ``max_tokens`` tokens; with ``train`` the forward keeps a state every 64
-    positions for the backward of the same batch.  Calls on one object must be
-    ordered."""
+    ``max_tokens`` tokens (no buffer depends on the number of sequences:
+    ``max_seqs`` is not looked at); with ``train`` the forward keeps a state every
+    64 positions for the backward of the same batch.  Calls on one object must
+    be ordered."""
 
     def __init__(self, max_tokens: int, max_seqs: int, dim: int, device="cuda", train: bool = True):
         import torch
@@ -502,6 +503,9 @@ class SequenceLayer:
     projection in full width are the caching allocator's for the length of a
     call, so a model's layers share them.  ``step`` is one token of each running
     sequence (serving), with states in a pool of slots.
+
+    The backward reads the 8-bit checkpoints always; who wants its activations
+    in 16 bits calls TokenLayer and Recurrence.
 
     ``weight`` is a bf16 D x 3H tensor and ``bias`` an fp32 one of H values, both
     the caller's: ``backward`` leaves their gradients in fp32 and trains the
