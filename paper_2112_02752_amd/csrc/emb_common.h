@@ -285,8 +285,6 @@ constexpr uint64_t kWaitTicks = 2000000;
 constexpr uint32_t kDedupErrors = 3u;
 // error bit of the gradient combine: one of its waits ran out
 constexpr uint32_t kCombineError = 4u;
-// error bit of the recurrence (in its own workspace): a wait for the spans before ran out
-constexpr uint32_t kScanError = 8u;
 
 // Site codes of the waits: (kernel << 8) | (sort pass << 4) | wait.
 enum WaitSite : uint32_t {
@@ -297,7 +295,6 @@ enum WaitSite : uint32_t {
   kSiteRangeCounts = 0x105,  // range prefix block: its tiles' counts
   kSiteUnique = 0x200,       // unique look-back
   kSiteCombine = 0x300,      // gradient combine: crossing-segment rows
-  kSiteScan = 0x400,         // recurrence: the spans before
 };
 
 __device__ __forceinline__ uint64_t wait_clock() { return wall_clock64(); }

@@ -64,6 +64,9 @@ struct Rows {
 };
 
 constexpr int kSpan = EMB_SCAN_SPAN;
+// In the header of the recurrence's own workspace: error bit of a wait for the spans before that ran out, and the
+// wait's site (the dedup's and the combine's bits are 1, 2 and 4, their sites below 0x400)
+constexpr uint32_t kScanError = 8u, kSiteScan = 0x400u;
 
 struct ScanLaunch {
   int64_t N;
