@@ -532,6 +532,62 @@ size_t emb_weight_grad_workspace_size(int64_t rows, int32_t dim, int32_t cols);
 emb_status emb_weight_grad(int64_t rows, int32_t dim, int32_t cols, const emb_mat* x, const emb_mat* dy, float* dw,
                            int32_t add, void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Operators of a model's block: what stands between the projections of a model
+ * over such sequences, and its answers.  Rows are tokens.  A branch is added to
+ * the residual stream (with dropout while it trains) and the sum normalised;
+ * linear attention mixes a sequence's rows; log probabilities of given tokens
+ * are the answers.  Matrices and refusals are as above. */
+
+/* Residual addition, dropout and root-mean-square norm of every row:
+ *   t = residual + keep(x)       keep(x) = x / (1 - drop) or 0, see emb_dropout
+ *   y = weight * t / sqrt(mean(t^2) + eps)
+ * Sums are fp32; t is rounded to total's type first, and the norm is that of
+ * the rounded t, which the backward reads again.  x and y are of one type, and
+ * residual and total of one: x's, or fp32 beside bf16.  Each of residual, total
+ * and one of y and saved may be NULL (or have no data); t has x's type where
+ * both residual and total are left out.  saved: y as its type holds it in 8
+ * bits, as emb_save leaves it.  total may be residual's rows, y x's.
+ * 1 <= dim <= 16384, else EMB_EUNSUPPORTED.  With an eps of zero a row of zeros gives NaN, as
+ * do infinities and NaN in their own row; rows whose squares overflow fp32 give
+ * zeros. */
+typedef struct {
+  const float* weight; /* device [dim], or NULL: ones */
+  float eps;           /* >= 0 */
+  float drop;          /* share dropped, 0 <= drop < 1; 0: nothing */
+  uint64_t seed;
+  int64_t first_row;   /* number of the first row in the draws, >= 0 */
+} emb_norm;
+
+emb_status emb_norm_fwd(int64_t rows, int32_t dim, const emb_norm* norm, const emb_mat* x, const emb_mat* residual,
+                        const emb_mat* total, const emb_mat* y, const emb_mat* saved, void* stream);
+
+/* Backward of emb_norm_fwd from its total, n = t / sqrt(mean(t^2) + eps):
+ *   dtotal = arriving + (weight * dy - n * mean(weight * dy * n)) / sqrt(mean(t^2) + eps)
+ *   dbranch = keep(dtotal)       (of the values before they are rounded to dtotal's type)
+ *   dweight = sum over rows of dy * n   (+ dweight with add), in a fixed order
+ * The residual's gradient is dtotal.  dy and dbranch are of x's type, total,
+ * arriving (NULL: zero) and dtotal of the stream's; dtotal, dbranch and dweight
+ * (device fp32 [dim]) may be NULL.  dtotal may be arriving's rows, dbranch dy's.  ws (with
+ * dweight): device, 256-byte aligned, ws_bytes >= emb_norm_workspace_size (0
+ * for invalid sizes). */
+size_t emb_norm_workspace_size(int64_t rows, int32_t dim);
+emb_status emb_norm_bwd(int64_t rows, int32_t dim, const emb_norm* norm, const emb_mat* total, const emb_mat* dy,
+                        const emb_mat* arriving, const emb_mat* dtotal, const emb_mat* dbranch, float* dweight,
+                        int32_t add, void* ws, size_t ws_bytes, void* stream);
+
+/* Dropout whose mask is never stored: y = keep(x), its gradient is the same
+ * call on dy.  With P = round(65536 * drop) a value is dropped where its 16
+ * bits are below P, and else multiplied by 65536 / (65536 - P).  Columns
+ * 4 c .. 4 c + 3 of row r take their bits, lowest first, from the draw numbered
+ * k = (first_row + r) * ceil(dim / 4) + c:
+ *   mix(mix(seed + g) + (k + 1) * g),  g = 0x9e3779b97f4a7c15,
+ * mix being splitmix64's finaliser.  Draws depend on nothing else, so a batch
+ * may be cut into parts that give their first_row.  EMB_EINVAL where P is 65536.  x and y are of
+ * one type; y may be x's rows. */
+emb_status emb_dropout(int64_t rows, int32_t dim, float drop, uint64_t seed, int64_t first_row, const emb_mat* x,
+                       const emb_mat* y, void* stream);
+
 const char* emb_status_string(int32_t status);
 
 #ifdef __cplusplus

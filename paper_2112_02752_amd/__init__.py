@@ -32,7 +32,8 @@ EXPORTED = ("emb_pool_fwd", "emb_workspace_size", "emb_workspace_init", "emb_uni
             "emb_status_string", "emb_route_workspace_size", "emb_route_ids", "emb_route_ids_noalloc",
             "emb_pipeline_steps", "emb_unique_ids_batched",
             "emb_token_fwd", "emb_token_grad", "emb_scan_workspace_size", "emb_scan_fwd", "emb_scan_bwd",
-            "emb_scan_step", "emb_save", "emb_restore", "emb_weight_grad_workspace_size", "emb_weight_grad")
+            "emb_scan_step", "emb_save", "emb_restore", "emb_weight_grad_workspace_size", "emb_weight_grad",
+            "emb_norm_fwd", "emb_norm_workspace_size", "emb_norm_bwd", "emb_dropout")
 
 
 class EmbError(RuntimeError):
@@ -144,8 +145,9 @@ def lib():
         L.emb_workspace_status.argtypes = [vp, sz, vp, vp]
         L.emb_status_string.restype = ctypes.c_char_p
         L.emb_status_string.argtypes = [i32]
-        from .sequence import _declare
-        _declare(L)
+        from . import block, sequence
+        sequence._declare(L)
+        block._declare(L)
         _lib = L
     return _lib
 
@@ -767,3 +769,4 @@ class Pipeline:
 
 from .sequence import (Checkpoint, Mat, Recurrence, Scan, SequenceLayer, TokenLayer, scan_step,  # noqa: E402
                        scan_workspace_size, token_fwd, token_grad)
+from .block import Norm, dropout  # noqa: E402

@@ -1,0 +1,46 @@
+// Launch descriptors of the operators of a model's block (norm and dropout,
+// linear attention, log probabilities).  A launch enqueues nothing and returns
+// hipErrorNotSupported where a kernel's grid would be too large.
+#pragma once
+
+#include "seq_common.h"
+
+namespace emb {
+
+// A draw's key, and what it drops: values whose 16 bits are below `below`.
+struct Drop {
+  uint64_t key;
+  uint32_t below;  // 0: nothing
+  float scale;     // of kept values
+  int64_t first_row;
+};
+
+constexpr int kNormMaxDim = 16384;
+struct NormLaunch {
+  int64_t N;
+  int32_t D, dtype, stream_dtype;
+  int32_t aligned;  // every matrix and row begins at a multiple of 16 bytes
+  float eps;
+  const float* weight;
+  Drop drop;
+  // forward: x, residual (or none), total, y, saved (each may be none)
+  // backward: total, dy, arriving (or none), dtotal, dbranch (each may be none)
+  Rows x, residual, total, y, saved, dy, arriving, dtotal, dbranch;
+  float* dweight;
+  int32_t add;
+  float* ws;
+};
+size_t norm_ws_bytes(int64_t N, int32_t D);
+hipError_t launch_norm_fwd(const NormLaunch& p, hipStream_t s);
+hipError_t launch_norm_bwd(const NormLaunch& p, hipStream_t s);
+
+struct DropLaunch {
+  int64_t N;
+  int32_t D, dtype, aligned;
+  Drop drop;
+  Rows x, y;
+};
+Drop make_drop(float p, uint64_t seed, int64_t first_row);  // p below 1
+hipError_t launch_dropout(const DropLaunch& p, hipStream_t s);
+
+}  // namespace emb

@@ -2,6 +2,7 @@
 // layout, kernel dispatch.  No allocation, no synchronisation.
 #include <string.h>
 
+#include "api_common.h"
 #include "emb_common.h"
 #include "kernels.h"
 #include "seq_common.h"
@@ -11,8 +12,6 @@ using namespace emb;
 namespace {
 
 constexpr int64_t kMaxIndices = (int64_t)1 << 30;
-
-int dtype_bytes(int32_t dtype) { return dtype == EMB_FP32 ? 4 : (dtype == EMB_BF16 ? 2 : 0); }
 
 emb_status check_tables(const emb_tables* t, TableOffsets* ro, int64_t* total_rows) {
   if (t == nullptr || t->row_offset == nullptr || t->weights == nullptr) return EMB_EINVAL;
@@ -92,10 +91,6 @@ emb_status check_update(const emb_update* u) {
   return EMB_OK;
 }
 
-emb_status hip_status(hipError_t e) {
-  return e == hipSuccess ? EMB_OK : (e == hipErrorNotSupported ? EMB_EUNSUPPORTED : EMB_EHIP);
-}
-
 // host checks of a routing call; fills the launch descriptor (ws left null)
 emb_status route_prepare(const emb_tables* tables, const emb_batch* batch, int32_t world_size,
                          const int64_t* shard_start, int32_t* send_counts, int32_t* send_ids, int32_t* send_pos,
@@ -136,31 +131,10 @@ emb_status route_prepare(const emb_tables* tables, const emb_batch* batch, int32
 
 // ---- sequences of tokens
 
-constexpr int64_t kMaxTokens = ((int64_t)1 << 31) - 64 - 1;
-
 constexpr int64_t kMaxRowBytes = (int64_t)1 << 24;
 
 emb_status check_token(const emb_token* t, int64_t R) {
   return t == nullptr || t->pad_row >= R ? EMB_EINVAL : EMB_OK;
-}
-
-// a matrix with `cols` columns in use; saved: an 8-bit checkpoint, else fp32 or bf16
-emb_status check_mat(const emb_mat* m, int32_t cols, bool saved) {
-  if (m == nullptr || m->data == nullptr) return EMB_EINVAL;
-  if (saved) {
-    if (m->dtype != EMB_SAVED8 || m->exps == nullptr) return EMB_EINVAL;
-    const int64_t groups = (cols + (int64_t)EMB_SAVED_GROUP - 1) / EMB_SAVED_GROUP;
-    if (m->ld < groups * EMB_SAVED_GROUP || m->ld_exps < groups) return EMB_EINVAL;
-    if (m->ld % EMB_SAVED_GROUP != 0 || ((uintptr_t)m->data & 31u) != 0) return EMB_EINVAL;
-    return EMB_OK;
-  }
-  const int size = dtype_bytes(m->dtype);
-  if (size == 0 || m->ld < cols) return EMB_EINVAL;
-  return ((uintptr_t)m->data & (uintptr_t)(size - 1)) != 0 ? EMB_EINVAL : EMB_OK;
-}
-
-Rows rows_of(const emb_mat& m) {
-  return Rows{static_cast<char*>(m.data), m.ld * (m.dtype == EMB_SAVED8 ? 1 : dtype_bytes(m.dtype)), m.exps, m.ld_exps};
 }
 
 // whether a lane may take two 16-bit columns of a row (or two codes) as one word

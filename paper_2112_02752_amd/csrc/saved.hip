@@ -5,21 +5,13 @@
 // group's largest magnitude needs two exchanges within a quad.  One pass over
 // the data: bound by its bytes.  16384 x 3840 bf16 to 8 bits: 31 us, 6.1 TB/s; 1000 x
 // 200 fp32: 2.9 us each way, a launch and one load.
-#include "seq_common.h"
+#include "saved_codes.h"
 
 namespace emb {
 
 namespace {
 
-constexpr int kCols = 8;                          // columns a lane takes
-constexpr int kLanes = EMB_SAVED_GROUP / kCols;   // lanes a group
-static_assert(kLanes == 4, "the group's exchange is one within a quad");
-
-// largest of a quad's values, NaN and infinity being larger than any number as their bits
-__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
-  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xb1, 0xf, 0xf, true));  // quad_perm:[1,0,3,2]
-  return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4e, 0xf, 0xf, true));  // [2,3,0,1]
-}
+constexpr int kCols = kCodeCols, kLanes = kCodeLanes;
 
 template <typename T>
 __global__ __launch_bounds__(256) void k_save(SaveLaunch a) {
@@ -44,26 +36,10 @@ __global__ __launch_bounds__(256) void k_save(SaveLaunch a) {
       x[i] = v.get(0);
     }
   }
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < kCols; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-  top = quad_max(top);
-  const bool fine = top < 0x7f800000u;
-  // 127 * 2^e has the mantissa 0x7e0000: one more step of the exponent above it
-  int e = (int)((top + 0x1ffffu) >> 23) - 133;
-  e = min(max(e, -120), 121);
-  const float inverse = __uint_as_float((uint32_t)(127 - e) << 23);
-  uint32_t w[2] = {0u, 0u};
-#pragma unroll
-  for (int i = 0; i < kCols; ++i) {
-    float r = __builtin_rintf(x[i] * inverse);
-    r = fminf(fmaxf(r, -127.f), 127.f);
-    const uint32_t code = fine ? (uint32_t)(int)r & 0xffu : 0u;
-    w[i / 4] |= code << (8 * (i % 4));
-  }
-  *reinterpret_cast<u32x2*>(a.saved.p + row * a.saved.ld + col) = u32x2{w[0], w[1]};
-  if (lane % kLanes == 0)
-    const_cast<uint8_t*>(a.saved.exps)[row * a.saved.ld_exps + col / EMB_SAVED_GROUP] = fine ? (uint8_t)(e + 127) : 255;
+  u32x2 codes;
+  const uint8_t e = group_codes(x, codes);
+  *reinterpret_cast<u32x2*>(a.saved.p + row * a.saved.ld + col) = codes;
+  if (lane % kLanes == 0) const_cast<uint8_t*>(a.saved.exps)[row * a.saved.ld_exps + col / EMB_SAVED_GROUP] = e;
 }
 
 template <typename T>

@@ -1,0 +1,91 @@
+"""Plain forms in 64 bits of the operators of a model's block, in numpy, and what
+their tests share."""
+import numpy as np
+
+U = 2.0 ** -24
+HALF = {"fp32": 2.0 ** -24, "bf16": 2.0 ** -8}     # half a step relative to a value
+DEV = "cuda"
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def dt(name):
+    import torch
+    return torch.bfloat16 if name == "bf16" else torch.float32
+
+
+def strided(x, gap, shift, dtype):
+    """x on the GPU as columns of a wider matrix (gap columns after them, shift elements before the first), the rest
+    filled with 77; the matrix and all of its memory."""
+    import torch
+    n, d = x.shape
+    buf = torch.full((n * (d + gap) + shift + 8,), 77.0, dtype=dtype, device=DEV)
+    view = buf[shift:shift + n * (d + gap)].view(n, d + gap)[:, :d] if n else buf[:0].view(0, d)
+    view.copy_(torch.as_tensor(x).to(DEV))
+    return view, buf
+
+
+def untouched(view, buf, gap, shift):
+    """Whether nothing but the matrix was written."""
+    import torch
+    n, d = view.shape
+    keep = torch.ones_like(buf, dtype=torch.bool)
+    if n:
+        keep[shift:shift + n * (d + gap)].view(n, d + gap)[:, :d] = False
+    return bool((buf[keep] == 77).all())
+
+
+def host(t):
+    return t.detach().cpu().double().numpy()
+
+
+def within(got, want, bound, what):
+    """|got - want| <= bound everywhere; tells the worst place."""
+    got = host(got) if hasattr(got, "cpu") else got
+    off = np.abs(got - want)
+    bad = ~(off <= bound)
+    if bad.any():
+        i = np.unravel_index(np.argmax(np.where(bad, off / np.maximum(bound, 1e-300), 0)), off.shape)
+        raise AssertionError(f"{what}: {bad.sum()} of {bad.size} off, worst at {i}: {got[i]!r}, {want[i]!r} wanted, "
+                             f"{off[i]:.3g} of {np.broadcast_to(bound, off.shape)[i]:.3g}")
+
+
+# ---------------------------------------------------------------- dropout, norm
+
+def kept(rows, dim, drop, seed, first_row=0):
+    """Which values dropout keeps."""
+    with np.errstate(over="ignore"):
+        def mix(z):
+            z = (z ^ (z >> np.uint64(30))) * np.uint64(0xbf58476d1ce4e5b9)
+            z = (z ^ (z >> np.uint64(27))) * np.uint64(0x94d049bb133111eb)
+            return z ^ (z >> np.uint64(31))
+
+        g = np.uint64(0x9e3779b97f4a7c15)
+        per = (dim + 3) // 4
+        k = (np.uint64(first_row) + np.arange(rows, dtype=np.uint64))[:, None] * np.uint64(per) \
+            + np.arange(per, dtype=np.uint64)
+        z = mix(mix(np.array(seed % (1 << 64), dtype=np.uint64) + g) + (k + np.uint64(1)) * g)
+    bits = np.stack([(z >> np.uint64(16 * i)) & np.uint64(0xffff) for i in range(4)], 2).reshape(rows, 4 * per)
+    return bits[:, :dim] >= np.uint64(round(drop * 65536))
+
+
+def keep_scale(drop):
+    return 65536 / (65536 - round(drop * 65536))
+
+
+def dropped(x, drop, seed, first_row=0):
+    if round(drop * 65536) == 0:
+        return x
+    return np.where(kept(*x.shape, drop, seed, first_row), x * keep_scale(drop), 0.0)
+
+
+def norm_parts(total, weight, eps, dy):
+    """1 / root, n, dtotal without what arrives, and the magnitudes that its rounding errors follow."""
+    inv = 1 / np.sqrt((total * total).mean(1, keepdims=True) + eps)
+    n = total * inv
+    gw = dy * weight
+    grad = inv * (gw - n * (gw * n).mean(1, keepdims=True))
+    size = inv * (np.abs(gw) + np.abs(n) * np.abs(gw * n).mean(1, keepdims=True))
+    return inv, n, grad, size
