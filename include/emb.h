@@ -588,6 +588,64 @@ emb_status emb_norm_bwd(int64_t rows, int32_t dim, const emb_norm* norm, const e
 emb_status emb_dropout(int64_t rows, int32_t dim, float drop, uint64_t seed, int64_t first_row, const emb_mat* x,
                        const emb_mat* y, void* stream);
 
+/* Linear attention with a decay for each key head, over ragged sequences:
+ *   S_t = decay S_{t-1} + k_t^T v_t        (dk x dv, from first[m] or zero)
+ *   y_t = scale q_t S_t
+ * A token's row of q holds `heads` heads of dk columns, of k and v `groups`
+ * heads of dk and dv; `heads` is a multiple of `groups`, and consecutive
+ * heads / groups query heads share a key head.  Sequence m holds positions
+ * offsets[m] .. offsets[m+1]-1 as in emb_scan; rows from offsets[num_seqs] on
+ * are neither read nor written.  Inputs and outputs are of one type, fp32 or bf16.
+ * States and sums are fp32; with bf16 rows, weights within a chunk of 64
+ * positions and the state are rounded to bf16 where a row is multiplied with
+ * them, but never where they are kept.  An infinity or NaN in a row spoils the
+ * results of its sequence from its chunk's first position on (in the
+ * backward also those before it).
+ * EMB_EUNSUPPORTED for dk or dv above 256. */
+typedef struct {
+  int64_t num_tokens; /* N */
+  int32_t num_seqs;   /* M */
+  int32_t heads, groups, dk, dv;
+  const int32_t* offsets; /* device [M + 1] */
+  emb_mat q, k, v;
+  const float* decay; /* device [groups], 0 <= decay <= 1 */
+  float scale;
+  const float* first; /* device [M][groups][dk][dv] or NULL */
+} emb_heads;
+
+/* Bytes of the states kept between segments of up to num_tokens tokens (0 may
+ * be right for few; see the entry points for what is invalid): the forward
+ * writes them, the backward of the same batch reads them, and a backward needs
+ * as many again as workspace.  Nothing needs initialisation. */
+size_t emb_linear_states_size(int64_t num_tokens, int32_t groups, int32_t dk, int32_t dv);
+
+/* y: N rows of heads * dv columns.  last: device fp32 [M][groups][dk][dv],
+ * the state after each sequence (first or zero for an empty one), or NULL.
+ * states: device, 256-byte aligned, states_bytes >= emb_linear_states_size.
+ * Outputs may not overlap inputs. */
+emb_status emb_linear_fwd(const emb_heads* heads, const emb_mat* y, float* last, void* states, size_t states_bytes,
+                          void* stream);
+
+/* Backward, dS being the gradient at S_t from all of its uses:
+ *   dq_t = scale dy_t S_t^T (of every head),  dS_t = scale q_t^T dy_t (summed over
+ *   the group's heads) + decay dS_{t+1} (+ dlast[m] at the end),
+ *   dk_t = v_t dS_t^T,  dv_t = k_t dS_t,  dfirst[m] = decay dS at the first
+ *   position (dlast[m] if empty)
+ * dq, dk, dv: as q, k, v.  dlast, dfirst: as last, each may be NULL.  decay is
+ * a constant.  ws: like states. */
+emb_status emb_linear_bwd(const emb_heads* heads, const void* states, size_t states_bytes, const emb_mat* dy,
+                          const emb_mat* dq, const emb_mat* dk, const emb_mat* dv, const float* dlast, float* dfirst,
+                          void* ws, size_t ws_bytes, void* stream);
+
+/* One token of each of num_tokens running sequences (serving), as
+ * emb_scan_step: row i's state is state[slots[i]] (device fp32, num_slots of
+ * groups x dk x dv values, updated in place; slots NULL: slot i).  A token whose slot lies
+ * outside 0..num_slots-1 gets zeros and touches no state.  Slots must be
+ * distinct.  All in fp32. */
+emb_status emb_linear_step(int64_t num_tokens, int32_t heads, int32_t groups, int32_t dk, int32_t dv, const emb_mat* q,
+                           const emb_mat* k, const emb_mat* v, const float* decay, float scale, float* state,
+                           int64_t num_slots, const int32_t* slots, const emb_mat* y, void* stream);
+
 const char* emb_status_string(int32_t status);
 
 #ifdef __cplusplus

@@ -33,7 +33,8 @@ EXPORTED = ("emb_pool_fwd", "emb_workspace_size", "emb_workspace_init", "emb_uni
             "emb_pipeline_steps", "emb_unique_ids_batched",
             "emb_token_fwd", "emb_token_grad", "emb_scan_workspace_size", "emb_scan_fwd", "emb_scan_bwd",
             "emb_scan_step", "emb_save", "emb_restore", "emb_weight_grad_workspace_size", "emb_weight_grad",
-            "emb_norm_fwd", "emb_norm_workspace_size", "emb_norm_bwd", "emb_dropout")
+            "emb_norm_fwd", "emb_norm_workspace_size", "emb_norm_bwd", "emb_dropout",
+            "emb_linear_states_size", "emb_linear_fwd", "emb_linear_bwd", "emb_linear_step")
 
 
 class EmbError(RuntimeError):
@@ -769,4 +770,4 @@ class Pipeline:
 
 from .sequence import (Checkpoint, Mat, Recurrence, Scan, SequenceLayer, TokenLayer, scan_step,  # noqa: E402
                        scan_workspace_size, token_fwd, token_grad)
-from .block import Norm, dropout  # noqa: E402
+from .block import Heads, LinearAttention, Norm, dropout, linear_attention_step  # noqa: E402

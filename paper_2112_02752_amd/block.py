@@ -18,15 +18,26 @@ class CNorm(ctypes.Structure):
                 ("seed", ctypes.c_uint64), ("first_row", ctypes.c_int64)]
 
 
+class CHeads(ctypes.Structure):
+    _fields_ = [("num_tokens", ctypes.c_int64), ("num_seqs", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("dk", ctypes.c_int32), ("dv", ctypes.c_int32),
+                ("offsets", ctypes.c_void_p), ("q", CMat), ("k", CMat), ("v", CMat), ("decay", ctypes.c_void_p),
+                ("scale", ctypes.c_float), ("first", ctypes.c_void_p)]
+
+
 def _declare(L) -> None:
     vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
     f32, u64 = ctypes.c_float, ctypes.c_uint64
-    M, Nm = ctypes.POINTER(CMat), ctypes.POINTER(CNorm)
+    M, Nm, H = ctypes.POINTER(CMat), ctypes.POINTER(CNorm), ctypes.POINTER(CHeads)
     for name, res, args in (
             ("emb_norm_fwd", i32, [i64, i32, Nm, M, M, M, M, M, vp]),
             ("emb_norm_workspace_size", sz, [i64, i32]),
             ("emb_norm_bwd", i32, [i64, i32, Nm, M, M, M, M, M, vp, i32, vp, sz, vp]),
-            ("emb_dropout", i32, [i64, i32, f32, u64, i64, M, M, vp])):
+            ("emb_dropout", i32, [i64, i32, f32, u64, i64, M, M, vp]),
+            ("emb_linear_states_size", sz, [i64, i32, i32, i32]),
+            ("emb_linear_fwd", i32, [H, M, vp, vp, sz, vp]),
+            ("emb_linear_bwd", i32, [H, vp, sz, M, M, M, M, vp, vp, vp, sz, vp]),
+            ("emb_linear_step", i32, [i64, i32, i32, i32, i32, M, M, M, vp, f32, vp, i64, vp, M, vp])):
         fn = getattr(L, name)
         fn.restype, fn.argtypes = res, args
 
@@ -131,3 +142,138 @@ def dropout(x, y, drop: float, seed: int, first_row: int = 0, stream=None) -> No
     _want(y, x.rows, x.cols, "y")
     _check("emb_dropout", lib().emb_dropout(x.rows, x.cols, drop, seed & _SEED, first_row, x.ref, y.ref,
                                             _stream(stream)))
+
+
+# ---------------------------------------------------------------- linear attention
+
+def _head_widths(q, k, v, heads: int, groups: int):
+    """Widths of the heads, from the matrices' columns."""
+    if groups < 1 or heads < 1 or heads % groups != 0:
+        raise ValueError("heads are a multiple of groups")
+    if k.cols % groups != 0 or v.cols % groups != 0 or k.cols == 0 or v.cols == 0:
+        raise ValueError("keys and values have whole heads")
+    dk, dv = k.cols // groups, v.cols // groups
+    _want(q, k.rows, heads * dk, "q")
+    _want(v, k.rows, groups * dv, "v")
+    return dk, dv
+
+
+class Heads:
+    """The inputs of linear attention over ragged sequences (see emb_heads):
+    int32 offsets [M + 1] on the GPU, queries of ``heads`` heads, keys and values
+    of ``groups``, of one type, an fp32 decay for every key head and first
+    states [M][groups][dk][dv] or None."""
+
+    def __init__(self, offsets, q, k, v, decay, heads: int, groups: Optional[int] = None, scale: float = 1.0,
+                 first=None):
+        import torch
+        if offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.numel() < 1 or not offsets.is_contiguous():
+            raise ValueError("offsets are a contiguous int32 vector")
+        _device(offsets, "offsets")
+        self.heads, self.groups = heads, heads if groups is None else groups
+        self.q, self.k, self.v = _mat(q), _mat(k), _mat(v)
+        self.offsets, self.decay, self.scale, self.first = offsets, decay, scale, first
+        self._c = CHeads()
+        self.ref = ctypes.byref(self._c)
+        self._key = None
+        self.c()
+
+    def c(self) -> CHeads:
+        """The C descriptor; made again if a tensor has got other memory."""
+        q, k, v, first = self.q, self.k, self.v, self.first
+        key = (self.offsets.data_ptr(), self.offsets.numel(), q.tensor.data_ptr(), k.tensor.data_ptr(),
+               v.tensor.data_ptr(), self.decay.data_ptr(), first.data_ptr() if first is not None else 0)
+        if key != self._key:
+            for m in (q, k, v):
+                m.c()
+            self.tokens, self.seqs = k.rows, key[1] - 1
+            self.dk, self.dv = _head_widths(q, k, v, self.heads, self.groups)
+            self.states = (self.seqs, self.groups, self.dk, self.dv)
+            c = self._c
+            c.num_tokens, c.num_seqs, c.heads, c.groups = self.tokens, self.seqs, self.heads, self.groups
+            c.dk, c.dv, c.offsets, c.scale = self.dk, self.dv, key[0], self.scale
+            c.q, c.k, c.v = q._c, k._c, v._c
+            c.decay = _floats(self.decay, (self.groups,), "decay")
+            c.first = _floats(first, self.states, "first")
+            self._key = key
+        return self._c
+
+
+class LinearAttention:
+    """Linear attention with a decay for each key head, with its workspace, for
+    batches of up to ``max_tokens`` tokens (no buffer depends on the number of
+    sequences: ``max_seqs`` is not looked at); with ``train`` there is room for
+    the backward of the last forward's batch, which reads the states that the
+    forward left here.  Calls on one object must be ordered."""
+
+    def __init__(self, max_tokens: int, max_seqs: int, heads: int, groups: int, dk: int, dv: int, device="cuda",
+                 train: bool = True):
+        import torch
+        if heads < 1 or groups < 1 or heads % groups != 0 or dk < 1 or dv < 1:
+            raise ValueError("heads are a multiple of groups, and of at least one column")
+        self.max_tokens, self.max_seqs = max_tokens, max_seqs
+        self.heads, self.groups, self.dk, self.dv = heads, groups, dk, dv
+        size = int(lib().emb_linear_states_size(max_tokens, groups, dk, dv))
+        new = lambda: _device(torch.empty(max(size, 256), dtype=torch.uint8, device=device),  # noqa: E731
+                              "a linear attention's workspace")
+        self.states = new()
+        self.ws = new() if train else None
+        self._states, self._ws, self._size = self.states.data_ptr(), _ptr(self.ws), max(size, 256)
+        self._tokens = None
+
+    def _take(self, heads: Heads):
+        heads.c()
+        if heads.tokens > self.max_tokens or (heads.heads, heads.groups, heads.dk, heads.dv) != (
+                self.heads, self.groups, self.dk, self.dv):
+            raise ValueError("batch larger than the linear attention's buffers, or of other heads")
+        return heads.ref
+
+    def forward(self, heads: Heads, y, last=None, stream=None) -> None:
+        """y (N x heads * dv), and the state after each sequence into ``last``
+        (fp32 [M][groups][dk][dv])."""
+        ref = self._take(heads)
+        y = _mat(y)
+        _want(y, heads.tokens, self.heads * self.dv, "y")
+        self._tokens = None
+        _check("emb_linear_fwd", lib().emb_linear_fwd(ref, y.ref, _floats(last, heads.states, "last"), self._states,
+                                                      self._size, _stream(stream)))
+        self._tokens = heads.tokens, heads.seqs
+
+    def backward(self, heads: Heads, dy, dq, dk, dv, dlast=None, dfirst=None, stream=None) -> None:
+        """Gradients of the last forward, whose inputs these are: of the
+        queries, keys, values and first states, from those of y and of the last
+        states."""
+        ref = self._take(heads)
+        if self.ws is None or self._tokens != (heads.tokens, heads.seqs):
+            raise ValueError("backward follows the forward of the same batch on an object made with train")
+        mats = [_mat(m) for m in (dy, dq, dk, dv)]
+        for m, cols, name in zip(mats, (self.heads * self.dv, self.heads * self.dk, self.groups * self.dk,
+                                        self.groups * self.dv), ("dy", "dq", "dk", "dv")):
+            _want(m, heads.tokens, cols, name)
+        _check("emb_linear_bwd", lib().emb_linear_bwd(
+            ref, self._states, self._size, *(m.ref for m in mats), _floats(dlast, heads.states, "dlast"),
+            _floats(dfirst, heads.states, "dfirst"), self._ws, self._size, _stream(stream)))
+
+
+def linear_attention_step(q, k, v, decay, state, y, heads: int, groups: Optional[int] = None, scale: float = 1.0,
+                          slots=None, stream=None) -> None:
+    """One token of each running sequence (emb_linear_step): row i of q, k, v
+    and y belongs to ``state[slots[i]]`` (fp32 [slots][groups][dk][dv], updated in
+    place; ``slots`` int32, None: row i); tokens whose slot is no row of
+    ``state`` get zeros."""
+    q, k, v, y = _mat(q), _mat(k), _mat(v), _mat(y)
+    groups = heads if groups is None else groups
+    dk, dv = _head_widths(q, k, v, heads, groups)
+    n = k.rows
+    _want(y, n, heads * dv, "y")
+    rows = int(state.shape[0])
+    sp = None
+    if slots is not None:
+        if slots.numel() != n or slots.element_size() != 4 or slots.is_floating_point() or not slots.is_contiguous():
+            raise ValueError("slots are a contiguous int32 vector, one a token")
+        sp = _device(slots, "slots").data_ptr()
+    elif n > rows:
+        raise ValueError("more tokens than states")
+    _check("emb_linear_step", lib().emb_linear_step(
+        n, heads, groups, dk, dv, q.ref, k.ref, v.ref, _floats(decay, (groups,), "decay"), scale,
+        _floats(state, (rows, groups, dk, dv), "state"), rows, sp, y.ref, _stream(stream)))

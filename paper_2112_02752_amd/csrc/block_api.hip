@@ -55,6 +55,54 @@ emb_status check_norm(int64_t rows, int32_t dim, const emb_norm* norm, const emb
   return EMB_OK;
 }
 
+emb_status check_shape(int32_t heads, int32_t groups, int32_t dk, int32_t dv) {
+  if (heads < 1 || groups < 1 || heads % groups != 0 || dk < 1 || dv < 1) return EMB_EINVAL;
+  // (columns of a row are counted in 32 bits)
+  if (dk > kLinMaxDim || dv > kLinMaxDim || heads > (1 << 20)) return EMB_EUNSUPPORTED;
+  return EMB_OK;
+}
+
+emb_status check_heads(const emb_heads* h, LinLaunch* p) {
+  if (h == nullptr || h->num_tokens < 0 || h->num_seqs < 0) return EMB_EINVAL;
+  emb_status st = check_shape(h->heads, h->groups, h->dk, h->dv);
+  if (st != EMB_OK) return st;
+  if (h->num_tokens > kMaxTokens) return EMB_EUNSUPPORTED;
+  if (h->num_tokens > 0 && h->num_seqs == 0) return EMB_EINVAL;
+  if (h->offsets == nullptr || ((uintptr_t)h->offsets & 3u) != 0) return EMB_EINVAL;
+  if (h->num_seqs > 0 && (h->decay == nullptr || ((uintptr_t)h->decay & 3u) != 0)) return EMB_EINVAL;
+  if (((uintptr_t)h->first & 3u) != 0 || !isfinite(h->scale)) return EMB_EINVAL;
+  p->N = h->num_tokens;
+  p->M = h->num_seqs;
+  p->heads = h->heads;
+  p->groups = h->groups;
+  p->dk = h->dk;
+  p->dv = h->dv;
+  p->offsets = h->offsets;
+  p->decay = h->decay;
+  p->scale = h->scale;
+  p->first = h->first;
+  if (h->num_tokens == 0) return EMB_OK;
+  const emb_mat* all[3] = {&h->q, &h->k, &h->v};
+  const int32_t cols[3] = {h->heads * h->dk, h->groups * h->dk, h->groups * h->dv};
+  for (int i = 0; i < 3; ++i) {
+    if ((st = check_mat(all[i], cols[i], false)) != EMB_OK) return st;
+    if (all[i]->dtype != h->q.dtype) return EMB_EINVAL;
+  }
+  p->dtype = h->q.dtype;
+  p->q = rows_of(h->q);
+  p->k = rows_of(h->k);
+  p->v = rows_of(h->v);
+  const int size = dtype_bytes(p->dtype);
+  p->aligned = vectors(p->q) && vectors(p->k) && vectors(p->v) && h->dk * size % 16 == 0 && h->dv * size % 16 == 0;
+  return EMB_OK;
+}
+
+emb_status check_states(const LinLaunch& p, const void* at, size_t bytes) {
+  const size_t need = lin_states_bytes(p.N, p.groups, p.dk, p.dv);
+  if (need > 0 && at == nullptr) return EMB_EINVAL;
+  return bytes < need || ((uintptr_t)at & 255u) != 0 ? EMB_EWORKSPACE : EMB_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -130,6 +178,93 @@ emb_status emb_dropout(int64_t rows, int32_t dim, float drop, uint64_t seed, int
   p.y = rows_of(*y);
   p.aligned = vectors(p.x) && vectors(p.y);
   return hip_status(launch_dropout(p, (hipStream_t)stream));
+}
+
+size_t emb_linear_states_size(int64_t num_tokens, int32_t groups, int32_t dk, int32_t dv) {
+  if (num_tokens < 0 || num_tokens > kMaxTokens || check_shape(groups, groups, dk, dv) != EMB_OK) return 0;
+  return lin_states_bytes(num_tokens, groups, dk, dv);
+}
+
+emb_status emb_linear_fwd(const emb_heads* heads, const emb_mat* y, float* last, void* states, size_t states_bytes,
+                          void* stream) {
+  LinLaunch p{};
+  emb_status st = check_heads(heads, &p);
+  if (st != EMB_OK) return st;
+  // (a sequence's last state may be written before its first is read)
+  if (((uintptr_t)last & 3u) != 0 || (last != nullptr && last == heads->first)) return EMB_EINVAL;
+  if (p.N > 0) {
+    if ((st = check_mat(y, p.heads * p.dv, false)) != EMB_OK) return st;
+    if (y->dtype != p.dtype) return EMB_EINVAL;
+    p.y = rows_of(*y);
+    p.aligned = p.aligned && vectors(p.y);
+  }
+  if ((st = check_states(p, states, states_bytes)) != EMB_OK) return st;
+  if (p.M == 0) return EMB_OK;
+  p.last = last;
+  p.states = static_cast<float*>(states);
+  return hip_status(launch_lin_fwd(p, (hipStream_t)stream));
+}
+
+emb_status emb_linear_bwd(const emb_heads* heads, const void* states, size_t states_bytes, const emb_mat* dy,
+                          const emb_mat* dq, const emb_mat* dk, const emb_mat* dv, const float* dlast, float* dfirst,
+                          void* ws, size_t ws_bytes, void* stream) {
+  LinLaunch p{};
+  emb_status st = check_heads(heads, &p);
+  if (st != EMB_OK) return st;
+  if ((((uintptr_t)dlast | (uintptr_t)dfirst) & 3u) != 0 || (dfirst != nullptr && dfirst == dlast)) return EMB_EINVAL;
+  if (p.N > 0) {
+    const emb_mat* all[4] = {dy, dq, dk, dv};
+    const int32_t cols[4] = {p.heads * p.dv, p.heads * p.dk, p.groups * p.dk, p.groups * p.dv};
+    Rows* const to[4] = {&p.dy, &p.dq, &p.dkey, &p.dval};
+    for (int i = 0; i < 4; ++i) {
+      if ((st = check_mat(all[i], cols[i], false)) != EMB_OK) return st;
+      if (all[i]->dtype != p.dtype) return EMB_EINVAL;
+      *to[i] = rows_of(*all[i]);
+      p.aligned = p.aligned && vectors(*to[i]);
+    }
+  }
+  if ((st = check_states(p, states, states_bytes)) != EMB_OK) return st;
+  if ((st = check_states(p, ws, ws_bytes)) != EMB_OK) return st;
+  if (ws != nullptr && ws == states) return EMB_EINVAL;
+  if (p.M == 0) return EMB_OK;
+  p.dlast = dlast;
+  p.dfirst = dfirst;
+  p.states = static_cast<float*>(const_cast<void*>(states));
+  p.grads = static_cast<float*>(ws);
+  return hip_status(launch_lin_bwd(p, (hipStream_t)stream));
+}
+
+emb_status emb_linear_step(int64_t num_tokens, int32_t heads, int32_t groups, int32_t dk, int32_t dv, const emb_mat* q,
+                           const emb_mat* k, const emb_mat* v, const float* decay, float scale, float* state,
+                           int64_t num_slots, const int32_t* slots, const emb_mat* y, void* stream) {
+  if (num_tokens < 0 || num_slots < 0 || !isfinite(scale)) return EMB_EINVAL;
+  emb_status st = check_shape(heads, groups, dk, dv);
+  if (st != EMB_OK) return st;
+  if (num_tokens > kMaxTokens) return EMB_EUNSUPPORTED;
+  if (num_tokens == 0) return EMB_OK;
+  if (decay == nullptr || (num_slots > 0 && state == nullptr)) return EMB_EINVAL;
+  if ((((uintptr_t)decay | (uintptr_t)state | (uintptr_t)slots) & 3u) != 0) return EMB_EINVAL;
+  const emb_mat* all[4] = {q, k, v, y};
+  const int32_t cols[4] = {heads * dk, groups * dk, groups * dv, heads * dv};
+  LinStepLaunch p{};
+  Rows* const to[4] = {&p.q, &p.k, &p.v, &p.y};
+  for (int i = 0; i < 4; ++i) {
+    if ((st = check_mat(all[i], cols[i], false)) != EMB_OK) return st;
+    if (all[i]->dtype != q->dtype) return EMB_EINVAL;
+    *to[i] = rows_of(*all[i]);
+  }
+  p.N = num_tokens;
+  p.num_slots = num_slots;
+  p.heads = heads;
+  p.groups = groups;
+  p.dk = dk;
+  p.dv = dv;
+  p.dtype = q->dtype;
+  p.scale = scale;
+  p.decay = decay;
+  p.state = state;
+  p.slots = slots;
+  return hip_status(launch_lin_step(p, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -43,4 +43,37 @@ struct DropLaunch {
 Drop make_drop(float p, uint64_t seed, int64_t first_row);  // p below 1
 hipError_t launch_dropout(const DropLaunch& p, hipStream_t s);
 
+// Heads of linear attention are at most this wide.
+constexpr int kLinMaxDim = 256;
+struct LinLaunch {
+  int64_t N;
+  int32_t M, heads, groups, dk, dv, dtype;
+  int32_t aligned;  // every matrix, row and head begins at a multiple of 16 bytes
+  float scale;
+  const int32_t* offsets;
+  const float* decay;
+  Rows q, k, v, y;         // forward
+  Rows dy, dq, dkey, dval; // backward
+  const float* first;      // [M][groups][dk][dv] or none, as are the next three
+  float* last;
+  const float* dlast;
+  float* dfirst;
+  float* states;  // at the boundaries between segments: the forward's, read by the backward
+  float* grads;   // the backward's
+};
+size_t lin_states_bytes(int64_t N, int32_t groups, int32_t dk, int32_t dv);
+hipError_t launch_lin_fwd(const LinLaunch& p, hipStream_t s);
+hipError_t launch_lin_bwd(const LinLaunch& p, hipStream_t s);
+
+struct LinStepLaunch {
+  int64_t N, num_slots;
+  int32_t heads, groups, dk, dv, dtype;
+  float scale;
+  const float* decay;
+  Rows q, k, v, y;
+  float* state;
+  const int32_t* slots;
+};
+hipError_t launch_lin_step(const LinStepLaunch& p, hipStream_t s);
+
 }  // namespace emb

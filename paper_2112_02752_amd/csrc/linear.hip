@@ -1,0 +1,571 @@
+// Linear attention with a decay for each key head (gfx950).
+//
+//   S_t = g S_{t-1} + k_t^T v_t,   y_t = scale q_t S_t
+//
+// over ragged sequences, in chunks of C positions.  With S the state before a
+// chunk of n positions (i, j: positions within it)
+//
+//   y_i = scale ( g^(i+1) q_i S + sum over j <= i of g^(i-j) (q_i . k_j) v_j )
+//   S'  = g^n S + sum over j of g^(n-1-j) k_j^T v_j
+//
+// and all four results of the operator are this one form of rows a, b, c:
+//
+//   y :  a = q,  b = k,  c = v,  in order
+//   dq:  a = dy, b = v,  c = k,  in order (the state is S transposed)
+//   dv:  a = k,  b = q,  c = dy, backwards, the state being the gradient G that
+//        arrives at the state after a position
+//   dk:  a = v,  b = dy, c = q,  backwards, with G transposed
+//
+// Heads that share keys and values: in order a has the heads' rows, backwards b
+// and c have them, and sums over the heads arise by themselves.
+//
+// Sequences are cut into segments of L positions from their begin.  A boundary
+// at position p (a segment's begin that is not its sequence's) is number
+// p / L - 1: no two have the same one, and a sequence's are consecutive.  Three
+// launches: sums of every segment that a boundary follows (backwards: precedes),
+// the boundaries' states from them one after another, and the form itself,
+// every segment from its boundary's state.
+#include "block_common.h"
+
+namespace emb {
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256;  // four wavefronts, each a quarter of the columns of c
+
+// What a matrix instruction's operand is made of: lane l holds row (or column)
+// l % 16 and, with q = l / 16, part of a block of kBlock summed indexes.
+template <typename T>
+struct Operand;
+
+// v_mfma 16 x 16 x 32: eight of 32 indexes a lane, 8 q .. 8 q + 7; from a state 4 q + e and 16 + 4 q + e
+template <>
+struct Operand<bf16> {
+  static constexpr int kChunk = 64, kBlock = 32, kPad = 8, kVec = 8;
+  typedef uint16_t Value;
+  bf16x8 v;
+  // row `at` (an address in LDS), indexes 0 .. kBlock - 1 of it
+  __device__ __forceinline__ void row(const Value* at, int q) { v = *reinterpret_cast<const bf16x8*>(at + 8 * q); }
+  __device__ __forceinline__ void row_as_state(const Value* at, int q) {
+    const u32x2 lo = *reinterpret_cast<const u32x2*>(at + 4 * q), hi = *reinterpret_cast<const u32x2*>(at + 16 + 4 * q);
+    v = __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
+  }
+  // column l % 16 of 16 from `at` on, rows 0 .. kBlock - 1 of `ld` values: the transposing load gives a lane four rows
+  // of its column where the 16 lanes of a quarter point at those rows' 16 columns in order
+  template <int LD>
+  __device__ __forceinline__ void column(const Value* at, int q, int l) {
+    const Value* p = at + (8 * q + l / 4) * LD + 4 * (l % 4);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + 4 * LD));
+    const u32x2 a = __builtin_bit_cast(u32x2, lo), b = __builtin_bit_cast(u32x2, hi);
+    v = __builtin_bit_cast(bf16x8, u32x4{a.x, a.y, b.x, b.y});
+  }
+  // 32 indexes of a state: two tiles
+  __device__ __forceinline__ void state(const f32x4* tiles, int stride) {
+    const f32x4 a = tiles[0], b = tiles[stride];
+    v = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w)});
+  }
+  // this operand times weights, in two parts that hold 16 bits of the products
+  __device__ __forceinline__ void weighted(const Operand& from, const float (&w)[8], Operand& rest) {
+    const u32x4 x = __builtin_bit_cast(u32x4, from.v);
+    u32x4 hi, lo;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float a = bf16_lo(x[i]) * w[2 * i], b = bf16_hi(x[i]) * w[2 * i + 1];
+      hi[i] = pack_bf16(a, b);
+      lo[i] = pack_bf16(a - bf16_lo(hi[i]), b - bf16_hi(hi[i]));
+    }
+    v = __builtin_bit_cast(bf16x8, hi);
+    rest.v = __builtin_bit_cast(bf16x8, lo);
+  }
+  static constexpr int kParts = 2;
+  static __device__ __forceinline__ int index(int q, int e) { return 8 * q + e; }
+  static constexpr int kEach = 8;
+};
+
+// v_mfma 16 x 16 x 4, four times: a lane's four of 16 indexes are 4 q .. 4 q + 3, one a time
+template <>
+struct Operand<float> {
+  static constexpr int kChunk = 32, kBlock = 16, kPad = 4, kVec = 4;
+  typedef float Value;
+  f32x4 v;
+  __device__ __forceinline__ void row(const Value* at, int q) { v = *reinterpret_cast<const f32x4*>(at + 4 * q); }
+  __device__ __forceinline__ void row_as_state(const Value* at, int q) { row(at, q); }
+  template <int LD>
+  __device__ __forceinline__ void column(const Value* at, int q, int l) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = at[(4 * q + e) * LD + l];
+  }
+  __device__ __forceinline__ void state(const f32x4* tiles, int) { v = tiles[0]; }
+  __device__ __forceinline__ void weighted(const Operand& from, const float (&w)[4], Operand&) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = from.v[e] * w[e];
+  }
+  static constexpr int kParts = 1;
+  static __device__ __forceinline__ int index(int q, int e) { return 4 * q + e; }
+  static constexpr int kEach = 4;
+};
+
+// D[m][n] += sum over k of A[m][k] B[n][k]; lane l holds n = l % 16, m = 4 (l / 16) .. + 3
+__device__ __forceinline__ void mul(f32x4& d, const Operand<bf16>& a, const Operand<bf16>& b) {
+  d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, d, 0, 0, 0);
+}
+__device__ __forceinline__ void mul(f32x4& d, const Operand<float>& a, const Operand<float>& b) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) d = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[e], b.v[e], d, 0, 0, 0);
+}
+
+struct Form {
+  Rows a, b, c, out;
+  const float* bounds;  // states at the boundaries
+  const float* begin;   // of whole sequences: states that the sweep begins with, or none
+  float* end;           // and ends with, or none
+  int32_t da, dc;       // widths of a and b, of c and out
+  int32_t sd, sn;       // state: distance of two indexes of b, of c
+  float p_scale, u_scale, out_scale;  // of products a . b, of what the state gets, of out
+};
+
+struct Args {
+  int64_t N, L, bounds;  // segment length, number of boundaries
+  int32_t M, groups, per;  // heads of a group
+  int32_t aligned;
+  const int32_t* offsets;
+  const float* decay;
+  int64_t state;  // values of a group's state
+  Form f[3];
+  int32_t slices[3];
+  float* sums;
+};
+
+// g^e for a whole e >= 0, in 64 bits
+__device__ __forceinline__ double power(float g, int64_t e) {
+  double r = 1.0, b = (double)g;
+  for (; e > 0; e >>= 1) {
+    if (e & 1) r *= b;
+    b *= b;
+  }
+  return r;
+}
+
+struct Segment {
+  int64_t begin, end;
+  int32_t seq;
+  bool first, last;  // of its sequence
+};
+
+// the boundary of this number: the segment that begins there; false if there is none
+__device__ __forceinline__ bool boundary(const Args& a, int64_t number, int lane, Segment& s) {
+  const int64_t pos = (number + 1) * a.L;
+  s.seq = wave_upper_bound(a.offsets, a.M + 1, (int32_t)pos, lane) - 1;
+  if (s.seq < 0 || s.seq >= a.M) return false;
+  const int64_t o = a.offsets[s.seq], e = min((int64_t)a.offsets[s.seq + 1], a.N);
+  if (pos == o) return false;
+  s.begin = o + (pos - o + a.L - 1) / a.L * a.L;
+  if (s.begin >= e) return false;
+  s.end = min(s.begin + a.L, e);
+  s.first = false;
+  s.last = s.end == e;
+  return true;
+}
+// segments: the boundaries', then the sequences' first ones
+__device__ __forceinline__ bool segment(const Args& a, int64_t number, int lane, Segment& s) {
+  if (number < a.bounds) return boundary(a, number, lane, s);
+  s.seq = (int32_t)(number - a.bounds);
+  const int64_t e = min((int64_t)a.offsets[s.seq + 1], a.N);
+  s.begin = min((int64_t)a.offsets[s.seq], e);
+  s.end = min(s.begin + a.L, e);
+  s.first = true;
+  s.last = s.end == e;
+  return true;
+}
+
+// Rows of a chunk into LDS: row r is position p0 + r (REV: p0 - r), `n` of them, `w` columns from byte `at` of a row on;
+// zeros where there are none.
+template <typename T, int W, bool REV>
+__device__ __forceinline__ void stage(typename Operand<T>::Value* lds, const Rows& m, int64_t at, int w, int64_t p0, int n,
+                                      bool aligned) {
+  constexpr int kVec = Operand<T>::kVec, kRow = W / kVec, kLd = W + Operand<T>::kPad;
+  static_assert(Operand<T>::kChunk * kRow % kThreads == 0, "whole rounds");
+#pragma unroll
+  for (int i = 0; i < Operand<T>::kChunk * kRow / kThreads; ++i) {
+    const int x = i * kThreads + threadIdx.x, r = x / kRow, col = x % kRow * kVec;
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if (r < n && col < w) {
+      const char* p = m.p + (REV ? p0 - r : p0 + r) * m.ld + at + col * (int)sizeof(typename Operand<T>::Value);
+      if (aligned && col + kVec <= w) {
+        v = *reinterpret_cast<const u32x4*>(p);
+      } else {
+        const auto* e = reinterpret_cast<const typename Operand<T>::Value*>(p);
+        if constexpr (kVec == 8) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (col + k < w) v[k / 2] |= (uint32_t)e[k] << (16 * (k % 2));
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (col + k < w) v[k] = __float_as_uint(e[k]);
+        }
+      }
+    }
+    *reinterpret_cast<u32x4*>(lds + r * kLd + col) = v;
+  }
+}
+
+// DA: widest a and b; DC: columns of c that a block takes.  OUT: the form itself, else the sums of the segment that ends
+// (REV: begins) at a boundary.
+template <typename T, int DA, int DC, bool REV, bool OUT>
+__device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t number, int group, int slice) {
+  typedef Operand<T> Op;
+  typedef typename Op::Value Value;
+  constexpr int C = Op::kChunk, KB = Op::kBlock, TC = C / 16, TD = DA / 16, TN = DC / 64, KC = C / KB, KD = DA / KB;
+  constexpr int LA = DA + Op::kPad, LC = DC + Op::kPad, LP = C + Op::kPad;
+  __shared__ __align__(16) Value s_a[OUT ? C * LA : 1], s_b[C * LA], s_c[C * LC], s_p[OUT ? C * LP : 1];
+  __shared__ float s_pow[C + 1];
+  const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), l = lane % 16, q = lane / 16;
+  Segment s;
+  if (OUT ? !segment(args, number, lane, s) : !boundary(args, number, lane, s)) return;
+  if (!OUT && !REV) {  // the segment before
+    s.end = s.begin;
+    s.begin -= args.L;
+  }
+  const float g = args.decay[group];
+  if (threadIdx.x <= C) s_pow[threadIdx.x] = (float)power(g, threadIdx.x);
+  if constexpr (OUT) {
+    for (int i = threadIdx.x; i < C * LP; i += kThreads) s_p[i] = 0;
+  }
+  const int size = sizeof(Value), c0 = slice * DC, wc = min(DC, f.dc - c0), n0 = wave * 16 * TN;
+  const int64_t states = (int64_t)args.groups * args.state, mine = (int64_t)group * args.state;
+  // the state: lane l holds column n0 + 16 t + l % 16, rows 16 d + 4 q ..
+  f32x4 st[TD][TN];
+  const float* from = nullptr;
+  if constexpr (OUT) {
+    if (REV ? s.last : s.first) from = f.begin != nullptr ? f.begin + s.seq * states + mine : nullptr;
+    else from = f.bounds + ((REV ? s.end : s.begin) / args.L - 1) * states + mine;
+  }
+#pragma unroll
+  for (int d = 0; d < TD; ++d)
+#pragma unroll
+    for (int t = 0; t < TN; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int row = 16 * d + 4 * q + e, col = n0 + 16 * t + l;
+        st[d][t][e] = from != nullptr && row < f.da && col < wc ? from[(int64_t)row * f.sd + (int64_t)(c0 + col) * f.sn] : 0.f;
+      }
+  const int heads = OUT || REV ? args.per : 1;
+  f32x4 o[TC][TN];
+  for (int64_t at = 0; at < s.end - s.begin; at += C) {
+    const int n = (int)min((int64_t)C, s.end - s.begin - at);
+    const int64_t p0 = REV ? s.end - 1 - at : s.begin + at;
+    for (int h = 0; h < heads; ++h) {
+      const int64_t head = (int64_t)group * args.per + h;
+      const bool new_a = !REV || h == 0, new_b = REV || h == 0;
+      __syncthreads();
+      if (OUT && new_a) stage<T, DA, REV>(s_a, f.a, (REV ? group : head) * f.da * size, f.da, p0, n, args.aligned);
+      if (new_b) {
+        stage<T, DA, REV>(s_b, f.b, (REV ? head : group) * f.da * size, f.da, p0, n, args.aligned);
+        stage<T, DC, REV>(s_c, f.c, ((REV ? head : group) * f.dc + c0) * size, wc, p0, n, args.aligned);
+      }
+      __syncthreads();
+      if constexpr (OUT) {
+        // products a . b of the tiles on and below the diagonal, weighted, to LDS (those above it stay zero)
+        for (int t = wave; t < TC * (TC + 1) / 2; t += 4) {
+          int ti = 0, tj = t;
+          while (tj > ti) tj -= ++ti;
+          f32x4 p = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < KD; ++k) {
+            Op x, y;
+            x.row(s_b + (16 * tj + l) * LA + k * KB, q);
+            y.row(s_a + (16 * ti + l) * LA + k * KB, q);
+            mul(p, x, y);
+          }
+          const int far = 16 * (ti - tj) + l - 4 * q;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[e] = far - e >= 0 ? p[e] * (f.p_scale * s_pow[max(far - e, 0)]) : 0.f;
+          Value* to = s_p + (16 * ti + l) * LP + 16 * tj + 4 * q;
+          // (weights of bf16 rows are rounded as the rows are: to bf16)
+          if constexpr (sizeof(Value) == 2) *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3])};
+          else *reinterpret_cast<f32x4*>(to) = p;
+        }
+        if (new_a) {
+          // what the state before the chunk gives; lane l: row 16 i + l % 16, columns 4 q ..
+#pragma unroll
+          for (int i = 0; i < TC; ++i)
+#pragma unroll
+            for (int t = 0; t < TN; ++t) o[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < KD; ++k) {
+            Op x[TN];
+#pragma unroll
+            for (int t = 0; t < TN; ++t) x[t].state(&st[k * KB / 16][t], TN);
+#pragma unroll
+            for (int i = 0; i < TC; ++i) {
+              Op y;
+              y.row_as_state(s_a + (16 * i + l) * LA + k * KB, q);
+#pragma unroll
+              for (int t = 0; t < TN; ++t) mul(o[i][t], x[t], y);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < TC; ++i) {
+            const float w = s_pow[16 * i + l + (REV ? 0 : 1)];
+#pragma unroll
+            for (int t = 0; t < TN; ++t) o[i][t] *= w;
+          }
+        }
+        __syncthreads();
+      }
+      Op c[KC][TN];
+#pragma unroll
+      for (int k = 0; k < KC; ++k)
+#pragma unroll
+        for (int t = 0; t < TN; ++t) c[k][t].template column<LC>(s_c + k * KB * LC + n0 + 16 * t, q, l);
+      if constexpr (OUT) {
+#pragma unroll
+        for (int i = 0; i < TC; ++i)
+#pragma unroll
+          for (int k = 0; k <= 16 * i / KB; ++k) {
+            Op y;
+            y.row(s_p + (16 * i + l) * LP + k * KB, q);
+#pragma unroll
+            for (int t = 0; t < TN; ++t) mul(o[i][t], c[k][t], y);
+          }
+        if (!REV || h == heads - 1) {
+          const int64_t col0 = (REV ? group : head) * f.dc + c0;
+#pragma unroll
+          for (int i = 0; i < TC; ++i) {
+            const int r = 16 * i + l;
+            if (r >= n) continue;
+            char* to = f.out.p + (REV ? p0 - r : p0 + r) * f.out.ld;
+#pragma unroll
+            for (int t = 0; t < TN; ++t) {
+              const int col = n0 + 16 * t + 4 * q;
+              float v[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[e] = o[i][t][e] * f.out_scale;
+              if (args.aligned && col + 4 <= wc) {
+                Vec<T, 4>::store(to + (col0 + col) * size, v);
+              } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const float one[1] = {v[e]};
+                  if (col + e < wc) Vec<T, 1>::store(to + (col0 + col + e) * size, one);
+                }
+              }
+            }
+          }
+        }
+      }
+      if (REV || h == heads - 1) {
+        // (the last chunk's state is only for who asks for it)
+        const float all = REV && h > 0 ? 1.f : s_pow[n];
+#pragma unroll
+        for (int d = 0; d < TD; ++d)
+#pragma unroll
+          for (int t = 0; t < TN; ++t) st[d][t] *= all;
+#pragma unroll
+        for (int k = 0; k < KC; ++k) {
+          float w[Op::kEach];
+#pragma unroll
+          for (int e = 0; e < Op::kEach; ++e)
+            w[e] = f.u_scale * s_pow[max(n - (REV ? 0 : 1) - (k * KB + Op::index(q, e)), 0)];
+          Op x[TN], rest[TN];
+#pragma unroll
+          for (int t = 0; t < TN; ++t) x[t].weighted(c[k][t], w, rest[t]);
+#pragma unroll
+          for (int d = 0; d < TD; ++d) {
+            Op y;
+            y.template column<LA>(s_b + k * KB * LA + 16 * d, q, l);
+#pragma unroll
+            for (int t = 0; t < TN; ++t) {
+              mul(st[d][t], y, x[t]);
+              if constexpr (Op::kParts > 1) mul(st[d][t], y, rest[t]);
+            }
+          }
+        }
+      }
+    }
+  }
+  float* to = nullptr;
+  if constexpr (!OUT) to = args.sums + number * states + mine;
+  else if (f.end != nullptr && (REV ? s.first : s.last)) to = f.end + s.seq * states + mine;
+  if (to == nullptr) return;
+#pragma unroll
+  for (int d = 0; d < TD; ++d)
+#pragma unroll
+    for (int t = 0; t < TN; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int row = 16 * d + 4 * q + e, col = n0 + 16 * t + l;
+        if (row < f.da && col < wc) to[(int64_t)row * f.sd + (int64_t)(c0 + col) * f.sn] = st[d][t][e];
+      }
+}
+
+template <typename T, int DA, int DC, bool REV, bool OUT>
+__global__ __launch_bounds__(kThreads, 2) void k_linear(Args a, int which) {
+  const Form& f = a.f[which];
+  int64_t at = blockIdx.x;
+  const int slice = (int)(at % a.slices[which]);
+  at /= a.slices[which];
+  sweep<T, DA, DC, REV, OUT>(a, f, at / a.groups, (int)(at % a.groups), slice);
+}
+
+// States at a sequence's boundaries from the sums between them, in place: in order, or backwards.
+template <int V, bool REV>
+__global__ __launch_bounds__(kThreads) void k_linear_chain(Args a, const float* begin) {
+  const int lane = threadIdx.x % kWave;
+  const int64_t slices = (a.state + kThreads * V - 1) / (kThreads * V);
+  int64_t at = blockIdx.x;
+  const int64_t i = (at % slices * kThreads + threadIdx.x) * V;
+  at /= slices;
+  const int group = (int)(at % a.groups);
+  const int64_t number = at / a.groups;
+  Segment s;
+  // one block a sequence: its first boundary's
+  if (!boundary(a, number, lane, s)) return;
+  const int64_t o = a.offsets[s.seq], e = min((int64_t)a.offsets[s.seq + 1], a.N);
+  if (s.begin - o != a.L || i >= a.state) return;
+  const int64_t count = (e - o - 1) / a.L, states = (int64_t)a.groups * a.state;
+  const float g = a.decay[group];
+  const float whole = (float)power(g, a.L), part = (float)power(g, e - o - count * a.L);
+  float* p = a.sums + number * states + group * a.state + i;
+  float v[V] = {};
+  if (begin != nullptr) {
+    Vec<float, V> x;
+    x.load(begin + s.seq * states + group * a.state + i);
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[k] = x.get(k);
+  }
+  constexpr int kAhead = 8;
+  for (int64_t b = 0; b < count; b += kAhead) {
+    Vec<float, V> x[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (b + j < count) x[j].load(p + (REV ? count - 1 - b - j : b + j) * states);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (b + j >= count) break;
+      const float w = REV && b + j == 0 ? part : whole;
+#pragma unroll
+      for (int k = 0; k < V; ++k) v[k] = w * v[k] + x[j].get(k);
+      Vec<float, V>::store(p + (REV ? count - 1 - b - j : b + j) * states, v);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- host
+
+// Segments: as long as it takes for no more than this many blocks of sums, twice as long each time.
+constexpr int64_t kMinLength = 256, kMaxBlocks = 1024;
+int64_t most_bounds(int groups) { return groups >= kMaxBlocks ? 1 : kMaxBlocks / groups; }
+int64_t length_for(int64_t N, int groups) {
+  int64_t L = kMinLength;
+  while (N > 0 && (N - 1) / L > most_bounds(groups)) L *= 2;
+  return L;
+}
+
+int columns_of(int da, int dc) { return da > 128 || dc <= 64 ? 64 : 128; }
+
+template <typename T, bool REV, bool OUT>
+hipError_t go(const Args& a, int which, hipStream_t s) {
+  const Form& f = a.f[which];
+  const int64_t blocks = (OUT ? a.bounds + a.M : a.bounds) * a.groups * a.slices[which];
+  if (blocks == 0) return hipSuccess;
+  const unsigned grid = (unsigned)blocks;
+  const bool wide = columns_of(f.da, f.dc) == 128;
+  if (f.da <= 64) {
+    if (wide) k_linear<T, 64, 128, REV, OUT><<<grid, kThreads, 0, s>>>(a, which);
+    else k_linear<T, 64, 64, REV, OUT><<<grid, kThreads, 0, s>>>(a, which);
+  } else if (f.da <= 128) {
+    if (wide) k_linear<T, 128, 128, REV, OUT><<<grid, kThreads, 0, s>>>(a, which);
+    else k_linear<T, 128, 64, REV, OUT><<<grid, kThreads, 0, s>>>(a, which);
+  } else {
+    k_linear<T, 256, 64, REV, OUT><<<grid, kThreads, 0, s>>>(a, which);
+  }
+  return hipGetLastError();
+}
+
+template <bool REV>
+hipError_t chain(const Args& a, const float* begin, hipStream_t s) {
+  if (a.bounds == 0) return hipSuccess;
+  const bool four = a.state % 4 == 0 && ((uintptr_t)begin & 15u) == 0;
+  const int64_t slices = (a.state + kThreads * (four ? 4 : 1) - 1) / (kThreads * (four ? 4 : 1));
+  const unsigned grid = (unsigned)(a.bounds * a.groups * slices);
+  if (four) k_linear_chain<4, REV><<<grid, kThreads, 0, s>>>(a, begin);
+  else k_linear_chain<1, REV><<<grid, kThreads, 0, s>>>(a, begin);
+  return hipGetLastError();
+}
+
+void add_form(Args& a, int which, const Form& f) {
+  a.f[which] = f;
+  a.slices[which] = (f.dc + columns_of(f.da, f.dc) - 1) / columns_of(f.da, f.dc);
+}
+
+void prepare(const LinLaunch& p, Args& a) {
+  a.N = p.N;
+  a.M = p.M;
+  a.groups = p.groups;
+  a.per = p.heads / p.groups;
+  a.aligned = p.aligned;
+  a.offsets = p.offsets;
+  a.decay = p.decay;
+  a.state = (int64_t)p.dk * p.dv;
+  a.L = length_for(p.N, p.groups);
+  a.bounds = p.N > 0 ? (p.N - 1) / a.L : 0;
+}
+// whether every grid is one (states are taken in pieces of 256 values or more)
+bool fits(const Args& a) {
+  int slices = 1;
+  for (int i = 0; i < 3; ++i) slices = a.slices[i] > slices ? a.slices[i] : slices;
+  return launchable((a.bounds + a.M) * a.groups * slices, kThreads) &&
+         launchable(a.bounds * a.groups * ((a.state + kThreads - 1) / kThreads), kThreads);
+}
+
+template <typename T>
+hipError_t forward(const LinLaunch& p, hipStream_t s) {
+  Args a{};
+  prepare(p, a);
+  a.sums = p.states;
+  add_form(a, 0, Form{p.q, p.k, p.v, p.y, p.states, p.first, p.last, p.dk, p.dv, p.dv, 1, 1.f, 1.f, p.scale});
+  if (!fits(a)) return hipErrorNotSupported;
+  hipError_t e = go<T, false, false>(a, 0, s);
+  if (e == hipSuccess) e = chain<false>(a, p.first, s);
+  if (e == hipSuccess) e = go<T, false, true>(a, 0, s);
+  return e;
+}
+
+template <typename T>
+hipError_t backward(const LinLaunch& p, hipStream_t s) {
+  Args a{};
+  prepare(p, a);
+  a.sums = p.grads;
+  add_form(a, 0, Form{p.k, p.q, p.dy, p.dval, p.grads, p.dlast, p.dfirst, p.dk, p.dv, p.dv, 1, p.scale, p.scale, 1.f});
+  add_form(a, 1, Form{p.v, p.dy, p.q, p.dkey, p.grads, p.dlast, nullptr, p.dv, p.dk, 1, p.dv, p.scale, p.scale, 1.f});
+  add_form(a, 2, Form{p.dy, p.v, p.k, p.dq, p.states, p.first, nullptr, p.dv, p.dk, 1, p.dv, 1.f, 1.f, p.scale});
+  if (!fits(a)) return hipErrorNotSupported;
+  hipError_t e = go<T, true, false>(a, 0, s);
+  if (e == hipSuccess) e = chain<true>(a, p.dlast, s);
+  if (e == hipSuccess) e = go<T, true, true>(a, 0, s);
+  if (e == hipSuccess) e = go<T, true, true>(a, 1, s);
+  if (e == hipSuccess) e = go<T, false, true>(a, 2, s);
+  return e;
+}
+
+}  // namespace
+
+size_t lin_states_bytes(int64_t N, int32_t groups, int32_t dk, int32_t dv) {
+  const int64_t most = most_bounds(groups), need = N > 0 ? (N - 1) / kMinLength : 0;
+  return align256(sizeof(float) * (size_t)(need < most ? need : most) * (size_t)groups * (size_t)dk * (size_t)dv);
+}
+
+hipError_t launch_lin_fwd(const LinLaunch& p, hipStream_t s) {
+  return p.dtype == EMB_FP32 ? forward<float>(p, s) : forward<bf16>(p, s);
+}
+hipError_t launch_lin_bwd(const LinLaunch& p, hipStream_t s) {
+  return p.dtype == EMB_FP32 ? backward<float>(p, s) : backward<bf16>(p, s);
+}
+
+}  // namespace emb

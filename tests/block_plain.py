@@ -89,3 +89,37 @@ def norm_parts(total, weight, eps, dy):
     grad = inv * (gw - n * (gw * n).mean(1, keepdims=True))
     size = inv * (np.abs(gw) + np.abs(n) * np.abs(gw * n).mean(1, keepdims=True))
     return inv, n, grad, size
+
+
+# ---------------------------------------------------------------- linear attention
+
+def linear(offs, q, k, v, decay, scale, first=None):
+    """q [n][g][r][dk], k [n][g][dk], v [n][g][dv]: y [n][g][r][dv], the last states and the state after every position."""
+    n, g, r, dk = q.shape
+    dv, m = v.shape[2], len(offs) - 1
+    y, last, every = np.zeros((n, g, r, dv)), np.zeros((m, g, dk, dv)), np.zeros((n, g, dk, dv))
+    for i in range(m):
+        s = np.zeros((g, dk, dv)) if first is None else first[i].copy()
+        for t in range(offs[i], offs[i + 1]):
+            s = decay[:, None, None] * s + k[t][:, :, None] * v[t][:, None]
+            every[t] = s
+            y[t] = scale * (q[t] @ s)
+        last[i] = s
+    return y, last, every
+
+
+def linear_back(offs, q, k, v, decay, scale, every, dy, dlast=None):
+    """Gradients of q, k, v and the first states."""
+    n, g, r, dk = q.shape
+    dv, m = v.shape[2], len(offs) - 1
+    dq, dkey, dval, dfirst = np.zeros_like(q), np.zeros_like(k), np.zeros_like(v), np.zeros((m, g, dk, dv))
+    for i in range(m):
+        s = np.zeros((g, dk, dv)) if dlast is None else dlast[i].copy()
+        for t in range(offs[i + 1] - 1, offs[i] - 1, -1):
+            s = s + scale * np.swapaxes(q[t], 1, 2) @ dy[t]
+            dq[t] = scale * (dy[t] @ np.swapaxes(every[t], 1, 2))
+            dkey[t] = (s @ v[t][:, :, None])[:, :, 0]
+            dval[t] = (k[t][:, None] @ s)[:, 0]
+            s = decay[:, None, None] * s
+        dfirst[i] = s
+    return dq, dkey, dval, dfirst

@@ -6,7 +6,7 @@ import ctypes
 import pytest
 
 import paper_2112_02752_amd as emb
-from paper_2112_02752_amd.block import CNorm
+from paper_2112_02752_amd.block import CHeads, CNorm
 from paper_2112_02752_amd.sequence import CMat, SAVED8
 
 OK, EINVAL, EWORKSPACE, EUNSUPPORTED = emb.EMB_OK, emb.EMB_EINVAL, emb.EMB_EWORKSPACE, emb.EMB_EUNSUPPORTED
@@ -111,3 +111,75 @@ def test_norm_of_the_binding():
         emb.Norm(torch.ones(8, dtype=torch.bfloat16))
     with pytest.raises(ValueError, match="fp32"):
         emb.Norm(torch.ones(16)[::2])
+
+
+def _heads(n=100, m=3, heads=4, groups=2, dk=16, dv=8, offsets=0x2000, q=None, k=None, v=None, decay=0x3000, scale=1.0,
+           first=None):
+    return CHeads(n, m, heads, groups, dk, dv, offsets, q or _m(), k or _m(), v or _m(), decay, scale, first)
+
+
+BAD_HEADS = [(dict(n=-1), EINVAL), (dict(m=-1), EINVAL), (dict(m=0), EINVAL), (dict(heads=0), EINVAL),
+             (dict(groups=0), EINVAL), (dict(heads=3), EINVAL), (dict(dk=0), EINVAL), (dict(dv=0), EINVAL),
+             (dict(dk=257), EUNSUPPORTED), (dict(dv=257), EUNSUPPORTED), (dict(n=1 << 31), EUNSUPPORTED),
+             (dict(offsets=None), EINVAL), (dict(offsets=0x2002), EINVAL), (dict(decay=None), EINVAL),
+             (dict(decay=0x3001), EINVAL), (dict(first=0x3002), EINVAL), (dict(scale=NAN), EINVAL),
+             (dict(scale=INF), EINVAL), (dict(q=_m(ld=63)), EINVAL), (dict(k=_m(data=None)), EINVAL),
+             (dict(v=_m(dtype=1)), EINVAL), (dict(q=_m(dtype=SAVED8)), EINVAL), (dict(k=_m(data=0x4001)), EINVAL),
+             # more blocks than a grid holds
+             (dict(m=(1 << 31) - 1), EUNSUPPORTED)]
+
+
+def test_linear_attention_refusals():
+    size = emb.lib().emb_linear_states_size
+    assert size(100, 2, 16, 8) == 0 and size(257, 2, 16, 8) == 1024
+    assert size(1 << 30, 2, 16, 8) == 512 * 1024            # segments grow instead
+    for bad in ((-1, 2, 16, 8), (1 << 31, 2, 16, 8), (10, 0, 16, 8), (10, 2, 0, 8), (10, 2, 16, 257)):
+        assert size(*bad) == 0
+
+    def fwd(h=None, y=_m(), last=0x5000, states=0x100000, bytes_=0):
+        return emb.lib().emb_linear_fwd(_ref(h or _heads()), _ref(y), last, states, bytes_, None)
+
+    def bwd(h=None, dy=_m(), dq=_m(), dk=_m(), dv=_m(), states=0x100000, bytes_=0, dlast=0x5000, dfirst=0x6000,
+            ws=0x200000, wsb=0):
+        return emb.lib().emb_linear_bwd(_ref(h or _heads()), states, bytes_, _ref(dy), _ref(dq), _ref(dk), _ref(dv),
+                                        dlast, dfirst, ws, wsb, None)
+
+    for kw, status in BAD_HEADS:
+        assert fwd(_heads(**kw)) == status, kw
+        assert bwd(_heads(**kw)) == status, kw
+    assert emb.lib().emb_linear_fwd(None, None, None, None, 0, None) == EINVAL
+    empty = _heads(n=0, m=0, q=_m(data=None), decay=None)
+    assert fwd(empty, y=None) == OK and bwd(empty, dy=None) == OK
+    assert fwd(y=None) == EINVAL
+    assert fwd(y=_m(ld=31)) == EINVAL
+    assert fwd(y=_m(dtype=1)) == EINVAL
+    assert fwd(last=0x5001) == EINVAL
+    assert fwd(_heads(first=0x5000), last=0x5000) == EINVAL
+    long = _heads(n=257)
+    assert fwd(long, bytes_=1023) == EWORKSPACE
+    assert fwd(long, states=0x100010, bytes_=1024) == EWORKSPACE
+    assert fwd(long, states=None, bytes_=1024) == EINVAL
+    for name in ("dy", "dq", "dk", "dv"):
+        for bad in (None, _m(data=None), _m(ld=15), _m(dtype=1)):
+            assert bwd(**{name: bad}) == EINVAL
+    assert bwd(dlast=0x6000) == EINVAL
+    assert bwd(dfirst=0x6002) == EINVAL
+    assert bwd(long, bytes_=1024) == EWORKSPACE
+    assert bwd(long, wsb=1024) == EWORKSPACE
+    assert bwd(long, bytes_=1024, wsb=1024, ws=0x100000) == EINVAL
+
+
+def test_linear_step_refusals():
+    def call(n=10, heads=4, groups=2, dk=16, dv=8, q=_m(), k=_m(), v=_m(), decay=0x3000, scale=1.0, state=0x5000,
+             num=20, slots=0x6000, y=_m()):
+        return emb.lib().emb_linear_step(n, heads, groups, dk, dv, _ref(q), _ref(k), _ref(v), decay, scale, state, num,
+                                         slots, _ref(y), None)
+
+    assert call(n=0, q=None, state=None) == OK
+    for kw in (dict(n=-1), dict(num=-1), dict(heads=3), dict(groups=0), dict(dk=0), dict(decay=None), dict(state=None),
+               dict(state=0x5001), dict(slots=0x6001), dict(scale=NAN), dict(q=None), dict(k=_m(ld=31)),
+               dict(v=_m(dtype=1)), dict(y=_m(data=None)), dict(y=_m(dtype=SAVED8))):
+        assert call(**kw) == EINVAL, kw
+    assert call(dk=257) == EUNSUPPORTED
+    assert call(n=1 << 31) == EUNSUPPORTED
+    assert call(n=1 << 28) == EUNSUPPORTED                 # more blocks than a grid holds
