@@ -646,6 +646,40 @@ emb_status emb_linear_step(int64_t num_tokens, int32_t heads, int32_t groups, in
                            const emb_mat* k, const emb_mat* v, const float* decay, float scale, float* state,
                            int64_t num_slots, const int32_t* slots, const emb_mat* y, void* stream);
 
+/* Answers: log probabilities of given tokens under every row's distribution
+ * p = softmax(z), z = scale * logits (scale: an inverse temperature above zero):
+ *   logp[r] = log p[ids[r]]          entropy[r] = - sum over v of p_v log p_v
+ * and the `top` largest logits' columns with their log probabilities, from the
+ * largest on, the lowest column first among equal ones (NaN is the largest).
+ * logits: fp32 or bf16, rows of `cols` columns.  An id outside 0 .. cols-1
+ * (usually -1) stands for no token: its logp is 0, and it contributes nothing
+ * to a gradient.  A logit of minus infinity is a token that cannot be; where no
+ * token can, logp and top_logp are minus infinity, entropy and gradient zero.
+ * NaN and plus infinity make their row's results NaN.  Sums are fp32.
+ * ids: device int32 or int64 (id_bytes 4 or 8).  logp, entropy (device fp32
+ * [rows]) may each be NULL, ids with logp.  top 0 .. EMB_MAX_TOP and <= cols;
+ * top_ids (device int32), top_logp (device fp32): [rows][top].  stats: device
+ * fp32, 16-byte aligned, [rows][4] for emb_logp_bwd, or NULL. */
+#define EMB_MAX_TOP 32
+emb_status emb_logp_fwd(int64_t rows, int32_t cols, const emb_mat* logits, const void* ids, int32_t id_bytes,
+                        float scale, float* logp, float* entropy, int32_t top, int32_t* top_ids, float* top_logp,
+                        float* stats, void* stream);
+
+/* Gradient of the logits from those of logp and entropy (device fp32 [rows],
+ * each may be NULL, ids with dlogp), and the forward's stats of the same logits:
+ *   dlogits_v = scale * (dlogp (1[v = id] - p_v) - dentropy p_v (log p_v + entropy))
+ * dlogits: of logits' type; it may be logits' rows. */
+emb_status emb_logp_bwd(int64_t rows, int32_t cols, const emb_mat* logits, const void* ids, int32_t id_bytes,
+                        float scale, const float* stats, const float* dlogp, const float* dentropy,
+                        const emb_mat* dlogits, void* stream);
+
+/* Both in one pass over the logits, where the gradient of logp is known before
+ * (a loss that weighs given tokens): logp, entropy as emb_logp_fwd, dlogits as
+ * emb_logp_bwd of dlogp.  dlogits may be logits' rows. */
+emb_status emb_logp_train(int64_t rows, int32_t cols, const emb_mat* logits, const void* ids, int32_t id_bytes,
+                          float scale, const float* dlogp, float* logp, float* entropy, const emb_mat* dlogits,
+                          void* stream);
+
 const char* emb_status_string(int32_t status);
 
 #ifdef __cplusplus

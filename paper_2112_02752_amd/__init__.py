@@ -34,7 +34,8 @@ EXPORTED = ("emb_pool_fwd", "emb_workspace_size", "emb_workspace_init", "emb_uni
             "emb_token_fwd", "emb_token_grad", "emb_scan_workspace_size", "emb_scan_fwd", "emb_scan_bwd",
             "emb_scan_step", "emb_save", "emb_restore", "emb_weight_grad_workspace_size", "emb_weight_grad",
             "emb_norm_fwd", "emb_norm_workspace_size", "emb_norm_bwd", "emb_dropout",
-            "emb_linear_states_size", "emb_linear_fwd", "emb_linear_bwd", "emb_linear_step")
+            "emb_linear_states_size", "emb_linear_fwd", "emb_linear_bwd", "emb_linear_step",
+            "emb_logp_fwd", "emb_logp_bwd", "emb_logp_train")
 
 
 class EmbError(RuntimeError):
@@ -770,4 +771,4 @@ class Pipeline:
 
 from .sequence import (Checkpoint, Mat, Recurrence, Scan, SequenceLayer, TokenLayer, scan_step,  # noqa: E402
                        scan_workspace_size, token_fwd, token_grad)
-from .block import Heads, LinearAttention, Norm, dropout, linear_attention_step  # noqa: E402
+from .block import Heads, LinearAttention, LogProbs, Norm, dropout, linear_attention_step  # noqa: E402

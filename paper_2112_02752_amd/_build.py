@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libemb.so")
 SOURCES = ["emb_api.hip", "pool_fwd.hip", "dedup.hip", "dedup_small.hip", "reduce.hip", "reduce_wave.hip", "misc.hip", "route.hip", "pipeline.hip",
-           "token.hip", "scan.hip", "saved.hip", "weight_grad.hip", "block_api.hip", "norm.hip", "linear.hip", "linear_step.hip"]
+           "token.hip", "scan.hip", "saved.hip", "weight_grad.hip", "block_api.hip", "norm.hip", "linear.hip", "linear_step.hip", "logprob.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

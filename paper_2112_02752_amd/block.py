@@ -37,7 +37,10 @@ def _declare(L) -> None:
             ("emb_linear_states_size", sz, [i64, i32, i32, i32]),
             ("emb_linear_fwd", i32, [H, M, vp, vp, sz, vp]),
             ("emb_linear_bwd", i32, [H, vp, sz, M, M, M, M, vp, vp, vp, sz, vp]),
-            ("emb_linear_step", i32, [i64, i32, i32, i32, i32, M, M, M, vp, f32, vp, i64, vp, M, vp])):
+            ("emb_linear_step", i32, [i64, i32, i32, i32, i32, M, M, M, vp, f32, vp, i64, vp, M, vp]),
+            ("emb_logp_fwd", i32, [i64, i32, M, vp, i32, f32, vp, vp, i32, vp, vp, vp, vp]),
+            ("emb_logp_bwd", i32, [i64, i32, M, vp, i32, f32, vp, vp, vp, M, vp]),
+            ("emb_logp_train", i32, [i64, i32, M, vp, i32, f32, vp, vp, vp, M, vp])):
         fn = getattr(L, name)
         fn.restype, fn.argtypes = res, args
 
@@ -277,3 +280,89 @@ def linear_attention_step(q, k, v, decay, state, y, heads: int, groups: Optional
     _check("emb_linear_step", lib().emb_linear_step(
         n, heads, groups, dk, dv, q.ref, k.ref, v.ref, _floats(decay, (groups,), "decay"), scale,
         _floats(state, (rows, groups, dk, dv), "state"), rows, sp, y.ref, _stream(stream)))
+
+
+# ---------------------------------------------------------------- answers
+
+MAX_TOP = 32        # EMB_MAX_TOP
+
+
+def _ids(ids, n: int):
+    """Address and bytes of a value of a contiguous int32 or int64 vector of n ids."""
+    if ids.dim() != 1 or ids.numel() != n or ids.is_floating_point() or ids.element_size() not in (4, 8) \
+            or not ids.is_contiguous():
+        raise ValueError(f"ids are a contiguous int32 or int64 vector of {n} values")
+    if not ids.is_cuda:
+        _device(ids, "ids")
+    return ids.data_ptr(), ids.element_size()
+
+
+class LogProbs:
+    """Log probabilities of given tokens under softmax(scale * logits), with the
+    entropy, the ``top`` likeliest tokens and the logits' gradient
+    (emb_logp_fwd), for up to ``max_rows`` rows of ``cols`` logits.  An id outside
+    the columns (usually -1) stands for no token.  ``forward`` leaves what
+    ``backward`` needs of each row here; ``train`` does both in one pass where
+    the gradient of the log probabilities is known before.  Calls of ``forward``
+    and ``backward`` on one object must be ordered."""
+
+    def __init__(self, max_rows: int, cols: int, top: int = 0, scale: float = 1.0, device="cuda"):
+        import torch
+        if cols < 1 or not 0 <= top <= min(cols, MAX_TOP):
+            raise ValueError(f"top is at most {MAX_TOP} and the number of columns")
+        if not 0.0 < scale < float("inf"):
+            raise ValueError("scale is above zero")
+        self.max_rows, self.cols, self.top, self.scale = max_rows, cols, top, scale
+        self.stats = _device(torch.empty((max(1, max_rows), 4), device=device), "a row's statistics")
+        self._stats = self.stats.data_ptr()
+        self._rows = None
+
+    def _take(self, logits, ids):
+        logits = _mat(logits)
+        n = logits.rows
+        _want(logits, n, self.cols, "logits")
+        if n > self.max_rows:
+            raise ValueError("more rows than there is room for")
+        return (logits, n) + (_ids(ids, n) if ids is not None else (None, 4))
+
+    def forward(self, logits, ids, logp, entropy=None, top_ids=None, top_logp=None, stream=None) -> None:
+        """``logp`` and ``entropy`` (fp32 [rows], each may be None, ``ids`` with
+        ``logp``), ``top_ids`` (int32) and ``top_logp`` (fp32) [rows][top]."""
+        import torch
+        logits, n, at, size = self._take(logits, ids)
+        tops = (n, self.top)
+        if self.top > 0:
+            if top_ids is None or top_logp is None:
+                raise ValueError("top alternatives want top_ids and top_logp")
+            if top_ids.shape != tops or top_ids.dtype != torch.int32 or not top_ids.is_contiguous():
+                raise ValueError(f"top_ids is a contiguous int32 tensor of shape {tops}")
+            _device(top_ids, "top_ids")
+        lp, tl = _floats(logp, (n,), "logp"), _floats(top_logp, tops, "top_logp") if self.top > 0 else None
+        self._rows = None
+        _check("emb_logp_fwd", lib().emb_logp_fwd(
+            n, self.cols, logits.ref, at, size, self.scale, lp, _floats(entropy, (n,), "entropy"), self.top,
+            _ptr(top_ids) if self.top > 0 else None, tl, self._stats, _stream(stream)))
+        self._rows = n
+
+    def backward(self, logits, ids, dlogp, dlogits, dentropy=None, stream=None) -> None:
+        """``dlogits`` from the gradients of the last forward's ``logp`` and
+        ``entropy`` (each may be None, ``ids`` with ``dlogp``); ``dlogits`` may be
+        ``logits``."""
+        logits, n, at, size = self._take(logits, ids)
+        if self._rows != n:
+            raise ValueError("backward follows the forward of the same rows")
+        dlogits = _mat(dlogits)
+        _want(dlogits, n, self.cols, "dlogits")
+        _check("emb_logp_bwd", lib().emb_logp_bwd(
+            n, self.cols, logits.ref, at, size, self.scale, self._stats, _floats(dlogp, (n,), "dlogp"),
+            _floats(dentropy, (n,), "dentropy"), dlogits.ref, _stream(stream)))
+
+    def train(self, logits, ids, logp, dlogp, dlogits, entropy=None, stream=None) -> None:
+        """``logp`` (and ``entropy``; each may be None) and the gradient of
+        sum(dlogp * logp) in ``dlogits``, which may be ``logits``."""
+        logits, n, at, size = self._take(logits, ids)
+        dlogits = _mat(dlogits)
+        _want(dlogits, n, self.cols, "dlogits")
+        _check("emb_logp_train", lib().emb_logp_train(
+            n, self.cols, logits.ref, at, size, self.scale, _floats(dlogp, (n,), "dlogp"), _floats(logp, (n,), "logp"),
+            _floats(entropy, (n,), "entropy"), dlogits.ref, _stream(stream)))

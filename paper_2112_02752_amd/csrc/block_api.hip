@@ -103,6 +103,38 @@ emb_status check_states(const LinLaunch& p, const void* at, size_t bytes) {
   return bytes < need || ((uintptr_t)at & 255u) != 0 ? EMB_EWORKSPACE : EMB_OK;
 }
 
+emb_status check_logits(int64_t rows, int32_t cols, const emb_mat* logits, const void* ids, int32_t id_bytes,
+                        float scale, LogpLaunch* p) {
+  if (rows < 0 || cols < 1 || !(scale > 0.f) || isinf(scale)) return EMB_EINVAL;
+  if (id_bytes != 4 && id_bytes != 8) return EMB_EINVAL;
+  if (((uintptr_t)ids & (uintptr_t)(id_bytes - 1)) != 0) return EMB_EINVAL;
+  if (rows > kMaxTokens || cols > kLogpMaxCols) return EMB_EUNSUPPORTED;
+  p->N = rows;
+  p->D = cols;
+  p->scale = scale;
+  p->ids = ids;
+  p->id_bytes = id_bytes;
+  if (rows == 0) return EMB_OK;
+  const emb_status st = check_mat(logits, cols, false);
+  if (st != EMB_OK) return st;
+  p->dtype = logits->dtype;
+  p->logits = rows_of(*logits);
+  return EMB_OK;
+}
+
+emb_status check_dlogits(const emb_mat* dlogits, LogpLaunch* p) {
+  const emb_status st = check_mat(dlogits, p->D, false);
+  if (st != EMB_OK) return st;
+  if (dlogits->dtype != p->dtype) return EMB_EINVAL;
+  p->dlogits = rows_of(*dlogits);
+  // in place: row by row
+  return p->dlogits.p == p->logits.p && p->dlogits.ld != p->logits.ld ? EMB_EINVAL : EMB_OK;
+}
+
+bool words(const void* a, const void* b, const void* c = nullptr) {
+  return (((uintptr_t)a | (uintptr_t)b | (uintptr_t)c) & 3u) == 0;
+}
+
 }  // namespace
 
 extern "C" {
@@ -265,6 +297,59 @@ emb_status emb_linear_step(int64_t num_tokens, int32_t heads, int32_t groups, in
   p.state = state;
   p.slots = slots;
   return hip_status(launch_lin_step(p, (hipStream_t)stream));
+}
+
+emb_status emb_logp_fwd(int64_t rows, int32_t cols, const emb_mat* logits, const void* ids, int32_t id_bytes,
+                        float scale, float* logp, float* entropy, int32_t top, int32_t* top_ids, float* top_logp,
+                        float* stats, void* stream) {
+  LogpLaunch p{};
+  const emb_status st = check_logits(rows, cols, logits, ids, id_bytes, scale, &p);
+  if (st != EMB_OK) return st;
+  if (top < 0 || top > cols) return EMB_EINVAL;
+  if (top > EMB_MAX_TOP) return EMB_EUNSUPPORTED;
+  if (!words(logp, entropy) || !words(top_ids, top_logp) || ((uintptr_t)stats & 15u) != 0) return EMB_EINVAL;
+  if (rows == 0) return EMB_OK;
+  if ((ids == nullptr) != (logp == nullptr)) return EMB_EINVAL;
+  if (top > 0 && (top_ids == nullptr || top_logp == nullptr)) return EMB_EINVAL;
+  p.logp = logp;
+  p.entropy = entropy;
+  p.top = top;
+  p.top_ids = top_ids;
+  p.top_logp = top_logp;
+  p.stats = stats;
+  return hip_status(launch_logp(p, (hipStream_t)stream));
+}
+
+emb_status emb_logp_bwd(int64_t rows, int32_t cols, const emb_mat* logits, const void* ids, int32_t id_bytes,
+                        float scale, const float* stats, const float* dlogp, const float* dentropy,
+                        const emb_mat* dlogits, void* stream) {
+  LogpLaunch p{};
+  emb_status st = check_logits(rows, cols, logits, ids, id_bytes, scale, &p);
+  if (st != EMB_OK) return st;
+  if (!words(dlogp, dentropy) || ((uintptr_t)stats & 15u) != 0) return EMB_EINVAL;
+  if (rows == 0) return EMB_OK;
+  if (stats == nullptr || (ids == nullptr) != (dlogp == nullptr)) return EMB_EINVAL;
+  if ((st = check_dlogits(dlogits, &p)) != EMB_OK) return st;
+  p.stats = const_cast<float*>(stats);
+  p.dlogp = dlogp;
+  p.dentropy = dentropy;
+  return hip_status(launch_logp_bwd(p, (hipStream_t)stream));
+}
+
+emb_status emb_logp_train(int64_t rows, int32_t cols, const emb_mat* logits, const void* ids, int32_t id_bytes,
+                          float scale, const float* dlogp, float* logp, float* entropy, const emb_mat* dlogits,
+                          void* stream) {
+  LogpLaunch p{};
+  emb_status st = check_logits(rows, cols, logits, ids, id_bytes, scale, &p);
+  if (st != EMB_OK) return st;
+  if (!words(dlogp, logp, entropy)) return EMB_EINVAL;
+  if (rows == 0) return EMB_OK;
+  if (ids == nullptr || dlogp == nullptr) return EMB_EINVAL;
+  if ((st = check_dlogits(dlogits, &p)) != EMB_OK) return st;
+  p.dlogp = dlogp;
+  p.logp = logp;
+  p.entropy = entropy;
+  return hip_status(launch_logp(p, (hipStream_t)stream));
 }
 
 }  // extern "C"

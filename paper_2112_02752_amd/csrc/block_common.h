@@ -76,4 +76,23 @@ struct LinStepLaunch {
 };
 hipError_t launch_lin_step(const LinStepLaunch& p, hipStream_t s);
 
+// Statistics of a row of logits that its gradient needs: largest logit, sum of
+// exp(scale (logit - largest)), entropy, one value unused.
+constexpr int kStats = 4;
+constexpr int32_t kLogpMaxCols = 1 << 30;
+struct LogpLaunch {
+  int64_t N;
+  int32_t D, dtype, id_bytes, top;
+  float scale;
+  Rows logits, dlogits;
+  const void* ids;  // or none
+  float *logp, *entropy;  // each may be none
+  int32_t* top_ids;
+  float* top_logp;
+  float* stats;  // forward: or none
+  const float *dlogp, *dentropy;  // each may be none
+};
+hipError_t launch_logp(const LogpLaunch& p, hipStream_t s);       // dlogits: with the gradient
+hipError_t launch_logp_bwd(const LogpLaunch& p, hipStream_t s);
+
 }  // namespace emb

@@ -123,3 +123,32 @@ def linear_back(offs, q, k, v, decay, scale, every, dy, dlast=None):
             s = decay[:, None, None] * s
         dfirst[i] = s
     return dq, dkey, dval, dfirst
+
+
+# ---------------------------------------------------------------- log probabilities
+
+def answers(x, ids, scale, top=0):
+    """Log probabilities of the ids, entropies, all log probabilities, and the top columns of rows of logits."""
+    z = x * scale
+    with np.errstate(invalid="ignore", divide="ignore"):
+        most = z.max(1, keepdims=True)
+        log = most + np.log(np.exp(z - most).sum(1, keepdims=True))
+        every = z - log
+        p = np.exp(every)
+        entropy = -np.where(p > 0, p * every, 0.0).sum(1)
+    real = (ids >= 0) & (ids < x.shape[1])
+    logp = np.where(real, every[np.arange(len(ids)), np.where(real, ids, 0)], 0.0)
+    order = np.argsort(-x, axis=1, kind="stable")[:, :top]
+    return logp, entropy, every, order
+
+
+def answers_back(every, ids, entropy, scale, dlogp, dentropy=None):
+    """Gradient of the logits."""
+    p = np.exp(every)
+    real = (ids >= 0) & (ids < every.shape[1])
+    dl = np.where(real, dlogp, 0.0)
+    dx = -dl[:, None] * p
+    dx[np.arange(len(ids))[real], ids[real]] += dl[real]
+    if dentropy is not None:
+        dx -= dentropy[:, None] * p * (np.where(p > 0, every, 0.0) + entropy[:, None])
+    return scale * dx

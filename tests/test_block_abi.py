@@ -183,3 +183,66 @@ def test_linear_step_refusals():
     assert call(dk=257) == EUNSUPPORTED
     assert call(n=1 << 31) == EUNSUPPORTED
     assert call(n=1 << 28) == EUNSUPPORTED                 # more blocks than a grid holds
+
+
+def test_log_probability_refusals():
+    L = emb.lib()
+
+    def fwd(n=10, d=64, x=_m(), ids=0x1000, size=8, scale=1.0, logp=0x2000, entropy=0x3000, top=2, ti=0x4000, tl=0x5000,
+            stats=0x6000):
+        return L.emb_logp_fwd(n, d, _ref(x), ids, size, scale, logp, entropy, top, ti, tl, stats, None)
+
+    def bwd(n=10, d=64, x=_m(), ids=0x1000, size=8, scale=1.0, stats=0x6000, dlogp=0x2000, dentropy=0x3000,
+            dx=_m(0x8000)):
+        return L.emb_logp_bwd(n, d, _ref(x), ids, size, scale, stats, dlogp, dentropy, _ref(dx), None)
+
+    def train(n=10, d=64, x=_m(), ids=0x1000, size=8, scale=1.0, dlogp=0x2000, logp=None, entropy=None, dx=_m(0x8000)):
+        return L.emb_logp_train(n, d, _ref(x), ids, size, scale, dlogp, logp, entropy, _ref(dx), None)
+
+    for call in (fwd, bwd, train):
+        for kw in (dict(n=-1), dict(d=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=NAN), dict(scale=INF),
+                   dict(size=2), dict(ids=0x1004), dict(ids=0x1002, size=4), dict(x=None), dict(x=_m(ld=63)),
+                   dict(x=_m(dtype=SAVED8)), dict(x=_m(data=0x4002)), dict(ids=None)):
+            assert call(**kw) == EINVAL, (call, kw)
+        assert call(n=1 << 31) == EUNSUPPORTED
+        assert call(d=(1 << 30) + 1, x=_m(ld=1 << 31)) == EUNSUPPORTED
+        assert call(n=0, x=None, ids=None) == OK
+    assert fwd(n=(1 << 31) - 100, d=1 << 20, x=_m(ld=1 << 20)) == EUNSUPPORTED   # more blocks than a grid holds
+    assert bwd(n=(1 << 31) - 100, d=1 << 20, x=_m(ld=1 << 20), dx=_m(0x8000, 1 << 20)) == EUNSUPPORTED
+    for kw in (dict(logp=None), dict(logp=0x2002), dict(entropy=0x3001), dict(top=-1), dict(top=65), dict(ti=None),
+               dict(tl=None), dict(ti=0x4002), dict(stats=0x6004)):
+        assert fwd(**kw) == EINVAL, kw
+    assert fwd(top=33) == EUNSUPPORTED
+    for call in (bwd, train):
+        for kw in (dict(dlogp=None), dict(dlogp=0x2002), dict(dx=None), dict(dx=_m(0x8000, 63)),
+                   dict(dx=_m(0x8000, 64, 1)), dict(dx=_m(0x4000, 65))):
+            assert call(**kw) == EINVAL, (call, kw)
+    assert bwd(stats=None) == EINVAL
+    assert bwd(stats=0x6004) == EINVAL
+
+
+def test_log_probabilities_of_the_binding():
+    for kw in (dict(cols=0), dict(cols=10, top=11), dict(cols=100, top=33), dict(cols=10, top=-1)):
+        with pytest.raises(ValueError, match="top"):
+            emb.LogProbs(4, **kw)
+    for scale in (0.0, -1.0, NAN, INF):
+        with pytest.raises(ValueError, match="scale"):
+            emb.LogProbs(4, 10, scale=scale)
+    with pytest.raises(ValueError, match="GPU"):
+        emb.LogProbs(4, 10, device="cpu")
+
+
+def test_linear_attention_of_the_binding():
+    import torch
+    with pytest.raises(ValueError, match="multiple"):
+        emb.LinearAttention(10, 1, 3, 2, 8, 8)
+    with pytest.raises(ValueError, match="column"):
+        emb.LinearAttention(10, 1, 2, 2, 0, 8)
+    with pytest.raises(ValueError, match="GPU"):
+        emb.LinearAttention(10, 1, 2, 2, 8, 8, device="cpu")
+    for bad in (torch.zeros(3), torch.zeros(3, dtype=torch.int64), torch.zeros((2, 2), dtype=torch.int32),
+                torch.zeros(6, dtype=torch.int32)[::2], torch.zeros(0, dtype=torch.int32)):
+        with pytest.raises(ValueError, match="offsets"):
+            emb.Heads(bad, None, None, None, None, heads=2)
+    with pytest.raises(ValueError, match="GPU"):
+        emb.Heads(torch.zeros(3, dtype=torch.int32), None, None, None, None, heads=2)
