@@ -601,7 +601,8 @@ emb_status emb_dropout(int64_t rows, int32_t dim, float drop, uint64_t seed, int
  * them, but never where they are kept.  An infinity or NaN in a row spoils the
  * results of its sequence from its chunk's first position on (in the
  * backward also those before it).
- * EMB_EUNSUPPORTED for dk or dv above 256. */
+ * EMB_EUNSUPPORTED for dk or dv above 256, and for rows of more than 16 MB from
+ * one to the next. */
 typedef struct {
   int64_t num_tokens; /* N */
   int32_t num_seqs;   /* M */

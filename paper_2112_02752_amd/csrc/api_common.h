@@ -14,6 +14,9 @@ inline emb_status hip_status(hipError_t e) {
 // tokens of one call
 constexpr int64_t kMaxTokens = ((int64_t)1 << 31) - 64 - 1;
 
+// bytes from a row to the next where offsets within a block's rows are 32 bits
+constexpr int64_t kMaxRowBytes = (int64_t)1 << 24;
+
 // a matrix with `cols` columns in use; saved: an 8-bit checkpoint, else fp32 or bf16
 inline emb_status check_mat(const emb_mat* m, int32_t cols, bool saved) {
   if (m == nullptr || m->data == nullptr) return EMB_EINVAL;

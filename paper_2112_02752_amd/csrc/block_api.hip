@@ -27,6 +27,9 @@ emb_status check_drop(float p, uint64_t seed, int64_t first_row, Drop* out) {
   return out->below > 0xffffu ? EMB_EINVAL : EMB_OK;
 }
 
+// (offsets within a chunk's rows are 32 bits)
+bool long_rows(const Rows& r) { return r.ld > kMaxRowBytes; }
+
 // sizes, weights, dropout; the residual stream's type from the first matrix of it that is there
 emb_status check_norm(int64_t rows, int32_t dim, const emb_norm* norm, const emb_mat* x, const emb_mat* const stream[3],
                       NormLaunch* p) {
@@ -92,6 +95,7 @@ emb_status check_heads(const emb_heads* h, LinLaunch* p) {
   p->q = rows_of(h->q);
   p->k = rows_of(h->k);
   p->v = rows_of(h->v);
+  if (long_rows(p->q) || long_rows(p->k) || long_rows(p->v)) return EMB_EUNSUPPORTED;
   const int size = dtype_bytes(p->dtype);
   p->aligned = vectors(p->q) && vectors(p->k) && vectors(p->v) && h->dk * size % 16 == 0 && h->dv * size % 16 == 0;
   return EMB_OK;
@@ -228,6 +232,7 @@ emb_status emb_linear_fwd(const emb_heads* heads, const emb_mat* y, float* last,
     if ((st = check_mat(y, p.heads * p.dv, false)) != EMB_OK) return st;
     if (y->dtype != p.dtype) return EMB_EINVAL;
     p.y = rows_of(*y);
+    if (long_rows(p.y)) return EMB_EUNSUPPORTED;
     p.aligned = p.aligned && vectors(p.y);
   }
   if ((st = check_states(p, states, states_bytes)) != EMB_OK) return st;
@@ -252,6 +257,7 @@ emb_status emb_linear_bwd(const emb_heads* heads, const void* states, size_t sta
       if ((st = check_mat(all[i], cols[i], false)) != EMB_OK) return st;
       if (all[i]->dtype != p.dtype) return EMB_EINVAL;
       *to[i] = rows_of(*all[i]);
+      if (long_rows(*to[i])) return EMB_EUNSUPPORTED;
       p.aligned = p.aligned && vectors(*to[i]);
     }
   }

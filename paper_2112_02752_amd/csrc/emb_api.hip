@@ -131,8 +131,6 @@ emb_status route_prepare(const emb_tables* tables, const emb_batch* batch, int32
 
 // ---- sequences of tokens
 
-constexpr int64_t kMaxRowBytes = (int64_t)1 << 24;
-
 emb_status check_token(const emb_token* t, int64_t R) {
   return t == nullptr || t->pad_row >= R ? EMB_EINVAL : EMB_OK;
 }

@@ -44,7 +44,8 @@ struct Operand;
 // v_mfma 16 x 16 x 32: eight of 32 indexes a lane, 8 q .. 8 q + 7; from a state 4 q + e and 16 + 4 q + e
 template <>
 struct Operand<bf16> {
-  static constexpr int kChunk = 64, kBlock = 32, kPad = 8, kVec = 8;
+  // (rows 16 values apart from whole lines of banks: eight rows' 16 bytes, and a quarter's four rows of 32, are apart)
+  static constexpr int kChunk = 64, kBlock = 32, kPad = 16, kPadP = 8, kVec = 8;
   typedef uint16_t Value;
   bf16x8 v;
   // row `at` (an address in LDS), indexes 0 .. kBlock - 1 of it
@@ -89,7 +90,7 @@ struct Operand<bf16> {
 // v_mfma 16 x 16 x 4, four times: a lane's four of 16 indexes are 4 q .. 4 q + 3, one a time
 template <>
 struct Operand<float> {
-  static constexpr int kChunk = 32, kBlock = 16, kPad = 4, kVec = 4;
+  static constexpr int kChunk = 32, kBlock = 16, kPad = 4, kPadP = 4, kVec = 4;
   typedef float Value;
   f32x4 v;
   __device__ __forceinline__ void row(const Value* at, int q) { v = *reinterpret_cast<const f32x4*>(at + 4 * q); }
@@ -125,6 +126,7 @@ struct Form {
   float* end;           // and ends with, or none
   int32_t da, dc;       // widths of a and b, of c and out
   int32_t sd, sn;       // state: distance of two indexes of b, of c
+  int32_t rev;          // backwards
   float p_scale, u_scale, out_scale;  // of products a . b, of what the state gets, of out
 };
 
@@ -182,52 +184,84 @@ __device__ __forceinline__ bool segment(const Args& a, int64_t number, int lane,
   return true;
 }
 
-// Rows of a chunk into LDS: row r is position p0 + r (REV: p0 - r), `n` of them, `w` columns from byte `at` of a row on;
-// zeros where there are none.
-template <typename T, int W, bool REV>
-__device__ __forceinline__ void stage(typename Operand<T>::Value* lds, const Rows& m, int64_t at, int w, int64_t p0, int n,
-                                      bool aligned) {
-  constexpr int kVec = Operand<T>::kVec, kRow = W / kVec, kLd = W + Operand<T>::kPad;
-  static_assert(Operand<T>::kChunk * kRow % kThreads == 0, "whole rounds");
+// A chunk's rows: offsets are 32 bits from the first of them in memory, and one past the last row's columns reads as zero
+// and is not written, so neither a chunk's last rows nor a head's last columns need a branch and loads stay in flight
+// together.  kNowhere is past any chunk, also with the distance of its rows (below 2^30) added or taken off.
+constexpr uint32_t kNowhere = 0x80000000u;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t from_base(const void* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
+}
+// rows p0 .. p0 + n - 1 (rev: down from p0), `w` columns from byte `at` of a row on; first() is row 0's offset, step() the
+// distance of two rows
+struct Chunk {
+  __amdgpu_buffer_rsrc_t rsrc;
+  int ld, top;
+  __device__ __forceinline__ Chunk(const Rows& m, int64_t at, int w, int size, int64_t p0, int n, bool rev) {
+    const int bytes = (n - 1) * (int)m.ld;
+    rsrc = from_base(m.p + (rev ? p0 - (n - 1) : p0) * m.ld + at, bytes + w * size);
+    ld = rev ? -(int)m.ld : (int)m.ld;
+    top = rev ? bytes : 0;
+  }
+};
+
+// Rows of a chunk on their way to LDS, in 16 bytes a lane, zeros where there are none.
+template <typename T, int W, bool ALIGNED>
+struct Rowset {
+  typedef typename Operand<T>::Value Value;
+  static constexpr int kVec = Operand<T>::kVec, kRow = W / kVec, kLd = W + Operand<T>::kPad;
+  static constexpr int kEach = Operand<T>::kChunk * kRow / kThreads, kApart = kThreads / kRow;
+  static_assert(Operand<T>::kChunk * kRow % kThreads == 0 && kThreads % kRow == 0, "whole rounds");
+  u32x4 v[kEach];
+  __device__ __forceinline__ void load(const Chunk& c, int w) {
+    const int r = threadIdx.x / kRow, col = threadIdx.x % kRow * kVec;
+    const uint32_t off = (uint32_t)(c.top + r * c.ld + col * (int)sizeof(Value));
+    if constexpr (ALIGNED) {
+      const uint32_t at = col < w ? off : kNowhere;
 #pragma unroll
-  for (int i = 0; i < Operand<T>::kChunk * kRow / kThreads; ++i) {
-    const int x = i * kThreads + threadIdx.x, r = x / kRow, col = x % kRow * kVec;
-    u32x4 v = {0u, 0u, 0u, 0u};
-    if (r < n && col < w) {
-      const char* p = m.p + (REV ? p0 - r : p0 + r) * m.ld + at + col * (int)sizeof(typename Operand<T>::Value);
-      if (aligned && col + kVec <= w) {
-        v = *reinterpret_cast<const u32x4*>(p);
-      } else {
-        const auto* e = reinterpret_cast<const typename Operand<T>::Value*>(p);
+      for (int i = 0; i < kEach; ++i)
+        v[i] = __builtin_amdgcn_raw_buffer_load_b128(c.rsrc, at + (uint32_t)(i * kApart * c.ld), 0, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const uint32_t row = off + (uint32_t)(i * kApart * c.ld);
         if constexpr (kVec == 8) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
-            if (col + k < w) v[k / 2] |= (uint32_t)e[k] << (16 * (k % 2));
+          for (int k = 0; k < 8; k += 2) {
+            const uint32_t lo = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(c.rsrc, col + k < w ? row + 2 * k : kNowhere, 0, 0);
+            const uint32_t hi =
+                (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(c.rsrc, col + k + 1 < w ? row + 2 * k + 2 : kNowhere, 0, 0);
+            v[i][k / 2] = lo | hi << 16;
+          }
         } else {
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            if (col + k < w) v[k] = __float_as_uint(e[k]);
+            v[i][k] = __builtin_amdgcn_raw_buffer_load_b32(c.rsrc, col + k < w ? row + 4 * k : kNowhere, 0, 0);
         }
       }
     }
-    *reinterpret_cast<u32x4*>(lds + r * kLd + col) = v;
   }
-}
+  __device__ __forceinline__ void put(Value* lds) const {
+    Value* to = lds + threadIdx.x / kRow * kLd + threadIdx.x % kRow * kVec;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) *reinterpret_cast<u32x4*>(to + i * kApart * kLd) = v[i];
+  }
+};
 
 // DA: widest a and b; DC: columns of c that a block takes.  OUT: the form itself, else the sums of the segment that ends
-// (REV: begins) at a boundary.
-template <typename T, int DA, int DC, bool REV, bool OUT>
+// (backwards: begins) at a boundary.
+template <typename T, int DA, int DC, bool OUT, bool ALIGNED>
 __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t number, int group, int slice) {
   typedef Operand<T> Op;
   typedef typename Op::Value Value;
   constexpr int C = Op::kChunk, KB = Op::kBlock, TC = C / 16, TD = DA / 16, TN = DC / 64, KC = C / KB, KD = DA / KB;
-  constexpr int LA = DA + Op::kPad, LC = DC + Op::kPad, LP = C + Op::kPad;
+  constexpr int LA = DA + Op::kPad, LC = DC + Op::kPad, LP = C + Op::kPadP;
   __shared__ __align__(16) Value s_a[OUT ? C * LA : 1], s_b[C * LA], s_c[C * LC], s_p[OUT ? C * LP : 1];
   __shared__ float s_pow[C + 1];
   const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), l = lane % 16, q = lane / 16;
+  const bool rev = f.rev;
   Segment s;
   if (OUT ? !segment(args, number, lane, s) : !boundary(args, number, lane, s)) return;
-  if (!OUT && !REV) {  // the segment before
+  if (!OUT && !rev) {  // the segment before
     s.end = s.begin;
     s.begin -= args.L;
   }
@@ -236,39 +270,59 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
   if constexpr (OUT) {
     for (int i = threadIdx.x; i < C * LP; i += kThreads) s_p[i] = 0;
   }
-  const int size = sizeof(Value), c0 = slice * DC, wc = min(DC, f.dc - c0), n0 = wave * 16 * TN;
+  constexpr int size = sizeof(Value);
+  const int c0 = slice * DC, wc = min(DC, f.dc - c0), n0 = wave * 16 * TN;
   const int64_t states = (int64_t)args.groups * args.state, mine = (int64_t)group * args.state;
+  const int heads = OUT || rev ? args.per : 1, length = (int)(s.end - s.begin);
+  Rowset<T, DA, ALIGNED> ra, rb;
+  Rowset<T, DC, ALIGNED> rc;
+  auto load = [&](int at, int h) {
+    const int n = min(C, length - at);
+    const int64_t p0 = rev ? s.end - 1 - at : s.begin + at;
+    const int64_t head = (int64_t)group * args.per + h;
+    if (OUT && (!rev || h == 0)) ra.load(Chunk(f.a, (rev ? group : head) * f.da * size, f.da, size, p0, n, rev), f.da);
+    if (rev || h == 0) {
+      rb.load(Chunk(f.b, (rev ? head : group) * f.da * size, f.da, size, p0, n, rev), f.da);
+      rc.load(Chunk(f.c, ((rev ? head : group) * f.dc + c0) * size, wc, size, p0, n, rev), wc);
+    }
+  };
+  if (length > 0) load(0, 0);
   // the state: lane l holds column n0 + 16 t + l % 16, rows 16 d + 4 q ..
-  f32x4 st[TD][TN];
+  auto place = [&](int d, int t, int e) {
+    const int row = 16 * d + 4 * q + e, col = n0 + 16 * t + l;
+    return row < f.da && col < wc ? (uint32_t)(row * f.sd + (c0 + col) * f.sn) * 4u : kNowhere;
+  };
+  f32x4 st[TD][TN] = {};
   const float* from = nullptr;
   if constexpr (OUT) {
-    if (REV ? s.last : s.first) from = f.begin != nullptr ? f.begin + s.seq * states + mine : nullptr;
-    else from = f.bounds + ((REV ? s.end : s.begin) / args.L - 1) * states + mine;
+    if (rev ? s.last : s.first) from = f.begin != nullptr ? f.begin + s.seq * states + mine : nullptr;
+    else from = f.bounds + ((rev ? s.end : s.begin) / args.L - 1) * states + mine;
+    if (from != nullptr) {
+      const auto base = from_base(from, 4 * (int)args.state);
+#pragma unroll
+      for (int d = 0; d < TD; ++d)
+#pragma unroll
+        for (int t = 0; t < TN; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            st[d][t][e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(base, place(d, t, e), 0, 0));
+    }
   }
-#pragma unroll
-  for (int d = 0; d < TD; ++d)
-#pragma unroll
-    for (int t = 0; t < TN; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int row = 16 * d + 4 * q + e, col = n0 + 16 * t + l;
-        st[d][t][e] = from != nullptr && row < f.da && col < wc ? from[(int64_t)row * f.sd + (int64_t)(c0 + col) * f.sn] : 0.f;
-      }
-  const int heads = OUT || REV ? args.per : 1;
   f32x4 o[TC][TN];
-  for (int64_t at = 0; at < s.end - s.begin; at += C) {
-    const int n = (int)min((int64_t)C, s.end - s.begin - at);
-    const int64_t p0 = REV ? s.end - 1 - at : s.begin + at;
+  for (int at = 0; at < length; at += C) {
+    const int n = min(C, length - at);
+    const int64_t p0 = rev ? s.end - 1 - at : s.begin + at;
     for (int h = 0; h < heads; ++h) {
-      const int64_t head = (int64_t)group * args.per + h;
-      const bool new_a = !REV || h == 0, new_b = REV || h == 0;
+      const bool new_a = !rev || h == 0, new_b = rev || h == 0, last = h == heads - 1;
       __syncthreads();
-      if (OUT && new_a) stage<T, DA, REV>(s_a, f.a, (REV ? group : head) * f.da * size, f.da, p0, n, args.aligned);
+      if (OUT && new_a) ra.put(s_a);
       if (new_b) {
-        stage<T, DA, REV>(s_b, f.b, (REV ? head : group) * f.da * size, f.da, p0, n, args.aligned);
-        stage<T, DC, REV>(s_c, f.c, ((REV ? head : group) * f.dc + c0) * size, wc, p0, n, args.aligned);
+        rb.put(s_b);
+        rc.put(s_c);
       }
       __syncthreads();
+      if (!last) load(at, h + 1);
+      else if (at + C < length) load(at + C, 0);
       if constexpr (OUT) {
         // products a . b of the tiles on and below the diagonal, weighted, to LDS (those above it stay zero)
         for (int t = wave; t < TC * (TC + 1) / 2; t += 4) {
@@ -311,7 +365,7 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
           }
 #pragma unroll
           for (int i = 0; i < TC; ++i) {
-            const float w = s_pow[16 * i + l + (REV ? 0 : 1)];
+            const float w = s_pow[16 * i + l + (rev ? 0 : 1)];
 #pragma unroll
             for (int t = 0; t < TN; ++t) o[i][t] *= w;
           }
@@ -333,35 +387,37 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
 #pragma unroll
             for (int t = 0; t < TN; ++t) mul(o[i][t], c[k][t], y);
           }
-        if (!REV || h == heads - 1) {
-          const int64_t col0 = (REV ? group : head) * f.dc + c0;
+        if (!rev || last) {
+          const int64_t col0 = (rev ? (int64_t)group : (int64_t)group * args.per + h) * f.dc + c0;
+          const Chunk out(f.out, col0 * size, wc, size, p0, n, rev);
 #pragma unroll
-          for (int i = 0; i < TC; ++i) {
-            const int r = 16 * i + l;
-            if (r >= n) continue;
-            char* to = f.out.p + (REV ? p0 - r : p0 + r) * f.out.ld;
+          for (int t = 0; t < TN; ++t) {
+            const int col = n0 + 16 * t + 4 * q;
+            const uint32_t row = (uint32_t)(out.top + l * out.ld + col * size);
+            const uint32_t off = col < wc ? row : kNowhere;
 #pragma unroll
-            for (int t = 0; t < TN; ++t) {
-              const int col = n0 + 16 * t + 4 * q;
-              float v[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) v[e] = o[i][t][e] * f.out_scale;
-              if (args.aligned && col + 4 <= wc) {
-                Vec<T, 4>::store(to + (col0 + col) * size, v);
-              } else {
+            for (int i = 0; i < TC; ++i) {
+              const uint32_t to = off + (uint32_t)(16 * i * out.ld);
+              const f32x4 v = o[i][t] * f.out_scale;
+              if constexpr (!ALIGNED) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                  const float one[1] = {v[e]};
-                  if (col + e < wc) Vec<T, 1>::store(to + (col0 + col + e) * size, one);
+                  const uint32_t one = col + e < wc ? to + (uint32_t)(e * size) : kNowhere;
+                  if constexpr (size == 2)
+                    __builtin_amdgcn_raw_buffer_store_b16((uint16_t)pack_bf16(v[e], 0.f), out.rsrc, one, 0, 0);
+                  else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[e]), out.rsrc, one, 0, 0);
                 }
+              } else if constexpr (size == 2) {
+                __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}, out.rsrc, to, 0, 0);
+              } else {
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), out.rsrc, to, 0, 0);
               }
             }
           }
         }
       }
-      if (REV || h == heads - 1) {
-        // (the last chunk's state is only for who asks for it)
-        const float all = REV && h > 0 ? 1.f : s_pow[n];
+      if (rev || last) {
+        const float all = rev && h > 0 ? 1.f : s_pow[n];
 #pragma unroll
         for (int d = 0; d < TD; ++d)
 #pragma unroll
@@ -371,7 +427,7 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
           float w[Op::kEach];
 #pragma unroll
           for (int e = 0; e < Op::kEach; ++e)
-            w[e] = f.u_scale * s_pow[max(n - (REV ? 0 : 1) - (k * KB + Op::index(q, e)), 0)];
+            w[e] = f.u_scale * s_pow[max(n - (rev ? 0 : 1) - (k * KB + Op::index(q, e)), 0)];
           Op x[TN], rest[TN];
 #pragma unroll
           for (int t = 0; t < TN; ++t) x[t].weighted(c[k][t], w, rest[t]);
@@ -391,26 +447,28 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
   }
   float* to = nullptr;
   if constexpr (!OUT) to = args.sums + number * states + mine;
-  else if (f.end != nullptr && (REV ? s.first : s.last)) to = f.end + s.seq * states + mine;
+  else if (f.end != nullptr && (rev ? s.first : s.last)) to = f.end + s.seq * states + mine;
   if (to == nullptr) return;
+  const auto base = from_base(to, 4 * (int)args.state);
 #pragma unroll
   for (int d = 0; d < TD; ++d)
 #pragma unroll
     for (int t = 0; t < TN; ++t)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int row = 16 * d + 4 * q + e, col = n0 + 16 * t + l;
-        if (row < f.da && col < wc) to[(int64_t)row * f.sd + (int64_t)(c0 + col) * f.sn] = st[d][t][e];
-      }
+      for (int e = 0; e < 4; ++e)
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(st[d][t][e]), base, place(d, t, e), 0, 0);
 }
 
-template <typename T, int DA, int DC, bool REV, bool OUT>
-__global__ __launch_bounds__(kThreads, 2) void k_linear(Args a, int which) {
-  const Form& f = a.f[which];
-  int64_t at = blockIdx.x;
-  const int slice = (int)(at % a.slices[which]);
-  at /= a.slices[which];
-  sweep<T, DA, DC, REV, OUT>(a, f, at / a.groups, (int)(at % a.groups), slice);
+// `forms` of the forms from `first` on, which have as many slices each, in one launch
+template <typename T, int DA, int DC, bool OUT, bool ALIGNED>
+__global__ __launch_bounds__(kThreads, DA > 128 ? 1 : 2) void k_linear(Args a, int first, int forms) {
+  uint32_t at = blockIdx.x;
+  const Form& f = a.f[first + (int)(at % (uint32_t)forms)];
+  at /= (uint32_t)forms;
+  const uint32_t slices = (uint32_t)a.slices[first], groups = (uint32_t)a.groups;
+  const int slice = (int)(at % slices);
+  at /= slices;
+  sweep<T, DA, DC, OUT, ALIGNED>(a, f, at / groups, (int)(at % groups), slice);
 }
 
 // States at a sequence's boundaries from the sums between them, in place: in order, or backwards.
@@ -467,25 +525,36 @@ int64_t length_for(int64_t N, int groups) {
   return L;
 }
 
-int columns_of(int da, int dc) { return da > 128 || dc <= 64 ? 64 : 128; }
+// Columns of c that a block takes, and the widest a and b of the kernel that does (rows that are not aligned are for any
+// width up to 128, or to 256).
+int columns_of(const Args& a, int da, int dc) { return !a.aligned || da > 128 || dc <= 64 ? 64 : 128; }
+int width_of(const Args& a, int da) { return da > 128 ? 256 : a.aligned && da <= 64 ? 64 : 128; }
 
-template <typename T, bool REV, bool OUT>
-hipError_t go(const Args& a, int which, hipStream_t s) {
-  const Form& f = a.f[which];
-  const int64_t blocks = (OUT ? a.bounds + a.M : a.bounds) * a.groups * a.slices[which];
+template <typename T, bool OUT>
+hipError_t go(const Args& a, int first, int forms, hipStream_t s) {
+  const Form& f = a.f[first];
+  const int64_t blocks = (OUT ? a.bounds + a.M : a.bounds) * a.groups * a.slices[first] * forms;
   if (blocks == 0) return hipSuccess;
   const unsigned grid = (unsigned)blocks;
-  const bool wide = columns_of(f.da, f.dc) == 128;
-  if (f.da <= 64) {
-    if (wide) k_linear<T, 64, 128, REV, OUT><<<grid, kThreads, 0, s>>>(a, which);
-    else k_linear<T, 64, 64, REV, OUT><<<grid, kThreads, 0, s>>>(a, which);
-  } else if (f.da <= 128) {
-    if (wide) k_linear<T, 128, 128, REV, OUT><<<grid, kThreads, 0, s>>>(a, which);
-    else k_linear<T, 128, 64, REV, OUT><<<grid, kThreads, 0, s>>>(a, which);
+  const int da = width_of(a, f.da), dc = columns_of(a, f.da, f.dc);
+  if (!a.aligned) {
+    if (da == 128) k_linear<T, 128, 64, OUT, false><<<grid, kThreads, 0, s>>>(a, first, forms);
+    else k_linear<T, 256, 64, OUT, false><<<grid, kThreads, 0, s>>>(a, first, forms);
+  } else if (da == 64) {
+    if (dc == 128) k_linear<T, 64, 128, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms);
+    else k_linear<T, 64, 64, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms);
+  } else if (da == 128) {
+    if (dc == 128) k_linear<T, 128, 128, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms);
+    else k_linear<T, 128, 64, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms);
   } else {
-    k_linear<T, 256, 64, REV, OUT><<<grid, kThreads, 0, s>>>(a, which);
+    k_linear<T, 256, 64, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms);
   }
   return hipGetLastError();
+}
+// whether two forms are taken by the same kernel
+bool alike(const Args& a, int i, int j) {
+  return width_of(a, a.f[i].da) == width_of(a, a.f[j].da) &&
+         columns_of(a, a.f[i].da, a.f[i].dc) == columns_of(a, a.f[j].da, a.f[j].dc) && a.slices[i] == a.slices[j];
 }
 
 template <bool REV>
@@ -501,7 +570,7 @@ hipError_t chain(const Args& a, const float* begin, hipStream_t s) {
 
 void add_form(Args& a, int which, const Form& f) {
   a.f[which] = f;
-  a.slices[which] = (f.dc + columns_of(f.da, f.dc) - 1) / columns_of(f.da, f.dc);
+  a.slices[which] = (f.dc + columns_of(a, f.da, f.dc) - 1) / columns_of(a, f.da, f.dc);
 }
 
 void prepare(const LinLaunch& p, Args& a) {
@@ -520,7 +589,7 @@ void prepare(const LinLaunch& p, Args& a) {
 bool fits(const Args& a) {
   int slices = 1;
   for (int i = 0; i < 3; ++i) slices = a.slices[i] > slices ? a.slices[i] : slices;
-  return launchable((a.bounds + a.M) * a.groups * slices, kThreads) &&
+  return launchable((a.bounds + a.M) * a.groups * slices * 3, kThreads) &&
          launchable(a.bounds * a.groups * ((a.state + kThreads - 1) / kThreads), kThreads);
 }
 
@@ -529,11 +598,11 @@ hipError_t forward(const LinLaunch& p, hipStream_t s) {
   Args a{};
   prepare(p, a);
   a.sums = p.states;
-  add_form(a, 0, Form{p.q, p.k, p.v, p.y, p.states, p.first, p.last, p.dk, p.dv, p.dv, 1, 1.f, 1.f, p.scale});
+  add_form(a, 0, Form{p.q, p.k, p.v, p.y, p.states, p.first, p.last, p.dk, p.dv, p.dv, 1, 0, 1.f, 1.f, p.scale});
   if (!fits(a)) return hipErrorNotSupported;
-  hipError_t e = go<T, false, false>(a, 0, s);
+  hipError_t e = go<T, false>(a, 0, 1, s);
   if (e == hipSuccess) e = chain<false>(a, p.first, s);
-  if (e == hipSuccess) e = go<T, false, true>(a, 0, s);
+  if (e == hipSuccess) e = go<T, true>(a, 0, 1, s);
   return e;
 }
 
@@ -542,15 +611,16 @@ hipError_t backward(const LinLaunch& p, hipStream_t s) {
   Args a{};
   prepare(p, a);
   a.sums = p.grads;
-  add_form(a, 0, Form{p.k, p.q, p.dy, p.dval, p.grads, p.dlast, p.dfirst, p.dk, p.dv, p.dv, 1, p.scale, p.scale, 1.f});
-  add_form(a, 1, Form{p.v, p.dy, p.q, p.dkey, p.grads, p.dlast, nullptr, p.dv, p.dk, 1, p.dv, p.scale, p.scale, 1.f});
-  add_form(a, 2, Form{p.dy, p.v, p.k, p.dq, p.states, p.first, nullptr, p.dv, p.dk, 1, p.dv, 1.f, 1.f, p.scale});
+  add_form(a, 0, Form{p.k, p.q, p.dy, p.dval, p.grads, p.dlast, p.dfirst, p.dk, p.dv, p.dv, 1, 1, p.scale, p.scale, 1.f});
+  add_form(a, 1, Form{p.v, p.dy, p.q, p.dkey, p.grads, p.dlast, nullptr, p.dv, p.dk, 1, p.dv, 1, p.scale, p.scale, 1.f});
+  add_form(a, 2, Form{p.dy, p.v, p.k, p.dq, p.states, p.first, nullptr, p.dv, p.dk, 1, p.dv, 0, 1.f, 1.f, p.scale});
   if (!fits(a)) return hipErrorNotSupported;
-  hipError_t e = go<T, true, false>(a, 0, s);
+  hipError_t e = go<T, false>(a, 0, 1, s);
   if (e == hipSuccess) e = chain<true>(a, p.dlast, s);
-  if (e == hipSuccess) e = go<T, true, true>(a, 0, s);
-  if (e == hipSuccess) e = go<T, true, true>(a, 1, s);
-  if (e == hipSuccess) e = go<T, false, true>(a, 2, s);
+  // (dk and dq have the same widths; with dv's too they are one launch, whose last blocks fill the device better)
+  const bool one = alike(a, 0, 1);
+  if (e == hipSuccess) e = go<T, true>(a, 0, one ? 3 : 1, s);
+  if (e == hipSuccess && !one) e = go<T, true>(a, 1, 2, s);
   return e;
 }
 
