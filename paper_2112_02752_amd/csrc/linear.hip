@@ -34,7 +34,7 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256;  // four wavefronts, each a quarter of the columns of c
+constexpr int kThreads = 256;  // of the chain
 
 // What a matrix instruction's operand is made of: lane l holds row (or column)
 // l % 16 and, with q = l / 16, part of a block of kBlock summed indexes.
@@ -44,9 +44,11 @@ struct Operand;
 // v_mfma 16 x 16 x 32: eight of 32 indexes a lane, 8 q .. 8 q + 7; from a state 4 q + e and 16 + 4 q + e
 template <>
 struct Operand<bf16> {
-  // (rows 16 values apart from whole lines of banks: eight rows' 16 bytes, and a quarter's four rows of 32, are apart)
-  static constexpr int kChunk = 64, kBlock = 32, kPad = 16, kPadP = 8, kVec = 8;
+  static constexpr int kChunk = 64, kBlock = 32, kPad = 8, kVec = 8, kParts = 3;
   typedef uint16_t Value;
+  // Distance of rows that are also read by columns: 12 (or 36) words past a multiple of 64 banks, so that 16 rows' 16
+  // bytes as well as four rows' 32 bytes lie apart
+  static constexpr int apart(int w) { return w == 64 ? 72 : w + 24; }
   bf16x8 v;
   // row `at` (an address in LDS), indexes 0 .. kBlock - 1 of it
   __device__ __forceinline__ void row(const Value* at, int q) { v = *reinterpret_cast<const bf16x8*>(at + 8 * q); }
@@ -65,24 +67,26 @@ struct Operand<bf16> {
     v = __builtin_bit_cast(bf16x8, u32x4{a.x, a.y, b.x, b.y});
   }
   // 32 indexes of a state: two tiles
-  __device__ __forceinline__ void state(const f32x4* tiles, int stride) {
-    const f32x4 a = tiles[0], b = tiles[stride];
+  __device__ __forceinline__ void state(f32x4 a, f32x4 b) {
     v = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w)});
   }
-  // this operand times weights, in two parts that hold 16 bits of the products
-  __device__ __forceinline__ void weighted(const Operand& from, const float (&w)[8], Operand& rest) {
+  // an operand times weights, in parts: each the nearest to what the parts before it leave, so three hold all bits
+  static __device__ __forceinline__ void weighted(const Operand& from, const float (&w)[8], Operand (&to)[kParts]) {
     const u32x4 x = __builtin_bit_cast(u32x4, from.v);
-    u32x4 hi, lo;
+    u32x4 r[kParts];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float a = bf16_lo(x[i]) * w[2 * i], b = bf16_hi(x[i]) * w[2 * i + 1];
-      hi[i] = pack_bf16(a, b);
-      lo[i] = pack_bf16(a - bf16_lo(hi[i]), b - bf16_hi(hi[i]));
+      float a = bf16_lo(x[i]) * w[2 * i], b = bf16_hi(x[i]) * w[2 * i + 1];
+#pragma unroll
+      for (int p = 0; p < kParts; ++p) {
+        r[p][i] = pack_bf16(a, b);
+        a -= bf16_lo(r[p][i]);
+        b -= bf16_hi(r[p][i]);
+      }
     }
-    v = __builtin_bit_cast(bf16x8, hi);
-    rest.v = __builtin_bit_cast(bf16x8, lo);
+#pragma unroll
+    for (int p = 0; p < kParts; ++p) to[p].v = __builtin_bit_cast(bf16x8, r[p]);
   }
-  static constexpr int kParts = 2;
   static __device__ __forceinline__ int index(int q, int e) { return 8 * q + e; }
   static constexpr int kEach = 8;
 };
@@ -90,8 +94,9 @@ struct Operand<bf16> {
 // v_mfma 16 x 16 x 4, four times: a lane's four of 16 indexes are 4 q .. 4 q + 3, one a time
 template <>
 struct Operand<float> {
-  static constexpr int kChunk = 32, kBlock = 16, kPad = 4, kPadP = 4, kVec = 4;
+  static constexpr int kChunk = 32, kBlock = 16, kPad = 4, kVec = 4, kParts = 1;
   typedef float Value;
+  static constexpr int apart(int w) { return w + kPad; }
   f32x4 v;
   __device__ __forceinline__ void row(const Value* at, int q) { v = *reinterpret_cast<const f32x4*>(at + 4 * q); }
   __device__ __forceinline__ void row_as_state(const Value* at, int q) { row(at, q); }
@@ -100,12 +105,11 @@ struct Operand<float> {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = at[(4 * q + e) * LD + l];
   }
-  __device__ __forceinline__ void state(const f32x4* tiles, int) { v = tiles[0]; }
-  __device__ __forceinline__ void weighted(const Operand& from, const float (&w)[4], Operand&) {
+  __device__ __forceinline__ void state(f32x4 a, f32x4) { v = a; }
+  static __device__ __forceinline__ void weighted(const Operand& from, const float (&w)[4], Operand (&to)[kParts]) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = from.v[e] * w[e];
+    for (int e = 0; e < 4; ++e) to[0].v[e] = from.v[e] * w[e];
   }
-  static constexpr int kParts = 1;
   static __device__ __forceinline__ int index(int q, int e) { return 4 * q + e; }
   static constexpr int kEach = 4;
 };
@@ -196,21 +200,22 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t from_base(const void* p, int b
 struct Chunk {
   __amdgpu_buffer_rsrc_t rsrc;
   int ld, top;
-  __device__ __forceinline__ Chunk(const Rows& m, int64_t at, int w, int size, int64_t p0, int n, bool rev) {
+  __device__ __forceinline__ Chunk(const Rows& m, int64_t at, int w, int size, int64_t p0, int n, bool rev, bool wanted = true) {
     const int bytes = (n - 1) * (int)m.ld;
-    rsrc = from_base(m.p + (rev ? p0 - (n - 1) : p0) * m.ld + at, bytes + w * size);
+    wanted = wanted && n > 0;
+    rsrc = from_base(m.p + (rev ? p0 - (n - 1) : p0) * m.ld + at, wanted ? bytes + w * size : 0);
     ld = rev ? -(int)m.ld : (int)m.ld;
     top = rev ? bytes : 0;
   }
 };
 
 // Rows of a chunk on their way to LDS, in 16 bytes a lane, zeros where there are none.
-template <typename T, int W, bool ALIGNED>
+template <typename T, int W, int THREADS, bool ALIGNED>
 struct Rowset {
   typedef typename Operand<T>::Value Value;
-  static constexpr int kVec = Operand<T>::kVec, kRow = W / kVec, kLd = W + Operand<T>::kPad;
-  static constexpr int kEach = Operand<T>::kChunk * kRow / kThreads, kApart = kThreads / kRow;
-  static_assert(Operand<T>::kChunk * kRow % kThreads == 0 && kThreads % kRow == 0, "whole rounds");
+  static constexpr int kVec = Operand<T>::kVec, kRow = W / kVec;
+  static constexpr int kEach = Operand<T>::kChunk * kRow / THREADS, kApart = THREADS / kRow;
+  static_assert(Operand<T>::kChunk * kRow % THREADS == 0 && THREADS % kRow == 0, "whole rounds");
   u32x4 v[kEach];
   __device__ __forceinline__ void load(const Chunk& c, int w) {
     const int r = threadIdx.x / kRow, col = threadIdx.x % kRow * kVec;
@@ -240,23 +245,24 @@ struct Rowset {
       }
     }
   }
-  __device__ __forceinline__ void put(Value* lds) const {
-    Value* to = lds + threadIdx.x / kRow * kLd + threadIdx.x % kRow * kVec;
+  __device__ __forceinline__ void put(Value* lds, int ld) const {
+    Value* to = lds + threadIdx.x / kRow * ld + threadIdx.x % kRow * kVec;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) *reinterpret_cast<u32x4*>(to + i * kApart * kLd) = v[i];
+    for (int i = 0; i < kEach; ++i) *reinterpret_cast<u32x4*>(to + i * kApart * ld) = v[i];
   }
 };
 
 // DA: widest a and b; DC: columns of c that a block takes.  OUT: the form itself, else the sums of the segment that ends
 // (backwards: begins) at a boundary.
-template <typename T, int DA, int DC, bool OUT, bool ALIGNED>
+template <typename T, int DA, int DC, int W, bool OUT, bool ALIGNED>
 __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t number, int group, int slice) {
   typedef Operand<T> Op;
   typedef typename Op::Value Value;
-  constexpr int C = Op::kChunk, KB = Op::kBlock, TC = C / 16, TD = DA / 16, TN = DC / 64, KC = C / KB, KD = DA / KB;
-  constexpr int LA = DA + Op::kPad, LC = DC + Op::kPad, LP = C + Op::kPadP;
-  __shared__ __align__(16) Value s_a[OUT ? C * LA : 1], s_b[C * LA], s_c[C * LC], s_p[OUT ? C * LP : 1];
-  __shared__ float s_pow[C + 1];
+  constexpr int C = Op::kChunk, KB = Op::kBlock, TC = C / 16, TD = DA / 16, KC = C / KB, KD = DA / KB;
+  constexpr int kThreads = kWave * W, TN = DC / (16 * W), kTiles = TC * (TC + 1) / 2;
+  constexpr int LA = DA + Op::kPad, LB = Op::apart(DA), LC = Op::apart(DC), LP = C + Op::kPad;
+  __shared__ __align__(16) Value s_a[OUT ? C * LA : 1], s_b[C * LB], s_c[C * LC], s_p[OUT ? C * LP : 1];
+  __shared__ float s_pows[16 + C + 1];  // powers of the decay; zeros where the exponent is negative
   const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), l = lane % 16, q = lane / 16;
   const bool rev = f.rev;
   Segment s;
@@ -266,30 +272,32 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
     s.begin -= args.L;
   }
   const float g = args.decay[group];
-  if (threadIdx.x <= C) s_pow[threadIdx.x] = (float)power(g, threadIdx.x);
+  float* const s_pow = s_pows + 16;
+  if (threadIdx.x < 16 + C + 1) s_pows[threadIdx.x] = threadIdx.x < 16 ? 0.f : (float)power(g, threadIdx.x - 16);
   if constexpr (OUT) {
     for (int i = threadIdx.x; i < C * LP; i += kThreads) s_p[i] = 0;
   }
   constexpr int size = sizeof(Value);
-  const int c0 = slice * DC, wc = min(DC, f.dc - c0), n0 = wave * 16 * TN;
+  const int c0 = slice * DC, wc = min(DC, f.dc - c0), n0 = 16 * TN * wave;
   const int64_t states = (int64_t)args.groups * args.state, mine = (int64_t)group * args.state;
   const int heads = OUT || rev ? args.per : 1, length = (int)(s.end - s.begin);
-  Rowset<T, DA, ALIGNED> ra, rb;
-  Rowset<T, DC, ALIGNED> rc;
+  Rowset<T, DA, kThreads, ALIGNED> ra, rb;
+  Rowset<T, DC, kThreads, ALIGNED> rc;
+  // (rows that a step does not need are loaded from nowhere: a branch around loads would wait for them at its end)
   auto load = [&](int at, int h) {
     const int n = min(C, length - at);
     const int64_t p0 = rev ? s.end - 1 - at : s.begin + at;
     const int64_t head = (int64_t)group * args.per + h;
-    if (OUT && (!rev || h == 0)) ra.load(Chunk(f.a, (rev ? group : head) * f.da * size, f.da, size, p0, n, rev), f.da);
-    if (rev || h == 0) {
-      rb.load(Chunk(f.b, (rev ? head : group) * f.da * size, f.da, size, p0, n, rev), f.da);
-      rc.load(Chunk(f.c, ((rev ? head : group) * f.dc + c0) * size, wc, size, p0, n, rev), wc);
-    }
+    if constexpr (OUT)
+      ra.load(Chunk(f.a, (rev ? group : head) * f.da * size, f.da, size, p0, n, rev, !rev || h == 0), f.da);
+    rb.load(Chunk(f.b, (rev ? head : group) * f.da * size, f.da, size, p0, n, rev, rev || h == 0), f.da);
+    rc.load(Chunk(f.c, ((rev ? head : group) * f.dc + c0) * size, wc, size, p0, n, rev, rev || h == 0), wc);
   };
-  if (length > 0) load(0, 0);
+  load(0, 0);
   // the state: lane l holds column n0 + 16 t + l % 16, rows 16 d + 4 q ..
-  auto place = [&](int d, int t, int e) {
-    const int row = 16 * d + 4 * q + e, col = n0 + 16 * t + l;
+  // (`from_l` is l, in a register of the caller's: the offsets of the first use are not kept for the second)
+  auto place = [&](int from_l, int d, int t, int e) {
+    const int row = 16 * d + 4 * q + e, col = n0 + 16 * t + from_l;
     return row < f.da && col < wc ? (uint32_t)(row * f.sd + (c0 + col) * f.sn) * 4u : kNowhere;
   };
   f32x4 st[TD][TN] = {};
@@ -305,7 +313,7 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
         for (int t = 0; t < TN; ++t)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            st[d][t][e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(base, place(d, t, e), 0, 0));
+            st[d][t][e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(base, place(l, d, t, e), 0, 0));
     }
   }
   f32x4 o[TC][TN];
@@ -314,36 +322,47 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
     const int64_t p0 = rev ? s.end - 1 - at : s.begin + at;
     for (int h = 0; h < heads; ++h) {
       const bool new_a = !rev || h == 0, new_b = rev || h == 0, last = h == heads - 1;
+      // (addresses are made again in every step: kept across it they take the registers that loads are on their way to)
+      int l = lane % 16, q = lane / 16;
+      asm volatile("" : "+v"(l), "+v"(q));
       __syncthreads();
-      if (OUT && new_a) ra.put(s_a);
+      if (OUT && new_a) ra.put(s_a, LA);
       if (new_b) {
-        rb.put(s_b);
-        rc.put(s_c);
+        rb.put(s_b, LB);
+        rc.put(s_c, LC);
       }
       __syncthreads();
-      if (!last) load(at, h + 1);
-      else if (at + C < length) load(at + C, 0);
+      load(last ? at + C : at, last ? 0 : h + 1);
       if constexpr (OUT) {
         // products a . b of the tiles on and below the diagonal, weighted, to LDS (those above it stay zero)
-        for (int t = wave; t < TC * (TC + 1) / 2; t += 4) {
-          int ti = 0, tj = t;
-          while (tj > ti) tj -= ++ti;
+#pragma unroll
+        for (int round = 0; round < (kTiles + W - 1) / W; ++round) {
+          const int t = round * W + wave;
+          if (t >= kTiles) break;
+          __builtin_amdgcn_sched_barrier(0);
+          const int ti = (t >= 1) + (t >= 3) + (t >= 6), tj = t - ti * (ti + 1) / 2;
           f32x4 p = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int k = 0; k < KD; ++k) {
             Op x, y;
-            x.row(s_b + (16 * tj + l) * LA + k * KB, q);
+            x.row(s_b + (16 * tj + l) * LB + k * KB, q);
             y.row(s_a + (16 * ti + l) * LA + k * KB, q);
             mul(p, x, y);
           }
           const int far = 16 * (ti - tj) + l - 4 * q;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) p[e] = far - e >= 0 ? p[e] * (f.p_scale * s_pow[max(far - e, 0)]) : 0.f;
+          for (int e = 0; e < 4; ++e) {
+            float w = s_pow[far - e];
+            asm volatile("" : "+v"(w));  // (read by every lane: no branch)
+            w *= f.p_scale;
+            p[e] = far - e >= 0 ? p[e] * w : 0.f;
+          }
           Value* to = s_p + (16 * ti + l) * LP + 16 * tj + 4 * q;
           // (weights of bf16 rows are rounded as the rows are: to bf16)
           if constexpr (sizeof(Value) == 2) *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3])};
           else *reinterpret_cast<f32x4*>(to) = p;
         }
+        __builtin_amdgcn_sched_barrier(0);
         if (new_a) {
           // what the state before the chunk gives; lane l: row 16 i + l % 16, columns 4 q ..
 #pragma unroll
@@ -354,7 +373,7 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
           for (int k = 0; k < KD; ++k) {
             Op x[TN];
 #pragma unroll
-            for (int t = 0; t < TN; ++t) x[t].state(&st[k * KB / 16][t], TN);
+            for (int t = 0; t < TN; ++t) x[t].state(st[k * KB / 16][t], st[(k * KB / 16 + 1) % TD][t]);
 #pragma unroll
             for (int i = 0; i < TC; ++i) {
               Op y;
@@ -416,6 +435,7 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
           }
         }
       }
+      __builtin_amdgcn_sched_barrier(0);
       if (rev || last) {
         const float all = rev && h > 0 ? 1.f : s_pow[n];
 #pragma unroll
@@ -424,22 +444,22 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
           for (int t = 0; t < TN; ++t) st[d][t] *= all;
 #pragma unroll
         for (int k = 0; k < KC; ++k) {
+          __builtin_amdgcn_sched_barrier(0);
           float w[Op::kEach];
 #pragma unroll
           for (int e = 0; e < Op::kEach; ++e)
             w[e] = f.u_scale * s_pow[max(n - (rev ? 0 : 1) - (k * KB + Op::index(q, e)), 0)];
-          Op x[TN], rest[TN];
+          Op x[TN][Op::kParts];
 #pragma unroll
-          for (int t = 0; t < TN; ++t) x[t].weighted(c[k][t], w, rest[t]);
+          for (int t = 0; t < TN; ++t) Op::weighted(c[k][t], w, x[t]);
 #pragma unroll
           for (int d = 0; d < TD; ++d) {
             Op y;
-            y.template column<LA>(s_b + k * KB * LA + 16 * d, q, l);
+            y.template column<LB>(s_b + k * KB * LB + 16 * d, q, l);
 #pragma unroll
-            for (int t = 0; t < TN; ++t) {
-              mul(st[d][t], y, x[t]);
-              if constexpr (Op::kParts > 1) mul(st[d][t], y, rest[t]);
-            }
+            for (int t = 0; t < TN; ++t)
+#pragma unroll
+              for (int p = 0; p < Op::kParts; ++p) mul(st[d][t], y, x[t][p]);
           }
         }
       }
@@ -449,6 +469,8 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
   if constexpr (!OUT) to = args.sums + number * states + mine;
   else if (f.end != nullptr && (rev ? s.first : s.last)) to = f.end + s.seq * states + mine;
   if (to == nullptr) return;
+  int other = l;
+  asm volatile("" : "+v"(other));
   const auto base = from_base(to, 4 * (int)args.state);
 #pragma unroll
   for (int d = 0; d < TD; ++d)
@@ -456,19 +478,19 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
     for (int t = 0; t < TN; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(st[d][t][e]), base, place(d, t, e), 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(st[d][t][e]), base, place(other, d, t, e), 0, 0);
 }
 
 // `forms` of the forms from `first` on, which have as many slices each, in one launch
-template <typename T, int DA, int DC, bool OUT, bool ALIGNED>
-__global__ __launch_bounds__(kThreads, DA > 128 ? 1 : 2) void k_linear(Args a, int first, int forms) {
+template <typename T, int DA, int DC, int W, bool OUT, bool ALIGNED>
+__global__ __launch_bounds__(kWave* W, DA > 128 ? 1 : 2) void k_linear(Args a, int first, int forms) {
   uint32_t at = blockIdx.x;
   const Form& f = a.f[first + (int)(at % (uint32_t)forms)];
   at /= (uint32_t)forms;
   const uint32_t slices = (uint32_t)a.slices[first], groups = (uint32_t)a.groups;
   const int slice = (int)(at % slices);
   at /= slices;
-  sweep<T, DA, DC, OUT, ALIGNED>(a, f, at / groups, (int)(at % groups), slice);
+  sweep<T, DA, DC, W, OUT, ALIGNED>(a, f, at / groups, (int)(at % groups), slice);
 }
 
 // States at a sequence's boundaries from the sums between them, in place: in order, or backwards.
@@ -538,16 +560,16 @@ hipError_t go(const Args& a, int first, int forms, hipStream_t s) {
   const unsigned grid = (unsigned)blocks;
   const int da = width_of(a, f.da), dc = columns_of(a, f.da, f.dc);
   if (!a.aligned) {
-    if (da == 128) k_linear<T, 128, 64, OUT, false><<<grid, kThreads, 0, s>>>(a, first, forms);
-    else k_linear<T, 256, 64, OUT, false><<<grid, kThreads, 0, s>>>(a, first, forms);
+    if (da == 128) k_linear<T, 128, 64, 4, OUT, false><<<grid, kThreads, 0, s>>>(a, first, forms);
+    else k_linear<T, 256, 64, 4, OUT, false><<<grid, kThreads, 0, s>>>(a, first, forms);
   } else if (da == 64) {
-    if (dc == 128) k_linear<T, 64, 128, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms);
-    else k_linear<T, 64, 64, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms);
+    if (dc == 128) k_linear<T, 64, 128, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms);
+    else k_linear<T, 64, 64, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms);
   } else if (da == 128) {
-    if (dc == 128) k_linear<T, 128, 128, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms);
-    else k_linear<T, 128, 64, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms);
+    if (dc == 128) k_linear<T, 128, 128, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms);
+    else k_linear<T, 128, 64, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms);
   } else {
-    k_linear<T, 256, 64, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms);
+    k_linear<T, 256, 64, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms);
   }
   return hipGetLastError();
 }
