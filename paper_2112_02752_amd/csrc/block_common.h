@@ -76,8 +76,8 @@ struct LinStepLaunch {
 };
 hipError_t launch_lin_step(const LinStepLaunch& p, hipStream_t s);
 
-// Statistics of a row of logits that its gradient needs: largest logit, sum of
-// exp(scale (logit - largest)), entropy, one value unused.
+// Statistics of a row of logits that its gradient needs: the power M of two
+// that it is relative to, sum of 2^(scale log2(e) logit - M), entropy, one value unused.
 constexpr int kStats = 4;
 constexpr int32_t kLogpMaxCols = 1 << 30;
 struct LogpLaunch {
@@ -94,5 +94,31 @@ struct LogpLaunch {
 };
 hipError_t launch_logp(const LogpLaunch& p, hipStream_t s);       // dlogits: with the gradient
 hipError_t launch_logp_bwd(const LogpLaunch& p, hipStream_t s);
+
+// ------------------------------------------------------------ device helpers
+
+// A reduction over the wavefront: within rows of 16 lanes by lane moves that
+// cost no more than the sum itself, then the four rows' (an exchange through
+// LDS would take its latency six times).  Every lane gets the result, the same
+// to the last bit.
+template <int CTRL>
+__device__ __forceinline__ float lane_move(float v) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float lane_at(float v, int l) { return __uint_as_float(lane_at(__float_as_uint(v), l)); }
+template <typename F>
+__device__ __forceinline__ float wave_reduce(float v, F op) {
+  v = op(v, lane_move<0xb1>(v));   // quad_perm:[1,0,3,2]
+  v = op(v, lane_move<0x4e>(v));   // quad_perm:[2,3,0,1]
+  v = op(v, lane_move<0x141>(v));  // row_half_mirror
+  v = op(v, lane_move<0x140>(v));  // row_mirror
+  return op(op(lane_at(v, 0), lane_at(v, 16)), op(lane_at(v, 32), lane_at(v, 48)));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  return wave_reduce(v, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ float wave_max(float v) {
+  return wave_reduce(v, [](float a, float b) { return fmaxf(a, b); });
+}
 
 }  // namespace emb

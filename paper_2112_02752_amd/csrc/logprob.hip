@@ -18,67 +18,48 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLowest = -1e30f;  // in place of minus infinity where a probability of zero multiplies it
+constexpr float kLn2 = 0.69314718055994530942f;
 
-// The vectors of 16 bytes that a row lies in: the first and the last may be shared with its neighbours.
+// A row of D values: whole vectors of 16 bytes where it lies on them, and before the first and after the last of them a
+// few values (less than a vector), which the first 16 lanes take one each.
 template <typename T>
 struct Row {
   static constexpr int kSize = Vec<T, 1>::kBytes, kEach = 16 / kSize;
-  const char* p;  // of the first vector
-  int head;       // columns of it that come before the row's
-  int cols, count;
+  typedef Vec<T, kEach> V;
+  const char* p;  // of the first whole vector
+  int cols, lead, count;  // columns before it, whole vectors
   __device__ __forceinline__ Row(const char* at, int D) {
-    head = (int)(((uintptr_t)at & 15u) / kSize);
-    p = at - head * kSize;
     cols = D;
-    count = (head + D + kEach - 1) / kEach;
+    lead = min((int)(-(intptr_t)at & 15) / kSize, D);
+    count = (D - lead) / kEach;
+    p = at + lead * kSize;
   }
-  // first column of a vector (negative in the first)
-  __device__ __forceinline__ int column(int v) const { return v * kEach - head; }
-  __device__ __forceinline__ bool whole(int v) const { return column(v) >= 0 && column(v) + kEach <= cols; }
-  // minus infinity where there are no columns
-  __device__ __forceinline__ Vec<T, kEach> load(int v) const {
-    Vec<T, kEach> x;
-    if (v < count && whole(v)) {
+  __device__ __forceinline__ int column(int v) const { return lead + v * kEach; }
+  // minus infinity where there is no vector
+  __device__ __forceinline__ V load(int v) const {
+    V x;
+    if (v < count) {
       x.load(p + (int64_t)v * 16);
     } else {
-      float t[kEach];
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        const int c = column(v) + i;
-        Vec<T, 1> one;
-        t[i] = -INFINITY;
-        if (v < count && c >= 0 && c < cols) {
-          one.load(p + (int64_t)v * 16 + i * kSize);
-          t[i] = one.get(0);
-        }
-      }
-      Vec<T, kEach>::store(&x, t);
+      constexpr uint32_t kNone = kSize == 2 ? 0xff80ff80u : 0xff800000u;
+      const u32x4 none = {kNone, kNone, kNone, kNone};
+      x.load(&none);
     }
     return x;
   }
-  __device__ __forceinline__ void store(char* to, int v, const float (&t)[kEach]) const {
-    if (whole(v)) {
-      Vec<T, kEach>::store(to + (int64_t)v * 16, t);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        const float one[1] = {t[i]};
-        if (column(v) + i >= 0 && column(v) + i < cols) Vec<T, 1>::store(to + (int64_t)v * 16 + i * kSize, one);
-      }
-    }
+  // the column of its own that lane t of those that share the row takes, or -1
+  __device__ __forceinline__ int edge(int t) const {
+    if (t < 8) return t < lead ? t : -1;
+    const int c = column(count) + t - 8;
+    return t < 16 && c < cols ? c : -1;
+  }
+  __device__ __forceinline__ const char* at(int c) const { return p + (int64_t)(c - lead) * kSize; }
+  __device__ __forceinline__ float value(int c) const {
+    Vec<T, 1> one;
+    one.load(at(c));
+    return one.get(0);
   }
 };
-
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int k = 1; k < kWave; k *= 2) v = fmaxf(v, __shfl_xor(v, k, kWave));
-  return v;
-}
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int k = 1; k < kWave; k *= 2) v += __shfl_xor(v, k, kWave);
-  return v;
-}
 
 // Order of the alternatives: greater values first (NaN before all, both zeros alike), then lower columns.
 __device__ __forceinline__ uint64_t order_key(float x, int col) {
@@ -105,213 +86,321 @@ __device__ __forceinline__ int64_t id_of(const LogpLaunch& a, int64_t row) {
   return a.id_bytes == 8 ? static_cast<const int64_t*>(a.ids)[row] : (int64_t) static_cast<const int32_t*>(a.ids)[row];
 }
 
-// What a row's gradient is made of: dx_v = p_v (all + slope (z_v - m)) + at the id's column `hot`
+// Exponents are taken to the base of two: with t = scale log2(e) and M = t m, rounded once, a value's power is
+// t x - M in one operation, and its error in M is the same for all of a row, so that it leaves probabilities as they are.
+// Sums of a part of a row, relative to its own M:
+struct Sums {
+  float m, s, a;  // M, sum of 2^(t x - M), sum of 2^(t x - M) (t x - M)
+};
+// the part's M from its largest value: where no token can be, every difference would be NaN
+__device__ __forceinline__ float reference(float t, float top) { return top == -INFINITY ? 0.f : t * top; }
+// x's power, and its share of the sums
+__device__ __forceinline__ void add_value(float x, float t, Sums& p) {
+  const float z = __builtin_fmaf(x, t, -p.m), e = __builtin_amdgcn_exp2f(z);
+  p.s += e;
+  p.a = __builtin_fmaf(e, fmaxf(z, kLowest), p.a);
+}
+__device__ __forceinline__ void refer_to(float m, Sums& p) {
+  const float by = p.m - m, f = __builtin_amdgcn_exp2f(by);
+  p.a = f * (p.a + p.s * by);
+  p.s *= f;
+  p.m = m;
+}
+
+// What a row's gradient is made of: dx_v = e_v (all + slope (t x_v - M)), and at the id's column `hot` more
 struct Slope {
-  float top, c, inv, all, slope, hot;
+  float t, m, all, slope, hot;
   int64_t id;
-  __device__ __forceinline__ Slope(const LogpLaunch& a, int64_t row, float top_, float sum, float entropy) {
+  __device__ __forceinline__ Slope(const LogpLaunch& a, int64_t row, float t_, float m_, float s, float entropy) {
     id = id_of(a, row);
-    const bool real = id >= 0 && id < a.D, none = top_ == -INFINITY;
-    const float dl = real && !none && a.dlogp != nullptr ? a.dlogp[row] : 0.f;
-    const float dh = !none && a.dentropy != nullptr ? a.dentropy[row] : 0.f;
-    // (no token can be: every factor is zero)
-    top = none ? 0.f : top_;
-    c = a.scale;
-    inv = none ? 0.f : 1.f / sum;
-    slope = -a.scale * dh;
-    all = dh != 0.f ? a.scale * (-dl - dh * (entropy - logf(sum))) : -a.scale * dl;
+    t = t_;
+    m = m_;
+    // (where no token can be, every e is zero)
+    const float inv = s == 0.f ? 0.f : a.scale / s;
+    const float dl = id >= 0 && id < a.D && s != 0.f && a.dlogp != nullptr ? a.dlogp[row] : 0.f;
+    const float dh = a.dentropy != nullptr && s != 0.f ? a.dentropy[row] : 0.f;
+    slope = -inv * dh * kLn2;
+    all = dh != 0.f ? inv * (-dl - dh * (entropy - logf(s))) : -inv * dl;
     hot = a.scale * dl;
-    if (!real) id = -1;
   }
-  __device__ __forceinline__ float operator()(float x, int col) const {
-    const float z = c * (x - top), e = __builtin_amdgcn_exp2f(z * kLog2e);
-    const float d = e * inv * (all + slope * fmaxf(z, kLowest));
-    return col == id ? d + hot : d;
+  template <bool ENTROPY>
+  __device__ __forceinline__ float value(float x) const {
+    const float z = __builtin_fmaf(x, t, -m), e = __builtin_amdgcn_exp2f(z);
+    if constexpr (ENTROPY) return e * __builtin_fmaf(slope, fmaxf(z, kLowest), all);
+    return e * all;
   }
 };
 
-// W wavefronts a row, R vectors a lane in registers (0: none, the row is read again).
+// The gradient at lane t's own column
+template <bool ENTROPY, typename T>
+__device__ __forceinline__ void put_edge(const Row<T>& r, const Slope& d, float x, int c, char* to) {
+  if (c < 0) return;
+  const float one[1] = {d.template value<ENTROPY>(x) + (c == d.id ? d.hot : 0.f)};
+  Vec<T, 1>::store(to + (int64_t)c * Row<T>::kSize, one);
+}
+// A vector's gradient; SAME: dlogits lies in vectors as the logits do
+template <bool ENTROPY, bool STREAM, bool SAME, typename T>
+__device__ __forceinline__ void put_grad(const Row<T>& r, const Slope& d, const typename Row<T>::V& x, int v, char* to) {
+  constexpr int E = Row<T>::kEach;
+  if (v >= r.count) return;
+  float g[E];
+#pragma unroll
+  for (int k = 0; k < E; ++k) g[k] = d.template value<ENTROPY>(x.get(k));
+  const int64_t mine = d.id - r.column(v);
+  if (mine >= 0 && mine < E) {
+#pragma unroll
+    for (int k = 0; k < E; ++k) g[k] += k == (int)mine ? d.hot : 0.f;
+  }
+  char* p = to + (int64_t)r.column(v) * Row<T>::kSize;
+  if constexpr (SAME) {
+    if constexpr (STREAM) Vec<T, E>::stream(p, g);
+    else Vec<T, E>::store(p, g);
+  } else {
+    Vec<T, E>::store_each(p, g);
+  }
+}
+
+// W wavefronts a row, R vectors a lane in registers (0: none, the row is read again, and dlogits may lie otherwise).
 template <int W>
 constexpr int kBlock = W <= 4 ? 256 : 64 * W;
+constexpr int kCandidates = 512;  // of a block, for the alternatives
 
-template <typename T, int W, int R>
-__global__ __launch_bounds__(kBlock<W>) void k_logp(LogpLaunch a) {
-  constexpr int kTeam = 64 * W, kRows = kBlock<W> / kTeam, kEach = Row<T>::kEach;
+template <typename T, int W, int R, bool GRAD, bool STREAM>
+__global__ __launch_bounds__(kBlock<W>, R <= 8 ? 8 : 4) void k_logp(LogpLaunch a) {
+  constexpr int kTeam = 64 * W, kRows = kBlock<W> / kTeam, E = Row<T>::kEach, kMost = kCandidates / kRows;
+  typedef typename Row<T>::V V;
   __shared__ float s_part[3][kBlock<W> / kWave];
-  __shared__ uint64_t s_top[kBlock<W> / kWave][EMB_MAX_TOP];
   const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), t = threadIdx.x % kTeam;
   const int64_t row = (int64_t)blockIdx.x * kRows + wave / W;
   if (row >= a.N) return;  // (W > 1: a row a block)
   const Row<T> r(a.logits.p + row * a.logits.ld, a.D);
-  Vec<T, kEach> x[R > 0 ? R : 1];
+  const float base2 = a.scale * kLog2e;
+  V x[R > 0 ? R : 1];
   if constexpr (R > 0) {
 #pragma unroll
     for (int i = 0; i < R; ++i) x[i] = r.load(t + i * kTeam);
   }
+  const int own = r.edge(t);
+  const float own_x = own >= 0 ? r.value(own) : -INFINITY;
+  // every vector of the row; values are taken apart anew by each use (kept, they would take twice the registers)
   auto each = [&](auto f) {
     if constexpr (R > 0) {
 #pragma unroll
-      for (int i = 0; i < R; ++i) f(x[i], t + i * kTeam);
+      for (int i = 0; i < R; ++i) {
+        if constexpr (Row<T>::kSize == 2) asm volatile("" : "+v"(x[i].w[0]), "+v"(x[i].w[1]), "+v"(x[i].w[2]), "+v"(x[i].w[3]));
+        f(x[i], t + i * kTeam);
+      }
     } else {
       for (int v = t; v < r.count; v += kTeam) f(r.load(v), v);
     }
   };
-  float top = -INFINITY;
-  each([&](const Vec<T, kEach>& v, int) {
+  float mine = own_x, most;  // largest of the lane's, of the wavefront's
+  Sums p{0.f, 0.f, 0.f};
+  if constexpr (R > 0) {
+    each([&](const V& v, int) {
 #pragma unroll
-    for (int k = 0; k < kEach; ++k) top = fmaxf(top, v.get(k));
-  });
-  top = wave_max(top);
-  if constexpr (W > 1) {
-    if (lane == 0) s_part[0][wave] = top;
-    __syncthreads();
+      for (int k = 0; k < E; ++k) mine = fmaxf(mine, v.get(k));
+    });
+    most = wave_max(mine);
+    p.m = reference(base2, most);
+    each([&](const V& v, int) {
 #pragma unroll
-    for (int w = 0; w < W; ++w) top = fmaxf(top, s_part[0][w]);
+      for (int k = 0; k < E; ++k) add_value(v.get(k), base2, p);
+    });
+    add_value(own_x, base2, p);
+  } else {
+    // one reading: the lane's sums follow its largest value
+    p.m = reference(base2, mine);
+    add_value(own_x, base2, p);
+    each([&](const V& v, int) {
+      float top = mine;
+#pragma unroll
+      for (int k = 0; k < E; ++k) top = fmaxf(top, v.get(k));
+      if (top > mine) {
+        const float m = reference(base2, top);
+        if (mine == -INFINITY) p.m = m;
+        else refer_to(m, p);
+        mine = top;
+      }
+#pragma unroll
+      for (int k = 0; k < E; ++k) add_value(v.get(k), base2, p);
+    });
+    most = wave_max(mine);
+    if (mine != -INFINITY) refer_to(reference(base2, most), p);
+    p.m = reference(base2, most);
   }
-  // (where no token can be, every difference would be NaN)
-  const float base = top == -INFINITY ? 0.f : top;
-  float sum = 0.f, along = 0.f;
-  each([&](const Vec<T, kEach>& v, int) {
-#pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-      const float z = a.scale * (v.get(k) - base), e = __builtin_amdgcn_exp2f(z * kLog2e);
-      sum += e;
-      along += e * fmaxf(z, kLowest);
-    }
-  });
-  sum = wave_sum(sum);
-  along = wave_sum(along);
+  p.s = wave_sum(p.s);
+  p.a = wave_sum(p.a);
+  float top = most;
   if constexpr (W > 1) {
-    if (lane == 0) s_part[1][wave] = sum, s_part[2][wave] = along;
+    if (lane == 0) s_part[0][wave] = most, s_part[1][wave] = p.s, s_part[2][wave] = p.a;
     __syncthreads();
-    sum = along = 0.f;
-#pragma unroll
-    for (int w = 0; w < W; ++w) sum += s_part[1][w], along += s_part[2][w];
+    // a lane takes a wavefront's sums (where no token can be they are zero, or NaN)
+    const float part = lane < W ? s_part[0][lane] : -INFINITY;
+    Sums o{reference(base2, part), lane < W ? s_part[1][lane] : 0.f, lane < W ? s_part[2][lane] : 0.f};
+    top = wave_max(part);
+    p.m = reference(base2, top);
+    if (part != -INFINITY) refer_to(p.m, o);
+    p.s = wave_sum(o.s);
+    p.a = wave_sum(o.a);
   }
-  if (sum != sum) top = NAN;  // (a largest value passes NaN over)
-  const bool none = top == -INFINITY;
-  const float log_sum = logf(sum), entropy = none ? 0.f : log_sum - along / sum;
+  const float log_sum = logf(p.s), entropy = p.s == 0.f ? 0.f : log_sum - kLn2 * (p.a / p.s);
+  auto log_prob = [&](float v) {
+    return p.s == 0.f ? -INFINITY : __builtin_fmaf(v, base2, -p.m) * kLn2 - log_sum;
+  };
   if (t == 0) {
     const int64_t id = id_of(a, row);
-    if (a.logp != nullptr) {
-      float l = 0.f;
-      if (id >= 0 && id < a.D) {
-        Vec<T, 1> v;
-        v.load(a.logits.p + row * a.logits.ld + id * Row<T>::kSize);
-        l = none ? -INFINITY : a.scale * (v.get(0) - base) - log_sum;
-      }
-      a.logp[row] = l;
-    }
+    if (a.logp != nullptr) a.logp[row] = id >= 0 && id < a.D ? log_prob(r.value((int)id)) : 0.f;
     if (a.entropy != nullptr) a.entropy[row] = entropy;
-    if (a.stats != nullptr) Vec<float, 4>::store(a.stats + row * kStats, {top, sum, entropy, 0.f});
+    if (a.stats != nullptr) Vec<float, 4>::store(a.stats + row * kStats, {p.m, p.s, entropy, 0.f});
   }
-  if (a.dlogits.p != nullptr) {
+  if constexpr (GRAD) {
     // in place: the id's logit is read before it is overwritten
     if constexpr (W > 1) {
       if (a.dlogits.p == a.logits.p) __syncthreads();
     } else {
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    const Slope d(a, row, top, sum, entropy);
+    const Slope d(a, row, base2, p.m, p.s, entropy);
     char* to = a.dlogits.p + row * a.dlogits.ld;
-    const bool same = (((uintptr_t)to ^ (uintptr_t)(a.logits.p + row * a.logits.ld)) & 15u) == 0;
-    each([&](const Vec<T, kEach>& v, int at) {
-      if (at >= r.count) return;
-      float g[kEach];
-#pragma unroll
-      for (int k = 0; k < kEach; ++k) g[k] = d(v.get(k), r.column(at) + k);
-      if (same) {
-        r.store(to - r.head * Row<T>::kSize, at, g);
-      } else {
-#pragma unroll
-        for (int k = 0; k < kEach; ++k) {
-          const float one[1] = {g[k]};
-          const int c = r.column(at) + k;
-          if (c >= 0 && c < a.D) Vec<T, 1>::store(to + (int64_t)c * Row<T>::kSize, one);
-        }
-      }
-    });
+    each([&](const V& v, int at) { put_grad<false, STREAM, (R > 0)>(r, d, v, at, to); });
+    put_edge<false>(r, d, own_x, own, to);
+    return;
   }
   if (a.top == 0) return;
-  // Every wavefront's best, one after another; a lane looks through its columns again when its best has been taken.
-  auto best_below = [&](uint64_t limit) {
-    uint64_t best = 0;
-    each([&](const Vec<T, kEach>& v, int at) {
-#pragma unroll
-      for (int k = 0; k < kEach; ++k) {
-        const int c = r.column(at) + k;
-        if (c < 0 || c >= a.D) continue;
-        const uint64_t key = order_key(v.get(k), c);
-        if (key < limit && key > best) best = key;
-      }
-    });
-    return best;
-  };
-  uint64_t mine = best_below(~0ull);
+  // The alternatives.  A wavefront's lanes have as many largest values as it has lanes: the `top`-th of them is a bound
+  // that at least `top` logits reach, so only those that reach the largest such bound are looked at.
+  __shared__ uint64_t s_list[kRows][kMost];
+  __shared__ int s_count[kRows];
+  const int mate = wave / W;
+  float bound = mine, left = mine;
+  uint64_t alive = ~0ull;
   for (int i = 0; i < a.top; ++i) {
-    const uint64_t best = wave_max_key(mine);  // (0: no column is left)
-    if (lane == 0) s_top[wave][i] = best;
-    if (best != 0 && mine == best) mine = best_below(best);
+    bound = wave_max(left);
+    const uint64_t at = __ballot(left == bound) & alive;
+    if (at == 0) break;  // (all that are left are minus infinity)
+    const int first = __ffsll((unsigned long long)at) - 1;
+    alive &= ~(1ull << first);
+    if (lane == first) left = -INFINITY;
   }
+  if (t == 0) s_count[mate] = 0;
+  if constexpr (W > 1) {
+    __syncthreads();
+    if (lane == 0) s_part[0][wave] = bound;
+    __syncthreads();
+    bound = wave_max(lane < W ? s_part[0][lane] : -INFINITY);
+  } else {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+  // (with NaN in the row every logit is looked at)
+  if (p.s != p.s) bound = NAN;
+  auto look = [&](float v, int c) {
+    if (v < bound) return;
+    const int i = atomicAdd(&s_count[mate], 1);
+    if (i < kMost) s_list[mate][i] = order_key(v, c);
+  };
+  each([&](const V& v, int at) {
+    float best = v.get(0);
+#pragma unroll
+    for (int k = 1; k < E; ++k) best = fmaxf(best, v.get(k));
+    if (best < bound || at >= r.count) return;
+#pragma unroll
+    for (int k = 0; k < E; ++k) look(v.get(k), r.column(at) + k);
+  });
+  if (own >= 0) look(own_x, own);
   auto put = [&](int i, uint64_t key) {
     a.top_ids[row * a.top + i] = (int32_t)~(uint32_t)key;
-    a.top_logp[row * a.top + i] = none ? -INFINITY : a.scale * (key_value(key) - base) - log_sum;
+    a.top_logp[row * a.top + i] = log_prob(key_value(key));
   };
+  if constexpr (W > 1) __syncthreads();
+  else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  const int count = s_count[mate];
+  if (count <= kMost) {
+    // a key's place is the number of greater ones (no two are the same)
+    for (int i = t; i < count; i += kTeam) {
+      const uint64_t key = s_list[mate][i];
+      int before = 0;
+      for (int j = 0; j < count; ++j) before += s_list[mate][j] > key;
+      if (before < a.top) put(before, key);
+    }
+    return;
+  }
+  // Too many reach it (ties, tokens that cannot be, NaN): every wavefront's best one after another; a lane looks through
+  // its columns again, in memory, when its best has been taken.  Then the wavefronts' lists are merged.
+  if constexpr (W > 1) __syncthreads();
+  uint64_t* const list = &s_list[0][0] + wave * EMB_MAX_TOP;
+  static_assert(kBlock<W> / kWave * EMB_MAX_TOP <= kCandidates, "a list for every wavefront");
+  auto best_below = [&](uint64_t limit) {
+    uint64_t best = 0;
+    if (own >= 0) {
+      const uint64_t key = order_key(own_x, own);
+      if (key < limit) best = key;
+    }
+#pragma unroll 1
+    for (int v = t; v < r.count; v += kTeam) {
+      const V w = r.load(v);
+#pragma unroll
+      for (int k = 0; k < E; ++k) {
+        const uint64_t key = order_key(w.get(k), r.column(v) + k);
+        if (key < limit && key > best) best = key;
+      }
+    }
+    return best;
+  };
+  uint64_t next = best_below(~0ull);
+  for (int i = 0; i < a.top; ++i) {
+    const uint64_t best = wave_max_key(next);  // (0: no column is left)
+    if (lane == 0) list[i] = best;
+    if (best != 0 && next == best) next = best_below(best);
+  }
   if constexpr (W > 1) {
     __syncthreads();
     if (wave > 0) return;
-    // the wavefronts' lists, merged
     int taken = 0;
-    uint64_t next = lane < W ? s_top[lane][0] : 0;
+    next = lane < W ? s_list[0][lane * EMB_MAX_TOP] : 0;
     for (int i = 0; i < a.top; ++i) {
       const uint64_t best = wave_max_key(next);
       if (lane == 0) put(i, best);
       if (next == best && lane < W) {
         ++taken;
-        next = taken < a.top ? s_top[lane][taken] : 0;
+        next = taken < a.top ? s_list[0][lane * EMB_MAX_TOP + taken] : 0;
       }
     }
   } else {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    if (lane < a.top) put(lane, s_top[wave][lane]);
+    if (lane < a.top) put(lane, list[lane]);
   }
 }
 
 // The gradient from the forward's statistics: each row's vectors by blocks.
 constexpr int kGradVecs = 4;
-template <typename T>
+template <typename T, bool ENTROPY, bool STREAM, bool SAME>
 __global__ __launch_bounds__(256) void k_logp_bwd(LogpLaunch a, int per) {
-  constexpr int kEach = Row<T>::kEach;
   const int64_t row = blockIdx.x / per;
   const int part = (int)(blockIdx.x % per);
   const Row<T> r(a.logits.p + row * a.logits.ld, a.D);
-  const float* st = a.stats + row * kStats;
-  const Slope d(a, row, st[0], st[1], st[2]);
-  char* to = a.dlogits.p + row * a.dlogits.ld;
-  const bool same = (((uintptr_t)to ^ (uintptr_t)(a.logits.p + row * a.logits.ld)) & 15u) == 0;
-  Vec<T, kEach> x[kGradVecs];
+  typename Row<T>::V x[kGradVecs];
   const int at = part * 256 * kGradVecs + threadIdx.x;
 #pragma unroll
   for (int i = 0; i < kGradVecs; ++i) x[i] = r.load(at + i * 256);
+  const int own = part == 0 ? r.edge(threadIdx.x) : -1;
+  const float own_x = own >= 0 ? r.value(own) : 0.f;
+  const float* st = a.stats + row * kStats;
+  const Slope d(a, row, a.scale * kLog2e, st[0], st[1], st[2]);
+  char* to = a.dlogits.p + row * a.dlogits.ld;
 #pragma unroll
-  for (int i = 0; i < kGradVecs; ++i) {
-    const int v = at + i * 256;
-    if (v >= r.count) break;
-    float g[kEach];
-#pragma unroll
-    for (int k = 0; k < kEach; ++k) g[k] = d(x[i].get(k), r.column(v) + k);
-    if (same) {
-      r.store(to - r.head * Row<T>::kSize, v, g);
-    } else {
-#pragma unroll
-      for (int k = 0; k < kEach; ++k) {
-        const float one[1] = {g[k]};
-        const int c = r.column(v) + k;
-        if (c >= 0 && c < a.D) Vec<T, 1>::store(to + (int64_t)c * Row<T>::kSize, one);
-      }
-    }
-  }
+  for (int i = 0; i < kGradVecs; ++i) put_grad<ENTROPY, STREAM, SAME>(r, d, x[i], at + i * 256, to);
+  put_edge<ENTROPY>(r, d, own_x, own, to);
+}
+
+// whether every row of the gradient lies as the logits' does
+bool alike(const LogpLaunch& p) {
+  return p.dlogits.p == nullptr || ((((uintptr_t)p.dlogits.p ^ (uintptr_t)p.logits.p) & 15u) == 0 &&
+                                    ((p.dlogits.ld ^ p.logits.ld) & 15) == 0);
+}
+// gradients that the L2 caches do not hold are stored past them
+bool streams(const LogpLaunch& p) {
+  return p.N * (int64_t)p.D * (p.dtype == EMB_FP32 ? 4 : 2) > kStreamBytes;
 }
 
 template <typename T, int W, int R>
@@ -319,27 +408,41 @@ hipError_t go(const LogpLaunch& p, hipStream_t s) {
   constexpr int kRows = kBlock<W> / (64 * W);
   const int64_t blocks = (p.N + kRows - 1) / kRows;
   if (!launchable(blocks, kBlock<W>)) return hipErrorNotSupported;
-  k_logp<T, W, R><<<(unsigned)blocks, kBlock<W>, 0, s>>>(p);
+  if (p.dlogits.p == nullptr) k_logp<T, W, R, false, false><<<(unsigned)blocks, kBlock<W>, 0, s>>>(p);
+  else if (streams(p)) k_logp<T, W, R, true, true><<<(unsigned)blocks, kBlock<W>, 0, s>>>(p);
+  else k_logp<T, W, R, true, false><<<(unsigned)blocks, kBlock<W>, 0, s>>>(p);
   return hipGetLastError();
-}
-
-// most vectors a row of D columns lies in
-template <typename T>
-int64_t vectors_of(int32_t D) {
-  constexpr int kEach = Row<T>::kEach;
-  return ((int64_t)D + 2 * (kEach - 1)) / kEach;
 }
 
 template <typename T>
 hipError_t by_width(const LogpLaunch& p, hipStream_t s) {
-  const int64_t n = vectors_of<T>(p.D);
+  const int64_t n = p.D / Row<T>::kEach;  // whole vectors, at most
+  if (!alike(p)) return n <= 512 ? go<T, 1, 0>(p, s) : go<T, 16, 0>(p, s);
   if (n <= 64 * 2) return go<T, 1, 2>(p, s);
   if (n <= 64 * 8) return go<T, 1, 8>(p, s);
   if (n <= 256 * 8) return go<T, 4, 8>(p, s);
   if (n <= 1024 * 4) return go<T, 16, 4>(p, s);
   if (n <= 1024 * 8) return go<T, 16, 8>(p, s);
   if (n <= 1024 * 16) return go<T, 16, 16>(p, s);
+  if (n <= 1024 * 25) return go<T, 16, 25>(p, s);
   return go<T, 16, 0>(p, s);
+}
+
+template <typename T>
+hipError_t back(const LogpLaunch& p, hipStream_t s) {
+  const int64_t n = p.D / Row<T>::kEach, per = n > 0 ? (n + 256 * kGradVecs - 1) / (256 * kGradVecs) : 1;
+  if (!launchable(per * p.N, 256)) return hipErrorNotSupported;
+  const unsigned blocks = (unsigned)(per * p.N);
+  const bool past = streams(p);
+  auto go = [&](auto entropy) {
+    constexpr bool H = decltype(entropy)::value;
+    if (!alike(p)) k_logp_bwd<T, H, false, false><<<blocks, 256, 0, s>>>(p, (int)per);
+    else if (past) k_logp_bwd<T, H, true, true><<<blocks, 256, 0, s>>>(p, (int)per);
+    else k_logp_bwd<T, H, false, true><<<blocks, 256, 0, s>>>(p, (int)per);
+  };
+  if (p.dentropy == nullptr) go(std::false_type{});
+  else go(std::true_type{});
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -349,13 +452,7 @@ hipError_t launch_logp(const LogpLaunch& p, hipStream_t s) {
 }
 
 hipError_t launch_logp_bwd(const LogpLaunch& p, hipStream_t s) {
-  const int64_t n = p.dtype == EMB_FP32 ? vectors_of<float>(p.D) : vectors_of<bf16>(p.D);
-  const int64_t per = (n + 256 * kGradVecs - 1) / (256 * kGradVecs);
-  if (!launchable(per * p.N, 256)) return hipErrorNotSupported;
-  const unsigned blocks = (unsigned)(per * p.N);
-  if (p.dtype == EMB_FP32) k_logp_bwd<float><<<blocks, 256, 0, s>>>(p, (int)per);
-  else k_logp_bwd<bf16><<<blocks, 256, 0, s>>>(p, (int)per);
-  return hipGetLastError();
+  return p.dtype == EMB_FP32 ? back<float>(p, s) : back<bf16>(p, s);
 }
 
 }  // namespace emb

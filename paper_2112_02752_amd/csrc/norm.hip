@@ -82,12 +82,6 @@ __device__ __forceinline__ float held(float v) {
   else return bf16_lo(pack_bf16(v, 0.f));
 }
 
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int k = 1; k < kWave; k *= 2) v += __shfl_xor(v, k, kWave);
-  return v;
-}
-
 // W wavefronts a row, K times eight columns a lane; blocks of kThreads hold whole rows.
 template <int W>
 struct Block {

@@ -4,11 +4,14 @@ hold, odd widths, strides, masked tokens, ties, rows without a target or
 without any token.
 
 Tolerances (u = 2^-24), z' = scale (x - largest x):
- - z' is rounded twice, its product with log2 e once more, the exponential by 2
-   u: e is off by (4 |z'| + 4) u of itself; a sum adds at most 16 * 8 values of a
-   lane (as many of the row as 1024 lanes share, where registers do not hold it), 6
-   exchanges and 16 wavefronts: A = 160 + cols / 1024 roundings.  The logarithm of the
-   sum is then off by B = sum of p (4 |z'| + 8) u + A u, and by 2 u of itself.
+ - z' (to the base of two) is rounded once, as is what it is multiplied with, its
+   reference point is the same for a row, and the exponential is off by 2 u: e is off
+   by (4 |z'| + 4) u of itself; a sum adds at most 16 * 8 values of a lane, 6
+   exchanges and 16 wavefronts, and is referred to another point twice, by 5 u.  Where
+   registers do not hold the row, a lane adds cols / 1024 values and is referred to
+   another point at most once a vector of four (5 u): A = 160 + 2.25 cols / 1024
+   roundings.  The logarithm of the sum is then off by B = sum of p (4 |z'| + 8) u +
+   A u, and by 2 u of itself.
  - the entropy's second sum errs by its terms' (4 |z'| + 8 + 2 A) u.
  - a probability is off by R = (4 |z'| + 16) u + B of itself, and below 2^-126 is zero.
 bf16 gradients are rounded: 2^-8 of them."""
@@ -45,7 +48,7 @@ class Bounds:
             z = np.abs(scale * (x - x.max(1, keepdims=True)))
         self.p = np.exp(every)
         self.z = np.where(self.p > 0, z, 0.0)
-        adds = 160 + x.shape[1] / 1024
+        adds = 160 + 2.25 * x.shape[1] / 1024
         log_sum = np.abs(every.max(1))
         self.log = (self.p * (4 * self.z + 8)).sum(1) * U + adds * U + 2 * U * log_sum
         self.entropy = self.log + (self.p * self.z * (4 * self.z + 8 + 2 * adds)).sum(1) * U + 4 * U * (entropy + log_sum)
@@ -114,9 +117,10 @@ def test_log_probabilities(n, d, gap, shift, kind):
     gone = real & np.isinf(z[at])
     assert np.array_equal(host(logp)[gone], np.full(gone.sum(), -np.inf))
     sure = ~gone
-    within(host(logp)[sure], want[sure], np.where(real, bounds.logp(every[at], z[at]), 0)[sure], "logp")
-    within(entropy, want_h, bounds.entropy, "entropy")
-    assert torch.equal(logp, logp2) and torch.equal(entropy, entropy2)
+    # (gradients that lie otherwise take another variant, whose sums have another order)
+    for l, h, name in ((logp, entropy, "forward"), (logp2, entropy2, "train")):
+        within(host(l)[sure], want[sure], np.where(real, bounds.logp(every[at], z[at]), 0)[sure], f"logp, {name}")
+        within(h, want_h, bounds.entropy, f"entropy, {name}")
     if top:
         assert np.array_equal(top_ids.cpu().numpy(), order)
         rows = np.arange(n)[:, None]
@@ -125,16 +129,16 @@ def test_log_probabilities(n, d, gap, shift, kind):
         assert (got[~some] == -np.inf).all()
         limit = bounds.log[:, None] + 3 * U * np.abs(zl) + 2 * U * np.abs(wl)
         within(got[some], wl[some], limit[some], "top logp")
-    for got, g, name in ((dx, dentropy, "dlogits"), (dx2, None, "dlogits of one pass")):
-        grad = answers_back(every, ids, want_h, f32, dlogp, g)
-        within(got, grad, bounds.grad(ids, dlogp, g) + HALF[kind] * np.abs(grad), name)
-    assert untouched(dx, buf, gap, shift) and untouched(dx2, buf2, gap + 1, shift)
     # in place
     other = x.clone() if gap == 0 else _logits(rng, n, d, kind, gap, shift)[0].copy_(x)
     answer.train(x, dev_ids, None, dl, x)
     answer.backward(other, dev_ids, dl, other, dentropy=dh)
     torch.cuda.synchronize()
-    assert torch.equal(x.contiguous(), dx2.contiguous()) and torch.equal(other.contiguous(), dx.contiguous())
+    for got, g, name in ((dx, dentropy, "dlogits"), (dx2, None, "dlogits of one pass"), (other, dentropy, "in place"),
+                         (x, None, "of one pass in place")):
+        grad = answers_back(every, ids, want_h, f32, dlogp, g)
+        within(got, grad, bounds.grad(ids, dlogp, g) + HALF[kind] * np.abs(grad), name)
+    assert untouched(dx, buf, gap, shift) and untouched(dx2, buf2, gap + 1, shift)
 
 
 @pytest.mark.parametrize("kind", ["fp32", "bf16"])
@@ -169,8 +173,8 @@ def test_rows_of_special_logits(d, kind):
     assert top_ids[0].tolist() == [0, 1, 2, 3] and (top_logp[0] == -inf).all()
     assert logp[1] == 0 and entropy[1] == 0 and (dx[1] == 0).all() and (dx2[1] == 0).all()
     assert top_ids[1].tolist() == [d - 1, 0, 1, 2] and top_logp[1].tolist() == [0, -inf, -inf, -inf]
-    # (adding equal values: 160 + d / 1024 roundings)
-    near = (170 + d / 1024) * U
+    # (adding equal values: 160 + 2.25 d / 1024 roundings)
+    near = (170 + 2.25 * d / 1024) * U
     assert abs(logp[2] + np.log(d)) < near + 2 * U * np.log(d) and abs(entropy[2] - np.log(d)) < near + 2 * U * np.log(d)
     assert top_ids[2].tolist() == [0, 1, 2, 3]
     for i in (3, 4, 5):
