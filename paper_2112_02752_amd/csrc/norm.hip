@@ -72,6 +72,17 @@ __device__ __forceinline__ void store_cols(char* p, int left, bool aligned, cons
     }
   }
 }
+// the same as it lies in memory
+template <typename T>
+__device__ __forceinline__ void load_vec(const char* p, int left, bool aligned, Vec<T, kCols>& x) {
+  if (aligned && left >= kCols) {
+    x.load(p);
+  } else {
+    float t[kCols];
+    load_cols<T>(p, left, false, t);
+    Vec<T, kCols>::store(&x, t);
+  }
+}
 template <typename T>
 constexpr int64_t kSize = Vec<T, 1>::kBytes;
 
@@ -82,10 +93,10 @@ __device__ __forceinline__ float held(float v) {
   else return bf16_lo(pack_bf16(v, 0.f));
 }
 
-// W wavefronts a row, K times eight columns a lane; blocks of kThreads hold whole rows.
+// W wavefronts a row, K times eight columns a lane; a block has one row, or four of a wavefront each.
 template <int W>
 struct Block {
-  static constexpr int kThreads = W <= 4 ? 256 : 64 * W, kRows = kThreads / (64 * W);
+  static constexpr int kThreads = W == 1 ? 256 : 64 * W, kRows = kThreads / (64 * W);
 };
 
 // sums over a row's wavefronts (W > 1: by the whole block)
@@ -167,48 +178,75 @@ __global__ __launch_bounds__(Block<W>::kThreads) void k_norm_fwd(NormLaunch a) {
 
 // Rows are dealt to the blocks in turn; a lane sums its columns of dw over the
 // rows of its wavefront, the block those of its wavefronts, k_norm_dw the blocks'.
-template <typename T, typename R, int W, int K>
+// AHEAD: the next row's values are on their way while a row is worked on, as
+// they lie in memory (of 16 bits each: registers do not hold more).
+template <typename T, typename R, int W, int K, bool AHEAD>
 __global__ __launch_bounds__(Block<W>::kThreads) void k_norm_bwd(NormLaunch a) {
   constexpr int kRows = Block<W>::kRows;
   __shared__ float s_part[2 * W];
   __shared__ float s_dw[kRows > 1 ? (kRows - 1) * K * kWave * kCols : 1];
   const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave);
   const int32_t per = (a.D + 3) / 4;
-  float dw[K][kCols] = {};
-  for (int64_t row = (int64_t)blockIdx.x * kRows + wave / W; row < a.N; row += (int64_t)gridDim.x * kRows) {
-    float t[K][kCols], g[K][kCols], sum[2] = {0.f, 0.f};
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  auto column = [&](int k) { return ((k * W + wave % W) * kWave + lane) * kCols; };
+  float dw[K][kCols] = {}, w[K][kCols];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int col = ((k * W + wave % W) * kWave + lane) * kCols, left = a.D - col;
-      load_cols<R>(a.total.p + row * a.total.ld + col * kSize<R>, left, a.aligned, t[k]);
-      load_cols<T>(a.dy.p + row * a.dy.ld + col * kSize<T>, left, a.aligned, g[k]);
+  for (int k = 0; k < K; ++k) {
+    if (a.weight != nullptr) {
+      load_cols<float>(reinterpret_cast<const char*>(a.weight + column(k)), a.D - column(k), a.aligned, w[k]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kCols; ++i) w[k][i] = 1.f;
     }
+  }
+  struct Loaded {
+    Vec<R, kCols> t[K], arriving[K];
+    Vec<T, kCols> g[K];
+  };
+  auto load = [&](int64_t row, Loaded& x) {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int col = ((k * W + wave % W) * kWave + lane) * kCols, left = a.D - col;
-      float w[kCols];
-      if (a.weight != nullptr) load_cols<float>(reinterpret_cast<const char*>(a.weight + col), left, a.aligned, w);
+      const int col = column(k), left = a.D - col;
+      load_vec<R>(a.total.p + row * a.total.ld + col * kSize<R>, left, a.aligned, x.t[k]);
+      load_vec<T>(a.dy.p + row * a.dy.ld + col * kSize<T>, left, a.aligned, x.g[k]);
+      if (a.arriving.p != nullptr)
+        load_vec<R>(a.arriving.p + row * a.arriving.ld + col * kSize<R>, left, a.aligned, x.arriving[k]);
+    }
+  };
+  int64_t row = (int64_t)blockIdx.x * kRows + wave / W;
+  Loaded x;
+  if constexpr (AHEAD) {
+    if (row < a.N) load(row, x);
+  }
+  for (; row < a.N; row += step) {
+    Loaded next;
+    if constexpr (AHEAD) {
+      if (row + step < a.N) load(row + step, next);
+    } else {
+      load(row, x);
+    }
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int i = 0; i < kCols; ++i) {
-        sum[0] += t[k][i] * t[k][i];
-        sum[1] += t[k][i] * g[k][i] * (a.weight != nullptr ? w[i] : 1.f);
+        const float t = x.t[k].get(i);
+        sum[0] += t * t;
+        sum[1] += t * x.g[k].get(i) * w[k][i];
       }
-    }
     row_sums<W, 2>(sum, s_part);
     const float inv = 1.f / sqrtf(sum[0] / (float)a.D + a.eps);
     const float along = sum[1] * inv / (float)a.D;  // mean(w dy n)
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int col = ((k * W + wave % W) * kWave + lane) * kCols, left = a.D - col;
-      float w[kCols], d[kCols];
-      if (a.weight != nullptr) load_cols<float>(reinterpret_cast<const char*>(a.weight + col), left, a.aligned, w);
-      if (a.arriving.p != nullptr) load_cols<R>(a.arriving.p + row * a.arriving.ld + col * kSize<R>, left, a.aligned, d);
+      const int col = column(k), left = a.D - col;
+      float d[kCols];
 #pragma unroll
       for (int i = 0; i < kCols; ++i) {
-        const float n = t[k][i] * inv;
-        dw[k][i] += g[k][i] * n;
-        const float v = inv * (g[k][i] * (a.weight != nullptr ? w[i] : 1.f) - n * along);
-        d[i] = a.arriving.p != nullptr ? d[i] + v : v;
+        const float n = x.t[k].get(i) * inv, g = x.g[k].get(i);
+        dw[k][i] += g * n;
+        d[i] = inv * (g * w[k][i] - n * along);
+        if (a.arriving.p != nullptr) d[i] += x.arriving[k].get(i);
       }
       if (a.dtotal.p != nullptr) store_cols<R>(a.dtotal.p + row * a.dtotal.ld + col * kSize<R>, left, a.aligned, d);
       if (a.dbranch.p != nullptr) {
@@ -216,6 +254,7 @@ __global__ __launch_bounds__(Block<W>::kThreads) void k_norm_bwd(NormLaunch a) {
         store_cols<T>(a.dbranch.p + row * a.dbranch.ld + col * kSize<T>, left, a.aligned, d);
       }
     }
+    if constexpr (AHEAD) x = next;
   }
   if (a.dweight == nullptr) return;
   if constexpr (kRows > 1) {
@@ -246,8 +285,16 @@ __global__ __launch_bounds__(1024) void k_norm_dw(const float* parts, int count,
   __shared__ float s_sum[16][kWave];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, col = blockIdx.x * kWave + lane;
   float v = 0.f;
-  if (col < D)
-    for (int r = wave; r < count; r += 16) v += parts[(int64_t)r * D + col];
+  constexpr int kAhead = 8;  // loads in flight
+  if (col < D) {
+    for (int r = wave; r < count; r += 16 * kAhead) {
+      float x[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) x[i] = r + 16 * i < count ? parts[(int64_t)(r + 16 * i) * D + col] : 0.f;
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) v += x[i];
+    }
+  }
   s_sum[wave][lane] = v;
   __syncthreads();
   if (wave > 0 || col >= D) return;
@@ -269,10 +316,11 @@ __global__ __launch_bounds__(256) void k_dropout(DropLaunch a) {
   store_cols<T>(a.y.p + row * a.y.ld + col * kSize<T>, left, a.aligned, x);
 }
 
-constexpr int kBwdBlocks = 512;
-int64_t bwd_blocks(int64_t N, int rows) {
-  const int64_t need = (N + rows - 1) / rows;
-  return need < kBwdBlocks ? need : kBwdBlocks;
+// Blocks of the backward: as many rows of dw are left to add.  32768 x 2048 bf16: 140 us with 256, 512 or 1024, and
+// 7, 11 and 26 more for adding them; narrow rows want more wavefronts to have as much in flight.
+int64_t bwd_blocks(int64_t N, int32_t D, int rows) {
+  const int64_t need = (N + rows - 1) / rows, most = D > 2 * kWave * kCols ? 256 : 512;
+  return need < most ? need : most;
 }
 
 template <typename T, typename R, int W, int K>
@@ -284,8 +332,9 @@ hipError_t fwd(const NormLaunch& p, hipStream_t s) {
 }
 template <typename T, typename R, int W, int K>
 hipError_t bwd(const NormLaunch& p, hipStream_t s) {
-  const int64_t blocks = bwd_blocks(p.N, Block<W>::kRows);
-  if (blocks > 0) k_norm_bwd<T, R, W, K><<<(unsigned)blocks, Block<W>::kThreads, 0, s>>>(p);
+  const int64_t blocks = bwd_blocks(p.N, p.D, Block<W>::kRows);
+  constexpr bool kAhead = kSize<T> == 2 && kSize<R> == 2;
+  if (blocks > 0) k_norm_bwd<T, R, W, K, kAhead><<<(unsigned)blocks, Block<W>::kThreads, 0, s>>>(p);
   if (p.dweight != nullptr)
     k_norm_dw<<<(unsigned)((p.D + kWave - 1) / kWave), 1024, 0, s>>>(p.ws, (int)blocks, p.D, p.dweight, p.add);
   return hipGetLastError();
@@ -300,8 +349,10 @@ hipError_t by_width(const NormLaunch& p, hipStream_t s) {
   using std::integral_constant;
   constexpr int kOne = kWave * kCols;
   if (p.D <= kOne) return go(integral_constant<int, 1>{}, integral_constant<int, 1>{});
-  if (p.D <= 2 * kOne) return go(integral_constant<int, 1>{}, integral_constant<int, 2>{});
-  if (p.D <= 4 * kOne) return go(integral_constant<int, 1>{}, integral_constant<int, 4>{});
+  // (forward: more wavefronts with less each, 32768 x 2048 104 us instead of 115; the backward exchanges two sums between
+  // them in every row: 140 either way)
+  if (p.D <= 2 * kOne) return go(integral_constant<int, BACK ? 1 : 2>{}, integral_constant<int, BACK ? 2 : 1>{});
+  if (p.D <= 4 * kOne) return go(integral_constant<int, BACK ? 1 : 4>{}, integral_constant<int, BACK ? 4 : 1>{});
   if (p.D <= 8 * kOne) return go(integral_constant<int, 4>{}, integral_constant<int, 2>{});
   if (p.D <= 16 * kOne) return go(integral_constant<int, 4>{}, integral_constant<int, 4>{});
   return go(integral_constant<int, 8>{}, integral_constant<int, 4>{});
@@ -325,7 +376,7 @@ Drop make_drop(float p, uint64_t seed, int64_t first_row) {
 }
 
 size_t norm_ws_bytes(int64_t N, int32_t D) {
-  return align256(sizeof(float) * (size_t)bwd_blocks(N, 1) * (size_t)D);
+  return align256(sizeof(float) * (size_t)bwd_blocks(N, D, 1) * (size_t)D);
 }
 
 hipError_t launch_norm_fwd(const NormLaunch& p, hipStream_t s) { return by_type<false>(p, s); }

@@ -7,8 +7,8 @@ a lane, 6 exchanges and 8 wavefronts one after another, 46 u of a sum of
 positive numbers, so 1 / root is off by 23 u, and by 4 u more for mean, eps,
 root and reciprocal: y is within 32 u.  The backward's second sum errs by 47 u of its terms'
 magnitudes and what it is multiplied with by 32 u: 96 u of the gradient's parts
-holds both.  A weight gradient adds the rows of a wavefront (one in 512 or
-fewer), 4 wavefronts, 32 blocks' rows and 16 partial sums one after another.
+holds both.  A weight gradient adds the rows of a wavefront (one in 256 or
+more), 4 wavefronts, 32 blocks' rows and 16 partial sums one after another.
 Results are then rounded to their type: half a step."""
 import numpy as np
 import pytest
@@ -83,7 +83,7 @@ def test_norm(n, d, gap, shift, types):
     within(branch_grad, scaled, (off * keep_scale(drop) + (U + HALF[kind]) * np.abs(scaled)) * (scaled != 0), "dbranch")
     assert untouched(dtotal, dbuf, gap, shift) and untouched(branch_grad, bbuf, gap, shift)
     terms = host(dy) * nn
-    depth = n / 512 + 4 + 32 + 16 + 34
+    depth = n / 256 + 4 + 32 + 16 + 34
     within(dw, terms.sum(0), depth * U * np.abs(terms).sum(0), "dweight")
     # added to what is there
     dw2 = torch.full((d,), 3.0, device=DEV)
