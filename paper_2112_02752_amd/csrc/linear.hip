@@ -316,21 +316,23 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
             st[d][t][e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(base, place(l, d, t, e), 0, 0));
     }
   }
+  auto put = [&](int h) {
+    if (OUT && (!rev || h == 0)) ra.put(s_a, LA);
+    if (rev || h == 0) {
+      rb.put(s_b, LB);
+      rc.put(s_c, LC);
+    }
+  };
+  put(0);
   f32x4 o[TC][TN];
   for (int at = 0; at < length; at += C) {
     const int n = min(C, length - at);
     const int64_t p0 = rev ? s.end - 1 - at : s.begin + at;
     for (int h = 0; h < heads; ++h) {
-      const bool new_a = !rev || h == 0, new_b = rev || h == 0, last = h == heads - 1;
+      const bool new_a = !rev || h == 0, last = h == heads - 1;
       // (addresses are made again in every step: kept across it they take the registers that loads are on their way to)
       int l = lane % 16, q = lane / 16;
       asm volatile("" : "+v"(l), "+v"(q));
-      __syncthreads();
-      if (OUT && new_a) ra.put(s_a, LA);
-      if (new_b) {
-        rb.put(s_b, LB);
-        rc.put(s_c, LC);
-      }
       __syncthreads();
       load(last ? at + C : at, last ? 0 : h + 1);
       if constexpr (OUT) {
@@ -406,9 +408,11 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
 #pragma unroll
             for (int t = 0; t < TN; ++t) mul(o[i][t], c[k][t], y);
           }
-        if (!rev || last) {
+        {
+          // (to nowhere where nothing is to be stored yet: as many stores follow the loads in every step, so that the
+          // wait for the loads does not take in the stores)
           const int64_t col0 = (rev ? (int64_t)group : (int64_t)group * args.per + h) * f.dc + c0;
-          const Chunk out(f.out, col0 * size, wc, size, p0, n, rev);
+          const Chunk out(f.out, col0 * size, wc, size, p0, n, rev, !rev || last);
 #pragma unroll
           for (int t = 0; t < TN; ++t) {
             const int col = n0 + 16 * t + 4 * q;
@@ -463,6 +467,8 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
           }
         }
       }
+      __syncthreads();
+      put(last ? 0 : h + 1);
     }
   }
   float* to = nullptr;
