@@ -597,8 +597,9 @@ emb_status emb_dropout(int64_t rows, int32_t dim, float drop, uint64_t seed, int
  * offsets[m] .. offsets[m+1]-1 as in emb_scan; rows from offsets[num_seqs] on
  * are neither read nor written.  Inputs and outputs are of one type, fp32 or bf16.
  * States and sums are fp32; with bf16 rows, weights within a chunk of 64
- * positions and the state are rounded to bf16 where a row is multiplied with
- * them, but never where they are kept.  An infinity or NaN in a row spoils the
+ * positions, and the state and what it gets of a row within a segment, are
+ * rounded to bf16 where rows are multiplied with them, but never where a state
+ * is kept from one segment or call to the next.  An infinity or NaN in a row spoils the
  * results of its sequence from its chunk's first position on (in the
  * backward also those before it).
  * EMB_EUNSUPPORTED for dk or dv above 256, and for rows of more than 16 MB from

@@ -70,22 +70,20 @@ struct Operand<bf16> {
   __device__ __forceinline__ void state(f32x4 a, f32x4 b) {
     v = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w)});
   }
-  // an operand times weights, in parts: each the nearest to what the parts before it leave, so three hold all bits
-  static __device__ __forceinline__ void weighted(const Operand& from, const float (&w)[8], Operand (&to)[kParts]) {
-    const u32x4 x = __builtin_bit_cast(u32x4, from.v);
-    u32x4 r[kParts];
+  __device__ __forceinline__ float get(int e) const {
+    const uint32_t w = __builtin_bit_cast(u32x4, v)[e / 2];
+    return e % 2 ? bf16_hi(w) : bf16_lo(w);
+  }
+  // the nearest to x, which is left with what that leaves of it (three times: nothing)
+  __device__ __forceinline__ void take(float (&x)[8]) {
+    u32x4 w;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      float a = bf16_lo(x[i]) * w[2 * i], b = bf16_hi(x[i]) * w[2 * i + 1];
-#pragma unroll
-      for (int p = 0; p < kParts; ++p) {
-        r[p][i] = pack_bf16(a, b);
-        a -= bf16_lo(r[p][i]);
-        b -= bf16_hi(r[p][i]);
-      }
+      w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+      x[2 * i] -= bf16_lo(w[i]);
+      x[2 * i + 1] -= bf16_hi(w[i]);
     }
-#pragma unroll
-    for (int p = 0; p < kParts; ++p) to[p].v = __builtin_bit_cast(bf16x8, r[p]);
+    v = __builtin_bit_cast(bf16x8, w);
   }
   static __device__ __forceinline__ int index(int q, int e) { return 8 * q + e; }
   static constexpr int kEach = 8;
@@ -106,10 +104,8 @@ struct Operand<float> {
     for (int e = 0; e < 4; ++e) v[e] = at[(4 * q + e) * LD + l];
   }
   __device__ __forceinline__ void state(f32x4 a, f32x4) { v = a; }
-  static __device__ __forceinline__ void weighted(const Operand& from, const float (&w)[4], Operand (&to)[kParts]) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) to[0].v[e] = from.v[e] * w[e];
-  }
+  __device__ __forceinline__ float get(int e) const { return v[e]; }
+  __device__ __forceinline__ void take(const float (&x)[4]) { v = f32x4{x[0], x[1], x[2], x[3]}; }
   static __device__ __forceinline__ int index(int q, int e) { return 4 * q + e; }
   static constexpr int kEach = 4;
 };
@@ -195,17 +191,16 @@ constexpr uint32_t kNowhere = 0x80000000u;
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t from_base(const void* p, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
 }
-// rows p0 .. p0 + n - 1 (rev: down from p0), `w` columns from byte `at` of a row on; first() is row 0's offset, step() the
-// distance of two rows
+// `n` rows from `row` on, which a step takes in order or (rev) from the last one up; `top` is its first one's offset, `ld`
+// the distance of two.
 struct Chunk {
   __amdgpu_buffer_rsrc_t rsrc;
   int ld, top;
-  __device__ __forceinline__ Chunk(const Rows& m, int64_t at, int w, int size, int64_t p0, int n, bool rev, bool wanted = true) {
-    const int bytes = (n - 1) * (int)m.ld;
-    wanted = wanted && n > 0;
-    rsrc = from_base(m.p + (rev ? p0 - (n - 1) : p0) * m.ld + at, wanted ? bytes + w * size : 0);
-    ld = rev ? -(int)m.ld : (int)m.ld;
-    top = rev ? bytes : 0;
+  __device__ __forceinline__ Chunk(const char* p, int stride, int64_t row, int n, int bytes, bool rev, bool wanted) {
+    const int span = (n - 1) * stride;
+    rsrc = from_base(p + row * stride, wanted && n > 0 ? span + bytes : 0);
+    ld = rev ? -stride : stride;
+    top = rev ? span : 0;
   }
 };
 
@@ -259,10 +254,11 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
   typedef Operand<T> Op;
   typedef typename Op::Value Value;
   constexpr int C = Op::kChunk, KB = Op::kBlock, TC = C / 16, TD = DA / 16, KC = C / KB, KD = DA / KB;
-  constexpr int kThreads = kWave * W, TN = DC / (16 * W), kTiles = TC * (TC + 1) / 2;
+  constexpr int kThreads = kWave * W, TN = DC / (16 * W);
   constexpr int LA = DA + Op::kPad, LB = Op::apart(DA), LC = Op::apart(DC), LP = C + Op::kPad;
   __shared__ __align__(16) Value s_a[OUT ? C * LA : 1], s_b[C * LB], s_c[C * LC], s_p[OUT ? C * LP : 1];
-  __shared__ float s_pows[16 + C + 1];  // powers of the decay; zeros where the exponent is negative
+  __shared__ float s_pow[C + 1];                 // powers of the decay
+  __shared__ __align__(16) float s_fade[2 * C];  // what a full chunk's rows enter the state with, then zeros
   const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), l = lane % 16, q = lane / 16;
   const bool rev = f.rev;
   Segment s;
@@ -272,26 +268,41 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
     s.begin -= args.L;
   }
   const float g = args.decay[group];
-  float* const s_pow = s_pows + 16;
-  if (threadIdx.x < 16 + C + 1) s_pows[threadIdx.x] = threadIdx.x < 16 ? 0.f : (float)power(g, threadIdx.x - 16);
-  if constexpr (OUT) {
-    for (int i = threadIdx.x; i < C * LP; i += kThreads) s_p[i] = 0;
+  for (int i = threadIdx.x; i < 2 * C; i += kThreads) {
+    if (i <= C) s_pow[i] = (float)power(g, i);
+    const int far = C - (rev ? 0 : 1) - i;
+    s_fade[i] = far >= 0 ? f.u_scale * (float)power(g, far) : 0.f;
   }
   constexpr int size = sizeof(Value);
   const int c0 = slice * DC, wc = min(DC, f.dc - c0), n0 = 16 * TN * wave;
   const int64_t states = (int64_t)args.groups * args.state, mine = (int64_t)group * args.state;
   const int heads = OUT || rev ? args.per : 1, length = (int)(s.end - s.begin);
+  // The matrices' places stay in scalar registers (loaded again from the arguments in every step, they would be waited for),
+  // from the group's columns on: heads are `apart` bytes from one another.
+  struct Place {
+    const char* p;
+    int ld, apart;
+  };
+  auto place_of = [&](const Rows& m, int cols, bool per_head, int first) {
+    Place x{m.p + ((int64_t)group * (per_head ? args.per : 1) * cols + first) * size, (int)m.ld, per_head ? cols * size : 0};
+    asm volatile("" : "+s"(x.p), "+s"(x.ld), "+s"(x.apart));
+    return x;
+  };
+  const Place pa = OUT ? place_of(f.a, f.da, !rev, 0) : Place{}, pb = place_of(f.b, f.da, rev, 0),
+              pc = place_of(f.c, f.dc, rev, c0), po = OUT ? place_of(f.out, f.dc, !rev, c0) : Place{};
+  int da = f.da;
+  asm volatile("" : "+s"(da));
+  auto chunk = [&](const Place& m, int at, int h, int n, int w, bool wanted) {
+    return Chunk(m.p + h * m.apart, m.ld, rev ? s.end - at - n : s.begin + at, n, w * size, rev, wanted);
+  };
   Rowset<T, DA, kThreads, ALIGNED> ra, rb;
   Rowset<T, DC, kThreads, ALIGNED> rc;
   // (rows that a step does not need are loaded from nowhere: a branch around loads would wait for them at its end)
   auto load = [&](int at, int h) {
     const int n = min(C, length - at);
-    const int64_t p0 = rev ? s.end - 1 - at : s.begin + at;
-    const int64_t head = (int64_t)group * args.per + h;
-    if constexpr (OUT)
-      ra.load(Chunk(f.a, (rev ? group : head) * f.da * size, f.da, size, p0, n, rev, !rev || h == 0), f.da);
-    rb.load(Chunk(f.b, (rev ? head : group) * f.da * size, f.da, size, p0, n, rev, rev || h == 0), f.da);
-    rc.load(Chunk(f.c, ((rev ? head : group) * f.dc + c0) * size, wc, size, p0, n, rev, rev || h == 0), wc);
+    if constexpr (OUT) ra.load(chunk(pa, at, h, n, da, !rev || h == 0), da);
+    rb.load(chunk(pb, at, h, n, da, rev || h == 0), da);
+    rc.load(chunk(pc, at, h, n, wc, rev || h == 0), wc);
   };
   load(0, 0);
   // the state: lane l holds column n0 + 16 t + l % 16, rows 16 d + 4 q ..
@@ -324,10 +335,27 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
     }
   };
   put(0);
+  __syncthreads();
+  // Weights of the products that a lane makes, in row l % 16 of its band, columns 4 q ..: in the tile on the diagonal, in
+  // the one before it, and how much less the tiles before that have
+  constexpr int kBands = OUT ? TC * TC / W : 1;
+  const int ti = wave * kBands / TC, tj = wave * kBands % TC;
+  float on[4], off[4], less[kBands];
+  if constexpr (OUT) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      on[e] = f.p_scale * s_pow[max(l - 4 * q - e, 0)];
+      off[e] = f.p_scale * s_pow[16 + l - 4 * q - e];
+    }
+#pragma unroll
+    for (int j = 0; j < kBands; ++j) less[j] = lane_at(s_pow[16 * max(ti - tj - j - 1, 0)], 0);
+  }
+  // A state that is kept gets weighted rows with all of their bits; one that only multiplies rows of this segment is
+  // rounded to theirs for that, and gets them rounded so.
+  const bool exact = f.end != nullptr && (rev ? s.first : s.last);
   f32x4 o[TC][TN];
   for (int at = 0; at < length; at += C) {
     const int n = min(C, length - at);
-    const int64_t p0 = rev ? s.end - 1 - at : s.begin + at;
     for (int h = 0; h < heads; ++h) {
       const bool new_a = !rev || h == 0, last = h == heads - 1;
       // (addresses are made again in every step: kept across it they take the registers that loads are on their way to)
@@ -336,35 +364,34 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
       __syncthreads();
       load(last ? at + C : at, last ? 0 : h + 1);
       if constexpr (OUT) {
-        // products a . b of the tiles on and below the diagonal, weighted, to LDS (those above it stay zero)
+        // products a . b of a band of 16 rows, weighted, to LDS: 16 W / C bands of columns a wavefront
+        f32x4 p[kBands];
+        Op y[KD];
 #pragma unroll
-        for (int round = 0; round < (kTiles + W - 1) / W; ++round) {
-          const int t = round * W + wave;
-          if (t >= kTiles) break;
-          __builtin_amdgcn_sched_barrier(0);
-          const int ti = (t >= 1) + (t >= 3) + (t >= 6), tj = t - ti * (ti + 1) / 2;
-          f32x4 p = {0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < KD; ++k) y[k].row(s_a + (16 * ti + l) * LA + k * KB, q);
 #pragma unroll
-          for (int k = 0; k < KD; ++k) {
-            Op x, y;
-            x.row(s_b + (16 * tj + l) * LB + k * KB, q);
-            y.row(s_a + (16 * ti + l) * LA + k * KB, q);
-            mul(p, x, y);
+        for (int j = 0; j < kBands; ++j) p[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < KD; ++k)
+#pragma unroll
+          for (int j = 0; j < kBands; ++j) {
+            Op x;
+            x.row(s_b + (16 * (tj + j) + l) * LB + k * KB, q);
+            mul(p[j], x, y[k]);
           }
-          const int far = 16 * (ti - tj) + l - 4 * q;
+#pragma unroll
+        for (int j = 0; j < kBands; ++j) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            float w = s_pow[far - e];
-            asm volatile("" : "+v"(w));  // (read by every lane: no branch)
-            w *= f.p_scale;
-            p[e] = far - e >= 0 ? p[e] * w : 0.f;
+            const float w = ti == tj + j ? on[e] : off[e] * less[j];
+            p[j][e] = 16 * (ti - tj - j) + l - 4 * q - e >= 0 ? p[j][e] * w : 0.f;
           }
-          Value* to = s_p + (16 * ti + l) * LP + 16 * tj + 4 * q;
+          Value* to = s_p + (16 * ti + l) * LP + 16 * (tj + j) + 4 * q;
           // (weights of bf16 rows are rounded as the rows are: to bf16)
-          if constexpr (sizeof(Value) == 2) *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3])};
-          else *reinterpret_cast<f32x4*>(to) = p;
+          if constexpr (sizeof(Value) == 2)
+            *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(p[j][0], p[j][1]), pack_bf16(p[j][2], p[j][3])};
+          else *reinterpret_cast<f32x4*>(to) = p[j];
         }
-        __builtin_amdgcn_sched_barrier(0);
         if (new_a) {
           // what the state before the chunk gives; lane l: row 16 i + l % 16, columns 4 q ..
 #pragma unroll
@@ -411,8 +438,7 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
         {
           // (to nowhere where nothing is to be stored yet: as many stores follow the loads in every step, so that the
           // wait for the loads does not take in the stores)
-          const int64_t col0 = (rev ? (int64_t)group : (int64_t)group * args.per + h) * f.dc + c0;
-          const Chunk out(f.out, col0 * size, wc, size, p0, n, rev, !rev || last);
+          const Chunk out = chunk(po, at, h, n, wc, !rev || last);
 #pragma unroll
           for (int t = 0; t < TN; ++t) {
             const int col = n0 + 16 * t + 4 * q;
@@ -450,20 +476,54 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
         for (int k = 0; k < KC; ++k) {
           __builtin_amdgcn_sched_barrier(0);
           float w[Op::kEach];
+          const int j = k * KB + Op::index(q, 0) + C - n;
+          if (n == C) {
 #pragma unroll
-          for (int e = 0; e < Op::kEach; ++e)
-            w[e] = f.u_scale * s_pow[max(n - (rev ? 0 : 1) - (k * KB + Op::index(q, e)), 0)];
-          Op x[TN][Op::kParts];
+            for (int e = 0; e < Op::kEach; e += 4) {
+              const f32x4 v = *reinterpret_cast<const f32x4*>(s_fade + j + e);
 #pragma unroll
-          for (int t = 0; t < TN; ++t) Op::weighted(c[k][t], w, x[t]);
+              for (int i = 0; i < 4; ++i) w[e + i] = v[i];
+            }
+          } else {
 #pragma unroll
-          for (int d = 0; d < TD; ++d) {
-            Op y;
-            y.template column<LB>(s_b + k * KB * LB + 16 * d, q, l);
+            for (int e = 0; e < Op::kEach; ++e) w[e] = s_fade[j + e];
+          }
+          float v[TN][Op::kEach];
+#pragma unroll
+          for (int t = 0; t < TN; ++t)
+#pragma unroll
+            for (int e = 0; e < Op::kEach; ++e) v[t][e] = c[k][t].get(e) * w[e];
+          if constexpr (!OUT) {
+            Op x[TN][Op::kParts];
 #pragma unroll
             for (int t = 0; t < TN; ++t)
 #pragma unroll
-              for (int p = 0; p < Op::kParts; ++p) mul(st[d][t], y, x[t][p]);
+              for (int p = 0; p < Op::kParts; ++p) x[t][p].take(v[t]);
+#pragma unroll
+            for (int d = 0; d < TD; ++d) {
+              Op y;
+              y.template column<LB>(s_b + k * KB * LB + 16 * d, q, l);
+#pragma unroll
+              for (int t = 0; t < TN; ++t)
+#pragma unroll
+                for (int p = 0; p < Op::kParts; ++p) mul(st[d][t], y, x[t][p]);
+            }
+          } else {
+            // (a loop: registers do not hold the parts together)
+            int left = exact ? Op::kParts : 1;
+#pragma unroll 1
+            do {
+              Op x[TN];
+#pragma unroll
+              for (int t = 0; t < TN; ++t) x[t].take(v[t]);
+#pragma unroll
+              for (int d = 0; d < TD; ++d) {
+                Op y;
+                y.template column<LB>(s_b + k * KB * LB + 16 * d, q, l);
+#pragma unroll
+                for (int t = 0; t < TN; ++t) mul(st[d][t], y, x[t]);
+              }
+            } while (--left > 0);
           }
         }
       }
