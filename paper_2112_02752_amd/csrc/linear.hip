@@ -255,8 +255,9 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
   typedef typename Op::Value Value;
   constexpr int C = Op::kChunk, KB = Op::kBlock, TC = C / 16, TD = DA / 16, KC = C / KB, KD = DA / KB;
   constexpr int kThreads = kWave * W, TN = DC / (16 * W);
-  constexpr int LA = DA + Op::kPad, LB = Op::apart(DA), LC = Op::apart(DC), LP = C + Op::kPad;
-  __shared__ __align__(16) Value s_a[OUT ? C * LA : 1], s_b[C * LB], s_c[C * LC], s_p[OUT ? C * LP : 1];
+  static_assert(!OUT || W == 4, "three squares of products");
+  constexpr int LA = DA + Op::kPad, LO = (DA > DC ? DA : DC) + Op::kPad, LB = Op::apart(DA), LC = Op::apart(DC), LP = C + Op::kPad;
+  __shared__ __align__(16) Value s_a[OUT ? C * LO : 1], s_b[C * LB], s_c[C * LC], s_p[OUT ? C * LP : 1];
   __shared__ float s_pow[C + 1];                 // powers of the decay
   __shared__ __align__(16) float s_fade[2 * C];  // what a full chunk's rows enter the state with, then zeros
   const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), l = lane % 16, q = lane / 16;
@@ -336,11 +337,11 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
   };
   put(0);
   __syncthreads();
-  // Weights of the products that a lane makes, in row l % 16 of its band, columns 4 q ..: in the tile on the diagonal, in
-  // the one before it, and how much less the tiles before that have
-  constexpr int kBands = OUT ? TC * TC / W : 1;
-  const int ti = wave * kBands / TC, tj = wave * kBands % TC;
-  float on[4], off[4], less[kBands];
+  // Weights of the products that a lane makes, in row l % 16 of a tile, columns 4 q ..: in one on the diagonal, in the one
+  // before it, and how much less those before that have
+  constexpr int kSide = TC / 2, kSquares = 3;  // (the fourth square is above the diagonal)
+  const int square = wave, ti = square >= 1 ? kSide : 0, tj = square >= 2 ? kSide : 0;
+  float on[4], off[4], less[2 * kSide - 1];
   if constexpr (OUT) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -348,7 +349,7 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
       off[e] = f.p_scale * s_pow[16 + l - 4 * q - e];
     }
 #pragma unroll
-    for (int j = 0; j < kBands; ++j) less[j] = lane_at(s_pow[16 * max(ti - tj - j - 1, 0)], 0);
+    for (int i = 0; i < 2 * kSide - 1; ++i) less[i] = lane_at(s_pow[16 * max(ti - tj + i - kSide, 0)], 0);
   }
   // A state that is kept gets weighted rows with all of their bits; one that only multiplies rows of this segment is
   // rounded to theirs for that, and gets them rounded so.
@@ -364,33 +365,42 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
       __syncthreads();
       load(last ? at + C : at, last ? 0 : h + 1);
       if constexpr (OUT) {
-        // products a . b of a band of 16 rows, weighted, to LDS: 16 W / C bands of columns a wavefront
-        f32x4 p[kBands];
-        Op y[KD];
+        // products a . b, weighted, to LDS: kSide x kSide tiles a wavefront, of the squares on and below the diagonal
+        if (square < kSquares) {
+          f32x4 p[kSide][kSide];
 #pragma unroll
-        for (int k = 0; k < KD; ++k) y[k].row(s_a + (16 * ti + l) * LA + k * KB, q);
+          for (int i = 0; i < kSide; ++i)
 #pragma unroll
-        for (int j = 0; j < kBands; ++j) p[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < kSide; ++j) p[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < KD; ++k)
+          for (int k = 0; k < KD; ++k) {
+            Op x[kSide], y[kSide];
 #pragma unroll
-          for (int j = 0; j < kBands; ++j) {
-            Op x;
-            x.row(s_b + (16 * (tj + j) + l) * LB + k * KB, q);
-            mul(p[j], x, y[k]);
+            for (int i = 0; i < kSide; ++i) {
+              x[i].row(s_b + (16 * (tj + i) + l) * LB + k * KB, q);
+              y[i].row(s_a + (16 * (ti + i) + l) * LA + k * KB, q);
+            }
+#pragma unroll
+            for (int i = 0; i < kSide; ++i)
+#pragma unroll
+              for (int j = 0; j < kSide; ++j) mul(p[i][j], x[j], y[i]);
           }
 #pragma unroll
-        for (int j = 0; j < kBands; ++j) {
+          for (int i = 0; i < kSide; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float w = ti == tj + j ? on[e] : off[e] * less[j];
-            p[j][e] = 16 * (ti - tj - j) + l - 4 * q - e >= 0 ? p[j][e] * w : 0.f;
-          }
-          Value* to = s_p + (16 * ti + l) * LP + 16 * (tj + j) + 4 * q;
-          // (weights of bf16 rows are rounded as the rows are: to bf16)
-          if constexpr (sizeof(Value) == 2)
-            *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(p[j][0], p[j][1]), pack_bf16(p[j][2], p[j][3])};
-          else *reinterpret_cast<f32x4*>(to) = p[j];
+            for (int j = 0; j < kSide; ++j) {
+              const int apart = ti - tj + i - j;  // tiles
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float w = apart == 0 ? on[e] : off[e] * less[kSide - 1 + i - j];
+                p[i][j][e] = 16 * apart + l - 4 * q - e >= 0 ? p[i][j][e] * w : 0.f;
+              }
+              Value* to = s_p + (16 * (ti + i) + l) * LP + 16 * (tj + j) + 4 * q;
+              // (weights of bf16 rows are rounded as the rows are: to bf16)
+              if constexpr (sizeof(Value) == 2)
+                *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(p[i][j][0], p[i][j][1]), pack_bf16(p[i][j][2], p[i][j][3])};
+              else *reinterpret_cast<f32x4*>(to) = p[i][j];
+            }
         }
         if (new_a) {
           // what the state before the chunk gives; lane l: row 16 i + l % 16, columns 4 q ..
@@ -439,16 +449,36 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
           // (to nowhere where nothing is to be stored yet: as many stores follow the loads in every step, so that the
           // wait for the loads does not take in the stores)
           const Chunk out = chunk(po, at, h, n, wc, !rev || last);
+          if constexpr (ALIGNED) {
+            // by way of the wavefront's own columns of s_a, which nobody reads any more then, so that lanes next to one
+            // another store whole pieces of rows
+            constexpr int kVec = Op::kVec, kRow = 16 * TN / kVec, kEach = C * kRow / kWave;
+            if (!rev || last) {
 #pragma unroll
-          for (int t = 0; t < TN; ++t) {
-            const int col = n0 + 16 * t + 4 * q;
-            const uint32_t row = (uint32_t)(out.top + l * out.ld + col * size);
-            const uint32_t off = col < wc ? row : kNowhere;
+              for (int i = 0; i < TC; ++i)
 #pragma unroll
-            for (int i = 0; i < TC; ++i) {
-              const uint32_t to = off + (uint32_t)(16 * i * out.ld);
-              const f32x4 v = o[i][t] * f.out_scale;
-              if constexpr (!ALIGNED) {
+                for (int t = 0; t < TN; ++t) {
+                  const f32x4 v = o[i][t] * f.out_scale;
+                  Value* to = s_a + (16 * i + l) * LO + n0 + 16 * t + 4 * q;
+                  if constexpr (size == 2) *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+                  else *reinterpret_cast<f32x4*>(to) = v;
+                }
+            }
+            const int r = lane / kRow, col = n0 + lane % kRow * kVec;
+            const uint32_t off_ = (uint32_t)(out.top + r * out.ld + col * size), at_ = col < wc ? off_ : kNowhere;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+              const u32x4 v = *reinterpret_cast<const u32x4*>(s_a + (r + i * (kWave / kRow)) * LO + col);
+              __builtin_amdgcn_raw_buffer_store_b128(v, out.rsrc, at_ + (uint32_t)(i * (kWave / kRow) * out.ld), 0, 0);
+            }
+          } else {
+#pragma unroll
+            for (int t = 0; t < TN; ++t) {
+              const int col = n0 + 16 * t + 4 * q;
+#pragma unroll
+              for (int i = 0; i < TC; ++i) {
+                const uint32_t to = (uint32_t)(out.top + (l + 16 * i) * out.ld + col * size);
+                const f32x4 v = o[i][t] * f.out_scale;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                   const uint32_t one = col + e < wc ? to + (uint32_t)(e * size) : kNowhere;
@@ -456,10 +486,6 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
                     __builtin_amdgcn_raw_buffer_store_b16((uint16_t)pack_bf16(v[e], 0.f), out.rsrc, one, 0, 0);
                   else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[e]), out.rsrc, one, 0, 0);
                 }
-              } else if constexpr (size == 2) {
-                __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}, out.rsrc, to, 0, 0);
-              } else {
-                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), out.rsrc, to, 0, 0);
               }
             }
           }
