@@ -56,11 +56,11 @@ struct Operand<bf16> {
     const u32x2 lo = *reinterpret_cast<const u32x2*>(at + 4 * q), hi = *reinterpret_cast<const u32x2*>(at + 16 + 4 * q);
     v = __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
   }
-  // column l % 16 of 16 from `at` on, rows 0 .. kBlock - 1 of `ld` values: the transposing load gives a lane four rows
-  // of its column where the 16 lanes of a quarter point at those rows' 16 columns in order
-  template <int LD>
+  // column APART (l / 4) + l % 4 from `at` on, rows 0 .. kBlock - 1 of LD values: the transposing load gives a lane four
+  // rows of its column where the 16 lanes of a quarter point at those rows' 16 columns in order, four each
+  template <int LD, int APART = 4>
   __device__ __forceinline__ void column(const Value* at, int q, int l) {
-    const Value* p = at + (8 * q + l / 4) * LD + 4 * (l % 4);
+    const Value* p = at + (8 * q + l / 4) * LD + APART * (l % 4);
     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
     const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + 4 * LD));
     const u32x2 a = __builtin_bit_cast(u32x2, lo), b = __builtin_bit_cast(u32x2, hi);
@@ -98,10 +98,10 @@ struct Operand<float> {
   f32x4 v;
   __device__ __forceinline__ void row(const Value* at, int q) { v = *reinterpret_cast<const f32x4*>(at + 4 * q); }
   __device__ __forceinline__ void row_as_state(const Value* at, int q) { row(at, q); }
-  template <int LD>
+  template <int LD, int APART = 4>
   __device__ __forceinline__ void column(const Value* at, int q, int l) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = at[(4 * q + e) * LD + l];
+    for (int e = 0; e < 4; ++e) v[e] = at[(4 * q + e) * LD + APART * (l / 4) + l % 4];
   }
   __device__ __forceinline__ void state(f32x4 a, f32x4) { v = a; }
   __device__ __forceinline__ float get(int e) const { return v[e]; }
@@ -247,21 +247,36 @@ struct Rowset {
   }
 };
 
+// A block's LDS: the rows of a chunk, a step's products, powers of the decay, and what a full chunk's rows enter the state
+// with, then zeros.
+template <typename T, int DA, int DC, bool OUT>
+struct Room {
+  typedef Operand<T> Op;
+  static constexpr int C = Op::kChunk, LA = DA + Op::kPad, LB = Op::apart(DA), LC = Op::apart(DC), LP = C + Op::kPad;
+  alignas(16) typename Op::Value a[OUT ? C * LA : 8], b[C * LB], c[C * LC], p[OUT ? C * LP : 8];
+  alignas(16) float fade[2 * C], pow[C + 1];
+};
+
 // DA: widest a and b; DC: columns of c that a block takes.  OUT: the form itself, else the sums of the segment that ends
 // (backwards: begins) at a boundary.
-template <typename T, int DA, int DC, int W, bool OUT, bool ALIGNED>
-__device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t number, int group, int slice) {
+template <typename T, int DA, int DC, int W, bool OUT, bool ALIGNED, bool REV>
+__device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t number, int group, int slice,
+                                      Room<T, DA, DC, OUT>& lds) {
   typedef Operand<T> Op;
   typedef typename Op::Value Value;
   constexpr int C = Op::kChunk, KB = Op::kBlock, TC = C / 16, TD = DA / 16, KC = C / KB, KD = DA / KB;
   constexpr int kThreads = kWave * W, TN = DC / (16 * W);
   static_assert(!OUT || W == 4, "three squares of products");
-  constexpr int LA = DA + Op::kPad, LO = (DA > DC ? DA : DC) + Op::kPad, LB = Op::apart(DA), LC = Op::apart(DC), LP = C + Op::kPad;
-  __shared__ __align__(16) Value s_a[OUT ? C * LO : 1], s_b[C * LB], s_c[C * LC], s_p[OUT ? C * LP : 1];
-  __shared__ float s_pow[C + 1];                 // powers of the decay
-  __shared__ __align__(16) float s_fade[2 * C];  // what a full chunk's rows enter the state with, then zeros
+  typedef Room<T, DA, DC, OUT> Lds;
+  constexpr int LA = Lds::LA, LB = Lds::LB, LC = Lds::LC, LP = Lds::LP;
+  Value* const s_a = lds.a;
+  Value* const s_b = lds.b;
+  Value* const s_c = lds.c;
+  Value* const s_p = lds.p;
+  float* const s_pow = lds.pow;
+  float* const s_fade = lds.fade;
   const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), l = lane % 16, q = lane / 16;
-  const bool rev = f.rev;
+  constexpr bool rev = REV;
   Segment s;
   if (OUT ? !segment(args, number, lane, s) : !boundary(args, number, lane, s)) return;
   if (!OUT && !rev) {  // the segment before
@@ -306,10 +321,12 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
     rc.load(chunk(pc, at, h, n, wc, rev || h == 0), wc);
   };
   load(0, 0);
-  // the state: lane l holds column n0 + 16 t + l % 16, rows 16 d + 4 q ..
+  // The state: lane l holds rows 16 d + 4 q .. of a column.  With two tiles of columns a wavefront, those of tile t are 8 j +
+  // 4 t + (0 .. 3), so that a lane's results of both are eight values in a row.
+  constexpr int kApart = 4 * TN, kTile = TN == 2 ? 4 : 16;
   // (`from_l` is l, in a register of the caller's: the offsets of the first use are not kept for the second)
   auto place = [&](int from_l, int d, int t, int e) {
-    const int row = 16 * d + 4 * q + e, col = n0 + 16 * t + from_l;
+    const int row = 16 * d + 4 * q + e, col = n0 + kTile * t + kApart * (from_l / 4) + from_l % 4;
     return row < f.da && col < wc ? (uint32_t)(row * f.sd + (c0 + col) * f.sn) * 4u : kNowhere;
   };
   f32x4 st[TD][TN] = {};
@@ -341,13 +358,15 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
   // before it, and how much less those before that have
   constexpr int kSide = TC / 2, kSquares = 3;  // (the fourth square is above the diagonal)
   const int square = wave, ti = square >= 1 ? kSide : 0, tj = square >= 2 ? kSide : 0;
-  float on[4], off[4], less[2 * kSide - 1];
+  float on[4], off[4], less[2 * kSide - 1], before[TC];
   if constexpr (OUT) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       on[e] = f.p_scale * s_pow[max(l - 4 * q - e, 0)];
       off[e] = f.p_scale * s_pow[16 + l - 4 * q - e];
     }
+#pragma unroll
+    for (int i = 0; i < TC; ++i) before[i] = lane_at(s_pow[16 * max(i - wave - 1, 0)], 0);
 #pragma unroll
     for (int i = 0; i < 2 * kSide - 1; ++i) less[i] = lane_at(s_pow[16 * max(ti - tj + i - kSide, 0)], 0);
   }
@@ -365,8 +384,51 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
       __syncthreads();
       load(last ? at + C : at, last ? 0 : h + 1);
       if constexpr (OUT) {
-        // products a . b, weighted, to LDS: kSide x kSide tiles a wavefront, of the squares on and below the diagonal
-        if (square < kSquares) {
+        auto put_products = [&](f32x4 p, int i, int j, float fade) {
+          // (of tile i, j; weights of bf16 rows are rounded as the rows are: to bf16)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float w = i == j ? on[e] : off[e] * fade;
+            p[e] = 16 * (i - j) + l - 4 * q - e >= 0 ? p[e] * w : 0.f;
+          }
+          Value* to = s_p + (16 * i + l) * LP + 16 * j + 4 * q;
+          if constexpr (sizeof(Value) == 2) *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3])};
+          else *reinterpret_cast<f32x4*>(to) = p;
+        };
+        if (new_a) {
+          // What the state before the chunk gives (lane l: row 16 i + l % 16), and on the way, as the rows of a are there,
+          // their products with 16 rows of b a wavefront, for LDS.  (Tiles above the diagonal are zeros.)
+          f32x4 p[TC];
+#pragma unroll
+          for (int i = 0; i < TC; ++i) {
+            p[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int t = 0; t < TN; ++t) o[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+          }
+#pragma unroll
+          for (int k = 0; k < KD; ++k) {
+            Op x[TN], z;
+            z.row_as_state(s_b + (16 * (wave % TC) + l) * LB + k * KB, q);
+#pragma unroll
+            for (int t = 0; t < TN; ++t) x[t].state(st[k * KB / 16][t], st[(k * KB / 16 + 1) % TD][t]);
+#pragma unroll
+            for (int i = 0; i < TC; ++i) {
+              Op y;
+              y.row_as_state(s_a + (16 * i + l) * LA + k * KB, q);
+              mul(p[i], z, y);
+#pragma unroll
+              for (int t = 0; t < TN; ++t) mul(o[i][t], x[t], y);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < TC; ++i) {
+            const float w = s_pow[16 * i + l + (rev ? 0 : 1)];
+#pragma unroll
+            for (int t = 0; t < TN; ++t) o[i][t] *= w;
+            if (wave < TC) put_products(p[i], i, wave, before[i]);
+          }
+        } else if (square < kSquares) {
+          // products alone: kSide x kSide tiles a wavefront, of the squares on and below the diagonal
           f32x4 p[kSide][kSide];
 #pragma unroll
           for (int i = 0; i < kSide; ++i)
@@ -388,45 +450,7 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
 #pragma unroll
           for (int i = 0; i < kSide; ++i)
 #pragma unroll
-            for (int j = 0; j < kSide; ++j) {
-              const int apart = ti - tj + i - j;  // tiles
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float w = apart == 0 ? on[e] : off[e] * less[kSide - 1 + i - j];
-                p[i][j][e] = 16 * apart + l - 4 * q - e >= 0 ? p[i][j][e] * w : 0.f;
-              }
-              Value* to = s_p + (16 * (ti + i) + l) * LP + 16 * (tj + j) + 4 * q;
-              // (weights of bf16 rows are rounded as the rows are: to bf16)
-              if constexpr (sizeof(Value) == 2)
-                *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(p[i][j][0], p[i][j][1]), pack_bf16(p[i][j][2], p[i][j][3])};
-              else *reinterpret_cast<f32x4*>(to) = p[i][j];
-            }
-        }
-        if (new_a) {
-          // what the state before the chunk gives; lane l: row 16 i + l % 16, columns 4 q ..
-#pragma unroll
-          for (int i = 0; i < TC; ++i)
-#pragma unroll
-            for (int t = 0; t < TN; ++t) o[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int k = 0; k < KD; ++k) {
-            Op x[TN];
-#pragma unroll
-            for (int t = 0; t < TN; ++t) x[t].state(st[k * KB / 16][t], st[(k * KB / 16 + 1) % TD][t]);
-#pragma unroll
-            for (int i = 0; i < TC; ++i) {
-              Op y;
-              y.row_as_state(s_a + (16 * i + l) * LA + k * KB, q);
-#pragma unroll
-              for (int t = 0; t < TN; ++t) mul(o[i][t], x[t], y);
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < TC; ++i) {
-            const float w = s_pow[16 * i + l + (rev ? 0 : 1)];
-#pragma unroll
-            for (int t = 0; t < TN; ++t) o[i][t] *= w;
-          }
+            for (int j = 0; j < kSide; ++j) put_products(p[i][j], ti + i, tj + j, less[kSide - 1 + i - j]);
         }
         __syncthreads();
       }
@@ -434,7 +458,7 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
 #pragma unroll
       for (int k = 0; k < KC; ++k)
 #pragma unroll
-        for (int t = 0; t < TN; ++t) c[k][t].template column<LC>(s_c + k * KB * LC + n0 + 16 * t, q, l);
+        for (int t = 0; t < TN; ++t) c[k][t].template column<LC, kApart>(s_c + k * KB * LC + n0 + kTile * t, q, l);
       if constexpr (OUT) {
 #pragma unroll
         for (int i = 0; i < TC; ++i)
@@ -449,42 +473,36 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
           // (to nowhere where nothing is to be stored yet: as many stores follow the loads in every step, so that the
           // wait for the loads does not take in the stores)
           const Chunk out = chunk(po, at, h, n, wc, !rev || last);
-          if constexpr (ALIGNED) {
-            // by way of the wavefront's own columns of s_a, which nobody reads any more then, so that lanes next to one
-            // another store whole pieces of rows
-            constexpr int kVec = Op::kVec, kRow = 16 * TN / kVec, kEach = C * kRow / kWave;
-            if (!rev || last) {
+          const int col = n0 + kApart * q;
 #pragma unroll
-              for (int i = 0; i < TC; ++i)
+          for (int i = 0; i < TC; ++i) {
+            const uint32_t row = (uint32_t)(out.top + (l + 16 * i) * out.ld + col * size);
+            float v[4 * TN];
 #pragma unroll
-                for (int t = 0; t < TN; ++t) {
-                  const f32x4 v = o[i][t] * f.out_scale;
-                  Value* to = s_a + (16 * i + l) * LO + n0 + 16 * t + 4 * q;
-                  if constexpr (size == 2) *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-                  else *reinterpret_cast<f32x4*>(to) = v;
-                }
-            }
-            const int r = lane / kRow, col = n0 + lane % kRow * kVec;
-            const uint32_t off_ = (uint32_t)(out.top + r * out.ld + col * size), at_ = col < wc ? off_ : kNowhere;
+            for (int t = 0; t < TN; ++t)
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-              const u32x4 v = *reinterpret_cast<const u32x4*>(s_a + (r + i * (kWave / kRow)) * LO + col);
-              __builtin_amdgcn_raw_buffer_store_b128(v, out.rsrc, at_ + (uint32_t)(i * (kWave / kRow) * out.ld), 0, 0);
-            }
-          } else {
+              for (int e = 0; e < 4; ++e) v[4 * t + e] = o[i][t][e] * f.out_scale;
+            if constexpr (!ALIGNED) {
 #pragma unroll
-            for (int t = 0; t < TN; ++t) {
-              const int col = n0 + 16 * t + 4 * q;
+              for (int e = 0; e < 4 * TN; ++e) {
+                const uint32_t to = col + e < wc ? row + (uint32_t)(e * size) : kNowhere;
+                if constexpr (size == 2)
+                  __builtin_amdgcn_raw_buffer_store_b16((uint16_t)pack_bf16(v[e], 0.f), out.rsrc, to, 0, 0);
+                else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[e]), out.rsrc, to, 0, 0);
+              }
+            } else {
+              // (a head's columns end at a multiple of 16 bytes)
 #pragma unroll
-              for (int i = 0; i < TC; ++i) {
-                const uint32_t to = (uint32_t)(out.top + (l + 16 * i) * out.ld + col * size);
-                const f32x4 v = o[i][t] * f.out_scale;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const uint32_t one = col + e < wc ? to + (uint32_t)(e * size) : kNowhere;
-                  if constexpr (size == 2)
-                    __builtin_amdgcn_raw_buffer_store_b16((uint16_t)pack_bf16(v[e], 0.f), out.rsrc, one, 0, 0);
-                  else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[e]), out.rsrc, one, 0, 0);
+              for (int e = 0; e < 4 * TN; e += 16 / size) {
+                const uint32_t to = col + e < wc ? row + (uint32_t)(e * size) : kNowhere;
+                if constexpr (size == 4) {
+                  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]}), out.rsrc, to, 0, 0);
+                } else if constexpr (TN == 1) {
+                  __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}, out.rsrc, to, 0, 0);
+                } else {
+                  __builtin_amdgcn_raw_buffer_store_b128(
+                      u32x4{pack_bf16(v[e], v[e + 1]), pack_bf16(v[e + 2], v[e + 3]), pack_bf16(v[e + 4], v[e + 5]), pack_bf16(v[e + 6], v[e + 7])},
+                      out.rsrc, to, 0, 0);
                 }
               }
             }
@@ -576,13 +594,16 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
 // `forms` of the forms from `first` on, which have as many slices each, in one launch
 template <typename T, int DA, int DC, int W, bool OUT, bool ALIGNED>
 __global__ __launch_bounds__(kWave* W, DA > 128 ? 1 : 2) void k_linear(Args a, int first, int forms) {
+  __shared__ Room<T, DA, DC, OUT> lds;
   uint32_t at = blockIdx.x;
   const Form& f = a.f[first + (int)(at % (uint32_t)forms)];
   at /= (uint32_t)forms;
   const uint32_t slices = (uint32_t)a.slices[first], groups = (uint32_t)a.groups;
   const int slice = (int)(at % slices);
   at /= slices;
-  sweep<T, DA, DC, W, OUT, ALIGNED>(a, f, at / groups, (int)(at % groups), slice);
+  // (apart: each needs fewer registers than one body for both)
+  if (f.rev) sweep<T, DA, DC, W, OUT, ALIGNED, true>(a, f, at / groups, (int)(at % groups), slice, lds);
+  else sweep<T, DA, DC, W, OUT, ALIGNED, false>(a, f, at / groups, (int)(at % groups), slice, lds);
 }
 
 // States at a sequence's boundaries from the sums between them, in place: in order, or backwards.
@@ -631,7 +652,7 @@ __global__ __launch_bounds__(kThreads) void k_linear_chain(Args a, const float* 
 // ---------------------------------------------------------------- host
 
 // Segments: as long as it takes for no more than this many blocks of sums, twice as long each time.
-constexpr int64_t kMinLength = 256, kMaxBlocks = 1024;
+constexpr int64_t kMinLength = 64, kMaxBlocks = 512;
 int64_t most_bounds(int groups) { return groups >= kMaxBlocks ? 1 : kMaxBlocks / groups; }
 int64_t length_for(int64_t N, int groups) {
   int64_t L = kMinLength;
