@@ -131,7 +131,8 @@ struct Form {
 };
 
 struct Args {
-  int64_t N, L, bounds;  // segment length, number of boundaries
+  int64_t N, bounds;  // number of boundaries
+  int32_t log;        // of the segment length L = 2^log
   int32_t M, groups, per;  // heads of a group
   int32_t aligned;
   const int32_t* offsets;
@@ -160,14 +161,26 @@ struct Segment {
 
 // the boundary of this number: the segment that begins there; false if there is none
 __device__ __forceinline__ bool boundary(const Args& a, int64_t number, int lane, Segment& s) {
-  const int64_t pos = (number + 1) * a.L;
-  s.seq = wave_upper_bound(a.offsets, a.M + 1, (int32_t)pos, lane) - 1;
-  if (s.seq < 0 || s.seq >= a.M) return false;
-  const int64_t o = a.offsets[s.seq], e = min((int64_t)a.offsets[s.seq + 1], a.N);
+  const int64_t pos = (number + 1) << a.log;
+  int64_t o, e;
+  if (a.M < kWave) {  // every offset in a lane
+    const int32_t v = lane <= a.M ? a.offsets[lane] : 0x7fffffff;
+    s.seq = __popcll(__ballot(v <= (int32_t)pos)) - 1;
+    if (s.seq < 0 || s.seq >= a.M) return false;
+    o = lane_at(v, s.seq);
+    e = lane_at(v, s.seq + 1);
+  } else {
+    s.seq = wave_upper_bound(a.offsets, a.M + 1, (int32_t)pos, lane) - 1;
+    if (s.seq < 0 || s.seq >= a.M) return false;
+    o = a.offsets[s.seq];
+    e = a.offsets[s.seq + 1];
+  }
+  e = min(e, a.N);
+  const int64_t L = (int64_t)1 << a.log;
   if (pos == o) return false;
-  s.begin = o + (pos - o + a.L - 1) / a.L * a.L;
+  s.begin = o + ((pos - o + L - 1) & -L);
   if (s.begin >= e) return false;
-  s.end = min(s.begin + a.L, e);
+  s.end = min(s.begin + L, e);
   s.first = false;
   s.last = s.end == e;
   return true;
@@ -178,7 +191,7 @@ __device__ __forceinline__ bool segment(const Args& a, int64_t number, int lane,
   s.seq = (int32_t)(number - a.bounds);
   const int64_t e = min((int64_t)a.offsets[s.seq + 1], a.N);
   s.begin = min((int64_t)a.offsets[s.seq], e);
-  s.end = min(s.begin + a.L, e);
+  s.end = min(s.begin + ((int64_t)1 << a.log), e);
   s.first = true;
   s.last = s.end == e;
   return true;
@@ -277,22 +290,9 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
   float* const s_fade = lds.fade;
   const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave), l = lane % 16, q = lane / 16;
   constexpr bool rev = REV;
-  Segment s;
-  if (OUT ? !segment(args, number, lane, s) : !boundary(args, number, lane, s)) return;
-  if (!OUT && !rev) {  // the segment before
-    s.end = s.begin;
-    s.begin -= args.L;
-  }
-  const float g = args.decay[group];
-  for (int i = threadIdx.x; i < 2 * C; i += kThreads) {
-    if (i <= C) s_pow[i] = (float)power(g, i);
-    const int far = C - (rev ? 0 : 1) - i;
-    s_fade[i] = far >= 0 ? f.u_scale * (float)power(g, far) : 0.f;
-  }
   constexpr int size = sizeof(Value);
   const int c0 = slice * DC, wc = min(DC, f.dc - c0), n0 = 16 * TN * wave;
   const int64_t states = (int64_t)args.groups * args.state, mine = (int64_t)group * args.state;
-  const int heads = OUT || rev ? args.per : 1, length = (int)(s.end - s.begin);
   // The matrices' places stay in scalar registers (loaded again from the arguments in every step, they would be waited for),
   // from the group's columns on: heads are `apart` bytes from one another.
   struct Place {
@@ -308,6 +308,15 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
               pc = place_of(f.c, f.dc, rev, c0), po = OUT ? place_of(f.out, f.dc, !rev, c0) : Place{};
   int da = f.da;
   asm volatile("" : "+s"(da));
+  // (what a block waits for at its begin, one after another: the offsets, then rows and states; the rest on the way)
+  const float g = args.decay[group];
+  Segment s;
+  if (OUT ? !segment(args, number, lane, s) : !boundary(args, number, lane, s)) return;
+  if (!OUT && !rev) {  // the segment before
+    s.end = s.begin;
+    s.begin -= (int64_t)1 << args.log;
+  }
+  const int heads = OUT || rev ? args.per : 1, length = (int)(s.end - s.begin);
   auto chunk = [&](const Place& m, int at, int h, int n, int w, bool wanted) {
     return Chunk(m.p + h * m.apart, m.ld, rev ? s.end - at - n : s.begin + at, n, w * size, rev, wanted);
   };
@@ -333,7 +342,7 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
   const float* from = nullptr;
   if constexpr (OUT) {
     if (rev ? s.last : s.first) from = f.begin != nullptr ? f.begin + s.seq * states + mine : nullptr;
-    else from = f.bounds + ((rev ? s.end : s.begin) / args.L - 1) * states + mine;
+    else from = f.bounds + (((rev ? s.end : s.begin) >> args.log) - 1) * states + mine;
     if (from != nullptr) {
       const auto base = from_base(from, 4 * (int)args.state);
 #pragma unroll
@@ -352,6 +361,14 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
       rc.put(s_c, LC);
     }
   };
+  // (a power for every exponent from C down)
+  for (int i = threadIdx.x; i < 2 * C; i += kThreads) {
+    const int at = i - (rev ? 0 : 1);
+    const float v = i <= C ? (float)power(g, C - i) : 0.f;
+    if (i <= C) s_pow[C - i] = v;
+    if (at >= 0) s_fade[at] = f.u_scale * v;
+    if (i == 2 * C - 1 && !rev) s_fade[i] = 0.f;
+  }
   put(0);
   __syncthreads();
   // Weights of the products that a lane makes, in row l % 16 of a tile, columns 4 q ..: in one on the diagonal, in the one
@@ -620,10 +637,10 @@ __global__ __launch_bounds__(kThreads) void k_linear_chain(Args a, const float* 
   // one block a sequence: its first boundary's
   if (!boundary(a, number, lane, s)) return;
   const int64_t o = a.offsets[s.seq], e = min((int64_t)a.offsets[s.seq + 1], a.N);
-  if (s.begin - o != a.L || i >= a.state) return;
-  const int64_t count = (e - o - 1) / a.L, states = (int64_t)a.groups * a.state;
+  if (s.begin - o != (int64_t)1 << a.log || i >= a.state) return;
+  const int64_t count = (e - o - 1) >> a.log, states = (int64_t)a.groups * a.state;
   const float g = a.decay[group];
-  const float whole = (float)power(g, a.L), part = (float)power(g, e - o - count * a.L);
+  const float whole = (float)power(g, (int64_t)1 << a.log), part = (float)power(g, e - o - (count << a.log));
   float* p = a.sums + number * states + group * a.state + i;
   float v[V] = {};
   if (begin != nullptr) {
@@ -651,13 +668,15 @@ __global__ __launch_bounds__(kThreads) void k_linear_chain(Args a, const float* 
 
 // ---------------------------------------------------------------- host
 
-// Segments: as long as it takes for no more than this many blocks of sums, twice as long each time.
-constexpr int64_t kMinLength = 64, kMaxBlocks = 512;
+// Segments: a chunk of 64 positions, or twice as long until there are no more blocks of sums than the device holds at
+// once (two a compute unit).
+constexpr int kMinLog = 6;
+constexpr int64_t kMaxBlocks = 512;
 int64_t most_bounds(int groups) { return groups >= kMaxBlocks ? 1 : kMaxBlocks / groups; }
-int64_t length_for(int64_t N, int groups) {
-  int64_t L = kMinLength;
-  while (N > 0 && (N - 1) / L > most_bounds(groups)) L *= 2;
-  return L;
+int log_length(int64_t N, int groups) {
+  int log = kMinLog;
+  while (N > 0 && (N - 1) >> log > most_bounds(groups)) ++log;
+  return log;
 }
 
 // Columns of c that a block takes, and the widest a and b of the kernel that does (rows that are not aligned are for any
@@ -717,8 +736,8 @@ void prepare(const LinLaunch& p, Args& a) {
   a.offsets = p.offsets;
   a.decay = p.decay;
   a.state = (int64_t)p.dk * p.dv;
-  a.L = length_for(p.N, p.groups);
-  a.bounds = p.N > 0 ? (p.N - 1) / a.L : 0;
+  a.log = log_length(p.N, p.groups);
+  a.bounds = p.N > 0 ? (p.N - 1) >> a.log : 0;
 }
 // whether every grid is one (states are taken in pieces of 256 values or more)
 bool fits(const Args& a) {
@@ -762,7 +781,7 @@ hipError_t backward(const LinLaunch& p, hipStream_t s) {
 }  // namespace
 
 size_t lin_states_bytes(int64_t N, int32_t groups, int32_t dk, int32_t dv) {
-  const int64_t most = most_bounds(groups), need = N > 0 ? (N - 1) / kMinLength : 0;
+  const int64_t most = most_bounds(groups), need = N > 0 ? (N - 1) >> kMinLog : 0;
   return align256(sizeof(float) * (size_t)(need < most ? need : most) * (size_t)groups * (size_t)dk * (size_t)dv);
 }
 
