@@ -596,12 +596,12 @@ emb_status emb_dropout(int64_t rows, int32_t dim, float drop, uint64_t seed, int
  * heads / groups query heads share a key head.  Sequence m holds positions
  * offsets[m] .. offsets[m+1]-1 as in emb_scan; rows from offsets[num_seqs] on
  * are neither read nor written.  Inputs and outputs are of one type, fp32 or bf16.
- * States and sums are fp32; with bf16 rows, weights within a chunk of 64
- * positions, and the state and what it gets of a row within a segment, are
- * rounded to bf16 where rows are multiplied with them, but never where a state
- * is kept from one segment or call to the next.  An infinity or NaN in a row spoils the
- * results of its sequence from its chunk's first position on (in the
- * backward also those before it).
+ * States and sums are fp32.  With bf16 rows, weights within a chunk of 64
+ * positions, and the state, are rounded to bf16 where rows are multiplied with
+ * them, and what the state gets of a row to 16 bits within a segment; a state
+ * that is kept from one segment or call to the next gets it with 24.  An
+ * infinity or NaN in a row spoils results of its sequence alone: from its
+ * chunk's first position on, in the backward also those before it.
  * EMB_EUNSUPPORTED for dk or dv above 256, and for rows of more than 16 MB from
  * one to the next. */
 typedef struct {
@@ -624,7 +624,7 @@ size_t emb_linear_states_size(int64_t num_tokens, int32_t groups, int32_t dk, in
 /* y: N rows of heads * dv columns.  last: device fp32 [M][groups][dk][dv],
  * the state after each sequence (first or zero for an empty one), or NULL.
  * states: device, 256-byte aligned, states_bytes >= emb_linear_states_size.
- * Outputs may not overlap inputs. */
+ * Outputs may not overlap inputs (EMB_EINVAL where they begin at one). */
 emb_status emb_linear_fwd(const emb_heads* heads, const emb_mat* y, float* last, void* states, size_t states_bytes,
                           void* stream);
 
@@ -634,7 +634,7 @@ emb_status emb_linear_fwd(const emb_heads* heads, const emb_mat* y, float* last,
  *   dk_t = v_t dS_t^T,  dv_t = k_t dS_t,  dfirst[m] = decay dS at the first
  *   position (dlast[m] if empty)
  * dq, dk, dv: as q, k, v.  dlast, dfirst: as last, each may be NULL.  decay is
- * a constant.  ws: like states. */
+ * a constant.  ws: like states.  Outputs may not overlap inputs, as above. */
 emb_status emb_linear_bwd(const emb_heads* heads, const void* states, size_t states_bytes, const emb_mat* dy,
                           const emb_mat* dq, const emb_mat* dk, const emb_mat* dv, const float* dlast, float* dfirst,
                           void* ws, size_t ws_bytes, void* stream);
@@ -643,7 +643,7 @@ emb_status emb_linear_bwd(const emb_heads* heads, const void* states, size_t sta
  * emb_scan_step: row i's state is state[slots[i]] (device fp32, num_slots of
  * groups x dk x dv values, updated in place; slots NULL: slot i).  A token whose slot lies
  * outside 0..num_slots-1 gets zeros and touches no state.  Slots must be
- * distinct.  All in fp32. */
+ * distinct, and y may not overlap the inputs.  Arithmetic is fp32. */
 emb_status emb_linear_step(int64_t num_tokens, int32_t heads, int32_t groups, int32_t dk, int32_t dv, const emb_mat* q,
                            const emb_mat* k, const emb_mat* v, const float* decay, float scale, float* state,
                            int64_t num_slots, const int32_t* slots, const emb_mat* y, void* stream);

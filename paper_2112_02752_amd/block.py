@@ -48,6 +48,19 @@ def _declare(L) -> None:
 _SEED = (1 << 64) - 1
 
 
+def _device_now() -> int:
+    import torch
+    return torch.cuda.current_device()
+
+
+def _here(*mats) -> None:
+    """A call runs on the current device: its matrices have to lie there."""
+    now = _device_now()
+    for m in mats:
+        if m is not None and m.tensor.get_device() != now:
+            raise ValueError("matrices lie on the current device (torch.cuda.device chooses it)")
+
+
 # ---------------------------------------------------------------- norm
 
 class Norm:
@@ -59,7 +72,8 @@ class Norm:
 
     ``weight`` is a contiguous fp32 vector on the GPU, the caller's.  ``drop``
     is the share dropped; its mask follows from the ``seed`` that a call gives,
-    so the backward is given the forward's.  ``max_rows`` sizes the weight
+    so the backward is given the forward's (and a captured call keeps the one it
+    was captured with).  ``max_rows`` sizes the weight
     gradient's workspace (0: no weight gradient).  Calls with a weight gradient
     on one object must be ordered."""
 
@@ -109,6 +123,7 @@ class Norm:
             saved = _mat(saved.mat)
             _want(saved, n, D, "saved")
         refs.append(saved)
+        _here(x, *refs)
         self._take(seed, first_row)
         _check("emb_norm_fwd", lib().emb_norm_fwd(n, D, self._ref, x.ref,
                                                   *(m.ref if m is not None else None for m in refs), _stream(stream)))
@@ -122,17 +137,18 @@ class Norm:
         n, D = total.rows, self.dim
         _want(total, n, D, "total")
         _want(dy, n, D, "dy")
-        refs = []
+        mats = []
         for m, name in ((arriving, "arriving"), (dtotal, "dtotal"), (branch, "branch")):
             if m is not None:
                 m = _mat(m)
                 _want(m, n, D, name)
-            refs.append(m.ref if m is not None else None)
+            mats.append(m)
+        _here(total, dy, *mats)
         if dweight is not None and n > self.max_rows:
             raise ValueError("batch larger than the norm's workspace")
         self._take(seed, first_row)
         _check("emb_norm_bwd", lib().emb_norm_bwd(
-            n, D, self._ref, total.ref, dy.ref, *refs, _floats(dweight, (D,), "dweight"), int(add), self._ws,
+            n, D, self._ref, total.ref, dy.ref, *(m.ref if m is not None else None for m in mats), _floats(dweight, (D,), "dweight"), int(add), self._ws,
             self._wsb, _stream(stream)))
 
 
@@ -143,6 +159,7 @@ def dropout(x, y, drop: float, seed: int, first_row: int = 0, stream=None) -> No
     same call on dy.  y may be x."""
     x, y = _mat(x), _mat(y)
     _want(y, x.rows, x.cols, "y")
+    _here(x, y)
     _check("emb_dropout", lib().emb_dropout(x.rows, x.cols, drop, seed & _SEED, first_row, x.ref, y.ref,
                                             _stream(stream)))
 
@@ -237,6 +254,7 @@ class LinearAttention:
         ref = self._take(heads)
         y = _mat(y)
         _want(y, heads.tokens, self.heads * self.dv, "y")
+        _here(heads.q, heads.k, heads.v, y)
         self._tokens = None
         _check("emb_linear_fwd", lib().emb_linear_fwd(ref, y.ref, _floats(last, heads.states, "last"), self._states,
                                                       self._size, _stream(stream)))
@@ -253,6 +271,7 @@ class LinearAttention:
         for m, cols, name in zip(mats, (self.heads * self.dv, self.heads * self.dk, self.groups * self.dk,
                                         self.groups * self.dv), ("dy", "dq", "dk", "dv")):
             _want(m, heads.tokens, cols, name)
+        _here(heads.q, heads.k, heads.v, *mats)
         _check("emb_linear_bwd", lib().emb_linear_bwd(
             ref, self._states, self._size, *(m.ref for m in mats), _floats(dlast, heads.states, "dlast"),
             _floats(dfirst, heads.states, "dfirst"), self._ws, self._size, _stream(stream)))
@@ -269,6 +288,7 @@ def linear_attention_step(q, k, v, decay, state, y, heads: int, groups: Optional
     dk, dv = _head_widths(q, k, v, heads, groups)
     n = k.rows
     _want(y, n, heads * dv, "y")
+    _here(q, k, v, y)
     rows = int(state.shape[0])
     sp = None
     if slots is not None:
@@ -323,6 +343,7 @@ class LogProbs:
         _want(logits, n, self.cols, "logits")
         if n > self.max_rows:
             raise ValueError("more rows than there is room for")
+        _here(logits)
         return (logits, n) + (_ids(ids, n) if ids is not None else (None, 4))
 
     def forward(self, logits, ids, logp, entropy=None, top_ids=None, top_logp=None, stream=None) -> None:
@@ -353,6 +374,7 @@ class LogProbs:
             raise ValueError("backward follows the forward of the same rows")
         dlogits = _mat(dlogits)
         _want(dlogits, n, self.cols, "dlogits")
+        _here(dlogits)
         _check("emb_logp_bwd", lib().emb_logp_bwd(
             n, self.cols, logits.ref, at, size, self.scale, self._stats, _floats(dlogp, (n,), "dlogp"),
             _floats(dentropy, (n,), "dentropy"), dlogits.ref, _stream(stream)))
@@ -363,6 +385,7 @@ class LogProbs:
         logits, n, at, size = self._take(logits, ids)
         dlogits = _mat(dlogits)
         _want(dlogits, n, self.cols, "dlogits")
+        _here(dlogits)
         _check("emb_logp_train", lib().emb_logp_train(
             n, self.cols, logits.ref, at, size, self.scale, _floats(dlogp, (n,), "dlogp"), _floats(logp, (n,), "logp"),
             _floats(entropy, (n,), "entropy"), dlogits.ref, _stream(stream)))

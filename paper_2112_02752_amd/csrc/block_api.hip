@@ -101,6 +101,11 @@ emb_status check_heads(const emb_heads* h, LinLaunch* p) {
   return EMB_OK;
 }
 
+// whether a written matrix begins where one that is read does
+bool meets(const Rows& out, const LinLaunch& p) {
+  return out.p == p.q.p || out.p == p.k.p || out.p == p.v.p || (p.dy.p != nullptr && out.p == p.dy.p);
+}
+
 emb_status check_states(const LinLaunch& p, const void* at, size_t bytes) {
   const size_t need = lin_states_bytes(p.N, p.groups, p.dk, p.dv);
   if (need > 0 && at == nullptr) return EMB_EINVAL;
@@ -233,6 +238,7 @@ emb_status emb_linear_fwd(const emb_heads* heads, const emb_mat* y, float* last,
     if (y->dtype != p.dtype) return EMB_EINVAL;
     p.y = rows_of(*y);
     if (long_rows(p.y)) return EMB_EUNSUPPORTED;
+    if (meets(p.y, p)) return EMB_EINVAL;
     p.aligned = p.aligned && vectors(p.y);
   }
   if ((st = check_states(p, states, states_bytes)) != EMB_OK) return st;
@@ -248,7 +254,8 @@ emb_status emb_linear_bwd(const emb_heads* heads, const void* states, size_t sta
   LinLaunch p{};
   emb_status st = check_heads(heads, &p);
   if (st != EMB_OK) return st;
-  if ((((uintptr_t)dlast | (uintptr_t)dfirst) & 3u) != 0 || (dfirst != nullptr && dfirst == dlast)) return EMB_EINVAL;
+  if ((((uintptr_t)dlast | (uintptr_t)dfirst) & 3u) != 0 || (dfirst != nullptr && (dfirst == dlast || dfirst == heads->first)))
+    return EMB_EINVAL;
   if (p.N > 0) {
     const emb_mat* all[4] = {dy, dq, dk, dv};
     const int32_t cols[4] = {p.heads * p.dv, p.heads * p.dk, p.groups * p.dk, p.groups * p.dv};
@@ -258,6 +265,7 @@ emb_status emb_linear_bwd(const emb_heads* heads, const void* states, size_t sta
       if (all[i]->dtype != p.dtype) return EMB_EINVAL;
       *to[i] = rows_of(*all[i]);
       if (long_rows(*to[i])) return EMB_EUNSUPPORTED;
+      if (i > 0 && meets(*to[i], p)) return EMB_EINVAL;
       p.aligned = p.aligned && vectors(*to[i]);
     }
   }

@@ -387,8 +387,8 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
 #pragma unroll
     for (int i = 0; i < 2 * kSide - 1; ++i) less[i] = lane_at(s_pow[16 * max(ti - tj + i - kSide, 0)], 0);
   }
-  // A state that is kept gets weighted rows with all of their bits; one that only multiplies rows of this segment is
-  // rounded to theirs for that, and gets them rounded so.
+  // A state that is kept gets weighted rows with all of their 24 bits, in three parts; one that only multiplies rows of this
+  // segment, and is rounded to bf16 for that, gets 16 of them.
   const bool exact = f.end != nullptr && (rev ? s.first : s.last);
   f32x4 o[TC][TN];
   for (int at = 0; at < length; at += C) {
@@ -413,8 +413,8 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
           else *reinterpret_cast<f32x4*>(to) = p;
         };
         if (new_a) {
-          // What the state before the chunk gives (lane l: row 16 i + l % 16), and on the way, as the rows of a are there,
-          // their products with 16 rows of b a wavefront, for LDS.  (Tiles above the diagonal are zeros.)
+          // What the state before the chunk gives (lane l: row 16 i + l % 16), and in order on the way, as the rows of a are
+          // there, their products with 16 rows of b a wavefront, for LDS.  (Tiles above the diagonal are zeros.)
           f32x4 p[TC];
 #pragma unroll
           for (int i = 0; i < TC; ++i) {
@@ -425,14 +425,14 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
 #pragma unroll
           for (int k = 0; k < KD; ++k) {
             Op x[TN], z;
-            z.row_as_state(s_b + (16 * (wave % TC) + l) * LB + k * KB, q);
+            if constexpr (!rev) z.row_as_state(s_b + (16 * (wave % TC) + l) * LB + k * KB, q);
 #pragma unroll
             for (int t = 0; t < TN; ++t) x[t].state(st[k * KB / 16][t], st[(k * KB / 16 + 1) % TD][t]);
 #pragma unroll
             for (int i = 0; i < TC; ++i) {
               Op y;
               y.row_as_state(s_a + (16 * i + l) * LA + k * KB, q);
-              mul(p[i], z, y);
+              if constexpr (!rev) mul(p[i], z, y);
 #pragma unroll
               for (int t = 0; t < TN; ++t) mul(o[i][t], x[t], y);
             }
@@ -442,10 +442,12 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
             const float w = s_pow[16 * i + l + (rev ? 0 : 1)];
 #pragma unroll
             for (int t = 0; t < TN; ++t) o[i][t] *= w;
-            if (wave < TC) put_products(p[i], i, wave, before[i]);
+            if (!rev && wave < TC) put_products(p[i], i, wave, before[i]);
           }
-        } else if (square < kSquares) {
-          // products alone: kSide x kSide tiles a wavefront, of the squares on and below the diagonal
+        }
+        if (rev && square < kSquares) {
+          // backwards, where rows of b are new in every step: kSide x kSide tiles a wavefront, of the squares on and below
+          // the diagonal
           f32x4 p[kSide][kSide];
 #pragma unroll
           for (int i = 0; i < kSide; ++i)
@@ -549,17 +551,18 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
 #pragma unroll
             for (int e = 0; e < Op::kEach; ++e) w[e] = s_fade[j + e];
           }
-          float v[TN][Op::kEach];
+          // parts `from` up to `to` of the rows times their weights
+          auto add = [&](auto from, auto to) {
+            constexpr int F = decltype(from)::value, P = decltype(to)::value;
+            Op x[TN][P];
 #pragma unroll
-          for (int t = 0; t < TN; ++t)
+            for (int t = 0; t < TN; ++t) {
+              float v[Op::kEach];
 #pragma unroll
-            for (int e = 0; e < Op::kEach; ++e) v[t][e] = c[k][t].get(e) * w[e];
-          if constexpr (!OUT) {
-            Op x[TN][Op::kParts];
+              for (int e = 0; e < Op::kEach; ++e) v[e] = c[k][t].get(e) * w[e];
 #pragma unroll
-            for (int t = 0; t < TN; ++t)
-#pragma unroll
-              for (int p = 0; p < Op::kParts; ++p) x[t][p].take(v[t]);
+              for (int p = 0; p < P; ++p) x[t][p].take(v);
+            }
 #pragma unroll
             for (int d = 0; d < TD; ++d) {
               Op y;
@@ -567,24 +570,15 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
 #pragma unroll
               for (int t = 0; t < TN; ++t)
 #pragma unroll
-                for (int p = 0; p < Op::kParts; ++p) mul(st[d][t], y, x[t][p]);
+                for (int p = F; p < P; ++p) mul(st[d][t], y, x[t][p]);
             }
+          };
+          using std::integral_constant;
+          if constexpr (!OUT || Op::kParts == 1) {
+            add(integral_constant<int, 0>{}, integral_constant<int, Op::kParts>{});
           } else {
-            // (a loop: registers do not hold the parts together)
-            int left = exact ? Op::kParts : 1;
-#pragma unroll 1
-            do {
-              Op x[TN];
-#pragma unroll
-              for (int t = 0; t < TN; ++t) x[t].take(v[t]);
-#pragma unroll
-              for (int d = 0; d < TD; ++d) {
-                Op y;
-                y.template column<LB>(s_b + k * KB * LB + 16 * d, q, l);
-#pragma unroll
-                for (int t = 0; t < TN; ++t) mul(st[d][t], y, x[t]);
-              }
-            } while (--left > 0);
+            add(integral_constant<int, 0>{}, integral_constant<int, 2>{});
+            if (exact) add(integral_constant<int, 2>{}, integral_constant<int, Op::kParts>{});
           }
         }
       }
@@ -740,10 +734,10 @@ void prepare(const LinLaunch& p, Args& a) {
   a.bounds = p.N > 0 ? (p.N - 1) >> a.log : 0;
 }
 // whether every grid is one (states are taken in pieces of 256 values or more)
-bool fits(const Args& a) {
+bool fits(const Args& a, int forms) {
   int slices = 1;
   for (int i = 0; i < 3; ++i) slices = a.slices[i] > slices ? a.slices[i] : slices;
-  return launchable((a.bounds + a.M) * a.groups * slices * 3, kThreads) &&
+  return launchable((a.bounds + a.M) * a.groups * slices * forms, kThreads) &&
          launchable(a.bounds * a.groups * ((a.state + kThreads - 1) / kThreads), kThreads);
 }
 
@@ -753,7 +747,7 @@ hipError_t forward(const LinLaunch& p, hipStream_t s) {
   prepare(p, a);
   a.sums = p.states;
   add_form(a, 0, Form{p.q, p.k, p.v, p.y, p.states, p.first, p.last, p.dk, p.dv, p.dv, 1, 0, 1.f, 1.f, p.scale});
-  if (!fits(a)) return hipErrorNotSupported;
+  if (!fits(a, 1)) return hipErrorNotSupported;
   hipError_t e = go<T, false>(a, 0, 1, s);
   if (e == hipSuccess) e = chain<false>(a, p.first, s);
   if (e == hipSuccess) e = go<T, true>(a, 0, 1, s);
@@ -768,7 +762,7 @@ hipError_t backward(const LinLaunch& p, hipStream_t s) {
   add_form(a, 0, Form{p.k, p.q, p.dy, p.dval, p.grads, p.dlast, p.dfirst, p.dk, p.dv, p.dv, 1, 1, p.scale, p.scale, 1.f});
   add_form(a, 1, Form{p.v, p.dy, p.q, p.dkey, p.grads, p.dlast, nullptr, p.dv, p.dk, 1, p.dv, 1, p.scale, p.scale, 1.f});
   add_form(a, 2, Form{p.dy, p.v, p.k, p.dq, p.states, p.first, nullptr, p.dv, p.dk, 1, p.dv, 0, 1.f, 1.f, p.scale});
-  if (!fits(a)) return hipErrorNotSupported;
+  if (!fits(a, 3)) return hipErrorNotSupported;
   hipError_t e = go<T, false>(a, 0, 1, s);
   if (e == hipSuccess) e = chain<true>(a, p.dlast, s);
   // (dk and dq have the same widths; with dv's too they are one launch, whose last blocks fill the device better)

@@ -113,7 +113,7 @@ def test_norm_of_the_binding():
         emb.Norm(torch.ones(16)[::2])
 
 
-def _heads(n=100, m=3, heads=4, groups=2, dk=16, dv=8, offsets=0x2000, q=None, k=None, v=None, decay=0x3000, scale=1.0,
+def _heads(n=60, m=3, heads=4, groups=2, dk=16, dv=8, offsets=0x2000, q=None, k=None, v=None, decay=0x3000, scale=1.0,
            first=None):
     return CHeads(n, m, heads, groups, dk, dv, offsets, q or _m(), k or _m(), v or _m(), decay, scale, first)
 
@@ -131,15 +131,15 @@ BAD_HEADS = [(dict(n=-1), EINVAL), (dict(m=-1), EINVAL), (dict(m=0), EINVAL), (d
 
 def test_linear_attention_refusals():
     size = emb.lib().emb_linear_states_size
-    assert size(100, 2, 16, 8) == 0 and size(257, 2, 16, 8) == 1024
-    assert size(1 << 30, 2, 16, 8) == 512 * 1024            # segments grow instead
+    assert size(64, 2, 16, 8) == 0 and size(65, 2, 16, 8) == 1024
+    assert size(1 << 30, 2, 16, 8) == 256 * 1024            # segments grow instead
     for bad in ((-1, 2, 16, 8), (1 << 31, 2, 16, 8), (10, 0, 16, 8), (10, 2, 0, 8), (10, 2, 16, 257)):
         assert size(*bad) == 0
 
-    def fwd(h=None, y=_m(), last=0x5000, states=0x100000, bytes_=0):
+    def fwd(h=None, y=_m(0x7000), last=0x5000, states=0x100000, bytes_=0):
         return emb.lib().emb_linear_fwd(_ref(h or _heads()), _ref(y), last, states, bytes_, None)
 
-    def bwd(h=None, dy=_m(), dq=_m(), dk=_m(), dv=_m(), states=0x100000, bytes_=0, dlast=0x5000, dfirst=0x6000,
+    def bwd(h=None, dy=_m(0x7000), dq=_m(0x8000), dk=_m(0x9000), dv=_m(0xa000), states=0x100000, bytes_=0, dlast=0x5000, dfirst=0x6000,
             ws=0x200000, wsb=0):
         return emb.lib().emb_linear_bwd(_ref(h or _heads()), states, bytes_, _ref(dy), _ref(dq), _ref(dk), _ref(dv),
                                         dlast, dfirst, ws, wsb, None)
@@ -154,8 +154,17 @@ def test_linear_attention_refusals():
     assert fwd(y=_m(ld=31)) == EINVAL
     assert fwd(y=_m(dtype=1)) == EINVAL
     assert fwd(last=0x5001) == EINVAL
+    assert fwd(y=_m(0x4000)) == EINVAL                     # over an input
+    far = _m(0x7000, (1 << 22) + 4)
+    assert fwd(y=far) == EUNSUPPORTED                      # rows of more than 16 MB
+    assert fwd(_heads(k=far)) == EUNSUPPORTED
+    assert bwd(dk=far) == EUNSUPPORTED
+    for name in ("dq", "dk", "dv"):
+        for over in (0x4000, 0x7000):
+            assert bwd(**{name: _m(over)}) == EINVAL
+    assert bwd(_heads(first=0x6000)) == EINVAL             # first states' gradient over them
     assert fwd(_heads(first=0x5000), last=0x5000) == EINVAL
-    long = _heads(n=257)
+    long = _heads(n=65)
     assert fwd(long, bytes_=1023) == EWORKSPACE
     assert fwd(long, states=0x100010, bytes_=1024) == EWORKSPACE
     assert fwd(long, states=None, bytes_=1024) == EINVAL
@@ -246,3 +255,31 @@ def test_linear_attention_of_the_binding():
             emb.Heads(bad, None, None, None, None, heads=2)
     with pytest.raises(ValueError, match="GPU"):
         emb.Heads(torch.zeros(3, dtype=torch.int32), None, None, None, None, heads=2)
+
+
+def test_matrices_of_another_device(monkeypatch):
+    """Refused before the library is called."""
+    import torch
+    from paper_2112_02752_amd import block
+
+    class Stub(emb.Mat):
+        """A matrix without a GPU."""
+
+        def __init__(self, rows, cols, device):
+            self.tensor, self.exps, self.rows, self.cols = self, None, rows, cols
+            self._at, self.device, self._c = 0, device, CMat()
+            self.ref = ctypes.byref(self._c)
+
+        def data_ptr(self):
+            return 0
+
+        def get_device(self):
+            return self.device
+
+    monkeypatch.setattr(block, "_device_now", lambda: 1)
+    with pytest.raises(ValueError, match="current device"):
+        emb.dropout(Stub(4, 8, 0), Stub(4, 8, 1), 0.1, 1)
+    with pytest.raises(ValueError, match="current device"):
+        emb.dropout(Stub(4, 8, 1), Stub(4, 8, 0), 0.1, 1)
+    with pytest.raises(ValueError, match="current device"):
+        emb.linear_attention_step(Stub(4, 8, 1), Stub(4, 8, 1), Stub(4, 8, 0), None, torch.zeros(4), Stub(4, 8, 1), 2)

@@ -10,9 +10,9 @@ rows and powers of the decay; with |.| for the same sums of magnitudes:
    roundings (power, product) for each chunk of 32 or 64 positions: (T + width + 32) 2u |.|
    with T the longest sequence and the wider head;
  - bf16 rows: a term within a chunk has its weight rounded to bf16, one from
-   before it the state, which itself has got rows times weights that were rounded so since
-   the segment's begin: (2 * 2^-8 + 2^-16) |.|; the result is rounded, 2^-8 of it.  States
-   that are kept get weighted rows with 24 bits: as fp32, u more.
+   before it the state, 2^-8 |.|; that has got rows times weights with 16 bits
+   since the segment's begin, 2^-16 |.|; the result is rounded, 2^-8 of it.  States that are
+   kept get weighted rows with 24 bits: as fp32, u more.
 """
 import numpy as np
 import pytest
@@ -93,7 +93,7 @@ class Batch:
         low = self.kind == "bf16"
         for got, want, size, name in ((self.y, y, ya, "y"), (self.dq, dq, dqa, "dq"), (self.dk, dkey, dka, "dk"),
                                       (self.dv, dval, dva, "dv")):
-            bound = (near + (2.0 ** -7 + 2.0 ** -16 if low else 0)) * size + HALF[self.kind] * np.abs(want)
+            bound = (near + (2.0 ** -8 + 2.0 ** -16 if low else 0)) * size + HALF[self.kind] * np.abs(want)
             within(host(got)[:n].reshape(want.shape), want, bound, name)
         for got, want, size, name in ((self.last, last, lasta, "last"), (self.dfirst, dfirst, dfirsta, "dfirst")):
             within(got, want, (near + U) * size, name)
@@ -253,7 +253,7 @@ def test_tokens_one_by_one_continue_a_prompt(kind):
         emb.linear_attention_step(b.q[i:i + 1], b.k[i:i + 1], b.v[i:i + 1], b.decay, state, y, heads=h, groups=g,
                                   scale=b.scale)
         size = b.scale * (np.abs(q[i]).reshape(g, h // g, dk) @ every[i]).reshape(1, -1)
-        near = 2 * (305 + 64 + 32) * 2 * U + (2.0 ** -7 + 2.0 ** -16 if kind == "bf16" else 0)
+        near = 2 * (305 + 64 + 32) * 2 * U + (2.0 ** -8 + 2.0 ** -16 if kind == "bf16" else 0)
         within(y, host(whole[i:i + 1]), near * size + 2 * HALF[kind] * np.abs(host(whole[i:i + 1])), i)
 
 
