@@ -270,11 +270,11 @@ struct Room {
   alignas(16) float fade[2 * C], pow[C + 1];
 };
 
-// DA: widest a and b; DC: columns of c that a block takes.  OUT: the form itself, else the sums of the segment that ends
-// (backwards: begins) at a boundary.
+// DA: widest a and b; DC: columns of c that a block takes; head: one of the group's (in order), or all (-1).  OUT: the form
+// itself, else the sums of the segment that ends (backwards: begins) at a boundary.
 template <typename T, int DA, int DC, int W, bool OUT, bool ALIGNED, bool REV>
 __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t number, int group, int slice,
-                                      Room<T, DA, DC, OUT>& lds) {
+                                      int head, Room<T, DA, DC, OUT>& lds) {
   typedef Operand<T> Op;
   typedef typename Op::Value Value;
   constexpr int C = Op::kChunk, KB = Op::kBlock, TC = C / 16, TD = DA / 16, KC = C / KB, KD = DA / KB;
@@ -316,20 +316,27 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
     s.end = s.begin;
     s.begin -= (int64_t)1 << args.log;
   }
-  const int heads = OUT || rev ? args.per : 1, length = (int)(s.end - s.begin);
+  const int length = (int)(s.end - s.begin);
+  const int begin = max(head, 0), until = head >= 0 ? head + 1 : OUT || rev ? args.per : 1;  // heads
   auto chunk = [&](const Place& m, int at, int h, int n, int w, bool wanted) {
     return Chunk(m.p + h * m.apart, m.ld, rev ? s.end - at - n : s.begin + at, n, w * size, rev, wanted);
   };
+  // A step is a head of a chunk; its rows are on their way while the one before it is worked on.
+  struct Step {
+    int at, h;
+  };
+  auto after = [&](Step x) { return x.h + 1 < until ? Step{x.at, x.h + 1} : Step{x.at + C, begin}; };
   Rowset<T, DA, kThreads, ALIGNED> ra, rb;
   Rowset<T, DC, kThreads, ALIGNED> rc;
   // (rows that a step does not need are loaded from nowhere: a branch around loads would wait for them at its end)
-  auto load = [&](int at, int h) {
-    const int n = min(C, length - at);
-    if constexpr (OUT) ra.load(chunk(pa, at, h, n, da, !rev || h == 0), da);
-    rb.load(chunk(pb, at, h, n, da, rev || h == 0), da);
-    rc.load(chunk(pc, at, h, n, wc, rev || h == 0), wc);
+  auto load = [&](Step x) {
+    const int n = min(C, length - x.at);
+    if constexpr (OUT) ra.load(chunk(pa, x.at, x.h, n, da, !rev || x.h == begin), da);
+    rb.load(chunk(pb, x.at, x.h, n, da, rev || x.h == begin), da);
+    rc.load(chunk(pc, x.at, x.h, n, wc, rev || x.h == begin), wc);
   };
-  load(0, 0);
+  Step now{0, begin};
+  load(now);
   // The state: lane l holds rows 16 d + 4 q .. of a column.  With two tiles of columns a wavefront, those of tile t are 8 j +
   // 4 t + (0 .. 3), so that a lane's results of both are eight values in a row.
   constexpr int kApart = 4 * TN, kTile = TN == 2 ? 4 : 16;
@@ -355,8 +362,8 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
     }
   }
   auto put = [&](int h) {
-    if (OUT && (!rev || h == 0)) ra.put(s_a, LA);
-    if (rev || h == 0) {
+    if (OUT && (!rev || h == begin)) ra.put(s_a, LA);
+    if (rev || h == begin) {
       rb.put(s_b, LB);
       rc.put(s_c, LC);
     }
@@ -369,7 +376,7 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
     if (at >= 0) s_fade[at] = f.u_scale * v;
     if (i == 2 * C - 1 && !rev) s_fade[i] = 0.f;
   }
-  put(0);
+  put(begin);
   __syncthreads();
   // Weights of the products that a lane makes, in row l % 16 of a tile, columns 4 q ..: in one on the diagonal, in the one
   // before it, and how much less those before that have
@@ -389,206 +396,207 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
   }
   // A state that is kept gets weighted rows with all of their 24 bits, in three parts; one that only multiplies rows of this
   // segment, and is rounded to bf16 for that, gets 16 of them.
-  const bool exact = f.end != nullptr && (rev ? s.first : s.last);
+  const bool exact = f.end != nullptr && begin == 0 && (rev ? s.first : s.last);
   f32x4 o[TC][TN];
-  for (int at = 0; at < length; at += C) {
-    const int n = min(C, length - at);
-    for (int h = 0; h < heads; ++h) {
-      const bool new_a = !rev || h == 0, last = h == heads - 1;
-      // (addresses are made again in every step: kept across it they take the registers that loads are on their way to)
-      int l = lane % 16, q = lane / 16;
-      asm volatile("" : "+v"(l), "+v"(q));
-      __syncthreads();
-      load(last ? at + C : at, last ? 0 : h + 1);
-      if constexpr (OUT) {
-        auto put_products = [&](f32x4 p, int i, int j, float fade) {
-          // (of tile i, j; weights of bf16 rows are rounded as the rows are: to bf16)
+  while (now.at < length) {
+    const int at = now.at, h = now.h, n = min(C, length - at);
+    const bool new_a = !rev || h == begin, last = h == until - 1;
+    // (addresses are made again in every step: kept across it they take the registers that loads are on their way to)
+    int l = lane % 16, q = lane / 16;
+    asm volatile("" : "+v"(l), "+v"(q));
+    __syncthreads();
+    const Step next = after(now);
+    load(next);
+    if constexpr (OUT) {
+      auto put_products = [&](f32x4 p, int i, int j, float fade) {
+        // (of tile i, j; weights of bf16 rows are rounded as the rows are: to bf16)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float w = i == j ? on[e] : off[e] * fade;
-            p[e] = 16 * (i - j) + l - 4 * q - e >= 0 ? p[e] * w : 0.f;
-          }
-          Value* to = s_p + (16 * i + l) * LP + 16 * j + 4 * q;
-          if constexpr (sizeof(Value) == 2) *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3])};
-          else *reinterpret_cast<f32x4*>(to) = p;
-        };
-        if (new_a) {
-          // What the state before the chunk gives (lane l: row 16 i + l % 16), and in order on the way, as the rows of a are
-          // there, their products with 16 rows of b a wavefront, for LDS.  (Tiles above the diagonal are zeros.)
-          f32x4 p[TC];
+        for (int e = 0; e < 4; ++e) {
+          const float w = i == j ? on[e] : off[e] * fade;
+          p[e] = 16 * (i - j) + l - 4 * q - e >= 0 ? p[e] * w : 0.f;
+        }
+        Value* to = s_p + (16 * i + l) * LP + 16 * j + 4 * q;
+        if constexpr (sizeof(Value) == 2) *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3])};
+        else *reinterpret_cast<f32x4*>(to) = p;
+      };
+      if (new_a) {
+        // What the state before the chunk gives (lane l: row 16 i + l % 16), and in order on the way, as the rows of a are
+        // there, their products with 16 rows of b a wavefront, for LDS.  (Tiles above the diagonal are zeros.)
+        f32x4 p[TC];
+#pragma unroll
+        for (int i = 0; i < TC; ++i) {
+          p[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int t = 0; t < TN; ++t) o[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+#pragma unroll
+        for (int k = 0; k < KD; ++k) {
+          Op x[TN], z;
+          if constexpr (!rev) z.row_as_state(s_b + (16 * (wave % TC) + l) * LB + k * KB, q);
+#pragma unroll
+          for (int t = 0; t < TN; ++t) x[t].state(st[k * KB / 16][t], st[(k * KB / 16 + 1) % TD][t]);
 #pragma unroll
           for (int i = 0; i < TC; ++i) {
-            p[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int t = 0; t < TN; ++t) o[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-          }
-#pragma unroll
-          for (int k = 0; k < KD; ++k) {
-            Op x[TN], z;
-            if constexpr (!rev) z.row_as_state(s_b + (16 * (wave % TC) + l) * LB + k * KB, q);
-#pragma unroll
-            for (int t = 0; t < TN; ++t) x[t].state(st[k * KB / 16][t], st[(k * KB / 16 + 1) % TD][t]);
-#pragma unroll
-            for (int i = 0; i < TC; ++i) {
-              Op y;
-              y.row_as_state(s_a + (16 * i + l) * LA + k * KB, q);
-              if constexpr (!rev) mul(p[i], z, y);
-#pragma unroll
-              for (int t = 0; t < TN; ++t) mul(o[i][t], x[t], y);
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < TC; ++i) {
-            const float w = s_pow[16 * i + l + (rev ? 0 : 1)];
-#pragma unroll
-            for (int t = 0; t < TN; ++t) o[i][t] *= w;
-            if (!rev && wave < TC) put_products(p[i], i, wave, before[i]);
-          }
-        }
-        if (rev && square < kSquares) {
-          // backwards, where rows of b are new in every step: kSide x kSide tiles a wavefront, of the squares on and below
-          // the diagonal
-          f32x4 p[kSide][kSide];
-#pragma unroll
-          for (int i = 0; i < kSide; ++i)
-#pragma unroll
-            for (int j = 0; j < kSide; ++j) p[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int k = 0; k < KD; ++k) {
-            Op x[kSide], y[kSide];
-#pragma unroll
-            for (int i = 0; i < kSide; ++i) {
-              x[i].row(s_b + (16 * (tj + i) + l) * LB + k * KB, q);
-              y[i].row(s_a + (16 * (ti + i) + l) * LA + k * KB, q);
-            }
-#pragma unroll
-            for (int i = 0; i < kSide; ++i)
-#pragma unroll
-              for (int j = 0; j < kSide; ++j) mul(p[i][j], x[j], y[i]);
-          }
-#pragma unroll
-          for (int i = 0; i < kSide; ++i)
-#pragma unroll
-            for (int j = 0; j < kSide; ++j) put_products(p[i][j], ti + i, tj + j, less[kSide - 1 + i - j]);
-        }
-        __syncthreads();
-      }
-      Op c[KC][TN];
-#pragma unroll
-      for (int k = 0; k < KC; ++k)
-#pragma unroll
-        for (int t = 0; t < TN; ++t) c[k][t].template column<LC, kApart>(s_c + k * KB * LC + n0 + kTile * t, q, l);
-      if constexpr (OUT) {
-#pragma unroll
-        for (int i = 0; i < TC; ++i)
-#pragma unroll
-          for (int k = 0; k <= 16 * i / KB; ++k) {
             Op y;
-            y.row(s_p + (16 * i + l) * LP + k * KB, q);
+            y.row_as_state(s_a + (16 * i + l) * LA + k * KB, q);
+            if constexpr (!rev) mul(p[i], z, y);
 #pragma unroll
-            for (int t = 0; t < TN; ++t) mul(o[i][t], c[k][t], y);
+            for (int t = 0; t < TN; ++t) mul(o[i][t], x[t], y);
           }
-        {
-          // (to nowhere where nothing is to be stored yet: as many stores follow the loads in every step, so that the
-          // wait for the loads does not take in the stores)
-          const Chunk out = chunk(po, at, h, n, wc, !rev || last);
-          const int col = n0 + kApart * q;
+        }
 #pragma unroll
-          for (int i = 0; i < TC; ++i) {
-            const uint32_t row = (uint32_t)(out.top + (l + 16 * i) * out.ld + col * size);
-            float v[4 * TN];
+        for (int i = 0; i < TC; ++i) {
+          const float w = s_pow[16 * i + l + (rev ? 0 : 1)];
+#pragma unroll
+          for (int t = 0; t < TN; ++t) o[i][t] *= w;
+          if (!rev && wave < TC) put_products(p[i], i, wave, before[i]);
+        }
+      }
+      if (rev && square < kSquares) {
+        // backwards, where rows of b are new in every step: kSide x kSide tiles a wavefront, of the squares on and below
+        // the diagonal
+        f32x4 p[kSide][kSide];
+#pragma unroll
+        for (int i = 0; i < kSide; ++i)
+#pragma unroll
+          for (int j = 0; j < kSide; ++j) p[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < KD; ++k) {
+          Op x[kSide], y[kSide];
+#pragma unroll
+          for (int i = 0; i < kSide; ++i) {
+            x[i].row(s_b + (16 * (tj + i) + l) * LB + k * KB, q);
+            y[i].row(s_a + (16 * (ti + i) + l) * LA + k * KB, q);
+          }
+#pragma unroll
+          for (int i = 0; i < kSide; ++i)
+#pragma unroll
+            for (int j = 0; j < kSide; ++j) mul(p[i][j], x[j], y[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kSide; ++i)
+#pragma unroll
+          for (int j = 0; j < kSide; ++j) put_products(p[i][j], ti + i, tj + j, less[kSide - 1 + i - j]);
+      }
+      __syncthreads();
+    }
+    Op c[KC][TN];
+#pragma unroll
+    for (int k = 0; k < KC; ++k)
+#pragma unroll
+      for (int t = 0; t < TN; ++t) c[k][t].template column<LC, kApart>(s_c + k * KB * LC + n0 + kTile * t, q, l);
+    if constexpr (OUT) {
+#pragma unroll
+      for (int i = 0; i < TC; ++i)
+#pragma unroll
+        for (int k = 0; k <= 16 * i / KB; ++k) {
+          Op y;
+          y.row(s_p + (16 * i + l) * LP + k * KB, q);
+#pragma unroll
+          for (int t = 0; t < TN; ++t) mul(o[i][t], c[k][t], y);
+        }
+      {
+        // (to nowhere where nothing is to be stored yet: as many stores follow the loads in every step, so that the
+        // wait for the loads does not take in the stores)
+        const Chunk out = chunk(po, at, h, n, wc, !rev || last);
+        const int col = n0 + kApart * q;
+#pragma unroll
+        for (int i = 0; i < TC; ++i) {
+          const uint32_t row = (uint32_t)(out.top + (l + 16 * i) * out.ld + col * size);
+          float v[4 * TN];
+#pragma unroll
+          for (int t = 0; t < TN; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * t + e] = o[i][t][e] * f.out_scale;
+          if constexpr (!ALIGNED) {
+#pragma unroll
+            for (int e = 0; e < 4 * TN; ++e) {
+              const uint32_t to = col + e < wc ? row + (uint32_t)(e * size) : kNowhere;
+              if constexpr (size == 2)
+                __builtin_amdgcn_raw_buffer_store_b16((uint16_t)pack_bf16(v[e], 0.f), out.rsrc, to, 0, 0);
+              else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[e]), out.rsrc, to, 0, 0);
+            }
+          } else {
+            // (a head's columns end at a multiple of 16 bytes)
+#pragma unroll
+            for (int e = 0; e < 4 * TN; e += 16 / size) {
+              const uint32_t to = col + e < wc ? row + (uint32_t)(e * size) : kNowhere;
+              if constexpr (size == 4) {
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]}), out.rsrc, to, 0, 0);
+              } else if constexpr (TN == 1) {
+                __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}, out.rsrc, to, 0, 0);
+              } else {
+                __builtin_amdgcn_raw_buffer_store_b128(
+                    u32x4{pack_bf16(v[e], v[e + 1]), pack_bf16(v[e + 2], v[e + 3]), pack_bf16(v[e + 4], v[e + 5]), pack_bf16(v[e + 6], v[e + 7])},
+                    out.rsrc, to, 0, 0);
+              }
+            }
+          }
+        }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    // (what a segment's last chunk leaves is only for a state that is kept)
+    if ((rev || last) && (!OUT || exact || at + C < length)) {
+      const float all = rev && h > begin ? 1.f : s_pow[n];
+#pragma unroll
+      for (int d = 0; d < TD; ++d)
+#pragma unroll
+        for (int t = 0; t < TN; ++t) st[d][t] *= all;
+#pragma unroll
+      for (int k = 0; k < KC; ++k) {
+        __builtin_amdgcn_sched_barrier(0);
+        float w[Op::kEach];
+        const int j = k * KB + Op::index(q, 0) + C - n;
+        if (n == C) {
+#pragma unroll
+          for (int e = 0; e < Op::kEach; e += 4) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(s_fade + j + e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[e + i] = v[i];
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < Op::kEach; ++e) w[e] = s_fade[j + e];
+        }
+        // parts `from` up to `to` of the rows times their weights
+        auto add = [&](auto from, auto to) {
+          constexpr int F = decltype(from)::value, P = decltype(to)::value;
+          Op x[TN][P];
+#pragma unroll
+          for (int t = 0; t < TN; ++t) {
+            float v[Op::kEach];
+#pragma unroll
+            for (int e = 0; e < Op::kEach; ++e) v[e] = c[k][t].get(e) * w[e];
+#pragma unroll
+            for (int p = 0; p < P; ++p) x[t][p].take(v);
+          }
+#pragma unroll
+          for (int d = 0; d < TD; ++d) {
+            Op y;
+            y.template column<LB>(s_b + k * KB * LB + 16 * d, q, l);
 #pragma unroll
             for (int t = 0; t < TN; ++t)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) v[4 * t + e] = o[i][t][e] * f.out_scale;
-            if constexpr (!ALIGNED) {
-#pragma unroll
-              for (int e = 0; e < 4 * TN; ++e) {
-                const uint32_t to = col + e < wc ? row + (uint32_t)(e * size) : kNowhere;
-                if constexpr (size == 2)
-                  __builtin_amdgcn_raw_buffer_store_b16((uint16_t)pack_bf16(v[e], 0.f), out.rsrc, to, 0, 0);
-                else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[e]), out.rsrc, to, 0, 0);
-              }
-            } else {
-              // (a head's columns end at a multiple of 16 bytes)
-#pragma unroll
-              for (int e = 0; e < 4 * TN; e += 16 / size) {
-                const uint32_t to = col + e < wc ? row + (uint32_t)(e * size) : kNowhere;
-                if constexpr (size == 4) {
-                  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]}), out.rsrc, to, 0, 0);
-                } else if constexpr (TN == 1) {
-                  __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}, out.rsrc, to, 0, 0);
-                } else {
-                  __builtin_amdgcn_raw_buffer_store_b128(
-                      u32x4{pack_bf16(v[e], v[e + 1]), pack_bf16(v[e + 2], v[e + 3]), pack_bf16(v[e + 4], v[e + 5]), pack_bf16(v[e + 6], v[e + 7])},
-                      out.rsrc, to, 0, 0);
-                }
-              }
-            }
+              for (int p = F; p < P; ++p) mul(st[d][t], y, x[t][p]);
           }
+        };
+        using std::integral_constant;
+        if constexpr (!OUT || Op::kParts == 1) {
+          add(integral_constant<int, 0>{}, integral_constant<int, Op::kParts>{});
+        } else {
+          add(integral_constant<int, 0>{}, integral_constant<int, 2>{});
+          if (exact) add(integral_constant<int, 2>{}, integral_constant<int, Op::kParts>{});
         }
       }
-      __builtin_amdgcn_sched_barrier(0);
-      if (rev || last) {
-        const float all = rev && h > 0 ? 1.f : s_pow[n];
-#pragma unroll
-        for (int d = 0; d < TD; ++d)
-#pragma unroll
-          for (int t = 0; t < TN; ++t) st[d][t] *= all;
-#pragma unroll
-        for (int k = 0; k < KC; ++k) {
-          __builtin_amdgcn_sched_barrier(0);
-          float w[Op::kEach];
-          const int j = k * KB + Op::index(q, 0) + C - n;
-          if (n == C) {
-#pragma unroll
-            for (int e = 0; e < Op::kEach; e += 4) {
-              const f32x4 v = *reinterpret_cast<const f32x4*>(s_fade + j + e);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) w[e + i] = v[i];
-            }
-          } else {
-#pragma unroll
-            for (int e = 0; e < Op::kEach; ++e) w[e] = s_fade[j + e];
-          }
-          // parts `from` up to `to` of the rows times their weights
-          auto add = [&](auto from, auto to) {
-            constexpr int F = decltype(from)::value, P = decltype(to)::value;
-            Op x[TN][P];
-#pragma unroll
-            for (int t = 0; t < TN; ++t) {
-              float v[Op::kEach];
-#pragma unroll
-              for (int e = 0; e < Op::kEach; ++e) v[e] = c[k][t].get(e) * w[e];
-#pragma unroll
-              for (int p = 0; p < P; ++p) x[t][p].take(v);
-            }
-#pragma unroll
-            for (int d = 0; d < TD; ++d) {
-              Op y;
-              y.template column<LB>(s_b + k * KB * LB + 16 * d, q, l);
-#pragma unroll
-              for (int t = 0; t < TN; ++t)
-#pragma unroll
-                for (int p = F; p < P; ++p) mul(st[d][t], y, x[t][p]);
-            }
-          };
-          using std::integral_constant;
-          if constexpr (!OUT || Op::kParts == 1) {
-            add(integral_constant<int, 0>{}, integral_constant<int, Op::kParts>{});
-          } else {
-            add(integral_constant<int, 0>{}, integral_constant<int, 2>{});
-            if (exact) add(integral_constant<int, 2>{}, integral_constant<int, Op::kParts>{});
-          }
-        }
-      }
-      __syncthreads();
-      put(last ? 0 : h + 1);
     }
+    __syncthreads();
+    put(next.h);
+    now = next;
   }
   float* to = nullptr;
   if constexpr (!OUT) to = args.sums + number * states + mine;
-  else if (f.end != nullptr && (rev ? s.first : s.last)) to = f.end + s.seq * states + mine;
+  else if (exact) to = f.end + s.seq * states + mine;
   if (to == nullptr) return;
   int other = l;
   asm volatile("" : "+v"(other));
@@ -602,9 +610,9 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
         __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(st[d][t][e]), base, place(other, d, t, e), 0, 0);
 }
 
-// `forms` of the forms from `first` on, which have as many slices each, in one launch
+// `forms` of the forms from `first` on, which have as many slices each, in one launch; `split`: in order, a block a head
 template <typename T, int DA, int DC, int W, bool OUT, bool ALIGNED>
-__global__ __launch_bounds__(kWave* W, DA > 128 ? 1 : 2) void k_linear(Args a, int first, int forms) {
+__global__ __launch_bounds__(kWave* W, DA > 128 ? 1 : 2) void k_linear(Args a, int first, int forms, int split) {
   __shared__ Room<T, DA, DC, OUT> lds;
   uint32_t at = blockIdx.x;
   const Form& f = a.f[first + (int)(at % (uint32_t)forms)];
@@ -612,9 +620,14 @@ __global__ __launch_bounds__(kWave* W, DA > 128 ? 1 : 2) void k_linear(Args a, i
   const uint32_t slices = (uint32_t)a.slices[first], groups = (uint32_t)a.groups;
   const int slice = (int)(at % slices);
   at /= slices;
+  int head = -1;
+  if (split) {
+    head = (int)(at % (uint32_t)a.per);
+    at /= (uint32_t)a.per;
+  }
   // (apart: each needs fewer registers than one body for both)
-  if (f.rev) sweep<T, DA, DC, W, OUT, ALIGNED, true>(a, f, at / groups, (int)(at % groups), slice, lds);
-  else sweep<T, DA, DC, W, OUT, ALIGNED, false>(a, f, at / groups, (int)(at % groups), slice, lds);
+  if (f.rev) sweep<T, DA, DC, W, OUT, ALIGNED, true>(a, f, at / groups, (int)(at % groups), slice, head, lds);
+  else sweep<T, DA, DC, W, OUT, ALIGNED, false>(a, f, at / groups, (int)(at % groups), slice, head, lds);
 }
 
 // States at a sequence's boundaries from the sums between them, in place: in order, or backwards.
@@ -678,24 +691,31 @@ int log_length(int64_t N, int groups) {
 int columns_of(const Args& a, int da, int dc) { return !a.aligned || da > 128 || dc <= 64 ? 64 : 128; }
 int width_of(const Args& a, int da) { return da > 128 ? 256 : a.aligned && da <= 64 ? 64 : 128; }
 
+// Blocks that the device holds at once: two a compute unit.
+constexpr int64_t kResident = 512;
+
 template <typename T, bool OUT>
 hipError_t go(const Args& a, int first, int forms, hipStream_t s) {
   const Form& f = a.f[first];
-  const int64_t blocks = (OUT ? a.bounds + a.M : a.bounds) * a.groups * a.slices[first] * forms;
+  int64_t blocks = (OUT ? a.bounds + a.M : a.bounds) * a.groups * a.slices[first] * forms;
+  // Few blocks in order: one for every head, each of which makes the state (1501 tokens in 23 sequences, 2 x 3 heads: 23 us
+  // all heads in a block).
+  const int split = OUT && forms == 1 && !f.rev && a.per > 1 && blocks * a.per <= kResident;
+  if (split) blocks *= a.per;
   if (blocks == 0) return hipSuccess;
   const unsigned grid = (unsigned)blocks;
   const int da = width_of(a, f.da), dc = columns_of(a, f.da, f.dc);
   if (!a.aligned) {
-    if (da == 128) k_linear<T, 128, 64, 4, OUT, false><<<grid, kThreads, 0, s>>>(a, first, forms);
-    else k_linear<T, 256, 64, 4, OUT, false><<<grid, kThreads, 0, s>>>(a, first, forms);
+    if (da == 128) k_linear<T, 128, 64, 4, OUT, false><<<grid, kThreads, 0, s>>>(a, first, forms, split);
+    else k_linear<T, 256, 64, 4, OUT, false><<<grid, kThreads, 0, s>>>(a, first, forms, split);
   } else if (da == 64) {
-    if (dc == 128) k_linear<T, 64, 128, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms);
-    else k_linear<T, 64, 64, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms);
+    if (dc == 128) k_linear<T, 64, 128, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms, split);
+    else k_linear<T, 64, 64, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms, split);
   } else if (da == 128) {
-    if (dc == 128) k_linear<T, 128, 128, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms);
-    else k_linear<T, 128, 64, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms);
+    if (dc == 128) k_linear<T, 128, 128, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms, split);
+    else k_linear<T, 128, 64, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms, split);
   } else {
-    k_linear<T, 256, 64, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms);
+    k_linear<T, 256, 64, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms, split);
   }
   return hipGetLastError();
 }
