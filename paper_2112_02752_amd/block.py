@@ -49,8 +49,10 @@ _SEED = (1 << 64) - 1
 
 
 def _device_now() -> int:
+    """The current device (where PyTorch offers it, without what its Python call adds)."""
     import torch
-    return torch.cuda.current_device()
+    raw = getattr(torch._C, "_cuda_getDevice", None)
+    return raw() if raw is not None and torch.cuda.is_initialized() else torch.cuda.current_device()
 
 
 def _here(*mats) -> None:
