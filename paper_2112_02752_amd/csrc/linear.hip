@@ -270,11 +270,11 @@ struct Room {
   alignas(16) float fade[2 * C], pow[C + 1];
 };
 
-// DA: widest a and b; DC: columns of c that a block takes; head: one of the group's (in order), or all (-1).  OUT: the form
-// itself, else the sums of the segment that ends (backwards: begins) at a boundary.
+// DA: widest a and b; DC: columns of c that a block takes; begin .. until - 1: of the group's heads (in order, a part of
+// them may be).  OUT: the form itself, else the sums of the segment that ends (backwards: begins) at a boundary.
 template <typename T, int DA, int DC, int W, bool OUT, bool ALIGNED, bool REV>
 __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t number, int group, int slice,
-                                      int head, Room<T, DA, DC, OUT>& lds) {
+                                      int begin, int until, Room<T, DA, DC, OUT>& lds) {
   typedef Operand<T> Op;
   typedef typename Op::Value Value;
   constexpr int C = Op::kChunk, KB = Op::kBlock, TC = C / 16, TD = DA / 16, KC = C / KB, KD = DA / KB;
@@ -317,7 +317,6 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
     s.begin -= (int64_t)1 << args.log;
   }
   const int length = (int)(s.end - s.begin);
-  const int begin = max(head, 0), until = head >= 0 ? head + 1 : OUT || rev ? args.per : 1;  // heads
   auto chunk = [&](const Place& m, int at, int h, int n, int w, bool wanted) {
     return Chunk(m.p + h * m.apart, m.ld, rev ? s.end - at - n : s.begin + at, n, w * size, rev, wanted);
   };
@@ -610,9 +609,10 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
         __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(st[d][t][e]), base, place(other, d, t, e), 0, 0);
 }
 
-// `forms` of the forms from `first` on, which have as many slices each, in one launch; `split`: in order, a block a head
+// `forms` of the forms from `first` on, which have as many slices each, in one launch; `parts`: blocks that share a
+// group's heads (in order)
 template <typename T, int DA, int DC, int W, bool OUT, bool ALIGNED>
-__global__ __launch_bounds__(kWave* W, DA > 128 ? 1 : 2) void k_linear(Args a, int first, int forms, int split) {
+__global__ __launch_bounds__(kWave* W, DA > 128 ? 1 : 2) void k_linear(Args a, int first, int forms, int parts) {
   __shared__ Room<T, DA, DC, OUT> lds;
   uint32_t at = blockIdx.x;
   const Form& f = a.f[first + (int)(at % (uint32_t)forms)];
@@ -620,14 +620,11 @@ __global__ __launch_bounds__(kWave* W, DA > 128 ? 1 : 2) void k_linear(Args a, i
   const uint32_t slices = (uint32_t)a.slices[first], groups = (uint32_t)a.groups;
   const int slice = (int)(at % slices);
   at /= slices;
-  int head = -1;
-  if (split) {
-    head = (int)(at % (uint32_t)a.per);
-    at /= (uint32_t)a.per;
-  }
+  const int each = a.per / parts, begin = (int)(at % (uint32_t)parts) * each, until = OUT || f.rev ? begin + each : 1;
+  at /= (uint32_t)parts;
   // (apart: each needs fewer registers than one body for both)
-  if (f.rev) sweep<T, DA, DC, W, OUT, ALIGNED, true>(a, f, at / groups, (int)(at % groups), slice, head, lds);
-  else sweep<T, DA, DC, W, OUT, ALIGNED, false>(a, f, at / groups, (int)(at % groups), slice, head, lds);
+  if (f.rev) sweep<T, DA, DC, W, OUT, ALIGNED, true>(a, f, at / groups, (int)(at % groups), slice, begin, until, lds);
+  else sweep<T, DA, DC, W, OUT, ALIGNED, false>(a, f, at / groups, (int)(at % groups), slice, begin, until, lds);
 }
 
 // States at a sequence's boundaries from the sums between them, in place: in order, or backwards.
@@ -698,24 +695,30 @@ template <typename T, bool OUT>
 hipError_t go(const Args& a, int first, int forms, hipStream_t s) {
   const Form& f = a.f[first];
   int64_t blocks = (OUT ? a.bounds + a.M : a.bounds) * a.groups * a.slices[first] * forms;
-  // Few blocks in order: one for every head, each of which makes the state (1501 tokens in 23 sequences, 2 x 3 heads: 23 us
-  // all heads in a block).
-  const int split = OUT && forms == 1 && !f.rev && a.per > 1 && blocks * a.per <= kResident;
-  if (split) blocks *= a.per;
+  // In order the heads of a group may be shared by blocks, each of which makes the state: what that costs (about half of a
+  // head's work, and as much again for a block's begin and end) against rounds of blocks on the device.  Four heads, 700
+  // blocks of all: 115 us with one, 107 with two; three, 92 blocks (1501 tokens): 23 us with all in a block, 18 with one.
+  int parts = 1;
+  if (OUT && forms == 1 && !f.rev) {
+    auto cost = [&](int n) { return (float)((blocks * n + kResident - 1) / kResident) * ((float)(a.per / n) + 0.9f); };
+    for (int n = 2; n <= a.per; ++n)
+      if (a.per % n == 0 && blocks * n < ((int64_t)1 << 22) && cost(n) < 0.95f * cost(parts)) parts = n;
+  }
+  blocks *= parts;
   if (blocks == 0) return hipSuccess;
   const unsigned grid = (unsigned)blocks;
   const int da = width_of(a, f.da), dc = columns_of(a, f.da, f.dc);
   if (!a.aligned) {
-    if (da == 128) k_linear<T, 128, 64, 4, OUT, false><<<grid, kThreads, 0, s>>>(a, first, forms, split);
-    else k_linear<T, 256, 64, 4, OUT, false><<<grid, kThreads, 0, s>>>(a, first, forms, split);
+    if (da == 128) k_linear<T, 128, 64, 4, OUT, false><<<grid, kThreads, 0, s>>>(a, first, forms, parts);
+    else k_linear<T, 256, 64, 4, OUT, false><<<grid, kThreads, 0, s>>>(a, first, forms, parts);
   } else if (da == 64) {
-    if (dc == 128) k_linear<T, 64, 128, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms, split);
-    else k_linear<T, 64, 64, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms, split);
+    if (dc == 128) k_linear<T, 64, 128, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms, parts);
+    else k_linear<T, 64, 64, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms, parts);
   } else if (da == 128) {
-    if (dc == 128) k_linear<T, 128, 128, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms, split);
-    else k_linear<T, 128, 64, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms, split);
+    if (dc == 128) k_linear<T, 128, 128, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms, parts);
+    else k_linear<T, 128, 64, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms, parts);
   } else {
-    k_linear<T, 256, 64, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms, split);
+    k_linear<T, 256, 64, 4, OUT, true><<<grid, kThreads, 0, s>>>(a, first, forms, parts);
   }
   return hipGetLastError();
 }
