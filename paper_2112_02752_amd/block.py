@@ -150,8 +150,8 @@ class Norm:
             raise ValueError("batch larger than the norm's workspace")
         self._take(seed, first_row)
         _check("emb_norm_bwd", lib().emb_norm_bwd(
-            n, D, self._ref, total.ref, dy.ref, *(m.ref if m is not None else None for m in mats), _floats(dweight, (D,), "dweight"), int(add), self._ws,
-            self._wsb, _stream(stream)))
+            n, D, self._ref, total.ref, dy.ref, *(m.ref if m is not None else None for m in mats),
+            _floats(dweight, (D,), "dweight"), int(add), self._ws, self._wsb, _stream(stream)))
 
 
 def dropout(x, y, drop: float, seed: int, first_row: int = 0, stream=None) -> None:

@@ -24,7 +24,20 @@
 // p / L - 1: no two have the same one, and a sequence's are consecutive.  Three
 // launches: sums of every segment that a boundary follows (backwards: precedes),
 // the boundaries' states from them one after another, and the form itself,
-// every segment from its boundary's state.
+// every segment from its boundary's state.  All sums have a fixed order.
+//
+// A block takes a segment's key head; its four wavefronts have the columns of c
+// and of the state in quarters, the state in registers from chunk to chunk, and
+// the rows of a chunk in LDS, loaded a step (a head of a chunk) ahead.  Products
+// a . b go through LDS once, from the wavefronts that make them to all.
+//
+// Bound.  One prompt of 32768 tokens, 16 heads of 128 x 128: 214 us, of which sums 77 (293 MB,
+// 3.8 TB/s), boundaries 13 and the form 125 (571 MB, 4.5 TB/s).  A training batch of 48
+// sequences, 32768 x 16 heads (4 key heads) of 128: forward 160 (sums 29, boundaries 17, the form
+// 115), backward 380 (sums 73, boundaries 17, the three forms 290, 1.09 GB at 3.8 TB/s).  There
+// LDS is busy a third of the time (its reads: every wavefront takes all rows of a and b),
+// the matrix units a fifth; the rest is the latency of a step's
+// phases at two blocks a compute unit, and the last round of blocks.
 #include "block_common.h"
 
 namespace emb {
@@ -56,8 +69,9 @@ struct Operand<bf16> {
     const u32x2 lo = *reinterpret_cast<const u32x2*>(at + 4 * q), hi = *reinterpret_cast<const u32x2*>(at + 16 + 4 * q);
     v = __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
   }
-  // column APART (l / 4) + l % 4 from `at` on, rows 0 .. kBlock - 1 of LD values: the transposing load gives a lane four
-  // rows of its column where the 16 lanes of a quarter point at those rows' 16 columns in order, four each
+  // column APART (l / 4) + l % 4 from `at` on, rows 0 .. kBlock - 1 of LD values: the transposing load gives
+  // a lane four rows of its column where the 16 lanes of a quarter point at those rows' 16 columns in order,
+  // four each
   template <int LD, int APART = 4>
   __device__ __forceinline__ void column(const Value* at, int q, int l) {
     const Value* p = at + (8 * q + l / 4) * LD + APART * (l % 4);
@@ -197,15 +211,16 @@ __device__ __forceinline__ bool segment(const Args& a, int64_t number, int lane,
   return true;
 }
 
-// A chunk's rows: offsets are 32 bits from the first of them in memory, and one past the last row's columns reads as zero
-// and is not written, so neither a chunk's last rows nor a head's last columns need a branch and loads stay in flight
-// together.  kNowhere is past any chunk, also with the distance of its rows (below 2^30) added or taken off.
+// A chunk's rows: offsets are 32 bits from the first of them in memory, and one past the last row's columns
+// reads as zero and is not written, so neither a chunk's last rows nor a head's last columns need a branch
+// and loads stay in flight together.  kNowhere is past any chunk, also with the distance of its rows (below
+// 2^30) added or taken off.
 constexpr uint32_t kNowhere = 0x80000000u;
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t from_base(const void* p, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
 }
-// `n` rows from `row` on, which a step takes in order or (rev) from the last one up; `top` is its first one's offset, `ld`
-// the distance of two.
+// `n` rows from `row` on, which a step takes in order or (rev) from the last one up; `top` is its first one's
+// offset, `ld` the distance of two.
 struct Chunk {
   __amdgpu_buffer_rsrc_t rsrc;
   int ld, top;
@@ -260,8 +275,8 @@ struct Rowset {
   }
 };
 
-// A block's LDS: the rows of a chunk, a step's products, powers of the decay, and what a full chunk's rows enter the state
-// with, then zeros.
+// A block's LDS: the rows of a chunk, a step's products, powers of the decay, and what a full chunk's rows
+// enter the state with, then zeros.
 template <typename T, int DA, int DC, bool OUT>
 struct Room {
   typedef Operand<T> Op;
@@ -270,8 +285,9 @@ struct Room {
   alignas(16) float fade[2 * C], pow[C + 1];
 };
 
-// DA: widest a and b; DC: columns of c that a block takes; begin .. until - 1: of the group's heads (in order, a part of
-// them may be).  OUT: the form itself, else the sums of the segment that ends (backwards: begins) at a boundary.
+// DA: widest a and b; DC: columns of c that a block takes; begin .. until - 1: of the group's heads (in
+// order, a part of them may be).  OUT: the form itself, else the sums of the segment that ends (backwards:
+// begins) at a boundary.
 template <typename T, int DA, int DC, int W, bool OUT, bool ALIGNED, bool REV>
 __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t number, int group, int slice,
                                       int begin, int until, Room<T, DA, DC, OUT>& lds) {
@@ -293,8 +309,8 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
   constexpr int size = sizeof(Value);
   const int c0 = slice * DC, wc = min(DC, f.dc - c0), n0 = 16 * TN * wave;
   const int64_t states = (int64_t)args.groups * args.state, mine = (int64_t)group * args.state;
-  // The matrices' places stay in scalar registers (loaded again from the arguments in every step, they would be waited for),
-  // from the group's columns on: heads are `apart` bytes from one another.
+  // The matrices' places stay in scalar registers (loaded again from the arguments in every step, they would
+  // be waited for), from the group's columns on: heads are `apart` bytes from one another.
   struct Place {
     const char* p;
     int ld, apart;
@@ -336,8 +352,8 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
   };
   Step now{0, begin};
   load(now);
-  // The state: lane l holds rows 16 d + 4 q .. of a column.  With two tiles of columns a wavefront, those of tile t are 8 j +
-  // 4 t + (0 .. 3), so that a lane's results of both are eight values in a row.
+  // The state: lane l holds rows 16 d + 4 q .. of a column.  With two tiles of columns a wavefront, those of
+  // tile t are 8 j + 4 t + (0 .. 3), so that a lane's results of both are eight values in a row.
   constexpr int kApart = 4 * TN, kTile = TN == 2 ? 4 : 16;
   // (`from_l` is l, in a register of the caller's: the offsets of the first use are not kept for the second)
   auto place = [&](int from_l, int d, int t, int e) {
@@ -377,8 +393,8 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
   }
   put(begin);
   __syncthreads();
-  // Weights of the products that a lane makes, in row l % 16 of a tile, columns 4 q ..: in one on the diagonal, in the one
-  // before it, and how much less those before that have
+  // Weights of the products that a lane makes, in row l % 16 of a tile, columns 4 q ..: in one on the
+  // diagonal, in the one before it, and how much less those before that have
   constexpr int kSide = TC / 2, kSquares = 3;  // (the fourth square is above the diagonal)
   const int square = wave, ti = square >= 1 ? kSide : 0, tj = square >= 2 ? kSide : 0;
   float on[4], off[4], less[2 * kSide - 1], before[TC];
@@ -393,8 +409,8 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
 #pragma unroll
     for (int i = 0; i < 2 * kSide - 1; ++i) less[i] = lane_at(s_pow[16 * max(ti - tj + i - kSide, 0)], 0);
   }
-  // A state that is kept gets weighted rows with all of their 24 bits, in three parts; one that only multiplies rows of this
-  // segment, and is rounded to bf16 for that, gets 16 of them.
+  // A state that is kept gets weighted rows with all of their 24 bits, in three parts; one that only
+  // multiplies rows of this segment, and is rounded to bf16 for that, gets 16 of them.
   const bool exact = f.end != nullptr && begin == 0 && (rev ? s.first : s.last);
   f32x4 o[TC][TN];
   while (now.at < length) {
@@ -419,8 +435,9 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
         else *reinterpret_cast<f32x4*>(to) = p;
       };
       if (new_a) {
-        // What the state before the chunk gives (lane l: row 16 i + l % 16), and in order on the way, as the rows of a are
-        // there, their products with 16 rows of b a wavefront, for LDS.  (Tiles above the diagonal are zeros.)
+        // What the state before the chunk gives (lane l: row 16 i + l % 16), and in order on the way, as the
+        // rows of a are there, their products with 16 rows of b a wavefront, for LDS.  (Tiles above the
+        // diagonal are zeros.)
         f32x4 p[TC];
 #pragma unroll
         for (int i = 0; i < TC; ++i) {
@@ -452,8 +469,8 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
         }
       }
       if (rev && square < kSquares) {
-        // backwards, where rows of b are new in every step: kSide x kSide tiles a wavefront, of the squares on and below
-        // the diagonal
+        // backwards, where rows of b are new in every step: kSide x kSide tiles a wavefront, of the squares
+        // on and below the diagonal
         f32x4 p[kSide][kSide];
 #pragma unroll
         for (int i = 0; i < kSide; ++i)
@@ -521,12 +538,14 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
             for (int e = 0; e < 4 * TN; e += 16 / size) {
               const uint32_t to = col + e < wc ? row + (uint32_t)(e * size) : kNowhere;
               if constexpr (size == 4) {
-                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]}), out.rsrc, to, 0, 0);
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]}),
+                                                       out.rsrc, to, 0, 0);
               } else if constexpr (TN == 1) {
                 __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}, out.rsrc, to, 0, 0);
               } else {
                 __builtin_amdgcn_raw_buffer_store_b128(
-                    u32x4{pack_bf16(v[e], v[e + 1]), pack_bf16(v[e + 2], v[e + 3]), pack_bf16(v[e + 4], v[e + 5]), pack_bf16(v[e + 6], v[e + 7])},
+                    u32x4{pack_bf16(v[e], v[e + 1]), pack_bf16(v[e + 2], v[e + 3]), pack_bf16(v[e + 4], v[e + 5]),
+                          pack_bf16(v[e + 6], v[e + 7])},
                     out.rsrc, to, 0, 0);
               }
             }
@@ -683,8 +702,8 @@ int log_length(int64_t N, int groups) {
   return log;
 }
 
-// Columns of c that a block takes, and the widest a and b of the kernel that does (rows that are not aligned are for any
-// width up to 128, or to 256).
+// Columns of c that a block takes, and the widest a and b of the kernel that does (rows that are not aligned
+// are for any width up to 128, or to 256).
 int columns_of(const Args& a, int da, int dc) { return !a.aligned || da > 128 || dc <= 64 ? 64 : 128; }
 int width_of(const Args& a, int da) { return da > 128 ? 256 : a.aligned && da <= 64 ? 64 : 128; }
 
@@ -695,9 +714,10 @@ template <typename T, bool OUT>
 hipError_t go(const Args& a, int first, int forms, hipStream_t s) {
   const Form& f = a.f[first];
   int64_t blocks = (OUT ? a.bounds + a.M : a.bounds) * a.groups * a.slices[first] * forms;
-  // In order the heads of a group may be shared by blocks, each of which makes the state: what that costs (about half of a
-  // head's work, and as much again for a block's begin and end) against rounds of blocks on the device.  Four heads, 700
-  // blocks of all: 115 us with one, 107 with two; three, 92 blocks (1501 tokens): 23 us with all in a block, 18 with one.
+  // In order the heads of a group may be shared by blocks, each of which makes the state: what that costs
+  // (about half of a head's work, and as much again for a block's begin and end) against rounds of blocks on
+  // the device.  Four heads, 700 blocks of all: 115 us with one, 107 with two; three, 92 blocks (1501
+  // tokens): 23 us with all in a block, 18 with one.
   int parts = 1;
   if (OUT && forms == 1 && !f.rev) {
     auto cost = [&](int n) { return (float)((blocks * n + kResident - 1) / kResident) * ((float)(a.per / n) + 0.9f); };

@@ -9,7 +9,12 @@
 // its squares and its norm, so every matrix is read or written once.  The
 // backward sums the squares again (the row is there anyhow), so nothing is kept
 // of the forward but t.  A mask is never stored: a draw is a function of the
-// seed, the row and the column.
+// seed, the row and the column; 16 bits a value, so a share is held to 2^-16.
+//
+// Bound by the bytes.  32768 x 2048 bf16 with dropout: forward with the output in 8 bits
+// 105 us (608 MB, 5.8 TB/s), backward 140 (671 MB, 4.8 TB/s) and 5 for the weight
+// gradient's last sum.  Dropout alone, 65536 x 2048: 90 us, 6.0 TB/s.  64 x 1536: 3.4 us, one
+// load and one exchange.
 #include "block_common.h"
 #include "saved_codes.h"
 
@@ -349,8 +354,8 @@ hipError_t by_width(const NormLaunch& p, hipStream_t s) {
   using std::integral_constant;
   constexpr int kOne = kWave * kCols;
   if (p.D <= kOne) return go(integral_constant<int, 1>{}, integral_constant<int, 1>{});
-  // (forward: more wavefronts with less each, 32768 x 2048 104 us instead of 115; the backward exchanges two sums between
-  // them in every row: 140 either way)
+  // (forward: more wavefronts with less each, 32768 x 2048 104 us instead of 115; the backward exchanges two
+  // sums between them in every row: 140 either way)
   if (p.D <= 2 * kOne) return go(integral_constant<int, BACK ? 1 : 2>{}, integral_constant<int, BACK ? 2 : 1>{});
   if (p.D <= 4 * kOne) return go(integral_constant<int, BACK ? 1 : 4>{}, integral_constant<int, BACK ? 4 : 1>{});
   if (p.D <= 8 * kOne) return go(integral_constant<int, 4>{}, integral_constant<int, 2>{});
