@@ -547,7 +547,8 @@ emb_status emb_weight_grad(int64_t rows, int32_t dim, int32_t cols, const emb_ma
  * residual and total of one: x's, or fp32 beside bf16.  Each of residual, total
  * and one of y and saved may be NULL (or have no data); t has x's type where
  * both residual and total are left out.  saved: y as its type holds it in 8
- * bits, as emb_save leaves it.  total may be residual's rows, y x's.
+ * bits, as emb_save leaves it.  total may be residual's rows, y x's (here and
+ * below EMB_EINVAL where an output begins at an input with other strides).
  * 1 <= dim <= 16384, else EMB_EUNSUPPORTED.  With an eps of zero a row of zeros gives NaN, as
  * do infinities and NaN in their own row; rows whose squares overflow fp32 give
  * zeros. */
@@ -643,7 +644,8 @@ emb_status emb_linear_bwd(const emb_heads* heads, const void* states, size_t sta
  * emb_scan_step: row i's state is state[slots[i]] (device fp32, num_slots of
  * groups x dk x dv values, updated in place; slots NULL: slot i).  A token whose slot lies
  * outside 0..num_slots-1 gets zeros and touches no state.  Slots must be
- * distinct, and y may not overlap the inputs.  Arithmetic is fp32. */
+ * distinct, and y may not overlap the inputs (EMB_EINVAL where it begins at one).
+ * Arithmetic is fp32. */
 emb_status emb_linear_step(int64_t num_tokens, int32_t heads, int32_t groups, int32_t dk, int32_t dv, const emb_mat* q,
                            const emb_mat* k, const emb_mat* v, const float* decay, float scale, float* state,
                            int64_t num_slots, const int32_t* slots, const emb_mat* y, void* stream);
@@ -677,7 +679,8 @@ emb_status emb_logp_bwd(int64_t rows, int32_t cols, const emb_mat* logits, const
 
 /* Both in one pass over the logits, where the gradient of logp is known before
  * (a loss that weighs given tokens): logp, entropy as emb_logp_fwd, dlogits as
- * emb_logp_bwd of dlogp.  dlogits may be logits' rows. */
+ * emb_logp_bwd of dlogp.  dlogits may be logits' rows; logp and entropy may not be
+ * dlogp. */
 emb_status emb_logp_train(int64_t rows, int32_t cols, const emb_mat* logits, const void* ids, int32_t id_bytes,
                           float scale, const float* dlogp, float* logp, float* entropy, const emb_mat* dlogits,
                           void* stream);

@@ -55,12 +55,16 @@ def _device_now() -> int:
     return raw() if raw is not None and torch.cuda.is_initialized() else torch.cuda.current_device()
 
 
-def _here(*mats) -> None:
-    """A call runs on the current device: its matrices have to lie there."""
+def _here(mats, tensors) -> None:
+    """A call runs on the current device: its matrices and vectors (None: left
+    out) have to lie there."""
     now = _device_now()
     for m in mats:
         if m is not None and m.tensor.get_device() != now:
             raise ValueError("matrices lie on the current device (torch.cuda.device chooses it)")
+    for t in tensors:
+        if t is not None and t.get_device() != now:
+            raise ValueError("tensors lie on the current device (torch.cuda.device chooses it)")
 
 
 # ---------------------------------------------------------------- norm
@@ -125,7 +129,7 @@ class Norm:
             saved = _mat(saved.mat)
             _want(saved, n, D, "saved")
         refs.append(saved)
-        _here(x, *refs)
+        _here((x, *refs), (self.weight,))
         self._take(seed, first_row)
         _check("emb_norm_fwd", lib().emb_norm_fwd(n, D, self._ref, x.ref,
                                                   *(m.ref if m is not None else None for m in refs), _stream(stream)))
@@ -145,7 +149,7 @@ class Norm:
                 m = _mat(m)
                 _want(m, n, D, name)
             mats.append(m)
-        _here(total, dy, *mats)
+        _here((total, dy, *mats), (self.weight, dweight, self.ws))
         if dweight is not None and n > self.max_rows:
             raise ValueError("batch larger than the norm's workspace")
         self._take(seed, first_row)
@@ -161,7 +165,7 @@ def dropout(x, y, drop: float, seed: int, first_row: int = 0, stream=None) -> No
     same call on dy.  y may be x."""
     x, y = _mat(x), _mat(y)
     _want(y, x.rows, x.cols, "y")
-    _here(x, y)
+    _here((x, y), ())
     _check("emb_dropout", lib().emb_dropout(x.rows, x.cols, drop, seed & _SEED, first_row, x.ref, y.ref,
                                             _stream(stream)))
 
@@ -256,7 +260,7 @@ class LinearAttention:
         ref = self._take(heads)
         y = _mat(y)
         _want(y, heads.tokens, self.heads * self.dv, "y")
-        _here(heads.q, heads.k, heads.v, y)
+        _here((heads.q, heads.k, heads.v, y), (heads.offsets, heads.decay, heads.first, last, self.states))
         self._tokens = None
         _check("emb_linear_fwd", lib().emb_linear_fwd(ref, y.ref, _floats(last, heads.states, "last"), self._states,
                                                       self._size, _stream(stream)))
@@ -273,7 +277,8 @@ class LinearAttention:
         for m, cols, name in zip(mats, (self.heads * self.dv, self.heads * self.dk, self.groups * self.dk,
                                         self.groups * self.dv), ("dy", "dq", "dk", "dv")):
             _want(m, heads.tokens, cols, name)
-        _here(heads.q, heads.k, heads.v, *mats)
+        _here((heads.q, heads.k, heads.v, *mats),
+              (heads.offsets, heads.decay, heads.first, dlast, dfirst, self.states, self.ws))
         _check("emb_linear_bwd", lib().emb_linear_bwd(
             ref, self._states, self._size, *(m.ref for m in mats), _floats(dlast, heads.states, "dlast"),
             _floats(dfirst, heads.states, "dfirst"), self._ws, self._size, _stream(stream)))
@@ -290,7 +295,7 @@ def linear_attention_step(q, k, v, decay, state, y, heads: int, groups: Optional
     dk, dv = _head_widths(q, k, v, heads, groups)
     n = k.rows
     _want(y, n, heads * dv, "y")
-    _here(q, k, v, y)
+    _here((q, k, v, y), (decay, state, slots))
     rows = int(state.shape[0])
     sp = None
     if slots is not None:
@@ -339,20 +344,20 @@ class LogProbs:
         self._stats = self.stats.data_ptr()
         self._rows = None
 
-    def _take(self, logits, ids):
+    def _take(self, logits, ids, *tensors):
         logits = _mat(logits)
         n = logits.rows
         _want(logits, n, self.cols, "logits")
         if n > self.max_rows:
             raise ValueError("more rows than there is room for")
-        _here(logits)
+        _here((logits,), (ids, self.stats) + tensors)
         return (logits, n) + (_ids(ids, n) if ids is not None else (None, 4))
 
     def forward(self, logits, ids, logp, entropy=None, top_ids=None, top_logp=None, stream=None) -> None:
         """``logp`` and ``entropy`` (fp32 [rows], each may be None, ``ids`` with
         ``logp``), ``top_ids`` (int32) and ``top_logp`` (fp32) [rows][top]."""
         import torch
-        logits, n, at, size = self._take(logits, ids)
+        logits, n, at, size = self._take(logits, ids, logp, entropy, top_ids, top_logp)
         tops = (n, self.top)
         if self.top > 0:
             if top_ids is None or top_logp is None:
@@ -371,12 +376,12 @@ class LogProbs:
         """``dlogits`` from the gradients of the last forward's ``logp`` and
         ``entropy`` (each may be None, ``ids`` with ``dlogp``); ``dlogits`` may be
         ``logits``."""
-        logits, n, at, size = self._take(logits, ids)
+        logits, n, at, size = self._take(logits, ids, dlogp, dentropy)
         if self._rows != n:
             raise ValueError("backward follows the forward of the same rows")
         dlogits = _mat(dlogits)
         _want(dlogits, n, self.cols, "dlogits")
-        _here(dlogits)
+        _here((dlogits,), ())
         _check("emb_logp_bwd", lib().emb_logp_bwd(
             n, self.cols, logits.ref, at, size, self.scale, self._stats, _floats(dlogp, (n,), "dlogp"),
             _floats(dentropy, (n,), "dentropy"), dlogits.ref, _stream(stream)))
@@ -384,10 +389,10 @@ class LogProbs:
     def train(self, logits, ids, logp, dlogp, dlogits, entropy=None, stream=None) -> None:
         """``logp`` (and ``entropy``; each may be None) and the gradient of
         sum(dlogp * logp) in ``dlogits``, which may be ``logits``."""
-        logits, n, at, size = self._take(logits, ids)
+        logits, n, at, size = self._take(logits, ids, logp, dlogp, entropy)
         dlogits = _mat(dlogits)
         _want(dlogits, n, self.cols, "dlogits")
-        _here(dlogits)
+        _here((dlogits,), ())
         _check("emb_logp_train", lib().emb_logp_train(
             n, self.cols, logits.ref, at, size, self.scale, _floats(dlogp, (n,), "dlogp"), _floats(logp, (n,), "logp"),
             _floats(entropy, (n,), "entropy"), dlogits.ref, _stream(stream)))

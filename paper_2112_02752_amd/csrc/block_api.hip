@@ -2,6 +2,8 @@
 // dispatch.  No allocation, no synchronisation.
 #include <math.h>
 
+#include <initializer_list>
+
 #include "api_common.h"
 #include "block_common.h"
 
@@ -10,6 +12,13 @@ using namespace emb;
 namespace {
 
 bool vectors(const Rows& r) { return (((uintptr_t)r.p | (uintptr_t)r.ld) & 15u) == 0; }
+
+// whether an output over an input is not so row by row
+bool across(int64_t rows, const Rows& out, std::initializer_list<Rows> in) {
+  for (const Rows& r : in)
+    if (rows > 1 && out.p != nullptr && out.p == r.p && out.ld != r.ld) return true;
+  return false;
+}
 
 // a matrix that a call may do without
 emb_status check_opt(const emb_mat* m, int32_t cols, int32_t dtype, Rows* out) {
@@ -137,7 +146,7 @@ emb_status check_dlogits(const emb_mat* dlogits, LogpLaunch* p) {
   if (dlogits->dtype != p->dtype) return EMB_EINVAL;
   p->dlogits = rows_of(*dlogits);
   // in place: row by row
-  return p->dlogits.p == p->logits.p && p->dlogits.ld != p->logits.ld ? EMB_EINVAL : EMB_OK;
+  return across(p->N, p->dlogits, {p->logits}) ? EMB_EINVAL : EMB_OK;
 }
 
 bool words(const void* a, const void* b, const void* c = nullptr) {
@@ -163,6 +172,7 @@ emb_status emb_norm_fwd(int64_t rows, int32_t dim, const emb_norm* norm, const e
     p.saved = rows_of(*saved);
   }
   if (p.y.p == nullptr && p.saved.p == nullptr) return EMB_EINVAL;
+  if (across(rows, p.total, {p.x, p.residual}) || across(rows, p.y, {p.x, p.residual})) return EMB_EINVAL;
   p.aligned = p.aligned && vectors(p.x) && vectors(p.residual) && vectors(p.total) && vectors(p.y);
   return hip_status(launch_norm_fwd(p, (hipStream_t)stream));
 }
@@ -191,6 +201,8 @@ emb_status emb_norm_bwd(int64_t rows, int32_t dim, const emb_norm* norm, const e
     if ((st = check_opt(arriving, dim, p.stream_dtype, &p.arriving)) != EMB_OK) return st;
     if ((st = check_opt(dtotal, dim, p.stream_dtype, &p.dtotal)) != EMB_OK) return st;
     if ((st = check_opt(dbranch, dim, p.dtype, &p.dbranch)) != EMB_OK) return st;
+    for (const Rows& out : {p.dtotal, p.dbranch})
+      if (across(rows, out, {p.total, p.dy, p.arriving})) return EMB_EINVAL;
     p.aligned = p.aligned && vectors(p.total) && vectors(p.dy) && vectors(p.arriving) && vectors(p.dtotal) &&
                 vectors(p.dbranch);
   }
@@ -217,6 +229,7 @@ emb_status emb_dropout(int64_t rows, int32_t dim, float drop, uint64_t seed, int
   p.dtype = x->dtype;
   p.x = rows_of(*x);
   p.y = rows_of(*y);
+  if (across(rows, p.y, {p.x})) return EMB_EINVAL;
   p.aligned = vectors(p.x) && vectors(p.y);
   return hip_status(launch_dropout(p, (hipStream_t)stream));
 }
@@ -254,8 +267,8 @@ emb_status emb_linear_bwd(const emb_heads* heads, const void* states, size_t sta
   LinLaunch p{};
   emb_status st = check_heads(heads, &p);
   if (st != EMB_OK) return st;
-  if ((((uintptr_t)dlast | (uintptr_t)dfirst) & 3u) != 0 || (dfirst != nullptr && (dfirst == dlast || dfirst == heads->first)))
-    return EMB_EINVAL;
+  if ((((uintptr_t)dlast | (uintptr_t)dfirst) & 3u) != 0) return EMB_EINVAL;
+  if (dfirst != nullptr && (dfirst == dlast || dfirst == heads->first)) return EMB_EINVAL;
   if (p.N > 0) {
     const emb_mat* all[4] = {dy, dq, dk, dv};
     const int32_t cols[4] = {p.heads * p.dv, p.heads * p.dk, p.groups * p.dk, p.groups * p.dv};
@@ -299,6 +312,8 @@ emb_status emb_linear_step(int64_t num_tokens, int32_t heads, int32_t groups, in
     if (all[i]->dtype != q->dtype) return EMB_EINVAL;
     *to[i] = rows_of(*all[i]);
   }
+  // (blocks of a token's other heads read its rows)
+  if (p.y.p == p.q.p || p.y.p == p.k.p || p.y.p == p.v.p) return EMB_EINVAL;
   p.N = num_tokens;
   p.num_slots = num_slots;
   p.heads = heads;
@@ -358,7 +373,7 @@ emb_status emb_logp_train(int64_t rows, int32_t cols, const emb_mat* logits, con
   if (st != EMB_OK) return st;
   if (!words(dlogp, logp, entropy)) return EMB_EINVAL;
   if (rows == 0) return EMB_OK;
-  if (ids == nullptr || dlogp == nullptr) return EMB_EINVAL;
+  if (ids == nullptr || dlogp == nullptr || dlogp == logp || dlogp == entropy) return EMB_EINVAL;
   if ((st = check_dlogits(dlogits, &p)) != EMB_OK) return st;
   p.dlogp = dlogp;
   p.logp = logp;

@@ -203,8 +203,8 @@ __device__ __forceinline__ bool boundary(const Args& a, int64_t number, int lane
 __device__ __forceinline__ bool segment(const Args& a, int64_t number, int lane, Segment& s) {
   if (number < a.bounds) return boundary(a, number, lane, s);
   s.seq = (int32_t)(number - a.bounds);
-  const int64_t e = min((int64_t)a.offsets[s.seq + 1], a.N);
-  s.begin = min((int64_t)a.offsets[s.seq], e);
+  const int64_t e = min((int64_t)max(a.offsets[s.seq + 1], 0), a.N);
+  s.begin = min((int64_t)max(a.offsets[s.seq], 0), e);
   s.end = min(s.begin + ((int64_t)1 << a.log), e);
   s.first = true;
   s.last = s.end == e;
@@ -659,7 +659,7 @@ __global__ __launch_bounds__(kThreads) void k_linear_chain(Args a, const float* 
   Segment s;
   // one block a sequence: its first boundary's
   if (!boundary(a, number, lane, s)) return;
-  const int64_t o = a.offsets[s.seq], e = min((int64_t)a.offsets[s.seq + 1], a.N);
+  const int64_t o = max(a.offsets[s.seq], 0), e = min((int64_t)a.offsets[s.seq + 1], a.N);
   if (s.begin - o != (int64_t)1 << a.log || i >= a.state) return;
   const int64_t count = (e - o - 1) >> a.log, states = (int64_t)a.groups * a.state;
   const float g = a.decay[group];

@@ -180,7 +180,7 @@ def test_linear_attention_refusals():
 
 def test_linear_step_refusals():
     def call(n=10, heads=4, groups=2, dk=16, dv=8, q=_m(), k=_m(), v=_m(), decay=0x3000, scale=1.0, state=0x5000,
-             num=20, slots=0x6000, y=_m()):
+             num=20, slots=0x6000, y=_m(0x7000)):
         return emb.lib().emb_linear_step(n, heads, groups, dk, dv, _ref(q), _ref(k), _ref(v), decay, scale, state, num,
                                          slots, _ref(y), None)
 
@@ -283,3 +283,44 @@ def test_matrices_of_another_device(monkeypatch):
         emb.dropout(Stub(4, 8, 1), Stub(4, 8, 0), 0.1, 1)
     with pytest.raises(ValueError, match="current device"):
         emb.linear_attention_step(Stub(4, 8, 1), Stub(4, 8, 1), Stub(4, 8, 0), None, torch.zeros(4), Stub(4, 8, 1), 2)
+    class Vector:
+        def __init__(self, device):
+            self.device = device
+
+        def get_device(self):
+            return self.device
+
+    mats = [Stub(4, 8, 1) for _ in range(4)]
+    for bad in range(3):
+        decay, state, slots = (Vector(0 if i == bad else 1) for i in range(3))
+        with pytest.raises(ValueError, match="tensors lie on the current device"):
+            emb.linear_attention_step(*mats[:3], decay, state, mats[3], 2, slots=slots)
+
+
+def test_outputs_across_inputs():
+    """An output in place has its input's strides; what other blocks still read is not written."""
+    L, a, b = emb.lib(), _m(0x4000, 64), _m(0x4000, 80)
+    other, out = _m(0x8000, 64), _m(0xc000, 64)
+    n, d, norm = 10, 32, _norm()
+
+    def fwd(x=other, residual=None, total=None, y=out, rows=n):
+        return L.emb_norm_fwd(rows, d, _ref(norm), _ref(x), _ref(residual), _ref(total), _ref(y), None, None)
+
+    for kw in (dict(x=a, y=b), dict(residual=a, total=b), dict(x=a, total=b), dict(residual=b, y=a)):
+        assert fwd(**kw) == EINVAL, kw
+
+    def bwd(total=other, dy=_m(0x9000), arriving=None, dtotal=None, dbranch=None):
+        return L.emb_norm_bwd(n, d, _ref(norm), _ref(total), _ref(dy), _ref(arriving), _ref(dtotal), _ref(dbranch),
+                              None, 0, None, 0, None)
+
+    for out_name in ("dtotal", "dbranch"):
+        for in_name in ("total", "dy", "arriving"):
+            assert bwd(**{out_name: a, in_name: b}) == EINVAL, (out_name, in_name)
+    assert L.emb_dropout(n, d, 0.5, 1, 0, _ref(a), _ref(b), None) == EINVAL
+    assert L.emb_logp_bwd(n, d, _ref(a), 0x1000, 4, 1.0, 0x2000, 0x3000, None, _ref(b), None) == EINVAL
+    assert L.emb_logp_train(n, d, _ref(a), 0x1000, 4, 1.0, 0x2000, 0x3000, None, _ref(b), None) == EINVAL
+    for logp, entropy in ((0x2000, None), (None, 0x2000)):
+        assert L.emb_logp_train(n, d, _ref(a), 0x1000, 4, 1.0, 0x2000, logp, entropy, _ref(out), None) == EINVAL
+    for at in (0x4000, 0x5000, 0x6000):
+        assert L.emb_linear_step(n, 2, 2, 16, 16, _ref(_m(0x4000)), _ref(_m(0x5000)), _ref(_m(0x6000)), 0x1000, 1.0,
+                                 0x2000, n, None, _ref(_m(at)), None) == EINVAL

@@ -206,3 +206,67 @@ def test_prompts_and_single_tokens():
         assert float((lp - want_lp[put(at)]).abs().max()) <= 2 * NEAR * float(want_lp.abs().max())
     untouched = [i for i in range(9) if i not in slots]
     assert (pool[untouched] == 7.0).all()
+
+
+def test_refusals_of_the_binding():
+    """Tensors that do not fit their call, are of other types, or lie elsewhere."""
+    import torch
+    import paper_2112_02752_amd as emb
+    x = lambda *shape: torch.zeros(shape, device="cuda")  # noqa: E731
+    norm = emb.Norm(x(16), max_rows=4)
+    for call in (lambda: norm.forward(x(4, 15), x(4, 16)), lambda: norm.forward(x(4, 16), x(3, 16)),
+                 lambda: norm.forward(x(4, 16), x(4, 16).cpu()), lambda: norm.forward(x(4, 16), x(4, 32)[:, ::2]),
+                 lambda: norm.forward(x(4, 16).half(), x(4, 16).half()),
+                 lambda: norm.backward(x(5, 16), x(5, 16), dweight=x(16)),
+                 lambda: norm.backward(x(4, 16), x(4, 16), dweight=x(15)),
+                 lambda: norm.backward(x(4, 16), x(4, 16), dweight=x(16).cpu()),
+                 lambda: norm.backward(x(4, 16), x(4, 16), dweight=x(16).double()),
+                 lambda: emb.dropout(x(4, 16), x(4, 17), 0.5, 1)):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: norm.forward(x(4, 16)), lambda: norm.forward(x(4, 16), x(4, 16).bfloat16()),
+                 lambda: norm.forward(x(4, 16), x(4, 16), residual=x(4, 16).bfloat16()),
+                 lambda: norm.forward(x(4, 16), x(4, 16), first_row=-1),
+                 lambda: emb.dropout(x(4, 16), x(4, 16), 1.0, 1)):
+        with pytest.raises(emb.EmbError):
+            call()
+
+    offsets = torch.tensor([0, 40, 70], dtype=torch.int32, device="cuda")
+    q, k, v, decay, states = x(70, 32), x(70, 16), x(70, 24), x(2), x(2, 2, 8, 12)
+    new = lambda **kw: emb.Heads(**{**dict(offsets=offsets, q=q, k=k, v=v, decay=decay, heads=4, groups=2), **kw})  # noqa: E731
+    for kw in (dict(heads=3), dict(groups=3), dict(q=x(70, 31)), dict(q=x(69, 32)), dict(v=x(69, 24)), dict(k=x(70, 15)),
+               dict(decay=x(3)), dict(decay=decay.cpu()), dict(decay=decay.double()), dict(first=x(3, 2, 8, 12)),
+               dict(first=states.cpu()), dict(offsets=offsets.long())):
+        with pytest.raises(ValueError):
+            new(**kw)
+    h = new()
+    att, small, served = (emb.LinearAttention(t, 2, 4, 2, 8, 12, train=train)
+                          for t, train in ((70, True), (69, True), (70, False)))
+    y = x(70, 48)
+    for call in (lambda: small.forward(h, y), lambda: att.forward(h, x(70, 47)), lambda: att.forward(h, y, last=x(1, 2, 8, 12)),
+                 lambda: att.forward(h, y.cpu()), lambda: att.forward(h, y, last=states.cpu()),
+                 lambda: att.backward(h, y, x(70, 32), x(70, 16), x(70, 24))):     # no forward yet
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(emb.EmbError):
+        att.forward(h, y.bfloat16())
+    att.forward(h, y)
+    served.forward(h, y)
+    with pytest.raises(ValueError, match="train"):
+        served.backward(h, y, x(70, 32), x(70, 16), x(70, 24))
+    with pytest.raises(ValueError):
+        att.backward(h, y, x(70, 32), x(70, 16), x(70, 23))
+    with pytest.raises(ValueError):
+        att.backward(h, y, x(70, 32), x(70, 16), x(70, 24), dlast=x(2, 2, 8, 11))
+    with pytest.raises(emb.EmbError):
+        att.backward(h, y, q, x(70, 16), x(70, 24))          # over its queries
+
+    one = lambda **kw: emb.linear_attention_step(**{**dict(  # noqa: E731
+        q=x(3, 32), k=x(3, 16), v=x(3, 24), decay=decay, state=x(5, 2, 8, 12), y=x(3, 48), heads=4, groups=2), **kw})
+    slots = torch.arange(3, dtype=torch.int32, device="cuda")
+    one(slots=slots)
+    for kw in (dict(slots=slots[:2]), dict(slots=slots.long()), dict(slots=slots.float()), dict(slots=slots.cpu()),
+               dict(state=x(2, 2, 8, 12)), dict(state=x(5, 2, 8, 11)), dict(decay=x(1)), dict(y=x(3, 47)), dict(q=x(2, 32))):
+        with pytest.raises(ValueError):
+            one(**kw)
+    torch.cuda.synchronize()
