@@ -48,11 +48,17 @@ def _declare(L) -> None:
 _SEED = (1 << 64) - 1
 
 
+_ask_device = None
+
+
 def _device_now() -> int:
     """The current device (where PyTorch offers it, without what its Python call adds)."""
-    import torch
-    raw = getattr(torch._C, "_cuda_getDevice", None)
-    return raw() if raw is not None and torch.cuda.is_initialized() else torch.cuda.current_device()
+    global _ask_device
+    if _ask_device is None:
+        import torch
+        torch.cuda.current_device()     # initialises
+        _ask_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    return _ask_device()
 
 
 def _here(mats, tensors) -> None:
@@ -60,7 +66,7 @@ def _here(mats, tensors) -> None:
     out) have to lie there."""
     now = _device_now()
     for m in mats:
-        if m is not None and m.tensor.get_device() != now:
+        if m is not None and m.device != now:
             raise ValueError("matrices lie on the current device (torch.cuda.device chooses it)")
     for t in tensors:
         if t is not None and t.get_device() != now:

@@ -68,7 +68,8 @@ class Mat:
     comes from ``Checkpoint.columns``.  Kept by a program between calls, it
     costs a call one address check."""
 
-    __slots__ = ("tensor", "exps", "rows", "cols", "_c", "_at", "_at_exps", "_fixed", "_first", "ref")
+    __slots__ = ("tensor", "exps", "rows", "cols", "_c", "_at", "_at_exps", "_fixed", "_first", "ref",
+                 "device")
 
     def __init__(self, tensor, exps=None, cols: Optional[int] = None, first: int = 0):
         self.tensor, self.exps, self._fixed, self._first = tensor, exps, cols, first
@@ -99,6 +100,7 @@ class Mat:
             raise ValueError(f"columns {first} on of {wide}")
         self.rows, self.cols = rows, wide - first if cols is None else cols
         at = self._at = tensor.data_ptr()
+        self.device = tensor.get_device()
         self._at_exps = exps.data_ptr() if exps is not None else None
         c = self._c
         c.ld, c.dtype, c.ld_exps = ld, dtype, le
