@@ -31,13 +31,13 @@
 // the rows of a chunk in LDS, loaded a step (a head of a chunk) ahead.  Products
 // a . b go through LDS once, from the wavefronts that make them to all.
 //
-// Bound.  One prompt of 32768 tokens, 16 heads of 128 x 128: 214 us, of which sums 77 (293 MB,
-// 3.8 TB/s), boundaries 13 and the form 125 (571 MB, 4.5 TB/s).  A training batch of 48
-// sequences, 32768 x 16 heads (4 key heads) of 128: forward 160 (sums 29, boundaries 17, the form
-// 115), backward 380 (sums 73, boundaries 17, the three forms 290, 1.09 GB at 3.8 TB/s).  There
-// LDS is busy a third of the time (its reads: every wavefront takes all rows of a and b),
-// the matrix units a fifth; the rest is the latency of a step's
-// phases at two blocks a compute unit, and the last round of blocks.
+// Bound.  One prompt of 32768 tokens, 16 heads of 128 x 128: 216 us, of which sums 75 (293 MB,
+// 3.9 TB/s), boundaries 13 and the form 133 (571 MB, 4.3 TB/s).  A training batch of 48
+// sequences, 32768 x 16 heads (4 key heads) of 128: forward 164 (sums 29, boundaries 16, the form
+// 119), backward 385 (sums 71, boundaries 16, the three forms 299, 1.09 GB at 3.6 TB/s) where a
+// profiler separates them, 464 together among calls.  There LDS is busy a third of the time (its
+// reads: every wavefront takes all rows of a and b), the matrix units a fifth; the rest is the
+// latency of a step's phases at two blocks a compute unit, and the last round of blocks.
 #include "block_common.h"
 
 namespace emb {
@@ -57,7 +57,7 @@ struct Operand;
 // v_mfma 16 x 16 x 32: eight of 32 indexes a lane, 8 q .. 8 q + 7; from a state 4 q + e and 16 + 4 q + e
 template <>
 struct Operand<bf16> {
-  static constexpr int kChunk = 64, kBlock = 32, kPad = 8, kVec = 8, kParts = 3;
+  static constexpr int kChunk = 64, kBlock = 32, kPad = 8, kVec = 8, kParts = 3, kWeights = 2;
   typedef uint16_t Value;
   // Distance of rows that are also read by columns: 12 (or 36) words past a multiple of 64 banks, so that 16 rows' 16
   // bytes as well as four rows' 32 bytes lie apart
@@ -106,7 +106,7 @@ struct Operand<bf16> {
 // v_mfma 16 x 16 x 4, four times: a lane's four of 16 indexes are 4 q .. 4 q + 3, one a time
 template <>
 struct Operand<float> {
-  static constexpr int kChunk = 32, kBlock = 16, kPad = 4, kVec = 4, kParts = 1;
+  static constexpr int kChunk = 32, kBlock = 16, kPad = 4, kVec = 4, kParts = 1, kWeights = 1;
   typedef float Value;
   static constexpr int apart(int w) { return w + kPad; }
   f32x4 v;
@@ -280,8 +280,9 @@ struct Rowset {
 template <typename T, int DA, int DC, bool OUT>
 struct Room {
   typedef Operand<T> Op;
-  static constexpr int C = Op::kChunk, LA = DA + Op::kPad, LB = Op::apart(DA), LC = Op::apart(DC), LP = C + Op::kPad;
-  alignas(16) typename Op::Value a[OUT ? C * LA : 8], b[C * LB], c[C * LC], p[OUT ? C * LP : 8];
+  static constexpr int C = Op::kChunk, LA = DA + Op::kPad, LB = Op::apart(DA), LC = Op::apart(DC), LP = C + Op::kPad,
+                       P = C * LP;
+  alignas(16) typename Op::Value a[OUT ? C * LA : 8], b[C * LB], c[C * LC], p[OUT ? Op::kWeights * P : 8];
   alignas(16) float fade[2 * C], pow[C + 1];
 };
 
@@ -424,15 +425,24 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
     load(next);
     if constexpr (OUT) {
       auto put_products = [&](f32x4 p, int i, int j, float fade) {
-        // (of tile i, j; weights of bf16 rows are rounded as the rows are: to bf16)
+        // (of tile i, j; weights of bf16 rows have two parts of bf16, 16 bits: with one alone a short sequence is off by
+        // 0.0024 of y where y's own rounding is 0.0015; the second part is 4% of a form's time)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float w = i == j ? on[e] : off[e] * fade;
           p[e] = 16 * (i - j) + l - 4 * q - e >= 0 ? p[e] * w : 0.f;
         }
         Value* to = s_p + (16 * i + l) * LP + 16 * j + 4 * q;
-        if constexpr (sizeof(Value) == 2) *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3])};
-        else *reinterpret_cast<f32x4*>(to) = p;
+        if constexpr (sizeof(Value) == 2) {
+#pragma unroll
+          for (int part = 0; part < Op::kWeights; ++part) {
+            const u32x2 w{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3])};
+            *reinterpret_cast<u32x2*>(to + part * Lds::P) = w;
+            p -= f32x4{bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
+          }
+        } else {
+          *reinterpret_cast<f32x4*>(to) = p;
+        }
       };
       if (new_a) {
         // What the state before the chunk gives (lane l: row 16 i + l % 16), and in order on the way, as the
@@ -506,10 +516,13 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
       for (int i = 0; i < TC; ++i)
 #pragma unroll
         for (int k = 0; k <= 16 * i / KB; ++k) {
-          Op y;
-          y.row(s_p + (16 * i + l) * LP + k * KB, q);
+          Op y[Op::kWeights];
 #pragma unroll
-          for (int t = 0; t < TN; ++t) mul(o[i][t], c[k][t], y);
+          for (int part = 0; part < Op::kWeights; ++part) y[part].row(s_p + part * Lds::P + (16 * i + l) * LP + k * KB, q);
+#pragma unroll
+          for (int t = 0; t < TN; ++t)
+#pragma unroll
+            for (int part = 0; part < Op::kWeights; ++part) mul(o[i][t], c[k][t], y[part]);
         }
       {
         // (to nowhere where nothing is to be stored yet: as many stores follow the loads in every step, so that the
