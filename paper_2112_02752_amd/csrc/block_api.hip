@@ -52,7 +52,6 @@ emb_status check_norm(int64_t rows, int32_t dim, const emb_norm* norm, const emb
   p->D = dim;
   p->eps = norm->eps;
   p->weight = norm->weight;
-  p->aligned = ((uintptr_t)norm->weight & 15u) == 0;
   if (rows == 0) return EMB_OK;
   if (x == nullptr || x->data == nullptr) return EMB_EINVAL;
   p->dtype = x->dtype;
@@ -173,7 +172,6 @@ emb_status emb_norm_fwd(int64_t rows, int32_t dim, const emb_norm* norm, const e
   }
   if (p.y.p == nullptr && p.saved.p == nullptr) return EMB_EINVAL;
   if (across(rows, p.total, {p.x, p.residual}) || across(rows, p.y, {p.x, p.residual})) return EMB_EINVAL;
-  p.aligned = p.aligned && vectors(p.x) && vectors(p.residual) && vectors(p.total) && vectors(p.y);
   return hip_status(launch_norm_fwd(p, (hipStream_t)stream));
 }
 
@@ -203,8 +201,6 @@ emb_status emb_norm_bwd(int64_t rows, int32_t dim, const emb_norm* norm, const e
     if ((st = check_opt(dbranch, dim, p.dtype, &p.dbranch)) != EMB_OK) return st;
     for (const Rows& out : {p.dtotal, p.dbranch})
       if (across(rows, out, {p.total, p.dy, p.arriving})) return EMB_EINVAL;
-    p.aligned = p.aligned && vectors(p.total) && vectors(p.dy) && vectors(p.arriving) && vectors(p.dtotal) &&
-                vectors(p.dbranch);
   }
   if (rows == 0 && dweight == nullptr) return EMB_OK;
   p.dweight = dweight;
@@ -230,7 +226,6 @@ emb_status emb_dropout(int64_t rows, int32_t dim, float drop, uint64_t seed, int
   p.x = rows_of(*x);
   p.y = rows_of(*y);
   if (across(rows, p.y, {p.x})) return EMB_EINVAL;
-  p.aligned = vectors(p.x) && vectors(p.y);
   return hip_status(launch_dropout(p, (hipStream_t)stream));
 }
 

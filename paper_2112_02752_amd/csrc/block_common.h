@@ -19,7 +19,6 @@ constexpr int kNormMaxDim = 16384;
 struct NormLaunch {
   int64_t N;
   int32_t D, dtype, stream_dtype;
-  int32_t aligned;  // every matrix and row begins at a multiple of 16 bytes
   float eps;
   const float* weight;
   Drop drop;
@@ -36,7 +35,7 @@ hipError_t launch_norm_bwd(const NormLaunch& p, hipStream_t s);
 
 struct DropLaunch {
   int64_t N;
-  int32_t D, dtype, aligned;
+  int32_t D, dtype;
   Drop drop;
   Rows x, y;
 };

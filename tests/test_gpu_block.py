@@ -37,7 +37,10 @@ def _data(rng, n, d, dtype, gap, shift, std=1.0):
 SIZES = [(1, 1, 0, 0), (1, 8, 0, 0), (5, 3, 1, 0), (3, 512, 0, 0), (70, 513, 0, 1), (9, 520, 8, 0), (33, 1024, 8, 8),
          (6, 1030, 0, 0), (64, 1536, 0, 0), (5, 2048, 0, 0), (4, 2049, 0, 3), (3, 2056, 0, 0), (7, 4096, 0, 0),
          (3, 4100, 0, 0), (2, 8192, 0, 0), (3, 8200, 8, 0), (2, 16384, 0, 0), (2, 16383, 0, 0), (3001, 40, 0, 0),
-         (2500, 264, 8, 0), (0, 64, 0, 0)]
+         (2500, 264, 8, 0), (0, 64, 0, 0),
+         # several rows a wavefront, the last ones of a block not there
+         (57, 64, 0, 0), (58, 63, 0, 1), (3, 24, 8, 8), (1025, 13, 0, 0), (61, 65, 3, 0), (129, 128, 0, 0), (2101, 120, 8, 1),
+         (37, 127, 0, 1), (66, 129, 0, 0), (41, 250, 6, 1), (43, 256, 0, 3), (47, 257, 0, 0)]
 
 
 @pytest.mark.parametrize("types", [("fp32", "fp32"), ("bf16", "bf16"), ("bf16", "fp32")])
@@ -148,6 +151,38 @@ def test_norm_extreme_rows():
     assert torch.allclose(y[2], torch.ones(96), rtol=32 * U) and torch.allclose(y[5], torch.ones(96), rtol=1e-6)
     assert torch.isnan(y[3, 5]) and (y[3, :5] == 0).all() and torch.isnan(y[4]).all()
     assert saved.exps.cpu()[3].tolist()[0] == 255 and (saved.exps.cpu()[4] == 255).all()
+
+
+@pytest.mark.parametrize("d", [40, 61, 136, 250, 264, 1000, 1029, 4104])
+def test_infinities_at_a_rows_end(d):
+    """They keep to their row, where lanes past its end read them again."""
+    import torch
+    import paper_2112_02752_amd as emb
+    n = 21
+    rng = np.random.default_rng(d)
+    total, dy = (torch.from_numpy(rng.standard_normal((n, d)).astype(np.float32)).to(DEV) for _ in range(2))
+    total[4, d - 1], total[11, d - 2], dy[7, d - 1], dy[13, d - 3] = (float(v) for v in ("inf", "nan", "inf", "nan"))
+    bad = {4, 7, 11, 13}
+    norm = emb.Norm(torch.ones(d, device=DEV), max_rows=n)
+    y, kept_total, dtotal, dbranch = (torch.empty_like(dy) for _ in range(4))
+    norm.forward(total, y, total=kept_total)
+    norm.backward(kept_total, dy, dtotal=dtotal, branch=dbranch)
+    t, g = host(total), host(dy)
+    with np.errstate(all="ignore"):
+        inv = 1 / np.sqrt((t * t).mean(1, keepdims=True) + 1e-6)
+        along = (g * t * inv).mean(1, keepdims=True)
+        want_y, want_d = t * inv, inv * (g - t * inv * along)
+    for i in range(n):
+        if i in (4, 11):
+            assert np.array_equal(np.isfinite(host(y)[i]), np.isfinite(want_y[i])), i
+        else:       # a sum of d terms, in at most 64 of a lane and 12 of lanes
+            within(y[i], want_y[i], (2 * 80) * U * np.abs(want_y[i]), i)
+        if i in bad:
+            assert not np.isfinite(host(dtotal)[i]).any() or i == 4, i
+        else:
+            near = 4 * 80 * U * inv[i] * (np.abs(g[i]) + np.abs(t[i] * inv[i]) * np.abs(g[i] * t[i] * inv[i]).mean())
+            within(dtotal[i], want_d[i], near, i)
+            assert torch.equal(dbranch[i], dtotal[i])
 
 
 @pytest.mark.parametrize("kind", ["fp32", "bf16"])
