@@ -141,6 +141,7 @@ struct Form {
   int32_t da, dc;       // widths of a and b, of c and out
   int32_t sd, sn;       // state: distance of two indexes of b, of c
   int32_t rev;          // backwards
+  int32_t cols;         // columns of c that a block takes
   float p_scale, u_scale, out_scale;  // of products a . b, of what the state gets, of out
 };
 
@@ -717,7 +718,7 @@ int log_length(int64_t N, int groups) {
 
 // Columns of c that a block takes, and the widest a and b of the kernel that does (rows that are not aligned
 // are for any width up to 128, or to 256).
-int columns_of(const Args& a, int da, int dc) { return !a.aligned || da > 128 || dc <= 64 ? 64 : 128; }
+int columns_of(const Args& a, int da, int dc, bool narrow) { return narrow || !a.aligned || da > 128 || dc <= 64 ? 64 : 128; }
 int width_of(const Args& a, int da) { return da > 128 ? 256 : a.aligned && da <= 64 ? 64 : 128; }
 
 // Blocks that the device holds at once: two a compute unit.
@@ -740,7 +741,7 @@ hipError_t go(const Args& a, int first, int forms, hipStream_t s) {
   blocks *= parts;
   if (blocks == 0) return hipSuccess;
   const unsigned grid = (unsigned)blocks;
-  const int da = width_of(a, f.da), dc = columns_of(a, f.da, f.dc);
+  const int da = width_of(a, f.da), dc = f.cols;
   if (!a.aligned) {
     if (da == 128) k_linear<T, 128, 64, 4, OUT, false><<<grid, kThreads, 0, s>>>(a, first, forms, parts);
     else k_linear<T, 256, 64, 4, OUT, false><<<grid, kThreads, 0, s>>>(a, first, forms, parts);
@@ -758,7 +759,7 @@ hipError_t go(const Args& a, int first, int forms, hipStream_t s) {
 // whether two forms are taken by the same kernel
 bool alike(const Args& a, int i, int j) {
   return width_of(a, a.f[i].da) == width_of(a, a.f[j].da) &&
-         columns_of(a, a.f[i].da, a.f[i].dc) == columns_of(a, a.f[j].da, a.f[j].dc) && a.slices[i] == a.slices[j];
+         a.f[i].cols == a.f[j].cols && a.slices[i] == a.slices[j];
 }
 
 template <bool REV>
@@ -772,9 +773,10 @@ hipError_t chain(const Args& a, const float* begin, hipStream_t s) {
   return hipGetLastError();
 }
 
-void add_form(Args& a, int which, const Form& f) {
+void add_form(Args& a, int which, const Form& f, bool narrow = false) {
   a.f[which] = f;
-  a.slices[which] = (f.dc + columns_of(a, f.da, f.dc) - 1) / columns_of(a, f.da, f.dc);
+  a.f[which].cols = columns_of(a, f.da, f.dc, narrow);
+  a.slices[which] = (f.dc + a.f[which].cols - 1) / a.f[which].cols;
 }
 
 void prepare(const LinLaunch& p, Args& a) {
@@ -797,12 +799,21 @@ bool fits(const Args& a, int forms) {
          launchable(a.bounds * a.groups * ((a.state + kThreads - 1) / kThreads), kThreads);
 }
 
+// fp32 products are most of a wavefront's time (matrix units do a fraction of the bf16 ones): blocks of half the
+// columns, as long as the device holds them at once.  Forward and backward of 4 heads of 128 x 128, 1001 tokens in 4
+// sequences, 2 key heads: 62 us, 87 with whole ones; 2001 tokens, one key head: 83 and 114.
+template <typename T>
+bool narrow(const Args& a, int forms) {
+  return sizeof(T) == 4 && 2 * forms * (a.bounds + a.M) * a.groups <= kResident;
+}
+
 template <typename T>
 hipError_t forward(const LinLaunch& p, hipStream_t s) {
   Args a{};
   prepare(p, a);
   a.sums = p.states;
-  add_form(a, 0, Form{p.q, p.k, p.v, p.y, p.states, p.first, p.last, p.dk, p.dv, p.dv, 1, 0, 1.f, 1.f, p.scale});
+  add_form(a, 0, Form{p.q, p.k, p.v, p.y, p.states, p.first, p.last, p.dk, p.dv, p.dv, 1, 0, 0, 1.f, 1.f, p.scale},
+           narrow<T>(a, a.per));
   if (!fits(a, 1)) return hipErrorNotSupported;
   hipError_t e = go<T, false>(a, 0, 1, s);
   if (e == hipSuccess) e = chain<false>(a, p.first, s);
@@ -815,9 +826,12 @@ hipError_t backward(const LinLaunch& p, hipStream_t s) {
   Args a{};
   prepare(p, a);
   a.sums = p.grads;
-  add_form(a, 0, Form{p.k, p.q, p.dy, p.dval, p.grads, p.dlast, p.dfirst, p.dk, p.dv, p.dv, 1, 1, p.scale, p.scale, 1.f});
-  add_form(a, 1, Form{p.v, p.dy, p.q, p.dkey, p.grads, p.dlast, nullptr, p.dv, p.dk, 1, p.dv, 1, p.scale, p.scale, 1.f});
-  add_form(a, 2, Form{p.dy, p.v, p.k, p.dq, p.states, p.first, nullptr, p.dv, p.dk, 1, p.dv, 0, 1.f, 1.f, p.scale});
+  add_form(a, 0, Form{p.k, p.q, p.dy, p.dval, p.grads, p.dlast, p.dfirst, p.dk, p.dv, p.dv, 1, 1, 0, p.scale, p.scale, 1.f},
+           narrow<T>(a, 1));
+  add_form(a, 1, Form{p.v, p.dy, p.q, p.dkey, p.grads, p.dlast, nullptr, p.dv, p.dk, 1, p.dv, 1, 0, p.scale, p.scale, 1.f},
+           narrow<T>(a, 2));
+  add_form(a, 2, Form{p.dy, p.v, p.k, p.dq, p.states, p.first, nullptr, p.dv, p.dk, 1, p.dv, 0, 0, 1.f, 1.f, p.scale},
+           narrow<T>(a, 2));
   if (!fits(a, 3)) return hipErrorNotSupported;
   hipError_t e = go<T, false>(a, 0, 1, s);
   if (e == hipSuccess) e = chain<true>(a, p.dlast, s);
