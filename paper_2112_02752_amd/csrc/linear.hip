@@ -31,11 +31,11 @@
 // the rows of a chunk in LDS, loaded a step (a head of a chunk) ahead.  Products
 // a . b go through LDS once, from the wavefronts that make them to all.
 //
-// Bound.  One prompt of 32768 tokens, 16 heads of 128 x 128: 216 us, of which sums 75 (293 MB,
+// Bound.  One prompt of 32768 tokens, 16 heads of 128 x 128: 220 us, of which sums 75 (293 MB,
 // 3.9 TB/s), boundaries 13 and the form 133 (571 MB, 4.3 TB/s).  A training batch of 48
 // sequences, 32768 x 16 heads (4 key heads) of 128: forward 164 (sums 29, boundaries 16, the form
 // 119), backward 385 (sums 71, boundaries 16, the three forms 299, 1.09 GB at 3.6 TB/s) where a
-// profiler separates them, 464 together among calls.  There LDS is busy a third of the time (its
+// profiler separates them, 471 together among calls.  There LDS is busy a third of the time (its
 // reads: every wavefront takes all rows of a and b), the matrix units a fifth; the rest is the
 // latency of a step's phases at two blocks a compute unit, and the last round of blocks.
 #include "block_common.h"
@@ -141,7 +141,6 @@ struct Form {
   int32_t da, dc;       // widths of a and b, of c and out
   int32_t sd, sn;       // state: distance of two indexes of b, of c
   int32_t rev;          // backwards
-  int32_t cols;         // columns of c that a block takes
   float p_scale, u_scale, out_scale;  // of products a . b, of what the state gets, of out
 };
 
@@ -156,6 +155,7 @@ struct Args {
   Form f[3];
   int32_t slices[3];
   float* sums;
+  int32_t cols[3];  // columns of c that a block takes
 };
 
 // g^e for a whole e >= 0, in 64 bits
@@ -741,7 +741,7 @@ hipError_t go(const Args& a, int first, int forms, hipStream_t s) {
   blocks *= parts;
   if (blocks == 0) return hipSuccess;
   const unsigned grid = (unsigned)blocks;
-  const int da = width_of(a, f.da), dc = f.cols;
+  const int da = width_of(a, f.da), dc = a.cols[first];
   if (!a.aligned) {
     if (da == 128) k_linear<T, 128, 64, 4, OUT, false><<<grid, kThreads, 0, s>>>(a, first, forms, parts);
     else k_linear<T, 256, 64, 4, OUT, false><<<grid, kThreads, 0, s>>>(a, first, forms, parts);
@@ -759,7 +759,7 @@ hipError_t go(const Args& a, int first, int forms, hipStream_t s) {
 // whether two forms are taken by the same kernel
 bool alike(const Args& a, int i, int j) {
   return width_of(a, a.f[i].da) == width_of(a, a.f[j].da) &&
-         a.f[i].cols == a.f[j].cols && a.slices[i] == a.slices[j];
+         a.cols[i] == a.cols[j] && a.slices[i] == a.slices[j];
 }
 
 template <bool REV>
@@ -775,8 +775,8 @@ hipError_t chain(const Args& a, const float* begin, hipStream_t s) {
 
 void add_form(Args& a, int which, const Form& f, bool narrow = false) {
   a.f[which] = f;
-  a.f[which].cols = columns_of(a, f.da, f.dc, narrow);
-  a.slices[which] = (f.dc + a.f[which].cols - 1) / a.f[which].cols;
+  a.cols[which] = columns_of(a, f.da, f.dc, narrow);
+  a.slices[which] = (f.dc + a.cols[which] - 1) / a.cols[which];
 }
 
 void prepare(const LinLaunch& p, Args& a) {
@@ -812,7 +812,7 @@ hipError_t forward(const LinLaunch& p, hipStream_t s) {
   Args a{};
   prepare(p, a);
   a.sums = p.states;
-  add_form(a, 0, Form{p.q, p.k, p.v, p.y, p.states, p.first, p.last, p.dk, p.dv, p.dv, 1, 0, 0, 1.f, 1.f, p.scale},
+  add_form(a, 0, Form{p.q, p.k, p.v, p.y, p.states, p.first, p.last, p.dk, p.dv, p.dv, 1, 0, 1.f, 1.f, p.scale},
            narrow<T>(a, a.per));
   if (!fits(a, 1)) return hipErrorNotSupported;
   hipError_t e = go<T, false>(a, 0, 1, s);
@@ -826,11 +826,11 @@ hipError_t backward(const LinLaunch& p, hipStream_t s) {
   Args a{};
   prepare(p, a);
   a.sums = p.grads;
-  add_form(a, 0, Form{p.k, p.q, p.dy, p.dval, p.grads, p.dlast, p.dfirst, p.dk, p.dv, p.dv, 1, 1, 0, p.scale, p.scale, 1.f},
+  add_form(a, 0, Form{p.k, p.q, p.dy, p.dval, p.grads, p.dlast, p.dfirst, p.dk, p.dv, p.dv, 1, 1, p.scale, p.scale, 1.f},
            narrow<T>(a, 1));
-  add_form(a, 1, Form{p.v, p.dy, p.q, p.dkey, p.grads, p.dlast, nullptr, p.dv, p.dk, 1, p.dv, 1, 0, p.scale, p.scale, 1.f},
+  add_form(a, 1, Form{p.v, p.dy, p.q, p.dkey, p.grads, p.dlast, nullptr, p.dv, p.dk, 1, p.dv, 1, p.scale, p.scale, 1.f},
            narrow<T>(a, 2));
-  add_form(a, 2, Form{p.dy, p.v, p.k, p.dq, p.states, p.first, nullptr, p.dv, p.dk, 1, p.dv, 0, 0, 1.f, 1.f, p.scale},
+  add_form(a, 2, Form{p.dy, p.v, p.k, p.dq, p.states, p.first, nullptr, p.dv, p.dk, 1, p.dv, 0, 1.f, 1.f, p.scale},
            narrow<T>(a, 2));
   if (!fits(a, 3)) return hipErrorNotSupported;
   hipError_t e = go<T, false>(a, 0, 1, s);
