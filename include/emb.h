@@ -597,10 +597,10 @@ emb_status emb_dropout(int64_t rows, int32_t dim, float drop, uint64_t seed, int
  * heads / groups query heads share a key head.  Sequence m holds positions
  * offsets[m] .. offsets[m+1]-1 as in emb_scan; rows from offsets[num_seqs] on
  * are neither read nor written.  Inputs and outputs are of one type, fp32 or bf16.
- * States and sums are fp32.  With bf16 rows, the state is rounded to bf16 where
- * rows are multiplied with it, weights within a chunk of 64 positions to 16
- * bits, and what the state gets of a row to 16 bits within a segment; a state
- * that is kept from one segment or call to the next gets it with 24.  An
+ * States and sums are fp32.  With bf16 rows, the state where rows are multiplied
+ * with it, weights within a chunk of 64 positions and what the state gets of a
+ * row within a segment are rounded to 16 bits; a state that is kept from one
+ * segment or call to the next gets it with 24.  An
  * infinity or NaN in a row spoils results of its sequence alone: from its
  * chunk's first position on, in the backward also those before it.
  * EMB_EUNSUPPORTED for dk or dv above 256, and for rows of more than 16 MB from

@@ -57,7 +57,7 @@ struct Operand;
 // v_mfma 16 x 16 x 32: eight of 32 indexes a lane, 8 q .. 8 q + 7; from a state 4 q + e and 16 + 4 q + e
 template <>
 struct Operand<bf16> {
-  static constexpr int kChunk = 64, kBlock = 32, kPad = 8, kVec = 8, kParts = 3, kWeights = 2;
+  static constexpr int kChunk = 64, kBlock = 32, kPad = 8, kVec = 8, kParts = 3, kWeights = 2, kStates = 2;
   typedef uint16_t Value;
   // Distance of rows that are also read by columns: 12 (or 36) words past a multiple of 64 banks, so that 16 rows' 16
   // bytes as well as four rows' 32 bytes lie apart
@@ -80,9 +80,12 @@ struct Operand<bf16> {
     const u32x2 a = __builtin_bit_cast(u32x2, lo), b = __builtin_bit_cast(u32x2, hi);
     v = __builtin_bit_cast(bf16x8, u32x4{a.x, a.y, b.x, b.y});
   }
-  // 32 indexes of a state: two tiles
-  __device__ __forceinline__ void state(f32x4 a, f32x4 b) {
-    v = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w)});
+  // 32 indexes of a state, two tiles: the nearest to them, which are left with what that leaves of them
+  __device__ __forceinline__ void state(f32x4& a, f32x4& b) {
+    const u32x4 w{pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w)};
+    v = __builtin_bit_cast(bf16x8, w);
+    a -= f32x4{bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
+    b -= f32x4{bf16_lo(w.z), bf16_hi(w.z), bf16_lo(w.w), bf16_hi(w.w)};
   }
   __device__ __forceinline__ float get(int e) const {
     const uint32_t w = __builtin_bit_cast(u32x4, v)[e / 2];
@@ -106,7 +109,7 @@ struct Operand<bf16> {
 // v_mfma 16 x 16 x 4, four times: a lane's four of 16 indexes are 4 q .. 4 q + 3, one a time
 template <>
 struct Operand<float> {
-  static constexpr int kChunk = 32, kBlock = 16, kPad = 4, kVec = 4, kParts = 1, kWeights = 1;
+  static constexpr int kChunk = 32, kBlock = 16, kPad = 4, kVec = 4, kParts = 1, kWeights = 1, kStates = 1;
   typedef float Value;
   static constexpr int apart(int w) { return w + kPad; }
   f32x4 v;
@@ -117,7 +120,7 @@ struct Operand<float> {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = at[(4 * q + e) * LD + APART * (l / 4) + l % 4];
   }
-  __device__ __forceinline__ void state(f32x4 a, f32x4) { v = a; }
+  __device__ __forceinline__ void state(const f32x4& a, const f32x4&) { v = a; }
   __device__ __forceinline__ float get(int e) const { return v[e]; }
   __device__ __forceinline__ void take(const float (&x)[4]) { v = f32x4{x[0], x[1], x[2], x[3]}; }
   static __device__ __forceinline__ int index(int q, int e) { return 4 * q + e; }
@@ -412,7 +415,7 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
     for (int i = 0; i < 2 * kSide - 1; ++i) less[i] = lane_at(s_pow[16 * max(ti - tj + i - kSide, 0)], 0);
   }
   // A state that is kept gets weighted rows with all of their 24 bits, in three parts; one that only
-  // multiplies rows of this segment, and is rounded to bf16 for that, gets 16 of them.
+  // multiplies rows of this segment, and is rounded to 16 bits for that, gets 16 of them.
   const bool exact = f.end != nullptr && begin == 0 && (rev ? s.first : s.last);
   f32x4 o[TC][TN];
   while (now.at < length) {
@@ -458,17 +461,26 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
         }
 #pragma unroll
         for (int k = 0; k < KD; ++k) {
-          Op x[TN], z;
+          Op x[Op::kStates][TN], z;
           if constexpr (!rev) z.row_as_state(s_b + (16 * (wave % TC) + l) * LB + k * KB, q);
+          // (of bf16 rows, the state has two parts, 16 bits: results that cancel in it, as queries across a component that
+          // keys and values share have them, were off by up to a seventh of y with one; 32768 tokens, 16 heads of 128 x
+          // 128: 220 us, 216 with one part; their training with 4 key heads: 491, 466 with one)
 #pragma unroll
-          for (int t = 0; t < TN; ++t) x[t].state(st[k * KB / 16][t], st[(k * KB / 16 + 1) % TD][t]);
+          for (int t = 0; t < TN; ++t) {
+            f32x4 lo = st[k * KB / 16][t], hi = st[(k * KB / 16 + 1) % TD][t];
+#pragma unroll
+            for (int part = 0; part < Op::kStates; ++part) x[part][t].state(lo, hi);
+          }
 #pragma unroll
           for (int i = 0; i < TC; ++i) {
             Op y;
             y.row_as_state(s_a + (16 * i + l) * LA + k * KB, q);
             if constexpr (!rev) mul(p[i], z, y);
 #pragma unroll
-            for (int t = 0; t < TN; ++t) mul(o[i][t], x[t], y);
+            for (int t = 0; t < TN; ++t)
+#pragma unroll
+              for (int part = 0; part < Op::kStates; ++part) mul(o[i][t], x[part][t], y);
           }
         }
 #pragma unroll
