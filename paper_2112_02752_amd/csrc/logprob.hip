@@ -362,10 +362,10 @@ __global__ __launch_bounds__(kBlock<W>, R <= 8 ? 8 : 4) void k_logp(LogpLaunch a
   }
   // Too many reach it (ties, tokens that cannot be, NaN): every wavefront's best one after another; a lane
   // looks through its columns again, in memory, when its best has been taken.  Then the wavefronts' lists are
-  // merged.
+  // merged.  (The lists lie over the row's own candidates: other rows of the block are not waited for.)
   if constexpr (W > 1) __syncthreads();
-  uint64_t* const list = &s_list[0][0] + wave * EMB_MAX_TOP;
-  static_assert(kBlock<W> / kWave * EMB_MAX_TOP <= kCandidates, "a list for every wavefront");
+  uint64_t* const list = s_list[mate] + wave % W * EMB_MAX_TOP;
+  static_assert(W * EMB_MAX_TOP <= kMost, "a list for every wavefront of a row");
   auto best_below = [&](uint64_t limit) {
     uint64_t best = 0;
     if (own >= 0) {
@@ -393,13 +393,13 @@ __global__ __launch_bounds__(kBlock<W>, R <= 8 ? 8 : 4) void k_logp(LogpLaunch a
     __syncthreads();
     if (wave > 0) return;
     int taken = 0;
-    next = lane < W ? s_list[0][lane * EMB_MAX_TOP] : 0;
+    next = lane < W ? s_list[mate][lane * EMB_MAX_TOP] : 0;
     for (int i = 0; i < a.top; ++i) {
       const uint64_t best = wave_max_key(next);
       if (lane == 0) put(i, best);
       if (next == best && lane < W) {
         ++taken;
-        next = taken < a.top ? s_list[0][lane * EMB_MAX_TOP + taken] : 0;
+        next = taken < a.top ? s_list[mate][lane * EMB_MAX_TOP + taken] : 0;
       }
     }
   } else {
