@@ -67,10 +67,11 @@ struct Row {
   }
 };
 
-// Order of the alternatives: greater values first (NaN before all, both zeros alike), then lower columns.
+// Order of the alternatives: greater values first (NaN before all, both zeros alike), then lower columns.  No key is all
+// ones or zero, the limit of a first search and what finds nothing.
 __device__ __forceinline__ uint64_t order_key(float x, int col) {
   uint32_t u = __float_as_uint(x + 0.f);
-  if (x != x) u = 0x7fffffffu;
+  if (x != x) u = 0x7fc00000u;
   u = (u & 0x80000000u) != 0 ? ~u : u | 0x80000000u;
   return (uint64_t)u << 32 | (uint32_t)~col;
 }

@@ -72,3 +72,23 @@ def test_rows_of_a_block(d, top, kind):
         a, b = a.double(), b.double()
         same |= (a - b).abs() <= U * (2 * (160 + 2.25 * d / 1024) + 2 * np.log(d) + 2 * (a.abs() + b.abs()))
     assert same.all()
+
+
+@pytest.mark.parametrize("kind", ["fp32", "bf16"])
+@pytest.mark.parametrize("d", [9, 100, 600, 3001, 20000, 300000])
+@pytest.mark.parametrize("top", [1, 5, 32])
+def test_nan_is_the_largest_from_column_zero_on(d, top, kind):
+    """Rows of NaN in the first column, the first few, the last and first, and all: lowest columns first, then the numbers."""
+    import torch
+    import paper_2112_02752_amd as emb
+    top = min(top, d)
+    x = torch.arange(d, dtype=torch.float32).remainder(7).repeat(6, 1)
+    x[0, 0] = x[1, :3] = x[2, 0] = x[2, d - 1] = x[3] = np.nan
+    x[4, d - 1] = np.nan
+    x = x.to(dt(kind)).to(DEV)
+    x[5, 0] = -torch.full((), np.nan, device=DEV)       # its sign is nothing
+    ids, logp = torch.full((6, top), -7, dtype=torch.int32, device=DEV), torch.zeros((6, top), device=DEV)
+    emb.LogProbs(6, d, top=top).forward(x, None, None, top_ids=ids, top_logp=logp)
+    want = np.argsort(np.where(np.isnan(host(x)), -np.inf, -host(x)), axis=1, kind="stable")[:, :top]
+    assert np.array_equal(ids.cpu().numpy(), want)
+    assert logp.isnan().all()
