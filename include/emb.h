@@ -659,7 +659,9 @@ emb_status emb_linear_step(int64_t num_tokens, int32_t heads, int32_t groups, in
  * (usually -1) stands for no token: its logp is 0, and it contributes nothing
  * to a gradient.  A logit of minus infinity is a token that cannot be; where no
  * token can, logp and top_logp are minus infinity, entropy and gradient zero.
- * NaN and plus infinity make their row's results NaN.  Sums are fp32.
+ * Large finite numbers in its place (masks of any size, the lowest among them) are
+ * logits like others: a row of nothing else is uniform.  NaN and plus infinity
+ * make their row's results NaN.  Sums are fp32.
  * ids: device int32 or int64 (id_bytes 4 or 8).  logp, entropy (device fp32
  * [rows]) may each be NULL, ids with logp.  top 0 .. EMB_MAX_TOP and <= cols;
  * top_ids (device int32), top_logp (device fp32): [rows][top].  stats: device

@@ -75,8 +75,8 @@ struct LinStepLaunch {
 };
 hipError_t launch_lin_step(const LinStepLaunch& p, hipStream_t s);
 
-// Statistics of a row of logits that its gradient needs: the power M of two
-// that it is relative to, sum of 2^(scale log2(e) logit - M), entropy, one value unused.
+// Statistics of a row of logits that its gradient needs: the largest logit m (zero where no token can be), sum of
+// 2^(scale log2(e) (logit - m)), entropy, one value unused.
 constexpr int kStats = 4;
 constexpr int32_t kLogpMaxCols = 1 << 30;
 struct LogpLaunch {

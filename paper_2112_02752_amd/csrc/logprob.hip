@@ -16,6 +16,8 @@
 // fp32: forward 30 us (4.0 TB/s), gradient from the statistics 37 (6.4 TB/s).  64 x 50000
 // with 8 alternatives, a row a compute unit: 10.3 us, of which the exponentials
 // and sums of 50000 values by one compute unit take about 3, their loads as long.
+#include <float.h>
+
 #include "block_common.h"
 
 namespace emb {
@@ -23,7 +25,7 @@ namespace emb {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kLowest = -1e30f;  // in place of minus infinity where a probability of zero multiplies it
+constexpr float kLowest = -1024.f;  // in place of lower powers where what they are multiplied with is zero
 constexpr float kLn2 = 0.69314718055994530942f;
 
 // A row of D values: whole vectors of 16 bytes where it lies on them, and before the first and after the last of them a
@@ -93,28 +95,31 @@ __device__ __forceinline__ int64_t id_of(const LogpLaunch& a, int64_t row) {
   return a.id_bytes == 8 ? static_cast<const int64_t*>(a.ids)[row] : (int64_t) static_cast<const int32_t*>(a.ids)[row];
 }
 
-// Exponents are taken to the base of two: with t = scale log2(e) and M = t m, rounded once, a value's power is
-// t x - M in one operation, and its error in M is the same for all of a row, so that it leaves probabilities
-// as they are.  Sums of a part of a row, relative to its own M:
+// Exponents are taken to the base of two: with t = scale log2(e) a value's power is (x - m) t, m being the largest value.
+// The difference is formed first: t x - t m by one operation has the rounding of t m as its error, which for masks of
+// large finite numbers is more than exponents are (some hundreds at 1e10), and a part of a row may hold nothing else.  Sums of a
+// part of a row, relative to its own m:
 struct Sums {
-  float m, s, a;  // M, sum of 2^(t x - M), sum of 2^(t x - M) (t x - M)
+  float m, s, a;  // m, sum of 2^((x - m) t), sum of 2^((x - m) t) (x - m) t
 };
-// the part's M from its largest value: where no token can be, every difference would be NaN
-__device__ __forceinline__ float reference(float t, float top) { return top == -INFINITY ? 0.f : t * top; }
+// the part's m from its largest value: where no token can be, every difference would be NaN
+__device__ __forceinline__ float reference(float top) { return top == -INFINITY ? 0.f : top; }
+// (a power of zero where x is m, whatever the scale)
+__device__ __forceinline__ float base2(float scale) { return fminf(scale * kLog2e, FLT_MAX); }
 // x's power, and its share of the sums
 __device__ __forceinline__ void add_value(float x, float t, Sums& p) {
-  const float z = __builtin_fmaf(x, t, -p.m), e = __builtin_amdgcn_exp2f(z);
+  const float z = (x - p.m) * t, e = __builtin_amdgcn_exp2f(z);
   p.s += e;
   p.a = __builtin_fmaf(e, fmaxf(z, kLowest), p.a);
 }
-__device__ __forceinline__ void refer_to(float m, Sums& p) {
-  const float by = p.m - m, f = __builtin_amdgcn_exp2f(by);
-  p.a = f * (p.a + p.s * by);
+__device__ __forceinline__ void refer_to(float m, float t, Sums& p) {
+  const float by = (p.m - m) * t, f = __builtin_amdgcn_exp2f(by);
+  p.a = f * __builtin_fmaf(p.s, fmaxf(by, kLowest), p.a);
   p.s *= f;
   p.m = m;
 }
 
-// What a row's gradient is made of: dx_v = e_v (all + slope (t x_v - M)), and at the id's column `hot` more
+// What a row's gradient is made of: dx_v = e_v (all + slope (x_v - m) t), and at the id's column `hot` more
 struct Slope {
   float t, m, all, slope, hot;
   int64_t id;
@@ -132,7 +137,7 @@ struct Slope {
   }
   template <bool ENTROPY>
   __device__ __forceinline__ float value(float x) const {
-    const float z = __builtin_fmaf(x, t, -m), e = __builtin_amdgcn_exp2f(z);
+    const float z = (x - m) * t, e = __builtin_amdgcn_exp2f(z);
     if constexpr (ENTROPY) return e * __builtin_fmaf(slope, fmaxf(z, kLowest), all);
     return e * all;
   }
@@ -188,7 +193,7 @@ __global__ __launch_bounds__(kBlock<W>, R <= 8 ? 8 : 4) void k_logp(LogpLaunch a
     if (t == 0) s_count[wave / W] = 0;
   }
   const Row<T> r(a.logits.p + row * a.logits.ld, a.D);
-  const float base2 = a.scale * kLog2e;
+  const float t2 = base2(a.scale);
   V x[R > 0 ? R : 1];
   if constexpr (R > 0) {
 #pragma unroll
@@ -216,32 +221,32 @@ __global__ __launch_bounds__(kBlock<W>, R <= 8 ? 8 : 4) void k_logp(LogpLaunch a
       for (int k = 0; k < E; ++k) mine = fmaxf(mine, v.get(k));
     });
     most = wave_max(mine);
-    p.m = reference(base2, most);
+    p.m = reference(most);
     each([&](const V& v, int) {
 #pragma unroll
-      for (int k = 0; k < E; ++k) add_value(v.get(k), base2, p);
+      for (int k = 0; k < E; ++k) add_value(v.get(k), t2, p);
     });
-    add_value(own_x, base2, p);
+    add_value(own_x, t2, p);
   } else {
     // one reading: the lane's sums follow its largest value
-    p.m = reference(base2, mine);
-    add_value(own_x, base2, p);
+    p.m = reference(mine);
+    add_value(own_x, t2, p);
     each([&](const V& v, int) {
       float top = mine;
 #pragma unroll
       for (int k = 0; k < E; ++k) top = fmaxf(top, v.get(k));
       if (top > mine) {
-        const float m = reference(base2, top);
+        const float m = reference(top);
         if (mine == -INFINITY) p.m = m;
-        else refer_to(m, p);
+        else refer_to(m, t2, p);
         mine = top;
       }
 #pragma unroll
-      for (int k = 0; k < E; ++k) add_value(v.get(k), base2, p);
+      for (int k = 0; k < E; ++k) add_value(v.get(k), t2, p);
     });
     most = wave_max(mine);
-    if (mine != -INFINITY) refer_to(reference(base2, most), p);
-    p.m = reference(base2, most);
+    if (mine != -INFINITY) refer_to(reference(most), t2, p);
+    p.m = reference(most);
   }
   p.s = wave_sum(p.s);
   p.a = wave_sum(p.a);
@@ -251,16 +256,16 @@ __global__ __launch_bounds__(kBlock<W>, R <= 8 ? 8 : 4) void k_logp(LogpLaunch a
     __syncthreads();
     // a lane takes a wavefront's sums (where no token can be they are zero, or NaN)
     const float part = lane < W ? s_part[0][lane] : -INFINITY;
-    Sums o{reference(base2, part), lane < W ? s_part[1][lane] : 0.f, lane < W ? s_part[2][lane] : 0.f};
+    Sums o{reference(part), lane < W ? s_part[1][lane] : 0.f, lane < W ? s_part[2][lane] : 0.f};
     top = wave_max(part);
-    p.m = reference(base2, top);
-    if (part != -INFINITY) refer_to(p.m, o);
+    p.m = reference(top);
+    if (part != -INFINITY) refer_to(p.m, t2, o);
     p.s = wave_sum(o.s);
     p.a = wave_sum(o.a);
   }
   const float log_sum = logf(p.s), entropy = p.s == 0.f ? 0.f : log_sum - kLn2 * (p.a / p.s);
   auto log_prob = [&](float v) {
-    return p.s == 0.f ? -INFINITY : __builtin_fmaf(v, base2, -p.m) * kLn2 - log_sum;
+    return p.s == 0.f ? -INFINITY : (v - p.m) * a.scale - log_sum;
   };
   if (t == 0) {
     const int64_t id = id_of(a, row);
@@ -275,7 +280,7 @@ __global__ __launch_bounds__(kBlock<W>, R <= 8 ? 8 : 4) void k_logp(LogpLaunch a
     } else {
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    const Slope d(a, row, base2, p.m, p.s, entropy);
+    const Slope d(a, row, t2, p.m, p.s, entropy);
     char* to = a.dlogits.p + row * a.dlogits.ld;
     each([&](const V& v, int at) { put_grad<false, STREAM, (R > 0)>(r, d, v, at, to); });
     put_edge<false>(r, d, own_x, own, to);
@@ -423,7 +428,7 @@ __global__ __launch_bounds__(256) void k_logp_bwd(LogpLaunch a, int per) {
   const int own = part == 0 ? r.edge(threadIdx.x) : -1;
   const float own_x = own >= 0 ? r.value(own) : 0.f;
   const float* st = a.stats + row * kStats;
-  const Slope d(a, row, a.scale * kLog2e, st[0], st[1], st[2]);
+  const Slope d(a, row, base2(a.scale), st[0], st[1], st[2]);
   char* to = a.dlogits.p + row * a.dlogits.ld;
 #pragma unroll
   for (int i = 0; i < kGradVecs; ++i) put_grad<ENTROPY, STREAM, SAME>(r, d, x[i], at + i * 256, to);
