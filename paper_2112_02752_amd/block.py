@@ -87,7 +87,7 @@ class Norm:
     so the backward is given the forward's (and a captured call keeps the one it
     was captured with).  ``max_rows`` sizes the weight
     gradient's workspace (0: no weight gradient).  Calls with a weight gradient
-    on one object must be ordered."""
+    on one object must be ordered; others need not be, nor come from one thread."""
 
     def __init__(self, weight, eps: float = 1e-6, drop: float = 0.0, max_rows: int = 0):
         import torch
@@ -100,9 +100,7 @@ class Norm:
         if not 0.0 <= eps < float("inf"):
             raise ValueError("eps is a number of at least 0")
         self._at = _floats(weight, (self.dim,), "weight")
-        self.max_rows = max_rows
-        self._c = CNorm(self._at, eps, drop, 0, 0)
-        self._ref = ctypes.byref(self._c)
+        self.eps, self.drop, self.max_rows = eps, drop, max_rows
         self.ws, self._ws, self._wsb = None, None, 0
         if max_rows > 0:
             self._wsb = int(lib().emb_norm_workspace_size(max_rows, self.dim))
@@ -111,12 +109,12 @@ class Norm:
             self.ws = torch.empty(self._wsb, dtype=torch.uint8, device=weight.device)
             self._ws = self.ws.data_ptr()
 
-    def _take(self, seed: int, first_row: int) -> None:
-        c = self._c
+    def _call(self, seed: int, first_row: int):
+        """A call's descriptor: its own, for another thread's call may come before this one has read it."""
         at = self.weight.data_ptr()
         if at != self._at:      # the tensor has got other memory
-            self._at = c.weight = _floats(self.weight, (self.dim,), "weight")
-        c.seed, c.first_row = seed & _SEED, first_row
+            at = self._at = _floats(self.weight, (self.dim,), "weight")
+        return ctypes.byref(CNorm(at, self.eps, self.drop, seed & _SEED, first_row))
 
     def forward(self, x, y=None, residual=None, total=None, saved: Optional[Checkpoint] = None, seed: int = 0,
                 first_row: int = 0, stream=None) -> None:
@@ -136,8 +134,7 @@ class Norm:
             _want(saved, n, D, "saved")
         refs.append(saved)
         _here((x, *refs), (self.weight,))
-        self._take(seed, first_row)
-        _check("emb_norm_fwd", lib().emb_norm_fwd(n, D, self._ref, x.ref,
+        _check("emb_norm_fwd", lib().emb_norm_fwd(n, D, self._call(seed, first_row), x.ref,
                                                   *(m.ref if m is not None else None for m in refs), _stream(stream)))
 
     def backward(self, total, dy, dtotal=None, branch=None, arriving=None, dweight=None, add: bool = False,
@@ -158,9 +155,8 @@ class Norm:
         _here((total, dy, *mats), (self.weight, dweight, self.ws))
         if dweight is not None and n > self.max_rows:
             raise ValueError("batch larger than the norm's workspace")
-        self._take(seed, first_row)
         _check("emb_norm_bwd", lib().emb_norm_bwd(
-            n, D, self._ref, total.ref, dy.ref, *(m.ref if m is not None else None for m in mats),
+            n, D, self._call(seed, first_row), total.ref, dy.ref, *(m.ref if m is not None else None for m in mats),
             _floats(dweight, (D,), "dweight"), int(add), self._ws, self._wsb, _stream(stream)))
 
 
