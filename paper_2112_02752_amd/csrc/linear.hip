@@ -31,13 +31,15 @@
 // the rows of a chunk in LDS, loaded a step (a head of a chunk) ahead.  Products
 // a . b go through LDS once, from the wavefronts that make them to all.
 //
-// Bound.  One prompt of 32768 tokens, 16 heads of 128 x 128: 220 us, of which sums 75 (293 MB,
-// 3.9 TB/s), boundaries 13 and the form 133 (571 MB, 4.3 TB/s).  A training batch of 48
-// sequences, 32768 x 16 heads (4 key heads) of 128: forward 164 (sums 29, boundaries 16, the form
-// 119), backward 385 (sums 71, boundaries 16, the three forms 299, 1.09 GB at 3.6 TB/s) where a
-// profiler separates them, 471 together among calls.  There LDS is busy a third of the time (its
-// reads: every wavefront takes all rows of a and b), the matrix units a fifth; the rest is the
+// Bound.  One prompt of 32768 tokens, 16 heads of 128 x 128: 221 us, of which sums 75 (293 MB,
+// 3.9 TB/s), boundaries 13 and the form 137 (571 MB, 4.2 TB/s).  A training batch of 48
+// sequences, 32768 x 16 heads (4 key heads) of 128: forward 182 (sums 29, boundaries 17, the form
+// 137), backward 406 (sums 70, boundaries 16, the three forms 320, 1.09 GB at 3.4 TB/s) where a
+// profiler separates them, 492 together among calls.  There LDS is busy a third of the time (its
+// reads: every wavefront takes all rows of a and b), the matrix units a quarter; the rest is the
 // latency of a step's phases at two blocks a compute unit, and the last round of blocks.
+// Rows or heads that do not begin at multiples of 16 bytes are loaded and stored value by value:
+// 16384 tokens in 24 sequences, 16 heads of 65 x 72, forward and backward 1047 us, of 64 x 72 274.
 #include "block_common.h"
 
 namespace emb {
@@ -465,7 +467,7 @@ __device__ __forceinline__ void sweep(const Args& args, const Form& f, int64_t n
           if constexpr (!rev) z.row_as_state(s_b + (16 * (wave % TC) + l) * LB + k * KB, q);
           // (of bf16 rows, the state has two parts, 16 bits: results that cancel in it, as queries across a component that
           // keys and values share have them, were off by up to a seventh of y with one; 32768 tokens, 16 heads of 128 x
-          // 128: 220 us, 216 with one part; their training with 4 key heads: 491, 466 with one)
+          // 128: 221 us, 216 with one part; their training with 4 key heads: 492, 466 with one)
 #pragma unroll
           for (int t = 0; t < TN; ++t) {
             f32x4 lo = st[k * KB / 16][t], hi = st[(k * KB / 16 + 1) % TD][t];
@@ -742,8 +744,8 @@ hipError_t go(const Args& a, int first, int forms, hipStream_t s) {
   int64_t blocks = (OUT ? a.bounds + a.M : a.bounds) * a.groups * a.slices[first] * forms;
   // In order the heads of a group may be shared by blocks, each of which makes the state: what that costs
   // (about half of a head's work, and as much again for a block's begin and end) against rounds of blocks on
-  // the device.  Four heads, 700 blocks of all: 115 us with one, 107 with two; three, 92 blocks (1501
-  // tokens): 23 us with all in a block, 18 with one.
+  // the device.  Four heads, 700 blocks of all: 137 us with one block a group, 130 with two, 148 with four;
+  // three, 92 blocks (1501 tokens): 23 us with all in a block, 18 with one.
   int parts = 1;
   if (OUT && forms == 1 && !f.rev) {
     auto cost = [&](int n) { return (float)((blocks * n + kResident - 1) / kResident) * ((float)(a.per / n) + 0.9f); };

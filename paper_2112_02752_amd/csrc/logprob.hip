@@ -12,9 +12,9 @@
 // (above 25600 vectors of 16 bytes), and gradients that lie otherwise than their
 // logits, are read twice.
 //
-// Bound.  8192 x 50000 bf16 with its gradient: 340 us, 1.64 GB at 4.8 TB/s.  301 x 100001
-// fp32: forward 30 us (4.0 TB/s), gradient from the statistics 37 (6.4 TB/s).  64 x 50000
-// with 8 alternatives, a row a compute unit: 10.3 us, of which the exponentials
+// Bound.  8192 x 50000 bf16 with its gradient: 348 us, 1.64 GB at 4.7 TB/s.  301 x 100001
+// fp32: forward 28 us (4.3 TB/s), gradient from the statistics 38 (6.5 TB/s).  64 x 50000
+// with 8 alternatives, a row a compute unit: 10.4 us, of which the exponentials
 // and sums of 50000 values by one compute unit take about 3, their loads as long.
 #include <float.h>
 
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(kBlock<W>, R <= 8 ? 8 : 4) void k_logp(LogpLaunch a
   if (a.top == 0) return;
   // The alternatives.  The row's lanes are 64 groups, each with its largest value; the `top`-th of those is a
   // bound that at least `top` logits reach (and few more do), so only those that reach it are looked at.  64
-  // x 50000 bf16: 7.2 us without alternatives, 10.3 with 8 and 11.5 with 20; when every wavefront found its
+  // x 50000 bf16: 7.6 us without alternatives, 10.4 with 8 and 11.4 with 20; when every wavefront found its
   // lanes' `top` largest one by one 13.4 and 20.9.
   static_assert(EMB_MAX_TOP <= 64, "a group for each");
   const int mate = wave / W;
@@ -456,6 +456,12 @@ hipError_t go(const LogpLaunch& p, hipStream_t s) {
   return hipGetLastError();
 }
 
+// The fewest wavefronts and registers that hold a row.  Forward / with gradient in us, bf16, the variant that is taken
+// and the next one on the same rows: 100 vectors (16384 rows) 10/17 and 21/28; 400 (16384) 32/46 and 77/89; 2040 (8224)
+// 64/96 and 98/122; 4000 (4194) 63/92 and 91/115; 8000 (2097) 62/90 and 117/153; 16000 (1048) 84/129 and 104/157;
+// 25500 (657) 77/131 and, without registers, 49/164.  (What reads a row once is faster without registers from 4000
+// vectors on: 16000, 50 us.  With the row in 20 or 24 vectors a lane instead of 25: 20000 (838) 84/129 and 90/141 for
+// 91/145.)
 template <typename T>
 hipError_t by_width(const LogpLaunch& p, hipStream_t s) {
   const int64_t n = p.D / Row<T>::kEach;  // whole vectors, at most
