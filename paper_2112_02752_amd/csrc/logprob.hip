@@ -97,8 +97,8 @@ __device__ __forceinline__ int64_t id_of(const LogpLaunch& a, int64_t row) {
 
 // Exponents are taken to the base of two: with t = scale log2(e) a value's power is (x - m) t, m being the largest value.
 // The difference is formed first: t x - t m by one operation has the rounding of t m as its error, which for masks of
-// large finite numbers is more than exponents are (some hundreds at 1e10), and a part of a row may hold nothing else.  Sums of a
-// part of a row, relative to its own m:
+// large finite numbers is more than exponents are (some hundreds at 1e10), and a part of a row may hold nothing else.
+// Sums of a part of a row, relative to its own m:
 struct Sums {
   float m, s, a;  // m, sum of 2^((x - m) t), sum of 2^((x - m) t) (x - m) t
 };
